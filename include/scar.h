@@ -47,8 +47,10 @@ typedef struct scar_ctx scar_ctx; /* opaque; created by scar_ckpt_init, freed by
 
 /* Element type.  SCAR_F32 scores blocks by the squared l2 distance (the norm of
  * the appendix proofs of Theorems 4.1/4.2); SCAR_I32 by the integer l1 distance
- * (twice the length-scaled total variation that Appendix C uses for LDA). */
-typedef enum { SCAR_F32 = 0, SCAR_I32 = 1 } scar_dtype;
+ * (twice the length-scaled total variation that Appendix C uses for LDA).  The
+ * 16-bit types are operand types of the training-step operators (scar_xent_*,
+ * scar_gnorm_*) only: checkpoint contexts refuse them. */
+typedef enum { SCAR_F32 = 0, SCAR_I32 = 1, SCAR_BF16 = 2, SCAR_F16 = 3 } scar_dtype;
 
 /* Which norm measures the distance of a block to its saved copy.  DEFAULT is the
  * one above for the element type.  L1 on SCAR_F32 data scores a block by
@@ -428,6 +430,124 @@ int scar_ckpt_debug_select_stamps(scar_ctx *ctx, int64_t stamps[32]);
 
 /* Waits for the stream, frees everything the context owns (never x). */
 int scar_ckpt_destroy(scar_ctx *ctx);
+
+/* ==== The training step the checkpoints are taken between ===========================
+ * The paper checkpoints iterative-convergent training (Eq. 1); its first workload is
+ * multinomial logistic regression.  The two operators below are the ends of such a
+ * step on the GPU: the loss of a linear map followed by a softmax cross entropy with
+ * its gradient, and the global norm of a gradient with clipping (which bounds one
+ * step, and with it the perturbation a recovery undoes).  Both follow the conventions
+ * at the top of this file: a handle owns the workspaces, all work runs on the stream
+ * given at init in call order, arguments are checked before anything is enqueued,
+ * nothing throws, calls only enqueue (so they can be captured in a CUDA graph) and a *_status call waits.  Operands may be
+ * float32, bfloat16 or float16; sums, softmax statistics and norms are float32 or
+ * wider whatever the operands are. */
+
+/* ---- Linear softmax cross entropy ------------------------------------------------------
+ * With h [T, D] (one row per token or sample), w [V, D] (one row per class) and labels
+ * [T]: z = h w^T, lse_t = log sum_v exp(z_tv),
+ *   row_loss_t = lse_t - z_{t, label_t}
+ *   loss       = sum_t row_loss_t / n     n = rows that count (MEAN; 1 if there are
+ *                                         none) or 1 (SUM)
+ *   dz_tv      = (grad_scale / n) (exp(z_tv - lse_t) - [v = label_t])
+ *   dh = dz w,  dw = dz^T h
+ * A row whose label is ignore_label does not count: its row_loss is 0, its row of dh
+ * is zero and whatever its row of h holds (NaN, infinities) reaches nothing.  A label
+ * outside [0, V) that is not ignore_label is treated the same and counted
+ * (scar_xent_status).  Without any row that counts the loss and both gradients are 0.
+ * The T x V matrix of logits is never stored: the loss alone keeps two numbers per row
+ * and group of classes, the gradients go through pieces of the rows in a block of
+ * workspace whose size `workspace_bytes` bounds. */
+typedef struct scar_xent scar_xent; /* opaque; created by scar_xent_init, freed by scar_xent_destroy */
+
+typedef enum { SCAR_MEAN = 0, SCAR_SUM = 1 } scar_reduction;
+
+typedef struct {
+    uint64_t max_tokens;  /* most rows of h a call may have, < 2^31 */
+    uint64_t n_classes;   /* V, 1 .. 2^31 - 1 */
+    uint64_t dim;         /* D, 1 .. 2^31 - 1 */
+    int64_t ignore_label;
+    uint64_t workspace_bytes; /* bound on the block of dz that is held at a time; 0 = 1 GiB.  At least the
+                                 256 rows of one piece are held, and all rows are when that needs less memory
+                                 than dw's float32 sums over several pieces would. */
+    scar_dtype dtype;         /* of h, w, dh, dw: SCAR_F32, SCAR_BF16 or SCAR_F16 */
+    scar_reduction reduction;
+    int loss_only;            /* non-zero: no workspace for gradients; scar_xent_loss_grad returns SCAR_ERR_STATE */
+} scar_xent_config;
+
+typedef struct {
+    float loss;
+    uint64_t rows;    /* rows that counted in the most recent call */
+    uint64_t ignored; /* rows whose label was ignore_label */
+    uint64_t bad;     /* rows whose label was outside [0, V) and not ignore_label */
+} scar_xent_info;
+
+/* Creates the operator with its workspaces on the current device.  cuda_stream is a cudaStream_t (NULL = default
+ * stream).  Waits for the stream.  On error *out is NULL. */
+int scar_xent_init(scar_xent **out, const scar_xent_config *cfg, void *cuda_stream);
+
+/* Loss of n_tokens rows.  d_h, d_w: DEVICE matrices, row-major, rows h_pitch / w_pitch elements apart (>= D), at
+ * any address their element type allows; rows that lie on 16-byte boundaries are read in place, others are
+ * copied first.  d_labels: DEVICE int64.  d_row_loss: DEVICE float[n_tokens] or NULL.  d_loss: DEVICE float or
+ * NULL. */
+int scar_xent_loss(scar_xent *op, const void *d_h, uint64_t h_pitch, const void *d_w, uint64_t w_pitch,
+                   const int64_t *d_labels, uint64_t n_tokens, float *d_row_loss, float *d_loss);
+
+/* The same with the gradients, in one call (a training step knows the scale of its loss beforehand).
+ * d_dh [T, D], d_dw [V, D]: DEVICE matrices of the operator's type, overwritten; neither may overlap an input. */
+int scar_xent_loss_grad(scar_xent *op, const void *d_h, uint64_t h_pitch, const void *d_w, uint64_t w_pitch,
+                        const int64_t *d_labels, uint64_t n_tokens, float grad_scale, float *d_row_loss,
+                        float *d_loss, void *d_dh, uint64_t dh_pitch, void *d_dw, uint64_t dw_pitch);
+
+/* Waits for the stream and returns the record of the most recent call.  SCAR_ERR_TIMEOUT if a wait inside one of
+ * its kernels gave up (its outputs are then invalid; the operator stays usable). */
+int scar_xent_status(scar_xent *op, scar_xent_info *out);
+uint64_t scar_xent_workspace_bytes(const scar_xent *op); /* device memory the operator holds */
+uint64_t scar_xent_launch_count(const scar_xent *op);    /* kernels launched so far */
+int scar_xent_destroy(scar_xent *op);
+
+/* ---- Global gradient norm and clipping ---------------------------------------------------
+ * Over a list of tensors g_1 .. g_k of any lengths (0 included), types and addresses:
+ *   norm = sqrt(sum g^2) | sum |g| | max |g|        (scar_gnorm_kind)
+ *   coef = min(1, max_norm / norm), 1 when norm is 0
+ *   out_i = coef * g_i, rounded once
+ * Sums run in float32 over short runs and in double across them, in an order that
+ * depends on the lengths alone: equal inputs give equal bits.  A NaN or an infinity in
+ * the tensors gives the IEEE result of these formulas (norm NaN: all outputs NaN; norm
+ * infinite: coef 0, NaN where g is infinite) and is reported (scar_gnorm_status), so
+ * that a caller can leave the step out. */
+typedef struct scar_gnorm scar_gnorm; /* opaque; created by scar_gnorm_init, freed by scar_gnorm_destroy */
+
+typedef enum { SCAR_GNORM_L2 = 0, SCAR_GNORM_L1 = 1, SCAR_GNORM_MAX = 2 } scar_gnorm_kind;
+
+typedef struct {
+    const void *d_data; /* DEVICE, n_elems elements of type dtype, aligned to one element */
+    void *d_out;        /* DEVICE, same type and length, or NULL: scar_gnorm_clip works in place */
+    uint64_t n_elems;
+    scar_dtype dtype; /* SCAR_F32, SCAR_BF16 or SCAR_F16 */
+} scar_tensor;
+
+typedef struct {
+    double norm;
+    double coef;        /* 1 after scar_gnorm_norm */
+    uint64_t nonfinite; /* 1 when the norm is NaN or infinite, else 0 */
+} scar_gnorm_info;
+
+/* Registers the caller's tensors (HOST array, read before the call returns); they must stay valid and in place
+ * until scar_gnorm_destroy or until scar_gnorm_bind gives their new addresses.  An output may be its own input
+ * (the same as NULL) but may not overlap another tensor.  Waits for the stream. */
+int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_tensors, scar_gnorm_kind kind,
+                    void *cuda_stream);
+/* New addresses for the same lengths and types (SCAR_ERR_LAYOUT otherwise).  Waits for the stream. */
+int scar_gnorm_bind(scar_gnorm *op, const scar_tensor *h_tensors, uint64_t n_tensors);
+/* The norm alone.  d_norm: DEVICE float or NULL.  Enqueue only. */
+int scar_gnorm_norm(scar_gnorm *op, float *d_norm);
+/* Norm and scaled outputs; max_norm >= 0 (infinity leaves the values as they are).  Enqueue only. */
+int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm);
+/* Waits for the stream and returns the record of the most recent call. */
+int scar_gnorm_status(scar_gnorm *op, scar_gnorm_info *out);
+uint64_t scar_gnorm_launch_count(const scar_gnorm *op);
+int scar_gnorm_destroy(scar_gnorm *op);
 
 /* Static description of an error code. */
 const char *scar_strerror(int code);

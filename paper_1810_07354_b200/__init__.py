@@ -9,6 +9,10 @@ or a CUDA device is missing.
 from .api import (  # noqa: F401
     SCAR_F32,
     SCAR_I32,
+    SCAR_BF16,
+    SCAR_F16,
+    GradientNorm,
+    LinearCrossEntropy,
     ScarError,
     ScarCheckpoint,
     lib_path,

@@ -16,8 +16,10 @@ from typing import Optional
 
 import numpy as np
 
-SCAR_F32, SCAR_I32 = 0, 1
+SCAR_F32, SCAR_I32, SCAR_BF16, SCAR_F16 = 0, 1, 2, 3
 SCAR_NORM_DEFAULT, SCAR_NORM_L1 = 0, 1
+SCAR_MEAN, SCAR_SUM = 0, 1
+SCAR_GNORM_L2, SCAR_GNORM_L1, SCAR_GNORM_MAX = 0, 1, 2
 SCAR_OK = 0
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -46,6 +48,24 @@ class scar_norm_info(C.Structure):
 
 class scar_drain_view(C.Structure):
     _fields_ = [("info", scar_save_info), ("h_sel", C.c_void_p), ("h_poff", C.c_void_p), ("h_payload", C.c_void_p)]
+
+
+class scar_xent_config(C.Structure):
+    _fields_ = [("max_tokens", C.c_uint64), ("n_classes", C.c_uint64), ("dim", C.c_uint64),
+                ("ignore_label", C.c_int64), ("workspace_bytes", C.c_uint64), ("dtype", C.c_int),
+                ("reduction", C.c_int), ("loss_only", C.c_int)]
+
+
+class scar_xent_info(C.Structure):
+    _fields_ = [("loss", C.c_float), ("rows", C.c_uint64), ("ignored", C.c_uint64), ("bad", C.c_uint64)]
+
+
+class scar_tensor(C.Structure):
+    _fields_ = [("d_data", C.c_void_p), ("d_out", C.c_void_p), ("n_elems", C.c_uint64), ("dtype", C.c_int)]
+
+
+class scar_gnorm_info(C.Structure):
+    _fields_ = [("norm", C.c_double), ("coef", C.c_double), ("nonfinite", C.c_uint64)]
 
 
 def lib_path() -> str:
@@ -102,6 +122,20 @@ _SIGS = {
     "scar_irreducible_error": (_dbl, [_dbl, _dbl]),
     "scar_ckpt_selftest_arm_timeout": (_int, [_vp]),
     "scar_ckpt_debug_select_stamps": (_int, [_vp, C.POINTER(C.c_int64)]),
+    "scar_xent_init": (_int, [C.POINTER(_vp), C.POINTER(scar_xent_config), _vp]),
+    "scar_xent_loss": (_int, [_vp, _vp, _u64, _vp, _u64, _vp, _u64, _vp, _vp]),
+    "scar_xent_loss_grad": (_int, [_vp, _vp, _u64, _vp, _u64, _vp, _u64, C.c_float, _vp, _vp, _vp, _u64, _vp, _u64]),
+    "scar_xent_status": (_int, [_vp, C.POINTER(scar_xent_info)]),
+    "scar_xent_workspace_bytes": (_u64, [_vp]),
+    "scar_xent_launch_count": (_u64, [_vp]),
+    "scar_xent_destroy": (_int, [_vp]),
+    "scar_gnorm_init": (_int, [C.POINTER(_vp), C.POINTER(scar_tensor), _u64, _int, _vp]),
+    "scar_gnorm_bind": (_int, [_vp, C.POINTER(scar_tensor), _u64]),
+    "scar_gnorm_norm": (_int, [_vp, _vp]),
+    "scar_gnorm_clip": (_int, [_vp, C.c_float, _vp]),
+    "scar_gnorm_status": (_int, [_vp, C.POINTER(scar_gnorm_info)]),
+    "scar_gnorm_launch_count": (_u64, [_vp]),
+    "scar_gnorm_destroy": (_int, [_vp]),
     "scar_ckpt_destroy": (_int, [_vp]),
     "scar_strerror": (C.c_char_p, [_int]),
 }
@@ -417,6 +451,79 @@ def scar_ckpt_destroy(ctx: int) -> None:
     _check(load_library().scar_ckpt_destroy(ctx), "scar_ckpt_destroy")
 
 
+# ---- the training step ----------------------------------------------------------------------
+
+
+def scar_xent_init(config: scar_xent_config, cuda_stream: int = 0) -> int:
+    op = _vp()
+    _check(load_library().scar_xent_init(C.byref(op), C.byref(config), cuda_stream or None), "scar_xent_init")
+    return op.value
+
+
+def scar_xent_loss(op: int, d_h, h_pitch: int, d_w, w_pitch: int, d_labels, n_tokens: int, d_row_loss, d_loss) -> None:
+    _check(load_library().scar_xent_loss(op, d_h, h_pitch, d_w, w_pitch, d_labels, n_tokens, d_row_loss, d_loss),
+           "scar_xent_loss")
+
+
+def scar_xent_loss_grad(op: int, d_h, h_pitch: int, d_w, w_pitch: int, d_labels, n_tokens: int, grad_scale: float,
+                        d_row_loss, d_loss, d_dh, dh_pitch: int, d_dw, dw_pitch: int) -> None:
+    """Raw device addresses throughout (rows may be further apart than ``dim``: a tensor's own strides decide)."""
+    _check(load_library().scar_xent_loss_grad(op, d_h, h_pitch, d_w, w_pitch, d_labels, n_tokens, grad_scale, d_row_loss,
+                                              d_loss, d_dh, dh_pitch, d_dw, dw_pitch), "scar_xent_loss_grad")
+
+
+def scar_xent_status(op: int) -> scar_xent_info:
+    out = scar_xent_info()
+    _check(load_library().scar_xent_status(op, C.byref(out)), "scar_xent_status")
+    return out
+
+
+def scar_xent_workspace_bytes(op: int) -> int:
+    return int(load_library().scar_xent_workspace_bytes(op))
+
+
+def scar_xent_launch_count(op: int) -> int:
+    return int(load_library().scar_xent_launch_count(op))
+
+
+def scar_xent_destroy(op: int) -> None:
+    _check(load_library().scar_xent_destroy(op), "scar_xent_destroy")
+
+
+def scar_gnorm_init(tensors, kind: int = SCAR_GNORM_L2, cuda_stream: int = 0) -> int:
+    """``tensors``: a ctypes array of :class:`scar_tensor`."""
+    op = _vp()
+    _check(load_library().scar_gnorm_init(C.byref(op), tensors, len(tensors), kind, cuda_stream or None),
+           "scar_gnorm_init")
+    return op.value
+
+
+def scar_gnorm_bind(op: int, tensors) -> None:
+    _check(load_library().scar_gnorm_bind(op, tensors, len(tensors)), "scar_gnorm_bind")
+
+
+def scar_gnorm_norm(op: int, d_norm) -> None:
+    _check(load_library().scar_gnorm_norm(op, d_norm), "scar_gnorm_norm")
+
+
+def scar_gnorm_clip(op: int, max_norm: float, d_norm) -> None:
+    _check(load_library().scar_gnorm_clip(op, max_norm, d_norm), "scar_gnorm_clip")
+
+
+def scar_gnorm_status(op: int) -> scar_gnorm_info:
+    out = scar_gnorm_info()
+    _check(load_library().scar_gnorm_status(op, C.byref(out)), "scar_gnorm_status")
+    return out
+
+
+def scar_gnorm_launch_count(op: int) -> int:
+    return int(load_library().scar_gnorm_launch_count(op))
+
+
+def scar_gnorm_destroy(op: int) -> None:
+    _check(load_library().scar_gnorm_destroy(op), "scar_gnorm_destroy")
+
+
 # ---------------------------------------------------------------------------------------------
 
 
@@ -542,6 +649,192 @@ class ScarCheckpoint:
         if getattr(self, "ctx", None):
             scar_ckpt_destroy(self.ctx)
             self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class _OnStream:
+    """Runs a handle's calls on its own stream and orders them with the stream the caller is working on: the handle's
+    stream first waits for the caller's, and the caller's for the handle's afterwards.  Nothing happens where the two
+    are the same."""
+
+    def _bind_stream(self, stream, device):
+        import torch
+
+        self._device = torch.device(device)
+        self._stream = stream if stream is not None else torch.cuda.current_stream(self._device)
+
+    def _enter(self, *tensors):
+        import torch
+
+        here = torch.cuda.current_stream(self._device)
+        if here == self._stream:
+            return None
+        self._stream.wait_stream(here)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self._stream)
+        return here
+
+    def _leave(self, here):
+        if here is not None:
+            here.wait_stream(self._stream)
+
+
+def _operand_type(dtype) -> int:
+    import torch
+
+    types = {torch.float32: SCAR_F32, torch.bfloat16: SCAR_BF16, torch.float16: SCAR_F16}
+    if dtype not in types:
+        raise TypeError(f"{dtype}: the training-step operators take float32, bfloat16 and float16")
+    return types[dtype]
+
+
+class LinearCrossEntropy(_OnStream):
+    """Softmax cross entropy of ``h @ w.T`` against integer labels, with its gradients, without the matrix of logits.
+
+    ``max_tokens`` rows at most per call, ``n_classes`` x ``dim`` weights, all operands of ``dtype`` (float32,
+    bfloat16 or float16).  Rows whose label is ``ignore_label`` do not count; ``reduction`` is ``"mean"`` (over the
+    rows that count) or ``"sum"``.  ``workspace_bytes`` bounds the block of logit gradients held at a time
+    (0: 1 GiB).  ``loss_only`` handles hold no workspace for gradients."""
+
+    def __init__(self, max_tokens: int, n_classes: int, dim: int, dtype, reduction: str = "mean",
+                 ignore_label: int = -100, workspace_bytes: int = 0, loss_only: bool = False, stream=None,
+                 device="cuda"):
+        import torch
+
+        cfg = scar_xent_config(max_tokens=max_tokens, n_classes=n_classes, dim=dim, ignore_label=ignore_label,
+                               workspace_bytes=workspace_bytes, dtype=_operand_type(dtype),
+                               reduction={"mean": SCAR_MEAN, "sum": SCAR_SUM}[reduction], loss_only=int(loss_only))
+        self.max_tokens, self.n_classes, self.dim, self.dtype = max_tokens, n_classes, dim, dtype
+        self._bind_stream(stream, device)
+        with torch.cuda.device(self._device):
+            self.op = scar_xent_init(cfg, self._stream.cuda_stream)
+
+    def _matrix(self, name: str, m, rows: int):
+        if m.dtype != self.dtype or not m.is_cuda:
+            raise TypeError(f"{name}: a CUDA tensor of {self.dtype} is wanted")
+        if m.dim() != 2 or tuple(m.shape) != (rows, self.dim) or (self.dim > 1 and m.stride(1) != 1):
+            raise ValueError(f"{name}: shape ({rows}, {self.dim}) with contiguous rows is wanted")
+        return m.data_ptr(), (m.stride(0) if rows > 1 else max(m.stride(0), self.dim))
+
+    def _call(self, grad: bool, h, w, labels, grad_scale, row_loss, dh, dw):
+        import torch
+
+        n = labels.numel()
+        if labels.dtype != torch.int64 or not labels.is_cuda or not labels.is_contiguous():
+            raise TypeError("labels: a contiguous CUDA tensor of int64 is wanted")
+        hp, wp = self._matrix("h", h, n), self._matrix("w", w, self.n_classes)
+        dev = h.device
+        if row_loss is None:
+            row_loss = torch.empty(n, dtype=torch.float32, device=dev)
+        elif row_loss.dtype != torch.float32 or row_loss.numel() != n or not row_loss.is_contiguous():
+            raise ValueError("row_loss: one contiguous float32 per row is wanted")
+        loss = torch.empty((), dtype=torch.float32, device=dev)
+        if grad:
+            dh = torch.empty((n, self.dim), dtype=self.dtype, device=dev) if dh is None else dh
+            dw = torch.empty((self.n_classes, self.dim), dtype=self.dtype, device=dev) if dw is None else dw
+            dhp, dwp = self._matrix("dh", dh, n), self._matrix("dw", dw, self.n_classes)
+        here = self._enter(h, w, labels, row_loss, loss, dh, dw)
+        if grad:
+            scar_xent_loss_grad(self.op, *hp, *wp, labels.data_ptr(), n, grad_scale, row_loss.data_ptr(), loss.data_ptr(),
+                                *dhp, *dwp)
+        else:
+            scar_xent_loss(self.op, *hp, *wp, labels.data_ptr(), n, row_loss.data_ptr(), loss.data_ptr())
+        self._leave(here)
+        return (loss, row_loss, dh, dw) if grad else (loss, row_loss)
+
+    def loss(self, h, w, labels, row_loss=None):
+        """``(loss, row_loss)``: a float32 scalar and one float32 per row, on the device."""
+        return self._call(False, h, w, labels, 0.0, row_loss, None, None)
+
+    def loss_and_grad(self, h, w, labels, grad_scale: float = 1.0, row_loss=None, dh=None, dw=None):
+        """``(loss, row_loss, dh, dw)``: the gradients are those of ``grad_scale * loss``, in the operands' type."""
+        return self._call(True, h, w, labels, grad_scale, row_loss, dh, dw)
+
+    def status(self) -> scar_xent_info:
+        """Waits; rows that counted, rows ignored, labels out of range in the most recent call."""
+        return scar_xent_status(self.op)
+
+    def workspace_bytes(self) -> int:
+        return scar_xent_workspace_bytes(self.op)
+
+    def close(self):
+        if getattr(self, "op", None):
+            scar_xent_destroy(self.op)
+            self.op = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class GradientNorm(_OnStream):
+    """Global norm over a list of CUDA tensors (contiguous; float32, bfloat16, float16, mixed) and clipping by it.
+
+    ``out``: tensors that receive the scaled values, or None to scale in place.  ``kind``: ``"l2"``, ``"l1"`` or
+    ``"max"``.  The tensors are registered once; :meth:`bind` gives new ones of the same lengths and types."""
+
+    def __init__(self, tensors, out=None, kind: str = "l2", stream=None):
+        import torch
+
+        tensors = list(tensors)
+        self._bind_stream(stream, tensors[0].device if tensors else "cuda")
+        table = self._table(tensors, out)
+        with torch.cuda.device(self._device):
+            self.op = scar_gnorm_init(table, {"l2": SCAR_GNORM_L2, "l1": SCAR_GNORM_L1, "max": SCAR_GNORM_MAX}[kind],
+                                      self._stream.cuda_stream)
+
+    def _table(self, tensors, out):
+        out = [None] * len(tensors) if out is None else list(out)
+        if len(out) != len(tensors):
+            raise ValueError("out: one tensor per input is wanted")
+        table = (scar_tensor * len(tensors))()
+        for e, t, o in zip(table, tensors, out):
+            for x in (t, o):
+                if x is not None and (not x.is_cuda or not x.is_contiguous() or x.device != tensors[0].device):
+                    raise ValueError("contiguous tensors on one CUDA device are wanted")
+            if o is not None and (o.dtype != t.dtype or o.numel() != t.numel()):
+                raise ValueError("an output has its input's type and length")
+            e.d_data, e.n_elems, e.dtype = t.data_ptr(), t.numel(), _operand_type(t.dtype)
+            e.d_out = None if o is None else o.data_ptr()
+        self._tensors, self._out = tensors, out  # kept alive as long as they are registered
+        return table
+
+    def bind(self, tensors, out=None):
+        scar_gnorm_bind(self.op, self._table(list(tensors), out))
+
+    def _run(self, call):
+        import torch
+
+        norm = torch.empty((), dtype=torch.float32, device=self._device)
+        here = self._enter(norm)
+        call(norm.data_ptr())
+        self._leave(here)
+        return norm
+
+    def norm(self):
+        """The norm, a float32 scalar on the device."""
+        return self._run(lambda d: scar_gnorm_norm(self.op, d))
+
+    def clip(self, max_norm: float):
+        """Scales every tensor by ``min(1, max_norm / norm)``; returns the norm before scaling."""
+        return self._run(lambda d: scar_gnorm_clip(self.op, max_norm, d))
+
+    def status(self) -> scar_gnorm_info:
+        """Waits; norm and factor of the most recent call in double, and whether the norm was finite."""
+        return scar_gnorm_status(self.op)
+
+    def close(self):
+        if getattr(self, "op", None):
+            scar_gnorm_destroy(self.op)
+            self.op = None
 
     def __del__(self):
         try:

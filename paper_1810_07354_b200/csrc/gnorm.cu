@@ -1,0 +1,294 @@
+// Global gradient norm over a list of tensors, and clipping (scar_gnorm_* of scar.h).
+//
+// The tensors are cut into pieces of at most kPieceBytes on the host, once; a CTA walks over pieces with a fixed
+// stride, so which CTA adds what depends on the lengths alone and the result is the same bits every time.
+#include <new>
+#include <vector>
+
+#include "train_common.cuh"
+
+using namespace scar;
+
+namespace {
+
+constexpr int kNormThreads = 512;
+constexpr unsigned kPieceBytes = 32768;
+
+struct Piece {
+    const void *src;
+    void *dst;
+    unsigned n;   // elements
+    int dtype;
+};
+
+struct NormRecord {
+    double norm;
+    double coef;
+    unsigned long long nonfinite;
+};
+
+// One term of the norm, and how two partial results join.
+template <int KIND> __device__ __forceinline__ void add_term(float &a, float v) {
+    if (KIND == SCAR_GNORM_L2) a = fmaf(v, v, a);
+    else if (KIND == SCAR_GNORM_L1) a += fabsf(v);
+    else a = (fabsf(v) > a || v != v) ? fabsf(v) : a;  // a NaN stays: nothing compares above it
+}
+template <int KIND, typename W> __device__ __forceinline__ W join(W a, W b) {
+    if (KIND != SCAR_GNORM_MAX) return a + b;
+    return (a != a) ? a : ((b > a || b != b) ? b : a);
+}
+
+template <int KIND> __device__ __forceinline__ double cta_join(double v, double *sh) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = join<KIND>(v, __shfl_xor_sync(0xffffffffu, v, o));
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = threadIdx.x < kNormThreads / 32 ? sh[threadIdx.x & 31] : 0.0;
+    if (threadIdx.x < 32) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) v = join<KIND>(v, __shfl_xor_sync(0xffffffffu, v, o));
+    }
+    return v;  // thread 0
+}
+
+template <int KIND, typename T> __device__ __forceinline__ double piece_norm(const Piece &p) {
+    const T *s = static_cast<const T *>(p.src);
+    float a = 0.f;
+    for (unsigned i = threadIdx.x; i < p.n; i += kNormThreads) add_term<KIND>(a, to_f32<T>(s[i]));
+    return (double)a;
+}
+
+template <int KIND>
+__global__ void __launch_bounds__(kNormThreads)
+k_gnorm_partials(const Piece *__restrict__ pieces, unsigned n_pieces, double *__restrict__ part) {
+    __shared__ double sh[32];
+    double v = 0.0;
+    for (unsigned i = blockIdx.x; i < n_pieces; i += gridDim.x) {
+        const Piece p = pieces[i];
+        const double w = p.dtype == SCAR_F32    ? piece_norm<KIND, float>(p)
+                         : p.dtype == SCAR_BF16 ? piece_norm<KIND, __nv_bfloat16>(p)
+                                                : piece_norm<KIND, __half>(p);
+        v = join<KIND>(v, w);
+    }
+    v = cta_join<KIND>(v, sh);
+    if (threadIdx.x == 0) part[blockIdx.x] = v;
+}
+
+template <int KIND>
+__global__ void __launch_bounds__(kNormThreads)
+k_gnorm_final(const double *__restrict__ part, unsigned n, float max_norm, bool clip, NormRecord *rec, float *d_norm) {
+    __shared__ double sh[32];
+    double v = 0.0;
+    for (unsigned i = threadIdx.x; i < n; i += kNormThreads) v = join<KIND>(v, part[i]);
+    v = cta_join<KIND>(v, sh);
+    if (threadIdx.x) return;
+    if (KIND == SCAR_GNORM_L2) v = sqrt(v);
+    double coef = 1.0;
+    if (clip && !(v <= (double)max_norm)) coef = (double)max_norm / v;
+    rec->norm = v;
+    rec->coef = coef;
+    rec->nonfinite = !isfinite(v);
+    if (d_norm) *d_norm = (float)v;
+}
+
+template <typename T> __device__ __forceinline__ void scale_piece(const Piece &p, float coef) {
+    const T *s = static_cast<const T *>(p.src);
+    T *d = static_cast<T *>(p.dst);
+    for (unsigned i = threadIdx.x; i < p.n; i += kNormThreads) d[i] = from_f32<T>(to_f32<T>(s[i]) * coef);
+}
+
+__global__ void __launch_bounds__(kNormThreads)
+k_gnorm_scale(const Piece *__restrict__ pieces, unsigned n_pieces, const NormRecord *__restrict__ rec) {
+    const float coef = (float)rec->coef;
+    for (unsigned i = blockIdx.x; i < n_pieces; i += gridDim.x) {
+        const Piece p = pieces[i];
+        if (p.dtype == SCAR_F32) scale_piece<float>(p, coef);
+        else if (p.dtype == SCAR_BF16) scale_piece<__nv_bfloat16>(p, coef);
+        else scale_piece<__half>(p, coef);
+    }
+}
+
+}  // namespace
+
+struct scar_gnorm {
+    int device = 0;
+    cudaStream_t stream = nullptr;
+    scar_gnorm_kind kind = SCAR_GNORM_L2;
+    std::vector<uint64_t> lengths;
+    std::vector<int> types;
+    std::vector<Piece> h_pieces;
+    Piece *pieces = nullptr;
+    double *part = nullptr;
+    NormRecord *rec = nullptr;
+    NormRecord *h_rec = nullptr;  // pinned
+    unsigned grid = 1;
+    bool ran = false;
+    uint64_t launches = 0;
+};
+
+namespace {
+
+int check_tensors(const scar_tensor *t, uint64_t n) {
+    if (n && !t) return SCAR_ERR_INVALID_ARG;
+    uint64_t pieces = 0;
+    for (uint64_t i = 0; i < n; ++i) {
+        if (!is_operand_type(t[i].dtype)) return SCAR_ERR_INVALID_ARG;
+        const unsigned b = elem_size(t[i].dtype);
+        if (t[i].n_elems >= (1ull << 48)) return SCAR_ERR_LAYOUT;
+        if (t[i].n_elems && !t[i].d_data) return SCAR_ERR_INVALID_ARG;
+        if ((uintptr_t)t[i].d_data % b || (uintptr_t)t[i].d_out % b) return SCAR_ERR_INVALID_ARG;
+        pieces += (t[i].n_elems * b + kPieceBytes - 1) / kPieceBytes;
+    }
+    return pieces < (1ull << 31) ? SCAR_OK : SCAR_ERR_CAPACITY;
+}
+
+void cut(scar_gnorm *op, const scar_tensor *t, uint64_t n) {
+    op->h_pieces.clear();
+    for (uint64_t i = 0; i < n; ++i) {
+        const unsigned b = elem_size(t[i].dtype), most = kPieceBytes / b;
+        const char *src = static_cast<const char *>(t[i].d_data);
+        char *dst = t[i].d_out ? static_cast<char *>(t[i].d_out) : const_cast<char *>(src);
+        for (uint64_t at = 0; at < t[i].n_elems; at += most) {
+            const uint64_t left = t[i].n_elems - at;
+            op->h_pieces.push_back({src + at * b, dst + at * b, (unsigned)(left < most ? left : most), t[i].dtype});
+        }
+    }
+}
+
+int upload(scar_gnorm *op) {
+    if (!op->h_pieces.empty())
+        TRAIN_TRY(cudaMemcpyAsync(op->pieces, op->h_pieces.data(), op->h_pieces.size() * sizeof(Piece),
+                                  cudaMemcpyHostToDevice, op->stream));
+    TRAIN_TRY(cudaStreamSynchronize(op->stream));
+    return SCAR_OK;
+}
+
+template <int KIND> void launch_norm(scar_gnorm *op, float max_norm, bool clip, float *d_norm) {
+    const unsigned n = (unsigned)op->h_pieces.size();
+    k_gnorm_partials<KIND><<<op->grid, kNormThreads, 0, op->stream>>>(op->pieces, n, op->part);
+    k_gnorm_final<KIND><<<1, kNormThreads, 0, op->stream>>>(op->part, op->grid, max_norm, clip, op->rec, d_norm);
+    op->launches += 2;
+}
+
+int run_norm(scar_gnorm *op, float max_norm, bool clip, float *d_norm) {
+    if (op->kind == SCAR_GNORM_L2) launch_norm<SCAR_GNORM_L2>(op, max_norm, clip, d_norm);
+    else if (op->kind == SCAR_GNORM_L1) launch_norm<SCAR_GNORM_L1>(op, max_norm, clip, d_norm);
+    else launch_norm<SCAR_GNORM_MAX>(op, max_norm, clip, d_norm);
+    TRAIN_TRY(cudaGetLastError());
+    op->ran = true;
+    return SCAR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_tensors, scar_gnorm_kind kind,
+                    void *cuda_stream) {
+    if (!out) return SCAR_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (kind != SCAR_GNORM_L2 && kind != SCAR_GNORM_L1 && kind != SCAR_GNORM_MAX) return SCAR_ERR_INVALID_ARG;
+    int rc = check_tensors(h_tensors, n_tensors);
+    if (rc != SCAR_OK) return rc;
+    scar_gnorm *op = nullptr;
+    try {
+        op = new scar_gnorm();
+        for (uint64_t i = 0; i < n_tensors; ++i) {
+            op->lengths.push_back(h_tensors[i].n_elems);
+            op->types.push_back(h_tensors[i].dtype);
+        }
+        cut(op, h_tensors, n_tensors);
+    } catch (...) {
+        delete op;
+        return SCAR_ERR_ALLOC;
+    }
+    op->stream = static_cast<cudaStream_t>(cuda_stream);
+    op->kind = kind;
+    auto setup = [&]() -> int {
+        int sms = 0;
+        TRAIN_TRY(cudaGetDevice(&op->device));
+        TRAIN_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, op->device));
+        const unsigned most = 4u * (unsigned)sms, n = (unsigned)op->h_pieces.size();
+        op->grid = n < 1 ? 1 : (n < most ? n : most);
+        if (cudaMalloc(&op->pieces, (n ? n : 1) * sizeof(Piece)) != cudaSuccess ||
+            cudaMalloc(&op->part, op->grid * sizeof(double)) != cudaSuccess ||
+            cudaMalloc(&op->rec, sizeof(NormRecord)) != cudaSuccess ||
+            cudaMallocHost(&op->h_rec, sizeof(NormRecord)) != cudaSuccess) {
+            cudaGetLastError();
+            return SCAR_ERR_ALLOC;
+        }
+        return upload(op);
+    };
+    rc = setup();
+    if (rc != SCAR_OK) {
+        scar_gnorm_destroy(op);
+        return rc;
+    }
+    *out = op;
+    return SCAR_OK;
+}
+
+int scar_gnorm_bind(scar_gnorm *op, const scar_tensor *h_tensors, uint64_t n_tensors) {
+    if (!op) return SCAR_ERR_INVALID_ARG;
+    int rc = check_tensors(h_tensors, n_tensors);
+    if (rc != SCAR_OK) return rc;
+    if (n_tensors != op->lengths.size()) return SCAR_ERR_LAYOUT;
+    for (uint64_t i = 0; i < n_tensors; ++i)
+        if (h_tensors[i].n_elems != op->lengths[i] || h_tensors[i].dtype != op->types[i]) return SCAR_ERR_LAYOUT;
+    if ((rc = check_current_device(op->device)) != SCAR_OK) return rc;
+    TRAIN_TRY(cudaStreamSynchronize(op->stream));
+    try {
+        cut(op, h_tensors, n_tensors);
+    } catch (...) {
+        return SCAR_ERR_ALLOC;
+    }
+    return upload(op);
+}
+
+int scar_gnorm_norm(scar_gnorm *op, float *d_norm) {
+    if (!op) return SCAR_ERR_INVALID_ARG;
+    const int rc = check_current_device(op->device);
+    if (rc != SCAR_OK) return rc;
+    return run_norm(op, 0.f, false, d_norm);
+}
+
+int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm) {
+    if (!op || !(max_norm >= 0.f)) return SCAR_ERR_INVALID_ARG;
+    int rc = check_current_device(op->device);
+    if (rc != SCAR_OK) return rc;
+    if ((rc = run_norm(op, max_norm, true, d_norm)) != SCAR_OK) return rc;
+    if (op->h_pieces.empty()) return SCAR_OK;
+    k_gnorm_scale<<<op->grid, kNormThreads, 0, op->stream>>>(op->pieces, (unsigned)op->h_pieces.size(), op->rec);
+    op->launches += 1;
+    TRAIN_TRY(cudaGetLastError());
+    return SCAR_OK;
+}
+
+int scar_gnorm_status(scar_gnorm *op, scar_gnorm_info *out) {
+    if (!op || !out) return SCAR_ERR_INVALID_ARG;
+    const int rc = check_current_device(op->device);
+    if (rc != SCAR_OK) return rc;
+    if (!op->ran) return SCAR_ERR_STATE;
+    TRAIN_TRY(cudaMemcpyAsync(op->h_rec, op->rec, sizeof(NormRecord), cudaMemcpyDeviceToHost, op->stream));
+    TRAIN_TRY(cudaStreamSynchronize(op->stream));
+    out->norm = op->h_rec->norm;
+    out->coef = op->h_rec->coef;
+    out->nonfinite = op->h_rec->nonfinite;
+    return SCAR_OK;
+}
+
+uint64_t scar_gnorm_launch_count(const scar_gnorm *op) { return op ? op->launches : 0; }
+
+int scar_gnorm_destroy(scar_gnorm *op) {
+    if (!op) return SCAR_ERR_INVALID_ARG;
+    const bool ok = cudaStreamSynchronize(op->stream) == cudaSuccess;
+    cudaFree(op->pieces);
+    cudaFree(op->part);
+    cudaFree(op->rec);
+    if (op->h_rec) cudaFreeHost(op->h_rec);
+    delete op;
+    if (!ok) cudaGetLastError();
+    return ok ? SCAR_OK : SCAR_ERR_CUDA;
+}
+
+}  // extern "C"
