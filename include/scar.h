@@ -487,8 +487,9 @@ typedef struct {
 int scar_xent_init(scar_xent **out, const scar_xent_config *cfg, void *cuda_stream);
 
 /* Loss of n_tokens rows.  d_h, d_w: DEVICE matrices, row-major, rows h_pitch / w_pitch elements apart (>= D), at
- * any address their element type allows; rows that lie on 16-byte boundaries are read in place, others are
- * copied first.  d_labels: DEVICE int64.  d_row_loss: DEVICE float[n_tokens] or NULL.  d_loss: DEVICE float or
+ * any address their element type allows.  16-bit rows of w that lie on 16-byte boundaries are read in place, others
+ * are copied first (with a dim that is a multiple of 8, the first such call allocates that copy: make it before a
+ * stream capture).  d_labels: DEVICE int64.  d_row_loss: DEVICE float[n_tokens] or NULL.  d_loss: DEVICE float or
  * NULL. */
 int scar_xent_loss(scar_xent *op, const void *d_h, uint64_t h_pitch, const void *d_w, uint64_t w_pitch,
                    const int64_t *d_labels, uint64_t n_tokens, float *d_row_loss, float *d_loss);

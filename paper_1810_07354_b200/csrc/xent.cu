@@ -1,32 +1,39 @@
 // Linear softmax cross entropy with its gradient (scar_xent_* of scar.h).
 //
-// Rows that do not count are dropped first; the others go through the products in pieces, each of which holds the
-// logits of its rows until their gradient has taken their place.
+// A call:  rows that count are listed (k_xent_rows) and copied together (k_xent_place; float32 is split into three
+// bfloat16 planes on the way, w too).  The rows then go through the products in pieces:
+//   z = h w^T        the product's epilogue keeps, per row and 128 classes, the maximum and the sum of exponentials, and
+//                    for gradients the exponentials relative to that maximum, in float16 (k_tc_gemm, kProb / kStat)
+//   dz               k_xent_dz joins a row's groups to lse and turns the exponentials into dz, in place
+//   dh = dz w, dw = dz^T h
+// so the logits are computed once (6 n V D operations, not 8) and exist only in tensor memory.  float32 operators, and
+// products with too few tiles to fill the GPU (their sum over D is split over CTAs), pass through float32 logits of the
+// piece instead (kPart and k_xent_softmax).  k_xent_loss adds the row losses.
 #include <algorithm>
 #include <new>
 #include <vector>
 
-#include "train_common.cuh"
+#include "tc_gemm.cuh"
 
 using namespace scar;
 
 namespace {
 
 constexpr int kRowThreads = 1024;
-constexpr int kTile = 64;   // edge of a CTA's output tile
-constexpr int kTileK = 16;
+constexpr unsigned kNone = 0xffffffffu;
 
 struct XentRecord {
-    double sum;  // of the row losses
     float loss;
     unsigned rows, ignored, bad;
     unsigned error;
 };
 
-// Compacts the rows that count: idx[0 .. rows) are their numbers, ascending.  One CTA: the labels of a step are few.
+// Compacts the rows that count, in order: row_of[0 .. rows) are their numbers, pos is the inverse (kNone for the rest).
+// One CTA: the labels of a step are few.
 __global__ void __launch_bounds__(kRowThreads)
 k_xent_rows(const long long *__restrict__ labels, unsigned n, long long ignore, unsigned n_classes,
-            unsigned *__restrict__ idx, float *__restrict__ row_loss, XentRecord *rec) {
+            unsigned *__restrict__ row_of, unsigned *__restrict__ pos, int *__restrict__ label, float *__restrict__ row_loss,
+            XentRecord *rec) {
     __shared__ unsigned sh[kRowThreads / 32], base, n_ign, n_bad;
     if (threadIdx.x == 0) base = n_ign = n_bad = 0;
     __syncthreads();
@@ -34,8 +41,9 @@ k_xent_rows(const long long *__restrict__ labels, unsigned n, long long ignore, 
     for (unsigned at = 0; at < n; at += kRowThreads) {
         const unsigned t = at + threadIdx.x;
         bool keep = false, bad = false, ign = false;
+        long long y = 0;
         if (t < n) {
-            const long long y = labels[t];
+            y = labels[t];
             ign = y == ignore;
             keep = !ign && y >= 0 && y < (long long)n_classes;
             bad = !ign && !keep;
@@ -49,18 +57,20 @@ k_xent_rows(const long long *__restrict__ labels, unsigned n, long long ignore, 
             if (mb) atomicAdd(&n_bad, __popc(mb));
         }
         __syncthreads();
-        unsigned before = base, all = 0;
-        for (unsigned w = 0; w < kRowThreads / 32; ++w) {
-            if (w < warp) before += sh[w];
-            all += sh[w];
+        const unsigned mine = sh[lane];
+        const unsigned before = base + __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0u);
+        const unsigned all = __reduce_add_sync(0xffffffffu, mine);
+        const unsigned r = before + __popc(m & ((1u << lane) - 1u));
+        if (keep) {
+            row_of[r] = t;
+            label[r] = (int)y;
         }
-        if (keep) idx[before + __popc(m & ((1u << lane) - 1u))] = t;
+        if (t < n) pos[t] = keep ? r : kNone;
         __syncthreads();
         if (threadIdx.x == 0) base += all;
         __syncthreads();
     }
     if (threadIdx.x == 0) {
-        rec->sum = 0.0;
         rec->rows = base;
         rec->ignored = n_ign;
         rec->bad = n_bad;
@@ -69,30 +79,83 @@ k_xent_rows(const long long *__restrict__ labels, unsigned n, long long ignore, 
     }
 }
 
-// out(m, n) = sum_k A(m, k) B(n, k), 64 x 64 outputs per CTA, float32 throughout.  A, B: load(row, k) or 0 outside.
-template <typename FA, typename FB, typename FO>
-__device__ __forceinline__ void gemm_tile(unsigned m0, unsigned n0, unsigned K, FA a, FB b, FO out) {
-    __shared__ float sa[kTileK][kTile + 4], sb[kTileK][kTile + 4];
-    const unsigned tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (unsigned k0 = 0; k0 < K; k0 += kTileK) {
-        for (unsigned i = threadIdx.x; i < kTile * kTileK; i += 256) {
-            const unsigned r = i / kTileK, k = i % kTileK;
-            sa[k][r] = k0 + k < K ? a(m0 + r, k0 + k) : 0.f;
-            sb[k][r] = k0 + k < K ? b(n0 + r, k0 + k) : 0.f;
+union Eight {
+    uint4 u;
+    __nv_bfloat16 b[8];
+    __half h[8];
+    unsigned short s[8];
+};
+
+// x = p0 + p1 + p2, each the bfloat16 next to what is left.  A finite value above the largest bfloat16 is cut, not
+// rounded to infinity; an infinity or a NaN stays in p0.
+__device__ __forceinline__ void split3(float x, __nv_bfloat16 &p0, __nv_bfloat16 &p1, __nv_bfloat16 &p2) {
+    p0 = __float2bfloat16_rn(x);
+    if (!isfinite(__bfloat162float(p0))) {
+        p0 = __float2bfloat16_rz(x);
+        if (!isfinite(x)) {
+            p0 = __float2bfloat16_rn(x);
+            p1 = p2 = __float2bfloat16_rn(0.f);
+            return;
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kTileK; ++k) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ty * 4 + i], sb[k][tx * 4 + j], acc[i][j]);
-        }
-        __syncthreads();
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) out(m0 + ty * 4 + i, n0 + tx * 4 + j, acc[i][j]);
+    const float r1 = x - __bfloat162float(p0);
+    p1 = __float2bfloat16_rn(r1);
+    p2 = __float2bfloat16_rn(r1 - __bfloat162float(p1));
+}
+
+// Copies rows into the layout the products read: rows of dp elements (zeros behind the last), 16-byte aligned, one plane
+// for the 16-bit types and three for float32.  With `pos`, row t goes to pos[t]; rows that do not count are left out and
+// their row of `zero` (dh) is cleared, and the rows behind the last one are zero up to a multiple of 64.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_xent_place(const T *__restrict__ src, unsigned long long pitch, unsigned n, unsigned d, unsigned dp, bool vec,
+             unsigned short *__restrict__ dst, unsigned long long plane, const unsigned *__restrict__ pos,
+             const unsigned *__restrict__ rows, T *__restrict__ zero, unsigned long long zero_pitch) {
+    const unsigned groups = dp / 8;
+    const unsigned long long total = (unsigned long long)(n + (pos ? 64u : 0u)) * groups;
+    for (unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 256) {
+        const unsigned r = total >> 32 ? (unsigned)(i / groups) : (unsigned)i / groups;
+        const unsigned c = (unsigned)(i - (unsigned long long)r * groups) * 8;
+        unsigned to = r;
+        if (pos) {
+            if (r >= n) {
+                to = *rows + (r - n);
+                if (to >= (*rows + 63) / 64 * 64) continue;
+                for (int p = 0; p < (sizeof(T) == 4 ? 3 : 1); ++p)
+                    *reinterpret_cast<uint4 *>(dst + p * plane + (unsigned long long)to * dp + c) = make_uint4(0, 0, 0, 0);
+                continue;
+            }
+            to = pos[r];
+            if (to == kNone) {
+                if (zero)
+                    for (unsigned j = 0; j < 8 && c + j < d; ++j) zero[r * zero_pitch + c + j] = from_f32<T>(0.f);
+                continue;
+            }
+        }
+        const T *s = src + r * pitch + c;
+        unsigned short *o = dst + (unsigned long long)to * dp + c;
+        if constexpr (sizeof(T) == 2) {
+            Eight x;
+            if (vec && c + 8 <= d) x.u = *reinterpret_cast<const uint4 *>(s);
+            else
+                for (int j = 0; j < 8; ++j) x.s[j] = c + j < d ? reinterpret_cast<const unsigned short *>(s)[j] : (unsigned short)0;
+            *reinterpret_cast<uint4 *>(o) = x.u;
+        } else {
+            float x[8];
+            if (vec && c + 8 <= d) {
+                const float4 a = *reinterpret_cast<const float4 *>(s), b = *reinterpret_cast<const float4 *>(s + 4);
+                x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+                x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+            } else {
+                for (int j = 0; j < 8; ++j) x[j] = c + j < d ? s[j] : 0.f;
+            }
+            Eight p[3];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) split3(x[j], p[0].b[j], p[1].b[j], p[2].b[j]);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(o + q * plane) = p[q].u;
+        }
+    }
 }
 
 struct Piece {
@@ -101,18 +164,6 @@ struct Piece {
         return rec->rows > first ? min(most, rec->rows - first) : 0u;
     }
 };
-
-template <typename T>
-__global__ void __launch_bounds__(256)
-k_xent_logits(const T *h, uint64_t hp, const T *w, uint64_t wp, unsigned V, unsigned D, const unsigned *idx,
-              const XentRecord *rec, Piece p, float *z) {
-    const unsigned R = p.rows(rec), m0 = blockIdx.y * kTile;
-    if (m0 >= R) return;
-    gemm_tile(m0, blockIdx.x * kTile, D,
-              [&](unsigned r, unsigned k) { return r < R ? to_f32<T>(h[idx[p.first + r] * hp + k]) : 0.f; },
-              [&](unsigned v, unsigned k) { return v < V ? to_f32<T>(w[v * wp + k]) : 0.f; },
-              [&](unsigned r, unsigned v, float x) { if (r < R && v < V) z[(uint64_t)r * V + v] = x; });
-}
 
 __device__ __forceinline__ float cta_max(float v, float *sh) {
     for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -133,76 +184,151 @@ __device__ __forceinline__ float cta_add(float v, float *sh) {
     return v;
 }
 
-// One CTA per row: loss, and with GRAD the row's logits become exp(z - lse) - [v = label].
+// What the products read as dz: bfloat16 as it is; float16 times 2^15 (|dz| <= 1, and a probability of 1e-6 would be
+// next to float16's smallest step), taken out again by the products' scale.
+constexpr float kDzF16 = 32768.f;
+
+struct DzOut {
+    unsigned short *dz;        // [planes][rows][pitch]
+    unsigned long long pitch;  // classes rounded up to a multiple of 8
+    unsigned long long plane;
+    int dt;
+};
+
+// One CTA per row of the piece: joins the row's groups of 128 classes to lse and the loss; with GRAD turns the row's
+// scaled exponentials into dz in place.  Rows behind the last one up to a multiple of 64 become zero (the dw product
+// runs over whole groups of 64 rows).
 template <bool GRAD>
 __global__ void __launch_bounds__(256)
-k_xent_softmax(float *z, unsigned V, const long long *labels, const unsigned *idx, const XentRecord *rec, Piece p,
-               float *row_loss) {
+k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups, const int *__restrict__ label,
+          const float *__restrict__ label_z, const unsigned *__restrict__ row_of, const XentRecord *__restrict__ rec, Piece p,
+          float *__restrict__ row_loss) {
     __shared__ float sh[8];
-    const unsigned r = blockIdx.x;
-    if (r >= p.rows(rec)) return;
-    const unsigned t = idx[p.first + r];
-    const unsigned y = (unsigned)labels[t];
-    float *row = z + (uint64_t)r * V;
-    float top = -INFINITY;
-    for (unsigned v = threadIdx.x; v < V; v += 256) top = fmaxf(top, row[v]);
+    const unsigned r = blockIdx.x, R = p.rows(rec);
+    unsigned short *row = GRAD ? o.dz + (unsigned long long)r * o.pitch : nullptr;
+    if (r >= R) {
+        if (GRAD && r < (R + 63) / 64 * 64)
+            for (unsigned v = threadIdx.x * 8; v < o.pitch; v += 256 * 8) *reinterpret_cast<uint4 *>(row + v) = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const float2 *st = stat + (unsigned long long)r * groups;
+    float top = -INFINITY, s = 0.f;
+    for (unsigned i = threadIdx.x; i < groups; i += 256) top = fmaxf(top, st[i].y > 0.f ? st[i].x : -INFINITY);
     top = cta_max(top, sh);
-    float s = 0.f;
-    for (unsigned v = threadIdx.x; v < V; v += 256) s += expf(row[v] - top);
+    for (unsigned i = threadIdx.x; i < groups; i += 256) {
+        const float2 e = st[i];
+        if (e.y != 0.f) s = fmaf(e.y, expf(e.x - top), s);  // a NaN sum goes through
+    }
     s = cta_add(s, sh);
-    const float lse = top + logf(s);
-    const float zl = row[y];
-    __syncthreads();
-    if (threadIdx.x == 0) row_loss[t] = lse - zl;
+    const float lse = top + logf(s * (1.f / kProbScale));
+    const float zl = label_z[p.first + r];
+    if (threadIdx.x == 0) row_loss[row_of[p.first + r]] = lse - zl;
     if (!GRAD) return;
-    for (unsigned v = threadIdx.x; v < V; v += 256) row[v] = v == y ? expm1f(row[v] - lse) : expf(row[v] - lse);
+    const unsigned y = (unsigned)label[p.first + r];
+    const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
+    for (unsigned v = threadIdx.x * 8; v < V; v += 256 * 8) {
+        const float2 e = st[v >> 7];
+        const float f = e.y != 0.f ? expf(e.x - lse) * (held / kProbScale) : 0.f;
+        Eight x;
+        x.u = *reinterpret_cast<const uint4 *>(row + v);
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            w[j] = __half2float(x.h[j]) * f;
+            if (v + j == y) w[j] = expm1f(zl - lse) * held;
+        }
+        if (o.dt == SCAR_F16) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x.h[j] = __float2half_rn(w[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x.b[j] = __float2bfloat16_rn(w[j]);
+        }
+        *reinterpret_cast<uint4 *>(row + v) = x.u;
+    }
 }
 
-__device__ __forceinline__ float grad_factor(const XentRecord *rec, float scale, bool mean) {
-    return mean ? scale / (float)max(rec->rows, 1u) : scale;
-}
-
-template <typename T>
+// The same from float32 logits of the piece in `splits` parts (their sum replaces the first part).
+template <bool GRAD>
 __global__ void __launch_bounds__(256)
-k_xent_dh(const float *dz, const T *w, uint64_t wp, unsigned V, unsigned D, const unsigned *idx, const XentRecord *rec,
-          Piece p, float scale, bool mean, T *dh, uint64_t dhp) {
-    const unsigned R = p.rows(rec), m0 = blockIdx.y * kTile;
-    if (m0 >= R) return;
-    const float g = grad_factor(rec, scale, mean);
-    gemm_tile(m0, blockIdx.x * kTile, V,
-              [&](unsigned r, unsigned v) { return r < R ? dz[(uint64_t)r * V + v] : 0.f; },
-              [&](unsigned d, unsigned v) { return d < D ? to_f32<T>(w[v * wp + d]) : 0.f; },
-              [&](unsigned r, unsigned d, float x) { if (r < R && d < D) dh[idx[p.first + r] * dhp + d] = from_f32<T>(x * g); });
+k_xent_softmax(float *__restrict__ part, unsigned splits, unsigned long long part_stride, DzOut o, unsigned V,
+               const int *__restrict__ label, const unsigned *__restrict__ row_of, const XentRecord *__restrict__ rec, Piece p,
+               float *__restrict__ row_loss) {
+    __shared__ float sh[8];
+    const unsigned r = blockIdx.x, R = p.rows(rec);
+    unsigned short *row = GRAD ? o.dz + (unsigned long long)r * o.pitch : nullptr;
+    const int planes = o.dt == SCAR_F32 ? 3 : 1;
+    if (r >= R) {
+        if (GRAD && r < (R + 63) / 64 * 64)
+            for (int q = 0; q < planes; ++q)
+                for (unsigned v = threadIdx.x * 8; v < o.pitch; v += 256 * 8)
+                    *reinterpret_cast<uint4 *>(row + q * o.plane + v) = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    float *z = part + (unsigned long long)r * V;
+    float top = -INFINITY;
+    for (unsigned v = threadIdx.x; v < V; v += 256) {
+        float x = z[v];
+        for (unsigned q = 1; q < splits; ++q) x += z[q * part_stride + v];
+        if (splits > 1) z[v] = x;
+        top = fmaxf(top, x);
+    }
+    top = cta_max(top, sh);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float s = 0.f;
+    for (unsigned v = threadIdx.x; v < V; v += 256) s += expf(z[v] - ref);
+    s = cta_add(s, sh);
+    const float lse = ref + logf(s);
+    const unsigned y = (unsigned)label[p.first + r];
+    const float zl = z[y];
+    if (threadIdx.x == 0) row_loss[row_of[p.first + r]] = lse - zl;
+    if (!GRAD) return;
+    const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
+    for (unsigned v = threadIdx.x * 8; v < V; v += 256 * 8) {
+        Eight x[3];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float w = 0.f;
+            if (v + j < V) w = (v + j == y ? expm1f(zl - lse) : expf(z[v + j] - lse)) * held;
+            if (o.dt == SCAR_F32) split3(w, x[0].b[j], x[1].b[j], x[2].b[j]);
+            else if (o.dt == SCAR_F16) x[0].h[j] = __float2half_rn(w);
+            else x[0].b[j] = __float2bfloat16_rn(w);
+        }
+        for (int q = 0; q < planes; ++q) *reinterpret_cast<uint4 *>(row + q * o.plane + v) = x[q].u;
+    }
 }
 
-template <typename T>
+// Adds the parts of a split product and does what the product's own epilogue does without a split.
 __global__ void __launch_bounds__(256)
-k_xent_dw(const float *dz, const T *h, uint64_t hp, unsigned V, unsigned D, const unsigned *idx, const XentRecord *rec,
-          Piece p, float scale, bool mean, bool first, bool last, float *acc, T *dw, uint64_t dwp) {
-    const unsigned R = p.rows(rec);
-    const float g = grad_factor(rec, scale, mean);
-    gemm_tile(blockIdx.y * kTile, blockIdx.x * kTile, R,
-              [&](unsigned v, unsigned r) { return v < V ? dz[(uint64_t)r * V + v] : 0.f; },
-              [&](unsigned d, unsigned r) { return d < D ? to_f32<T>(h[idx[p.first + r] * hp + d]) : 0.f; },
-              [&](unsigned v, unsigned d, float x) {
-                  if (v >= V || d >= D) return;
-                  if (!first) x += acc[(uint64_t)v * D + d];
-                  if (last) dw[v * dwp + d] = from_f32<T>(x * g);
-                  else acc[(uint64_t)v * D + d] = x;
-              });
-}
-
-// Rows of dh that do not count are zero.
-template <typename T>
-__global__ void __launch_bounds__(256)
-k_xent_zero_rows(const long long *labels, long long ignore, unsigned V, unsigned D, T *dh, uint64_t dhp) {
-    const long long y = labels[blockIdx.x];
-    if (y != ignore && y >= 0 && y < (long long)V) return;
-    for (unsigned d = threadIdx.x; d < D; d += 256) dh[blockIdx.x * dhp + d] = from_f32<T>(0.f);
+k_xent_combine(const __grid_constant__ TcArgs g) {
+    const unsigned rows = *g.rows, mine = rows > g.first ? min(g.most, rows - g.first) : 0u;
+    const unsigned m = g.dyn == 0 ? mine : g.m;
+    const unsigned groups = (g.n + 7) / 8;
+    const float f = g.mean ? g.scale / (float)max(rows, 1u) : g.scale;
+    const unsigned long long stride = (unsigned long long)g.m * g.n, total = (unsigned long long)m * groups;
+    const bool vec = (g.n & 3u) == 0;
+    for (unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 256) {
+        const unsigned row = total >> 32 ? (unsigned)(i / groups) : (unsigned)i / groups;
+        const unsigned col = (unsigned)(i - (unsigned long long)row * groups) * 8;
+        const float *p = g.part + (unsigned long long)row * g.n + col;
+        float x[8] = {};
+        for (unsigned s = 0; s < g.splits; ++s, p += stride) {
+            if (vec && col + 8 <= g.n) {
+                const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
+                x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (col + j < g.n) x[j] += p[j];
+            }
+        }
+        store_out8(g, x, row, g.row_map ? g.row_map[g.first + row] : row, col, f);
+    }
 }
 
 __global__ void __launch_bounds__(kRowThreads)
-k_xent_loss(const float *row_loss, unsigned n, bool mean, XentRecord *rec, float *d_loss) {
+k_xent_loss(const float *__restrict__ row_loss, unsigned n, bool mean, XentRecord *rec, float *d_loss) {
     __shared__ double sh[32];
     double s = 0.0;
     for (unsigned t = threadIdx.x; t < n; t += kRowThreads) s += row_loss[t];
@@ -212,10 +338,18 @@ k_xent_loss(const float *row_loss, unsigned n, bool mean, XentRecord *rec, float
     if (threadIdx.x) return;
     s = 0.0;
     for (int w = 0; w < 32; ++w) s += sh[w];
-    rec->sum = s;
     rec->loss = (float)(mean ? s / (double)max(rec->rows, 1u) : s);
     if (d_loss) *d_loss = rec->loss;
 }
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// A 16-bit matrix as the products read it: `planes` of rows x inner, rows `pitch` elements apart.
+struct Operand {
+    const void *p;
+    uint64_t inner, rows, pitch, planes, plane;
+};
 
 }  // namespace
 
@@ -223,13 +357,25 @@ struct scar_xent {
     int device = 0;
     cudaStream_t stream = nullptr;
     scar_xent_config cfg{};
-    unsigned piece = 0;  // rows per piece
-    unsigned *idx = nullptr;
-    float *row_loss = nullptr;
-    float *z = nullptr;
+    EncodeTiled encode = nullptr;
+    unsigned pairs = 74;       // CTA pairs the GPU holds at a time
+    unsigned planes = 1;
+    unsigned piece = 0;        // rows per piece, a multiple of 64
+    uint64_t vp = 0, dp = 0;   // classes and dim, rounded up to a multiple of 8
+    uint64_t h_rows = 0;
+    unsigned groups = 0;       // groups of 128 classes, two per tile
+    unsigned *row_of = nullptr, *pos = nullptr;
+    int *label = nullptr;
+    float *label_z = nullptr, *row_loss = nullptr;
+    unsigned short *h = nullptr;   // compacted h
+    unsigned short *w = nullptr;   // w in planes, or copied to 16-byte rows (allocated by the first call that needs it)
+    unsigned short *dz = nullptr;  // the piece's exponentials, then dz
+    float2 *stat = nullptr;
+    float *part = nullptr;         // float32 logits of the piece, or parts of split products
+    uint64_t part_bytes = 0;
     float *acc = nullptr;
     XentRecord *rec = nullptr;
-    XentRecord *h_rec = nullptr;  // pinned
+    XentRecord *h_rec = nullptr;   // pinned
     std::vector<void *> owned;
     uint64_t bytes = 0;
     uint64_t launches = 0;
@@ -257,58 +403,243 @@ int check_call(const scar_xent *op, const void *h, uint64_t hp, const void *w, u
     const unsigned b = elem_size(op->cfg.dtype);
     if (n > op->cfg.max_tokens) return SCAR_ERR_CAPACITY;
     if (n && (!h || !labels)) return SCAR_ERR_INVALID_ARG;
-    if (hp < op->cfg.dim || wp < op->cfg.dim || hp >= (1ull << 40) || wp >= (1ull << 40)) return SCAR_ERR_INVALID_ARG;
+    if (hp < op->cfg.dim || wp < op->cfg.dim || hp >= (1ull << 38) || wp >= (1ull << 38)) return SCAR_ERR_INVALID_ARG;
     if ((uintptr_t)h % b || (uintptr_t)w % b || (uintptr_t)labels % 8) return SCAR_ERR_INVALID_ARG;
     return check_current_device(op->device);
 }
 
+bool rows_aligned(const void *p, uint64_t pitch, unsigned elem) { return (uintptr_t)p % 16 == 0 && pitch * elem % 16 == 0; }
+
+// The tensor map of an operand: boxes of 64 values of k by box_rows rows (K-major), or of 64 of its own dimension by 64
+// values of k (MN-major; box_rows = 64).
+int make_map(const scar_xent *op, CUtensorMap *map, const Operand &x, unsigned box_rows) {
+    const cuuint64_t dims[3] = {x.inner, x.rows, x.planes}, strides[2] = {x.pitch * 2, (x.planes > 1 ? x.plane : x.pitch) * 2};
+    const cuuint32_t box[3] = {kBK, box_rows, 1}, step[3] = {1, 1, 1};
+    const CUresult rc = op->encode(map, op->cfg.dtype == SCAR_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                                   const_cast<void *>(x.p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? SCAR_OK : SCAR_ERR_CUDA;
+}
+
+// How many parts to cut the sum over k into.  In units of one pair's 64 values of k: a wave of tiles costs its length
+// and about four for the exposed part of its epilogue; parts cost their way through memory and the launch that joins
+// them (about 12 units, and 6.5 TB/s).
+unsigned choose_splits(const scar_xent *op, uint64_t m, uint64_t n, uint64_t k, int bn, uint64_t part_bytes) {
+    const double unit_s = 0.28e-6 * (op->planes == 3 ? 3 : 1);
+    const uint64_t tiles = ((m + kBM - 1) / kBM) * ((n + bn - 1) / bn), kb = (k + kBK - 1) / kBK;
+    double best = 0;
+    unsigned got = 1;
+    for (unsigned s = 1; s <= 32 && s <= kb; ++s) {
+        if (s > 1 && (m * n * 4 * s > part_bytes || tiles * s > 4ull * op->pairs)) break;
+        const double waves = (double)((tiles * s + op->pairs - 1) / op->pairs);
+        double cost = waves * ((double)((kb + s - 1) / s) + 4);
+        if (s > 1) cost += 12 + (double)m * n * 4 * (2 * s) / 6.5e12 / unit_s;
+        if (s == 1 || cost < best * 0.97) {
+            best = cost;
+            got = s;
+        }
+    }
+    return got;
+}
+
+template <int PL, bool A_MN, bool B_MN, Epi EPI> void launch_tc(scar_xent *op, const TcArgs &g) {
+    using S = TcShape<PL>;
+    const uint64_t tiles = (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + S::BN - 1) / S::BN) * g.splits;
+    const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, op->pairs);
+    if (!pairs) return;
+    k_tc_gemm<PL, A_MN, B_MN, EPI><<<2 * pairs, kGemmThreads, S::kSmem, op->stream>>>(g);
+    op->launches++;
+}
+
+template <int PL, bool A_MN, bool B_MN, Epi EPI> bool allow_smem() {
+    return cudaFuncSetAttribute(k_tc_gemm<PL, A_MN, B_MN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<PL>::kSmem) == cudaSuccess;
+}
+template <int PL> bool allow_smem_all() {
+    return allow_smem<PL, false, false, Epi::kPart>() && allow_smem<PL, false, true, Epi::kPart>() && allow_smem<PL, true, true, Epi::kPart>() &&
+           allow_smem<PL, false, true, Epi::kOut>() && allow_smem<PL, true, true, Epi::kOut>();
+}
+
+// A product that ends in an output, split over k or not.
+template <int PL, bool A_MN> void launch_out(scar_xent *op, TcArgs g) {
+    g.splits = choose_splits(op, g.m, g.n, g.k, TcShape<PL>::BN, op->part_bytes);
+    if (g.splits == 1) {
+        launch_tc<PL, A_MN, true, Epi::kOut>(op, g);
+        return;
+    }
+    launch_tc<PL, A_MN, true, Epi::kPart>(op, g);
+    const uint64_t todo = (uint64_t)g.m * ((g.n + 7) / 8);
+    k_xent_combine<<<(unsigned)std::min<uint64_t>((todo + 255) / 256, 16 * op->pairs), 256, 0, op->stream>>>(g);
+    op->launches++;
+}
+
 template <typename T>
-void run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, const int64_t *labels, unsigned n,
-              bool grad, float scale, float *row_loss, float *d_loss, T *dh, uint64_t dhp, T *dw, uint64_t dwp) {
+int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, const int64_t *labels, unsigned n, bool grad, float scale,
+             float *row_loss, float *d_loss, T *dh, uint64_t dhp, T *dw, uint64_t dwp) {
+    constexpr int PL = sizeof(T) == 4 ? 3 : 1;
+    using S = TcShape<PL>;
     const unsigned V = (unsigned)op->cfg.n_classes, D = (unsigned)op->cfg.dim;
     const bool mean = op->cfg.reduction == SCAR_MEAN;
     const long long *y = reinterpret_cast<const long long *>(labels);
     cudaStream_t s = op->stream;
+    int rc;
     if (!row_loss) row_loss = op->row_loss;
-    auto tiles = [](unsigned v) { return (v + kTile - 1) / kTile; };
-    k_xent_rows<<<1, kRowThreads, 0, s>>>(y, n, op->cfg.ignore_label, V, op->idx, row_loss, op->rec);
-    op->launches++;
-    if (grad && n) {
-        k_xent_zero_rows<T><<<n, 256, 0, s>>>(y, op->cfg.ignore_label, V, D, dh, dhp);
+
+    // w in place where its rows lie on 16-byte boundaries, else (and in float32 always) through a copy of its own
+    const bool w_copied = PL == 3 || !rows_aligned(w, wp, sizeof(T));
+    if (w_copied && !op->w && (rc = xent_alloc(op, &op->w, (uint64_t)PL * V * op->dp * 2)) != SCAR_OK) return rc;
+    const Operand oh{op->h, D, op->h_rows, op->dp, PL, op->h_rows * op->dp};
+    const Operand ow = w_copied ? Operand{op->w, D, V, op->dp, PL, (uint64_t)V * op->dp} : Operand{w, D, V, wp, 1, (uint64_t)V * wp};
+    const Operand oz{op->dz, V, op->piece, op->vp, PL, (uint64_t)op->piece * op->vp};
+    TcArgs logits{}, dhg{}, dwg{};
+    if ((rc = make_map(op, &logits.a, oh, 128)) != SCAR_OK || (rc = make_map(op, &logits.b, ow, S::BN / 2)) != SCAR_OK) return rc;
+    if (grad && ((rc = make_map(op, &dhg.a, oz, 128)) != SCAR_OK || (rc = make_map(op, &dhg.b, ow, 64)) != SCAR_OK ||
+                 (rc = make_map(op, &dwg.a, oz, 64)) != SCAR_OK || (rc = make_map(op, &dwg.b, oh, 64)) != SCAR_OK))
+        return rc;
+
+    k_xent_rows<<<1, kRowThreads, 0, s>>>(y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec);
+    const unsigned most_ctas = 16 * op->pairs;
+    auto ctas = [&](uint64_t rows) { return (unsigned)std::min<uint64_t>((rows * (op->dp / 8) + 255) / 256, most_ctas); };
+    k_xent_place<T><<<ctas(n + 64), 256, 0, s>>>(h, hp, n, D, (unsigned)op->dp, rows_aligned(h, hp, sizeof(T)), op->h, oh.plane, op->pos,
+                                                 &op->rec->rows, grad ? dh : nullptr, dhp);
+    op->launches += 2;
+    if (w_copied) {
+        k_xent_place<T><<<ctas(V), 256, 0, s>>>(w, wp, V, D, (unsigned)op->dp, rows_aligned(w, wp, sizeof(T)), op->w, ow.plane, nullptr, nullptr,
+                                                nullptr, 0);
         op->launches++;
     }
-    for (unsigned at = 0; at < std::max(n, 1u); at += op->piece) {
+
+    TcArgs base{};
+    base.rows = &op->rec->rows;
+    base.error = &op->rec->error;
+    base.bf16 = op->cfg.dtype != SCAR_F16;
+    base.part = op->part;
+    base.out_type = op->cfg.dtype;
+    base.mean = mean;
+    base.scale = op->cfg.dtype == SCAR_F16 ? scale / kDzF16 : scale;
+    auto fill = [&](TcArgs &g, unsigned m, unsigned nn, unsigned k, int dyn) {
+        const CUtensorMap a = g.a, b = g.b;
+        g = base;
+        g.a = a;
+        g.b = b;
+        g.m = m;
+        g.n = nn;
+        g.k = k;
+        g.dyn = dyn;
+        g.n_fast = nn < m;
+        g.splits = 1;
+    };
+    for (unsigned at = 0; at == 0 || at < n; at += op->piece) {
+        const unsigned rows = std::min(op->piece, n - at), rows64 = (rows + 63) / 64 * 64;
         const Piece p{at, op->piece};
-        const unsigned rows = std::min(op->piece, n - at);
+        base.first = at;
+        base.most = op->piece;
+        const DzOut dz{op->dz, op->vp, oz.plane, op->cfg.dtype};
         if (rows) {
-            k_xent_logits<T><<<dim3(tiles(V), tiles(rows)), 256, 0, s>>>(h, hp, w, wp, V, D, op->idx, op->rec, p, op->z);
-            if (grad) k_xent_softmax<true><<<rows, 256, 0, s>>>(op->z, V, y, op->idx, op->rec, p, row_loss);
-            else k_xent_softmax<false><<<rows, 256, 0, s>>>(op->z, V, y, op->idx, op->rec, p, row_loss);
-            op->launches += 2;
+            fill(logits, rows, V, D, 0);
+            logits.a_row0 = at;
+            logits.prob = reinterpret_cast<__half *>(op->dz);
+            logits.prob_pitch = op->vp;
+            logits.stat = op->stat;
+            logits.stat_pitch = op->groups;
+            logits.label = op->label;
+            logits.label_z = op->label_z;
+            logits.splits = choose_splits(op, rows, V, D, S::BN, op->part_bytes);
+            if (PL == 3 || logits.splits > 1) {
+                launch_tc<PL, false, false, Epi::kPart>(op, logits);
+                if (grad)
+                    k_xent_softmax<true><<<rows64, 256, 0, s>>>(op->part, logits.splits, (uint64_t)rows * V, dz, V, op->label, op->row_of, op->rec, p,
+                                                                row_loss);
+                else
+                    k_xent_softmax<false><<<rows64, 256, 0, s>>>(op->part, logits.splits, (uint64_t)rows * V, dz, V, op->label, op->row_of, op->rec, p,
+                                                                 row_loss);
+            } else if (grad) {
+                if constexpr (PL == 1) launch_tc<1, false, false, Epi::kProb>(op, logits);
+                k_xent_dz<true><<<rows64, 256, 0, s>>>(dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, op->rec, p, row_loss);
+            } else {
+                if constexpr (PL == 1) launch_tc<1, false, false, Epi::kStat>(op, logits);
+                k_xent_dz<false><<<rows, 256, 0, s>>>(dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, op->rec, p, row_loss);
+            }
+            op->launches++;
         }
         if (!grad) continue;
         if (rows) {
-            k_xent_dh<T><<<dim3(tiles(D), tiles(rows)), 256, 0, s>>>(op->z, w, wp, V, D, op->idx, op->rec, p, scale, mean, dh, dhp);
-            op->launches++;
+            fill(dhg, rows, D, V, 0);
+            dhg.out = dh;
+            dhg.out_pitch = dhp;
+            dhg.out_vec = rows_aligned(dh, dhp, sizeof(T));
+            dhg.row_map = op->row_of;
+            launch_out<PL, false>(op, dhg);
         }
-        k_xent_dw<T><<<dim3(tiles(D), tiles(V)), 256, 0, s>>>(op->z, h, hp, V, D, op->idx, op->rec, p, scale, mean, at == 0,
-                                                              at + op->piece >= n, op->acc, dw, dwp);
-        op->launches++;
+        fill(dwg, V, D, rows, 1);
+        dwg.b_row0 = at;
+        dwg.out = dw;
+        dwg.out_pitch = dwp;
+        dwg.out_vec = rows_aligned(dw, dwp, sizeof(T));
+        if (n > op->piece) {  // several pieces: their sums in float32, in dw itself when it is float32
+            dwg.acc = PL == 3 ? reinterpret_cast<float *>(dw) : op->acc;
+            dwg.acc_pitch = PL == 3 ? dwp : D;
+            dwg.acc_vec = PL == 3 ? dwg.out_vec : D % 4 == 0;
+            dwg.acc_first = at == 0;
+            dwg.acc_last = at + (uint64_t)op->piece >= n;
+        }
+        launch_out<PL, true>(op, dwg);
+        if ((uint64_t)at + op->piece >= n) break;
     }
     k_xent_loss<<<1, kRowThreads, 0, s>>>(row_loss, n, mean, op->rec, d_loss);
     op->launches++;
+    return SCAR_OK;
 }
 
 int call(scar_xent *op, const void *h, uint64_t hp, const void *w, uint64_t wp, const int64_t *labels, uint64_t n,
          bool grad, float scale, float *row_loss, float *d_loss, void *dh, uint64_t dhp, void *dw, uint64_t dwp) {
-    dispatch_operand(op->cfg.dtype, [&](auto e) {
-        using T = decltype(e);
-        run_xent<T>(op, static_cast<const T *>(h), hp, static_cast<const T *>(w), wp, labels, (unsigned)n, grad, scale,
-                    row_loss, d_loss, static_cast<T *>(dh), dhp, static_cast<T *>(dw), dwp);
-    });
+    int rc = SCAR_OK;
+    try {
+        dispatch_operand(op->cfg.dtype, [&](auto e) {
+            using T = decltype(e);
+            rc = run_xent<T>(op, static_cast<const T *>(h), hp, static_cast<const T *>(w), wp, labels, (unsigned)n, grad, scale,
+                             row_loss, d_loss, static_cast<T *>(dh), dhp, static_cast<T *>(dw), dwp);
+        });
+    } catch (...) {
+        rc = SCAR_ERR_ALLOC;
+    }
+    if (rc != SCAR_OK) return rc;
     TRAIN_TRY(cudaGetLastError());
     op->ran = true;
     return SCAR_OK;
+}
+
+// Rows per piece and the workspaces that go by it.
+int size_workspaces(scar_xent *op) {
+    const scar_xent_config &c = op->cfg;
+    const uint64_t V = c.n_classes, D = c.dim, T = std::max<uint64_t>(c.max_tokens, 1);
+    const bool f32 = c.dtype == SCAR_F32, grad = !c.loss_only;
+    op->planes = f32 ? 3 : 1;
+    op->vp = round_up(V, 8);
+    op->dp = round_up(D, 8);
+    op->groups = (unsigned)(2 * ((V + 255) / 256));
+    const uint64_t limit = c.workspace_bytes ? c.workspace_bytes : 1ull << 30;
+    const uint64_t row = f32 ? 4 * V + (grad ? 6 * op->vp : 0) : 8ull * op->groups + (grad ? 2 * op->vp : 0);
+    uint64_t piece = std::max<uint64_t>(limit / row / 256 * 256, 256);
+    if (grad && !f32 && piece < T && T * row <= piece * row + V * D * 4) piece = T;
+    op->piece = (unsigned)round_up(std::min(piece, T), 64);
+    op->h_rows = round_up(T, 64);
+    int rc;
+    if ((rc = xent_alloc(op, &op->row_of, 4 * T)) != SCAR_OK || (rc = xent_alloc(op, &op->pos, 4 * T)) != SCAR_OK ||
+        (rc = xent_alloc(op, &op->label, 4 * T)) != SCAR_OK || (rc = xent_alloc(op, &op->label_z, 4 * T)) != SCAR_OK ||
+        (rc = xent_alloc(op, &op->row_loss, 4 * T)) != SCAR_OK || (rc = xent_alloc(op, &op->rec, sizeof(XentRecord))) != SCAR_OK ||
+        (rc = xent_alloc(op, &op->h, op->planes * op->h_rows * op->dp * 2)) != SCAR_OK)
+        return rc;
+    if (!f32 && (rc = xent_alloc(op, &op->stat, 8ull * op->groups * op->piece)) != SCAR_OK) return rc;
+    if (grad && (rc = xent_alloc(op, &op->dz, op->planes * (uint64_t)op->piece * op->vp * 2)) != SCAR_OK) return rc;
+    if (grad && !f32 && op->piece < T && (rc = xent_alloc(op, &op->acc, V * D * 4)) != SCAR_OK) return rc;
+    if ((f32 || D % 8) && (rc = xent_alloc(op, &op->w, op->planes * V * op->dp * 2)) != SCAR_OK) return rc;
+    // parts of split products: as many as choose_splits may ask for, up to 64 MiB
+    const uint64_t P = std::min<uint64_t>(op->piece, T);
+    uint64_t most = P * V;
+    if (grad) most = std::max(most, std::max(P * D, V * D));
+    op->part_bytes = std::min<uint64_t>(64ull << 20, most * 4 * 32);
+    if (f32) op->part_bytes = std::max(op->part_bytes, P * V * 4);
+    return xent_alloc(op, &op->part, op->part_bytes);
 }
 
 }  // namespace
@@ -329,22 +660,19 @@ int scar_xent_init(scar_xent **out, const scar_xent_config *cfg, void *cuda_stre
     op->stream = static_cast<cudaStream_t>(cuda_stream);
     auto setup = [&]() -> int {
         TRAIN_TRY(cudaGetDevice(&op->device));
-        const uint64_t row = 4 * cfg->n_classes, limit = cfg->workspace_bytes ? cfg->workspace_bytes : 1ull << 30;
-        uint64_t piece = std::max<uint64_t>(limit / row / 256 * 256, 256);
-        const bool sums = cfg->dtype != SCAR_F32;  // dw itself holds the sums of a float32 operator
-        if (piece < cfg->max_tokens && !cfg->loss_only &&
-            cfg->max_tokens * row <= piece * row + cfg->n_classes * cfg->dim * 4)
-            piece = cfg->max_tokens;
-        op->piece = (unsigned)std::min<uint64_t>(piece, std::max<uint64_t>(cfg->max_tokens, 1));
-        int rc;
-        if ((rc = xent_alloc(op, &op->idx, 4 * cfg->max_tokens)) != SCAR_OK) return rc;
-        if ((rc = xent_alloc(op, &op->row_loss, 4 * cfg->max_tokens)) != SCAR_OK) return rc;
-        if ((rc = xent_alloc(op, &op->rec, sizeof(XentRecord))) != SCAR_OK) return rc;
-        if ((rc = xent_alloc(op, &op->z, (uint64_t)op->piece * row)) != SCAR_OK) return rc;
-        (void)sums;
-        if (!cfg->loss_only && op->piece < cfg->max_tokens &&
-            (rc = xent_alloc(op, &op->acc, cfg->n_classes * cfg->dim * 4)) != SCAR_OK)
-            return rc;
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        TRAIN_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found));
+        if (found != cudaDriverEntryPointSuccess || !fn) return SCAR_ERR_CUDA;
+        op->encode = reinterpret_cast<EncodeTiled>(fn);
+        if (cfg->dtype == SCAR_F32 ? !(allow_smem_all<3>())
+                                   : !(allow_smem_all<1>() && allow_smem<1, false, false, Epi::kProb>() && allow_smem<1, false, false, Epi::kStat>()))
+            return SCAR_ERR_CUDA;
+        int sms = 0;
+        TRAIN_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, op->device));
+        op->pairs = std::max(1, sms / 2);
+        const int rc = size_workspaces(op);
+        if (rc != SCAR_OK) return rc;
         if (cudaMallocHost(&op->h_rec, sizeof(XentRecord)) != cudaSuccess) {
             cudaGetLastError();
             return SCAR_ERR_ALLOC;
