@@ -1,7 +1,11 @@
 // Global gradient norm over a list of tensors, and clipping (scar_gnorm_* of scar.h).
 //
-// The tensors are cut into pieces of at most kPieceBytes on the host, once; a CTA walks over pieces with a fixed
-// stride, so which CTA adds what depends on the lengths alone and the result is the same bits every time.
+// The tensors are cut into pieces of at most kPieceBytes on the host, once, so that every piece but a tensor's first
+// begins on a 16-byte boundary.  A CTA walks over pieces with a fixed stride: which CTA adds what depends on the lengths
+// alone, the last CTA to finish adds the CTAs' sums in their order, and the result is the same bits every time.
+// Bound by HBM: one read for the norm, one read and one write for the scaled values.  The second kernel is already
+// resident when the first ends (programmatic launch) and walks the pieces backwards, so that what the first read last
+// is still in L2.
 #include <new>
 #include <vector>
 
@@ -12,7 +16,9 @@ using namespace scar;
 namespace {
 
 constexpr int kNormThreads = 512;
-constexpr unsigned kPieceBytes = 32768;
+constexpr unsigned kPieceBytes = 32768;  // four 16-byte loads per thread, all in flight together
+constexpr int kVecs = kPieceBytes / 16 / kNormThreads;
+constexpr unsigned kCtasPerSm = 4;
 
 struct Piece {
     const void *src;
@@ -51,35 +57,80 @@ template <int KIND> __device__ __forceinline__ double cta_join(double v, double 
     return v;  // thread 0
 }
 
+template <typename T> union Vec {
+    static constexpr int n = 16 / sizeof(T);
+    uint4 u;
+    T v[n];
+};
+
+// A piece as its vector part and what lies before and behind it (fewer elements than a vector each).
+template <typename T> struct Split {
+    const T *src;
+    unsigned head, vecs, n;
+    __device__ __forceinline__ explicit Split(const Piece &p) : src(static_cast<const T *>(p.src)), n(p.n) {
+        head = min(n, (unsigned)((0u - (unsigned)(uintptr_t)src) & 15u) / (unsigned)sizeof(T));
+        vecs = (n - head) / Vec<T>::n;
+    }
+    // The one element outside the vectors that thread t looks after, or n.
+    __device__ __forceinline__ unsigned edge(unsigned t) const {
+        const unsigned tail = head + vecs * Vec<T>::n;
+        return t < head ? t : min(n, tail + (t - head));
+    }
+    __device__ __forceinline__ void load(Vec<T> (&x)[kVecs]) const {
+        const uint4 *b = reinterpret_cast<const uint4 *>(src + head);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const unsigned at = threadIdx.x + i * kNormThreads;
+            x[i].u = at < vecs ? b[at] : make_uint4(0, 0, 0, 0);
+        }
+    }
+};
+
 template <int KIND, typename T> __device__ __forceinline__ double piece_norm(const Piece &p) {
-    const T *s = static_cast<const T *>(p.src);
-    float a = 0.f;
-    for (unsigned i = threadIdx.x; i < p.n; i += kNormThreads) add_term<KIND>(a, to_f32<T>(s[i]));
-    return (double)a;
+    const Split<T> s(p);
+    Vec<T> x[kVecs];
+    s.load(x);
+    float a[2] = {0.f, 0.f};
+    const unsigned e = s.edge(threadIdx.x);
+    if (e < s.n && threadIdx.x < 2 * Vec<T>::n) add_term<KIND>(a[0], to_f32<T>(s.src[e]));
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int j = 0; j < Vec<T>::n; ++j) add_term<KIND>(a[j & 1], to_f32<T>(x[i].v[j]));
+    return join<KIND>((double)a[0], (double)a[1]);
 }
 
+// Every CTA leaves its part; the last one to do so joins them all.
 template <int KIND>
-__global__ void __launch_bounds__(kNormThreads)
-k_gnorm_partials(const Piece *__restrict__ pieces, unsigned n_pieces, double *__restrict__ part) {
+__global__ void __launch_bounds__(kNormThreads, kCtasPerSm)
+k_gnorm_norm(const Piece *__restrict__ pieces, unsigned n_pieces, double *part, unsigned *ticket, float max_norm, bool clip,
+             NormRecord *rec, float *d_norm) {
     __shared__ double sh[32];
+    __shared__ bool last;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     double v = 0.0;
+    Piece next{};
+    if (blockIdx.x < n_pieces) next = pieces[blockIdx.x];
     for (unsigned i = blockIdx.x; i < n_pieces; i += gridDim.x) {
-        const Piece p = pieces[i];
+        const Piece p = next;
+        if (i + gridDim.x < n_pieces) next = pieces[i + gridDim.x];
         const double w = p.dtype == SCAR_F32    ? piece_norm<KIND, float>(p)
                          : p.dtype == SCAR_BF16 ? piece_norm<KIND, __nv_bfloat16>(p)
                                                 : piece_norm<KIND, __half>(p);
         v = join<KIND>(v, w);
     }
     v = cta_join<KIND>(v, sh);
-    if (threadIdx.x == 0) part[blockIdx.x] = v;
-}
-
-template <int KIND>
-__global__ void __launch_bounds__(kNormThreads)
-k_gnorm_final(const double *__restrict__ part, unsigned n, float max_norm, bool clip, NormRecord *rec, float *d_norm) {
-    __shared__ double sh[32];
-    double v = 0.0;
-    for (unsigned i = threadIdx.x; i < n; i += kNormThreads) v = join<KIND>(v, part[i]);
+    if (threadIdx.x == 0) {
+        part[blockIdx.x] = v;
+        __threadfence();
+        last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    v = 0.0;
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += kNormThreads) v = join<KIND>(v, __ldcg(part + i));
+    __syncthreads();
     v = cta_join<KIND>(v, sh);
     if (threadIdx.x) return;
     if (KIND == SCAR_GNORM_L2) v = sqrt(v);
@@ -89,19 +140,42 @@ k_gnorm_final(const double *__restrict__ part, unsigned n, float max_norm, bool 
     rec->coef = coef;
     rec->nonfinite = !isfinite(v);
     if (d_norm) *d_norm = (float)v;
+    *ticket = 0;  // for the next call
 }
 
 template <typename T> __device__ __forceinline__ void scale_piece(const Piece &p, float coef) {
-    const T *s = static_cast<const T *>(p.src);
+    const Split<T> s(p);
+    Vec<T> x[kVecs];
+    s.load(x);
     T *d = static_cast<T *>(p.dst);
-    for (unsigned i = threadIdx.x; i < p.n; i += kNormThreads) d[i] = from_f32<T>(to_f32<T>(s[i]) * coef);
+    const unsigned e = s.edge(threadIdx.x);
+    if (e < s.n && threadIdx.x < 2 * Vec<T>::n) d[e] = from_f32<T>(to_f32<T>(s.src[e]) * coef);
+    const bool vec = (((uintptr_t)p.dst ^ (uintptr_t)p.src) & 15) == 0;
+    d += s.head;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const unsigned at = threadIdx.x + i * kNormThreads;
+#pragma unroll
+        for (int j = 0; j < Vec<T>::n; ++j) x[i].v[j] = from_f32<T>(to_f32<T>(x[i].v[j]) * coef);
+        if (at >= s.vecs) continue;
+        if (vec) {
+            __stcs(reinterpret_cast<uint4 *>(d) + at, x[i].u);
+        } else {
+#pragma unroll
+            for (int j = 0; j < Vec<T>::n; ++j) d[at * Vec<T>::n + j] = x[i].v[j];
+        }
+    }
 }
 
-__global__ void __launch_bounds__(kNormThreads)
-k_gnorm_scale(const Piece *__restrict__ pieces, unsigned n_pieces, const NormRecord *__restrict__ rec) {
+__global__ void __launch_bounds__(kNormThreads, kCtasPerSm)
+k_gnorm_scale(const Piece *__restrict__ pieces, unsigned n_pieces, const NormRecord *rec) {
+    Piece next{};
+    if (blockIdx.x < n_pieces) next = pieces[n_pieces - 1 - blockIdx.x];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const float coef = (float)rec->coef;
     for (unsigned i = blockIdx.x; i < n_pieces; i += gridDim.x) {
-        const Piece p = pieces[i];
+        const Piece p = next;
+        if (i + gridDim.x < n_pieces) next = pieces[n_pieces - 1 - (i + gridDim.x)];
         if (p.dtype == SCAR_F32) scale_piece<float>(p, coef);
         else if (p.dtype == SCAR_BF16) scale_piece<__nv_bfloat16>(p, coef);
         else scale_piece<__half>(p, coef);
@@ -119,6 +193,7 @@ struct scar_gnorm {
     std::vector<Piece> h_pieces;
     Piece *pieces = nullptr;
     double *part = nullptr;
+    unsigned *ticket = nullptr;
     NormRecord *rec = nullptr;
     NormRecord *h_rec = nullptr;  // pinned
     unsigned grid = 1;
@@ -137,7 +212,7 @@ int check_tensors(const scar_tensor *t, uint64_t n) {
         if (t[i].n_elems >= (1ull << 48)) return SCAR_ERR_LAYOUT;
         if (t[i].n_elems && !t[i].d_data) return SCAR_ERR_INVALID_ARG;
         if ((uintptr_t)t[i].d_data % b || (uintptr_t)t[i].d_out % b) return SCAR_ERR_INVALID_ARG;
-        pieces += (t[i].n_elems * b + kPieceBytes - 1) / kPieceBytes;
+        pieces += (t[i].n_elems * b + kPieceBytes - 1) / kPieceBytes + 1;
     }
     return pieces < (1ull << 31) ? SCAR_OK : SCAR_ERR_CAPACITY;
 }
@@ -148,9 +223,11 @@ void cut(scar_gnorm *op, const scar_tensor *t, uint64_t n) {
         const unsigned b = elem_size(t[i].dtype), most = kPieceBytes / b;
         const char *src = static_cast<const char *>(t[i].d_data);
         char *dst = t[i].d_out ? static_cast<char *>(t[i].d_out) : const_cast<char *>(src);
-        for (uint64_t at = 0; at < t[i].n_elems; at += most) {
-            const uint64_t left = t[i].n_elems - at;
-            op->h_pieces.push_back({src + at * b, dst + at * b, (unsigned)(left < most ? left : most), t[i].dtype});
+        const unsigned head = (unsigned)((uintptr_t)src % 16) / b;  // the first piece ends where a later one may begin
+        for (uint64_t at = 0; at < t[i].n_elems;) {
+            const uint64_t left = t[i].n_elems - at, size = most - (at ? 0 : head);
+            op->h_pieces.push_back({src + at * b, dst + at * b, (unsigned)(left < size ? left : size), t[i].dtype});
+            at += size;
         }
     }
 }
@@ -165,9 +242,8 @@ int upload(scar_gnorm *op) {
 
 template <int KIND> void launch_norm(scar_gnorm *op, float max_norm, bool clip, float *d_norm) {
     const unsigned n = (unsigned)op->h_pieces.size();
-    k_gnorm_partials<KIND><<<op->grid, kNormThreads, 0, op->stream>>>(op->pieces, n, op->part);
-    k_gnorm_final<KIND><<<1, kNormThreads, 0, op->stream>>>(op->part, op->grid, max_norm, clip, op->rec, d_norm);
-    op->launches += 2;
+    k_gnorm_norm<KIND><<<op->grid, kNormThreads, 0, op->stream>>>(op->pieces, n, op->part, op->ticket, max_norm, clip, op->rec, d_norm);
+    op->launches += 1;
 }
 
 int run_norm(scar_gnorm *op, float max_norm, bool clip, float *d_norm) {
@@ -208,15 +284,16 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
         int sms = 0;
         TRAIN_TRY(cudaGetDevice(&op->device));
         TRAIN_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, op->device));
-        const unsigned most = 4u * (unsigned)sms, n = (unsigned)op->h_pieces.size();
+        const unsigned most = kCtasPerSm * (unsigned)sms, n = (unsigned)op->h_pieces.size();
         op->grid = n < 1 ? 1 : (n < most ? n : most);
         if (cudaMalloc(&op->pieces, (n ? n : 1) * sizeof(Piece)) != cudaSuccess ||
             cudaMalloc(&op->part, op->grid * sizeof(double)) != cudaSuccess ||
-            cudaMalloc(&op->rec, sizeof(NormRecord)) != cudaSuccess ||
+            cudaMalloc(&op->rec, sizeof(NormRecord)) != cudaSuccess || cudaMalloc(&op->ticket, sizeof(unsigned)) != cudaSuccess ||
             cudaMallocHost(&op->h_rec, sizeof(NormRecord)) != cudaSuccess) {
             cudaGetLastError();
             return SCAR_ERR_ALLOC;
         }
+        TRAIN_TRY(cudaMemsetAsync(op->ticket, 0, sizeof(unsigned), op->stream));
         return upload(op);
     };
     rc = setup();
@@ -258,9 +335,17 @@ int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm) {
     if (rc != SCAR_OK) return rc;
     if ((rc = run_norm(op, max_norm, true, d_norm)) != SCAR_OK) return rc;
     if (op->h_pieces.empty()) return SCAR_OK;
-    k_gnorm_scale<<<op->grid, kNormThreads, 0, op->stream>>>(op->pieces, (unsigned)op->h_pieces.size(), op->rec);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = op->grid;
+    cfg.blockDim = kNormThreads;
+    cfg.stream = op->stream;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    TRAIN_TRY(cudaLaunchKernelEx(&cfg, k_gnorm_scale, (const Piece *)op->pieces, (unsigned)op->h_pieces.size(), (const NormRecord *)op->rec));
     op->launches += 1;
-    TRAIN_TRY(cudaGetLastError());
     return SCAR_OK;
 }
 
@@ -284,6 +369,7 @@ int scar_gnorm_destroy(scar_gnorm *op) {
     const bool ok = cudaStreamSynchronize(op->stream) == cudaSuccess;
     cudaFree(op->pieces);
     cudaFree(op->part);
+    cudaFree(op->ticket);
     cudaFree(op->rec);
     if (op->h_rec) cudaFreeHost(op->h_rec);
     delete op;

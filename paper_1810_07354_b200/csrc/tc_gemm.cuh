@@ -30,6 +30,11 @@ constexpr unsigned long long kWaitNs = 2000000000ull;  // a wait inside the kern
 
 enum class Epi { kPart, kOut, kProb, kStat };
 
+// The logits of 16-bit operands (Epi::kProb, kStat) are summed in registers over rounds of this many stages (1024
+// values of k, 64 instructions): in one accumulator over a dim of 4096 the dropped low bits put a row's loss off by
+// 1.2e-6 of itself.  dh and dw are rounded to 16 bits and need no rounds.
+constexpr unsigned kRound = 16;
+
 template <int PL> struct TcShape {
     static constexpr int BN = PL == 1 ? 256 : 128;
     static constexpr int kABytes = 128 * kBK * 2;       // one plane of one CTA's rows of A
@@ -86,7 +91,7 @@ __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
         : "=r"(ok)
         : "r"(bar), "r"(parity)
         : "memory");
@@ -117,6 +122,14 @@ __device__ __forceinline__ void mbar_arrive_leader(uint32_t bar) {
     asm volatile(
         "{\n .reg .b32 ra;\n mapa.shared::cluster.u32 ra, %0, 0;\n mbarrier.arrive.release.cluster.shared::cluster.b64 _, [ra];\n}\n" ::"r"(bar)
         : "memory");
+}
+// One lane of a converged warp.  The loops below run in all lanes with warp-uniform values and only the issuing of
+// copies and matrix instructions is left to one: a loop that a single lane runs keeps its descriptors in per-lane
+// registers, and moving them where the instructions take them from cost 200 of 700 clocks per stage.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
+    return p;
 }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -158,6 +171,13 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float *v) {
         : "r"(addr));
 }
 
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float *v) {
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+}
 // The loads above are done: nothing that uses their registers moves before this point.
 template <int N> __device__ __forceinline__ void tmem_loaded(float (&v)[N]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -179,6 +199,13 @@ template <bool MN> __device__ __forceinline__ uint64_t smem_desc(uint32_t addr) 
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | lead << 16 | stride << 32 | 1ull << 46 | 2ull << 61;
 }
 template <bool MN> __device__ constexpr uint32_t k_step_bytes() { return MN ? 2048 : 32; }  // 16 values of k
+
+// This warp has read its part of an accumulator.
+__device__ __forceinline__ void acc_release(uint32_t bar, unsigned lane) {
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive_leader(bar);
+}
 
 struct TileWalk {
     unsigned m, k, mt, nt, total, kb, splits;
@@ -357,10 +384,12 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ __align__(8) unsigned long long bars[2 * S::kStages + 2 * S::kAccs];
     __shared__ uint32_t tmem_base;
+    constexpr bool kLogits = EPI == Epi::kProb || EPI == Epi::kStat;
+    constexpr unsigned kPer = PL == 3 ? 1u : kLogits ? kRound : 0xffffffffu;  // stages per accumulator
     const uint32_t stage0 = smem_addr(smem);
     const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages;
     const uint32_t acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 8 * S::kAccs;
-    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const unsigned pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
@@ -388,18 +417,15 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
     bool ok = true;
 
     if (warp == kEpiWarps) {  // loads
-        if (lane == 0) {
-            unsigned it = 0;
-            for (unsigned t = pair; t < walk.total && ok; t += pairs) {
-                unsigned mi, ni, s, k0, k1;
-                walk.at(t, mi, ni, s, k0, k1);
-                const int am = (int)(mi * kBM + rank * 128), bn = (int)(ni * S::BN + rank * (S::BN / 2));
-                for (unsigned kb = k0; kb < k1; ++kb, ++it) {
-                    const unsigned st = it % S::kStages, ph = (it / S::kStages) & 1;
-                    if (!mbar_wait(empty + 8 * st, ph ^ 1, g.error)) {
-                        ok = false;
-                        break;
-                    }
+        unsigned st = 0, ph = 0;
+        for (unsigned t = pair; t < walk.total && ok; t += pairs) {
+            unsigned mi, ni, s, k0, k1;
+            walk.at(t, mi, ni, s, k0, k1);
+            const int am = (int)(mi * kBM + rank * 128), bn = (int)(ni * S::BN + rank * (S::BN / 2));
+            for (unsigned kb = k0; kb < k1; ++kb) {
+                ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * st, ph ^ 1, g.error));
+                if (!ok) break;
+                if (elect_one()) {
                     const uint32_t bar = full + 8 * st, dst = stage0 + st * S::kStageBytes;
                     if (rank == 0) mbar_expect(bar, 2 * S::kStageBytes);
                     const int kk = (int)(kb * kBK);
@@ -420,50 +446,59 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                         }
                     }
                 }
+                __syncwarp();
+                if (++st == S::kStages) {
+                    st = 0;
+                    ph ^= 1;
+                }
             }
         }
     } else if (warp == kEpiWarps + 1) {  // matrix instructions, first CTA of the pair
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             const uint32_t type = g.bf16 ? 1u : 0u;
             const uint32_t idesc = 1u << 4 | type << 7 | type << 10 | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
                                    (uint32_t)(S::BN >> 3) << 17 | (uint32_t)(kBM >> 4) << 24;
-            unsigned it = 0, ac = 0;
+            const uint64_t desc_a = smem_desc<A_MN>(stage0), desc_b = smem_desc<B_MN>(stage0 + PL * S::kABytes);
+            unsigned st = 0, ph = 0, ac = 0, aph = 1;
             for (unsigned t = pair; t < walk.total && ok; t += pairs) {
                 unsigned mi, ni, s, k0, k1;
                 walk.at(t, mi, ni, s, k0, k1);
-                uint32_t d = 0;
-                for (unsigned kb = k0; kb < k1; ++kb, ++it) {
-                    const unsigned st = it % S::kStages, ph = (it / S::kStages) & 1;
-                    if (PL == 3 || kb == k0) {
-                        const unsigned a = ac % S::kAccs;
-                        if (!mbar_wait(acc_empty + 8 * a, ((ac / S::kAccs) & 1) ^ 1, g.error)) {
-                            ok = false;
-                            break;
-                        }
-                        d = tmem + a * S::BN;
+                unsigned left = 0;  // stages left of the accumulator
+                for (unsigned kb = k0; kb < k1; ++kb) {
+                    const bool fresh = left == 0;
+                    if (fresh) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(acc_empty + 8 * ac, aph, g.error));
+                        if (!ok) break;
+                        left = min(kPer, k1 - kb);
                     }
-                    if (!mbar_wait(full + 8 * st, ph, g.error)) {
-                        ok = false;
-                        break;
-                    }
+                    ok = __all_sync(0xffffffffu, mbar_wait(full + 8 * st, ph, g.error));
+                    if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t sa = stage0 + st * S::kStageBytes, sb = sa + PL * S::kABytes;
-                    constexpr int kPairs = PL == 1 ? 1 : 6;
-                    constexpr int pa[6] = {PL == 1 ? 0 : 2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
-                    bool add = PL == 1 ? kb != k0 : false;
+                    const uint32_t d = tmem + ac * S::BN;
+                    --left;
+                    if (elect_one()) {
+                        constexpr int kPairs = PL == 1 ? 1 : 6;
+                        constexpr int pa[6] = {PL == 1 ? 0 : 2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
 #pragma unroll
-                    for (int q = 0; q < kPairs; ++q) {
-                        const uint64_t da = smem_desc<A_MN>(sa + pa[q] * S::kABytes), db = smem_desc<B_MN>(sb + pb[q] * S::kBBytes);
+                        for (int q = 0; q < kPairs; ++q) {
+                            const uint64_t da = desc_a + ((st * S::kStageBytes + pa[q] * S::kABytes) >> 4);
+                            const uint64_t db = desc_b + ((st * S::kStageBytes + pb[q] * S::kBBytes) >> 4);
 #pragma unroll
-                        for (int k = 0; k < kBK / 16; ++k) {
-                            mma_pair(d, da + (k * k_step_bytes<A_MN>() >> 4), db + (k * k_step_bytes<B_MN>() >> 4), idesc, add);
-                            add = true;
+                            for (int k = 0; k < kBK / 16; ++k)
+                                mma_pair(d, da + (k * k_step_bytes<A_MN>() >> 4), db + (k * k_step_bytes<B_MN>() >> 4), idesc,
+                                         q + k > 0 || !fresh);
                         }
+                        mma_commit(empty + 8 * st);
+                        if (left == 0) mma_commit(acc_full + 8 * ac);
                     }
-                    mma_commit(empty + 8 * st);
-                    if (PL == 3 || kb + 1 == k1) {
-                        mma_commit(acc_full + 8 * (ac % S::kAccs));
-                        ++ac;
+                    __syncwarp();
+                    if (++st == S::kStages) {
+                        st = 0;
+                        ph ^= 1;
+                    }
+                    if (left == 0 && ++ac == S::kAccs) {
+                        ac = 0;
+                        aph ^= 1;
                     }
                 }
             }
@@ -476,32 +511,39 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
             unsigned mi, ni, s, k0, k1;
             walk.at(t, mi, ni, s, k0, k1);
             float v[S::kCols];
-            const unsigned rounds = PL == 3 ? k1 - k0 : (k1 > k0 ? 1u : 0u);
-            if (PL == 3 || rounds == 0) {
+            const unsigned rounds = k1 > k0 ? (k1 - k0 - 1) / kPer + 1 : 0u;
+            if (rounds == 0) {
 #pragma unroll
                 for (int j = 0; j < S::kCols; ++j) v[j] = 0.f;
             }
-            for (unsigned r = 0; r < rounds; ++r, ++ac) {
+            // the first round is the tile's accumulator itself, later ones are added to it
+            if (rounds) {
                 const unsigned a = ac % S::kAccs;
                 ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, (ac / S::kAccs) & 1, g.error));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t src = tmem + a * S::BN + half * S::kCols + (quad * 32u << 16);
-                if (PL == 1) {
 #pragma unroll
-                    for (int j = 0; j < S::kCols; j += 32) tmem_load32(src + j, v + j);
-                    tmem_loaded(v);
-                } else {
-                    float u[S::kCols];
+                for (int j = 0; j < S::kCols; j += 32) tmem_load32(src + j, v + j);
+                tmem_loaded(v);
+                acc_release(acc_empty + 8 * a, lane);
+                ++ac;
+            }
+            for (unsigned r = 1; r < rounds; ++r, ++ac) {
+                const unsigned a = ac % S::kAccs;
+                ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, (ac / S::kAccs) & 1, g.error));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t src = tmem + a * S::BN + half * S::kCols + (quad * 32u << 16);
 #pragma unroll
-                    for (int j = 0; j < S::kCols; j += 32) tmem_load32(src + j, u + j);
+                for (int j = 0; j < S::kCols; j += 16) {  // 16 at a time: 128 sums and 32 more registers do not fit
+                    float u[16];
+                    tmem_load16(src + j, u);
                     tmem_loaded(u);
 #pragma unroll
-                    for (int j = 0; j < S::kCols; ++j) v[j] += u[j];
+                    for (int i = 0; i < 16; ++i) v[j + i] += u[i];
                 }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive_leader(acc_empty + 8 * a);
+                acc_release(acc_empty + 8 * a, lane);
             }
             if (!ok) break;
             const unsigned row = mi * kBM + rank * 128 + quad * 32 + lane, col = ni * S::BN + half * S::kCols;
