@@ -2,12 +2,14 @@
 //
 //   C(m, n) = sum_k A(m, k) B(n, k),   A, B 16-bit, C float32 in tensor memory
 //
-// A pair of CTAs (a cluster of two, one per SM) computes a tile of 256 x BN: each CTA stages its own 128 rows of A
+// A pair of CTAs (a cluster of two, one per SM) computes a tile of 256 x 256: each CTA stages its own 128 rows of A
 // and its own half of B's rows with TMA, and one thread of the pair's first CTA issues the tcgen05.mma of both.
 // Per 64 values of k a CTA reads 32 KiB for 512 clocks of matrix work; a CTA working alone on 128 x 256 would read
 // 48 KiB for the same, more than L2 delivers to all SMs at once.  The kernel is persistent: pairs walk over the
-// tiles, one warp loads, one issues, eight read the finished accumulators, and with two (or four) accumulators in
-// tensor memory the products of the next tile run under the epilogue of the last.
+// tiles, one warp loads, one issues, eight read the finished accumulators, and with two accumulators in tensor memory the
+// products of the next tile run under the epilogue of the last.  Shared memory is the next limit: per 512 clocks a CTA
+// writes 32 KiB and its matrix unit reads 32 KiB, which is all of its 128 bytes a clock; a 256 x 128 tile would read
+// half as much again (and ran at three quarters of the rate).
 //
 // An operand may be stored with k contiguous ("K-major") or with its own dimension contiguous ("MN-major"): the
 // logits, dh and dw all read h, w and dz where they lie, without a transposed copy.
@@ -36,15 +38,16 @@ enum class Epi { kPart, kOut, kProb, kStat };
 constexpr unsigned kRound = 16;
 
 template <int PL> struct TcShape {
-    static constexpr int BN = PL == 1 ? 256 : 128;
-    static constexpr int kABytes = 128 * kBK * 2;       // one plane of one CTA's rows of A
-    static constexpr int kBBytes = BN / 2 * kBK * 2;    // one plane of one CTA's rows of B
-    static constexpr int kStageBytes = PL * (kABytes + kBBytes);
-    static constexpr int kStages = PL == 1 ? 6 : 3;
-    static constexpr int kAccs = 512 / BN;
-    static constexpr int kCols = BN / 2;  // columns of one epilogue thread
-    static constexpr int kSmem = kStages * kStageBytes + 1024 + 256;
+    static constexpr int kABytes = 128 * kBK * 2;  // one plane of one CTA's rows of A, and of its half of B's
+    static constexpr int kStageBytes = 2 * PL * kABytes;
+    static constexpr int kStages = PL == 1 ? 6 : 2;
 };
+constexpr int kBN = 256;
+constexpr int kAccs = 512 / kBN;
+constexpr int kCols = kBN / 2;        // columns of one epilogue thread
+constexpr int kWarpStage = 32 * 128;  // epilogue: 32 rows of 128 bytes per warp, on their way to memory
+constexpr int kTcSmem = 6 * 2 * 128 * kBK * 2 + kEpiWarps * kWarpStage + 1024;
+static_assert(TcShape<1>::kStages * TcShape<1>::kStageBytes == TcShape<3>::kStages * TcShape<3>::kStageBytes, "both fill 192 KiB");
 
 struct TcArgs {
     CUtensorMap a, b;
@@ -53,12 +56,15 @@ struct TcArgs {
     unsigned first, most;    // the piece's rows of the compacted list
     const unsigned *rows;    // rows that count (device)
     unsigned a_row0, b_row0; // where the piece starts in the row dimension of the tensor maps
-    unsigned splits;
+    unsigned splits;         // 1, or the launch's share of CTAs lets the kernel choose (pick_splits)
+    unsigned pairs;          // CTA pairs the GPU holds
+    unsigned most_splits;    // that fit the buffer of parts
+    int planes;
     int n_fast;              // tiles of one row of tiles run first (B is the smaller operand and stays in L2)
     int bf16;
     unsigned *error;
     // kPart
-    float *part;             // [splits][m][n]
+    float *part;             // [splits][m][n rounded up to 8]
     // kOut
     void *out;
     unsigned long long out_pitch;
@@ -207,16 +213,50 @@ __device__ __forceinline__ void acc_release(uint32_t bar, unsigned lane) {
     if (lane == 0) mbar_arrive_leader(bar);
 }
 
+// How many parts to cut the sum over k into.  In units of one pair's 64 values of k (0.28 us; six times that for planes):
+// a wave of tiles costs its length and about four for the exposed part of its epilogue; parts cost their way through
+// memory (6.5 TB/s) and the launch that joins them (about 3 us).
+__host__ __device__ inline float split_cost(unsigned s, unsigned long long tiles, unsigned kb, unsigned pairs, float out_bytes, int planes) {
+    const float unit = planes == 3 ? 1.7e-6f : 0.28e-6f;
+    const float waves = (float)((tiles * s + pairs - 1) / pairs);
+    const float cost = waves * ((float)((kb + s - 1) / s) + 4.f);
+    return s == 1 ? cost : cost * 1.03f + (3e-6f + out_bytes * (float)(2 * s) / 6.5e12f) / unit;
+}
+__host__ __device__ inline unsigned tiles_of(unsigned m, unsigned n) { return (unsigned)(((unsigned long long)m + kBM - 1) / kBM * (((unsigned long long)n + kBN - 1) / kBN)); }
+constexpr unsigned kMostSplits = 32;
+
+// The same choice for the rows that really take part, known on the device only: every lane of a warp rates one number.
+__device__ __forceinline__ unsigned pick_splits(const TcArgs &g, unsigned m, unsigned k) {
+    if (g.splits == 1) return 1;
+    const unsigned s = (threadIdx.x & 31) + 1, kb = (k + kBK - 1) / kBK;
+    float cost = s <= g.most_splits && s <= max(kb, 1u) ? split_cost(s, tiles_of(m, g.n), kb, g.pairs, (float)m * (float)g.n * 4.f, g.planes) : INFINITY;
+    unsigned best = s;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const float c = __shfl_xor_sync(0xffffffffu, cost, o);
+        const unsigned b = __shfl_xor_sync(0xffffffffu, best, o);
+        if (c < cost || (c == cost && b < best)) {
+            cost = c;
+            best = b;
+        }
+    }
+    return best;
+}
+__device__ __forceinline__ unsigned rows_of(const TcArgs &g) {
+    const unsigned rows = *g.rows;
+    return rows > g.first ? min(g.most, rows - g.first) : 0u;
+}
+
 struct TileWalk {
     unsigned m, k, mt, nt, total, kb, splits;
     int n_fast;
-    __device__ TileWalk(const TcArgs &g, int bn) {
-        const unsigned rows = *g.rows, mine = rows > g.first ? min(g.most, rows - g.first) : 0u;
+    __device__ explicit TileWalk(const TcArgs &g) {
+        const unsigned mine = rows_of(g);
         m = g.dyn == 0 ? mine : g.m;
         k = g.dyn == 1 ? mine : g.k;
         mt = (m + kBM - 1) / kBM;
-        nt = (g.n + bn - 1) / bn;
-        splits = g.splits;
+        nt = (g.n + kBN - 1) / kBN;
+        splits = pick_splits(g, m, k);
         total = mt * nt * splits;
         kb = (k + kBK - 1) / kBK;
         n_fast = g.n_fast;
@@ -237,143 +277,252 @@ struct TileWalk {
     }
 };
 
-template <int NC> __device__ __forceinline__ void epi_part(const TcArgs &g, const float (&v)[NC], unsigned m, unsigned row, unsigned col, unsigned s) {
-    if (row >= m) return;
-    float *p = g.part + ((unsigned long long)s * g.m + row) * g.n + col;
-    const bool vec = (g.n & 3u) == 0;
+// ---- Epilogue.  A thread of a warp holds 128 columns of one row.  They go to memory through 4 KiB of shared memory per
+// warp, 128 bytes of 32 rows at a time, so that a store of the warp writes whole lines: rows written straight from their
+// threads are 32 lines per store and took longer than the products of a tile with few values of k.  16-byte chunk c of
+// row r lies at chunk c ^ (r & 7): neither the rows' owners nor the readers of lines meet in a bank.
+union Chunk {
+    uint4 u;
+    float f[4];
+    __nv_bfloat16 b[8];
+    __half h[8];
+    unsigned short s[8];
+};
+__device__ __forceinline__ uint4 *stage_at(uint8_t *stage, unsigned row, unsigned chunk) {
+    return reinterpret_cast<uint4 *>(stage + row * 128 + ((chunk ^ (row & 7)) << 4));
+}
+template <typename F> __device__ __forceinline__ void stage_fill(uint8_t *stage, unsigned lane, F chunk) {
+    __syncwarp();
 #pragma unroll
-    for (int j = 0; j < NC; j += 4) {
-        if (vec) {
-            if (col + j < g.n) *reinterpret_cast<float4 *>(p + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-        } else {
+    for (int c = 0; c < 8; ++c) *stage_at(stage, lane, c) = chunk(c);
+    __syncwarp();
+}
+// Where the warp's rows go: `row` is this lane's row of C, `out` its row of the output.
+struct EpiRows {
+    unsigned m, row0;  // rows of C; first row of the warp
+    unsigned out;
+    __device__ __forceinline__ bool has(unsigned i) const { return row0 + i < m; }
+    __device__ __forceinline__ unsigned long long to(unsigned i) const { return __shfl_sync(0xffffffffu, out, i); }
+};
+
+__device__ __forceinline__ void epi_part(const TcArgs &g, const float (&v)[kCols], const EpiRows &rows, unsigned col0, unsigned s, uint8_t *stage, unsigned lane) {
+    const unsigned pitch = (g.n + 7) & ~7u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (col + j + i < g.n) p[j + i] = v[j + i];
+    for (int j = 0; j < kCols; j += 32) {
+        stage_fill(stage, lane, [&](int c) {
+            Chunk x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.f[i] = v[j + c * 4 + i];
+            return x.u;
+        });
+        const unsigned c = lane & 7, col = col0 + j + c * 4;
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const unsigned r = i + (lane >> 3);
+            const uint4 x = *stage_at(stage, r, c);
+            if (rows.has(r) && col < pitch)
+                *reinterpret_cast<uint4 *>(g.part + ((unsigned long long)s * g.m + rows.row0 + r) * pitch + col) = x;
         }
     }
 }
 
-// Eight neighbouring results of one row: to the float32 sums over pieces, or scaled and rounded once to the output.
-__device__ __forceinline__ void store_out8(const TcArgs &g, float (&x)[8], unsigned long long row, unsigned long long out_row, unsigned col, float f) {
+// Four neighbouring results of one row: to the float32 sums over pieces, or scaled and rounded once to the output.
+__device__ __forceinline__ void store_out4(const TcArgs &g, float4 v, unsigned long long row, unsigned long long out_row, unsigned col, float f) {
+    if (col >= g.n) return;
     const unsigned left = g.n - col;
+    float x[4] = {v.x, v.y, v.z, v.w};
     if (g.acc) {
         float *a = g.acc + row * g.acc_pitch + col;
-        const bool whole = g.acc_vec && left >= 8;
+        const bool whole = g.acc_vec && left >= 4;
         if (!g.acc_first) {
             if (whole) {
-                const float4 p = *reinterpret_cast<const float4 *>(a), q = *reinterpret_cast<const float4 *>(a + 4);
+                const float4 p = *reinterpret_cast<const float4 *>(a);
                 x[0] += p.x; x[1] += p.y; x[2] += p.z; x[3] += p.w;
-                x[4] += q.x; x[5] += q.y; x[6] += q.z; x[7] += q.w;
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 4; ++i)
                     if (i < left) x[i] += a[i];
             }
         }
         if (!g.acc_last) {
             if (whole) {
                 *reinterpret_cast<float4 *>(a) = make_float4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<float4 *>(a + 4) = make_float4(x[4], x[5], x[6], x[7]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 4; ++i)
                     if (i < left) a[i] = x[i];
             }
             return;
         }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= f;
-    const bool whole = g.out_vec && left >= 8;
+    for (int i = 0; i < 4; ++i) x[i] *= f;
+    const bool whole = g.out_vec && left >= 4;
     if (g.out_type == SCAR_F32) {
         float *o = static_cast<float *>(g.out) + out_row * g.out_pitch + col;
         if (whole) {
             *reinterpret_cast<float4 *>(o) = make_float4(x[0], x[1], x[2], x[3]);
-            *reinterpret_cast<float4 *>(o + 4) = make_float4(x[4], x[5], x[6], x[7]);
             return;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4; ++i)
             if (i < left) o[i] = x[i];
         return;
     }
-    union {
-        __nv_bfloat16 b[8];
-        __half h[8];
-        uint4 u;
-        unsigned short s[8];
-    } y;
-    if (g.out_type == SCAR_BF16) {
+    Chunk y;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y.b[i] = __float2bfloat16_rn(x[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y.h[i] = __float2half_rn(x[i]);
+    for (int i = 0; i < 4; ++i) {
+        if (g.out_type == SCAR_BF16) y.b[i] = __float2bfloat16_rn(x[i]);
+        else y.h[i] = __float2half_rn(x[i]);
     }
     unsigned short *o = static_cast<unsigned short *>(g.out) + out_row * g.out_pitch + col;
     if (whole) {
-        *reinterpret_cast<uint4 *>(o) = y.u;
+        *reinterpret_cast<uint2 *>(o) = make_uint2(y.u.x, y.u.y);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i)
         if (i < left) o[i] = y.s[i];
 }
 
-template <int NC> __device__ __forceinline__ void epi_out(const TcArgs &g, const float (&v)[NC], unsigned m, unsigned row, unsigned col, float f) {
-    if (row >= m) return;
-    const unsigned long long out_row = g.row_map ? g.row_map[g.first + row] : row;
+// Packed 16-bit rows of 64 columns from the stage to `base` (row pitch in elements), columns [0, left) of them.
+__device__ __forceinline__ void flush16(uint8_t *stage, unsigned short *base, unsigned long long pitch, bool vec, const EpiRows &rows, unsigned left, unsigned lane) {
+    if (vec) {
+        const unsigned c = lane & 7;
 #pragma unroll
-    for (int j = 0; j < NC; j += 8) {
-        if (col + j >= g.n) break;
-        float x[8];
+        for (int i = 0; i < 32; i += 4) {
+            const unsigned r = i + (lane >> 3);
+            const unsigned long long to = rows.to(r);
+            Chunk x;
+            x.u = *stage_at(stage, r, c);
+            if (!rows.has(r) || c * 8 >= left) continue;
+            unsigned short *o = base + to * pitch + c * 8;
+            if (c * 8 + 8 <= left) {
+                *reinterpret_cast<uint4 *>(o) = x.u;
+            } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = v[j + i];
-        store_out8(g, x, row, out_row, col + j, f);
+                for (int k = 0; k < 8; ++k)
+                    if (c * 8 + k < left) o[k] = x.s[k];
+            }
+        }
+        return;
+    }
+    // any row may begin between two 4-byte words: lane l then takes columns 2l + 1 and 2l + 2, and lane 0 the first one
+    const unsigned short *st = reinterpret_cast<const unsigned short *>(stage);
+    for (unsigned r = 0; r < 32; ++r) {
+        if (!rows.has(r)) break;
+        unsigned short *o = base + rows.to(r) * pitch;
+        const unsigned odd = (unsigned)((uintptr_t)o >> 1) & 1u, a = 2 * lane + odd, b = a + 1;
+        const unsigned short x = st[r * 64 + (((a >> 3) ^ (r & 7)) << 3) + (a & 7)];
+        const unsigned short y = b < 64 ? st[r * 64 + (((b >> 3) ^ (r & 7)) << 3) + (b & 7)] : (unsigned short)0;
+        if (b < 64 && b < left) *reinterpret_cast<unsigned *>(o + a) = (unsigned)x | (unsigned)y << 16;
+        else if (a < left) o[a] = x;
+        if (odd && lane == 0 && left) o[0] = st[r * 64 + ((r & 7) << 3)];
+    }
+}
+
+__device__ __forceinline__ void epi_out(const TcArgs &g, const float (&v)[kCols], const EpiRows &rows, unsigned col0, float f, uint8_t *stage, unsigned lane) {
+    if (g.out_type != SCAR_F32 && !g.acc) {
+#pragma unroll
+        for (int j = 0; j < kCols; j += 64) {
+            if (col0 + j >= g.n) break;
+            stage_fill(stage, lane, [&](int c) {
+                Chunk x;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (g.out_type == SCAR_BF16) x.b[i] = __float2bfloat16_rn(v[j + c * 8 + i] * f);
+                    else x.h[i] = __float2half_rn(v[j + c * 8 + i] * f);
+                }
+                return x.u;
+            });
+            flush16(stage, static_cast<unsigned short *>(g.out) + col0 + j, g.out_pitch, g.out_vec, rows, g.n - (col0 + j), lane);
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < kCols; j += 32) {
+        if (col0 + j >= g.n) break;
+        stage_fill(stage, lane, [&](int c) {
+            Chunk x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.f[i] = v[j + c * 4 + i];
+            return x.u;
+        });
+        if (g.out_type == SCAR_F32 && !g.out_vec) {  // a line per row, wherever it begins
+            const unsigned col = col0 + j + lane;
+            for (unsigned r = 0; r < 32 && rows.has(r); ++r) {
+                const unsigned long long to = rows.to(r);
+                float x = reinterpret_cast<const float *>(stage)[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
+                if (col >= g.n) continue;
+                float *o = static_cast<float *>(g.out) + to * g.out_pitch + col;  // acc, where there is one, is the output
+                if (g.acc && !g.acc_first) x += *o;
+                *o = g.acc && !g.acc_last ? x : x * f;
+            }
+        } else {
+            const unsigned c = lane & 7, col = col0 + j + c * 4;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const unsigned r = i + (lane >> 3);
+                const unsigned long long to = rows.to(r);
+                Chunk x;
+                x.u = *stage_at(stage, r, c);
+                if (rows.has(r)) store_out4(g, make_float4(x.f[0], x.f[1], x.f[2], x.f[3]), rows.row0 + r, to, col, f);
+            }
+        }
     }
 }
 
 // One row's 128 logits of this thread: their maximum, the sum of their exponentials relative to it, the label's logit,
 // and with STORE the exponentials themselves.  A group whose maximum is -inf is taken relative to 0 (all zeros).
-template <bool STORE, int NC>
-__device__ __forceinline__ void epi_prob(const TcArgs &g, float (&v)[NC], unsigned m, unsigned row, unsigned col, unsigned group) {
-    if (row >= m) return;
+template <bool STORE>
+__device__ __forceinline__ void epi_prob(const TcArgs &g, float (&v)[kCols], const EpiRows &rows, unsigned row, unsigned col, unsigned group, uint8_t *stage,
+                                         unsigned lane) {
     const unsigned left = g.n > col ? g.n - col : 0u;
-    if (left < NC) {
+    if (left < kCols) {
 #pragma unroll
-        for (int j = 0; j < NC; ++j)
+        for (int j = 0; j < kCols; ++j)
             if (j >= left) v[j] = -INFINITY;
     }
-    const unsigned at = (unsigned)g.label[g.first + row] - col;
-    if (at < NC) {
+    const bool mine = row < rows.m;
+    const unsigned at = mine ? (unsigned)g.label[g.first + row] - col : 0xffffffffu;
+    if (at < kCols) {
         float z = 0.f;
 #pragma unroll
-        for (int j = 0; j < NC; ++j) z = j == at ? v[j] : z;
+        for (int j = 0; j < kCols; ++j) z = j == at ? v[j] : z;
         g.label_z[g.first + row] = z;
     }
     float top = v[0];
 #pragma unroll
-    for (int j = 1; j < NC; ++j) top = fmaxf(top, v[j]);
+    for (int j = 1; j < kCols; ++j) top = fmaxf(top, v[j]);
     const float ref = top == -INFINITY ? 0.f : top;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    __half *p = STORE ? g.prob + (unsigned long long)row * g.prob_pitch + col : nullptr;
 #pragma unroll
-    for (int j = 0; j < NC; j += 8) {
-        union {
-            __half2 h[4];
-            uint4 u;
-        } y;
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            // the difference first: it is small where the exponential is not, and so is its rounding
-            const float e0 = ex2(fmaf(v[j + i] - ref, kLog2e, kProbLog2));
-            const float e1 = ex2(fmaf(v[j + i + 1] - ref, kLog2e, kProbLog2));
-            s[(i >> 1) & 3] += e0 + e1;
-            if (STORE) y.h[i >> 1] = __floats2half2_rn(e0, e1);
-        }
-        if (STORE && j < left) *reinterpret_cast<uint4 *>(p + j) = y.u;
+    for (int j = 0; j < kCols; ++j) {
+        // the difference first: it is small where the exponential is not, and so is its rounding
+        v[j] = ex2(fmaf(v[j] - ref, kLog2e, kProbLog2));
+        s[j & 3] += v[j];
     }
-    g.stat[(unsigned long long)row * g.stat_pitch + group] = make_float2(ref, (s[0] + s[1]) + (s[2] + s[3]));
+    if (mine) g.stat[(unsigned long long)row * g.stat_pitch + group] = make_float2(ref, (s[0] + s[1]) + (s[2] + s[3]));
+    if constexpr (!STORE) return;
+    else
+#pragma unroll
+    for (int j = 0; j < kCols; j += 64) {
+        if (j >= left) break;
+        stage_fill(stage, lane, [&](int c) {
+            Chunk x;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x.h[i] = __float2half_rn(v[j + c * 8 + i]);
+            return x.u;
+        });
+        const unsigned c = lane & 7;
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const unsigned r = i + (lane >> 3);
+            const uint4 x = *stage_at(stage, r, c);
+            if (rows.has(r) && j + c * 8 < left)  // the pitch is a multiple of 8
+                *reinterpret_cast<uint4 *>(g.prob + (unsigned long long)(rows.row0 + r) * g.prob_pitch + col + j + c * 8) = x;
+        }
+    }
 }
 
 template <int PL, bool A_MN, bool B_MN, Epi EPI>
@@ -382,23 +531,24 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
     using S = TcShape<PL>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ __align__(8) unsigned long long bars[2 * S::kStages + 2 * S::kAccs];
+    __shared__ __align__(8) unsigned long long bars[2 * S::kStages + 2 * kAccs];
     __shared__ uint32_t tmem_base;
     constexpr bool kLogits = EPI == Epi::kProb || EPI == Epi::kStat;
     constexpr unsigned kPer = PL == 3 ? 1u : kLogits ? kRound : 0xffffffffu;  // stages per accumulator
     const uint32_t stage0 = smem_addr(smem);
     const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages;
-    const uint32_t acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 8 * S::kAccs;
+    const uint32_t acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 8 * kAccs;
     const unsigned warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const unsigned pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
         }
-        for (int i = 0; i < S::kAccs; ++i) {
+        for (int i = 0; i < kAccs; ++i) {
             mbar_init(acc_full + 8 * i, 1);
             mbar_init(acc_empty + 8 * i, 2 * kEpiWarps);
         }
@@ -413,7 +563,8 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
     cluster_sync_all();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_base;
-    const TileWalk walk(g, S::BN);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const TileWalk walk(g);
     bool ok = true;
 
     if (warp == kEpiWarps) {  // loads
@@ -421,7 +572,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
         for (unsigned t = pair; t < walk.total && ok; t += pairs) {
             unsigned mi, ni, s, k0, k1;
             walk.at(t, mi, ni, s, k0, k1);
-            const int am = (int)(mi * kBM + rank * 128), bn = (int)(ni * S::BN + rank * (S::BN / 2));
+            const int am = (int)(mi * kBM + rank * 128), bn = (int)(ni * kBN + rank * (kBN / 2));
             for (unsigned kb = k0; kb < k1; ++kb) {
                 ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * st, ph ^ 1, g.error));
                 if (!ok) break;
@@ -431,7 +582,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                     const int kk = (int)(kb * kBK);
 #pragma unroll
                     for (int p = 0; p < PL; ++p) {
-                        const uint32_t da = dst + p * S::kABytes, db = dst + PL * S::kABytes + p * S::kBBytes;
+                        const uint32_t da = dst + p * S::kABytes, db = dst + PL * S::kABytes + p * S::kABytes;
                         if (A_MN) {
                             tma_load(da, &g.a, bar, am, (int)g.a_row0 + kk, p);
                             tma_load(da + 8192, &g.a, bar, am + 64, (int)g.a_row0 + kk, p);
@@ -440,7 +591,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                         }
                         if (B_MN) {
                             tma_load(db, &g.b, bar, bn, (int)g.b_row0 + kk, p);
-                            if (S::BN == 256) tma_load(db + 8192, &g.b, bar, bn + 64, (int)g.b_row0 + kk, p);
+                            tma_load(db + 8192, &g.b, bar, bn + 64, (int)g.b_row0 + kk, p);
                         } else {
                             tma_load(db, &g.b, bar, kk, (int)g.b_row0 + bn, p);
                         }
@@ -457,7 +608,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
         if (rank == 0) {
             const uint32_t type = g.bf16 ? 1u : 0u;
             const uint32_t idesc = 1u << 4 | type << 7 | type << 10 | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
-                                   (uint32_t)(S::BN >> 3) << 17 | (uint32_t)(kBM >> 4) << 24;
+                                   (uint32_t)(kBN >> 3) << 17 | (uint32_t)(kBM >> 4) << 24;
             const uint64_t desc_a = smem_desc<A_MN>(stage0), desc_b = smem_desc<B_MN>(stage0 + PL * S::kABytes);
             unsigned st = 0, ph = 0, ac = 0, aph = 1;
             for (unsigned t = pair; t < walk.total && ok; t += pairs) {
@@ -474,7 +625,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                     ok = __all_sync(0xffffffffu, mbar_wait(full + 8 * st, ph, g.error));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t d = tmem + ac * S::BN;
+                    const uint32_t d = tmem + ac * kBN;
                     --left;
                     if (elect_one()) {
                         constexpr int kPairs = PL == 1 ? 1 : 6;
@@ -482,7 +633,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
 #pragma unroll
                         for (int q = 0; q < kPairs; ++q) {
                             const uint64_t da = desc_a + ((st * S::kStageBytes + pa[q] * S::kABytes) >> 4);
-                            const uint64_t db = desc_b + ((st * S::kStageBytes + pb[q] * S::kBBytes) >> 4);
+                            const uint64_t db = desc_b + ((st * S::kStageBytes + pb[q] * S::kABytes) >> 4);
 #pragma unroll
                             for (int k = 0; k < kBK / 16; ++k)
                                 mma_pair(d, da + (k * k_step_bytes<A_MN>() >> 4), db + (k * k_step_bytes<B_MN>() >> 4), idesc,
@@ -496,47 +647,48 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                         st = 0;
                         ph ^= 1;
                     }
-                    if (left == 0 && ++ac == S::kAccs) {
+                    if (left == 0 && ++ac == kAccs) {
                         ac = 0;
                         aph ^= 1;
                     }
                 }
             }
         }
-    } else {  // epilogue
+    } else if (warp < kEpiWarps) {  // epilogue
         const unsigned quad = warp & 3, half = warp >> 2;
+        uint8_t *stage = smem + S::kStages * S::kStageBytes + warp * kWarpStage;
         const float f = EPI == Epi::kOut ? (g.mean ? g.scale / (float)max(*g.rows, 1u) : g.scale) : 0.f;
         unsigned ac = 0;
         for (unsigned t = pair; t < walk.total && ok; t += pairs) {
             unsigned mi, ni, s, k0, k1;
             walk.at(t, mi, ni, s, k0, k1);
-            float v[S::kCols];
+            float v[kCols];
             const unsigned rounds = k1 > k0 ? (k1 - k0 - 1) / kPer + 1 : 0u;
             if (rounds == 0) {
 #pragma unroll
-                for (int j = 0; j < S::kCols; ++j) v[j] = 0.f;
+                for (int j = 0; j < kCols; ++j) v[j] = 0.f;
             }
             // the first round is the tile's accumulator itself, later ones are added to it
             if (rounds) {
-                const unsigned a = ac % S::kAccs;
-                ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, (ac / S::kAccs) & 1, g.error));
+                const unsigned a = ac % kAccs;
+                ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, (ac / kAccs) & 1, g.error));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t src = tmem + a * S::BN + half * S::kCols + (quad * 32u << 16);
+                const uint32_t src = tmem + a * kBN + half * kCols + (quad * 32u << 16);
 #pragma unroll
-                for (int j = 0; j < S::kCols; j += 32) tmem_load32(src + j, v + j);
+                for (int j = 0; j < kCols; j += 32) tmem_load32(src + j, v + j);
                 tmem_loaded(v);
                 acc_release(acc_empty + 8 * a, lane);
                 ++ac;
             }
             for (unsigned r = 1; r < rounds; ++r, ++ac) {
-                const unsigned a = ac % S::kAccs;
-                ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, (ac / S::kAccs) & 1, g.error));
+                const unsigned a = ac % kAccs;
+                ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, (ac / kAccs) & 1, g.error));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t src = tmem + a * S::BN + half * S::kCols + (quad * 32u << 16);
+                const uint32_t src = tmem + a * kBN + half * kCols + (quad * 32u << 16);
 #pragma unroll
-                for (int j = 0; j < S::kCols; j += 16) {  // 16 at a time: 128 sums and 32 more registers do not fit
+                for (int j = 0; j < kCols; j += 16) {  // 16 at a time: 128 sums and 32 more registers do not fit
                     float u[16];
                     tmem_load16(src + j, u);
                     tmem_loaded(u);
@@ -546,10 +698,12 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                 acc_release(acc_empty + 8 * a, lane);
             }
             if (!ok) break;
-            const unsigned row = mi * kBM + rank * 128 + quad * 32 + lane, col = ni * S::BN + half * S::kCols;
-            if (EPI == Epi::kPart) epi_part(g, v, walk.m, row, col, s);
-            else if (EPI == Epi::kOut) epi_out(g, v, walk.m, row, col, f);
-            else epi_prob<EPI == Epi::kProb>(g, v, walk.m, row, col, 2 * ni + half);
+            const unsigned row0 = mi * kBM + rank * 128 + quad * 32, row = row0 + lane, col = ni * kBN + half * kCols;
+            EpiRows rows{walk.m, row0, row};
+            if (EPI == Epi::kOut && g.row_map && row < walk.m) rows.out = g.row_map[g.first + row];
+            if (EPI == Epi::kPart) epi_part(g, v, rows, col, s, stage, lane);
+            else if (EPI == Epi::kOut) epi_out(g, v, rows, col, f, stage, lane);
+            else epi_prob<EPI == Epi::kProb>(g, v, rows, row, col, 2 * ni + half, stage, lane);
         }
     }
     if (!ok) {  // let copies and instructions in flight end before the memory they use is given back

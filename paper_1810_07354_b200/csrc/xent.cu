@@ -28,6 +28,12 @@ struct XentRecord {
     unsigned error;
 };
 
+// Every kernel of a call is launched while the one before it may still run; nothing is touched before that one is done.
+__device__ __forceinline__ void griddep_start() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Compacts the rows that count, in order: row_of[0 .. rows) are their numbers, pos is the inverse (kNone for the rest).
 // One CTA: the labels of a step are few.
 __global__ void __launch_bounds__(kRowThreads)
@@ -35,6 +41,7 @@ k_xent_rows(const long long *__restrict__ labels, unsigned n, long long ignore, 
             unsigned *__restrict__ row_of, unsigned *__restrict__ pos, int *__restrict__ label, float *__restrict__ row_loss,
             XentRecord *rec) {
     __shared__ unsigned sh[kRowThreads / 32], base, n_ign, n_bad;
+    griddep_start();
     if (threadIdx.x == 0) base = n_ign = n_bad = 0;
     __syncthreads();
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -111,6 +118,7 @@ __global__ void __launch_bounds__(256)
 k_xent_place(const T *__restrict__ src, unsigned long long pitch, unsigned n, unsigned d, unsigned dp, bool vec,
              unsigned short *__restrict__ dst, unsigned long long plane, const unsigned *__restrict__ pos,
              const unsigned *__restrict__ rows, T *__restrict__ zero, unsigned long long zero_pitch) {
+    griddep_start();
     const unsigned groups = dp / 8;
     const unsigned long long total = (unsigned long long)(n + (pos ? 64u : 0u)) * groups;
     for (unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 256) {
@@ -204,6 +212,7 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
           const float *__restrict__ label_z, const unsigned *__restrict__ row_of, const XentRecord *__restrict__ rec, Piece p,
           float *__restrict__ row_loss) {
     __shared__ float sh[8];
+    griddep_start();
     const unsigned r = blockIdx.x, R = p.rows(rec);
     unsigned short *row = GRAD ? o.dz + (unsigned long long)r * o.pitch : nullptr;
     if (r >= R) {
@@ -248,14 +257,14 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
     }
 }
 
-// The same from float32 logits of the piece in `splits` parts (their sum replaces the first part).
+// The same from float32 logits of the piece in parts (their sum replaces the first part): one pass for the running
+// maximum and sum of every thread, one for dz.
 template <bool GRAD>
 __global__ void __launch_bounds__(256)
-k_xent_softmax(float *__restrict__ part, unsigned splits, unsigned long long part_stride, DzOut o, unsigned V,
-               const int *__restrict__ label, const unsigned *__restrict__ row_of, const XentRecord *__restrict__ rec, Piece p,
-               float *__restrict__ row_loss) {
+k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict__ label, const unsigned *__restrict__ row_of, float *__restrict__ row_loss) {
     __shared__ float sh[8];
-    const unsigned r = blockIdx.x, R = p.rows(rec);
+    griddep_start();
+    const unsigned r = blockIdx.x, R = rows_of(g), V = g.n, pitch = (V + 7) & ~7u;
     unsigned short *row = GRAD ? o.dz + (unsigned long long)r * o.pitch : nullptr;
     const int planes = o.dt == SCAR_F32 ? 3 : 1;
     if (r >= R) {
@@ -265,71 +274,81 @@ k_xent_softmax(float *__restrict__ part, unsigned splits, unsigned long long par
                     *reinterpret_cast<uint4 *>(row + q * o.plane + v) = make_uint4(0, 0, 0, 0);
         return;
     }
-    float *z = part + (unsigned long long)r * V;
-    float top = -INFINITY;
-    for (unsigned v = threadIdx.x; v < V; v += 256) {
-        float x = z[v];
-        for (unsigned q = 1; q < splits; ++q) x += z[q * part_stride + v];
-        if (splits > 1) z[v] = x;
-        top = fmaxf(top, x);
+    const unsigned splits = pick_splits(g, R, g.k);
+    const unsigned long long stride = (unsigned long long)g.m * pitch;
+    float *z = g.part + (unsigned long long)r * pitch;
+    float top = -INFINITY, s = 0.f;
+    for (unsigned v = threadIdx.x * 4; v < V; v += 256 * 4) {
+        float4 a = *reinterpret_cast<const float4 *>(z + v);
+        if (splits > 1) {
+#pragma unroll 4
+            for (unsigned q = 1; q < splits; ++q) {
+                const float4 b = *reinterpret_cast<const float4 *>(z + q * stride + v);
+                a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+            }
+            *reinterpret_cast<float4 *>(z + v) = a;
+        }
+        const float x[4] = {a.x, v + 1 < V ? a.y : -INFINITY, v + 2 < V ? a.z : -INFINITY, v + 3 < V ? a.w : -INFINITY};
+        const float t = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        if (t > top) {
+            s *= expf(top - t);
+            top = t;
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s += expf(x[i] - ref);
     }
-    top = cta_max(top, sh);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float s = 0.f;
-    for (unsigned v = threadIdx.x; v < V; v += 256) s += expf(z[v] - ref);
-    s = cta_add(s, sh);
+    const float all = cta_max(top, sh);
+    const float ref = all == -INFINITY ? 0.f : all;
+    s = cta_add(s != 0.f ? s * expf((top == -INFINITY ? 0.f : top) - ref) : 0.f, sh);
     const float lse = ref + logf(s);
-    const unsigned y = (unsigned)label[p.first + r];
+    const unsigned y = (unsigned)label[g.first + r];
     const float zl = z[y];
-    if (threadIdx.x == 0) row_loss[row_of[p.first + r]] = lse - zl;
+    if (threadIdx.x == 0) row_loss[row_of[g.first + r]] = lse - zl;
     if (!GRAD) return;
     const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
     for (unsigned v = threadIdx.x * 8; v < V; v += 256 * 8) {
-        Eight x[3];
+        const float4 a = *reinterpret_cast<const float4 *>(z + v), b = *reinterpret_cast<const float4 *>(z + v + 4);
+        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        Eight w[3];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float w = 0.f;
-            if (v + j < V) w = (v + j == y ? expm1f(zl - lse) : expf(z[v + j] - lse)) * held;
-            if (o.dt == SCAR_F32) split3(w, x[0].b[j], x[1].b[j], x[2].b[j]);
-            else if (o.dt == SCAR_F16) x[0].h[j] = __float2half_rn(w);
-            else x[0].b[j] = __float2bfloat16_rn(w);
+            float d = 0.f;
+            if (v + j < V) d = (v + j == y ? expm1f(zl - lse) : expf(x[j] - lse)) * held;
+            if (o.dt == SCAR_F32) split3(d, w[0].b[j], w[1].b[j], w[2].b[j]);
+            else if (o.dt == SCAR_F16) w[0].h[j] = __float2half_rn(d);
+            else w[0].b[j] = __float2bfloat16_rn(d);
         }
-        for (int q = 0; q < planes; ++q) *reinterpret_cast<uint4 *>(row + q * o.plane + v) = x[q].u;
+        for (int q = 0; q < planes; ++q) *reinterpret_cast<uint4 *>(row + q * o.plane + v) = w[q].u;
     }
 }
 
 // Adds the parts of a split product and does what the product's own epilogue does without a split.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(128)
 k_xent_combine(const __grid_constant__ TcArgs g) {
-    const unsigned rows = *g.rows, mine = rows > g.first ? min(g.most, rows - g.first) : 0u;
-    const unsigned m = g.dyn == 0 ? mine : g.m;
-    const unsigned groups = (g.n + 7) / 8;
-    const float f = g.mean ? g.scale / (float)max(rows, 1u) : g.scale;
-    const unsigned long long stride = (unsigned long long)g.m * g.n, total = (unsigned long long)m * groups;
-    const bool vec = (g.n & 3u) == 0;
-    for (unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 256) {
+    griddep_start();
+    const unsigned mine = rows_of(g), m = g.dyn == 0 ? mine : g.m, k = g.dyn == 1 ? mine : g.k;
+    const unsigned groups = (g.n + 3) / 4, pitch = (g.n + 7) & ~7u, splits = pick_splits(g, m, k);
+    const float f = g.mean ? g.scale / (float)max(*g.rows, 1u) : g.scale;
+    const unsigned long long stride = (unsigned long long)g.m * pitch, total = (unsigned long long)m * groups;
+    for (unsigned long long i = (unsigned long long)blockIdx.x * 128 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 128) {
         const unsigned row = total >> 32 ? (unsigned)(i / groups) : (unsigned)i / groups;
-        const unsigned col = (unsigned)(i - (unsigned long long)row * groups) * 8;
-        const float *p = g.part + (unsigned long long)row * g.n + col;
-        float x[8] = {};
-        for (unsigned s = 0; s < g.splits; ++s, p += stride) {
-            if (vec && col + 8 <= g.n) {
-                const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
-                x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (col + j < g.n) x[j] += p[j];
-            }
+        const unsigned col = (unsigned)(i - (unsigned long long)row * groups) * 4;
+        const float *p = g.part + (unsigned long long)row * pitch + col;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (unsigned s = 0; s < splits; ++s) {
+            const float4 a = *reinterpret_cast<const float4 *>(p + s * stride);
+            x.x += a.x; x.y += a.y; x.z += a.z; x.w += a.w;
         }
-        store_out8(g, x, row, g.row_map ? g.row_map[g.first + row] : row, col, f);
+        store_out4(g, x, row, g.row_map ? g.row_map[g.first + row] : row, col, f);
     }
 }
 
 __global__ void __launch_bounds__(kRowThreads)
 k_xent_loss(const float *__restrict__ row_loss, unsigned n, bool mean, XentRecord *rec, float *d_loss) {
     __shared__ double sh[32];
+    griddep_start();
     double s = 0.0;
     for (unsigned t = threadIdx.x; t < n; t += kRowThreads) s += row_loss[t];
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -379,7 +398,7 @@ struct scar_xent {
     std::vector<void *> owned;
     uint64_t bytes = 0;
     uint64_t launches = 0;
-    bool ran = false;
+    bool ran = false, failed = false;
 };
 
 namespace {
@@ -421,38 +440,49 @@ int make_map(const scar_xent *op, CUtensorMap *map, const Operand &x, unsigned b
     return rc == CUDA_SUCCESS ? SCAR_OK : SCAR_ERR_CUDA;
 }
 
-// How many parts to cut the sum over k into.  In units of one pair's 64 values of k: a wave of tiles costs its length
-// and about four for the exposed part of its epilogue; parts cost their way through memory and the launch that joins
-// them (about 12 units, and 6.5 TB/s).
-unsigned choose_splits(const scar_xent *op, uint64_t m, uint64_t n, uint64_t k, int bn, uint64_t part_bytes) {
-    const double unit_s = 0.28e-6 * (op->planes == 3 ? 3 : 1);
-    const uint64_t tiles = ((m + kBM - 1) / kBM) * ((n + bn - 1) / bn), kb = (k + kBK - 1) / kBK;
-    double best = 0;
-    unsigned got = 1;
-    for (unsigned s = 1; s <= 32 && s <= kb; ++s) {
-        if (s > 1 && (m * n * 4 * s > part_bytes || tiles * s > 4ull * op->pairs)) break;
-        const double waves = (double)((tiles * s + op->pairs - 1) / op->pairs);
-        double cost = waves * ((double)((kb + s - 1) / s) + 4);
-        if (s > 1) cost += 12 + (double)m * n * 4 * (2 * s) / 6.5e12 / unit_s;
-        if (s == 1 || cost < best * 0.97) {
+// Launches a kernel of the call's chain: it may start while the one before it still runs (griddep_start waits for it).
+template <typename... P, typename... A> void launch(scar_xent *op, void (*kernel)(P...), unsigned grid, unsigned threads, unsigned smem, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = threads;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = op->stream;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess) op->launches++;
+    else op->failed = true;
+}
+
+// Sets the product's `splits`: 1, or more than 1 where cutting the sum over k pays for all the rows the call has.
+void choose_splits(const scar_xent *op, TcArgs &g) {
+    const uint64_t part = (uint64_t)g.m * round_up(g.n, 8) * 4;
+    g.pairs = op->pairs;
+    g.planes = op->planes;
+    g.most_splits = (unsigned)std::min<uint64_t>(kMostSplits, std::max<uint64_t>(1, part ? op->part_bytes / part : 1));
+    g.splits = 1;
+    const unsigned kb = (g.k + kBK - 1) / kBK;
+    const uint64_t tiles = (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + kBN - 1) / kBN);
+    float best = split_cost(1, tiles, kb, op->pairs, 0.f, op->planes);
+    for (unsigned s = 2; s <= g.most_splits && s <= kb; ++s) {
+        const float cost = split_cost(s, tiles, kb, op->pairs, (float)g.m * (float)g.n * 4.f, op->planes);
+        if (cost < best) {
             best = cost;
-            got = s;
+            g.splits = s;
         }
     }
-    return got;
 }
 
 template <int PL, bool A_MN, bool B_MN, Epi EPI> void launch_tc(scar_xent *op, const TcArgs &g) {
-    using S = TcShape<PL>;
-    const uint64_t tiles = (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + S::BN - 1) / S::BN) * g.splits;
+    const uint64_t tiles = (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + kBN - 1) / kBN) * (g.splits > 1 ? g.most_splits : 1);
     const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, op->pairs);
-    if (!pairs) return;
-    k_tc_gemm<PL, A_MN, B_MN, EPI><<<2 * pairs, kGemmThreads, S::kSmem, op->stream>>>(g);
-    op->launches++;
+    if (pairs) launch(op, k_tc_gemm<PL, A_MN, B_MN, EPI>, 2 * pairs, kGemmThreads, kTcSmem, g);
 }
 
 template <int PL, bool A_MN, bool B_MN, Epi EPI> bool allow_smem() {
-    return cudaFuncSetAttribute(k_tc_gemm<PL, A_MN, B_MN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<PL>::kSmem) == cudaSuccess;
+    return cudaFuncSetAttribute(k_tc_gemm<PL, A_MN, B_MN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) == cudaSuccess;
 }
 template <int PL> bool allow_smem_all() {
     return allow_smem<PL, false, false, Epi::kPart>() && allow_smem<PL, false, true, Epi::kPart>() && allow_smem<PL, true, true, Epi::kPart>() &&
@@ -461,26 +491,23 @@ template <int PL> bool allow_smem_all() {
 
 // A product that ends in an output, split over k or not.
 template <int PL, bool A_MN> void launch_out(scar_xent *op, TcArgs g) {
-    g.splits = choose_splits(op, g.m, g.n, g.k, TcShape<PL>::BN, op->part_bytes);
+    choose_splits(op, g);
     if (g.splits == 1) {
         launch_tc<PL, A_MN, true, Epi::kOut>(op, g);
         return;
     }
     launch_tc<PL, A_MN, true, Epi::kPart>(op, g);
-    const uint64_t todo = (uint64_t)g.m * ((g.n + 7) / 8);
-    k_xent_combine<<<(unsigned)std::min<uint64_t>((todo + 255) / 256, 16 * op->pairs), 256, 0, op->stream>>>(g);
-    op->launches++;
+    const uint64_t todo = (uint64_t)g.m * ((g.n + 3) / 4);
+    launch(op, k_xent_combine, (unsigned)std::min<uint64_t>((todo + 127) / 128, 32 * op->pairs), 128, 0, g);
 }
 
 template <typename T>
 int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, const int64_t *labels, unsigned n, bool grad, float scale,
              float *row_loss, float *d_loss, T *dh, uint64_t dhp, T *dw, uint64_t dwp) {
     constexpr int PL = sizeof(T) == 4 ? 3 : 1;
-    using S = TcShape<PL>;
     const unsigned V = (unsigned)op->cfg.n_classes, D = (unsigned)op->cfg.dim;
     const bool mean = op->cfg.reduction == SCAR_MEAN;
     const long long *y = reinterpret_cast<const long long *>(labels);
-    cudaStream_t s = op->stream;
     int rc;
     if (!row_loss) row_loss = op->row_loss;
 
@@ -491,22 +518,18 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
     const Operand ow = w_copied ? Operand{op->w, D, V, op->dp, PL, (uint64_t)V * op->dp} : Operand{w, D, V, wp, 1, (uint64_t)V * wp};
     const Operand oz{op->dz, V, op->piece, op->vp, PL, (uint64_t)op->piece * op->vp};
     TcArgs logits{}, dhg{}, dwg{};
-    if ((rc = make_map(op, &logits.a, oh, 128)) != SCAR_OK || (rc = make_map(op, &logits.b, ow, S::BN / 2)) != SCAR_OK) return rc;
+    if ((rc = make_map(op, &logits.a, oh, 128)) != SCAR_OK || (rc = make_map(op, &logits.b, ow, kBN / 2)) != SCAR_OK) return rc;
     if (grad && ((rc = make_map(op, &dhg.a, oz, 128)) != SCAR_OK || (rc = make_map(op, &dhg.b, ow, 64)) != SCAR_OK ||
                  (rc = make_map(op, &dwg.a, oz, 64)) != SCAR_OK || (rc = make_map(op, &dwg.b, oh, 64)) != SCAR_OK))
         return rc;
 
-    k_xent_rows<<<1, kRowThreads, 0, s>>>(y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec);
+    launch(op, k_xent_rows, 1, kRowThreads, 0, y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec);
     const unsigned most_ctas = 16 * op->pairs;
     auto ctas = [&](uint64_t rows) { return (unsigned)std::min<uint64_t>((rows * (op->dp / 8) + 255) / 256, most_ctas); };
-    k_xent_place<T><<<ctas(n + 64), 256, 0, s>>>(h, hp, n, D, (unsigned)op->dp, rows_aligned(h, hp, sizeof(T)), op->h, oh.plane, op->pos,
-                                                 &op->rec->rows, grad ? dh : nullptr, dhp);
-    op->launches += 2;
-    if (w_copied) {
-        k_xent_place<T><<<ctas(V), 256, 0, s>>>(w, wp, V, D, (unsigned)op->dp, rows_aligned(w, wp, sizeof(T)), op->w, ow.plane, nullptr, nullptr,
-                                                nullptr, 0);
-        op->launches++;
-    }
+    launch(op, k_xent_place<T>, ctas(n + 64), 256, 0, h, hp, n, D, (unsigned)op->dp, rows_aligned(h, hp, sizeof(T)), op->h, oh.plane, op->pos, &op->rec->rows,
+           grad ? dh : nullptr, dhp);
+    if (w_copied)
+        launch(op, k_xent_place<T>, ctas(V), 256, 0, w, wp, V, D, (unsigned)op->dp, rows_aligned(w, wp, sizeof(T)), op->w, ow.plane, nullptr, nullptr, nullptr, 0);
 
     TcArgs base{};
     base.rows = &op->rec->rows;
@@ -543,23 +566,20 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
             logits.stat_pitch = op->groups;
             logits.label = op->label;
             logits.label_z = op->label_z;
-            logits.splits = choose_splits(op, rows, V, D, S::BN, op->part_bytes);
+            choose_splits(op, logits);
             if (PL == 3 || logits.splits > 1) {
                 launch_tc<PL, false, false, Epi::kPart>(op, logits);
-                if (grad)
-                    k_xent_softmax<true><<<rows64, 256, 0, s>>>(op->part, logits.splits, (uint64_t)rows * V, dz, V, op->label, op->row_of, op->rec, p,
-                                                                row_loss);
-                else
-                    k_xent_softmax<false><<<rows64, 256, 0, s>>>(op->part, logits.splits, (uint64_t)rows * V, dz, V, op->label, op->row_of, op->rec, p,
-                                                                 row_loss);
-            } else if (grad) {
-                if constexpr (PL == 1) launch_tc<1, false, false, Epi::kProb>(op, logits);
-                k_xent_dz<true><<<rows64, 256, 0, s>>>(dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, op->rec, p, row_loss);
-            } else {
-                if constexpr (PL == 1) launch_tc<1, false, false, Epi::kStat>(op, logits);
-                k_xent_dz<false><<<rows, 256, 0, s>>>(dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, op->rec, p, row_loss);
+                if (grad) launch(op, k_xent_softmax<true>, rows64, 256, 0, logits, dz, op->label, op->row_of, row_loss);
+                else launch(op, k_xent_softmax<false>, rows, 256, 0, logits, dz, op->label, op->row_of, row_loss);
+            } else if constexpr (PL == 1) {
+                if (grad) {
+                    launch_tc<1, false, false, Epi::kProb>(op, logits);
+                    launch(op, k_xent_dz<true>, rows64, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, op->rec, p, row_loss);
+                } else {
+                    launch_tc<1, false, false, Epi::kStat>(op, logits);
+                    launch(op, k_xent_dz<false>, rows, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, op->rec, p, row_loss);
+                }
             }
-            op->launches++;
         }
         if (!grad) continue;
         if (rows) {
@@ -577,16 +597,20 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
         dwg.out_vec = rows_aligned(dw, dwp, sizeof(T));
         if (n > op->piece) {  // several pieces: their sums in float32, in dw itself when it is float32
             dwg.acc = PL == 3 ? reinterpret_cast<float *>(dw) : op->acc;
-            dwg.acc_pitch = PL == 3 ? dwp : D;
-            dwg.acc_vec = PL == 3 ? dwg.out_vec : D % 4 == 0;
+            dwg.acc_pitch = PL == 3 ? dwp : op->dp;
+            dwg.acc_vec = PL == 3 ? dwg.out_vec : 1;
             dwg.acc_first = at == 0;
             dwg.acc_last = at + (uint64_t)op->piece >= n;
         }
         launch_out<PL, true>(op, dwg);
         if ((uint64_t)at + op->piece >= n) break;
     }
-    k_xent_loss<<<1, kRowThreads, 0, s>>>(row_loss, n, mean, op->rec, d_loss);
-    op->launches++;
+    launch(op, k_xent_loss, 1, kRowThreads, 0, row_loss, n, mean, op->rec, d_loss);
+    if (op->failed) {
+        op->failed = false;
+        cudaGetLastError();
+        return SCAR_ERR_CUDA;
+    }
     return SCAR_OK;
 }
 
@@ -631,14 +655,14 @@ int size_workspaces(scar_xent *op) {
         return rc;
     if (!f32 && (rc = xent_alloc(op, &op->stat, 8ull * op->groups * op->piece)) != SCAR_OK) return rc;
     if (grad && (rc = xent_alloc(op, &op->dz, op->planes * (uint64_t)op->piece * op->vp * 2)) != SCAR_OK) return rc;
-    if (grad && !f32 && op->piece < T && (rc = xent_alloc(op, &op->acc, V * D * 4)) != SCAR_OK) return rc;
+    if (grad && !f32 && op->piece < T && (rc = xent_alloc(op, &op->acc, V * op->dp * 4)) != SCAR_OK) return rc;
     if ((f32 || D % 8) && (rc = xent_alloc(op, &op->w, op->planes * V * op->dp * 2)) != SCAR_OK) return rc;
     // parts of split products: as many as choose_splits may ask for, up to 64 MiB
     const uint64_t P = std::min<uint64_t>(op->piece, T);
-    uint64_t most = P * V;
-    if (grad) most = std::max(most, std::max(P * D, V * D));
+    uint64_t most = P * op->vp;
+    if (grad) most = std::max(most, std::max(P * op->dp, V * op->dp));
     op->part_bytes = std::min<uint64_t>(64ull << 20, most * 4 * 32);
-    if (f32) op->part_bytes = std::max(op->part_bytes, P * V * 4);
+    if (f32) op->part_bytes = std::max(op->part_bytes, P * op->vp * 4);
     return xent_alloc(op, &op->part, op->part_bytes);
 }
 
