@@ -305,24 +305,77 @@ struct EpiRows {
     __device__ __forceinline__ unsigned long long to(unsigned i) const { return __shfl_sync(0xffffffffu, out, i); }
 };
 
-__device__ __forceinline__ void epi_part(const TcArgs &g, const float (&v)[kCols], const EpiRows &rows, unsigned col0, unsigned s, uint8_t *stage, unsigned lane) {
-    const unsigned pitch = (g.n + 7) & ~7u;
+// Where a tile's float32 values go: a part of a split product, float32 sums over pieces, or a float32 output.
+struct F32Out {
+    float *p;
+    unsigned long long pitch;
+    unsigned cols;
+    bool vec, add;  // rows on 16-byte boundaries; add to what is there
+    float scale;    // of the sum
+};
+
+__device__ __forceinline__ float out_scale(const TcArgs &g) { return g.mean ? g.scale / (float)max(*g.rows, 1u) : g.scale; }
+template <Epi EPI> __device__ __forceinline__ F32Out f32_out(const TcArgs &g) {
+    if (EPI == Epi::kPart) return {g.part, (g.n + 7) & ~7u, (g.n + 7) & ~7u, true, false, 1.f};
+    return {g.acc ? g.acc : static_cast<float *>(g.out), g.acc ? g.acc_pitch : g.out_pitch, g.n, g.acc ? g.acc_vec != 0 : g.out_vec != 0,
+            g.acc && !g.acc_first, g.acc && !g.acc_last ? 1.f : out_scale(g)};
+}
+template <Epi EPI> __device__ __forceinline__ EpiRows epi_rows(const TcArgs &g, unsigned m, unsigned row0, unsigned s, unsigned lane) {
+    EpiRows rows{m, row0, row0 + lane};
+    if (EPI == Epi::kOut && g.row_map && rows.out < m) rows.out = g.row_map[g.first + rows.out];
+    if (EPI == Epi::kPart) rows.out += s * g.m;
+    return rows;
+}
+
+// The code below runs once per tile on eight warps that are all at different places: it is kept short (loops over chunks
+// of columns stay loops), since fetching instructions was most of its time when everything was unrolled.
+
+// 32 columns of 32 rows from the stage, kBatch stores at a time.
+template <int kBatch>
+__device__ __forceinline__ void flush_f32(uint8_t *stage, const F32Out &o, const EpiRows &rows, unsigned col0, unsigned lane) {
+    if (o.vec) {
+        const unsigned c = lane & 7, col = col0 + c * 4;
+        float *const base = o.p + col;
+        const bool whole = col + 4 <= o.cols;
+#pragma unroll 1
+        for (int h = 0; h < 32; h += 4 * kBatch) {
+            Chunk x[kBatch];
+            float *at[kBatch];
 #pragma unroll
-    for (int j = 0; j < kCols; j += 32) {
-        stage_fill(stage, lane, [&](int c) {
-            Chunk x;
+            for (int i = 0; i < kBatch; ++i) {
+                const unsigned r = h + i * 4 + (lane >> 3);
+                at[i] = base + rows.to(r) * o.pitch;
+                x[i].u = *stage_at(stage, r, c);
+                if (!rows.has(r) || col >= o.cols) at[i] = nullptr;
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x.f[i] = v[j + c * 4 + i];
-            return x.u;
-        });
-        const unsigned c = lane & 7, col = col0 + j + c * 4;
+            for (int i = 0; i < kBatch; ++i) {
+                if (!at[i]) continue;
+                if (whole) {
+                    if (o.add) {
+                        const float4 y = *reinterpret_cast<const float4 *>(at[i]);
+                        x[i].f[0] += y.x; x[i].f[1] += y.y; x[i].f[2] += y.z; x[i].f[3] += y.w;
+                    }
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const unsigned r = i + (lane >> 3);
-            const uint4 x = *stage_at(stage, r, c);
-            if (rows.has(r) && col < pitch)
-                *reinterpret_cast<uint4 *>(g.part + ((unsigned long long)s * g.m + rows.row0 + r) * pitch + col) = x;
+                    for (int q = 0; q < 4; ++q) x[i].f[q] *= o.scale;
+                    *reinterpret_cast<uint4 *>(at[i]) = x[i].u;
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 3; ++q)
+                        if (col + q < o.cols) at[i][q] = ((o.add ? at[i][q] : 0.f) + x[i].f[q]) * o.scale;
+                }
+            }
         }
+        return;
+    }
+    const unsigned col = col0 + lane;  // a line per row, wherever it begins
+#pragma unroll 4
+    for (unsigned r = 0; r < 32; ++r) {
+        float *p = o.p + rows.to(r) * o.pitch + col;
+        float x = reinterpret_cast<const float *>(stage)[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
+        if (!rows.has(r) || col >= o.cols) continue;
+        if (o.add) x += *p;
+        *p = x * o.scale;
     }
 }
 
@@ -409,67 +462,49 @@ __device__ __forceinline__ void flush16(uint8_t *stage, unsigned short *base, un
     }
     // any row may begin between two 4-byte words: lane l then takes columns 2l + 1 and 2l + 2, and lane 0 the first one
     const unsigned short *st = reinterpret_cast<const unsigned short *>(stage);
+#pragma unroll 4
     for (unsigned r = 0; r < 32; ++r) {
-        if (!rows.has(r)) break;
         unsigned short *o = base + rows.to(r) * pitch;
         const unsigned odd = (unsigned)((uintptr_t)o >> 1) & 1u, a = 2 * lane + odd, b = a + 1;
         const unsigned short x = st[r * 64 + (((a >> 3) ^ (r & 7)) << 3) + (a & 7)];
         const unsigned short y = b < 64 ? st[r * 64 + (((b >> 3) ^ (r & 7)) << 3) + (b & 7)] : (unsigned short)0;
+        if (!rows.has(r)) continue;
         if (b < 64 && b < left) *reinterpret_cast<unsigned *>(o + a) = (unsigned)x | (unsigned)y << 16;
         else if (a < left) o[a] = x;
         if (odd && lane == 0 && left) o[0] = st[r * 64 + ((r & 7) << 3)];
     }
 }
 
-__device__ __forceinline__ void epi_out(const TcArgs &g, const float (&v)[kCols], const EpiRows &rows, unsigned col0, float f, uint8_t *stage, unsigned lane) {
-    if (g.out_type != SCAR_F32 && !g.acc) {
-#pragma unroll
-        for (int j = 0; j < kCols; j += 64) {
-            if (col0 + j >= g.n) break;
-            stage_fill(stage, lane, [&](int c) {
-                Chunk x;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (g.out_type == SCAR_BF16) x.b[i] = __float2bfloat16_rn(v[j + c * 8 + i] * f);
-                    else x.h[i] = __float2half_rn(v[j + c * 8 + i] * f);
-                }
-                return x.u;
-            });
-            flush16(stage, static_cast<unsigned short *>(g.out) + col0 + j, g.out_pitch, g.out_vec, rows, g.n - (col0 + j), lane);
-        }
-        return;
+// 32 columns of the last of several pieces: added to the float32 sums of the others, scaled and rounded to 16 bits.
+__device__ __forceinline__ void flush_last16(uint8_t *stage, const TcArgs &g, const EpiRows &rows, unsigned col0, float f, unsigned lane) {
+    const unsigned c = lane & 7;
+#pragma unroll 2
+    for (int i = 0; i < 32; i += 4) {
+        const unsigned r = i + (lane >> 3);
+        const unsigned long long to = rows.to(r);
+        Chunk x;
+        x.u = *stage_at(stage, r, c);
+        if (rows.has(r)) store_out4(g, make_float4(x.f[0], x.f[1], x.f[2], x.f[3]), rows.row0 + r, to, col0 + c * 4, f);
     }
+}
+
+__device__ __forceinline__ uint4 pack_half8(const float *v) {
+    union {
+        __half2 h[4];
+        uint4 u;
+    } x;
 #pragma unroll
-    for (int j = 0; j < kCols; j += 32) {
-        if (col0 + j >= g.n) break;
-        stage_fill(stage, lane, [&](int c) {
-            Chunk x;
+    for (int i = 0; i < 4; ++i) x.h[i] = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+    return x.u;
+}
+__device__ __forceinline__ uint4 pack_bf8(const float *v) {
+    union {
+        __nv_bfloat162 h[4];
+        uint4 u;
+    } x;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x.f[i] = v[j + c * 4 + i];
-            return x.u;
-        });
-        if (g.out_type == SCAR_F32 && !g.out_vec) {  // a line per row, wherever it begins
-            const unsigned col = col0 + j + lane;
-            for (unsigned r = 0; r < 32 && rows.has(r); ++r) {
-                const unsigned long long to = rows.to(r);
-                float x = reinterpret_cast<const float *>(stage)[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
-                if (col >= g.n) continue;
-                float *o = static_cast<float *>(g.out) + to * g.out_pitch + col;  // acc, where there is one, is the output
-                if (g.acc && !g.acc_first) x += *o;
-                *o = g.acc && !g.acc_last ? x : x * f;
-            }
-        } else {
-            const unsigned c = lane & 7, col = col0 + j + c * 4;
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const unsigned r = i + (lane >> 3);
-                const unsigned long long to = rows.to(r);
-                Chunk x;
-                x.u = *stage_at(stage, r, c);
-                if (rows.has(r)) store_out4(g, make_float4(x.f[0], x.f[1], x.f[2], x.f[3]), rows.row0 + r, to, col, f);
-            }
-        }
-    }
+    for (int i = 0; i < 4; ++i) x.h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    return x.u;
 }
 
 // One row's 128 logits of this thread: their maximum, the sum of their exponentials relative to it, the label's logit,
@@ -503,24 +538,21 @@ __device__ __forceinline__ void epi_prob(const TcArgs &g, float (&v)[kCols], con
         s[j & 3] += v[j];
     }
     if (mine) g.stat[(unsigned long long)row * g.stat_pitch + group] = make_float2(ref, (s[0] + s[1]) + (s[2] + s[3]));
-    if constexpr (!STORE) return;
-    else
+    if constexpr (STORE) {
+#pragma unroll 1
+        for (int j = 0; j < 2; ++j) {
+            if (j * 64 >= left) break;
+            if (j == 0) stage_fill(stage, lane, [&](int c) { return pack_half8(v + c * 8); });
+            else stage_fill(stage, lane, [&](int c) { return pack_half8(v + 64 + c * 8); });
+            const unsigned c = lane & 7;
+            __half *base = g.prob + (unsigned long long)rows.row0 * g.prob_pitch + col + j * 64 + c * 8;
 #pragma unroll
-    for (int j = 0; j < kCols; j += 64) {
-        if (j >= left) break;
-        stage_fill(stage, lane, [&](int c) {
-            Chunk x;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x.h[i] = __float2half_rn(v[j + c * 8 + i]);
-            return x.u;
-        });
-        const unsigned c = lane & 7;
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const unsigned r = i + (lane >> 3);
-            const uint4 x = *stage_at(stage, r, c);
-            if (rows.has(r) && j + c * 8 < left)  // the pitch is a multiple of 8
-                *reinterpret_cast<uint4 *>(g.prob + (unsigned long long)(rows.row0 + r) * g.prob_pitch + col + j + c * 8) = x;
+            for (int i = 0; i < 32; i += 4) {
+                const unsigned r = i + (lane >> 3);
+                const uint4 x = *stage_at(stage, r, c);
+                if (rows.has(r) && j * 64 + c * 8 < left)  // the pitch is a multiple of 8
+                    *reinterpret_cast<uint4 *>(base + (unsigned long long)r * g.prob_pitch) = x;
+            }
         }
     }
 }
@@ -657,53 +689,121 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
     } else if (warp < kEpiWarps) {  // epilogue
         const unsigned quad = warp & 3, half = warp >> 2;
         uint8_t *stage = smem + S::kStages * S::kStageBytes + warp * kWarpStage;
-        const float f = EPI == Epi::kOut ? (g.mean ? g.scale / (float)max(*g.rows, 1u) : g.scale) : 0.f;
-        unsigned ac = 0;
-        for (unsigned t = pair; t < walk.total && ok; t += pairs) {
+        constexpr bool kRegs = PL == 3 || kLogits;  // sums over rounds, or a whole row at a time: all columns in registers
+        unsigned ac = 0, aph = 0;
+        for (unsigned t = pair; t < walk.total; t += pairs) {
             unsigned mi, ni, s, k0, k1;
             walk.at(t, mi, ni, s, k0, k1);
-            float v[kCols];
-            const unsigned rounds = k1 > k0 ? (k1 - k0 - 1) / kPer + 1 : 0u;
-            if (rounds == 0) {
+            const unsigned rounds = k1 > k0 ? (kPer == 1 ? k1 - k0 : (k1 - k0 - 1) / kPer + 1) : 0u;
+            const uint32_t lanes = tmem + half * kCols + (quad * 32u << 16);
+            if constexpr (kRegs) {
+                float v[kCols];
+                if (rounds == 0) {
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) v[j] = 0.f;
-            }
-            // the first round is the tile's accumulator itself, later ones are added to it
-            if (rounds) {
-                const unsigned a = ac % kAccs;
-                ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, (ac / kAccs) & 1, g.error));
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t src = tmem + a * kBN + half * kCols + (quad * 32u << 16);
-#pragma unroll
-                for (int j = 0; j < kCols; j += 32) tmem_load32(src + j, v + j);
-                tmem_loaded(v);
-                acc_release(acc_empty + 8 * a, lane);
-                ++ac;
-            }
-            for (unsigned r = 1; r < rounds; ++r, ++ac) {
-                const unsigned a = ac % kAccs;
-                ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, (ac / kAccs) & 1, g.error));
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t src = tmem + a * kBN + half * kCols + (quad * 32u << 16);
-#pragma unroll
-                for (int j = 0; j < kCols; j += 16) {  // 16 at a time: 128 sums and 32 more registers do not fit
-                    float u[16];
-                    tmem_load16(src + j, u);
-                    tmem_loaded(u);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[j + i] += u[i];
+                    for (int j = 0; j < kCols; ++j) v[j] = 0.f;
                 }
-                acc_release(acc_empty + 8 * a, lane);
+                // the first round is the tile's accumulator itself, later ones are added to it
+                if (rounds) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, g.error));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int j = 0; j < kCols; j += 32) tmem_load32(lanes + ac * kBN + j, v + j);
+                    tmem_loaded(v);
+                    acc_release(acc_empty + 8 * ac, lane);
+                    if (++ac == kAccs) {
+                        ac = 0;
+                        aph ^= 1;
+                    }
+                }
+#pragma unroll 1
+                for (unsigned r = 1; r < rounds; ++r) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, g.error));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int j = 0; j < kCols; j += 16) {  // 16 at a time: 128 sums and 32 more registers do not fit
+                        float u[16];
+                        tmem_load16(lanes + ac * kBN + j, u);
+                        tmem_loaded(u);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[j + i] += u[i];
+                    }
+                    acc_release(acc_empty + 8 * ac, lane);
+                    if (++ac == kAccs) {
+                        ac = 0;
+                        aph ^= 1;
+                    }
+                }
+                if (!ok) break;
+                const EpiRows rows = epi_rows<EPI>(g, walk.m, mi * kBM + rank * 128 + quad * 32, s, lane);
+                const unsigned col = ni * kBN + half * kCols;
+                if constexpr (kLogits) {
+                    epi_prob<EPI == Epi::kProb>(g, v, rows, rows.row0 + lane, col, 2 * ni + half, stage, lane);
+                } else {
+                    const F32Out o = f32_out<EPI>(g);
+#pragma unroll 1
+                    for (int j = 0; j < 4; ++j) {
+                        if (col + j * 32 >= o.cols) break;
+                        auto fill = [&](const float *x) {
+                            stage_fill(stage, lane, [&](int c) { return make_uint4(__float_as_uint(x[4 * c]), __float_as_uint(x[4 * c + 1]), __float_as_uint(x[4 * c + 2]), __float_as_uint(x[4 * c + 3])); });
+                        };
+                        if (j == 0) fill(v);
+                        else if (j == 1) fill(v + 32);
+                        else if (j == 2) fill(v + 64);
+                        else fill(v + 96);
+                        flush_f32<2>(stage, o, rows, col + j * 32, lane);
+                    }
+                }
+            } else {
+                const EpiRows rows = epi_rows<EPI>(g, walk.m, mi * kBM + rank * 128 + quad * 32, s, lane);
+                const unsigned col = ni * kBN + half * kCols;
+                const F32Out o = f32_out<EPI>(g);
+                const bool to16 = EPI == Epi::kOut && g.out_type != SCAR_F32;
+                const bool last16 = to16 && g.acc && g.acc_last, pack16 = to16 && !g.acc;
+                const float f = EPI == Epi::kOut ? out_scale(g) : 1.f;
+                if (rounds) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, g.error));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                }
+#pragma unroll 1
+                for (unsigned j = 0; j < kCols && col + j < g.n;) {
+                    if (pack16) {
+                        float v[64] = {};
+                        if (rounds) {
+                            tmem_load32(lanes + ac * kBN + j, v);
+                            tmem_load32(lanes + ac * kBN + j + 32, v + 32);
+                            tmem_loaded(v);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) v[i] *= f;
+                        if (g.out_type == SCAR_BF16) stage_fill(stage, lane, [&](int c) { return pack_bf8(v + c * 8); });
+                        else stage_fill(stage, lane, [&](int c) { return pack_half8(v + c * 8); });
+                        flush16(stage, static_cast<unsigned short *>(g.out) + col + j, g.out_pitch, g.out_vec, rows, g.n - (col + j), lane);
+                        j += 64;
+                    } else {
+                        float v[32] = {};
+                        if (rounds) {
+                            tmem_load32(lanes + ac * kBN + j, v);
+                            tmem_loaded(v);
+                        }
+                        stage_fill(stage, lane, [&](int c) {
+                            return make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+                        });
+                        if (last16) flush_last16(stage, g, rows, col + j, f, lane);
+                        else flush_f32<8>(stage, o, rows, col + j, lane);
+                        j += 32;
+                    }
+                }
+                if (rounds) {
+                    acc_release(acc_empty + 8 * ac, lane);
+                    if (++ac == kAccs) {
+                        ac = 0;
+                        aph ^= 1;
+                    }
+                }
             }
-            if (!ok) break;
-            const unsigned row0 = mi * kBM + rank * 128 + quad * 32, row = row0 + lane, col = ni * kBN + half * kCols;
-            EpiRows rows{walk.m, row0, row};
-            if (EPI == Epi::kOut && g.row_map && row < walk.m) rows.out = g.row_map[g.first + row];
-            if (EPI == Epi::kPart) epi_part(g, v, rows, col, s, stage, lane);
-            else if (EPI == Epi::kOut) epi_out(g, v, rows, col, f, stage, lane);
-            else epi_prob<EPI == Epi::kProb>(g, v, rows, row, col, 2 * ni + half, stage, lane);
         }
     }
     if (!ok) {  // let copies and instructions in flight end before the memory they use is given back

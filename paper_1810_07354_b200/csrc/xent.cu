@@ -235,25 +235,37 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
     if (!GRAD) return;
     const unsigned y = (unsigned)label[p.first + r];
     const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
-    for (unsigned v = threadIdx.x * 8; v < V; v += 256 * 8) {
-        const float2 e = st[v >> 7];
-        const float f = e.y != 0.f ? expf(e.x - lse) * (held / kProbScale) : 0.f;
-        Eight x;
-        x.u = *reinterpret_cast<const uint4 *>(row + v);
-        float w[8];
+    constexpr int kBatch = 4;  // 16-byte loads of a thread in flight
+    for (unsigned v0 = threadIdx.x * 8; v0 < V; v0 += kBatch * 256 * 8) {
+        Eight x[kBatch];
+        float2 e[kBatch];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            w[j] = __half2float(x.h[j]) * f;
-            if (v + j == y) w[j] = expm1f(zl - lse) * held;
+        for (int i = 0; i < kBatch; ++i) {
+            const unsigned v = v0 + i * 256 * 8;
+            if (v >= V) break;
+            x[i].u = __ldcs(reinterpret_cast<const uint4 *>(row + v));
+            e[i] = st[v >> 7];
         }
-        if (o.dt == SCAR_F16) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x.h[j] = __float2half_rn(w[j]);
-        } else {
+        for (int i = 0; i < kBatch; ++i) {
+            const unsigned v = v0 + i * 256 * 8;
+            if (v >= V) break;
+            const float f = e[i].y != 0.f ? expf(e[i].x - lse) * (held / kProbScale) : 0.f;
+            float w[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x.b[j] = __float2bfloat16_rn(w[j]);
+            for (int j = 0; j < 8; ++j) {
+                w[j] = __half2float(x[i].h[j]) * f;
+                if (v + j == y) w[j] = expm1f(zl - lse) * held;
+            }
+            if (o.dt == SCAR_F16) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[i].h[j] = __float2half_rn(w[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[i].b[j] = __float2bfloat16_rn(w[j]);
+            }
+            *reinterpret_cast<uint4 *>(row + v) = x[i].u;
         }
-        *reinterpret_cast<uint4 *>(row + v) = x.u;
     }
 }
 
@@ -278,6 +290,7 @@ k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict_
     const unsigned long long stride = (unsigned long long)g.m * pitch;
     float *z = g.part + (unsigned long long)r * pitch;
     float top = -INFINITY, s = 0.f;
+#pragma unroll 2
     for (unsigned v = threadIdx.x * 4; v < V; v += 256 * 4) {
         float4 a = *reinterpret_cast<const float4 *>(z + v);
         if (splits > 1) {
