@@ -50,7 +50,7 @@ constexpr int kTcSmem = 6 * 2 * 128 * kBK * 2 + kEpiWarps * kWarpStage + 1024;
 static_assert(TcShape<1>::kStages * TcShape<1>::kStageBytes == TcShape<3>::kStages * TcShape<3>::kStageBytes, "both fill 192 KiB");
 
 struct TcArgs {
-    CUtensorMap a, b;
+    CUtensorMap a, b, c;     // c: the result, where whole boxes of it can be stored (c_map)
     unsigned m, n, k;        // extents; the one `dyn` names is an upper bound
     int dyn;                 // 0: m, 1: k is the number of rows of this piece
     unsigned first, most;    // the piece's rows of the compacted list
@@ -63,6 +63,7 @@ struct TcArgs {
     int n_fast;              // tiles of one row of tiles run first (B is the smaller operand and stays in L2)
     int bf16;
     unsigned *error;
+    int c_map;
     // kPart
     float *part;             // [splits][m][n rounded up to 8]
     // kOut
@@ -76,8 +77,6 @@ struct TcArgs {
     float scale;             // of the result: scale / rows when mean
     int mean;
     // kProb, kStat
-    __half *prob;
-    unsigned long long prob_pitch;
     float2 *stat;            // [row][2 * n tiles]: maximum and sum of exponentials of 128 columns
     unsigned stat_pitch;
     const int *label;        // of the compacted rows
@@ -123,10 +122,11 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, unsigne
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// Arrives at the same barrier in the pair's first CTA.
+// Arrives at the same barrier in the pair's first CTA.  Relaxed: what it reports are reads of tensor memory that are done
+// (tcgen05.wait::ld); releasing would also wait for the warp's stores of the tile before, about 2000 clocks.
 __device__ __forceinline__ void mbar_arrive_leader(uint32_t bar) {
     asm volatile(
-        "{\n .reg .b32 ra;\n mapa.shared::cluster.u32 ra, %0, 0;\n mbarrier.arrive.release.cluster.shared::cluster.b64 _, [ra];\n}\n" ::"r"(bar)
+        "{\n .reg .b32 ra;\n mapa.shared::cluster.u32 ra, %0, 0;\n mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [ra];\n}\n" ::"r"(bar)
         : "memory");
 }
 // One lane of a converged warp.  The loops below run in all lanes with warp-uniform values and only the issuing of
@@ -152,6 +152,21 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, u
         "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
         "l"(map), "r"(bar & 0xFEFFFFFFu), "r"(x), "r"(y), "r"(plane)
         : "memory");
+}
+// A box of 32 rows of 128 bytes from a warp's stage (whose swizzle is the tensor map's) to memory; what lies outside the
+// tensor is left out.  The copy is asynchronous: stage_free waits until the stage has been read.
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int x, int y, int plane) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (elect_one()) {
+        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(plane) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ void stage_free() {
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
 }
 __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
@@ -292,7 +307,7 @@ __device__ __forceinline__ uint4 *stage_at(uint8_t *stage, unsigned row, unsigne
     return reinterpret_cast<uint4 *>(stage + row * 128 + ((chunk ^ (row & 7)) << 4));
 }
 template <typename F> __device__ __forceinline__ void stage_fill(uint8_t *stage, unsigned lane, F chunk) {
-    __syncwarp();
+    stage_free();
 #pragma unroll
     for (int c = 0; c < 8; ++c) *stage_at(stage, lane, c) = chunk(c);
     __syncwarp();
@@ -544,15 +559,7 @@ __device__ __forceinline__ void epi_prob(const TcArgs &g, float (&v)[kCols], con
             if (j * 64 >= left) break;
             if (j == 0) stage_fill(stage, lane, [&](int c) { return pack_half8(v + c * 8); });
             else stage_fill(stage, lane, [&](int c) { return pack_half8(v + 64 + c * 8); });
-            const unsigned c = lane & 7;
-            __half *base = g.prob + (unsigned long long)rows.row0 * g.prob_pitch + col + j * 64 + c * 8;
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const unsigned r = i + (lane >> 3);
-                const uint4 x = *stage_at(stage, r, c);
-                if (rows.has(r) && j * 64 + c * 8 < left)  // the pitch is a multiple of 8
-                    *reinterpret_cast<uint4 *>(base + (unsigned long long)r * g.prob_pitch) = x;
-            }
+            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j * 64), (int)rows.row0, 0);
         }
     }
 }
@@ -745,14 +752,22 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
 #pragma unroll 1
                     for (int j = 0; j < 4; ++j) {
                         if (col + j * 32 >= o.cols) break;
+                        // a map stores what is staged: scaled already
+                        const float f = EPI == Epi::kOut && g.c_map ? o.scale : 1.f;
                         auto fill = [&](const float *x) {
-                            stage_fill(stage, lane, [&](int c) { return make_uint4(__float_as_uint(x[4 * c]), __float_as_uint(x[4 * c + 1]), __float_as_uint(x[4 * c + 2]), __float_as_uint(x[4 * c + 3])); });
+                            stage_fill(stage, lane, [&](int c) {
+                                return make_uint4(__float_as_uint(x[4 * c] * f), __float_as_uint(x[4 * c + 1] * f), __float_as_uint(x[4 * c + 2] * f), __float_as_uint(x[4 * c + 3] * f));
+                            });
                         };
                         if (j == 0) fill(v);
                         else if (j == 1) fill(v + 32);
                         else if (j == 2) fill(v + 64);
                         else fill(v + 96);
-                        flush_f32<2>(stage, o, rows, col + j * 32, lane);
+                        if (EPI == Epi::kPart || g.c_map) {
+                            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j * 32), (int)rows.row0, EPI == Epi::kPart ? (int)s : 0);
+                        } else {
+                            flush_f32<2>(stage, o, rows, col + j * 32, lane);
+                        }
                     }
                 }
             } else {
@@ -780,7 +795,10 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                         for (int i = 0; i < 64; ++i) v[i] *= f;
                         if (g.out_type == SCAR_BF16) stage_fill(stage, lane, [&](int c) { return pack_bf8(v + c * 8); });
                         else stage_fill(stage, lane, [&](int c) { return pack_half8(v + c * 8); });
-                        flush16(stage, static_cast<unsigned short *>(g.out) + col + j, g.out_pitch, g.out_vec, rows, g.n - (col + j), lane);
+                        if (g.c_map) {
+                            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j), (int)rows.row0, 0);
+                        } else
+                            flush16(stage, static_cast<unsigned short *>(g.out) + col + j, g.out_pitch, g.out_vec, rows, g.n - (col + j), lane);
                         j += 64;
                     } else {
                         float v[32] = {};
@@ -791,7 +809,9 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                         stage_fill(stage, lane, [&](int c) {
                             return make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
                         });
-                        if (last16) flush_last16(stage, g, rows, col + j, f, lane);
+                        if (EPI == Epi::kPart) {
+                            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j), (int)rows.row0, (int)s);
+                        } else if (last16) flush_last16(stage, g, rows, col + j, f, lane);
                         else flush_f32<8>(stage, o, rows, col + j, lane);
                         j += 32;
                     }
@@ -806,6 +826,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
             }
         }
     }
+    if (warp < kEpiWarps) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // this warp's stores are in memory
     if (!ok) {  // let copies and instructions in flight end before the memory they use is given back
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     }

@@ -110,6 +110,24 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 &p0, __nv_bfloat16
     p2 = __float2bfloat16_rn(r1 - __bfloat162float(p1));
 }
 
+// 16 bytes that begin `by` bytes (even, below 16) into the 32 bytes a, b.
+__device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, unsigned by) {
+    unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (by & 8) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (by & 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    if (by & 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Copies rows into the layout the products read: rows of dp elements (zeros behind the last), 16-byte aligned, one plane
 // for the 16-bit types and three for float32.  With `pos`, row t goes to pos[t]; rows that do not count are left out and
 // their row of `zero` (dh) is cleared, and the rows behind the last one are zero up to a multiple of 64.
@@ -144,8 +162,12 @@ k_xent_place(const T *__restrict__ src, unsigned long long pitch, unsigned n, un
         unsigned short *o = dst + (unsigned long long)to * dp + c;
         if constexpr (sizeof(T) == 2) {
             Eight x;
+            const unsigned by = (unsigned)(uintptr_t)s & 15u;
             if (vec && c + 8 <= d) x.u = *reinterpret_cast<const uint4 *>(s);
-            else
+            else if (c && c + 16 <= d) {  // the two aligned words that hold it lie within the row
+                const uint4 *a = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(s) - by);
+                x.u = by ? shifted(a[0], a[1], by) : a[0];
+            } else
                 for (int j = 0; j < 8; ++j) x.s[j] = c + j < d ? reinterpret_cast<const unsigned short *>(s)[j] : (unsigned short)0;
             *reinterpret_cast<uint4 *>(o) = x.u;
         } else {
@@ -443,14 +465,37 @@ int check_call(const scar_xent *op, const void *h, uint64_t hp, const void *w, u
 bool rows_aligned(const void *p, uint64_t pitch, unsigned elem) { return (uintptr_t)p % 16 == 0 && pitch * elem % 16 == 0; }
 
 // The tensor map of an operand: boxes of 64 values of k by box_rows rows (K-major), or of 64 of its own dimension by 64
-// values of k (MN-major; box_rows = 64).
-int make_map(const scar_xent *op, CUtensorMap *map, const Operand &x, unsigned box_rows) {
-    const cuuint64_t dims[3] = {x.inner, x.rows, x.planes}, strides[2] = {x.pitch * 2, (x.planes > 1 ? x.plane : x.pitch) * 2};
-    const cuuint32_t box[3] = {kBK, box_rows, 1}, step[3] = {1, 1, 1};
-    const CUresult rc = op->encode(map, op->cfg.dtype == SCAR_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
-                                   const_cast<void *>(x.p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+// values of k (MN-major; box_rows = 64); or of a result: boxes of 128 bytes by 32 rows.
+int make_map(const scar_xent *op, CUtensorMap *map, const Operand &x, unsigned box_rows, unsigned elem = 2) {
+    const cuuint64_t dims[3] = {x.inner, x.rows, x.planes}, strides[2] = {x.pitch * elem, (x.planes > 1 ? x.plane : x.pitch) * elem};
+    const cuuint32_t box[3] = {128 / elem, box_rows, 1}, step[3] = {1, 1, 1};
+    const CUtensorMapDataType type = elem == 4                      ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                     : op->cfg.dtype == SCAR_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                                 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    const CUresult rc = op->encode(map, type, 3, const_cast<void *>(x.p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return rc == CUDA_SUCCESS ? SCAR_OK : SCAR_ERR_CUDA;
+}
+
+// A 16-bit or float32 matrix from rows on 16-byte boundaries to rows anywhere, a warp per row: whole 16-byte words of the
+// destination, its ends element by element.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_xent_unplace(const T *__restrict__ src, unsigned long long src_pitch, unsigned n, unsigned d, T *__restrict__ dst, unsigned long long pitch) {
+    griddep_start();
+    constexpr unsigned kVec = 16 / sizeof(T);
+    const unsigned lane = threadIdx.x & 31;
+    for (unsigned long long r = blockIdx.x * 8ull + (threadIdx.x >> 5); r < n; r += gridDim.x * 8ull) {
+        const T *s = src + r * src_pitch;
+        T *o = dst + r * pitch;
+        const unsigned head = min(d, (unsigned)((0u - (unsigned)(uintptr_t)o) & 15u) / (unsigned)sizeof(T)), words = (d - head) / kVec, tail = head + words * kVec;
+        if (lane < head) o[lane] = s[lane];
+        if (tail + lane < d) o[tail + lane] = s[tail + lane];
+        const uint4 *a = reinterpret_cast<const uint4 *>(s);  // head is shorter than a word: word w lies in a[w] and a[w + 1]
+#pragma unroll 4
+        for (unsigned w = lane; w < words; w += 32)
+            *reinterpret_cast<uint4 *>(o + head + w * kVec) = head ? shifted(a[w], a[w + 1], head * (unsigned)sizeof(T)) : a[w];
+    }
 }
 
 // Launches a kernel of the call's chain: it may start while the one before it still runs (griddep_start waits for it).
@@ -488,7 +533,11 @@ void choose_splits(const scar_xent *op, TcArgs &g) {
     }
 }
 
-template <int PL, bool A_MN, bool B_MN, Epi EPI> void launch_tc(scar_xent *op, const TcArgs &g) {
+template <int PL, bool A_MN, bool B_MN, Epi EPI> void launch_tc(scar_xent *op, TcArgs g) {
+    if (EPI == Epi::kPart) {
+        const uint64_t pitch = round_up(g.n, 8);
+        if (make_map(op, &g.c, {g.part, pitch, g.m, pitch, g.splits > 1 ? g.most_splits : 1u, g.m * pitch}, 32, 4) != SCAR_OK) op->failed = true;
+    }
     const uint64_t tiles = (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + kBN - 1) / kBN) * (g.splits > 1 ? g.most_splits : 1);
     const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, op->pairs);
     if (pairs) launch(op, k_tc_gemm<PL, A_MN, B_MN, EPI>, 2 * pairs, kGemmThreads, kTcSmem, g);
@@ -553,10 +602,11 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
     base.mean = mean;
     base.scale = op->cfg.dtype == SCAR_F16 ? scale / kDzF16 : scale;
     auto fill = [&](TcArgs &g, unsigned m, unsigned nn, unsigned k, int dyn) {
-        const CUtensorMap a = g.a, b = g.b;
+        const CUtensorMap a = g.a, b = g.b, c = g.c;
         g = base;
         g.a = a;
         g.b = b;
+        g.c = c;
         g.m = m;
         g.n = nn;
         g.k = k;
@@ -573,8 +623,7 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
         if (rows) {
             fill(logits, rows, V, D, 0);
             logits.a_row0 = at;
-            logits.prob = reinterpret_cast<__half *>(op->dz);
-            logits.prob_pitch = op->vp;
+            if (PL == 1 && grad && (rc = make_map(op, &logits.c, oz, 32)) != SCAR_OK) return rc;
             logits.stat = op->stat;
             logits.stat_pitch = op->groups;
             logits.label = op->label;
@@ -615,7 +664,20 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
             dwg.acc_first = at == 0;
             dwg.acc_last = at + (uint64_t)op->piece >= n;
         }
+        // Rows of dw that do not lie on 16-byte boundaries would be stored in pieces of lines, at a tenth of the rate: they go
+        // through the room of w's copy, which is done with by now, and from there to their places.  A tensor map's store
+        // clips rows to whole 16-byte words only, so rows of a length between two go the epilogue's own way.
+        const bool through_w = !dwg.acc && !dwg.out_vec && w_copied;
+        if (through_w) {
+            dwg.out = op->w;
+            dwg.out_pitch = op->dp;
+            dwg.out_vec = 1;
+        }
+        dwg.c_map = !dwg.acc && (through_w || (dwg.out_vec && D * sizeof(T) % 16 == 0));
+        if (dwg.c_map && (rc = make_map(op, &dwg.c, {dwg.out, D, V, dwg.out_pitch, 1, 0}, 32, sizeof(T))) != SCAR_OK) return rc;
         launch_out<PL, true>(op, dwg);
+        if (through_w)
+            launch(op, k_xent_unplace<T>, (unsigned)std::min<uint64_t>((V + 7) / 8, 16 * op->pairs), 256, 0, reinterpret_cast<const T *>(op->w), op->dp, V, D, dw, dwp);
         if ((uint64_t)at + op->piece >= n) break;
     }
     launch(op, k_xent_loss, 1, kRowThreads, 0, row_loss, n, mean, op->rec, d_loss);
