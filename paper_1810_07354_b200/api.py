@@ -665,15 +665,15 @@ class _OnStream:
     def _bind_stream(self, stream, device):
         import torch
 
-        self._device = torch.device(device)
+        device = torch.device(device)
+        self._device = torch.device(device.type, torch.cuda.current_device() if device.index is None else device.index)
         self._stream = stream if stream is not None else torch.cuda.current_stream(self._device)
+        self._torch, self._here = torch, torch._C._cuda_getCurrentRawStream  # the stream's address alone: no object per call
 
     def _enter(self, *tensors):
-        import torch
-
-        here = torch.cuda.current_stream(self._device)
-        if here == self._stream:
+        if self._here(self._device.index) == self._stream.cuda_stream:
             return None
+        here = self._torch.cuda.current_stream(self._device)
         self._stream.wait_stream(here)
         for t in tensors:
             if t is not None:
@@ -723,13 +723,12 @@ class LinearCrossEntropy(_OnStream):
         return m.data_ptr(), (m.stride(0) if rows > 1 else max(m.stride(0), self.dim))
 
     def _call(self, grad: bool, h, w, labels, grad_scale, row_loss, dh, dw):
-        import torch
-
+        torch = self._torch
         n = labels.numel()
         if labels.dtype != torch.int64 or not labels.is_cuda or not labels.is_contiguous():
             raise TypeError("labels: a contiguous CUDA tensor of int64 is wanted")
         hp, wp = self._matrix("h", h, n), self._matrix("w", w, self.n_classes)
-        dev = h.device
+        dev = self._device
         if row_loss is None:
             row_loss = torch.empty(n, dtype=torch.float32, device=dev)
         elif row_loss.dtype != torch.float32 or row_loss.numel() != n or not row_loss.is_contiguous():
@@ -811,9 +810,7 @@ class GradientNorm(_OnStream):
         scar_gnorm_bind(self.op, self._table(list(tensors), out))
 
     def _run(self, call):
-        import torch
-
-        norm = torch.empty((), dtype=torch.float32, device=self._device)
+        norm = self._torch.empty((), dtype=self._torch.float32, device=self._device)
         here = self._enter(norm)
         call(norm.data_ptr())
         self._leave(here)

@@ -8,7 +8,7 @@
 //   dh = dz w, dw = dz^T h
 // so the logits are computed once (6 n V D operations, not 8) and exist only in tensor memory.  float32 operators, and
 // products with too few tiles to fill the GPU (their sum over D is split over CTAs), pass through float32 logits of the
-// piece instead (kPart and k_xent_softmax).  k_xent_loss adds the row losses.
+// piece instead (kPart and k_xent_softmax).  The last CTA of the last softmax adds the row losses.
 #include <algorithm>
 #include <new>
 #include <vector>
@@ -26,6 +26,7 @@ struct XentRecord {
     float loss;
     unsigned rows, ignored, bad;
     unsigned error;
+    unsigned done;  // CTAs of the last softmax kernel that are through
 };
 
 // Every kernel of a call is launched while the one before it may still run; nothing is touched before that one is done.
@@ -35,54 +36,67 @@ __device__ __forceinline__ void griddep_start() {
 }
 
 // Compacts the rows that count, in order: row_of[0 .. rows) are their numbers, pos is the inverse (kNone for the rest).
-// One CTA: the labels of a step are few.
+// One CTA, eight neighbouring labels per thread at a time: the labels of a step are few.
+constexpr int kLabels = 8;
 __global__ void __launch_bounds__(kRowThreads)
 k_xent_rows(const long long *__restrict__ labels, unsigned n, long long ignore, unsigned n_classes,
             unsigned *__restrict__ row_of, unsigned *__restrict__ pos, int *__restrict__ label, float *__restrict__ row_loss,
-            XentRecord *rec) {
-    __shared__ unsigned sh[kRowThreads / 32], base, n_ign, n_bad;
+            XentRecord *rec, float *d_loss) {
+    __shared__ unsigned sh[kRowThreads / 32], n_ign, n_bad;
     griddep_start();
-    if (threadIdx.x == 0) base = n_ign = n_bad = 0;
-    __syncthreads();
+    if (threadIdx.x == 0) n_ign = n_bad = 0;
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (unsigned at = 0; at < n; at += kRowThreads) {
-        const unsigned t = at + threadIdx.x;
-        bool keep = false, bad = false, ign = false;
-        long long y = 0;
-        if (t < n) {
-            y = labels[t];
-            ign = y == ignore;
-            keep = !ign && y >= 0 && y < (long long)n_classes;
-            bad = !ign && !keep;
-            if (!keep) row_loss[t] = 0.f;
+    unsigned base = 0, ign = 0, bad = 0;
+    for (unsigned long long at = 0; at < n; at += kRowThreads * kLabels) {
+        const unsigned long long t0 = at + threadIdx.x * kLabels;
+        long long y[kLabels];
+        unsigned keep = 0;
+#pragma unroll
+        for (int i = 0; i < kLabels; ++i) y[i] = t0 + i < n ? labels[t0 + i] : ignore;
+#pragma unroll
+        for (int i = 0; i < kLabels; ++i) {
+            if (t0 + i >= n) continue;
+            if (y[i] == ignore) ++ign;
+            else if (y[i] >= 0 && y[i] < (long long)n_classes) keep |= 1u << i;
+            else ++bad;
+            if (!(keep >> i & 1u)) {
+                row_loss[t0 + i] = 0.f;
+                pos[t0 + i] = kNone;
+            }
         }
-        const unsigned m = __ballot_sync(0xffffffffu, keep);
-        const unsigned mi = __ballot_sync(0xffffffffu, ign), mb = __ballot_sync(0xffffffffu, bad);
-        if (lane == 0) {
-            sh[warp] = __popc(m);
-            if (mi) atomicAdd(&n_ign, __popc(mi));
-            if (mb) atomicAdd(&n_bad, __popc(mb));
+        const unsigned mine = __popc(keep);
+        unsigned scan = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned v = __shfl_up_sync(0xffffffffu, scan, o);
+            if (lane >= o) scan += v;
         }
         __syncthreads();
-        const unsigned mine = sh[lane];
-        const unsigned before = base + __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0u);
-        const unsigned all = __reduce_add_sync(0xffffffffu, mine);
-        const unsigned r = before + __popc(m & ((1u << lane) - 1u));
-        if (keep) {
-            row_of[r] = t;
-            label[r] = (int)y;
+        if (lane == 31) sh[warp] = scan;
+        __syncthreads();
+        const unsigned all = sh[lane];
+        unsigned r = base + __reduce_add_sync(0xffffffffu, lane < warp ? all : 0u) + scan - mine;
+        base += __reduce_add_sync(0xffffffffu, all);
+#pragma unroll
+        for (int i = 0; i < kLabels; ++i) {
+            if (!(keep >> i & 1u)) continue;
+            row_of[r] = (unsigned)(t0 + i);
+            label[r] = (int)y[i];
+            pos[t0 + i] = r++;
         }
-        if (t < n) pos[t] = keep ? r : kNone;
-        __syncthreads();
-        if (threadIdx.x == 0) base += all;
-        __syncthreads();
     }
+    __syncthreads();
+    if (ign) atomicAdd(&n_ign, ign);
+    if (bad) atomicAdd(&n_bad, bad);
+    __syncthreads();
     if (threadIdx.x == 0) {
         rec->rows = base;
         rec->ignored = n_ign;
         rec->bad = n_bad;
         rec->error = 0;
+        rec->done = 0;
         rec->loss = 0.f;
+        if (d_loss && n == 0) *d_loss = 0.f;
     }
 }
 
@@ -225,21 +239,55 @@ struct DzOut {
     int dt;
 };
 
+// Ends every CTA of a softmax kernel; with `n` (the last piece of a call) the last CTA to get here adds up the call's row
+// losses, in an order that depends on n alone.
+struct LossOut {
+    const float *row_loss;
+    unsigned n;
+    bool mean;
+    XentRecord *rec;
+    float *d_loss;
+};
+__device__ __forceinline__ void finish_loss(const LossOut &o) {
+    __shared__ double sh[8];
+    __shared__ bool last;
+    if (!o.n) return;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(&o.rec->done, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double s = 0.0;
+#pragma unroll 4
+    for (unsigned t = threadIdx.x; t < o.n; t += 256) s += __ldcg(o.row_loss + t);
+    for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x) return;
+    s = 0.0;
+    for (int w = 0; w < 8; ++w) s += sh[w];
+    o.rec->loss = (float)(o.mean ? s / (double)max(o.rec->rows, 1u) : s);
+    if (o.d_loss) *o.d_loss = o.rec->loss;
+}
+
 // One CTA per row of the piece: joins the row's groups of 128 classes to lse and the loss; with GRAD turns the row's
 // scaled exponentials into dz in place.  Rows behind the last one up to a multiple of 64 become zero (the dw product
 // runs over whole groups of 64 rows).
 template <bool GRAD>
 __global__ void __launch_bounds__(256)
 k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups, const int *__restrict__ label,
-          const float *__restrict__ label_z, const unsigned *__restrict__ row_of, const XentRecord *__restrict__ rec, Piece p,
-          float *__restrict__ row_loss) {
+          const float *__restrict__ label_z, const unsigned *__restrict__ row_of, Piece p, float *row_loss, LossOut loss) {
     __shared__ float sh[8];
     griddep_start();
-    const unsigned r = blockIdx.x, R = p.rows(rec);
+    const unsigned r = blockIdx.x, R = p.rows(loss.rec);
     unsigned short *row = GRAD ? o.dz + (unsigned long long)r * o.pitch : nullptr;
     if (r >= R) {
         if (GRAD && r < (R + 63) / 64 * 64)
             for (unsigned v = threadIdx.x * 8; v < o.pitch; v += 256 * 8) *reinterpret_cast<uint4 *>(row + v) = make_uint4(0, 0, 0, 0);
+        finish_loss(loss);
         return;
     }
     const float2 *st = stat + (unsigned long long)r * groups;
@@ -254,6 +302,7 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
     const float lse = top + logf(s * (1.f / kProbScale));
     const float zl = label_z[p.first + r];
     if (threadIdx.x == 0) row_loss[row_of[p.first + r]] = lse - zl;
+    finish_loss(loss);
     if (!GRAD) return;
     const unsigned y = (unsigned)label[p.first + r];
     const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
@@ -295,7 +344,7 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
 // maximum and sum of every thread, one for dz.
 template <bool GRAD>
 __global__ void __launch_bounds__(256)
-k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict__ label, const unsigned *__restrict__ row_of, float *__restrict__ row_loss) {
+k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict__ label, const unsigned *__restrict__ row_of, float *row_loss, LossOut loss) {
     __shared__ float sh[8];
     griddep_start();
     const unsigned r = blockIdx.x, R = rows_of(g), V = g.n, pitch = (V + 7) & ~7u;
@@ -306,6 +355,7 @@ k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict_
             for (int q = 0; q < planes; ++q)
                 for (unsigned v = threadIdx.x * 8; v < o.pitch; v += 256 * 8)
                     *reinterpret_cast<uint4 *>(row + q * o.plane + v) = make_uint4(0, 0, 0, 0);
+        finish_loss(loss);
         return;
     }
     const unsigned splits = pick_splits(g, R, g.k);
@@ -340,6 +390,7 @@ k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict_
     const unsigned y = (unsigned)label[g.first + r];
     const float zl = z[y];
     if (threadIdx.x == 0) row_loss[row_of[g.first + r]] = lse - zl;
+    finish_loss(loss);
     if (!GRAD) return;
     const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
     for (unsigned v = threadIdx.x * 8; v < V; v += 256 * 8) {
@@ -380,22 +431,6 @@ k_xent_combine(const __grid_constant__ TcArgs g) {
     }
 }
 
-__global__ void __launch_bounds__(kRowThreads)
-k_xent_loss(const float *__restrict__ row_loss, unsigned n, bool mean, XentRecord *rec, float *d_loss) {
-    __shared__ double sh[32];
-    griddep_start();
-    double s = 0.0;
-    for (unsigned t = threadIdx.x; t < n; t += kRowThreads) s += row_loss[t];
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
-    __syncthreads();
-    if (threadIdx.x) return;
-    s = 0.0;
-    for (int w = 0; w < 32; ++w) s += sh[w];
-    rec->loss = (float)(mean ? s / (double)max(rec->rows, 1u) : s);
-    if (d_loss) *d_loss = rec->loss;
-}
-
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
@@ -430,10 +465,12 @@ struct scar_xent {
     float *acc = nullptr;
     XentRecord *rec = nullptr;
     XentRecord *h_rec = nullptr;   // pinned
+    // tensor maps of the workspaces: h as rows (128 a box) and as columns, dz likewise and as a result, w's copy
+    CUtensorMap h_rows_map, h_cols_map, dz_rows_map, dz_cols_map, dz_out_map, w_rows_map, w_cols_map;
     std::vector<void *> owned;
     uint64_t bytes = 0;
     uint64_t launches = 0;
-    bool ran = false, failed = false;
+    bool ran = false, failed = false, have_w_maps = false;
 };
 
 namespace {
@@ -496,6 +533,26 @@ k_xent_unplace(const T *__restrict__ src, unsigned long long src_pitch, unsigned
         for (unsigned w = lane; w < words; w += 32)
             *reinterpret_cast<uint4 *>(o + head + w * kVec) = head ? shifted(a[w], a[w + 1], head * (unsigned)sizeof(T)) : a[w];
     }
+}
+
+// Maps of the operator's own buffers, made once.
+int map_workspaces(scar_xent *op) {
+    const uint64_t V = op->cfg.n_classes, D = op->cfg.dim;
+    const Operand oh{op->h, D, op->h_rows, op->dp, op->planes, op->h_rows * op->dp};
+    const Operand oz{op->dz, V, op->piece, op->vp, op->planes, (uint64_t)op->piece * op->vp};
+    int rc;
+    if ((rc = make_map(op, &op->h_rows_map, oh, 128)) != SCAR_OK || (rc = make_map(op, &op->h_cols_map, oh, 64)) != SCAR_OK) return rc;
+    if (!op->dz) return SCAR_OK;
+    if ((rc = make_map(op, &op->dz_rows_map, oz, 128)) != SCAR_OK || (rc = make_map(op, &op->dz_cols_map, oz, 64)) != SCAR_OK) return rc;
+    return make_map(op, &op->dz_out_map, oz, 32);
+}
+int map_w_copy(scar_xent *op) {
+    const uint64_t V = op->cfg.n_classes, D = op->cfg.dim;
+    const Operand ow{op->w, D, V, op->dp, op->planes, V * op->dp};
+    int rc;
+    if ((rc = make_map(op, &op->w_rows_map, ow, kBN / 2)) != SCAR_OK || (rc = make_map(op, &op->w_cols_map, ow, 64)) != SCAR_OK) return rc;
+    op->have_w_maps = true;
+    return SCAR_OK;
 }
 
 // Launches a kernel of the call's chain: it may start while the one before it still runs (griddep_start waits for it).
@@ -576,22 +633,28 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
     // w in place where its rows lie on 16-byte boundaries, else (and in float32 always) through a copy of its own
     const bool w_copied = PL == 3 || !rows_aligned(w, wp, sizeof(T));
     if (w_copied && !op->w && (rc = xent_alloc(op, &op->w, (uint64_t)PL * V * op->dp * 2)) != SCAR_OK) return rc;
-    const Operand oh{op->h, D, op->h_rows, op->dp, PL, op->h_rows * op->dp};
-    const Operand ow = w_copied ? Operand{op->w, D, V, op->dp, PL, (uint64_t)V * op->dp} : Operand{w, D, V, wp, 1, (uint64_t)V * wp};
-    const Operand oz{op->dz, V, op->piece, op->vp, PL, (uint64_t)op->piece * op->vp};
     TcArgs logits{}, dhg{}, dwg{};
-    if ((rc = make_map(op, &logits.a, oh, 128)) != SCAR_OK || (rc = make_map(op, &logits.b, ow, kBN / 2)) != SCAR_OK) return rc;
-    if (grad && ((rc = make_map(op, &dhg.a, oz, 128)) != SCAR_OK || (rc = make_map(op, &dhg.b, ow, 64)) != SCAR_OK ||
-                 (rc = make_map(op, &dwg.a, oz, 64)) != SCAR_OK || (rc = make_map(op, &dwg.b, oh, 64)) != SCAR_OK))
-        return rc;
+    logits.a = op->h_rows_map;
+    dwg.b = op->h_cols_map;
+    dhg.a = op->dz_rows_map;
+    dwg.a = op->dz_cols_map;
+    logits.c = op->dz_out_map;
+    if (w_copied) {
+        if (!op->have_w_maps && (rc = map_w_copy(op)) != SCAR_OK) return rc;
+        logits.b = op->w_rows_map;
+        dhg.b = op->w_cols_map;
+    } else {
+        const Operand ow{w, D, V, wp, 1, 0};
+        if ((rc = make_map(op, &logits.b, ow, kBN / 2)) != SCAR_OK || (grad && (rc = make_map(op, &dhg.b, ow, 64)) != SCAR_OK)) return rc;
+    }
 
-    launch(op, k_xent_rows, 1, kRowThreads, 0, y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec);
+    launch(op, k_xent_rows, 1, kRowThreads, 0, y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec, d_loss);
     const unsigned most_ctas = 16 * op->pairs;
     auto ctas = [&](uint64_t rows) { return (unsigned)std::min<uint64_t>((rows * (op->dp / 8) + 255) / 256, most_ctas); };
-    launch(op, k_xent_place<T>, ctas(n + 64), 256, 0, h, hp, n, D, (unsigned)op->dp, rows_aligned(h, hp, sizeof(T)), op->h, oh.plane, op->pos, &op->rec->rows,
+    launch(op, k_xent_place<T>, ctas(n + 64), 256, 0, h, hp, n, D, (unsigned)op->dp, rows_aligned(h, hp, sizeof(T)), op->h, op->h_rows * op->dp, op->pos, &op->rec->rows,
            grad ? dh : nullptr, dhp);
     if (w_copied)
-        launch(op, k_xent_place<T>, ctas(V), 256, 0, w, wp, V, D, (unsigned)op->dp, rows_aligned(w, wp, sizeof(T)), op->w, ow.plane, nullptr, nullptr, nullptr, 0);
+        launch(op, k_xent_place<T>, ctas(V), 256, 0, w, wp, V, D, (unsigned)op->dp, rows_aligned(w, wp, sizeof(T)), op->w, (uint64_t)V * op->dp, nullptr, nullptr, nullptr, 0);
 
     TcArgs base{};
     base.rows = &op->rec->rows;
@@ -619,11 +682,11 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
         const Piece p{at, op->piece};
         base.first = at;
         base.most = op->piece;
-        const DzOut dz{op->dz, op->vp, oz.plane, op->cfg.dtype};
+        const DzOut dz{op->dz, op->vp, (uint64_t)op->piece * op->vp, op->cfg.dtype};
+        const LossOut loss{row_loss, (uint64_t)at + op->piece >= n ? n : 0u, mean, op->rec, d_loss};
         if (rows) {
             fill(logits, rows, V, D, 0);
             logits.a_row0 = at;
-            if (PL == 1 && grad && (rc = make_map(op, &logits.c, oz, 32)) != SCAR_OK) return rc;
             logits.stat = op->stat;
             logits.stat_pitch = op->groups;
             logits.label = op->label;
@@ -631,15 +694,15 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
             choose_splits(op, logits);
             if (PL == 3 || logits.splits > 1) {
                 launch_tc<PL, false, false, Epi::kPart>(op, logits);
-                if (grad) launch(op, k_xent_softmax<true>, rows64, 256, 0, logits, dz, op->label, op->row_of, row_loss);
-                else launch(op, k_xent_softmax<false>, rows, 256, 0, logits, dz, op->label, op->row_of, row_loss);
+                if (grad) launch(op, k_xent_softmax<true>, rows64, 256, 0, logits, dz, op->label, op->row_of, row_loss, loss);
+                else launch(op, k_xent_softmax<false>, rows, 256, 0, logits, dz, op->label, op->row_of, row_loss, loss);
             } else if constexpr (PL == 1) {
                 if (grad) {
                     launch_tc<1, false, false, Epi::kProb>(op, logits);
-                    launch(op, k_xent_dz<true>, rows64, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, op->rec, p, row_loss);
+                    launch(op, k_xent_dz<true>, rows64, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, p, row_loss, loss);
                 } else {
                     launch_tc<1, false, false, Epi::kStat>(op, logits);
-                    launch(op, k_xent_dz<false>, rows, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, op->rec, p, row_loss);
+                    launch(op, k_xent_dz<false>, rows, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, p, row_loss, loss);
                 }
             }
         }
@@ -680,7 +743,6 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
             launch(op, k_xent_unplace<T>, (unsigned)std::min<uint64_t>((V + 7) / 8, 16 * op->pairs), 256, 0, reinterpret_cast<const T *>(op->w), op->dp, V, D, dw, dwp);
         if ((uint64_t)at + op->piece >= n) break;
     }
-    launch(op, k_xent_loss, 1, kRowThreads, 0, row_loss, n, mean, op->rec, d_loss);
     if (op->failed) {
         op->failed = false;
         cudaGetLastError();
@@ -770,8 +832,8 @@ int scar_xent_init(scar_xent **out, const scar_xent_config *cfg, void *cuda_stre
         int sms = 0;
         TRAIN_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, op->device));
         op->pairs = std::max(1, sms / 2);
-        const int rc = size_workspaces(op);
-        if (rc != SCAR_OK) return rc;
+        int rc = size_workspaces(op);
+        if (rc != SCAR_OK || (rc = map_workspaces(op)) != SCAR_OK) return rc;
         if (cudaMallocHost(&op->h_rec, sizeof(XentRecord)) != cudaSuccess) {
             cudaGetLastError();
             return SCAR_ERR_ALLOC;
