@@ -3,9 +3,12 @@
 // The tensors are cut into pieces of at most kPieceBytes on the host, once, so that every piece but a tensor's first
 // begins on a 16-byte boundary.  A CTA walks over pieces with a fixed stride: which CTA adds what depends on the lengths
 // alone, the last CTA to finish adds the CTAs' sums in their order, and the result is the same bits every time.
-// Bound by HBM: one read for the norm, one read and one write for the scaled values.  The second kernel is already
-// resident when the first ends (programmatic launch) and walks the pieces backwards, so that what the first read last
-// is still in L2.
+// Bound by HBM: one read for the norm, one read and one write for the scaled values.  The second kernel is launched
+// while the first runs (programmatic launch) and takes the pieces backwards, so that what the first read last is still
+// in L2; it has one CTA per piece, started in order, because CTAs that walk over pieces drift apart and then read and
+// write all over memory at once (a billion bfloat16 values: norm and scaling 901 us this way, 1077 with walking CTAs).
+// The norm alone reads 400 MB in 61 us (6.5 TB/s); pieces of 16 KiB rather than 32 are for lists of short tensors
+// (1200 tensors, 80 MB: 43.0 against 43.8 us).
 #include <new>
 #include <vector>
 
@@ -15,10 +18,10 @@ using namespace scar;
 
 namespace {
 
-constexpr int kNormThreads = 512;
-constexpr unsigned kPieceBytes = 32768;  // four 16-byte loads per thread, all in flight together
+constexpr int kNormThreads = 256;
+constexpr unsigned kPieceBytes = 16384;  // four 16-byte loads per thread, all in flight together
 constexpr int kVecs = kPieceBytes / 16 / kNormThreads;
-constexpr unsigned kCtasPerSm = 4;
+constexpr unsigned kCtasPerSm = 8;
 
 struct Piece {
     const void *src;
@@ -168,18 +171,13 @@ template <typename T> __device__ __forceinline__ void scale_piece(const Piece &p
 }
 
 __global__ void __launch_bounds__(kNormThreads, kCtasPerSm)
-k_gnorm_scale(const Piece *__restrict__ pieces, unsigned n_pieces, const NormRecord *rec) {
-    Piece next{};
-    if (blockIdx.x < n_pieces) next = pieces[n_pieces - 1 - blockIdx.x];
+k_gnorm_scale(const Piece *__restrict__ pieces, const NormRecord *rec) {
+    const Piece p = pieces[gridDim.x - 1 - blockIdx.x];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const float coef = (float)rec->coef;
-    for (unsigned i = blockIdx.x; i < n_pieces; i += gridDim.x) {
-        const Piece p = next;
-        if (i + gridDim.x < n_pieces) next = pieces[n_pieces - 1 - (i + gridDim.x)];
-        if (p.dtype == SCAR_F32) scale_piece<float>(p, coef);
-        else if (p.dtype == SCAR_BF16) scale_piece<__nv_bfloat16>(p, coef);
-        else scale_piece<__half>(p, coef);
-    }
+    if (p.dtype == SCAR_F32) scale_piece<float>(p, coef);
+    else if (p.dtype == SCAR_BF16) scale_piece<__nv_bfloat16>(p, coef);
+    else scale_piece<__half>(p, coef);
 }
 
 }  // namespace
@@ -336,7 +334,7 @@ int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm) {
     if ((rc = run_norm(op, max_norm, true, d_norm)) != SCAR_OK) return rc;
     if (op->h_pieces.empty()) return SCAR_OK;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = op->grid;
+    cfg.gridDim = (unsigned)op->h_pieces.size();
     cfg.blockDim = kNormThreads;
     cfg.stream = op->stream;
     cudaLaunchAttribute early{};
@@ -344,7 +342,7 @@ int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm) {
     early.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &early;
     cfg.numAttrs = 1;
-    TRAIN_TRY(cudaLaunchKernelEx(&cfg, k_gnorm_scale, (const Piece *)op->pieces, (unsigned)op->h_pieces.size(), (const NormRecord *)op->rec));
+    TRAIN_TRY(cudaLaunchKernelEx(&cfg, k_gnorm_scale, (const Piece *)op->pieces, (const NormRecord *)op->rec));
     op->launches += 1;
     return SCAR_OK;
 }
