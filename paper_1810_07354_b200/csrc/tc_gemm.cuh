@@ -263,12 +263,12 @@ __device__ __forceinline__ unsigned rows_of(const TcArgs &g) {
 }
 
 struct TileWalk {
-    unsigned m, k, mt, nt, total, kb, splits;
+    unsigned m, mt, nt, total, kb, splits;
     int n_fast;
+    TileWalk() = default;
     __device__ explicit TileWalk(const TcArgs &g) {
-        const unsigned mine = rows_of(g);
+        const unsigned mine = rows_of(g), k = g.dyn == 1 ? mine : g.k;
         m = g.dyn == 0 ? mine : g.m;
-        k = g.dyn == 1 ? mine : g.k;
         mt = (m + kBM - 1) / kBM;
         nt = (g.n + kBN - 1) / kBN;
         splits = pick_splits(g, m, k);
@@ -276,21 +276,39 @@ struct TileWalk {
         kb = (k + kBK - 1) / kBK;
         n_fast = g.n_fast;
     }
-    __device__ void at(unsigned t, unsigned &mi, unsigned &ni, unsigned &s, unsigned &k0, unsigned &k1) const {
-        const unsigned tiles = mt * nt;
-        s = t / tiles;
-        t -= s * tiles;
-        if (n_fast) {
-            ni = t % nt;
-            mi = t / nt;
-        } else {
-            mi = t % mt;
-            ni = t / mt;
-        }
-        k0 = (unsigned)((unsigned long long)kb * s / splits);
-        k1 = (unsigned)((unsigned long long)kb * (s + 1) / splits);
-    }
 };
+
+// One tile (and part of its sum) of a pair's list, the same for all warps of its CTAs.
+struct Turn {
+    unsigned which, mi, ni, s, k0, k1;
+};
+// The i-th turn of a pair, or false at the end of its list.  One product: tiles in rounds over the pairs.  Two products
+// that do not depend on one another, in one launch: the second one's tiles first go, in rounds, to the pairs that have a
+// tile of the first one less than the others and finish early by that; what is left goes in rounds to all.
+template <int N> __device__ __forceinline__ bool take_turn(const TileWalk *w, unsigned i, unsigned pair, unsigned pairs, Turn &t) {
+    unsigned at = pair + i * pairs;
+    t.which = 0;
+    if (at >= w[0].total) {
+        if (N == 1) return false;
+        const unsigned full = w[0].total / pairs, late = w[0].total % pairs;  // pairs below `late` have full + 1 tiles
+        const bool early = late && pair >= late;
+        const unsigned n_early = late ? pairs - late : 0u, j = i - full - (pair < late ? 1u : 0u);
+        const unsigned ahead = late ? min((w[0].kb + 4) / (w[N - 1].kb + 4), w[N - 1].total / n_early) : 0u;
+        if (early && j < ahead) at = (pair - late) + j * n_early;
+        else at = n_early * ahead + (early ? j - ahead : j) * pairs + (early ? pair - late : n_early + pair);
+        if (at >= w[N - 1].total) return false;
+        t.which = N - 1;
+    }
+    const TileWalk &k = w[t.which];
+    const unsigned tiles = k.mt * k.nt;
+    t.s = N == 1 ? at / tiles : 0u;
+    at -= t.s * tiles;
+    t.ni = k.n_fast ? at % k.nt : at / k.mt;
+    t.mi = k.n_fast ? at / k.nt : at % k.mt;
+    t.k0 = (unsigned)((unsigned long long)k.kb * t.s / k.splits);
+    t.k1 = (unsigned)((unsigned long long)k.kb * (t.s + 1) / k.splits);
+    return true;
+}
 
 // ---- Epilogue.  A thread of a warp holds 128 columns of one row.  They go to memory through 4 KiB of shared memory per
 // warp, 128 bytes of 32 rows at a time, so that a store of the warp writes whole lines: rows written straight from their
@@ -564,10 +582,15 @@ __device__ __forceinline__ void epi_prob(const TcArgs &g, float (&v)[kCols], con
     }
 }
 
-template <int PL, bool A_MN, bool B_MN, Epi EPI>
+// N = 2 runs two products with results of their own (kOut): the first one's A is K-major, the second one's MN-major.
+template <int N> struct TcSet {
+    TcArgs p[N];
+};
+template <int PL, bool A_MN, bool B_MN, Epi EPI, int N>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
-k_tc_gemm(const __grid_constant__ TcArgs g) {
+k_tc_gemm(const __grid_constant__ TcSet<N> set) {
     using S = TcShape<PL>;
+    __shared__ TileWalk walks[N];
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ __align__(8) unsigned long long bars[2 * S::kStages + 2 * kAccs];
@@ -603,17 +626,23 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_base;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const TileWalk walk(g);
+    if (warp < N) {
+        const TileWalk w(set.p[warp]);
+        if (lane == 0) walks[warp] = w;
+    }
+    __syncthreads();
+    unsigned *const error = set.p[0].error;
     bool ok = true;
+    Turn t;
 
     if (warp == kEpiWarps) {  // loads
         unsigned st = 0, ph = 0;
-        for (unsigned t = pair; t < walk.total && ok; t += pairs) {
-            unsigned mi, ni, s, k0, k1;
-            walk.at(t, mi, ni, s, k0, k1);
-            const int am = (int)(mi * kBM + rank * 128), bn = (int)(ni * kBN + rank * (kBN / 2));
-            for (unsigned kb = k0; kb < k1; ++kb) {
-                ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * st, ph ^ 1, g.error));
+        for (unsigned i = 0; ok && take_turn<N>(walks, i, pair, pairs, t); ++i) {
+            const TcArgs &g = set.p[N == 1 ? 0 : t.which];
+            const bool a_mn = N == 1 ? A_MN : t.which == 1;
+            const int am = (int)(t.mi * kBM + rank * 128), bn = (int)(t.ni * kBN + rank * (kBN / 2));
+            for (unsigned kb = t.k0; kb < t.k1; ++kb) {
+                ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * st, ph ^ 1, error));
                 if (!ok) break;
                 if (elect_one()) {
                     const uint32_t bar = full + 8 * st, dst = stage0 + st * S::kStageBytes;
@@ -622,7 +651,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
 #pragma unroll
                     for (int p = 0; p < PL; ++p) {
                         const uint32_t da = dst + p * S::kABytes, db = dst + PL * S::kABytes + p * S::kABytes;
-                        if (A_MN) {
+                        if (a_mn) {
                             tma_load(da, &g.a, bar, am, (int)g.a_row0 + kk, p);
                             tma_load(da + 8192, &g.a, bar, am + 64, (int)g.a_row0 + kk, p);
                         } else {
@@ -645,23 +674,23 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
         }
     } else if (warp == kEpiWarps + 1) {  // matrix instructions, first CTA of the pair
         if (rank == 0) {
-            const uint32_t type = g.bf16 ? 1u : 0u;
-            const uint32_t idesc = 1u << 4 | type << 7 | type << 10 | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
-                                   (uint32_t)(kBN >> 3) << 17 | (uint32_t)(kBM >> 4) << 24;
-            const uint64_t desc_a = smem_desc<A_MN>(stage0), desc_b = smem_desc<B_MN>(stage0 + PL * S::kABytes);
+            const uint32_t type = set.p[0].bf16 ? 1u : 0u;
+            const uint32_t idesc0 = 1u << 4 | type << 7 | type << 10 | (B_MN ? 1u << 16 : 0u) | (uint32_t)(kBN >> 3) << 17 | (uint32_t)(kBM >> 4) << 24;
+            const uint64_t desc_b = smem_desc<B_MN>(stage0 + PL * S::kABytes);
             unsigned st = 0, ph = 0, ac = 0, aph = 1;
-            for (unsigned t = pair; t < walk.total && ok; t += pairs) {
-                unsigned mi, ni, s, k0, k1;
-                walk.at(t, mi, ni, s, k0, k1);
+            for (unsigned i = 0; ok && take_turn<N>(walks, i, pair, pairs, t); ++i) {
+                const bool a_mn = N == 1 ? A_MN : t.which == 1;
+                const uint32_t idesc = idesc0 | (a_mn ? 1u << 15 : 0u), a_step = (a_mn ? k_step_bytes<true>() : k_step_bytes<false>()) >> 4;
+                const uint64_t desc_a = a_mn ? smem_desc<true>(stage0) : smem_desc<false>(stage0);
                 unsigned left = 0;  // stages left of the accumulator
-                for (unsigned kb = k0; kb < k1; ++kb) {
+                for (unsigned kb = t.k0; kb < t.k1; ++kb) {
                     const bool fresh = left == 0;
                     if (fresh) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(acc_empty + 8 * ac, aph, g.error));
+                        ok = __all_sync(0xffffffffu, mbar_wait(acc_empty + 8 * ac, aph, error));
                         if (!ok) break;
-                        left = min(kPer, k1 - kb);
+                        left = min(kPer, t.k1 - kb);
                     }
-                    ok = __all_sync(0xffffffffu, mbar_wait(full + 8 * st, ph, g.error));
+                    ok = __all_sync(0xffffffffu, mbar_wait(full + 8 * st, ph, error));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t d = tmem + ac * kBN;
@@ -675,7 +704,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                             const uint64_t db = desc_b + ((st * S::kStageBytes + pb[q] * S::kABytes) >> 4);
 #pragma unroll
                             for (int k = 0; k < kBK / 16; ++k)
-                                mma_pair(d, da + (k * k_step_bytes<A_MN>() >> 4), db + (k * k_step_bytes<B_MN>() >> 4), idesc,
+                                mma_pair(d, da + k * a_step, db + (k * k_step_bytes<B_MN>() >> 4), idesc,
                                          q + k > 0 || !fresh);
                         }
                         mma_commit(empty + 8 * st);
@@ -698,10 +727,9 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
         uint8_t *stage = smem + S::kStages * S::kStageBytes + warp * kWarpStage;
         constexpr bool kRegs = PL == 3 || kLogits;  // sums over rounds, or a whole row at a time: all columns in registers
         unsigned ac = 0, aph = 0;
-        for (unsigned t = pair; t < walk.total; t += pairs) {
-            unsigned mi, ni, s, k0, k1;
-            walk.at(t, mi, ni, s, k0, k1);
-            const unsigned rounds = k1 > k0 ? (kPer == 1 ? k1 - k0 : (k1 - k0 - 1) / kPer + 1) : 0u;
+        for (unsigned i = 0; take_turn<N>(walks, i, pair, pairs, t); ++i) {
+            const TcArgs &g = set.p[N == 1 ? 0 : t.which];
+            const unsigned rounds = t.k1 > t.k0 ? (kPer == 1 ? t.k1 - t.k0 : (t.k1 - t.k0 - 1) / kPer + 1) : 0u;
             const uint32_t lanes = tmem + half * kCols + (quad * 32u << 16);
             if constexpr (kRegs) {
                 float v[kCols];
@@ -711,7 +739,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                 }
                 // the first round is the tile's accumulator itself, later ones are added to it
                 if (rounds) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, g.error));
+                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, error));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -725,7 +753,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                 }
 #pragma unroll 1
                 for (unsigned r = 1; r < rounds; ++r) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, g.error));
+                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, error));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -743,10 +771,10 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                     }
                 }
                 if (!ok) break;
-                const EpiRows rows = epi_rows<EPI>(g, walk.m, mi * kBM + rank * 128 + quad * 32, s, lane);
-                const unsigned col = ni * kBN + half * kCols;
+                const EpiRows rows = epi_rows<EPI>(g, walks[t.which].m, t.mi * kBM + rank * 128 + quad * 32, t.s, lane);
+                const unsigned col = t.ni * kBN + half * kCols;
                 if constexpr (kLogits) {
-                    epi_prob<EPI == Epi::kProb>(g, v, rows, rows.row0 + lane, col, 2 * ni + half, stage, lane);
+                    epi_prob<EPI == Epi::kProb>(g, v, rows, rows.row0 + lane, col, 2 * t.ni + half, stage, lane);
                 } else {
                     const F32Out o = f32_out<EPI>(g);
 #pragma unroll 1
@@ -764,21 +792,21 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                         else if (j == 2) fill(v + 64);
                         else fill(v + 96);
                         if (EPI == Epi::kPart || g.c_map) {
-                            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j * 32), (int)rows.row0, EPI == Epi::kPart ? (int)s : 0);
+                            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j * 32), (int)rows.row0, EPI == Epi::kPart ? (int)t.s : 0);
                         } else {
                             flush_f32<2>(stage, o, rows, col + j * 32, lane);
                         }
                     }
                 }
             } else {
-                const EpiRows rows = epi_rows<EPI>(g, walk.m, mi * kBM + rank * 128 + quad * 32, s, lane);
-                const unsigned col = ni * kBN + half * kCols;
+                const EpiRows rows = epi_rows<EPI>(g, walks[t.which].m, t.mi * kBM + rank * 128 + quad * 32, t.s, lane);
+                const unsigned col = t.ni * kBN + half * kCols;
                 const F32Out o = f32_out<EPI>(g);
                 const bool to16 = EPI == Epi::kOut && g.out_type != SCAR_F32;
                 const bool last16 = to16 && g.acc && g.acc_last, pack16 = to16 && !g.acc;
                 const float f = EPI == Epi::kOut ? out_scale(g) : 1.f;
                 if (rounds) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, g.error));
+                    ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, error));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 }
@@ -810,7 +838,7 @@ k_tc_gemm(const __grid_constant__ TcArgs g) {
                             return make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
                         });
                         if (EPI == Epi::kPart) {
-                            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j), (int)rows.row0, (int)s);
+                            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j), (int)rows.row0, (int)t.s);
                         } else if (last16) flush_last16(stage, g, rows, col + j, f, lane);
                         else flush_f32<8>(stage, o, rows, col + j, lane);
                         j += 32;

@@ -590,27 +590,28 @@ void choose_splits(const scar_xent *op, TcArgs &g) {
     }
 }
 
+uint64_t tiles_of(const TcArgs &g) { return (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + kBN - 1) / kBN) * (g.splits > 1 ? g.most_splits : 1); }
+
 template <int PL, bool A_MN, bool B_MN, Epi EPI> void launch_tc(scar_xent *op, TcArgs g) {
     if (EPI == Epi::kPart) {
         const uint64_t pitch = round_up(g.n, 8);
         if (make_map(op, &g.c, {g.part, pitch, g.m, pitch, g.splits > 1 ? g.most_splits : 1u, g.m * pitch}, 32, 4) != SCAR_OK) op->failed = true;
     }
-    const uint64_t tiles = (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + kBN - 1) / kBN) * (g.splits > 1 ? g.most_splits : 1);
-    const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, op->pairs);
-    if (pairs) launch(op, k_tc_gemm<PL, A_MN, B_MN, EPI>, 2 * pairs, kGemmThreads, kTcSmem, g);
+    const unsigned pairs = (unsigned)std::min<uint64_t>(tiles_of(g), op->pairs);
+    if (pairs) launch(op, k_tc_gemm<PL, A_MN, B_MN, EPI, 1>, 2 * pairs, kGemmThreads, kTcSmem, TcSet<1>{g});
 }
 
-template <int PL, bool A_MN, bool B_MN, Epi EPI> bool allow_smem() {
-    return cudaFuncSetAttribute(k_tc_gemm<PL, A_MN, B_MN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) == cudaSuccess;
+template <typename K> bool allow_smem(K kernel) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) == cudaSuccess;
 }
 template <int PL> bool allow_smem_all() {
-    return allow_smem<PL, false, false, Epi::kPart>() && allow_smem<PL, false, true, Epi::kPart>() && allow_smem<PL, true, true, Epi::kPart>() &&
-           allow_smem<PL, false, true, Epi::kOut>() && allow_smem<PL, true, true, Epi::kOut>();
+    return allow_smem(k_tc_gemm<PL, false, false, Epi::kPart, 1>) && allow_smem(k_tc_gemm<PL, false, true, Epi::kPart, 1>) &&
+           allow_smem(k_tc_gemm<PL, true, true, Epi::kPart, 1>) && allow_smem(k_tc_gemm<PL, false, true, Epi::kOut, 1>) &&
+           allow_smem(k_tc_gemm<PL, true, true, Epi::kOut, 1>) && allow_smem(k_tc_gemm<PL, false, true, Epi::kOut, 2>);
 }
 
-// A product that ends in an output, split over k or not.
-template <int PL, bool A_MN> void launch_out(scar_xent *op, TcArgs g) {
-    choose_splits(op, g);
+// A product that ends in an output, its sum over k split or not.
+template <int PL, bool A_MN> void launch_out(scar_xent *op, const TcArgs &g) {
     if (g.splits == 1) {
         launch_tc<PL, A_MN, true, Epi::kOut>(op, g);
         return;
@@ -618,6 +619,21 @@ template <int PL, bool A_MN> void launch_out(scar_xent *op, TcArgs g) {
     launch_tc<PL, A_MN, true, Epi::kPart>(op, g);
     const uint64_t todo = (uint64_t)g.m * ((g.n + 3) / 4);
     launch(op, k_xent_combine, (unsigned)std::min<uint64_t>((todo + 127) / 128, 32 * op->pairs), 128, 0, g);
+}
+
+// dh and dw of a piece: one launch where neither is split, so that the second one's tiles fill the last round of the
+// first one's (4096 x 32000 x 2048: 120 tiles of 500 stages leave 28 of 74 pairs idle for half of that time).
+// Not where dw goes through the room of w's copy, which dh still reads.
+template <int PL> void launch_grads(scar_xent *op, TcArgs dhg, TcArgs dwg, bool through_w) {
+    choose_splits(op, dhg);
+    choose_splits(op, dwg);
+    if (dhg.splits == 1 && dwg.splits == 1 && !through_w) {
+        const unsigned pairs = (unsigned)std::min<uint64_t>(tiles_of(dhg) + tiles_of(dwg), op->pairs);
+        launch(op, k_tc_gemm<PL, false, true, Epi::kOut, 2>, 2 * pairs, kGemmThreads, kTcSmem, TcSet<2>{{dhg, dwg}});
+        return;
+    }
+    launch_out<PL, false>(op, dhg);
+    launch_out<PL, true>(op, dwg);
 }
 
 template <typename T>
@@ -713,7 +729,6 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
             dhg.out_pitch = dhp;
             dhg.out_vec = rows_aligned(dh, dhp, sizeof(T));
             dhg.row_map = op->row_of;
-            launch_out<PL, false>(op, dhg);
         }
         fill(dwg, V, D, rows, 1);
         dwg.b_row0 = at;
@@ -738,7 +753,12 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
         }
         dwg.c_map = !dwg.acc && (through_w || (dwg.out_vec && D * sizeof(T) % 16 == 0));
         if (dwg.c_map && (rc = make_map(op, &dwg.c, {dwg.out, D, V, dwg.out_pitch, 1, 0}, 32, sizeof(T))) != SCAR_OK) return rc;
-        launch_out<PL, true>(op, dwg);
+        if (rows) {
+            launch_grads<PL>(op, dhg, dwg, through_w);
+        } else {
+            choose_splits(op, dwg);
+            launch_out<PL, true>(op, dwg);
+        }
         if (through_w)
             launch(op, k_xent_unplace<T>, (unsigned)std::min<uint64_t>((V + 7) / 8, 16 * op->pairs), 256, 0, reinterpret_cast<const T *>(op->w), op->dp, V, D, dw, dwp);
         if ((uint64_t)at + op->piece >= n) break;
@@ -827,7 +847,7 @@ int scar_xent_init(scar_xent **out, const scar_xent_config *cfg, void *cuda_stre
         if (found != cudaDriverEntryPointSuccess || !fn) return SCAR_ERR_CUDA;
         op->encode = reinterpret_cast<EncodeTiled>(fn);
         if (cfg->dtype == SCAR_F32 ? !(allow_smem_all<3>())
-                                   : !(allow_smem_all<1>() && allow_smem<1, false, false, Epi::kProb>() && allow_smem<1, false, false, Epi::kStat>()))
+                                   : !(allow_smem_all<1>() && allow_smem(k_tc_gemm<1, false, false, Epi::kProb, 1>) && allow_smem(k_tc_gemm<1, false, false, Epi::kStat, 1>)))
             return SCAR_ERR_CUDA;
         int sms = 0;
         TRAIN_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, op->device));
