@@ -1,6 +1,6 @@
 // Linear softmax cross entropy with its gradient (scar_xent_* of scar.h).
 //
-// A call:  rows that count are listed (k_xent_rows) and copied together (k_xent_place; float32 is split into three
+// A call:  rows that count are listed and copied together (k_xent_rows, k_xent_place; float32 is split into three
 // bfloat16 planes on the way, w too).  The rows then go through the products in pieces:
 //   z = h w^T        the product's epilogue keeps, per row and 128 classes, the maximum and the sum of exponentials, and
 //                    for gradients the exponentials relative to that maximum, in float16 (k_tc_gemm, kProb / kStat)
@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kRowThreads = 1024;
 constexpr unsigned kNone = 0xffffffffu;
+constexpr unsigned kWarpRow = 2048;  // rows of up to this many classes have a warp of the softmax kernels each, longer ones a CTA
 
 struct XentRecord {
     float loss;
@@ -35,32 +36,40 @@ __device__ __forceinline__ void griddep_start() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// Compacts the rows that count, in order: row_of[0 .. rows) are their numbers, pos is the inverse (kNone for the rest).
-// One CTA, eight neighbouring labels per thread at a time: the labels of a step are few.
+// Lists the rows that count, in order: row_of[0 .. rows) are their numbers, pos is the inverse (kNone for the rest).  By one
+// CTA of kThreads, eight neighbouring labels per thread at a time: the labels of a step are few.
 constexpr int kLabels = 8;
-__global__ void __launch_bounds__(kRowThreads)
-k_xent_rows(const long long *__restrict__ labels, unsigned n, long long ignore, unsigned n_classes,
-            unsigned *__restrict__ row_of, unsigned *__restrict__ pos, int *__restrict__ label, float *__restrict__ row_loss,
-            XentRecord *rec, float *d_loss) {
-    __shared__ unsigned sh[kRowThreads / 32], n_ign, n_bad;
-    griddep_start();
+struct RowList {
+    const long long *labels;
+    unsigned n;
+    long long ignore;
+    unsigned n_classes;
+    unsigned *row_of, *pos;
+    int *label;
+    float *row_loss;
+    XentRecord *rec;
+    float *d_loss;
+};
+template <int kThreads, bool kWrite> __device__ __forceinline__ unsigned list_rows(const RowList &q, unsigned *pos) {
+    __shared__ unsigned sh[32], n_ign, n_bad;
     if (threadIdx.x == 0) n_ign = n_bad = 0;
+    if (threadIdx.x < 32) sh[threadIdx.x] = 0;
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned base = 0, ign = 0, bad = 0;
-    for (unsigned long long at = 0; at < n; at += kRowThreads * kLabels) {
+    for (unsigned long long at = 0; at < q.n; at += kThreads * kLabels) {
         const unsigned long long t0 = at + threadIdx.x * kLabels;
         long long y[kLabels];
         unsigned keep = 0;
 #pragma unroll
-        for (int i = 0; i < kLabels; ++i) y[i] = t0 + i < n ? labels[t0 + i] : ignore;
+        for (int i = 0; i < kLabels; ++i) y[i] = t0 + i < q.n ? q.labels[t0 + i] : q.ignore;
 #pragma unroll
         for (int i = 0; i < kLabels; ++i) {
-            if (t0 + i >= n) continue;
-            if (y[i] == ignore) ++ign;
-            else if (y[i] >= 0 && y[i] < (long long)n_classes) keep |= 1u << i;
+            if (t0 + i >= q.n) continue;
+            if (y[i] == q.ignore) ++ign;
+            else if (y[i] >= 0 && y[i] < (long long)q.n_classes) keep |= 1u << i;
             else ++bad;
             if (!(keep >> i & 1u)) {
-                row_loss[t0 + i] = 0.f;
+                if (kWrite) q.row_loss[t0 + i] = 0.f;
                 pos[t0 + i] = kNone;
             }
         }
@@ -80,24 +89,33 @@ k_xent_rows(const long long *__restrict__ labels, unsigned n, long long ignore, 
 #pragma unroll
         for (int i = 0; i < kLabels; ++i) {
             if (!(keep >> i & 1u)) continue;
-            row_of[r] = (unsigned)(t0 + i);
-            label[r] = (int)y[i];
+            if (kWrite) {
+                q.row_of[r] = (unsigned)(t0 + i);
+                q.label[r] = (int)y[i];
+            }
             pos[t0 + i] = r++;
         }
     }
     __syncthreads();
-    if (ign) atomicAdd(&n_ign, ign);
-    if (bad) atomicAdd(&n_bad, bad);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        rec->rows = base;
-        rec->ignored = n_ign;
-        rec->bad = n_bad;
-        rec->error = 0;
-        rec->done = 0;
-        rec->loss = 0.f;
-        if (d_loss && n == 0) *d_loss = 0.f;
+    if (kWrite) {
+        if (ign) atomicAdd(&n_ign, ign);
+        if (bad) atomicAdd(&n_bad, bad);
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            q.rec->rows = base;
+            q.rec->ignored = n_ign;
+            q.rec->bad = n_bad;
+            q.rec->error = 0;
+            q.rec->done = 0;
+            q.rec->loss = 0.f;
+            if (q.d_loss && q.n == 0) *q.d_loss = 0.f;
+        }
     }
+    return base;
+}
+__global__ void __launch_bounds__(kRowThreads) k_xent_rows(RowList q) {
+    griddep_start();
+    list_rows<kRowThreads, true>(q, q.pos);
 }
 
 union Eight {
@@ -142,63 +160,86 @@ __device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, unsigne
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Copies rows into the layout the products read: rows of dp elements (zeros behind the last), 16-byte aligned, one plane
-// for the 16-bit types and three for float32.  With `pos`, row t goes to pos[t]; rows that do not count are left out and
-// their row of `zero` (dh) is cleared, and the rows behind the last one are zero up to a multiple of 64.
-template <typename T>
+// Rows and where they are copied to in the layout the products read: rows of dp elements (zeros behind the last),
+// 16-byte aligned, one plane for the 16-bit types and three for float32.
+template <typename T> struct Copy {
+    const T *src;
+    unsigned long long pitch;
+    unsigned n;
+    bool vec;  // rows of src on 16-byte boundaries
+    unsigned short *dst;
+    unsigned long long plane;
+};
+// Eight elements from column c of row r to row `to`.
+template <typename T> __device__ __forceinline__ void copy_eight(const Copy<T> &q, unsigned r, unsigned to, unsigned c, unsigned d, unsigned dp) {
+    const T *s = q.src + r * q.pitch + c;
+    unsigned short *o = q.dst + (unsigned long long)to * dp + c;
+    if constexpr (sizeof(T) == 2) {
+        Eight x;
+        const unsigned by = (unsigned)(uintptr_t)s & 15u;
+        if (q.vec && c + 8 <= d) x.u = *reinterpret_cast<const uint4 *>(s);
+        else if (c && c + 16 <= d) {  // the two aligned words that hold it lie within the row
+            const uint4 *a = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(s) - by);
+            x.u = by ? shifted(a[0], a[1], by) : a[0];
+        } else
+            for (int j = 0; j < 8; ++j) x.s[j] = c + j < d ? reinterpret_cast<const unsigned short *>(s)[j] : (unsigned short)0;
+        *reinterpret_cast<uint4 *>(o) = x.u;
+    } else {
+        float x[8];
+        if (q.vec && c + 8 <= d) {
+            const float4 a = *reinterpret_cast<const float4 *>(s), b = *reinterpret_cast<const float4 *>(s + 4);
+            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+            x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        } else {
+            for (int j = 0; j < 8; ++j) x[j] = c + j < d ? s[j] : 0.f;
+        }
+        Eight p[3];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) split3(x[j], p[0].b[j], p[1].b[j], p[2].b[j]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4 *>(o + k * q.plane) = p[k].u;
+    }
+}
+
+// Row t of h goes to pos[t]; rows that do not count are left out and their row of `zero` (dh) is cleared, and the rows
+// behind the last one are zero up to a multiple of 64.  Then w, where it has to be copied.  SCAN: every CTA lists the rows
+// itself (the first one for all to come), which for up to kScanRows of them takes less time than a launch, unless the copies
+// are what takes the time (kScanGroups groups of eight elements: 16 MB of 16-bit values).
+constexpr unsigned kScanRows = 2048, kScanGroups = 1u << 20;
+template <typename T, bool SCAN>
 __global__ void __launch_bounds__(256)
-k_xent_place(const T *__restrict__ src, unsigned long long pitch, unsigned n, unsigned d, unsigned dp, bool vec,
-             unsigned short *__restrict__ dst, unsigned long long plane, const unsigned *__restrict__ pos,
-             const unsigned *__restrict__ rows, T *__restrict__ zero, unsigned long long zero_pitch) {
+k_xent_place(RowList q, Copy<T> h, Copy<T> w, unsigned d, unsigned dp, T *__restrict__ zero, unsigned long long zero_pitch) {
+    __shared__ unsigned spos[SCAN ? kScanRows : 1];
     griddep_start();
-    const unsigned groups = dp / 8;
-    const unsigned long long total = (unsigned long long)(n + (pos ? 64u : 0u)) * groups;
-    for (unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 256) {
+    unsigned rows;
+    if constexpr (SCAN) {
+        static_assert(kScanRows == 256 * kLabels, "one round of labels");
+        rows = blockIdx.x == 0 ? list_rows<256, true>(q, spos) : list_rows<256, false>(q, spos);
+        __syncthreads();
+    } else {
+        rows = q.rec->rows;
+    }
+    const unsigned groups = dp / 8, pad = (rows + 63) / 64 * 64;
+    const unsigned long long total = (unsigned long long)(h.n + 64u) * groups, step = (unsigned long long)gridDim.x * 256;
+    unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
+    for (; i < total; i += step) {
         const unsigned r = total >> 32 ? (unsigned)(i / groups) : (unsigned)i / groups;
         const unsigned c = (unsigned)(i - (unsigned long long)r * groups) * 8;
-        unsigned to = r;
-        if (pos) {
-            if (r >= n) {
-                to = *rows + (r - n);
-                if (to >= (*rows + 63) / 64 * 64) continue;
-                for (int p = 0; p < (sizeof(T) == 4 ? 3 : 1); ++p)
-                    *reinterpret_cast<uint4 *>(dst + p * plane + (unsigned long long)to * dp + c) = make_uint4(0, 0, 0, 0);
-                continue;
-            }
-            to = pos[r];
-            if (to == kNone) {
-                if (zero)
-                    for (unsigned j = 0; j < 8 && c + j < d; ++j) zero[r * zero_pitch + c + j] = from_f32<T>(0.f);
-                continue;
-            }
+        if (r >= h.n) {
+            const unsigned to = rows + (r - h.n);
+            if (to < pad)
+                for (int p = 0; p < (sizeof(T) == 4 ? 3 : 1); ++p) *reinterpret_cast<uint4 *>(h.dst + p * h.plane + (unsigned long long)to * dp + c) = make_uint4(0, 0, 0, 0);
+            continue;
         }
-        const T *s = src + r * pitch + c;
-        unsigned short *o = dst + (unsigned long long)to * dp + c;
-        if constexpr (sizeof(T) == 2) {
-            Eight x;
-            const unsigned by = (unsigned)(uintptr_t)s & 15u;
-            if (vec && c + 8 <= d) x.u = *reinterpret_cast<const uint4 *>(s);
-            else if (c && c + 16 <= d) {  // the two aligned words that hold it lie within the row
-                const uint4 *a = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(s) - by);
-                x.u = by ? shifted(a[0], a[1], by) : a[0];
-            } else
-                for (int j = 0; j < 8; ++j) x.s[j] = c + j < d ? reinterpret_cast<const unsigned short *>(s)[j] : (unsigned short)0;
-            *reinterpret_cast<uint4 *>(o) = x.u;
-        } else {
-            float x[8];
-            if (vec && c + 8 <= d) {
-                const float4 a = *reinterpret_cast<const float4 *>(s), b = *reinterpret_cast<const float4 *>(s + 4);
-                x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-                x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-            } else {
-                for (int j = 0; j < 8; ++j) x[j] = c + j < d ? s[j] : 0.f;
-            }
-            Eight p[3];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) split3(x[j], p[0].b[j], p[1].b[j], p[2].b[j]);
-#pragma unroll
-            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(o + q * plane) = p[q].u;
-        }
+        const unsigned to = SCAN ? spos[r] : q.pos[r];
+        if (to != kNone) copy_eight(h, r, to, c, d, dp);
+        else if (zero)
+            for (unsigned j = 0; j < 8 && c + j < d; ++j) zero[r * zero_pitch + c + j] = from_f32<T>(0.f);
+    }
+    const unsigned long long more = (unsigned long long)w.n * groups;
+    for (i -= total; i < more; i += step) {
+        const unsigned r = more >> 32 ? (unsigned)(i / groups) : (unsigned)i / groups;
+        copy_eight(w, r, r, (unsigned)(i - (unsigned long long)r * groups) * 8, d, dp);
     }
 }
 
@@ -273,53 +314,75 @@ __device__ __forceinline__ void finish_loss(const LossOut &o) {
     if (o.d_loss) *o.d_loss = o.rec->loss;
 }
 
-// One CTA per row of the piece: joins the row's groups of 128 classes to lse and the loss; with GRAD turns the row's
-// scaled exponentials into dz in place.  Rows behind the last one up to a multiple of 64 become zero (the dw product
-// runs over whole groups of 64 rows).
-template <bool GRAD>
+// Maximum and sum over the NT threads of a row: a warp, or the CTA of 256.
+template <int NT> __device__ __forceinline__ float row_max(float v, float *sh) {
+    if constexpr (NT == 256) v = cta_max(v, sh);
+    for (int o = NT == 256 ? 0 : 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+template <int NT> __device__ __forceinline__ float row_add(float v, float *sh) {
+    if constexpr (NT == 256) v = cta_add(v, sh);
+    for (int o = NT == 256 ? 0 : 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <int NT> __device__ __forceinline__ void zero_row(const DzOut &o, unsigned short *row, unsigned tid) {
+    for (int q = 0; q < (o.dt == SCAR_F32 ? 3 : 1); ++q)
+        for (unsigned v = tid * 8; v < o.pitch; v += NT * 8) *reinterpret_cast<uint4 *>(row + q * o.plane + v) = make_uint4(0, 0, 0, 0);
+}
+
+// NT threads (the CTA of 256, or a warp of it) per row of the piece: join the row's groups of 128 classes to lse and the
+// loss; with GRAD they turn the row's scaled exponentials into dz in place.  Rows behind the last one up to a multiple of
+// 64 become zero (the dw product runs over whole groups of 64 rows).  Bound by HBM: 2 bytes read and 2 written per value.
+template <bool GRAD, int NT>
 __global__ void __launch_bounds__(256)
 k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups, const int *__restrict__ label,
           const float *__restrict__ label_z, const unsigned *__restrict__ row_of, Piece p, float *row_loss, LossOut loss) {
     __shared__ float sh[8];
     griddep_start();
-    const unsigned r = blockIdx.x, R = p.rows(loss.rec);
-    unsigned short *row = GRAD ? o.dz + (unsigned long long)r * o.pitch : nullptr;
-    if (r >= R) {
-        if (GRAD && r < (R + 63) / 64 * 64)
-            for (unsigned v = threadIdx.x * 8; v < o.pitch; v += 256 * 8) *reinterpret_cast<uint4 *>(row + v) = make_uint4(0, 0, 0, 0);
-        finish_loss(loss);
-        return;
-    }
+    const unsigned r = blockIdx.x * (256 / NT) + threadIdx.x / NT, tid = threadIdx.x % NT, R = p.rows(loss.rec);
     const float2 *st = stat + (unsigned long long)r * groups;
-    float top = -INFINITY, s = 0.f;
-    for (unsigned i = threadIdx.x; i < groups; i += 256) top = fmaxf(top, st[i].y > 0.f ? st[i].x : -INFINITY);
-    top = cta_max(top, sh);
-    for (unsigned i = threadIdx.x; i < groups; i += 256) {
-        const float2 e = st[i];
-        if (e.y != 0.f) s = fmaf(e.y, expf(e.x - top), s);  // a NaN sum goes through
+    float lse = 0.f, zl = 0.f;
+    if (r < R) {
+        float top = -INFINITY, s = 0.f;
+#pragma unroll 2
+        for (unsigned i = tid; i < groups; i += NT) {
+            const float2 e = st[i];
+            top = fmaxf(top, e.y > 0.f ? e.x : -INFINITY);
+        }
+        top = row_max<NT>(top, sh);
+#pragma unroll 2
+        for (unsigned i = tid; i < groups; i += NT) {
+            const float2 e = st[i];
+            if (e.y != 0.f) s = fmaf(e.y, expf(e.x - top), s);  // a NaN sum goes through
+        }
+        s = row_add<NT>(s, sh);
+        lse = top + logf(s * (1.f / kProbScale));
+        zl = label_z[p.first + r];
+        if (tid == 0) row_loss[row_of[p.first + r]] = lse - zl;
     }
-    s = cta_add(s, sh);
-    const float lse = top + logf(s * (1.f / kProbScale));
-    const float zl = label_z[p.first + r];
-    if (threadIdx.x == 0) row_loss[row_of[p.first + r]] = lse - zl;
     finish_loss(loss);
     if (!GRAD) return;
+    unsigned short *row = o.dz + (unsigned long long)r * o.pitch;
+    if (r >= R) {
+        if (r < (R + 63) / 64 * 64) zero_row<NT>(o, row, tid);
+        return;
+    }
     const unsigned y = (unsigned)label[p.first + r];
     const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
-    constexpr int kBatch = 4;  // 16-byte loads of a thread in flight
-    for (unsigned v0 = threadIdx.x * 8; v0 < V; v0 += kBatch * 256 * 8) {
+    constexpr int kBatch = NT == 256 ? 4 : 2;  // 16-byte loads of a thread in flight
+    for (unsigned v0 = tid * 8; v0 < V; v0 += kBatch * NT * 8) {
         Eight x[kBatch];
         float2 e[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            const unsigned v = v0 + i * 256 * 8;
+            const unsigned v = v0 + i * NT * 8;
             if (v >= V) break;
             x[i].u = __ldcs(reinterpret_cast<const uint4 *>(row + v));
             e[i] = st[v >> 7];
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            const unsigned v = v0 + i * 256 * 8;
+            const unsigned v = v0 + i * NT * 8;
             if (v >= V) break;
             const float f = e[i].y != 0.f ? expf(e[i].x - lse) * (held / kProbScale) : 0.f;
             float w[8];
@@ -342,58 +405,59 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
 
 // The same from float32 logits of the piece in parts (their sum replaces the first part): one pass for the running
 // maximum and sum of every thread, one for dz.
-template <bool GRAD>
+template <bool GRAD, int NT>
 __global__ void __launch_bounds__(256)
 k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict__ label, const unsigned *__restrict__ row_of, float *row_loss, LossOut loss) {
     __shared__ float sh[8];
     griddep_start();
-    const unsigned r = blockIdx.x, R = rows_of(g), V = g.n, pitch = (V + 7) & ~7u;
-    unsigned short *row = GRAD ? o.dz + (unsigned long long)r * o.pitch : nullptr;
-    const int planes = o.dt == SCAR_F32 ? 3 : 1;
-    if (r >= R) {
-        if (GRAD && r < (R + 63) / 64 * 64)
-            for (int q = 0; q < planes; ++q)
-                for (unsigned v = threadIdx.x * 8; v < o.pitch; v += 256 * 8)
-                    *reinterpret_cast<uint4 *>(row + q * o.plane + v) = make_uint4(0, 0, 0, 0);
-        finish_loss(loss);
-        return;
-    }
+    const unsigned r = blockIdx.x * (256 / NT) + threadIdx.x / NT, tid = threadIdx.x % NT, R = rows_of(g), V = g.n, pitch = (V + 7) & ~7u;
     const unsigned splits = pick_splits(g, R, g.k);
     const unsigned long long stride = (unsigned long long)g.m * pitch;
     float *z = g.part + (unsigned long long)r * pitch;
-    float top = -INFINITY, s = 0.f;
+    float lse = 0.f, zl = 0.f;
+    unsigned y = 0;
+    if (r < R) {
+        float top = -INFINITY, s = 0.f;
 #pragma unroll 2
-    for (unsigned v = threadIdx.x * 4; v < V; v += 256 * 4) {
-        float4 a = *reinterpret_cast<const float4 *>(z + v);
-        if (splits > 1) {
+        for (unsigned v = tid * 4; v < V; v += NT * 4) {
+            float4 a = *reinterpret_cast<const float4 *>(z + v);
+            if (splits > 1) {
 #pragma unroll 4
-            for (unsigned q = 1; q < splits; ++q) {
-                const float4 b = *reinterpret_cast<const float4 *>(z + q * stride + v);
-                a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+                for (unsigned q = 1; q < splits; ++q) {
+                    const float4 b = *reinterpret_cast<const float4 *>(z + q * stride + v);
+                    a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+                }
+                *reinterpret_cast<float4 *>(z + v) = a;
             }
-            *reinterpret_cast<float4 *>(z + v) = a;
-        }
-        const float x[4] = {a.x, v + 1 < V ? a.y : -INFINITY, v + 2 < V ? a.z : -INFINITY, v + 3 < V ? a.w : -INFINITY};
-        const float t = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-        if (t > top) {
-            s *= expf(top - t);
-            top = t;
-        }
-        const float ref = top == -INFINITY ? 0.f : top;
+            const float x[4] = {a.x, v + 1 < V ? a.y : -INFINITY, v + 2 < V ? a.z : -INFINITY, v + 3 < V ? a.w : -INFINITY};
+            const float t = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+            if (t > top) {
+                s *= expf(top - t);
+                top = t;
+            }
+            const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s += expf(x[i] - ref);
+            for (int i = 0; i < 4; ++i) s += expf(x[i] - ref);
+        }
+        const float all = row_max<NT>(top, sh);
+        const float ref = all == -INFINITY ? 0.f : all;
+        s = row_add<NT>(s != 0.f ? s * expf((top == -INFINITY ? 0.f : top) - ref) : 0.f, sh);
+        lse = ref + logf(s);
+        y = (unsigned)label[g.first + r];
+        __syncwarp();
+        zl = z[y];
+        if (tid == 0) row_loss[row_of[g.first + r]] = lse - zl;
     }
-    const float all = cta_max(top, sh);
-    const float ref = all == -INFINITY ? 0.f : all;
-    s = cta_add(s != 0.f ? s * expf((top == -INFINITY ? 0.f : top) - ref) : 0.f, sh);
-    const float lse = ref + logf(s);
-    const unsigned y = (unsigned)label[g.first + r];
-    const float zl = z[y];
-    if (threadIdx.x == 0) row_loss[row_of[g.first + r]] = lse - zl;
     finish_loss(loss);
     if (!GRAD) return;
+    unsigned short *row = o.dz + (unsigned long long)r * o.pitch;
+    if (r >= R) {
+        if (r < (R + 63) / 64 * 64) zero_row<NT>(o, row, tid);
+        return;
+    }
     const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
-    for (unsigned v = threadIdx.x * 8; v < V; v += 256 * 8) {
+#pragma unroll 2
+    for (unsigned v = tid * 8; v < V; v += NT * 8) {
         const float4 a = *reinterpret_cast<const float4 *>(z + v), b = *reinterpret_cast<const float4 *>(z + v + 4);
         const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         Eight w[3];
@@ -405,7 +469,7 @@ k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict_
             else if (o.dt == SCAR_F16) w[0].h[j] = __float2half_rn(d);
             else w[0].b[j] = __float2bfloat16_rn(d);
         }
-        for (int q = 0; q < planes; ++q) *reinterpret_cast<uint4 *>(row + q * o.plane + v) = w[q].u;
+        for (int q = 0; q < (o.dt == SCAR_F32 ? 3 : 1); ++q) *reinterpret_cast<uint4 *>(row + q * o.plane + v) = w[q].u;
     }
 }
 
@@ -664,13 +728,17 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
         if ((rc = make_map(op, &logits.b, ow, kBN / 2)) != SCAR_OK || (grad && (rc = make_map(op, &dhg.b, ow, 64)) != SCAR_OK)) return rc;
     }
 
-    launch(op, k_xent_rows, 1, kRowThreads, 0, y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec, d_loss);
-    const unsigned most_ctas = 16 * op->pairs;
-    auto ctas = [&](uint64_t rows) { return (unsigned)std::min<uint64_t>((rows * (op->dp / 8) + 255) / 256, most_ctas); };
-    launch(op, k_xent_place<T>, ctas(n + 64), 256, 0, h, hp, n, D, (unsigned)op->dp, rows_aligned(h, hp, sizeof(T)), op->h, op->h_rows * op->dp, op->pos, &op->rec->rows,
-           grad ? dh : nullptr, dhp);
-    if (w_copied)
-        launch(op, k_xent_place<T>, ctas(V), 256, 0, w, wp, V, D, (unsigned)op->dp, rows_aligned(w, wp, sizeof(T)), op->w, (uint64_t)V * op->dp, nullptr, nullptr, nullptr, 0);
+    const RowList list{y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec, d_loss};
+    const Copy<T> ch{h, hp, n, rows_aligned(h, hp, sizeof(T)), op->h, op->h_rows * op->dp};
+    const Copy<T> cw{w, wp, w_copied ? V : 0u, rows_aligned(w, wp, sizeof(T)), op->w, (uint64_t)V * op->dp};
+    const uint64_t groups = ((uint64_t)n + 64 + cw.n) * (op->dp / 8);
+    const unsigned place_ctas = (unsigned)std::min<uint64_t>((groups + 255) / 256, 16 * op->pairs);
+    if (n <= kScanRows && groups <= kScanGroups) {
+        launch(op, k_xent_place<T, true>, place_ctas, 256, 0, list, ch, cw, D, (unsigned)op->dp, grad ? dh : nullptr, dhp);
+    } else {
+        launch(op, k_xent_rows, 1, kRowThreads, 0, list);
+        launch(op, k_xent_place<T, false>, place_ctas, 256, 0, list, ch, cw, D, (unsigned)op->dp, grad ? dh : nullptr, dhp);
+    }
 
     TcArgs base{};
     base.rows = &op->rec->rows;
@@ -708,18 +776,18 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
             logits.label = op->label;
             logits.label_z = op->label_z;
             choose_splits(op, logits);
+            // a warp per row where there are rows for a CTA of them on every SM, and a row is short or only its groups are read
+            const bool many = rows >= 16 * op->pairs, short_rows = many && V <= kWarpRow, warps = short_rows || (many && !grad);
+            const unsigned ctas = warps ? (rows64 + 7) / 8 : rows64;
             if (PL == 3 || logits.splits > 1) {
                 launch_tc<PL, false, false, Epi::kPart>(op, logits);
-                if (grad) launch(op, k_xent_softmax<true>, rows64, 256, 0, logits, dz, op->label, op->row_of, row_loss, loss);
-                else launch(op, k_xent_softmax<false>, rows, 256, 0, logits, dz, op->label, op->row_of, row_loss, loss);
+                auto kernel = short_rows ? (grad ? k_xent_softmax<true, 32> : k_xent_softmax<false, 32>) : (grad ? k_xent_softmax<true, 256> : k_xent_softmax<false, 256>);
+                launch(op, kernel, short_rows ? (rows64 + 7) / 8 : rows64, 256, 0, logits, dz, op->label, op->row_of, row_loss, loss);
             } else if constexpr (PL == 1) {
-                if (grad) {
-                    launch_tc<1, false, false, Epi::kProb>(op, logits);
-                    launch(op, k_xent_dz<true>, rows64, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, p, row_loss, loss);
-                } else {
-                    launch_tc<1, false, false, Epi::kStat>(op, logits);
-                    launch(op, k_xent_dz<false>, rows, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, p, row_loss, loss);
-                }
+                if (grad) launch_tc<1, false, false, Epi::kProb>(op, logits);
+                else launch_tc<1, false, false, Epi::kStat>(op, logits);
+                auto kernel = warps ? (grad ? k_xent_dz<true, 32> : k_xent_dz<false, 32>) : (grad ? k_xent_dz<true, 256> : k_xent_dz<false, 256>);
+                launch(op, kernel, ctas, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, p, row_loss, loss);
             }
         }
         if (!grad) continue;
