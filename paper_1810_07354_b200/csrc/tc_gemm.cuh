@@ -60,6 +60,7 @@ struct TcArgs {
     unsigned pairs;          // CTA pairs the GPU holds
     unsigned most_splits;    // that fit the buffer of parts
     int planes;
+    float join_s;            // time of the launch that joins parts
     int n_fast;              // tiles of one row of tiles run first (B is the smaller operand and stays in L2)
     int bf16;
     unsigned *error;
@@ -230,12 +231,13 @@ __device__ __forceinline__ void acc_release(uint32_t bar, unsigned lane) {
 
 // How many parts to cut the sum over k into.  In units of one pair's 64 values of k (0.28 us; six times that for planes):
 // a wave of tiles costs its length and about four for the exposed part of its epilogue; parts cost their way through
-// memory (6.5 TB/s) and the launch that joins them (about 3 us).
-__host__ __device__ inline float split_cost(unsigned s, unsigned long long tiles, unsigned kb, unsigned pairs, float out_bytes, int planes) {
-    const float unit = planes == 3 ? 1.7e-6f : 0.28e-6f;
+// memory (6.5 TB/s) and, where one is needed, the launch that joins them (`join_s`: about 5 us in a chain of launches).
+constexpr float kLaunchS = 5e-6f;
+__host__ __device__ inline float unit_s(int planes) { return planes == 3 ? 1.7e-6f : 0.28e-6f; }
+__host__ __device__ inline float split_cost(unsigned s, unsigned long long tiles, unsigned kb, unsigned pairs, float out_bytes, float join_s, int planes) {
     const float waves = (float)((tiles * s + pairs - 1) / pairs);
     const float cost = waves * ((float)((kb + s - 1) / s) + 4.f);
-    return s == 1 ? cost : cost * 1.03f + (3e-6f + out_bytes * (float)(2 * s) / 6.5e12f) / unit;
+    return s == 1 ? cost : cost * 1.03f + (join_s + out_bytes * (float)(2 * s) / 6.5e12f) / unit_s(planes);
 }
 __host__ __device__ inline unsigned tiles_of(unsigned m, unsigned n) { return (unsigned)(((unsigned long long)m + kBM - 1) / kBM * (((unsigned long long)n + kBN - 1) / kBN)); }
 constexpr unsigned kMostSplits = 32;
@@ -244,7 +246,7 @@ constexpr unsigned kMostSplits = 32;
 __device__ __forceinline__ unsigned pick_splits(const TcArgs &g, unsigned m, unsigned k) {
     if (g.splits == 1) return 1;
     const unsigned s = (threadIdx.x & 31) + 1, kb = (k + kBK - 1) / kBK;
-    float cost = s <= g.most_splits && s <= max(kb, 1u) ? split_cost(s, tiles_of(m, g.n), kb, g.pairs, (float)m * (float)g.n * 4.f, g.planes) : INFINITY;
+    float cost = s <= g.most_splits && s <= max(kb, 1u) ? split_cost(s, tiles_of(m, g.n), kb, g.pairs, (float)m * (float)g.n * 4.f, g.join_s, g.planes) : INFINITY;
     unsigned best = s;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -540,18 +542,15 @@ __device__ __forceinline__ uint4 pack_bf8(const float *v) {
     return x.u;
 }
 
-// One row's 128 logits of this thread: their maximum, the sum of their exponentials relative to it, the label's logit,
-// and with STORE the exponentials themselves.  A group whose maximum is -inf is taken relative to 0 (all zeros).
-template <bool STORE>
-__device__ __forceinline__ void epi_prob(const TcArgs &g, float (&v)[kCols], const EpiRows &rows, unsigned row, unsigned col, unsigned group, uint8_t *stage,
-                                         unsigned lane) {
+// One row's 128 logits of this thread: their maximum, the sum of their exponentials relative to it, the label's logit; with
+// KEEP the exponentials take the logits' place.  A group whose maximum is -inf is taken relative to 0 (all zeros).
+template <bool KEEP> __device__ __forceinline__ void epi_stat(const TcArgs &g, float (&v)[kCols], bool mine, unsigned row, unsigned col, unsigned group) {
     const unsigned left = g.n > col ? g.n - col : 0u;
     if (left < kCols) {
 #pragma unroll
         for (int j = 0; j < kCols; ++j)
             if (j >= left) v[j] = -INFINITY;
     }
-    const bool mine = row < rows.m;
     const unsigned at = mine ? (unsigned)g.label[g.first + row] - col : 0xffffffffu;
     if (at < kCols) {
         float z = 0.f;
@@ -567,18 +566,25 @@ __device__ __forceinline__ void epi_prob(const TcArgs &g, float (&v)[kCols], con
 #pragma unroll
     for (int j = 0; j < kCols; ++j) {
         // the difference first: it is small where the exponential is not, and so is its rounding
-        v[j] = ex2(fmaf(v[j] - ref, kLog2e, kProbLog2));
-        s[j & 3] += v[j];
+        const float e = ex2(fmaf(v[j] - ref, kLog2e, kProbLog2));
+        s[j & 3] += e;
+        if (KEEP) v[j] = e;
     }
     if (mine) g.stat[(unsigned long long)row * g.stat_pitch + group] = make_float2(ref, (s[0] + s[1]) + (s[2] + s[3]));
-    if constexpr (STORE) {
-#pragma unroll 1
-        for (int j = 0; j < 2; ++j) {
-            if (j * 64 >= left) break;
-            if (j == 0) stage_fill(stage, lane, [&](int c) { return pack_half8(v + c * 8); });
-            else stage_fill(stage, lane, [&](int c) { return pack_half8(v + 64 + c * 8); });
-            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j * 64), (int)rows.row0, 0);
-        }
+}
+
+// Packed 16-bit values of 32 rows x 64 columns to memory through the result's map, 32 columns at a time: the two halves of
+// the warp's stage alternate, so that one is filled while the other is read.
+template <typename F> __device__ __forceinline__ void store_halves(const CUtensorMap *map, uint8_t *stage, unsigned lane, bool any, unsigned cols, int col, int row0, F chunk) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (h * 32 >= cols) break;
+        uint8_t *half = stage + h * 2048;
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(half + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = chunk(h * 4 + c);
+        if (any) tma_store(map, smem_addr(half), col + h * 32, row0, 0);
     }
 }
 
@@ -774,8 +780,22 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
                 const EpiRows rows = epi_rows<EPI>(g, walks[t.which].m, t.mi * kBM + rank * 128 + quad * 32, t.s, lane);
                 const unsigned col = t.ni * kBN + half * kCols;
                 if constexpr (kLogits) {
-                    epi_prob<EPI == Epi::kProb>(g, v, rows, rows.row0 + lane, col, 2 * t.ni + half, stage, lane);
+                    const unsigned row = rows.row0 + lane;
+                    epi_stat<EPI == Epi::kProb>(g, v, row < rows.m, row, col, 2 * t.ni + half);
+                    if constexpr (EPI == Epi::kProb) {
+                        const unsigned left = g.n > col ? g.n - col : 0u;
+#pragma unroll 1
+                        for (int j = 0; j < 2; ++j) {
+                            if (j * 64 >= left) break;
+                            if (j == 0) store_halves(&g.c, stage, lane, rows.has(0), left, (int)col, (int)rows.row0, [&](int c) { return pack_half8(v + c * 8); });
+                            else store_halves(&g.c, stage, lane, rows.has(0), left - 64, (int)col + 64, (int)rows.row0, [&](int c) { return pack_half8(v + 64 + c * 8); });
+                        }
+                    }
                 } else {
+                    if (EPI == Epi::kPart && g.stat) {
+                        const unsigned row = rows.row0 + lane;
+                        epi_stat<false>(g, v, row < rows.m, row, col, 2 * t.ni + half);
+                    }
                     const F32Out o = f32_out<EPI>(g);
 #pragma unroll 1
                     for (int j = 0; j < 4; ++j) {
@@ -821,12 +841,15 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
                         }
 #pragma unroll
                         for (int i = 0; i < 64; ++i) v[i] *= f;
-                        if (g.out_type == SCAR_BF16) stage_fill(stage, lane, [&](int c) { return pack_bf8(v + c * 8); });
-                        else stage_fill(stage, lane, [&](int c) { return pack_half8(v + c * 8); });
+                        const bool bf = g.out_type == SCAR_BF16;
                         if (g.c_map) {
-                            if (rows.has(0)) tma_store(&g.c, smem_addr(stage), (int)(col + j), (int)rows.row0, 0);
-                        } else
-                            flush16(stage, static_cast<unsigned short *>(g.out) + col + j, g.out_pitch, g.out_vec, rows, g.n - (col + j), lane);
+                            store_halves(&g.c, stage, lane, rows.has(0), g.n - (col + j), (int)(col + j), (int)rows.row0,
+                                         [&](int c) { return bf ? pack_bf8(v + c * 8) : pack_half8(v + c * 8); });
+                            j += 64;
+                            continue;
+                        }
+                        stage_fill(stage, lane, [&](int c) { return bf ? pack_bf8(v + c * 8) : pack_half8(v + c * 8); });
+                        flush16(stage, static_cast<unsigned short *>(g.out) + col + j, g.out_pitch, g.out_vec, rows, g.n - (col + j), lane);
                         j += 64;
                     } else {
                         float v[32] = {};

@@ -37,7 +37,7 @@ __device__ __forceinline__ void griddep_start() {
 }
 
 // Lists the rows that count, in order: row_of[0 .. rows) are their numbers, pos is the inverse (kNone for the rest).  By one
-// CTA of kThreads, eight neighbouring labels per thread at a time: the labels of a step are few.
+// CTA of kThreads, eight labels per thread at a time (kThreads apart): the labels of a step are few.
 constexpr int kLabels = 8;
 struct RowList {
     const long long *labels;
@@ -51,50 +51,66 @@ struct RowList {
     float *d_loss;
 };
 template <int kThreads, bool kWrite> __device__ __forceinline__ unsigned list_rows(const RowList &q, unsigned *pos) {
-    __shared__ unsigned sh[32], n_ign, n_bad;
+    constexpr int kWarps = kThreads / 32, kCounts = kLabels * kWarps;  // rows that count, by round of labels and warp
+    __shared__ unsigned sh[kCounts], total, n_ign, n_bad;
     if (threadIdx.x == 0) n_ign = n_bad = 0;
-    if (threadIdx.x < 32) sh[threadIdx.x] = 0;
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned base = 0, ign = 0, bad = 0;
     for (unsigned long long at = 0; at < q.n; at += kThreads * kLabels) {
-        const unsigned long long t0 = at + threadIdx.x * kLabels;
+        const unsigned long long t0 = at + threadIdx.x;
         long long y[kLabels];
-        unsigned keep = 0;
+        unsigned before[kLabels], keep = 0;
 #pragma unroll
-        for (int i = 0; i < kLabels; ++i) y[i] = t0 + i < q.n ? q.labels[t0 + i] : q.ignore;
+        for (int i = 0; i < kLabels; ++i) y[i] = t0 + i * kThreads < q.n ? q.labels[t0 + i * kThreads] : q.ignore;
 #pragma unroll
         for (int i = 0; i < kLabels; ++i) {
-            if (t0 + i >= q.n) continue;
+            const bool k = y[i] != q.ignore && y[i] >= 0 && y[i] < (long long)q.n_classes;
+            const unsigned m = __ballot_sync(0xffffffffu, k);
+            before[i] = __popc(m & ((1u << lane) - 1u));
+            if (lane == 0) sh[i * kWarps + warp] = __popc(m);
+            keep |= (unsigned)k << i;
+            if (k || t0 + i * kThreads >= q.n) continue;
             if (y[i] == q.ignore) ++ign;
-            else if (y[i] >= 0 && y[i] < (long long)q.n_classes) keep |= 1u << i;
             else ++bad;
-            if (!(keep >> i & 1u)) {
-                if (kWrite) q.row_loss[t0 + i] = 0.f;
-                pos[t0 + i] = kNone;
+            if (kWrite) q.row_loss[t0 + i * kThreads] = 0.f;
+            pos[t0 + i * kThreads] = kNone;
+        }
+        __syncthreads();
+        if (warp == 0) {  // counts become sums of what is before them
+            constexpr int kEach = kCounts / 32;
+            unsigned c[kEach], sum = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                c[i] = sh[lane * kEach + i];
+                sum += c[i];
+            }
+            unsigned scan = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned v = __shfl_up_sync(0xffffffffu, scan, o);
+                if (lane >= o) scan += v;
+            }
+            if (lane == 31) total = scan;
+            scan -= sum;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                sh[lane * kEach + i] = scan;
+                scan += c[i];
             }
         }
-        const unsigned mine = __popc(keep);
-        unsigned scan = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned v = __shfl_up_sync(0xffffffffu, scan, o);
-            if (lane >= o) scan += v;
-        }
         __syncthreads();
-        if (lane == 31) sh[warp] = scan;
-        __syncthreads();
-        const unsigned all = sh[lane];
-        unsigned r = base + __reduce_add_sync(0xffffffffu, lane < warp ? all : 0u) + scan - mine;
-        base += __reduce_add_sync(0xffffffffu, all);
 #pragma unroll
         for (int i = 0; i < kLabels; ++i) {
             if (!(keep >> i & 1u)) continue;
+            const unsigned r = base + sh[i * kWarps + warp] + before[i];
             if (kWrite) {
-                q.row_of[r] = (unsigned)(t0 + i);
+                q.row_of[r] = (unsigned)(t0 + i * kThreads);
                 q.label[r] = (int)y[i];
             }
-            pos[t0 + i] = r++;
+            pos[t0 + i * kThreads] = r;
         }
+        base += total;
+        __syncthreads();
     }
     __syncthreads();
     if (kWrite) {
@@ -296,7 +312,7 @@ __device__ __forceinline__ void finish_loss(const LossOut &o) {
     __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();
-        last = atomicAdd(&o.rec->done, 1u) == gridDim.x - 1;
+        last = atomicAdd(&o.rec->done, 1u) == gridDim.x * gridDim.y - 1;
     }
     __syncthreads();
     if (!last) return;
@@ -331,11 +347,13 @@ template <int NT> __device__ __forceinline__ void zero_row(const DzOut &o, unsig
 }
 
 // NT threads (the CTA of 256, or a warp of it) per row of the piece: join the row's groups of 128 classes to lse and the
-// loss; with GRAD they turn the row's scaled exponentials into dz in place.  Rows behind the last one up to a multiple of
-// 64 become zero (the dw product runs over whole groups of 64 rows).  Bound by HBM: 2 bytes read and 2 written per value.
+// loss; with GRAD they turn the row's values into dz: scaled exponentials in place (z = nullptr), or float32 logits.  Rows
+// behind the last one up to a multiple of 64 become zero (the dw product runs over whole groups of 64 rows).  Few long
+// rows are cut into gridDim.y ranges of `span` classes, each of which joins the groups again.  Bound by HBM: 2 bytes (or
+// 4) read and 2 (or 6) written per value.
 template <bool GRAD, int NT>
 __global__ void __launch_bounds__(256)
-k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups, const int *__restrict__ label,
+k_xent_dz(DzOut o, unsigned V, unsigned span, const float *__restrict__ z, const float2 *__restrict__ stat, unsigned groups, const int *__restrict__ label,
           const float *__restrict__ label_z, const unsigned *__restrict__ row_of, Piece p, float *row_loss, LossOut loss) {
     __shared__ float sh[8];
     griddep_start();
@@ -344,13 +362,13 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
     float lse = 0.f, zl = 0.f;
     if (r < R) {
         float top = -INFINITY, s = 0.f;
-#pragma unroll 2
+#pragma unroll 4
         for (unsigned i = tid; i < groups; i += NT) {
             const float2 e = st[i];
             top = fmaxf(top, e.y > 0.f ? e.x : -INFINITY);
         }
         top = row_max<NT>(top, sh);
-#pragma unroll 2
+#pragma unroll 4
         for (unsigned i = tid; i < groups; i += NT) {
             const float2 e = st[i];
             if (e.y != 0.f) s = fmaf(e.y, expf(e.x - top), s);  // a NaN sum goes through
@@ -358,32 +376,50 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
         s = row_add<NT>(s, sh);
         lse = top + logf(s * (1.f / kProbScale));
         zl = label_z[p.first + r];
-        if (tid == 0) row_loss[row_of[p.first + r]] = lse - zl;
+        if (tid == 0 && blockIdx.y == 0) row_loss[row_of[p.first + r]] = lse - zl;
     }
     finish_loss(loss);
     if (!GRAD) return;
     unsigned short *row = o.dz + (unsigned long long)r * o.pitch;
+    const unsigned from = blockIdx.y * span;
     if (r >= R) {
-        if (r < (R + 63) / 64 * 64) zero_row<NT>(o, row, tid);
+        if (r < (R + 63) / 64 * 64 && from == 0) zero_row<NT>(o, row, tid);
         return;
     }
-    const unsigned y = (unsigned)label[p.first + r];
+    const unsigned y = (unsigned)label[p.first + r], to = V - from > span ? from + span : V;
     const float held = o.dt == SCAR_F16 ? kDzF16 : 1.f;
-    constexpr int kBatch = NT == 256 ? 4 : 2;  // 16-byte loads of a thread in flight
-    for (unsigned v0 = tid * 8; v0 < V; v0 += kBatch * NT * 8) {
+    if (o.dt == SCAR_F32) {
+        const float *zr = z + (unsigned long long)r * o.pitch;
+#pragma unroll 2
+        for (unsigned v = from + tid * 8; v < to; v += NT * 8) {
+            const float4 a = __ldcs(reinterpret_cast<const float4 *>(zr + v)), b = __ldcs(reinterpret_cast<const float4 *>(zr + v + 4));
+            const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            Eight w[3];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = v + j < V ? (v + j == y ? expm1f(zl - lse) : expf(x[j] - lse)) : 0.f;
+                split3(d, w[0].b[j], w[1].b[j], w[2].b[j]);
+            }
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(row + q * o.plane + v) = w[q].u;
+        }
+        return;
+    }
+    constexpr int kBatch = 4;  // 16-byte loads of a thread in flight
+    for (unsigned v0 = from + tid * 8; v0 < to; v0 += kBatch * NT * 8) {
         Eight x[kBatch];
         float2 e[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const unsigned v = v0 + i * NT * 8;
-            if (v >= V) break;
+            if (v >= to) break;
             x[i].u = __ldcs(reinterpret_cast<const uint4 *>(row + v));
             e[i] = st[v >> 7];
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const unsigned v = v0 + i * NT * 8;
-            if (v >= V) break;
+            if (v >= to) break;
             const float f = e[i].y != 0.f ? expf(e[i].x - lse) * (held / kProbScale) : 0.f;
             float w[8];
 #pragma unroll
@@ -403,8 +439,8 @@ k_xent_dz(DzOut o, unsigned V, const float2 *__restrict__ stat, unsigned groups,
     }
 }
 
-// The same from float32 logits of the piece in parts (their sum replaces the first part): one pass for the running
-// maximum and sum of every thread, one for dz.
+// The same from logits whose sum over k was split (their sum replaces the first part): one pass for the running maximum
+// and sum of every thread, one for dz.
 template <bool GRAD, int NT>
 __global__ void __launch_bounds__(256)
 k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict__ label, const unsigned *__restrict__ row_of, float *row_loss, LossOut loss) {
@@ -566,14 +602,14 @@ int check_call(const scar_xent *op, const void *h, uint64_t hp, const void *w, u
 bool rows_aligned(const void *p, uint64_t pitch, unsigned elem) { return (uintptr_t)p % 16 == 0 && pitch * elem % 16 == 0; }
 
 // The tensor map of an operand: boxes of 64 values of k by box_rows rows (K-major), or of 64 of its own dimension by 64
-// values of k (MN-major; box_rows = 64); or of a result: boxes of 128 bytes by 32 rows.
-int make_map(const scar_xent *op, CUtensorMap *map, const Operand &x, unsigned box_rows, unsigned elem = 2) {
+// values of k (MN-major; box_rows = 64); or of a result: boxes of 128 bytes (float32) or 64 (16-bit types) by 32 rows.
+int make_map(const scar_xent *op, CUtensorMap *map, const Operand &x, unsigned box_rows, unsigned elem = 2, unsigned box_bytes = 128) {
     const cuuint64_t dims[3] = {x.inner, x.rows, x.planes}, strides[2] = {x.pitch * elem, (x.planes > 1 ? x.plane : x.pitch) * elem};
-    const cuuint32_t box[3] = {128 / elem, box_rows, 1}, step[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {box_bytes / elem, box_rows, 1}, step[3] = {1, 1, 1};
     const CUtensorMapDataType type = elem == 4                      ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                      : op->cfg.dtype == SCAR_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                                  : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    const CUresult rc = op->encode(map, type, 3, const_cast<void *>(x.p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    const CUresult rc = op->encode(map, type, 3, const_cast<void *>(x.p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return rc == CUDA_SUCCESS ? SCAR_OK : SCAR_ERR_CUDA;
 }
@@ -608,7 +644,7 @@ int map_workspaces(scar_xent *op) {
     if ((rc = make_map(op, &op->h_rows_map, oh, 128)) != SCAR_OK || (rc = make_map(op, &op->h_cols_map, oh, 64)) != SCAR_OK) return rc;
     if (!op->dz) return SCAR_OK;
     if ((rc = make_map(op, &op->dz_rows_map, oz, 128)) != SCAR_OK || (rc = make_map(op, &op->dz_cols_map, oz, 64)) != SCAR_OK) return rc;
-    return make_map(op, &op->dz_out_map, oz, 32);
+    return make_map(op, &op->dz_out_map, oz, 32, 2, 64);
 }
 int map_w_copy(scar_xent *op) {
     const uint64_t V = op->cfg.n_classes, D = op->cfg.dim;
@@ -620,7 +656,7 @@ int map_w_copy(scar_xent *op) {
 }
 
 // Launches a kernel of the call's chain: it may start while the one before it still runs (griddep_start waits for it).
-template <typename... P, typename... A> void launch(scar_xent *op, void (*kernel)(P...), unsigned grid, unsigned threads, unsigned smem, A... args) {
+template <typename... P, typename... A> void launch(scar_xent *op, void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, A... args) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = threads;
@@ -635,23 +671,26 @@ template <typename... P, typename... A> void launch(scar_xent *op, void (*kernel
     else op->failed = true;
 }
 
-// Sets the product's `splits`: 1, or more than 1 where cutting the sum over k pays for all the rows the call has.
-void choose_splits(const scar_xent *op, TcArgs &g) {
+// Sets the product's `splits`: 1, or more than 1 where cutting the sum over k pays for all the rows the call has.  Returns
+// what it costs, in units of 64 values of k.
+float choose_splits(const scar_xent *op, TcArgs &g, float join_s) {
     const uint64_t part = (uint64_t)g.m * round_up(g.n, 8) * 4;
     g.pairs = op->pairs;
     g.planes = op->planes;
+    g.join_s = join_s;
     g.most_splits = (unsigned)std::min<uint64_t>(kMostSplits, std::max<uint64_t>(1, part ? op->part_bytes / part : 1));
     g.splits = 1;
     const unsigned kb = (g.k + kBK - 1) / kBK;
     const uint64_t tiles = (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + kBN - 1) / kBN);
-    float best = split_cost(1, tiles, kb, op->pairs, 0.f, op->planes);
+    float best = split_cost(1, tiles, kb, op->pairs, 0.f, join_s, op->planes);
     for (unsigned s = 2; s <= g.most_splits && s <= kb; ++s) {
-        const float cost = split_cost(s, tiles, kb, op->pairs, (float)g.m * (float)g.n * 4.f, op->planes);
+        const float cost = split_cost(s, tiles, kb, op->pairs, (float)g.m * (float)g.n * 4.f, join_s, op->planes);
         if (cost < best) {
             best = cost;
             g.splits = s;
         }
     }
+    return best;
 }
 
 uint64_t tiles_of(const TcArgs &g) { return (uint64_t)((g.m + kBM - 1) / kBM) * ((g.n + kBN - 1) / kBN) * (g.splits > 1 ? g.most_splits : 1); }
@@ -685,15 +724,20 @@ template <int PL, bool A_MN> void launch_out(scar_xent *op, const TcArgs &g) {
     launch(op, k_xent_combine, (unsigned)std::min<uint64_t>((todo + 127) / 128, 32 * op->pairs), 128, 0, g);
 }
 
-// dh and dw of a piece: one launch where neither is split, so that the second one's tiles fill the last round of the
-// first one's (4096 x 32000 x 2048: 120 tiles of 500 stages leave 28 of 74 pairs idle for half of that time).
-// Not where dw goes through the room of w's copy, which dh still reads.
+// dh and dw of a piece: one launch without splits, so that the second one's tiles fill the last round of the first one's
+// (4096 x 32000 x 2048: 120 tiles of 500 stages leave 28 of 74 pairs idle for half of that time), unless split products
+// with launches of their own are worth it (a dh of few tiles whose sum runs over very many classes).  Not where dw goes through the room of w's copy, which dh still reads.
 template <int PL> void launch_grads(scar_xent *op, TcArgs dhg, TcArgs dwg, bool through_w) {
-    choose_splits(op, dhg);
-    choose_splits(op, dwg);
-    if (dhg.splits == 1 && dwg.splits == 1 && !through_w) {
-        const unsigned pairs = (unsigned)std::min<uint64_t>(tiles_of(dhg) + tiles_of(dwg), op->pairs);
-        launch(op, k_tc_gemm<PL, false, true, Epi::kOut, 2>, 2 * pairs, kGemmThreads, kTcSmem, TcSet<2>{{dhg, dwg}});
+    const float apart = choose_splits(op, dhg, kLaunchS) + choose_splits(op, dwg, kLaunchS) + kLaunchS / unit_s(PL);
+    const unsigned pairs = op->pairs;
+    const float tile0 = (float)((dhg.k + kBK - 1) / kBK + 4), tile1 = (float)((dwg.k + kBK - 1) / kBK + 4);
+    const uint64_t tiles0 = (uint64_t)((dhg.m + kBM - 1) / kBM) * ((dhg.n + kBN - 1) / kBN), tiles1 = (uint64_t)((dwg.m + kBM - 1) / kBM) * ((dwg.n + kBN - 1) / kBN);
+    // the second one's tiles fill gaps where they are the shorter ones, and come on top where they are not
+    const float together = tile1 <= tile0 ? std::max(tile0, ((float)tiles0 * tile0 + (float)tiles1 * tile1) / (float)pairs)
+                                          : (float)((tiles0 + pairs - 1) / pairs) * tile0 + (float)((tiles1 + pairs - 1) / pairs) * tile1;
+    if (!through_w && together <= apart) {
+        dhg.splits = dwg.splits = 1;
+        launch(op, k_tc_gemm<PL, false, true, Epi::kOut, 2>, 2 * (unsigned)std::min<uint64_t>(tiles0 + tiles1, pairs), kGemmThreads, kTcSmem, TcSet<2>{{dhg, dwg}});
         return;
     }
     launch_out<PL, false>(op, dhg);
@@ -771,23 +815,29 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
         if (rows) {
             fill(logits, rows, V, D, 0);
             logits.a_row0 = at;
-            logits.stat = op->stat;
             logits.stat_pitch = op->groups;
             logits.label = op->label;
             logits.label_z = op->label_z;
-            choose_splits(op, logits);
-            // a warp per row where there are rows for a CTA of them on every SM, and a row is short or only its groups are read
-            const bool many = rows >= 16 * op->pairs, short_rows = many && V <= kWarpRow, warps = short_rows || (many && !grad);
-            const unsigned ctas = warps ? (rows64 + 7) / 8 : rows64;
-            if (PL == 3 || logits.splits > 1) {
+            choose_splits(op, logits, kLaunchS);  // the softmax of parts takes about that much longer
+            logits.stat = logits.splits == 1 ? op->stat : nullptr;
+            // a warp per row where a row is short (or only its groups are read) and there are rows for a CTA of them on every SM;
+            // for rows of up to 8192 classes, for four
+            const bool many = rows >= 16 * op->pairs, short_rows = (many && V <= kWarpRow) || (rows >= 64 * op->pairs && V <= 4 * kWarpRow);
+            if (logits.splits > 1) {
                 launch_tc<PL, false, false, Epi::kPart>(op, logits);
                 auto kernel = short_rows ? (grad ? k_xent_softmax<true, 32> : k_xent_softmax<false, 32>) : (grad ? k_xent_softmax<true, 256> : k_xent_softmax<false, 256>);
-                launch(op, kernel, short_rows ? (rows64 + 7) / 8 : rows64, 256, 0, logits, dz, op->label, op->row_of, row_loss, loss);
-            } else if constexpr (PL == 1) {
-                if (grad) launch_tc<1, false, false, Epi::kProb>(op, logits);
+                launch(op, kernel, dim3(short_rows ? (rows64 + 7) / 8 : rows64), 256, 0, logits, dz, op->label, op->row_of, row_loss, loss);
+            } else {
+                if constexpr (PL == 3) launch_tc<3, false, false, Epi::kPart>(op, logits);
+                else if (grad) launch_tc<1, false, false, Epi::kProb>(op, logits);
                 else launch_tc<1, false, false, Epi::kStat>(op, logits);
+                // few long rows: ranges of at least 4096 classes, for about two CTAs per SM
+                const bool warps = short_rows || (many && !grad);
+                const unsigned ranges = grad && !warps ? std::max(1u, std::min(V / 4096u, 4 * op->pairs / std::max(rows, 1u))) : 1u;
+                const unsigned span = (unsigned)round_up((V + ranges - 1) / ranges, 2048);
                 auto kernel = warps ? (grad ? k_xent_dz<true, 32> : k_xent_dz<false, 32>) : (grad ? k_xent_dz<true, 256> : k_xent_dz<false, 256>);
-                launch(op, kernel, ctas, 256, 0, dz, V, op->stat, op->groups, op->label, op->label_z, op->row_of, p, row_loss, loss);
+                launch(op, kernel, dim3(warps ? (rows64 + 7) / 8 : rows64, (V + span - 1) / span), 256, 0, dz, V, span, op->part, op->stat, op->groups, op->label,
+                       op->label_z, op->row_of, p, row_loss, loss);
             }
         }
         if (!grad) continue;
@@ -820,11 +870,11 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
             dwg.out_vec = 1;
         }
         dwg.c_map = !dwg.acc && (through_w || (dwg.out_vec && D * sizeof(T) % 16 == 0));
-        if (dwg.c_map && (rc = make_map(op, &dwg.c, {dwg.out, D, V, dwg.out_pitch, 1, 0}, 32, sizeof(T))) != SCAR_OK) return rc;
+        if (dwg.c_map && (rc = make_map(op, &dwg.c, {dwg.out, D, V, dwg.out_pitch, 1, 0}, 32, sizeof(T), PL == 1 ? 64 : 128)) != SCAR_OK) return rc;
         if (rows) {
             launch_grads<PL>(op, dhg, dwg, through_w);
         } else {
-            choose_splits(op, dwg);
+            choose_splits(op, dwg, kLaunchS);
             launch_out<PL, true>(op, dwg);
         }
         if (through_w)
@@ -867,7 +917,7 @@ int size_workspaces(scar_xent *op) {
     op->dp = round_up(D, 8);
     op->groups = (unsigned)(2 * ((V + 255) / 256));
     const uint64_t limit = c.workspace_bytes ? c.workspace_bytes : 1ull << 30;
-    const uint64_t row = f32 ? 4 * V + (grad ? 6 * op->vp : 0) : 8ull * op->groups + (grad ? 2 * op->vp : 0);
+    const uint64_t row = 8ull * op->groups + (f32 ? 4 * op->vp : 0) + (grad ? 2 * op->planes * op->vp : 0);
     uint64_t piece = std::max<uint64_t>(limit / row / 256 * 256, 256);
     if (grad && !f32 && piece < T && T * row <= piece * row + V * D * 4) piece = T;
     op->piece = (unsigned)round_up(std::min(piece, T), 64);
@@ -878,7 +928,7 @@ int size_workspaces(scar_xent *op) {
         (rc = xent_alloc(op, &op->row_loss, 4 * T)) != SCAR_OK || (rc = xent_alloc(op, &op->rec, sizeof(XentRecord))) != SCAR_OK ||
         (rc = xent_alloc(op, &op->h, op->planes * op->h_rows * op->dp * 2)) != SCAR_OK)
         return rc;
-    if (!f32 && (rc = xent_alloc(op, &op->stat, 8ull * op->groups * op->piece)) != SCAR_OK) return rc;
+    if ((rc = xent_alloc(op, &op->stat, 8ull * op->groups * op->piece)) != SCAR_OK) return rc;
     if (grad && (rc = xent_alloc(op, &op->dz, op->planes * (uint64_t)op->piece * op->vp * 2)) != SCAR_OK) return rc;
     if (grad && !f32 && op->piece < T && (rc = xent_alloc(op, &op->acc, V * op->dp * 4)) != SCAR_OK) return rc;
     if ((f32 || D % 8) && (rc = xent_alloc(op, &op->w, op->planes * V * op->dp * 2)) != SCAR_OK) return rc;
