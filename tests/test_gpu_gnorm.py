@@ -102,6 +102,22 @@ def test_inputs_and_outputs_at_different_offsets(dt):
 
 
 @gpu
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_a_tensor_beyond_32_bits(dt):
+    """2^31 + 77 values (4 GB): a few of them large, at places a 32-bit offset would miss; the rest zero."""
+    n = 2 ** 31 + 77
+    t = torch.zeros(n, dtype=TYPES[dt], device="cuda")
+    at = [0, 2 ** 30 - 1, 2 ** 31 - 1, 2 ** 31, n - 1]
+    for i in at:
+        t[i] = 3.0
+    op = GradientNorm([t])
+    want = math.sqrt(9.0 * len(at))
+    assert abs(float(op.clip(want / 3)) - want) <= 1e-6 * want
+    assert all(float(t[i]) == 1.0 for i in at) and abs(float(op.norm()) - want / 3) <= 1e-6 * want
+    op.close()
+
+
+@gpu
 def test_no_tensors_and_no_elements():
     for ts in ([], [torch.empty(0, device="cuda")], [torch.empty(0, device="cuda", dtype=torch.bfloat16)] * 3):
         op = GradientNorm(ts)

@@ -126,6 +126,53 @@ def test_larger_sizes(dt):
 
 @gpu
 @pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("T,V,D,ignored", [
+    (2500, 300, 64, 0.1), (5000, 9000, 40, 0.3), (4800, 120, 1000, 0.0),  # a warp per row of the softmax; rows listed by a kernel of their own
+    (3000, 1500, 72, 0.95),  # far fewer rows count than the launch was made for
+    (12, 30000, 96, 0.0),    # few long rows: cut into ranges
+    (40, 260, 6000, 0.2),    # few tiles: the sum over D is cut into parts
+    (700, 60000, 24, 0.1),   # dh sums over very many classes
+    (9000, 40, 48, 0.2),     # dw sums over very many rows
+])
+def test_every_way_through_the_kernels(dt, T, V, D, ignored):
+    h, w, y = make(T, V, D, TYPES[dt], seed=T + D, ignored=ignored)
+    op = LinearCrossEntropy(T, V, D, TYPES[dt])
+    check(op, h, w, y)
+    op.close()
+
+
+@gpu
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_offsets_beyond_32_bits(dt):
+    """w and dw of 2.4e9 values: rows behind the 2^31st and the 2^32nd value's byte are checked against the definition."""
+    T, V, D = 6, 300_000, 8000
+    w = torch.empty(V, D, dtype=TYPES[dt], device="cuda").normal_(std=1.5 / D ** 0.5)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    y = torch.tensor([0, V - 1, 268_435, 268_436, IGN, V - 2], device="cuda")
+    h = torch.randn(T, D, generator=g, device="cuda").to(TYPES[dt])
+    op = LinearCrossEntropy(T, V, D, TYPES[dt], reduction="sum")
+    loss, row, dh, dw = op.loss_and_grad(h, w, y)
+    kept = y >= 0
+    hd = torch.where(kept[:, None], h, torch.zeros_like(h)).double()
+    z = torch.cat([hd @ c.double().T for c in w.split(20_000)], 1)
+    lse = torch.logsumexp(z, 1)
+    want = torch.where(kept, lse - z.gather(1, y.clamp(min=0)[:, None])[:, 0], 0.0)
+    ez = 2 * gamma(D) * 50 + 2.0 ** -18
+    assert bool(((row.double() - want).abs() <= ez).all())
+    p = torch.exp(z - lse[:, None]) * kept[:, None]
+    p[torch.arange(T), y.clamp(min=0)] -= kept.double()
+    rows = torch.cat([torch.arange(0, 3), torch.arange(268_430, 268_440), torch.arange(V - 3, V)]).cuda()
+    u = UNIT[TYPES[dt]]
+    ref = p.T[rows] @ hd
+    tol = (u + 2.0 ** -11 + 2 * ez) * (p.T[rows].abs() @ hd.abs()) + u * ref.abs() + 2.0 ** -24
+    assert bool(((dw[rows].double() - ref).abs() <= tol).all())
+    ref = sum(p[:, i: i + 20_000] @ w[i: i + 20_000].double() for i in range(0, V, 20_000))
+    assert float((dh.double() - ref).norm()) <= u * float(ref.norm()) and not dh[4].any()
+    op.close()
+
+
+@gpu
+@pytest.mark.parametrize("dt", list(TYPES))
 def test_sum_and_scale(dt):
     h, w, y = make(70, 600, 96, TYPES[dt], seed=5, ignored=0.3)
     op = LinearCrossEntropy(70, 600, 96, TYPES[dt], reduction="sum")
