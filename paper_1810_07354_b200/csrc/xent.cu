@@ -421,21 +421,20 @@ k_xent_dz(DzOut o, unsigned V, unsigned span, const float *__restrict__ z, const
             const unsigned v = v0 + i * NT * 8;
             if (v >= to) break;
             const float f = e[i].y != 0.f ? expf(e[i].x - lse) * (held / kProbScale) : 0.f;
-            float w[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                w[j] = __half2float(x[i].h[j]) * f;
-                if (v + j == y) w[j] = expm1f(zl - lse) * held;
-            }
-            if (o.dt == SCAR_F16) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[i].h[j] = __float2half_rn(w[j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[i].b[j] = __float2bfloat16_rn(w[j]);
+            for (int j = 0; j < 8; j += 2) {
+                const float2 w = __half22float2(*reinterpret_cast<const __half2 *>(x[i].h + j));
+                if (o.dt == SCAR_F16) *reinterpret_cast<__half2 *>(x[i].h + j) = __floats2half2_rn(w.x * f, w.y * f);
+                else *reinterpret_cast<__nv_bfloat162 *>(x[i].b + j) = __floats2bfloat162_rn(w.x * f, w.y * f);
             }
             *reinterpret_cast<uint4 *>(row + v) = x[i].u;
         }
+    }
+    // the label's value, from its exact logit, by the thread that has just written what was there
+    if (y >= from && y < to && (y - from) / 8 % NT == tid) {
+        const float d = expm1f(zl - lse) * held;
+        if (o.dt == SCAR_F16) reinterpret_cast<__half *>(row)[y] = __float2half_rn(d);
+        else reinterpret_cast<__nv_bfloat16 *>(row)[y] = __float2bfloat16_rn(d);
     }
 }
 
