@@ -189,11 +189,11 @@ struct scar_gnorm {
     std::vector<uint64_t> lengths;
     std::vector<int> types;
     std::vector<Piece> h_pieces;
+    char *block = nullptr;  // the one allocation, which the pointers below lie in
     Piece *pieces = nullptr;
     double *part = nullptr;
     unsigned *ticket = nullptr;
     NormRecord *rec = nullptr;
-    NormRecord *h_rec = nullptr;  // pinned
     unsigned grid = 1;
     bool ran = false;
     uint64_t launches = 0;
@@ -284,13 +284,15 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
         TRAIN_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, op->device));
         const unsigned most = kCtasPerSm * (unsigned)sms, n = (unsigned)op->h_pieces.size();
         op->grid = n < 1 ? 1 : (n < most ? n : most);
-        if (cudaMalloc(&op->pieces, (n ? n : 1) * sizeof(Piece)) != cudaSuccess ||
-            cudaMalloc(&op->part, op->grid * sizeof(double)) != cudaSuccess ||
-            cudaMalloc(&op->rec, sizeof(NormRecord)) != cudaSuccess || cudaMalloc(&op->ticket, sizeof(unsigned)) != cudaSuccess ||
-            cudaMallocHost(&op->h_rec, sizeof(NormRecord)) != cudaSuccess) {
+        const uint64_t table = round_up((uint64_t)n * sizeof(Piece), 256), parts = round_up(op->grid * sizeof(double), 256);
+        if (cudaMalloc(&op->block, table + parts + 512) != cudaSuccess) {
             cudaGetLastError();
             return SCAR_ERR_ALLOC;
         }
+        op->pieces = reinterpret_cast<Piece *>(op->block);
+        op->part = reinterpret_cast<double *>(op->block + table);
+        op->rec = reinterpret_cast<NormRecord *>(op->block + table + parts);
+        op->ticket = reinterpret_cast<unsigned *>(op->block + table + parts + 256);
         TRAIN_TRY(cudaMemsetAsync(op->ticket, 0, sizeof(unsigned), op->stream));
         return upload(op);
     };
@@ -352,11 +354,12 @@ int scar_gnorm_status(scar_gnorm *op, scar_gnorm_info *out) {
     const int rc = check_current_device(op->device);
     if (rc != SCAR_OK) return rc;
     if (!op->ran) return SCAR_ERR_STATE;
-    TRAIN_TRY(cudaMemcpyAsync(op->h_rec, op->rec, sizeof(NormRecord), cudaMemcpyDeviceToHost, op->stream));
+    NormRecord rec;
+    TRAIN_TRY(cudaMemcpyAsync(&rec, op->rec, sizeof(NormRecord), cudaMemcpyDeviceToHost, op->stream));
     TRAIN_TRY(cudaStreamSynchronize(op->stream));
-    out->norm = op->h_rec->norm;
-    out->coef = op->h_rec->coef;
-    out->nonfinite = op->h_rec->nonfinite;
+    out->norm = rec.norm;
+    out->coef = rec.coef;
+    out->nonfinite = rec.nonfinite;
     return SCAR_OK;
 }
 
@@ -365,11 +368,7 @@ uint64_t scar_gnorm_launch_count(const scar_gnorm *op) { return op ? op->launche
 int scar_gnorm_destroy(scar_gnorm *op) {
     if (!op) return SCAR_ERR_INVALID_ARG;
     const bool ok = cudaStreamSynchronize(op->stream) == cudaSuccess;
-    cudaFree(op->pieces);
-    cudaFree(op->part);
-    cudaFree(op->ticket);
-    cudaFree(op->rec);
-    if (op->h_rec) cudaFreeHost(op->h_rec);
+    cudaFree(op->block);
     delete op;
     if (!ok) cudaGetLastError();
     return ok ? SCAR_OK : SCAR_ERR_CUDA;

@@ -563,7 +563,6 @@ struct scar_xent {
     uint64_t part_bytes = 0;
     float *acc = nullptr;
     XentRecord *rec = nullptr;
-    XentRecord *h_rec = nullptr;   // pinned
     // tensor maps of the workspaces: h as rows (128 a box) and as columns, dz likewise and as a result, w's copy
     CUtensorMap h_rows_map, h_cols_map, dz_rows_map, dz_cols_map, dz_out_map, w_rows_map, w_cols_map;
     std::vector<void *> owned;
@@ -918,26 +917,38 @@ int size_workspaces(scar_xent *op) {
     const uint64_t limit = c.workspace_bytes ? c.workspace_bytes : 1ull << 30;
     const uint64_t row = 8ull * op->groups + (f32 ? 4 * op->vp : 0) + (grad ? 2 * op->planes * op->vp : 0);
     uint64_t piece = std::max<uint64_t>(limit / row / 256 * 256, 256);
-    if (grad && !f32 && piece < T && T * row <= piece * row + V * D * 4) piece = T;
+    if (grad && !f32 && piece < T && (unsigned __int128)T * row <= (unsigned __int128)piece * row + V * D * 4) piece = T;
     op->piece = (unsigned)round_up(std::min(piece, T), 64);
     op->h_rows = round_up(T, 64);
-    int rc;
-    if ((rc = xent_alloc(op, &op->row_of, 4 * T)) != SCAR_OK || (rc = xent_alloc(op, &op->pos, 4 * T)) != SCAR_OK ||
-        (rc = xent_alloc(op, &op->label, 4 * T)) != SCAR_OK || (rc = xent_alloc(op, &op->label_z, 4 * T)) != SCAR_OK ||
-        (rc = xent_alloc(op, &op->row_loss, 4 * T)) != SCAR_OK || (rc = xent_alloc(op, &op->rec, sizeof(XentRecord))) != SCAR_OK ||
-        (rc = xent_alloc(op, &op->h, op->planes * op->h_rows * op->dp * 2)) != SCAR_OK)
-        return rc;
-    if ((rc = xent_alloc(op, &op->stat, 8ull * op->groups * op->piece)) != SCAR_OK) return rc;
-    if (grad && (rc = xent_alloc(op, &op->dz, op->planes * (uint64_t)op->piece * op->vp * 2)) != SCAR_OK) return rc;
-    if (grad && !f32 && op->piece < T && (rc = xent_alloc(op, &op->acc, V * op->dp * 4)) != SCAR_OK) return rc;
-    if ((f32 || D % 8) && (rc = xent_alloc(op, &op->w, op->planes * V * op->dp * 2)) != SCAR_OK) return rc;
     // parts of split products: as many as choose_splits may ask for, up to 64 MiB
     const uint64_t P = std::min<uint64_t>(op->piece, T);
     uint64_t most = P * op->vp;
     if (grad) most = std::max(most, std::max(P * op->dp, V * op->dp));
     op->part_bytes = std::min<uint64_t>(64ull << 20, most * 4 * 32);
     if (f32) op->part_bytes = std::max(op->part_bytes, P * op->vp * 4);
-    return xent_alloc(op, &op->part, op->part_bytes);
+    // all of it in one allocation: each one costs the caller a few hundred microseconds
+    struct {
+        void **p;
+        uint64_t bytes;
+    } const want[] = {
+        {(void **)&op->row_of, 4 * T}, {(void **)&op->pos, 4 * T}, {(void **)&op->label, 4 * T}, {(void **)&op->label_z, 4 * T},
+        {(void **)&op->row_loss, 4 * T}, {(void **)&op->rec, sizeof(XentRecord)}, {(void **)&op->h, op->planes * op->h_rows * op->dp * 2},
+        {(void **)&op->stat, 8ull * op->groups * op->piece}, {(void **)&op->part, op->part_bytes},
+        {(void **)&op->dz, grad ? op->planes * (uint64_t)op->piece * op->vp * 2 : 0},
+        {(void **)&op->acc, grad && !f32 && op->piece < T ? V * op->dp * 4 : 0},
+        {(void **)&op->w, f32 || D % 8 ? op->planes * V * op->dp * 2 : 0},
+    };
+    uint64_t total = 0;
+    for (const auto &x : want) total += round_up(x.bytes, 256);
+    char *block = nullptr;
+    const int rc = xent_alloc(op, &block, total);
+    if (rc != SCAR_OK) return rc;
+    for (const auto &x : want)
+        if (x.bytes) {
+            *x.p = block;
+            block += round_up(x.bytes, 256);
+        }
+    return SCAR_OK;
 }
 
 }  // namespace
@@ -971,10 +982,6 @@ int scar_xent_init(scar_xent **out, const scar_xent_config *cfg, void *cuda_stre
         op->pairs = std::max(1, sms / 2);
         int rc = size_workspaces(op);
         if (rc != SCAR_OK || (rc = map_workspaces(op)) != SCAR_OK) return rc;
-        if (cudaMallocHost(&op->h_rec, sizeof(XentRecord)) != cudaSuccess) {
-            cudaGetLastError();
-            return SCAR_ERR_ALLOC;
-        }
         TRAIN_TRY(cudaStreamSynchronize(op->stream));
         return SCAR_OK;
     };
@@ -1018,13 +1025,14 @@ int scar_xent_status(scar_xent *op, scar_xent_info *out) {
     const int rc = check_current_device(op->device);
     if (rc != SCAR_OK) return rc;
     if (!op->ran) return SCAR_ERR_STATE;
-    TRAIN_TRY(cudaMemcpyAsync(op->h_rec, op->rec, sizeof(XentRecord), cudaMemcpyDeviceToHost, op->stream));
+    XentRecord rec;
+    TRAIN_TRY(cudaMemcpyAsync(&rec, op->rec, sizeof(XentRecord), cudaMemcpyDeviceToHost, op->stream));
     TRAIN_TRY(cudaStreamSynchronize(op->stream));
-    out->loss = op->h_rec->loss;
-    out->rows = op->h_rec->rows;
-    out->ignored = op->h_rec->ignored;
-    out->bad = op->h_rec->bad;
-    return op->h_rec->error ? SCAR_ERR_TIMEOUT : SCAR_OK;
+    out->loss = rec.loss;
+    out->rows = rec.rows;
+    out->ignored = rec.ignored;
+    out->bad = rec.bad;
+    return rec.error ? SCAR_ERR_TIMEOUT : SCAR_OK;
 }
 
 uint64_t scar_xent_workspace_bytes(const scar_xent *op) { return op ? op->bytes : 0; }
@@ -1034,7 +1042,6 @@ int scar_xent_destroy(scar_xent *op) {
     if (!op) return SCAR_ERR_INVALID_ARG;
     const bool ok = cudaStreamSynchronize(op->stream) == cudaSuccess;
     for (void *p : op->owned) cudaFree(p);
-    if (op->h_rec) cudaFreeHost(op->h_rec);
     delete op;
     if (!ok) cudaGetLastError();
     return ok ? SCAR_OK : SCAR_ERR_CUDA;
