@@ -455,9 +455,12 @@ int scar_ckpt_destroy(scar_ctx *ctx);
  * is zero and whatever its row of h holds (NaN, infinities) reaches nothing.  A label
  * outside [0, V) that is not ignore_label is treated the same and counted
  * (scar_xent_status).  Without any row that counts the loss and both gradients are 0.
- * The T x V matrix of logits is never stored: the loss alone keeps two numbers per row
- * and group of classes, the gradients go through pieces of the rows in a block of
- * workspace whose size `workspace_bytes` bounds. */
+ * The T x V matrix of logits is never stored whole.  The loss alone keeps two
+ * numbers per row and group of 128 classes (float32 operands: a piece of float32
+ * logits too).  With gradients the rows go through in pieces; a piece's block holds
+ * exponentials in 16 bits that become dz in place (float32 operands: its float32
+ * logits and dz), and `workspace_bytes` bounds it.  In float32 an infinity in an
+ * operand acts as a NaN. */
 typedef struct scar_xent scar_xent; /* opaque; created by scar_xent_init, freed by scar_xent_destroy */
 
 typedef enum { SCAR_MEAN = 0, SCAR_SUM = 1 } scar_reduction;

@@ -56,7 +56,7 @@ struct TcArgs {
     unsigned first, most;    // the piece's rows of the compacted list
     const unsigned *rows;    // rows that count (device)
     unsigned a_row0, b_row0; // where the piece starts in the row dimension of the tensor maps
-    unsigned splits;         // 1, or the launch's share of CTAs lets the kernel choose (pick_splits)
+    unsigned splits;         // 1, or more: the kernel then chooses for the rows it finds (pick_splits)
     unsigned pairs;          // CTA pairs the GPU holds
     unsigned most_splits;    // that fit the buffer of parts
     int planes;
@@ -64,7 +64,7 @@ struct TcArgs {
     int n_fast;              // tiles of one row of tiles run first (B is the smaller operand and stays in L2)
     int bf16;
     unsigned *error;
-    int c_map;
+    int c_map;               // kOut: the result is stored through `c` (kPart and kProb always do)
     // kPart
     float *part;             // [splits][m][n rounded up to 8]
     // kOut
@@ -77,7 +77,7 @@ struct TcArgs {
     int acc_vec, acc_first, acc_last;
     float scale;             // of the result: scale / rows when mean
     int mean;
-    // kProb, kStat
+    // kProb, kStat, and kPart of float32 logits (stat set)
     float2 *stat;            // [row][2 * n tiles]: maximum and sum of exponentials of 128 columns
     unsigned stat_pitch;
     const int *label;        // of the compacted rows

@@ -6,9 +6,15 @@
 //                    for gradients the exponentials relative to that maximum, in float16 (k_tc_gemm, kProb / kStat)
 //   dz               k_xent_dz joins a row's groups to lse and turns the exponentials into dz, in place
 //   dh = dz w, dw = dz^T h
-// so the logits are computed once (6 n V D operations, not 8) and exist only in tensor memory.  float32 operators, and
-// products with too few tiles to fill the GPU (their sum over D is split over CTAs), pass through float32 logits of the
-// piece instead (kPart and k_xent_softmax).  The last CTA of the last softmax adds the row losses.
+// so the logits are computed once (6 n V D operations, not 8) and, for 16-bit operands, exist only in tensor memory.
+// float32 operands keep float32 logits of the piece beside the same statistics; products with too few tiles to fill the
+// GPU (their sum over D is cut into parts) leave float32 parts for k_xent_softmax.  The last CTA of the last softmax adds
+// the row losses.
+//
+// What bounds it, measured: many rows, the tensor cores (4096 x 32000 x 2048 bfloat16: the logits' product 325 us with
+// its pipe active 87 % of the time, dh and dw together 619 us, 93 %, at the 1.4 - 1.5 GHz that the power limit leaves;
+// 80 us for the dz pass at 5.3 TB/s); few rows, reading w (one row, 128000 x 4096: 5.6 TB/s); small sizes, the chain of
+// five to seven launches (16 x 2000 x 512: 34 us).
 #include <algorithm>
 #include <new>
 #include <vector>
