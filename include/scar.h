@@ -516,7 +516,7 @@ int scar_xent_destroy(scar_xent *op);
  *   coef = min(1, max_norm / norm), 1 when norm is 0
  *   out_i = coef * g_i, rounded once
  * Sums run in float32 over short runs and in double across them, in an order that
- * depends on the lengths alone: equal inputs give equal bits.  A NaN or an infinity in
+ * depends on the lengths and on the addresses modulo 16: equal inputs give equal bits.  A NaN or an infinity in
  * the tensors gives the IEEE result of these formulas (norm NaN: all outputs NaN; norm
  * infinite: coef 0, NaN where g is infinite) and is reported (scar_gnorm_status), so
  * that a caller can leave the step out. */

@@ -2,7 +2,7 @@
 //
 // The tensors are cut into pieces of at most kPieceBytes on the host, once, so that every piece but a tensor's first
 // begins on a 16-byte boundary.  A CTA walks over pieces with a fixed stride: which CTA adds what depends on the lengths
-// alone, the last CTA to finish adds the CTAs' sums in their order, and the result is the same bits every time.
+// and the addresses modulo 16 alone, the last CTA to finish adds the CTAs' sums in their order, and the result is the same bits every time.
 // Bound by HBM: one read for the norm, one read and one write for the scaled values.  The second kernel is launched
 // while the first runs (programmatic launch) and takes the pieces backwards, so that what the first read last is still
 // in L2; it has one CTA per piece, started in order, because CTAs that walk over pieces drift apart and then read and
@@ -201,22 +201,23 @@ struct scar_gnorm {
 
 namespace {
 
-int check_tensors(const scar_tensor *t, uint64_t n) {
+// Also gives the most pieces that tensors of these lengths can be cut into, wherever they lie.
+int check_tensors(const scar_tensor *t, uint64_t n, uint64_t &pieces) {
+    pieces = 0;
     if (n && !t) return SCAR_ERR_INVALID_ARG;
-    uint64_t pieces = 0;
     for (uint64_t i = 0; i < n; ++i) {
         if (!is_operand_type(t[i].dtype)) return SCAR_ERR_INVALID_ARG;
         const unsigned b = elem_size(t[i].dtype);
         if (t[i].n_elems >= (1ull << 48)) return SCAR_ERR_LAYOUT;
         if (t[i].n_elems && !t[i].d_data) return SCAR_ERR_INVALID_ARG;
         if ((uintptr_t)t[i].d_data % b || (uintptr_t)t[i].d_out % b) return SCAR_ERR_INVALID_ARG;
-        pieces += (t[i].n_elems * b + kPieceBytes - 1) / kPieceBytes + 1;
+        if (t[i].n_elems) pieces += (t[i].n_elems * b + kPieceBytes - 1) / kPieceBytes + 1;
     }
     return pieces < (1ull << 31) ? SCAR_OK : SCAR_ERR_CAPACITY;
 }
 
-void cut(scar_gnorm *op, const scar_tensor *t, uint64_t n) {
-    op->h_pieces.clear();
+std::vector<Piece> cut(const scar_tensor *t, uint64_t n) {
+    std::vector<Piece> got;
     for (uint64_t i = 0; i < n; ++i) {
         const unsigned b = elem_size(t[i].dtype), most = kPieceBytes / b;
         const char *src = static_cast<const char *>(t[i].d_data);
@@ -224,10 +225,11 @@ void cut(scar_gnorm *op, const scar_tensor *t, uint64_t n) {
         const unsigned head = (unsigned)((uintptr_t)src % 16) / b;  // the first piece ends where a later one may begin
         for (uint64_t at = 0; at < t[i].n_elems;) {
             const uint64_t left = t[i].n_elems - at, size = most - (at ? 0 : head);
-            op->h_pieces.push_back({src + at * b, dst + at * b, (unsigned)(left < size ? left : size), t[i].dtype});
+            got.push_back({src + at * b, dst + at * b, (unsigned)(left < size ? left : size), t[i].dtype});
             at += size;
         }
     }
+    return got;
 }
 
 int upload(scar_gnorm *op) {
@@ -262,7 +264,8 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
     if (!out) return SCAR_ERR_INVALID_ARG;
     *out = nullptr;
     if (kind != SCAR_GNORM_L2 && kind != SCAR_GNORM_L1 && kind != SCAR_GNORM_MAX) return SCAR_ERR_INVALID_ARG;
-    int rc = check_tensors(h_tensors, n_tensors);
+    uint64_t most_pieces = 0;
+    int rc = check_tensors(h_tensors, n_tensors, most_pieces);
     if (rc != SCAR_OK) return rc;
     scar_gnorm *op = nullptr;
     try {
@@ -271,7 +274,7 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
             op->lengths.push_back(h_tensors[i].n_elems);
             op->types.push_back(h_tensors[i].dtype);
         }
-        cut(op, h_tensors, n_tensors);
+        op->h_pieces = cut(h_tensors, n_tensors);
     } catch (...) {
         delete op;
         return SCAR_ERR_ALLOC;
@@ -284,7 +287,8 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
         TRAIN_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, op->device));
         const unsigned most = kCtasPerSm * (unsigned)sms, n = (unsigned)op->h_pieces.size();
         op->grid = n < 1 ? 1 : (n < most ? n : most);
-        const uint64_t table = round_up((uint64_t)n * sizeof(Piece), 256), parts = round_up(op->grid * sizeof(double), 256);
+        // room for any later addresses: tensors that begin elsewhere may be cut into a piece more each
+        const uint64_t table = round_up(most_pieces * sizeof(Piece), 256), parts = round_up(op->grid * sizeof(double), 256);
         if (cudaMalloc(&op->block, table + parts + 512) != cudaSuccess) {
             cudaGetLastError();
             return SCAR_ERR_ALLOC;
@@ -307,7 +311,8 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
 
 int scar_gnorm_bind(scar_gnorm *op, const scar_tensor *h_tensors, uint64_t n_tensors) {
     if (!op) return SCAR_ERR_INVALID_ARG;
-    int rc = check_tensors(h_tensors, n_tensors);
+    uint64_t most_pieces = 0;
+    int rc = check_tensors(h_tensors, n_tensors, most_pieces);
     if (rc != SCAR_OK) return rc;
     if (n_tensors != op->lengths.size()) return SCAR_ERR_LAYOUT;
     for (uint64_t i = 0; i < n_tensors; ++i)
@@ -315,7 +320,7 @@ int scar_gnorm_bind(scar_gnorm *op, const scar_tensor *h_tensors, uint64_t n_ten
     if ((rc = check_current_device(op->device)) != SCAR_OK) return rc;
     TRAIN_TRY(cudaStreamSynchronize(op->stream));
     try {
-        cut(op, h_tensors, n_tensors);
+        op->h_pieces = cut(h_tensors, n_tensors);
     } catch (...) {
         return SCAR_ERR_ALLOC;
     }

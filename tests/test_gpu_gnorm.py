@@ -195,6 +195,31 @@ def test_equal_inputs_give_equal_bits_and_new_addresses_are_used():
 
 
 @gpu
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_new_addresses_that_begin_elsewhere(dt):
+    """Tensors of whole pieces on 16-byte boundaries are later bound to places between two: each is cut into a piece more."""
+    lengths = [16384 // torch.empty(0, dtype=TYPES[dt]).element_size()] * 300
+    ts = tensors(lengths, [TYPES[dt]], seed=9)
+    out = [torch.empty_like(t) for t in ts]
+    op = GradientNorm(ts, out=out)
+    first = float(op.clip(1.0))
+    moved = tensors(lengths, [TYPES[dt]], seed=9, lead=(1,))  # other values, too
+    place = [torch.full((n + 3,), 7.0, dtype=TYPES[dt], device="cuda") for n in lengths]
+    op.bind(moved, out=[p[1:-2] for p in place])
+    want = exact_norm(moved, "l2")
+    got = float(op.clip(want / 2))
+    assert abs(got - want) <= (SUM_TOL + 2.0 ** -23) * want and got != first
+    u = UNIT[TYPES[dt]]
+    for m, p in zip(moved, place):
+        x = m.double() / 2
+        assert bool(((p[1:-2].double() - x).abs() <= (u + SUM_TOL + 2.0 ** -21) * x.abs() + 2.0 ** -24).all())
+        assert float(p[0]) == 7.0 and bool((p[-2:] == 7.0).all())
+    op.bind(ts, out=out)
+    assert float(op.clip(1.0)) == first
+    op.close()
+
+
+@gpu
 def test_another_stream_and_a_captured_graph():
     ts = tensors([200_000, 11], [torch.float32], seed=4)
     out = [torch.empty_like(t) for t in ts]

@@ -184,7 +184,7 @@ def test_sum_and_scale(dt):
 
 @gpu
 @pytest.mark.parametrize("dt", list(TYPES))
-@pytest.mark.parametrize("T,V,D", [(1000, 500, 64), (1300, 4100, 136), (600, 70, 2000)])
+@pytest.mark.parametrize("T,V,D", [(1000, 500, 64), (1300, 4100, 136), (600, 70, 2000), (900, 301, 67), (520, 2000, 1001)])
 def test_pieces_of_rows_give_what_all_rows_at_once_give(dt, T, V, D):
     """A small workspace forces several pieces (256 rows each), the last one short; ignored rows shift the others."""
     h, w, y = make(T, V, D, TYPES[dt], seed=9, ignored=0.25)
@@ -217,6 +217,32 @@ def test_strided_and_unaligned_operands_and_untouched_gaps(dt, D):
             left = buf.clone()
             left[lead: lead + v.shape[0] * (D + gap)].view(v.shape[0], D + gap)[:, :D] = 7.0
             assert bool((left == 7.0).all()), "bytes between and around the rows were written"
+    op.close()
+
+
+@gpu
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("D", [64, 72, 67])
+def test_every_operand_off_its_boundary_by_itself(dt, D):
+    """h, w, dh and dw each moved by one element while the others lie on 16-byte boundaries: the same bits."""
+    T, V, dtype = 130, 600, TYPES[dt]
+    h, w, y = make(T, V, D, dtype, seed=13, ignored=0.2)
+    op = LinearCrossEntropy(T, V, D, dtype)
+    want = check(op, h, w, y)
+
+    def moved(m):
+        buf = torch.full((m.numel() + 9,), 7.0, dtype=dtype, device="cuda")
+        v = buf[1: 1 + m.numel()].view_as(m)
+        v.copy_(m)
+        return buf, v
+
+    for which in range(4):
+        ops = [h, w, torch.empty_like(h), torch.empty_like(w)]
+        buf, ops[which] = moved(ops[which])
+        got = op.loss_and_grad(ops[0], ops[1], y, dh=ops[2], dw=ops[3])
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), which
+        assert float(buf[0]) == 7.0 and bool((buf[-8:] == 7.0).all())
     op.close()
 
 
