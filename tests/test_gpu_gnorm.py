@@ -80,6 +80,7 @@ LISTS = {
     "one element": [1], "two": [2, 1], "zeros among them": [0, 5, 0, 0, 3, 0], "around a vector": list(range(1, 40)),
     "around a piece": [8191, 8192, 8193, 16383, 16384, 16385], "long": [3_000_001], "long and short": [1_000_003, 1, 7, 500_000, 0, 33],
     "many": [(i * 37) % 1000 + 1 for i in range(1500)],
+    "as many pieces as are resident": [4096 * 592], "one more": [4096 * 592, 5], "hundreds of short ones": [100 + i for i in range(590)],
 }
 
 
