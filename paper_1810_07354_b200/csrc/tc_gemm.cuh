@@ -574,17 +574,21 @@ template <bool KEEP> __device__ __forceinline__ void epi_stat(const TcArgs &g, f
 }
 
 // Packed 16-bit values of 32 rows x 64 columns to memory through the result's map, 32 columns at a time: the two halves of
-// the warp's stage alternate, so that one is filled while the other is read.
-template <typename F> __device__ __forceinline__ void store_halves(const CUtensorMap *map, uint8_t *stage, unsigned lane, bool any, unsigned cols, int col, int row0, F chunk) {
+// the warp's stage alternate, so that one is filled while the other is read.  `half` is the one to fill next.  It changes with
+// every store and with nothing else (a last column tile may need one half only, a warp without rows none), so the newest store,
+// the one that may still be under way when the wait ends, never reads the half that is filled.
+template <typename F> __device__ __forceinline__ void store_halves(const CUtensorMap *map, uint8_t *stage, unsigned &half, unsigned lane, bool any, unsigned cols, int col, int row0, F chunk) {
+    if (!any) return;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if (h * 32 >= cols) break;
-        uint8_t *half = stage + h * 2048;
+        uint8_t *at = stage + half * 2048;
+        half ^= 1;
         asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
         __syncwarp();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(half + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = chunk(h * 4 + c);
-        if (any) tma_store(map, smem_addr(half), col + h * 32, row0, 0);
+        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(at + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = chunk(h * 4 + c);
+        tma_store(map, smem_addr(at), col + h * 32, row0, 0);
     }
 }
 
@@ -733,6 +737,7 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
         uint8_t *stage = smem + S::kStages * S::kStageBytes + warp * kWarpStage;
         constexpr bool kRegs = PL == 3 || kLogits;  // sums over rounds, or a whole row at a time: all columns in registers
         unsigned ac = 0, aph = 0;
+        unsigned half_next = 0;  // of the stage, for store_halves
         for (unsigned i = 0; take_turn<N>(walks, i, pair, pairs, t); ++i) {
             const TcArgs &g = set.p[N == 1 ? 0 : t.which];
             const unsigned rounds = t.k1 > t.k0 ? (kPer == 1 ? t.k1 - t.k0 : (t.k1 - t.k0 - 1) / kPer + 1) : 0u;
@@ -787,8 +792,8 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
 #pragma unroll 1
                         for (int j = 0; j < 2; ++j) {
                             if (j * 64 >= left) break;
-                            if (j == 0) store_halves(&g.c, stage, lane, rows.has(0), left, (int)col, (int)rows.row0, [&](int c) { return pack_half8(v + c * 8); });
-                            else store_halves(&g.c, stage, lane, rows.has(0), left - 64, (int)col + 64, (int)rows.row0, [&](int c) { return pack_half8(v + 64 + c * 8); });
+                            if (j == 0) store_halves(&g.c, stage, half_next, lane, rows.has(0), left, (int)col, (int)rows.row0, [&](int c) { return pack_half8(v + c * 8); });
+                            else store_halves(&g.c, stage, half_next, lane, rows.has(0), left - 64, (int)col + 64, (int)rows.row0, [&](int c) { return pack_half8(v + 64 + c * 8); });
                         }
                     }
                 } else {
@@ -843,7 +848,7 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
                         for (int i = 0; i < 64; ++i) v[i] *= f;
                         const bool bf = g.out_type == SCAR_BF16;
                         if (g.c_map) {
-                            store_halves(&g.c, stage, lane, rows.has(0), g.n - (col + j), (int)(col + j), (int)rows.row0,
+                            store_halves(&g.c, stage, half_next, lane, rows.has(0), g.n - (col + j), (int)(col + j), (int)rows.row0,
                                          [&](int c) { return bf ? pack_bf8(v + c * 8) : pack_half8(v + c * 8); });
                             j += 64;
                             continue;

@@ -336,6 +336,26 @@ def test_equal_inputs_give_equal_bits(dt):
 
 
 @gpu
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("T,V,D", [
+    (48, 60_000, 72), (20, 90_000, 24), (64, 40_000, 264), (30, 30_000, 520),  # dw: the last columns fill half a stage, on every tile
+    (1500, 30_017, 64), (700, 20_001, 128), (300, 45_031, 96),                 # exponentials: the same, and row tiles that end early
+])
+def test_results_stored_while_the_next_ones_are_staged(dt, T, V, D):
+    """Many tiles per CTA pair whose products take less time than their results: each of them waits for the stage that the
+    one before is still stored from.  Every value within its bound, and the same bits every time."""
+    h, w, y = make(T, V, D, TYPES[dt], seed=T + D)
+    op = LinearCrossEntropy(T, V, D, TYPES[dt])
+    first = check(op, h, w, y)
+    dh, dw, row = torch.empty_like(h), torch.empty_like(w), torch.empty(T, device="cuda")
+    for _ in range(30):
+        dw.fill_(7.0)
+        op.loss_and_grad(h, w, y, row_loss=row, dh=dh, dw=dw)
+        assert torch.equal(row, first[1]) and torch.equal(dh, first[2]) and torch.equal(dw, first[3])
+    op.close()
+
+
+@gpu
 def test_gradient_against_differences():
     """Central differences of the float32 operator's own loss along random directions.  The loss is smooth with a third
     derivative of order one along a unit step; with a step of 2^-5 the truncation is below 2^-10 / 6 and the rounding
