@@ -515,8 +515,9 @@ int scar_xent_destroy(scar_xent *op);
  *   norm = sqrt(sum g^2) | sum |g| | max |g|        (scar_gnorm_kind)
  *   coef = min(1, max_norm / norm), 1 when norm is 0
  *   out_i = coef * g_i, rounded once
- * Sums run in float32 over short runs and in double across them, in an order that
- * depends on the lengths and on the addresses modulo 16: equal inputs give equal bits.  A NaN or an infinity in
+ * Sums run in float32 over short runs (in double where a sum would leave float32's
+ * range, so any finite tensors have a finite norm in scar_gnorm_info; the float32 of it
+ * may be infinite) and in double across them, in an order that depends on the lengths and on the addresses modulo 16: equal inputs give equal bits.  A NaN or an infinity in
  * the tensors gives the IEEE result of these formulas (norm NaN: all outputs NaN; norm
  * infinite: coef 0, NaN where g is infinite) and is reported (scar_gnorm_status), so
  * that a caller can leave the step out. */

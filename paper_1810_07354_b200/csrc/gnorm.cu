@@ -90,18 +90,49 @@ template <typename T> struct Split {
     }
 };
 
-template <int KIND, typename T> __device__ __forceinline__ double piece_norm(const Piece &p) {
-    const Split<T> s(p);
-    Vec<T> x[kVecs];
-    s.load(x);
-    float a[2] = {0.f, 0.f};
+// A thread's values of a piece again, in double: a finite value's square is one there, whatever its size.
+template <int KIND, typename T> __device__ __noinline__ double wide_terms(Split<T> s) {
+    double a = 0.0;
+    auto add = [&](double v) { a += KIND == SCAR_GNORM_L2 ? v * v : fabs(v); };
     const unsigned e = s.edge(threadIdx.x);
-    if (e < s.n && threadIdx.x < 2 * Vec<T>::n) add_term<KIND>(a[0], to_f32<T>(s.src[e]));
+    if (e < s.n && threadIdx.x < 2 * Vec<T>::n) add(to_f32<T>(s.src[e]));
+    for (unsigned at = threadIdx.x; at < s.vecs; at += kNormThreads) {
+        const T *v = s.src + s.head + at * Vec<T>::n;
+        for (int j = 0; j < Vec<T>::n; ++j) add(to_f32<T>(v[j]));
+    }
+    return a;
+}
+
+// The terms of a thread's values (at most 33 of a 16-bit type): x its vectors, xe its edge element or 0.  They are summed in
+// float32, unless the sum leaves its range: squares of values above 1.8e19 are no float32, those of values below 1e-19 lose
+// bits or vanish.  A sum of at least 2^-120 has lost less than 2^-24 of itself (33 squares, each off by at most 2^-150); below
+// that, or not finite, the values are read again and summed in double (so are NaN and infinities, with the same result).
+template <int KIND, typename T> __device__ __forceinline__ double thread_terms(const Split<T> &s, const Vec<T> (&x)[kVecs], float xe) {
+    float a[2] = {0.f, 0.f};
+    add_term<KIND>(a[0], xe);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
 #pragma unroll
         for (int j = 0; j < Vec<T>::n; ++j) add_term<KIND>(a[j & 1], to_f32<T>(x[i].v[j]));
+    if (KIND != SCAR_GNORM_MAX) {
+        const float sum = a[0] + a[1];
+        if (!(sum >= (KIND == SCAR_GNORM_L2 ? 0x1p-120f : 0.f) && sum <= 3.402823466e38f)) {
+            constexpr unsigned kMagnitude = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+            unsigned any = __float_as_uint(xe) & 0x7fffffffu;
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) any |= (x[i].u.x | x[i].u.y | x[i].u.z | x[i].u.w) & kMagnitude;
+            if (any) return wide_terms<KIND, T>(s);  // not for zeros alone
+        }
+    }
     return join<KIND>((double)a[0], (double)a[1]);
+}
+
+template <int KIND, typename T> __device__ __forceinline__ double piece_norm(const Piece &p) {
+    const Split<T> s(p);
+    Vec<T> x[kVecs];
+    s.load(x);
+    const unsigned e = s.edge(threadIdx.x);
+    return thread_terms<KIND, T>(s, x, e < s.n && threadIdx.x < 2 * Vec<T>::n ? to_f32<T>(s.src[e]) : 0.f);
 }
 
 // From the joined sums: the record and the caller's copy of the norm.  Returns the factor.
@@ -206,13 +237,7 @@ __device__ __forceinline__ void clip_piece(const Piece &p, double *part, unsigne
     const unsigned e = s.edge(threadIdx.x);
     const bool edge = e < s.n && threadIdx.x < 2 * Vec<T>::n;
     const float xe = edge ? to_f32<T>(s.src[e]) : 0.f;
-    float a[2] = {0.f, 0.f};
-    add_term<KIND>(a[0], xe);
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-        for (int j = 0; j < Vec<T>::n; ++j) add_term<KIND>(a[j & 1], to_f32<T>(x[i].v[j]));
-    double v = cta_join<KIND>(join<KIND>(0.0, join<KIND>((double)a[0], (double)a[1])), sh);
+    double v = cta_join<KIND>(join<KIND>(0.0, thread_terms<KIND, T>(s, x, xe)), sh);
     if (threadIdx.x == 0) {
         part[blockIdx.x] = v;
         __threadfence();

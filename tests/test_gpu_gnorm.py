@@ -176,6 +176,50 @@ def test_values_whose_squares_leave_float32():
 
 
 @gpu
+@pytest.mark.parametrize("lengths", [[5000, 3, 17], [3_000_001, 40, 0, 777_777]], ids=["one launch", "two launches"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e30, 3e38, 1e-15, 1e-19, 1e-21, 1e-25, 1e-30, 1e-38])
+def test_l2_of_values_whose_squares_leave_float32(size, dt, lengths):
+    """The squares of these values are no float32, or have lost their bits; the norm is an ordinary one."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    ts = [torch.rand(n, generator=g, device="cuda").add_(0.1).mul_(size / 1.1).to(TYPES[dt]) for n in lengths]
+    want = exact_norm(ts, "l2")
+    out = [torch.empty_like(t) for t in ts]
+    op = GradientNorm(ts, out=out)
+    limit = float(torch.tensor(0.25 * want if want < 1e38 else 3e38))
+    tol = SUM_TOL + 2.0 ** -23
+    for got in (op.norm(), op.clip(limit)):
+        if want < 3e38:
+            assert abs(float(got) - want) <= tol * want + 2.0 ** -149
+        else:
+            assert float(got) == math.inf, "the float32 of a norm above its range"
+    info = op.status()
+    assert abs(info.norm - want) <= tol * want and abs(info.coef - limit / want) <= tol * info.coef and info.nonfinite == 0
+    u = UNIT[TYPES[dt]]
+    for t, o in zip(ts, out):
+        x = t.double() * (limit / want)
+        assert bool(((o.double() - x).abs() <= (u + tol + 2.0 ** -21) * x.abs() + (2.0 ** -149 if dt == "f32" else 2.0 ** -133)).all())
+    op.close()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["l2", "l1", "max"])
+@pytest.mark.parametrize("n", [5000, 3_000_001])
+def test_values_of_all_sizes_and_zeros_together(n, kind):
+    """One huge value among tiny ones and zeros, and tiny ones among zeros; sums of magnitudes above float32's range."""
+    for many, few in ((0.0, 1e-30), (1e-30, 1e25), (0.0, 1e25), (1e-25, 1.0), (3e38, 1e-30)):
+        t = torch.full((n,), many, device="cuda")
+        t[[1, n // 2, n - 1]] = few
+        op = GradientNorm([t], out=[torch.empty_like(t)], kind=kind)
+        want = exact_norm([t], kind)
+        op.clip(1.0)
+        info = op.status()
+        assert abs(info.norm - want) <= SUM_TOL * want and info.nonfinite == 0
+        assert abs(info.coef - min(1.0, 1.0 / want)) <= 2.0 ** -16 * info.coef
+        op.close()
+
+
+@gpu
 def test_equal_inputs_give_equal_bits_and_new_addresses_are_used():
     ts = tensors([100_003, 17, 900_000], [torch.bfloat16, torch.float32], seed=3)
     op = GradientNorm(ts)
