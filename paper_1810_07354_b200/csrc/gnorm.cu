@@ -203,6 +203,15 @@ template <typename T> __device__ __forceinline__ void store_scaled(const Split<T
         }
     }
 }
+// A factor below this has lost bits as a float32 or is about to: the values are scaled in double then (a norm far above the
+// limit, as only values near float32's largest give it), one by one, since such a call is rare.
+constexpr double kLeastCoef = 0x1p-100;
+template <typename T> __device__ __noinline__ void scale_wide(const void *src, void *dst, unsigned n, double coef) {
+    const T *s = static_cast<const T *>(src);
+    T *d = static_cast<T *>(dst);
+    for (unsigned i = threadIdx.x; i < n; i += kNormThreads) d[i] = from_f32<T>((float)((double)to_f32<T>(s[i]) * coef));
+}
+__device__ __forceinline__ bool is_wide(double coef) { return coef > 0.0 && coef < kLeastCoef; }
 template <typename T> __device__ __forceinline__ void scale_piece(const Piece &p, float coef) {
     const Split<T> s(p);
     Vec<T> x[kVecs];
@@ -217,6 +226,12 @@ __global__ void __launch_bounds__(kNormThreads, kCtasPerSm)
 k_gnorm_scale(const Piece *__restrict__ pieces, const NormRecord *rec) {
     const Piece p = pieces[gridDim.x - 1 - blockIdx.x];
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (is_wide(rec->coef)) {
+        if (p.dtype == SCAR_F32) scale_wide<float>(p.src, p.dst, p.n, rec->coef);
+        else if (p.dtype == SCAR_BF16) scale_wide<__nv_bfloat16>(p.src, p.dst, p.n, rec->coef);
+        else scale_wide<__half>(p.src, p.dst, p.n, rec->coef);
+        return;
+    }
     const float coef = (float)rec->coef;
     if (p.dtype == SCAR_F32) scale_piece<float>(p, coef);
     else if (p.dtype == SCAR_BF16) scale_piece<__nv_bfloat16>(p, coef);
@@ -230,7 +245,7 @@ k_gnorm_scale(const Piece *__restrict__ pieces, const NormRecord *rec) {
 // gives up after a second: nothing is then written and the record says so.  Measured against the two launches: 7.0 / 9.2 us
 // for 2^20 float32 values (most of it the launch), 9.2 / 10.3 us for 2.3 million.
 template <int KIND, typename T>
-__device__ __forceinline__ void clip_piece(const Piece &p, double *part, unsigned *ticket, float max_norm, NormRecord *rec, float *d_norm, double *sh, float *factor) {
+__device__ __forceinline__ void clip_piece(const Piece &p, double *part, unsigned *ticket, float max_norm, NormRecord *rec, float *d_norm, double *sh, double *factor) {
     const Split<T> s(p);
     Vec<T> x[kVecs];
     s.load(x);
@@ -254,22 +269,26 @@ __device__ __forceinline__ void clip_piece(const Piece &p, double *part, unsigne
                 if (now - t0 > 1000000000ull) break;
             }
         }
-        *factor = there ? 0.f : -1.f;
+        *factor = there ? 0.0 : -1.0;
         if (!there) rec->error = 1;
     }
     __syncthreads();
-    if (*factor < 0.f) return;
+    if (*factor < 0.0) return;
     v = 0.0;
     for (unsigned i = threadIdx.x; i < gridDim.x; i += kNormThreads) v = join<KIND>(v, __ldcg(part + i));
     __syncthreads();
     v = cta_join<KIND>(v, sh);
     if (threadIdx.x == 0) {
         if (blockIdx.x == 0) write_record<KIND>(v, max_norm, true, rec, d_norm);
-        *factor = (float)norm_factor<KIND>(v, max_norm, true);
+        *factor = norm_factor<KIND>(v, max_norm, true);
         if (atomicAdd(ticket + 1, 1u) == gridDim.x - 1) ticket[0] = ticket[1] = 0;
     }
     __syncthreads();
-    const float coef = *factor;
+    if (is_wide(*factor)) {
+        scale_wide<T>(p.src, p.dst, p.n, *factor);
+        return;
+    }
+    const float coef = (float)*factor;
     T *d = static_cast<T *>(p.dst);
     if (edge) d[e] = from_f32<T>(xe * coef);
     store_scaled(s, x, d, p, coef);
@@ -278,7 +297,7 @@ template <int KIND>
 __global__ void __launch_bounds__(kNormThreads, kCtasPerSm / 2)
 k_gnorm_clip(const Piece *__restrict__ pieces, double *part, unsigned *ticket, float max_norm, NormRecord *rec, float *d_norm) {
     __shared__ double sh[32];
-    __shared__ float factor;
+    __shared__ double factor;
     const Piece p = pieces[blockIdx.x];
     if (p.dtype == SCAR_F32) clip_piece<KIND, float>(p, part, ticket, max_norm, rec, d_norm, sh, &factor);
     else if (p.dtype == SCAR_BF16) clip_piece<KIND, __nv_bfloat16>(p, part, ticket, max_norm, rec, d_norm, sh, &factor);

@@ -220,6 +220,27 @@ def test_values_of_all_sizes_and_zeros_together(n, kind):
 
 
 @gpu
+@pytest.mark.parametrize("n", [5003, 3_000_001], ids=["one launch", "two launches"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_a_limit_far_below_the_norm(dt, n):
+    """The factor is below float32's normal range (3e-43 here, 8 bits of one); the scaled values are not."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    for lead in (0, 1):
+        t = torch.rand(n + lead, generator=g, device="cuda").add_(0.1).mul_(2e38).to(TYPES[dt])[lead:]
+        want = exact_norm([t], "l2")
+        limit = float(torch.tensor(3e-43 * want))
+        out = torch.empty_like(t)
+        ops = [GradientNorm([t], out=[out]), GradientNorm([t.clone()])]
+        ops[0].clip(limit)
+        x = t.double() * (limit / want)
+        u = UNIT[TYPES[dt]]
+        assert bool(((out.double() - x).abs() <= (u + SUM_TOL + 2.0 ** -21) * x.abs()).all())
+        ops[1].clip(limit)
+        assert torch.equal(ops[1]._tensors[0], out)
+        [op.close() for op in ops]
+
+
+@gpu
 def test_equal_inputs_give_equal_bits_and_new_addresses_are_used():
     ts = tensors([100_003, 17, 900_000], [torch.bfloat16, torch.float32], seed=3)
     op = GradientNorm(ts)
