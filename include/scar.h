@@ -543,7 +543,8 @@ typedef struct {
  * (the same as NULL) but may not overlap another tensor.  Waits for the stream. */
 int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_tensors, scar_gnorm_kind kind,
                     void *cuda_stream);
-/* New addresses for the same lengths and types (SCAR_ERR_LAYOUT otherwise).  Waits for the stream. */
+/* New addresses for the same lengths and types (SCAR_ERR_LAYOUT otherwise; the tensors registered before then stay).
+ * Waits for the stream.  Graphs that hold captured calls work on the new tensors from then on. */
 int scar_gnorm_bind(scar_gnorm *op, const scar_tensor *h_tensors, uint64_t n_tensors);
 /* The norm alone.  d_norm: DEVICE float or NULL.  Enqueue only. */
 int scar_gnorm_norm(scar_gnorm *op, float *d_norm);

@@ -1,14 +1,16 @@
 // Global gradient norm over a list of tensors, and clipping (scar_gnorm_* of scar.h).
 //
-// The tensors are cut into pieces of at most kPieceBytes on the host, once, so that every piece but a tensor's first
-// begins on a 16-byte boundary.  A CTA walks over pieces with a fixed stride: which CTA adds what depends on the lengths
-// and the addresses modulo 16 alone, the last CTA to finish adds the CTAs' sums in their order, and the result is the same bits every time.
+// The tensors are cut into pieces of kPieceBytes on the host, once, so that every piece but a tensor's first begins on a
+// 16-byte boundary.  A CTA walks over pieces with a fixed stride: on one GPU, which CTA adds what depends on the lengths, the
+// types and the addresses modulo 16 alone.  The last CTA to finish adds the CTAs' sums in their order: the result is the
+// same bits every time.
 // Bound by HBM: one read for the norm, one read and one write for the scaled values.  The second kernel is launched
 // while the first runs (programmatic launch) and takes the pieces backwards, so that what the first read last is still
 // in L2; it has one CTA per piece, started in order, because CTAs that walk over pieces drift apart and then read and
 // write all over memory at once (a billion bfloat16 values: norm and scaling 901 us this way, 1077 with walking CTAs).
 // The norm alone reads 400 MB in 61 us (6.5 TB/s); pieces of 16 KiB rather than 32 are for lists of short tensors
 // (1200 tensors, 80 MB: 43.0 against 43.8 us).
+#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -326,7 +328,7 @@ struct scar_gnorm {
 
 namespace {
 
-// Also gives the most pieces that tensors of these lengths can be cut into, wherever they lie.
+// Also gives the pieces that tensors of these lengths are cut into, wherever they lie.
 int check_tensors(const scar_tensor *t, uint64_t n, uint64_t &pieces) {
     pieces = 0;
     if (n && !t) return SCAR_ERR_INVALID_ARG;
@@ -336,21 +338,26 @@ int check_tensors(const scar_tensor *t, uint64_t n, uint64_t &pieces) {
         if (t[i].n_elems >= (1ull << 48)) return SCAR_ERR_LAYOUT;
         if (t[i].n_elems && !t[i].d_data) return SCAR_ERR_INVALID_ARG;
         if ((uintptr_t)t[i].d_data % b || (uintptr_t)t[i].d_out % b) return SCAR_ERR_INVALID_ARG;
-        if (t[i].n_elems) pieces += (t[i].n_elems * b + kPieceBytes - 1) / kPieceBytes + 1;
+        pieces += (t[i].n_elems * b + kPieceBytes - 1) / kPieceBytes;
     }
     return pieces < (1ull << 31) ? SCAR_OK : SCAR_ERR_CAPACITY;
 }
 
+// A tensor of b bytes has ceil(b / kPieceBytes) pieces wherever it lies, so that new addresses change neither the launches nor
+// their grids (a captured call stays right).  The first piece takes the elements before a 16-byte boundary and a piece's worth
+// behind them; what is left for the last one may then be nothing.
 std::vector<Piece> cut(const scar_tensor *t, uint64_t n) {
     std::vector<Piece> got;
     for (uint64_t i = 0; i < n; ++i) {
         const unsigned b = elem_size(t[i].dtype), most = kPieceBytes / b;
         const char *src = static_cast<const char *>(t[i].d_data);
         char *dst = t[i].d_out ? static_cast<char *>(t[i].d_out) : const_cast<char *>(src);
-        const unsigned head = (unsigned)((uintptr_t)src % 16) / b;  // the first piece ends where a later one may begin
-        for (uint64_t at = 0; at < t[i].n_elems;) {
-            const uint64_t left = t[i].n_elems - at, size = most - (at ? 0 : head);
-            got.push_back({src + at * b, dst + at * b, (unsigned)(left < size ? left : size), t[i].dtype});
+        const unsigned head = (unsigned)((0u - (uintptr_t)src) % 16) / b;
+        const uint64_t pieces = (t[i].n_elems + most - 1) / most;
+        uint64_t at = 0;
+        for (uint64_t p = 0; p < pieces; ++p) {
+            const uint64_t left = t[i].n_elems - at, size = std::min<uint64_t>(left, most + (p ? 0 : head));
+            got.push_back({src + at * b, dst + at * b, (unsigned)size, t[i].dtype});
             at += size;
         }
     }
@@ -395,8 +402,8 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
     if (!out) return SCAR_ERR_INVALID_ARG;
     *out = nullptr;
     if (kind != SCAR_GNORM_L2 && kind != SCAR_GNORM_L1 && kind != SCAR_GNORM_MAX) return SCAR_ERR_INVALID_ARG;
-    uint64_t most_pieces = 0;
-    int rc = check_tensors(h_tensors, n_tensors, most_pieces);
+    uint64_t n_pieces = 0;
+    int rc = check_tensors(h_tensors, n_tensors, n_pieces);
     if (rc != SCAR_OK) return rc;
     scar_gnorm *op = nullptr;
     try {
@@ -422,8 +429,7 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
         const unsigned most = kCtasPerSm * (unsigned)sms, n = (unsigned)op->h_pieces.size();
         op->grid = n < 1 ? 1 : (n < most ? n : most);
         op->resident = coop ? (unsigned)(per_sm * sms < (int)most ? per_sm * sms : (int)most) : 0u;
-        // room for any later addresses: tensors that begin elsewhere may be cut into a piece more each
-        const uint64_t table = round_up(most_pieces * sizeof(Piece), 256), parts = round_up(most * sizeof(double), 256);  // bound tensors may have more pieces
+        const uint64_t table = round_up(n_pieces * sizeof(Piece), 256), parts = round_up(op->grid * sizeof(double), 256);
         if (cudaMalloc(&op->block, table + parts + 512) != cudaSuccess) {
             cudaGetLastError();
             return SCAR_ERR_ALLOC;
@@ -446,8 +452,8 @@ int scar_gnorm_init(scar_gnorm **out, const scar_tensor *h_tensors, uint64_t n_t
 
 int scar_gnorm_bind(scar_gnorm *op, const scar_tensor *h_tensors, uint64_t n_tensors) {
     if (!op) return SCAR_ERR_INVALID_ARG;
-    uint64_t most_pieces = 0;
-    int rc = check_tensors(h_tensors, n_tensors, most_pieces);
+    uint64_t n_pieces = 0;
+    int rc = check_tensors(h_tensors, n_tensors, n_pieces);
     if (rc != SCAR_OK) return rc;
     if (n_tensors != op->lengths.size()) return SCAR_ERR_LAYOUT;
     for (uint64_t i = 0; i < n_tensors; ++i)

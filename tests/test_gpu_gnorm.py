@@ -317,6 +317,37 @@ def test_another_stream_and_a_captured_graph():
 
 
 @gpu
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("pieces", [3, 700], ids=["one launch", "two launches"])
+def test_a_captured_call_follows_new_addresses(dt, pieces):
+    """A graph holds a call's launches; bind then gives tensors that begin between two 16-byte boundaries, and others again."""
+    size = torch.empty(0, dtype=TYPES[dt]).element_size()
+    lengths = [16384 // size * pieces, 16384 // size, 5, 2 * 16384 // size - 1]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ts = tensors(lengths, [TYPES[dt]], seed=3)
+        op = GradientNorm(ts, stream=side)
+        norm = op.norm()  # the first call of the kernels is not a captured one
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            norm = op.clip(1.0)
+        for seed, lead in ((4, (1, 2, 3, 0)), (5, (0,)), (6, (7, 0, 1, 5))):
+            moved = tensors(lengths, [TYPES[dt]], seed=seed, lead=lead)
+            keep = [m.clone() for m in moved]
+            side.synchronize()
+            op.bind(moved)
+            graph.replay()
+            want = exact_norm(keep, "l2")
+            assert abs(float(norm) - want) <= (SUM_TOL + 2.0 ** -23) * want
+            for m, k in zip(moved, keep):
+                x = k.double() / want
+                tiny = 2.0 ** -24 if dt == "f16" else 0.0
+                assert bool(((m.double() - x).abs() <= (UNIT[TYPES[dt]] + SUM_TOL + 2.0 ** -21) * x.abs() + tiny).all())
+    side.synchronize()
+    op.close()
+
+
+@gpu
 def test_refusals():
     t = torch.ones(8, device="cuda")
     with pytest.raises(TypeError):
