@@ -550,9 +550,14 @@ int scar_gnorm_bind(scar_gnorm *op, const scar_tensor *h_tensors, uint64_t n_ten
 int scar_gnorm_norm(scar_gnorm *op, float *d_norm);
 /* Norm and scaled outputs; max_norm >= 0 (infinity leaves the values as they are).  Enqueue only. */
 int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm);
-/* Waits for the stream and returns the record of the most recent call.  SCAR_ERR_TIMEOUT if a wait inside a call's
- * kernel gave up since the last status (its outputs are then invalid; the operator is usable again). */
+/* Waits for the stream and returns the record of the most recent call. */
 int scar_gnorm_status(scar_gnorm *op, scar_gnorm_info *out);
+/* Short lists are clipped in one launch whose CTAs wait for one another, for a millisecond at most: if a kernel of another
+ * stream keeps some of them from starting for longer, the last one to run finishes the call by itself, with the same
+ * bits.  scar_gnorm_finished_alone waits for the stream and counts the calls that ended this way;
+ * scar_gnorm_selftest_arm_timeout makes the next clipping in one launch end so (host state only). */
+int scar_gnorm_finished_alone(scar_gnorm *op, uint64_t *calls);
+int scar_gnorm_selftest_arm_timeout(scar_gnorm *op);
 uint64_t scar_gnorm_launch_count(const scar_gnorm *op);
 int scar_gnorm_destroy(scar_gnorm *op);
 

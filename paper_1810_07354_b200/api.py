@@ -134,6 +134,8 @@ _SIGS = {
     "scar_gnorm_norm": (_int, [_vp, _vp]),
     "scar_gnorm_clip": (_int, [_vp, C.c_float, _vp]),
     "scar_gnorm_status": (_int, [_vp, C.POINTER(scar_gnorm_info)]),
+    "scar_gnorm_finished_alone": (_int, [_vp, C.POINTER(_u64)]),
+    "scar_gnorm_selftest_arm_timeout": (_int, [_vp]),
     "scar_gnorm_launch_count": (_u64, [_vp]),
     "scar_gnorm_destroy": (_int, [_vp]),
     "scar_ckpt_destroy": (_int, [_vp]),
@@ -514,6 +516,16 @@ def scar_gnorm_status(op: int) -> scar_gnorm_info:
     out = scar_gnorm_info()
     _check(load_library().scar_gnorm_status(op, C.byref(out)), "scar_gnorm_status")
     return out
+
+
+def scar_gnorm_finished_alone(op: int) -> int:
+    calls = _u64()
+    _check(load_library().scar_gnorm_finished_alone(op, C.byref(calls)), "scar_gnorm_finished_alone")
+    return int(calls.value)
+
+
+def scar_gnorm_selftest_arm_timeout(op: int) -> None:
+    _check(load_library().scar_gnorm_selftest_arm_timeout(op), "scar_gnorm_selftest_arm_timeout")
 
 
 def scar_gnorm_launch_count(op: int) -> int:

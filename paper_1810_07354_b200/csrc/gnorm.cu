@@ -36,7 +36,7 @@ struct NormRecord {
     double norm;
     double coef;
     unsigned long long nonfinite;
-    unsigned long long error;  // a wait gave up since this was last read
+    unsigned long long alone;  // calls that one CTA had to finish (k_gnorm_clip)
 };
 
 // One term of the norm, and how two partial results join.
@@ -224,30 +224,72 @@ template <typename T> __device__ __forceinline__ void scale_piece(const Piece &p
     store_scaled(s, x, d, p, coef);
 }
 
-__global__ void __launch_bounds__(kNormThreads, kCtasPerSm)
-k_gnorm_scale(const Piece *__restrict__ pieces, const NormRecord *rec) {
-    const Piece p = pieces[gridDim.x - 1 - blockIdx.x];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (is_wide(rec->coef)) {
-        if (p.dtype == SCAR_F32) scale_wide<float>(p.src, p.dst, p.n, rec->coef);
-        else if (p.dtype == SCAR_BF16) scale_wide<__nv_bfloat16>(p.src, p.dst, p.n, rec->coef);
-        else scale_wide<__half>(p.src, p.dst, p.n, rec->coef);
+__device__ __forceinline__ void scale_any(const Piece &p, double by) {
+    if (is_wide(by)) {
+        if (p.dtype == SCAR_F32) scale_wide<float>(p.src, p.dst, p.n, by);
+        else if (p.dtype == SCAR_BF16) scale_wide<__nv_bfloat16>(p.src, p.dst, p.n, by);
+        else scale_wide<__half>(p.src, p.dst, p.n, by);
         return;
     }
-    const float coef = (float)rec->coef;
+    const float coef = (float)by;
     if (p.dtype == SCAR_F32) scale_piece<float>(p, coef);
     else if (p.dtype == SCAR_BF16) scale_piece<__nv_bfloat16>(p, coef);
     else scale_piece<__half>(p, coef);
 }
 
-// Both steps in one cooperative launch, for lists of so few pieces that every one has a resident CTA (four per SM:
-// up to 9.7 MB): a CTA
-// keeps its piece in registers, leaves its part, waits until all parts are there and joins them itself, in the order of
-// k_gnorm_norm.  ticket[0] counts parts, ticket[1] the CTAs that have read them; the last of those clears both.  The wait
-// gives up after a second: nothing is then written and the record says so.  Measured against the two launches: 7.0 / 9.2 us
-// for 2^20 float32 values (most of it the launch), 9.2 / 10.3 us for 2.3 million.
+__global__ void __launch_bounds__(kNormThreads, kCtasPerSm)
+k_gnorm_scale(const Piece *__restrict__ pieces, const NormRecord *rec) {
+    const Piece p = pieces[gridDim.x - 1 - blockIdx.x];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    scale_any(p, rec->coef);
+}
+
+// Both steps in one cooperative launch, for lists of so few pieces that every one has a resident CTA (four per SM: up to
+// 9.7 MB): a CTA keeps its piece in registers, leaves its part, waits until all parts are there and joins them itself, in the
+// order of k_gnorm_norm.  Measured against the two launches: 7.0 / 9.2 us for 2^20 float32 values (most of it the launch), 9.2 / 10.3 us for
+// 2.3 million.
+//
+// ticket[0] counts parts, ticket[1] the CTAs that are done with them; the last of those clears both.  A kernel of another stream
+// may keep some of the CTAs from starting for as long as it likes, so the wait has an end (kPatienceNs): a CTA that reaches it
+// sets kGaveUp in ticket[0], unless all parts are there by then.  The CTAs agree, since the count cannot reach the grid's
+// without the bit once the bit is set: either all of them go on as above, or none does, and each leaves without having written
+// anything.  The last one to leave then finds all parts, whenever that is, and finishes the call by itself: same order, same bits.
+constexpr unsigned kGaveUp = 0x80000000u;
+constexpr unsigned long long kPatienceNs = 1000000ull;
+
+// Thread 0 of a CTA whose part is in place: true when all are there, false when the CTAs gave up.
+__device__ __forceinline__ bool all_parts(unsigned *ticket, unsigned long long patience_ns) {
+    __threadfence();
+    atomicAdd(ticket, 1u);
+    unsigned long long t0 = 0, now;
+    for (unsigned i = 1;; ++i) {
+        unsigned got;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(got) : "l"(ticket) : "memory");
+        if (got & kGaveUp) return false;
+        if (patience_ns) {
+            if (got == gridDim.x) return true;
+            if (i & 255u) continue;
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+            if (!t0) t0 = now;
+            if (now - t0 <= patience_ns) continue;
+        }
+        if (atomicCAS(ticket, got, got | kGaveUp) == got) return false;
+    }
+}
+
+enum After { kScaleMine, kLeave, kScaleAll };
+
+template <int KIND> __device__ __forceinline__ double join_parts(const double *part, double *sh) {
+    double v = 0.0;
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += kNormThreads) v = join<KIND>(v, __ldcg(part + i));
+    __syncthreads();
+    return cta_join<KIND>(v, sh);
+}
+
+// True for the CTA that is to scale all pieces by *factor.
 template <int KIND, typename T>
-__device__ __forceinline__ void clip_piece(const Piece &p, double *part, unsigned *ticket, float max_norm, NormRecord *rec, float *d_norm, double *sh, double *factor) {
+__device__ __forceinline__ bool clip_piece(const Piece &p, double *part, unsigned *ticket, float max_norm, unsigned long long patience_ns, NormRecord *rec, float *d_norm,
+                                           double *sh, double *factor, After *after) {
     const Split<T> s(p);
     Vec<T> x[kVecs];
     s.load(x);
@@ -257,53 +299,48 @@ __device__ __forceinline__ void clip_piece(const Piece &p, double *part, unsigne
     double v = cta_join<KIND>(join<KIND>(0.0, thread_terms<KIND, T>(s, x, xe)), sh);
     if (threadIdx.x == 0) {
         part[blockIdx.x] = v;
-        __threadfence();
-        atomicAdd(ticket, 1u);
-        unsigned long long t0 = 0, now;
-        bool there = false;
-        for (unsigned i = 0; !there; ++i) {
-            unsigned got;
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(got) : "l"(ticket) : "memory");
-            there = got >= gridDim.x;
-            if ((i & 255u) == 255u) {
-                asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
-                if (!t0) t0 = now;
-                if (now - t0 > 1000000000ull) break;
-            }
+        *after = kScaleMine;
+        if (!all_parts(ticket, patience_ns)) {
+            *after = atomicAdd(ticket + 1, 1u) == gridDim.x - 1 ? kScaleAll : kLeave;
+            __threadfence();
         }
-        *factor = there ? 0.0 : -1.0;
-        if (!there) rec->error = 1;
     }
     __syncthreads();
-    if (*factor < 0.0) return;
-    v = 0.0;
-    for (unsigned i = threadIdx.x; i < gridDim.x; i += kNormThreads) v = join<KIND>(v, __ldcg(part + i));
-    __syncthreads();
-    v = cta_join<KIND>(v, sh);
+    const After then = *after;
+    if (then == kLeave) return false;
+    v = join_parts<KIND>(part, sh);
     if (threadIdx.x == 0) {
-        if (blockIdx.x == 0) write_record<KIND>(v, max_norm, true, rec, d_norm);
+        if (blockIdx.x == 0 || then == kScaleAll) write_record<KIND>(v, max_norm, true, rec, d_norm);
         *factor = norm_factor<KIND>(v, max_norm, true);
-        if (atomicAdd(ticket + 1, 1u) == gridDim.x - 1) ticket[0] = ticket[1] = 0;
+        if (then == kScaleAll) rec->alone += 1;
+        if (then == kScaleAll || atomicAdd(ticket + 1, 1u) == gridDim.x - 1) ticket[0] = ticket[1] = 0;
     }
     __syncthreads();
+    if (then == kScaleAll) return true;
     if (is_wide(*factor)) {
         scale_wide<T>(p.src, p.dst, p.n, *factor);
-        return;
+        return false;
     }
     const float coef = (float)*factor;
     T *d = static_cast<T *>(p.dst);
     if (edge) d[e] = from_f32<T>(xe * coef);
     store_scaled(s, x, d, p, coef);
+    return false;
 }
 template <int KIND>
 __global__ void __launch_bounds__(kNormThreads, kCtasPerSm / 2)
-k_gnorm_clip(const Piece *__restrict__ pieces, double *part, unsigned *ticket, float max_norm, NormRecord *rec, float *d_norm) {
+k_gnorm_clip(const Piece *__restrict__ pieces, double *part, unsigned *ticket, float max_norm, unsigned long long patience_ns, NormRecord *rec, float *d_norm) {
     __shared__ double sh[32];
     __shared__ double factor;
+    __shared__ After after;
     const Piece p = pieces[blockIdx.x];
-    if (p.dtype == SCAR_F32) clip_piece<KIND, float>(p, part, ticket, max_norm, rec, d_norm, sh, &factor);
-    else if (p.dtype == SCAR_BF16) clip_piece<KIND, __nv_bfloat16>(p, part, ticket, max_norm, rec, d_norm, sh, &factor);
-    else clip_piece<KIND, __half>(p, part, ticket, max_norm, rec, d_norm, sh, &factor);
+    bool all;
+    if (p.dtype == SCAR_F32) all = clip_piece<KIND, float>(p, part, ticket, max_norm, patience_ns, rec, d_norm, sh, &factor, &after);
+    else if (p.dtype == SCAR_BF16) all = clip_piece<KIND, __nv_bfloat16>(p, part, ticket, max_norm, patience_ns, rec, d_norm, sh, &factor, &after);
+    else all = clip_piece<KIND, __half>(p, part, ticket, max_norm, patience_ns, rec, d_norm, sh, &factor, &after);
+    if (!all) return;
+#pragma unroll 1
+    for (unsigned i = 0; i < gridDim.x; ++i) scale_any(pieces[i], factor);
 }
 
 }  // namespace
@@ -323,6 +360,7 @@ struct scar_gnorm {
     unsigned grid = 1;
     unsigned resident = 0;  // CTAs of k_gnorm_clip that the GPU holds at a time
     bool ran = false;
+    bool no_patience = false;  // of the next k_gnorm_clip
     uint64_t launches = 0;
 };
 
@@ -480,10 +518,12 @@ int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm) {
     int rc = check_current_device(op->device);
     if (rc != SCAR_OK) return rc;
     if (!op->h_pieces.empty() && op->h_pieces.size() <= op->resident) {
-        void *args[] = {&op->pieces, &op->part, &op->ticket, &max_norm, &op->rec, &d_norm};
+        unsigned long long patience = op->no_patience ? 0 : kPatienceNs;
+        void *args[] = {&op->pieces, &op->part, &op->ticket, &max_norm, &patience, &op->rec, &d_norm};
         TRAIN_TRY(cudaLaunchCooperativeKernel(clip_kernel(op->kind), dim3((unsigned)op->h_pieces.size()), dim3(kNormThreads), args, 0, op->stream));
         op->launches += 1;
         op->ran = true;
+        op->no_patience = false;
         return SCAR_OK;
     }
     if ((rc = run_norm(op, max_norm, true, d_norm)) != SCAR_OK) return rc;
@@ -502,19 +542,40 @@ int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm) {
     return SCAR_OK;
 }
 
-int scar_gnorm_status(scar_gnorm *op, scar_gnorm_info *out) {
-    if (!op || !out) return SCAR_ERR_INVALID_ARG;
+namespace {
+int read_record(scar_gnorm *op, NormRecord *rec) {
     const int rc = check_current_device(op->device);
     if (rc != SCAR_OK) return rc;
+    TRAIN_TRY(cudaMemcpyAsync(rec, op->rec, sizeof(NormRecord), cudaMemcpyDeviceToHost, op->stream));
+    TRAIN_TRY(cudaStreamSynchronize(op->stream));
+    return SCAR_OK;
+}
+}  // namespace
+
+int scar_gnorm_status(scar_gnorm *op, scar_gnorm_info *out) {
+    if (!op || !out) return SCAR_ERR_INVALID_ARG;
     if (!op->ran) return SCAR_ERR_STATE;
     NormRecord rec;
-    TRAIN_TRY(cudaMemcpyAsync(&rec, op->rec, sizeof(NormRecord), cudaMemcpyDeviceToHost, op->stream));
-    TRAIN_TRY(cudaStreamSynchronize(op->stream));
+    const int rc = read_record(op, &rec);
+    if (rc != SCAR_OK) return rc;
     out->norm = rec.norm;
     out->coef = rec.coef;
     out->nonfinite = rec.nonfinite;
-    if (rec.error) TRAIN_TRY(cudaMemsetAsync(op->rec, 0, 512, op->stream));
-    return rec.error ? SCAR_ERR_TIMEOUT : SCAR_OK;
+    return SCAR_OK;
+}
+
+int scar_gnorm_selftest_arm_timeout(scar_gnorm *op) {
+    if (!op) return SCAR_ERR_INVALID_ARG;
+    op->no_patience = true;
+    return SCAR_OK;
+}
+
+int scar_gnorm_finished_alone(scar_gnorm *op, uint64_t *calls) {
+    if (!op || !calls) return SCAR_ERR_INVALID_ARG;
+    NormRecord rec;
+    const int rc = read_record(op, &rec);
+    if (rc == SCAR_OK) *calls = rec.alone;
+    return rc;
 }
 
 uint64_t scar_gnorm_launch_count(const scar_gnorm *op) { return op ? op->launches : 0; }

@@ -348,6 +348,56 @@ def test_a_captured_call_follows_new_addresses(dt, pieces):
 
 
 @gpu
+@pytest.mark.parametrize("kind", ["l2", "l1", "max"])
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16", "mixed"])
+@pytest.mark.parametrize("name", ["one element", "zeros among them", "around a vector", "around a piece", "as many pieces as are resident", "hundreds of short ones"])
+def test_a_wait_that_runs_out_changes_no_bit(name, dt, kind):
+    """The CTAs of a clipping in one launch give up their wait at once: the last of them finishes the call alone, and the
+    call after it finds everything as it was."""
+    types = list(TYPES.values()) if dt == "mixed" else [TYPES[dt]]
+    ts = tensors(LISTS[name], types, seed=5, lead=(0, 1, 3, 8), scale=1e-2)
+    place = tensors(LISTS[name], types, seed=5, lead=(0, 1, 3, 8), scale=1e-2)  # the bits depend on the addresses modulo 16
+    out = [torch.full_like(t, 7.0) for t in ts]
+    want = [torch.empty_like(t) for t in ts]
+    op, inp, ref = GradientNorm(ts, out=out, kind=kind), GradientNorm(place, kind=kind), GradientNorm(ts, out=want, kind=kind)
+    limit = 0.4 * exact_norm(ts, kind)
+    norm = float(ref.clip(limit))
+    for turn in range(3):
+        for o in (op, inp):
+            if turn != 1:
+                api.scar_gnorm_selftest_arm_timeout(o.op)
+        [o.fill_(7.0) for o in out]
+        [p.copy_(t) for p, t in zip(place, ts)]
+        assert float(op.clip(limit)) == norm and float(inp.clip(limit)) == norm
+        for o in (op, inp):
+            assert (o.status().norm, o.status().coef) == (ref.status().norm, ref.status().coef)
+            assert api.scar_gnorm_finished_alone(o.op) == (1, 1, 2)[turn]
+        assert all(torch.equal(a, w) and torch.equal(p, w) for a, p, w in zip(out, place, want))
+    assert api.scar_gnorm_finished_alone(ref.op) == 0
+    [o.close() for o in (op, inp, ref)]
+
+
+@gpu
+def test_a_clipping_in_one_launch_beside_a_busy_gpu():
+    """Other streams hold the multiprocessors while short lists are clipped: whichever way a call ends, its bits are the same."""
+    ts = tensors([4096 * 500, 100_003], [torch.float32], seed=8)
+    out = [torch.empty_like(t) for t in ts]
+    op = GradientNorm(ts, out=out)
+    norm = float(op.clip(1.0))
+    want = [o.clone() for o in out]
+    sides, a = [torch.cuda.Stream() for _ in range(2)], torch.randn(8192, 8192, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s in sides:
+            with torch.cuda.stream(s):
+                a @ a
+        [o.zero_() for o in out]
+        assert float(op.clip(1.0)) == norm and all(torch.equal(o, w) for o, w in zip(out, want))
+    torch.cuda.synchronize()
+    op.close()
+
+
+@gpu
 def test_refusals():
     t = torch.ones(8, device="cuda")
     with pytest.raises(TypeError):
@@ -389,3 +439,9 @@ def test_arguments_are_checked_before_any_device_work():
     assert lib.scar_gnorm_norm(None, None) == -1 and lib.scar_gnorm_clip(None, 1.0, None) == -1
     assert lib.scar_gnorm_bind(None, None, 0) == -1 and lib.scar_gnorm_status(None, None) == -1
     assert lib.scar_gnorm_destroy(None) == -1 and lib.scar_gnorm_launch_count(None) == 0
+
+
+def test_the_calls_about_a_wait_check_their_arguments():
+    _build.build()
+    lib = api.load_library()
+    assert lib.scar_gnorm_finished_alone(None, None) == -1 and lib.scar_gnorm_selftest_arm_timeout(None) == -1
