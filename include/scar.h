@@ -504,8 +504,10 @@ int scar_xent_loss_grad(scar_xent *op, const void *d_h, uint64_t h_pitch, const 
                         float *d_loss, void *d_dh, uint64_t dh_pitch, void *d_dw, uint64_t dw_pitch);
 
 /* Waits for the stream and returns the record of the most recent call.  SCAR_ERR_TIMEOUT if a wait inside one of
- * its kernels gave up (its outputs are then invalid; the operator stays usable). */
+ * its kernels gave up (its loss is then NaN, its other outputs are invalid; the operator stays usable). */
 int scar_xent_status(scar_xent *op, scar_xent_info *out);
+/* Self-test hook: the next call reports a wait that gave up (host state only; none does). */
+int scar_xent_selftest_arm_timeout(scar_xent *op);
 uint64_t scar_xent_workspace_bytes(const scar_xent *op); /* device memory the operator holds */
 uint64_t scar_xent_launch_count(const scar_xent *op);    /* kernels launched so far */
 int scar_xent_destroy(scar_xent *op);

@@ -126,6 +126,7 @@ _SIGS = {
     "scar_xent_loss": (_int, [_vp, _vp, _u64, _vp, _u64, _vp, _u64, _vp, _vp]),
     "scar_xent_loss_grad": (_int, [_vp, _vp, _u64, _vp, _u64, _vp, _u64, C.c_float, _vp, _vp, _vp, _u64, _vp, _u64]),
     "scar_xent_status": (_int, [_vp, C.POINTER(scar_xent_info)]),
+    "scar_xent_selftest_arm_timeout": (_int, [_vp]),
     "scar_xent_workspace_bytes": (_u64, [_vp]),
     "scar_xent_launch_count": (_u64, [_vp]),
     "scar_xent_destroy": (_int, [_vp]),
@@ -478,6 +479,10 @@ def scar_xent_status(op: int) -> scar_xent_info:
     out = scar_xent_info()
     _check(load_library().scar_xent_status(op, C.byref(out)), "scar_xent_status")
     return out
+
+
+def scar_xent_selftest_arm_timeout(op: int) -> None:
+    _check(load_library().scar_xent_selftest_arm_timeout(op), "scar_xent_selftest_arm_timeout")
 
 
 def scar_xent_workspace_bytes(op: int) -> int:

@@ -64,6 +64,7 @@ struct TcArgs {
     int n_fast;              // tiles of one row of tiles run first (B is the smaller operand and stays in L2)
     int bf16;
     unsigned *error;
+    float *loss[2];          // become NaN where a wait gives up (each may be nullptr)
     int c_map;               // kOut: the result is stored through `c` (kPart and kProb always do)
     // kPart
     float *part;             // [splits][m][n rounded up to 8]
@@ -885,6 +886,10 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
     if (warp < kEpiWarps) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // this warp's stores are in memory
     if (!ok) {  // let copies and instructions in flight end before the memory they use is given back
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        // for a caller who reads no status: a loss that is written after this is NaN by the error flag
+        if (lane == 0)
+            for (float *loss : set.p[0].loss)
+                if (loss) *loss = __int_as_float(0x7fffffff);
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

@@ -32,7 +32,7 @@ constexpr unsigned kWarpRow = 2048;  // rows of up to this many classes have a w
 struct XentRecord {
     float loss;
     unsigned rows, ignored, bad;
-    unsigned error;
+    unsigned error; // a wait inside a product gave up
     unsigned done;  // CTAs of the last softmax kernel that are through
 };
 
@@ -55,6 +55,7 @@ struct RowList {
     float *row_loss;
     XentRecord *rec;
     float *d_loss;
+    unsigned error;  // what the record's begins with: 1 in a self-test
 };
 template <int kThreads, bool kWrite> __device__ __forceinline__ unsigned list_rows(const RowList &q, unsigned *pos) {
     constexpr int kWarps = kThreads / 32, kCounts = kLabels * kWarps;  // rows that count, by round of labels and warp
@@ -127,7 +128,7 @@ template <int kThreads, bool kWrite> __device__ __forceinline__ unsigned list_ro
             q.rec->rows = base;
             q.rec->ignored = n_ign;
             q.rec->bad = n_bad;
-            q.rec->error = 0;
+            q.rec->error = q.error;
             q.rec->done = 0;
             q.rec->loss = 0.f;
             if (q.d_loss && q.n == 0) *q.d_loss = 0.f;
@@ -303,7 +304,7 @@ struct DzOut {
 };
 
 // Ends every CTA of a softmax kernel; with `n` (the last piece of a call) the last CTA to get here adds up the call's row
-// losses, in an order that depends on n alone.
+// losses, in an order that depends on n alone.  The loss is NaN once a wait inside a product of the call has given up.
 struct LossOut {
     const float *row_loss;
     unsigned n;
@@ -332,7 +333,7 @@ __device__ __forceinline__ void finish_loss(const LossOut &o) {
     if (threadIdx.x) return;
     s = 0.0;
     for (int w = 0; w < 8; ++w) s += sh[w];
-    o.rec->loss = (float)(o.mean ? s / (double)max(o.rec->rows, 1u) : s);
+    o.rec->loss = __ldcg(&o.rec->error) ? __int_as_float(0x7fffffff) : (float)(o.mean ? s / (double)max(o.rec->rows, 1u) : s);
     if (o.d_loss) *o.d_loss = o.rec->loss;
 }
 
@@ -575,6 +576,7 @@ struct scar_xent {
     uint64_t bytes = 0;
     uint64_t launches = 0;
     bool ran = false, failed = false, have_w_maps = false;
+    bool arm_error = false;  // the next call reports a wait that gave up
 };
 
 namespace {
@@ -776,7 +778,8 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
         if ((rc = make_map(op, &logits.b, ow, kBN / 2)) != SCAR_OK || (grad && (rc = make_map(op, &dhg.b, ow, 64)) != SCAR_OK)) return rc;
     }
 
-    const RowList list{y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec, d_loss};
+    const RowList list{y, n, op->cfg.ignore_label, V, op->row_of, op->pos, op->label, row_loss, op->rec, d_loss, op->arm_error ? 1u : 0u};
+    op->arm_error = false;
     const Copy<T> ch{h, hp, n, rows_aligned(h, hp, sizeof(T)), op->h, op->h_rows * op->dp};
     const Copy<T> cw{w, wp, w_copied ? V : 0u, rows_aligned(w, wp, sizeof(T)), op->w, (uint64_t)V * op->dp};
     const uint64_t groups = ((uint64_t)n + 64 + cw.n) * (op->dp / 8);
@@ -791,6 +794,8 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
     TcArgs base{};
     base.rows = &op->rec->rows;
     base.error = &op->rec->error;
+    base.loss[0] = &op->rec->loss;
+    base.loss[1] = d_loss;
     base.bf16 = op->cfg.dtype != SCAR_F16;
     base.part = op->part;
     base.out_type = op->cfg.dtype;
@@ -1039,6 +1044,12 @@ int scar_xent_status(scar_xent *op, scar_xent_info *out) {
     out->ignored = rec.ignored;
     out->bad = rec.bad;
     return rec.error ? SCAR_ERR_TIMEOUT : SCAR_OK;
+}
+
+int scar_xent_selftest_arm_timeout(scar_xent *op) {
+    if (!op) return SCAR_ERR_INVALID_ARG;
+    op->arm_error = true;
+    return SCAR_OK;
 }
 
 uint64_t scar_xent_workspace_bytes(const scar_xent *op) { return op ? op->bytes : 0; }

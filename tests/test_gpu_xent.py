@@ -409,6 +409,27 @@ def test_another_stream_and_a_captured_graph():
 
 
 @gpu
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("T,V,D,room", [(200, 1000, 128, 0), (700, 500, 64, 1), (40, 260, 6000, 0), (3000, 300, 64, 0)])
+def test_a_wait_that_gave_up_shows_in_the_loss(dt, T, V, D, room):
+    """A caller that reads no status sees a NaN; the call after it is a whole one.  (No wait is made to run out: the hook
+    sets the flag that one would set.)"""
+    h, w, y = make(T, V, D, TYPES[dt], seed=4, ignored=0.1)
+    op = LinearCrossEntropy(T, V, D, TYPES[dt], workspace_bytes=room)
+    want = op.loss_and_grad(h, w, y)
+    alone = op.loss(h, w, y)
+    for call in (op.loss_and_grad, op.loss):
+        api.scar_xent_selftest_arm_timeout(op.op)
+        assert bool(call(h, w, y)[0].isnan())
+        with pytest.raises(ScarError) as e:
+            op.status()
+        assert e.value.code == -6
+    assert all(torch.equal(a, b) for a, b in zip(op.loss_and_grad(h, w, y), want))
+    assert all(torch.equal(a, b) for a, b in zip(op.loss(h, w, y), alone)) and op.status().loss == float(alone[0])
+    op.close()
+
+
+@gpu
 def test_refusals_leave_everything_untouched():
     T, V, D = 8, 40, 16
     h, w, y = make(T, V, D, torch.bfloat16)
@@ -467,3 +488,8 @@ def test_arguments_are_checked_before_any_device_work():
     ctx, layout = C.c_void_p(), api.make_layout(1024, 0, 256, 8)
     for dt in (api.SCAR_BF16, api.SCAR_F16):  # operand types of these operators only
         assert lib.scar_ckpt_init(C.byref(ctx), 0x1000, dt, C.byref(layout), None) == -1
+
+
+def test_the_hook_checks_its_argument():
+    _build.build()
+    assert api.load_library().scar_xent_selftest_arm_timeout(None) == -1
