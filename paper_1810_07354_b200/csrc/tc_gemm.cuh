@@ -56,7 +56,8 @@ struct TcArgs {
     unsigned first, most;    // the piece's rows of the compacted list
     const unsigned *rows;    // rows that count (device)
     unsigned a_row0, b_row0; // where the piece starts in the row dimension of the tensor maps
-    unsigned splits;         // 1, or more: the kernel then chooses for the rows it finds (pick_splits)
+    unsigned splits;         // 1, or more: the product then chooses for the rows it finds (pick_splits) ...
+    unsigned *chosen;        // ... and leaves its choice here for the kernel that joins the parts
     unsigned pairs;          // CTA pairs the GPU holds
     unsigned most_splits;    // that fit the buffer of parts
     int planes;
@@ -243,7 +244,8 @@ __host__ __device__ inline float split_cost(unsigned s, unsigned long long tiles
 __host__ __device__ inline unsigned tiles_of(unsigned m, unsigned n) { return (unsigned)(((unsigned long long)m + kBM - 1) / kBM * (((unsigned long long)n + kBN - 1) / kBN)); }
 constexpr unsigned kMostSplits = 32;
 
-// The same choice for the rows that really take part, known on the device only: every lane of a warp rates one number.
+// The same choice for the rows that really take part, known on the device only: every lane of a warp rates one number.  Only
+// the product chooses; who reads its parts takes the number from parts_of, so that no rounding of a cost can part the two.
 __device__ __forceinline__ unsigned pick_splits(const TcArgs &g, unsigned m, unsigned k) {
     if (g.splits == 1) return 1;
     const unsigned s = (threadIdx.x & 31) + 1, kb = (k + kBK - 1) / kBK;
@@ -264,6 +266,8 @@ __device__ __forceinline__ unsigned rows_of(const TcArgs &g) {
     const unsigned rows = *g.rows;
     return rows > g.first ? min(g.most, rows - g.first) : 0u;
 }
+
+__device__ __forceinline__ unsigned parts_of(const TcArgs &g) { return g.splits == 1 ? 1u : *g.chosen; }
 
 struct TileWalk {
     unsigned m, mt, nt, total, kb, splits;
@@ -640,6 +644,7 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
     if (warp < N) {
         const TileWalk w(set.p[warp]);
         if (lane == 0) walks[warp] = w;
+        if (EPI == Epi::kPart && lane == 0 && blockIdx.x == 0 && set.p[0].splits > 1) *set.p[0].chosen = w.splits;
     }
     __syncthreads();
     unsigned *const error = set.p[0].error;

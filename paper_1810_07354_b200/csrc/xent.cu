@@ -34,6 +34,7 @@ struct XentRecord {
     unsigned rows, ignored, bad;
     unsigned error; // a wait inside a product gave up
     unsigned done;  // CTAs of the last softmax kernel that are through
+    unsigned splits; // parts of the split product that ran last
 };
 
 // Every kernel of a call is launched while the one before it may still run; nothing is touched before that one is done.
@@ -453,7 +454,7 @@ k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict_
     __shared__ float sh[8];
     griddep_start();
     const unsigned r = blockIdx.x * (256 / NT) + threadIdx.x / NT, tid = threadIdx.x % NT, R = rows_of(g), V = g.n, pitch = (V + 7) & ~7u;
-    const unsigned splits = pick_splits(g, R, g.k);
+    const unsigned splits = parts_of(g);
     const unsigned long long stride = (unsigned long long)g.m * pitch;
     float *z = g.part + (unsigned long long)r * pitch;
     float lse = 0.f, zl = 0.f;
@@ -519,8 +520,8 @@ k_xent_softmax(const __grid_constant__ TcArgs g, DzOut o, const int *__restrict_
 __global__ void __launch_bounds__(128)
 k_xent_combine(const __grid_constant__ TcArgs g) {
     griddep_start();
-    const unsigned mine = rows_of(g), m = g.dyn == 0 ? mine : g.m, k = g.dyn == 1 ? mine : g.k;
-    const unsigned groups = (g.n + 3) / 4, pitch = (g.n + 7) & ~7u, splits = pick_splits(g, m, k);
+    const unsigned m = g.dyn == 0 ? rows_of(g) : g.m;
+    const unsigned groups = (g.n + 3) / 4, pitch = (g.n + 7) & ~7u, splits = parts_of(g);
     const float f = g.mean ? g.scale / (float)max(*g.rows, 1u) : g.scale;
     const unsigned long long stride = (unsigned long long)g.m * pitch, total = (unsigned long long)m * groups;
     for (unsigned long long i = (unsigned long long)blockIdx.x * 128 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 128) {
@@ -794,6 +795,7 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
     TcArgs base{};
     base.rows = &op->rec->rows;
     base.error = &op->rec->error;
+    base.chosen = &op->rec->splits;
     base.loss[0] = &op->rec->loss;
     base.loss[1] = d_loss;
     base.bf16 = op->cfg.dtype != SCAR_F16;

@@ -142,6 +142,22 @@ def test_every_way_through_the_kernels(dt, T, V, D, ignored):
 
 
 @gpu
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("T,V,D", [(300, 260, 6000), (700, 60_000, 24), (6000, 40, 48), (1100, 520, 2000)])
+def test_parts_of_split_sums_for_any_number_of_rows_that_count(dt, T, V, D):
+    """Products whose sums are cut into parts, launched for T rows while from none to all of them count: the kernel that
+    joins the parts takes as many as there are."""
+    h, w, y = make(T, V, D, TYPES[dt], seed=V)
+    op = LinearCrossEntropy(T, V, D, TYPES[dt])
+    for kept in sorted({0, 1, 2, 63, 64, 65, 255, 256, 257, T // 4, T // 2, T - 1, T}):
+        some = y.clone()
+        g = torch.Generator(device="cuda").manual_seed(kept)
+        some[torch.randperm(T, generator=g, device="cuda")[kept:]] = IGN
+        check(op, h, w, some)
+    op.close()
+
+
+@gpu
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
 def test_offsets_beyond_32_bits(dt):
     """w and dw of 2.4e9 values: rows behind the 2^31st and the 2^32nd value's byte are checked against the definition."""
