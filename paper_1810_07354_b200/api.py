@@ -802,13 +802,18 @@ class GradientNorm(_OnStream):
 
         tensors = list(tensors)
         self._bind_stream(stream, tensors[0].device if tensors else "cuda")
+        out = self._outputs(tensors, out)
         table = self._table(tensors, out)
         with torch.cuda.device(self._device):
             self.op = scar_gnorm_init(table, {"l2": SCAR_GNORM_L2, "l1": SCAR_GNORM_L1, "max": SCAR_GNORM_MAX}[kind],
                                       self._stream.cuda_stream)
+        self._tensors, self._out = tensors, out  # kept alive as long as they are registered
+
+    @staticmethod
+    def _outputs(tensors, out):
+        return [None] * len(tensors) if out is None else list(out)
 
     def _table(self, tensors, out):
-        out = [None] * len(tensors) if out is None else list(out)
         if len(out) != len(tensors):
             raise ValueError("out: one tensor per input is wanted")
         table = (scar_tensor * len(tensors))()
@@ -820,11 +825,13 @@ class GradientNorm(_OnStream):
                 raise ValueError("an output has its input's type and length")
             e.d_data, e.n_elems, e.dtype = t.data_ptr(), t.numel(), _operand_type(t.dtype)
             e.d_out = None if o is None else o.data_ptr()
-        self._tensors, self._out = tensors, out  # kept alive as long as they are registered
         return table
 
     def bind(self, tensors, out=None):
-        scar_gnorm_bind(self.op, self._table(list(tensors), out))
+        tensors = list(tensors)
+        out = self._outputs(tensors, out)
+        scar_gnorm_bind(self.op, self._table(tensors, out))
+        self._tensors, self._out = tensors, out  # a refused list leaves the handle on the one before
 
     def _run(self, call):
         norm = self._torch.empty((), dtype=self._torch.float32, device=self._device)

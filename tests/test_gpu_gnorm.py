@@ -286,6 +286,25 @@ def test_new_addresses_that_begin_elsewhere(dt):
 
 
 @gpu
+def test_a_call_after_a_refused_bind():
+    """The handle goes on with the tensors it had, which nobody else holds any more."""
+    ts = tensors([100_003, 17], [torch.float32], seed=3)
+    want = exact_norm(ts, "l2")
+    op = GradientNorm(ts, kind="l2")
+    del ts
+    for bad in ([100_003], [100_003, 18], [100_002, 17]):
+        with pytest.raises(ScarError):
+            op.bind(tensors(bad, [torch.float32], seed=4))
+    with pytest.raises(ScarError):
+        op.bind(tensors([100_003, 17], [torch.bfloat16, torch.float32], seed=4))
+    fresh = [torch.full((100_003,), 3.0, device="cuda") for _ in range(8)]  # would lie where freed tensors were
+    assert abs(float(op.clip(want / 2)) - want) <= (SUM_TOL + 2.0 ** -23) * want
+    assert all(bool((f == 3.0).all()) for f in fresh)
+    assert abs(exact_norm(op._tensors, "l2") - want / 2) <= (SUM_TOL + 2.0 ** -20) * want
+    op.close()
+
+
+@gpu
 def test_another_stream_and_a_captured_graph():
     ts = tensors([200_000, 11], [torch.float32], seed=4)
     out = [torch.empty_like(t) for t in ts]
