@@ -733,8 +733,8 @@ class LinearCrossEntropy(_OnStream):
             self.op = scar_xent_init(cfg, self._stream.cuda_stream)
 
     def _matrix(self, name: str, m, rows: int):
-        if m.dtype != self.dtype or not m.is_cuda:
-            raise TypeError(f"{name}: a CUDA tensor of {self.dtype} is wanted")
+        if m.dtype != self.dtype or m.device != self._device:
+            raise TypeError(f"{name}: a tensor of {self.dtype} on {self._device} is wanted")
         if m.dim() != 2 or tuple(m.shape) != (rows, self.dim) or (self.dim > 1 and m.stride(1) != 1):
             raise ValueError(f"{name}: shape ({rows}, {self.dim}) with contiguous rows is wanted")
         return m.data_ptr(), (m.stride(0) if rows > 1 else max(m.stride(0), self.dim))
@@ -742,14 +742,14 @@ class LinearCrossEntropy(_OnStream):
     def _call(self, grad: bool, h, w, labels, grad_scale, row_loss, dh, dw):
         torch = self._torch
         n = labels.numel()
-        if labels.dtype != torch.int64 or not labels.is_cuda or not labels.is_contiguous():
-            raise TypeError("labels: a contiguous CUDA tensor of int64 is wanted")
-        hp, wp = self._matrix("h", h, n), self._matrix("w", w, self.n_classes)
         dev = self._device
+        if labels.dtype != torch.int64 or labels.device != dev or not labels.is_contiguous():
+            raise TypeError(f"labels: a contiguous tensor of int64 on {dev} is wanted")
+        hp, wp = self._matrix("h", h, n), self._matrix("w", w, self.n_classes)
         if row_loss is None:
             row_loss = torch.empty(n, dtype=torch.float32, device=dev)
-        elif row_loss.dtype != torch.float32 or row_loss.numel() != n or not row_loss.is_contiguous():
-            raise ValueError("row_loss: one contiguous float32 per row is wanted")
+        elif row_loss.dtype != torch.float32 or row_loss.device != dev or row_loss.numel() != n or not row_loss.is_contiguous():
+            raise ValueError(f"row_loss: one contiguous float32 per row on {dev} is wanted")
         loss = torch.empty((), dtype=torch.float32, device=dev)
         if grad:
             dh = torch.empty((n, self.dim), dtype=self.dtype, device=dev) if dh is None else dh
@@ -819,8 +819,8 @@ class GradientNorm(_OnStream):
         table = (scar_tensor * len(tensors))()
         for e, t, o in zip(table, tensors, out):
             for x in (t, o):
-                if x is not None and (not x.is_cuda or not x.is_contiguous() or x.device != tensors[0].device):
-                    raise ValueError("contiguous tensors on one CUDA device are wanted")
+                if x is not None and (x.device != self._device or not x.is_contiguous()):
+                    raise ValueError(f"contiguous tensors on {self._device} are wanted")
             if o is not None and (o.dtype != t.dtype or o.numel() != t.numel()):
                 raise ValueError("an output has its input's type and length")
             e.d_data, e.n_elems, e.dtype = t.data_ptr(), t.numel(), _operand_type(t.dtype)

@@ -487,6 +487,24 @@ def test_refusals_leave_everything_untouched():
     small.close()
 
 
+@gpu
+def test_host_tensors_are_refused():
+    T, V, D = 8, 40, 16
+    h, w, y = make(T, V, D, torch.float32)
+    op = LinearCrossEntropy(T, V, D, torch.float32)
+    with pytest.raises(ValueError):
+        op.loss(h, w, y, row_loss=torch.empty(T))
+    for args in ((h.cpu(), w, y), (h, w.cpu(), y), (h, w, y.cpu())):
+        with pytest.raises(TypeError):
+            op.loss(*args)
+    with pytest.raises(TypeError):
+        op.loss_and_grad(h, w, y, dh=torch.empty(T, D))
+    with pytest.raises(TypeError):
+        op.loss_and_grad(h, w, y, dw=torch.empty(V, D))
+    assert api.scar_xent_launch_count(op.op) == 0
+    op.close()
+
+
 def test_arguments_are_checked_before_any_device_work():
     _build.build()
     lib = api.load_library()

@@ -43,7 +43,7 @@ def handle(cls, **fields):
     stream = types.SimpleNamespace(cuda_stream=7)
     fake = types.SimpleNamespace(empty=lambda shape, dtype=None, device=None: Stand(*(shape if isinstance(shape, tuple) else () if shape == () else (shape,)), dtype=dtype, device=device),
                                  int64=torch.int64, float32=torch.float32)
-    op.__dict__.update(_device=HERE, _stream=stream, _torch=fake, _here=lambda index: 7, op=5, **fields)
+    op.__dict__.update(_device=HERE, _stream=stream, _torch=fake, _here=lambda index: 7, op=0, **fields)  # nothing to destroy
     return op
 
 
@@ -79,3 +79,30 @@ def test_a_refused_bind_keeps_the_registered_tensors(calls):
         op.bind([Stand(8), Stand(3)], [Stand(8)])
     assert op._tensors == second and len(calls.got) == 3
     op.close()
+
+
+def test_tensors_of_another_device_are_refused_before_anything_is_launched(calls):
+    op = handle(api.LinearCrossEntropy, max_tokens=4, n_classes=6, dim=8, dtype=torch.float32)
+    y = lambda **kw: Stand(4, dtype=torch.int64, **kw)  # noqa: E731
+    h, w, row = Stand(4, 8), Stand(6, 8), Stand(4)
+    op.loss(h, w, y(), row_loss=row)
+    op.loss_and_grad(h, w, y(), row_loss=row, dh=Stand(4, 8), dw=Stand(6, 8))
+    assert calls.got == ["scar_xent_loss", "scar_xent_loss_grad"]
+    for there in (OTHER, torch.device("cpu")):
+        def far(*shape):
+            return Stand(*shape, device=there)
+        for args, kw in (((far(4, 8), w, y()), {}), ((h, far(6, 8), y()), {}), ((h, w, y(device=there)), {}), ((h, w, y()), dict(row_loss=far(4)))):
+            with pytest.raises((TypeError, ValueError)):
+                op.loss(*args, **kw)
+            with pytest.raises((TypeError, ValueError)):
+                op.loss_and_grad(*args, **kw)
+        for kw in (dict(dh=far(4, 8)), dict(dw=far(6, 8))):
+            with pytest.raises((TypeError, ValueError)):
+                op.loss_and_grad(h, w, y(), **kw)
+    assert len(calls.got) == 2
+    norm = handle(api.GradientNorm)
+    norm.bind([Stand(8)])
+    for ts, out in (([Stand(8, device=OTHER)], None), ([Stand(8)], [Stand(8, device=OTHER)]), ([Stand(8, device=torch.device("cpu"))], None)):
+        with pytest.raises(ValueError):
+            norm.bind(ts, out)
+    assert len(calls.got) == 3
