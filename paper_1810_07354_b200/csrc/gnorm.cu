@@ -507,14 +507,14 @@ int scar_gnorm_bind(scar_gnorm *op, const scar_tensor *h_tensors, uint64_t n_ten
 }
 
 int scar_gnorm_norm(scar_gnorm *op, float *d_norm) {
-    if (!op) return SCAR_ERR_INVALID_ARG;
+    if (!op || (uintptr_t)d_norm % 4) return SCAR_ERR_INVALID_ARG;
     const int rc = check_current_device(op->device);
     if (rc != SCAR_OK) return rc;
     return run_norm(op, 0.f, false, d_norm);
 }
 
 int scar_gnorm_clip(scar_gnorm *op, float max_norm, float *d_norm) {
-    if (!op || !(max_norm >= 0.f)) return SCAR_ERR_INVALID_ARG;
+    if (!op || !(max_norm >= 0.f) || (uintptr_t)d_norm % 4) return SCAR_ERR_INVALID_ARG;
     int rc = check_current_device(op->device);
     if (rc != SCAR_OK) return rc;
     if (!op->h_pieces.empty() && op->h_pieces.size() <= op->resident) {

@@ -595,14 +595,16 @@ template <typename P> int xent_alloc(scar_xent *op, P **p, uint64_t bytes) {
     return SCAR_OK;
 }
 
+constexpr uint64_t kPitchEnd = 1ull << 38;  // a tensor map's row is shorter than 2^40 bytes
 int check_call(const scar_xent *op, const void *h, uint64_t hp, const void *w, uint64_t wp, const int64_t *labels,
-               uint64_t n) {
+               uint64_t n, const float *row_loss, const float *loss) {
     if (!op || !w) return SCAR_ERR_INVALID_ARG;
     const unsigned b = elem_size(op->cfg.dtype);
     if (n > op->cfg.max_tokens) return SCAR_ERR_CAPACITY;
     if (n && (!h || !labels)) return SCAR_ERR_INVALID_ARG;
-    if (hp < op->cfg.dim || wp < op->cfg.dim || hp >= (1ull << 38) || wp >= (1ull << 38)) return SCAR_ERR_INVALID_ARG;
-    if ((uintptr_t)h % b || (uintptr_t)w % b || (uintptr_t)labels % 8) return SCAR_ERR_INVALID_ARG;
+    if (hp < op->cfg.dim || wp < op->cfg.dim || hp >= kPitchEnd || wp >= kPitchEnd) return SCAR_ERR_INVALID_ARG;
+    if ((uintptr_t)h % b || (uintptr_t)w % b || (uintptr_t)labels % 8 || (uintptr_t)row_loss % 4 || (uintptr_t)loss % 4)
+        return SCAR_ERR_INVALID_ARG;
     return check_current_device(op->device);
 }
 
@@ -1014,7 +1016,7 @@ int scar_xent_init(scar_xent **out, const scar_xent_config *cfg, void *cuda_stre
 
 int scar_xent_loss(scar_xent *op, const void *d_h, uint64_t h_pitch, const void *d_w, uint64_t w_pitch,
                    const int64_t *d_labels, uint64_t n_tokens, float *d_row_loss, float *d_loss) {
-    const int rc = check_call(op, d_h, h_pitch, d_w, w_pitch, d_labels, n_tokens);
+    const int rc = check_call(op, d_h, h_pitch, d_w, w_pitch, d_labels, n_tokens, d_row_loss, d_loss);
     if (rc != SCAR_OK) return rc;
     return call(op, d_h, h_pitch, d_w, w_pitch, d_labels, n_tokens, false, 0.f, d_row_loss, d_loss, nullptr, 0, nullptr, 0);
 }
@@ -1022,12 +1024,12 @@ int scar_xent_loss(scar_xent *op, const void *d_h, uint64_t h_pitch, const void 
 int scar_xent_loss_grad(scar_xent *op, const void *d_h, uint64_t h_pitch, const void *d_w, uint64_t w_pitch,
                         const int64_t *d_labels, uint64_t n_tokens, float grad_scale, float *d_row_loss,
                         float *d_loss, void *d_dh, uint64_t dh_pitch, void *d_dw, uint64_t dw_pitch) {
-    const int rc = check_call(op, d_h, h_pitch, d_w, w_pitch, d_labels, n_tokens);
+    const int rc = check_call(op, d_h, h_pitch, d_w, w_pitch, d_labels, n_tokens, d_row_loss, d_loss);
     if (rc != SCAR_OK) return rc;
     const unsigned b = elem_size(op->cfg.dtype);
     if (op->cfg.loss_only) return SCAR_ERR_STATE;
     if (!d_dw || (n_tokens && !d_dh) || (uintptr_t)d_dh % b || (uintptr_t)d_dw % b) return SCAR_ERR_INVALID_ARG;
-    if (dh_pitch < op->cfg.dim || dw_pitch < op->cfg.dim || dh_pitch >= (1ull << 40) || dw_pitch >= (1ull << 40))
+    if (dh_pitch < op->cfg.dim || dw_pitch < op->cfg.dim || dh_pitch >= kPitchEnd || dw_pitch >= kPitchEnd)
         return SCAR_ERR_INVALID_ARG;
     return call(op, d_h, h_pitch, d_w, w_pitch, d_labels, n_tokens, true, grad_scale, d_row_loss, d_loss, d_dh, dh_pitch,
                 d_dw, dw_pitch);

@@ -438,6 +438,20 @@ def test_refusals():
     op.close()
 
 
+@gpu
+def test_a_norm_off_its_boundary_is_refused():
+    t = torch.ones(8, device="cuda")
+    op = GradientNorm([t])
+    lib, room = api.load_library(), torch.full((4,), 3.0, device="cuda")
+    for by in (1, 2, 3, 6):
+        assert lib.scar_gnorm_norm(op.op, room.data_ptr() + by) == -1
+        assert lib.scar_gnorm_clip(op.op, 1.0, room.data_ptr() + by) == -1
+    assert api.scar_gnorm_launch_count(op.op) == 0
+    torch.cuda.synchronize()
+    assert bool((room == 3.0).all()) and bool((t == 1.0).all())
+    op.close()
+
+
 def test_arguments_are_checked_before_any_device_work():
     _build.build()
     lib = api.load_library()

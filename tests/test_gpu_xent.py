@@ -505,6 +505,24 @@ def test_host_tensors_are_refused():
     op.close()
 
 
+@gpu
+def test_results_off_their_boundary_and_rows_too_far_apart_are_refused():
+    T, V, D = 8, 40, 16
+    h, w, y = make(T, V, D, torch.bfloat16)
+    op = LinearCrossEntropy(T, V, D, torch.bfloat16)
+    lib, room = api.load_library(), torch.full((64 + V * D,), 3.0, device="cuda")
+    a, good = room.data_ptr(), (h.data_ptr(), D, w.data_ptr(), D, y.data_ptr(), T)
+    for row, loss in ((a + 2, a + 64), (a + 1, None), (a, a + 65), (None, a + 66)):
+        assert lib.scar_xent_loss(op.op, *good, row, loss) == -1
+        assert lib.scar_xent_loss_grad(op.op, *good, 1.0, row, loss, a + 256, D, a + 512, D) == -1
+    for dhp, dwp in ((1 << 38, D), (D, 1 << 38)):
+        assert lib.scar_xent_loss_grad(op.op, *good, 1.0, None, None, a + 256, dhp, a + 512, dwp) == -1
+    assert api.scar_xent_launch_count(op.op) == 0
+    torch.cuda.synchronize()
+    assert bool((room == 3.0).all())
+    op.close()
+
+
 def test_arguments_are_checked_before_any_device_work():
     _build.build()
     lib = api.load_library()
