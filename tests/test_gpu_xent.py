@@ -188,6 +188,60 @@ def test_offsets_beyond_32_bits(dt):
 
 
 @gpu
+def test_float32_offsets_beyond_32_bits():
+    """2.4e9 float32 values of w and dw, three planes of which are 14.4 GB: rows behind the 2^31st value and behind the
+    2^32nd byte, of w, of a plane and of dw, against the definition."""
+    T, V, D = 6, 300_000, 8000
+    w = torch.empty(V, D, device="cuda").normal_(std=1.5 / D ** 0.5)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    y = torch.tensor([0, V - 1, 268_435, 134_217, IGN, V - 2], device="cuda")
+    h = torch.randn(T, D, generator=g, device="cuda")
+    op = LinearCrossEntropy(T, V, D, torch.float32, reduction="sum")
+    loss, row, dh, dw = op.loss_and_grad(h, w, y)
+    assert torch.equal(op.loss(h, w, y)[1], row)
+    kept = y >= 0
+    hd = torch.where(kept[:, None], h, torch.zeros_like(h)).double()
+    z = torch.cat([hd @ c.double().T for c in w.split(20_000)], 1)
+    lse = torch.logsumexp(z, 1)
+    want = torch.where(kept, lse - z.gather(1, y.clamp(min=0)[:, None])[:, 0], 0.0)
+    ez = 2 * gamma(D) * 50 + 2.0 ** -18
+    assert bool(((row.double() - want).abs() <= ez).all())
+    p = torch.exp(z - lse[:, None]) * kept[:, None]
+    p[torch.arange(T), y.clamp(min=0)] -= kept.double()
+    rows = torch.cat([torch.arange(0, 3), torch.arange(134_210, 134_225), torch.arange(268_430, 268_440), torch.arange(V - 3, V)]).cuda()
+    u = UNIT[torch.float32]
+    ref = p.T[rows] @ hd
+    tol = (u + 2 * ez) * (p.T[rows].abs() @ hd.abs()) + u * ref.abs() + 2.0 ** -36
+    assert bool(((dw[rows].double() - ref).abs() <= tol).all())
+    ref = sum(p[:, i: i + 20_000] @ w[i: i + 20_000].double() for i in range(0, V, 20_000))
+    assert float((dh.double() - ref).norm()) <= 2.0 ** -18 * float(ref.norm()) and not dh[4].any()
+    op.close()
+
+
+@gpu
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_counts_of_rows_that_do_not_count(dt):
+    T, V, D = 40, 200, 72
+    h, w, good = make(T, V, D, TYPES[dt])
+    op = LinearCrossEntropy(T, V, D, TYPES[dt])
+    for y, want in ((torch.full((T,), IGN, device="cuda"), (0, T, 0)), (torch.full((T,), V, device="cuda"), (0, 0, T)), (torch.full((T,), -1, device="cuda"), (0, 0, T)),
+                    (torch.full((T,), 2 ** 40, device="cuda"), (0, 0, T)), (torch.cat([good[:30], torch.tensor([IGN] * 7 + [-1, V, -2 ** 62], device="cuda")]), (30, 7, 3))):
+        for call in (op.loss, op.loss_and_grad):
+            call(h, w, y)
+            info = op.status()
+            assert (int(info.rows), int(info.ignored), int(info.bad)) == want
+    op.close()
+    T = 3000  # listed by a kernel of their own
+    h, w, y = make(T, V, D, TYPES[dt])
+    y[::3], y[1::300] = IGN, V
+    op = LinearCrossEntropy(T, V, D, TYPES[dt])
+    op.loss(h, w, y)
+    info = op.status()
+    assert (int(info.rows), int(info.ignored), int(info.bad)) == (1990, 1000, 10)
+    op.close()
+
+
+@gpu
 @pytest.mark.parametrize("dt", list(TYPES))
 def test_sum_and_scale(dt):
     h, w, y = make(70, 600, 96, TYPES[dt], seed=5, ignored=0.3)
