@@ -246,8 +246,9 @@ k_gnorm_scale(const Piece *__restrict__ pieces, const NormRecord *rec) {
 
 // Both steps in one cooperative launch, for lists of so few pieces that every one has a resident CTA (four per SM: up to
 // 9.7 MB): a CTA keeps its piece in registers, leaves its part, waits until all parts are there and joins them itself, in the
-// order of k_gnorm_norm.  Measured against the two launches: 7.0 / 9.2 us for 2^20 float32 values (most of it the launch), 9.2 / 10.3 us for
-// 2.3 million.
+// order of k_gnorm_norm.  What it saves is the host's second launch.  Calls back to back, one launch / two: 2^20 float32 values
+// 7.3 / 10.0 us, 2.3 million 9.3 / 10.1; 590 tensors of 100 8.2 / 10.0, of 4096 9.6 / 10.3.  Replayed from a graph, where the host has no
+// part, the two are even for short lists and one launch behind for long ones (10.3 / 9.9 us; 2.3 million 12.3 / 10.3).
 //
 // ticket[0] counts parts, ticket[1] the CTAs that are done with them; the last of those clears both.  A kernel of another stream
 // may keep some of the CTAs from starting for as long as it likes, so the wait has an end (kPatienceNs): a CTA that reaches it

@@ -27,7 +27,13 @@ namespace {
 
 constexpr int kRowThreads = 1024;
 constexpr unsigned kNone = 0xffffffffu;
-constexpr unsigned kWarpRow = 2048;  // rows of up to this many classes have a warp of the softmax kernels each, longer ones a CTA
+
+// A row of the softmax kernels has a warp or a CTA of its own.  Loss and gradients, replayed from a graph, dim 64, warp / CTA in us:
+//   bfloat16  1184 rows: 2048 classes 34.2 / 36.1, 4000 49.5 / 48.7;  4736 rows: 8192 classes 119 / 127, 16000 222 / 213
+//   float32   1184 rows: 1000 classes 58.3 / 57.4, 2048 67.5 / 61.4;  4736 rows: 4000 classes 189 / 194, 8192 314 / 310
+// so the limit is one of bytes: rows of 4 KiB (16-bit values or float32 logits) where there is a CTA of them for every SM,
+// of 16 KiB where there are four.  512 rows of 256 to 2048 classes: 24.7 / 26.7 to 33.0 / 33.4, float32 63.5 / 56.9: left to CTAs.
+constexpr unsigned kWarpRowBytes = 4096;
 
 struct XentRecord {
     float loss;
@@ -228,7 +234,8 @@ template <typename T> __device__ __forceinline__ void copy_eight(const Copy<T> &
 // Row t of h goes to pos[t]; rows that do not count are left out and their row of `zero` (dh) is cleared, and the rows
 // behind the last one are zero up to a multiple of 64.  Then w, where it has to be copied.  SCAN: every CTA lists the rows
 // itself (the first one for all to come), which for up to kScanRows of them takes less time than a launch, unless the copies
-// are what takes the time (kScanGroups groups of eight elements: 16 MB of 16-bit values).
+// are what takes the time (kScanGroups groups of eight elements: 16 MB of 16-bit values).  A call of 1000 classes, bfloat16,
+// listed by every CTA / by a launch: 16 rows of 64 26.7 / 29.5 us, 2048 rows of 64 34.9 / 38.9, of 1024 44.0 / 45.0, of 8192 117 / 114.
 constexpr unsigned kScanRows = 2048, kScanGroups = 1u << 20;
 template <typename T, bool SCAN>
 __global__ void __launch_bounds__(256)
@@ -833,9 +840,9 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
             logits.label_z = op->label_z;
             choose_splits(op, logits, kLaunchS);  // the softmax of parts takes about that much longer
             logits.stat = logits.splits == 1 ? op->stat : nullptr;
-            // a warp per row where a row is short (or only its groups are read) and there are rows for a CTA of them on every SM;
-            // for rows of up to 8192 classes, for four
-            const bool many = rows >= 16 * op->pairs, short_rows = (many && V <= kWarpRow) || (rows >= 64 * op->pairs && V <= 4 * kWarpRow);
+            const bool many = rows >= 16 * op->pairs;
+            const uint64_t row_bytes = (uint64_t)V * (PL == 3 ? 4 : 2);
+            const bool short_rows = (many && row_bytes <= kWarpRowBytes) || (rows >= 64 * op->pairs && row_bytes <= 4 * kWarpRowBytes);
             if (logits.splits > 1) {
                 launch_tc<PL, false, false, Epi::kPart>(op, logits);
                 auto kernel = short_rows ? (grad ? k_xent_softmax<true, 32> : k_xent_softmax<false, 32>) : (grad ? k_xent_softmax<true, 256> : k_xent_softmax<false, 256>);
@@ -844,9 +851,13 @@ int run_xent(scar_xent *op, const T *h, uint64_t hp, const T *w, uint64_t wp, co
                 if constexpr (PL == 3) launch_tc<3, false, false, Epi::kPart>(op, logits);
                 else if (grad) launch_tc<1, false, false, Epi::kProb>(op, logits);
                 else launch_tc<1, false, false, Epi::kStat>(op, logits);
-                // few long rows: ranges of at least 4096 classes, for about two CTAs per SM
-                const bool warps = short_rows || (many && !grad);
-                const unsigned ranges = grad && !warps ? std::max(1u, std::min(V / 4096u, 4 * op->pairs / std::max(rows, 1u))) : 1u;
+                // The loss alone reads a row's groups of 128 classes only.  Warp / CTA, bfloat16: 1184 rows of 8192 classes
+                // 22.6 / 22.6 us, of 32000 43.1 / 39.0; 3000 rows of 16000 51.3 / 55.4, of 64000 142 / 140; 8192 rows of 32000 177 / 193.
+                const bool warps = short_rows || (many && !grad && V <= 8ull * rows);
+                // Few long rows: ranges of at least 4096 classes, for about four CTAs per SM.  Cut / whole, 128000 classes: 8 rows
+                // 101 / 113 us, float32 261 / 325; 64000 classes: 200 rows (two ranges) 74.3 / 79.8, float32 191 / 223; 600 rows 132 / 135,
+                // 335 / 338; of 8192 classes 48.3 / 45.9.
+                const unsigned ranges = grad && !warps ? std::max(1u, std::min(V / 4096u, 8 * op->pairs / std::max(rows, 1u))) : 1u;
                 const unsigned span = (unsigned)round_up((V + ranges - 1) / ranges, 2048);
                 auto kernel = warps ? (grad ? k_xent_dz<true, 32> : k_xent_dz<false, 32>) : (grad ? k_xent_dz<true, 256> : k_xent_dz<false, 256>);
                 launch(op, kernel, dim3(warps ? (rows64 + 7) / 8 : rows64, (V + span - 1) / span), 256, 0, dz, V, span, op->part, op->stat, op->groups, op->label,
