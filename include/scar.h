@@ -455,12 +455,17 @@ int scar_ckpt_destroy(scar_ctx *ctx);
  * is zero and whatever its row of h holds (NaN, infinities) reaches nothing.  A label
  * outside [0, V) that is not ignore_label is treated the same and counted
  * (scar_xent_status).  Without any row that counts the loss and both gradients are 0.
- * The T x V matrix of logits is never stored whole.  The loss alone keeps two
- * numbers per row and group of 128 classes (float32 operands: a piece of float32
- * logits too).  With gradients the rows go through in pieces; a piece's block holds
- * exponentials in 16 bits that become dz in place (float32 operands: its float32
- * logits and dz), and `workspace_bytes` bounds it.  In float32 an infinity in an
- * operand acts as a NaN. */
+ * What is stored of the T x V values: the rows go through in pieces, as many at a time
+ * as `workspace_bytes` holds (all of them where that is enough).  With gradients a
+ * piece's block holds exponentials in float16 that become dz in place; float32 operands
+ * have a piece of float32 logits and dz as three bfloat16 planes.  The loss alone keeps
+ * two numbers per row and group of 128 classes (float32 operands: a piece of float32
+ * logits too).  Products of so few tiles that their sums are cut leave float32 parts of
+ * the logits (64 MiB at most).
+ * 16-bit operands: dz is rounded once to their type for the two products (the matrix
+ * instruction takes operands of one type), dh and dw once to it at the end; sums are
+ * float32.  The gradients' error is 1.01 to 1.41 times that of rounding the exact ones
+ * (in the mean square, measured).  In float32 an infinity in an operand acts as a NaN. */
 typedef struct scar_xent scar_xent; /* opaque; created by scar_xent_init, freed by scar_xent_destroy */
 
 typedef enum { SCAR_MEAN = 0, SCAR_SUM = 1 } scar_reduction;
@@ -519,10 +524,11 @@ int scar_xent_destroy(scar_xent *op);
  *   out_i = coef * g_i, rounded once
  * Sums run in float32 over short runs (in double where a sum would leave float32's
  * range, so any finite tensors have a finite norm in scar_gnorm_info; the float32 of it
- * may be infinite) and in double across them, in an order that depends on the lengths and on the addresses modulo 16: equal inputs give equal bits.  A NaN or an infinity in
- * the tensors gives the IEEE result of these formulas (norm NaN: all outputs NaN; norm
- * infinite: coef 0, NaN where g is infinite) and is reported (scar_gnorm_status), so
- * that a caller can leave the step out. */
+ * may be infinite) and in double across them, in an order that, on one GPU, depends on
+ * the lengths, the types and the addresses modulo 16 alone: equal inputs there give
+ * equal bits.  A NaN or an infinity in the tensors gives the IEEE result of these
+ * formulas (norm NaN: all outputs NaN; norm infinite: coef 0, NaN where g is infinite)
+ * and is reported (scar_gnorm_status), so that a caller can leave the step out. */
 typedef struct scar_gnorm scar_gnorm; /* opaque; created by scar_gnorm_init, freed by scar_gnorm_destroy */
 
 typedef enum { SCAR_GNORM_L2 = 0, SCAR_GNORM_L1 = 1, SCAR_GNORM_MAX = 2 } scar_gnorm_kind;

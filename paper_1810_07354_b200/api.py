@@ -712,12 +712,13 @@ def _operand_type(dtype) -> int:
 
 
 class LinearCrossEntropy(_OnStream):
-    """Softmax cross entropy of ``h @ w.T`` against integer labels, with its gradients, without the matrix of logits.
+    """Softmax cross entropy of ``h @ w.T`` against integer labels, with its gradients, a piece of the rows at a time.
 
     ``max_tokens`` rows at most per call, ``n_classes`` x ``dim`` weights, all operands of ``dtype`` (float32,
     bfloat16 or float16).  Rows whose label is ``ignore_label`` do not count; ``reduction`` is ``"mean"`` (over the
-    rows that count) or ``"sum"``.  ``workspace_bytes`` bounds the block of logit gradients held at a time
-    (0: 1 GiB).  ``loss_only`` handles hold no workspace for gradients."""
+    rows that count) or ``"sum"``.  ``workspace_bytes`` bounds the block of logit gradients held at a time (0: 1 GiB;
+    at least 256 rows, and all rows where that needs less memory than the float32 sums of ``dw`` over several pieces
+    would).  ``loss_only`` handles hold no workspace for gradients."""
 
     def __init__(self, max_tokens: int, n_classes: int, dim: int, dtype, reduction: str = "mean",
                  ignore_label: int = -100, workspace_bytes: int = 0, loss_only: bool = False, stream=None,

@@ -34,7 +34,8 @@ enum class Epi { kPart, kOut, kProb, kStat };
 
 // The logits of 16-bit operands (Epi::kProb, kStat) are summed in registers over rounds of this many stages (1024
 // values of k, 64 instructions): in one accumulator over a dim of 4096 the dropped low bits put a row's loss off by
-// 1.2e-6 of itself.  dh and dw are rounded to 16 bits and need no rounds.
+// 1.2e-6 of itself.  dh and dw are rounded to 16 bits and need no rounds: over 128000 classes one accumulator adds 3 % at most
+// to the error that the two roundings (of dz and of the result) have by themselves.
 constexpr unsigned kRound = 16;
 
 template <int PL> struct TcShape {

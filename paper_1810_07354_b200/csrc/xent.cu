@@ -6,7 +6,7 @@
 //                    for gradients the exponentials relative to that maximum, in float16 (k_tc_gemm, kProb / kStat)
 //   dz               k_xent_dz joins a row's groups to lse and turns the exponentials into dz, in place
 //   dh = dz w, dw = dz^T h
-// so the logits are computed once (6 n V D operations, not 8) and, for 16-bit operands, exist only in tensor memory.
+// so the logits are computed once (6 n V D operations, not 8) and, for 16-bit operands, exist as such in tensor memory alone.
 // float32 operands keep float32 logits of the piece beside the same statistics; products with too few tiles to fill the
 // GPU (their sum over D is cut into parts) leave float32 parts for k_xent_softmax.  The last CTA of the last softmax adds
 // the row losses.
@@ -300,6 +300,10 @@ __device__ __forceinline__ float cta_add(float v, float *sh) {
     return v;
 }
 
+// dz is rounded once to the operands' type, since the matrix instruction takes both operands in one type; the other way, two
+// planes of it, would double the products' time.  Error of dh in the mean square against that of rounding the exact dh alone,
+// 256 rows, 32000 classes: bfloat16 0.00187 / 0.00166, float16 2.47e-4 / 2.08e-4 (rounding the exact dz instead gives the same
+// three digits: what the exponentials' 11 bits add does not show).
 // What the products read as dz: bfloat16 as it is; float16 times 2^15 (|dz| <= 1, and a probability of 1e-6 would be
 // next to float16's smallest step), taken out again by the products' scale.
 constexpr float kDzF16 = 32768.f;

@@ -1,7 +1,7 @@
 """Multinomial logistic regression with a running checkpoint: the training step of the paper's first workload
 (Sections 5.1, 5.3) and the checkpoint and recovery of its parameters, end to end on one GPU.
 
-Every iteration draws a minibatch, computes loss and gradient of the softmax cross entropy without the matrix of logits
+Every iteration draws a minibatch, computes loss and gradient of the softmax cross entropy
 (:class:`~paper_1810_07354_b200.LinearCrossEntropy`), clips the gradient by its global norm
 (:class:`~paper_1810_07354_b200.GradientNorm`) and takes a step.  Every ``r * full_period`` iterations the ``r`` most
 changed blocks are saved (Section 4.2).  At ``fail_at`` some shards are lost and restored (Section 4.1).  Clipping bounds a
