@@ -11,9 +11,9 @@
 // GPU (their sum over D is cut into parts) leave float32 parts for k_xent_softmax.  The last CTA of the last softmax adds
 // the row losses.
 //
-// What bounds it, measured: many rows, the tensor cores (4096 x 32000 x 2048 bfloat16: the logits' product 325 us with
-// its pipe active 87 % of the time, dh and dw together 619 us, 93 %, at the 1.4 - 1.5 GHz that the power limit leaves;
-// 80 us for the dz pass at 5.3 TB/s); few rows, reading w (one row, 128000 x 4096: 5.6 TB/s); small sizes, the chain of
+// What bounds it, measured: many rows, the tensor cores (4096 x 32000 x 2048 bfloat16: the logits' product 300 us with
+// its pipe active 86 % of the time, dh and dw together 594 us, 94 %, at the 1.5 - 1.6 GHz that the power limit leaves;
+// 81 us for the dz pass at 5.2 TB/s); few rows, reading w (one row, 128000 x 4096: 5.6 TB/s); small sizes, the chain of
 // five to seven launches (16 x 2000 x 512: 34 us).
 #include <algorithm>
 #include <new>
