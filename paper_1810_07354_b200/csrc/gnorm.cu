@@ -108,7 +108,8 @@ template <int KIND, typename T> __device__ __noinline__ double wide_terms(Split<
 // The terms of a thread's values (at most 33 of a 16-bit type): x its vectors, xe its edge element or 0.  They are summed in
 // float32, unless the sum leaves its range: squares of values above 1.8e19 are no float32, those of values below 1e-19 lose
 // bits or vanish.  A sum of at least 2^-120 has lost less than 2^-24 of itself (33 squares, each off by at most 2^-150); below
-// that, or not finite, the values are read again and summed in double (so are NaN and infinities, with the same result).
+// that, or not finite, the values are read again and summed in double (so are NaN and infinities, with the same result): 400 MB
+// of which every thread's sum takes that way 84 us, of ordinary values or zeros 67, each call waited for.
 template <int KIND, typename T> __device__ __forceinline__ double thread_terms(const Split<T> &s, const Vec<T> (&x)[kVecs], float xe) {
     float a[2] = {0.f, 0.f};
     add_term<KIND>(a[0], xe);
@@ -206,7 +207,7 @@ template <typename T> __device__ __forceinline__ void store_scaled(const Split<T
     }
 }
 // A factor below this has lost bits as a float32 or is about to: the values are scaled in double then (a norm far above the
-// limit, as only values near float32's largest give it), one by one, since such a call is rare.
+// limit, as only values near float32's largest give it), one by one, since such a call is rare (400 MB: 291 us against 187).
 constexpr double kLeastCoef = 0x1p-100;
 template <typename T> __device__ __noinline__ void scale_wide(const void *src, void *dst, unsigned n, double coef) {
     const T *s = static_cast<const T *>(src);
@@ -254,7 +255,9 @@ k_gnorm_scale(const Piece *__restrict__ pieces, const NormRecord *rec) {
 // may keep some of the CTAs from starting for as long as it likes, so the wait has an end (kPatienceNs): a CTA that reaches it
 // sets kGaveUp in ticket[0], unless all parts are there by then.  The CTAs agree, since the count cannot reach the grid's
 // without the bit once the bit is set: either all of them go on as above, or none does, and each leaves without having written
-// anything.  The last one to leave then finds all parts, whenever that is, and finishes the call by itself: same order, same bits.
+// anything.  The last one to leave then finds all parts, whenever that is, and finishes the call by itself: same order, same bits
+// (2^20 values 0.18 ms, 592 pieces 0.40 ms).  A millisecond: parts are usually there within microseconds of one another, and CTAs
+// that wait keep their multiprocessors from whatever the missing ones wait for.
 constexpr unsigned kGaveUp = 0x80000000u;
 constexpr unsigned long long kPatienceNs = 1000000ull;
 
