@@ -49,7 +49,8 @@ typedef struct scar_ctx scar_ctx; /* opaque; created by scar_ckpt_init, freed by
  * the appendix proofs of Theorems 4.1/4.2); SCAR_I32 by the integer l1 distance
  * (twice the length-scaled total variation that Appendix C uses for LDA).  The
  * 16-bit types are operand types of the training-step operators (scar_xent_*,
- * scar_gnorm_*) only: checkpoint contexts refuse them. */
+ * scar_gnorm_*, scar_linear_*, scar_dropout_*, scar_resnorm_*) only: checkpoint
+ * contexts refuse them. */
 typedef enum { SCAR_F32 = 0, SCAR_I32 = 1, SCAR_BF16 = 2, SCAR_F16 = 3 } scar_dtype;
 
 /* Which norm measures the distance of a block to its saved copy.  DEFAULT is the
@@ -568,6 +569,144 @@ int scar_gnorm_finished_alone(scar_gnorm *op, uint64_t *calls);
 int scar_gnorm_selftest_arm_timeout(scar_gnorm *op);
 uint64_t scar_gnorm_launch_count(const scar_gnorm *op);
 int scar_gnorm_destroy(scar_gnorm *op);
+
+/* ==========================================================================
+ * Hidden layers
+ *
+ * What lies between a model's input and its loss: the operators below follow the
+ * conventions of the training step above (operand types, float32 or wider sums,
+ * streams, capture). */
+
+/* ---- Dropout -------------------------------------------------------------------------
+ * A mask that is computed from (seed, offset) wherever it is needed and stored nowhere:
+ * forward, backward and a step that is taken again after a recovery have the same one.
+ * Value (row t, column c) of a matrix is kept if its 16 bits are at least cut, and then
+ * multiplied by 65536 / (65536 - cut):
+ *   cut  = p 65536 rounded, between 1 and 65535 unless p is 0 or 1
+ *   bits = the (c mod 8)-th 16 bits, low halves first, of Philox 4x32 with ten rounds,
+ *          key = seed, counter = (c / 8, t, offset low, offset high)
+ * A value that is dropped becomes 0 whatever it was (NaN, infinities).  Calls that are to
+ * have masks of their own take different offsets (a step's number times the number of
+ * masks a step has, plus which). */
+typedef struct {
+    double p;          /* 0 .. 1: the share that is dropped */
+    uint64_t seed;
+    uint64_t offset;
+    const uint64_t *d_offset; /* DEVICE, added to offset, or NULL: a captured graph takes another mask at each
+                                 replay if the caller changes it in between */
+} scar_dropout;
+
+/* y = mask . x (+ residual), rounded once.  DEVICE matrices of rows x cols values of type dtype, rows a pitch of
+ * elements apart, at any address their type allows; d_residual may be NULL; y may be x or the residual itself (same
+ * address and pitch) and may not overlap them in any other way.  Applied to dy it gives dx.  Holds no workspace and
+ * no handle: enqueues on cuda_stream, on the current device.  rows and cols below 2^31. */
+int scar_dropout_apply(const scar_dropout *rule, scar_dtype dtype, const void *d_x, uint64_t x_pitch, const void *d_residual,
+                       uint64_t residual_pitch, void *d_y, uint64_t y_pitch, uint64_t rows, uint64_t cols, void *cuda_stream);
+
+/* ---- Linear layer --------------------------------------------------------------------
+ * With x [T, K], w [N, K], bias [N], residual [T, N]:
+ *   z = x w^T + bias,   y = residual + mask . act(z)
+ * and from dy [T, N] (the residual's gradient is dy itself):
+ *   dz = mask . dy . act'(z),   dx = dz w,   dw = dz^T x,   dbias = sum_t dz
+ * act: z; max(z, 0) (derivative 0 at 0); z Phi(z) with the Gaussian's distribution function Phi; z / (1 + exp(-z)).
+ * Forward leaves act'(z) in the caller's d_slope, [T][N rounded up to 8] values of float16 (float32 beside float32
+ * operands), for backward; the mask is computed again.  16-bit operands: y is rounded once, dz once for the two
+ * products (the matrix instruction takes operands of one type; a float16 dz beyond its range is infinite), dx, dw and
+ * dbias once; sums are float32.  In float32 an infinity in x, w or dy acts as a NaN in the products. */
+typedef struct scar_linear scar_linear; /* opaque; created by scar_linear_init, freed by scar_linear_destroy */
+
+typedef enum { SCAR_ACT_IDENTITY = 0, SCAR_ACT_RELU = 1, SCAR_ACT_GELU = 2, SCAR_ACT_SILU = 3 } scar_activation;
+
+typedef struct {
+    uint64_t max_rows;     /* most rows of x a call may have, < 2^31 */
+    uint64_t in_features;  /* K, 1 .. 2^31 - 1 */
+    uint64_t out_features; /* N, 1 .. 2^31 - 1 */
+    scar_dtype dtype;      /* of x, w, bias, residual, y and the gradients: SCAR_F32, SCAR_BF16 or SCAR_F16 */
+    scar_activation activation;
+    int forward_only;      /* non-zero: no workspace for gradients; scar_linear_backward returns SCAR_ERR_STATE */
+} scar_linear_config;
+
+/* Creates the operator with its workspaces on the current device.  Waits for the stream.  On error *out is NULL.
+ * Calls of one operator share its workspaces: graphs captured from it may not run at the same time. */
+int scar_linear_init(scar_linear **out, const scar_linear_config *cfg, void *cuda_stream);
+
+/* d_bias, d_residual, dropout (HOST, read before the call returns) and d_slope may be NULL.  DEVICE matrices, row-major,
+ * rows a pitch of elements apart, at any address their type allows; d_slope on a 16-byte boundary (NULL with
+ * SCAR_ACT_IDENTITY).  16-bit rows of x and w that lie on 16-byte boundaries are read in place, others are copied first
+ * (with in_features a multiple of 8, the first such call allocates that copy: make it before a stream capture).  y may
+ * be the residual itself (same address and pitch) and may overlap nothing else. */
+int scar_linear_forward(scar_linear *op, const void *d_x, uint64_t x_pitch, const void *d_w, uint64_t w_pitch, const void *d_bias,
+                        const void *d_residual, uint64_t residual_pitch, const scar_dropout *dropout, uint64_t n_rows, void *d_y,
+                        uint64_t y_pitch, void *d_slope);
+uint64_t scar_linear_slope_bytes(const scar_linear *op, uint64_t n_rows); /* of d_slope; 0 with SCAR_ACT_IDENTITY */
+
+/* Gradients with the x, w, d_slope and dropout of the forward call.  d_dx, d_dw and d_dbias are overwritten; each may be NULL
+ * (d_w is needed for d_dx only, d_x for d_dw).  None may overlap an input or another output.  Of no rows d_dw and d_dbias
+ * are zero. */
+int scar_linear_backward(scar_linear *op, const void *d_dy, uint64_t dy_pitch, const void *d_x, uint64_t x_pitch, const void *d_w,
+                         uint64_t w_pitch, const void *d_slope, const scar_dropout *dropout, uint64_t n_rows, void *d_dx, uint64_t dx_pitch,
+                         void *d_dw, uint64_t dw_pitch, void *d_dbias);
+
+/* Waits for the stream.  SCAR_ERR_TIMEOUT if a wait inside a kernel of the calls since the last status gave up (their
+ * outputs are invalid; the operator stays usable). */
+int scar_linear_status(scar_linear *op);
+/* Self-test hook: the next call reports a wait that gave up (none does). */
+int scar_linear_selftest_arm_timeout(scar_linear *op);
+uint64_t scar_linear_workspace_bytes(const scar_linear *op); /* device memory the operator holds */
+uint64_t scar_linear_launch_count(const scar_linear *op);    /* kernels launched so far */
+int scar_linear_destroy(scar_linear *op);
+
+/* ---- Norms around a residual block -----------------------------------------------------
+ * For the output f [T, D] of a block on the residual stream x [T, D], and the input n of the next block:
+ *   u = f, or N(f; w_post, b_post)            (post)
+ *   y = x + scale gate u                      (rounded to the operands' type)
+ *   n = N(y; w_pre, b_pre)                    (pre; of the rounded y)
+ *   N(v; w, b) = (v - mean v) / sqrt(var v + eps) w + b        SCAR_RESNORM_LAYER
+ *              = v / sqrt(mean v^2 + eps) w                    SCAR_RESNORM_RMS
+ * over each row.  The gate has a row for every rows_per_gate rows of x (1: for each; T: one for all), or is left out
+ * (1).  Without f, y is x and is not written.  Backward takes the gradients dy and dn of y and n:
+ *   dY = dy + N'(dn),  dx = dY,  dgate = scale sum dY u,  df = N'(scale gate dY),  dw = sum (dout hat),  db = sum dout
+ * with sums over the rows (of a gate) in an order that depends on the sizes alone: equal inputs give equal bits.
+ * Squares and sums are float32: rows with values above 1.8e19 have an infinite deviation. */
+typedef struct scar_resnorm scar_resnorm; /* opaque; created by scar_resnorm_init, freed by scar_resnorm_destroy */
+
+typedef enum { SCAR_RESNORM_RMS = 0, SCAR_RESNORM_LAYER = 1 } scar_resnorm_kind;
+#define SCAR_RESNORM_MAX_DIM 16384
+
+typedef struct {
+    uint64_t max_rows;  /* most rows a call may have, < 2^31 */
+    uint64_t dim;       /* D, 1 .. SCAR_RESNORM_MAX_DIM (SCAR_ERR_CAPACITY beyond) */
+    double eps;         /* >= 0 */
+    scar_dtype dtype;   /* of all tensors */
+    scar_resnorm_kind kind;
+    int forward_only;   /* non-zero: no workspace for gradients; scar_resnorm_backward returns SCAR_ERR_STATE */
+} scar_resnorm_config;
+
+typedef struct {
+    int post, pre;           /* which norms */
+    float scale;             /* of the block's output */
+    const void *d_gate;      /* DEVICE [T / rows_per_gate rounded up][D], or NULL */
+    uint64_t gate_pitch, rows_per_gate;
+    const void *d_w_post, *d_b_post, *d_w_pre, *d_b_pre; /* DEVICE [D], NULL: 1 and 0; the b's with SCAR_RESNORM_LAYER only */
+} scar_resnorm_block;
+
+/* Creates the operator with its workspace on the current device.  Waits for the stream.  On error *out is NULL.  Calls
+ * of one operator share its workspace: graphs captured from it may not run at the same time. */
+int scar_resnorm_init(scar_resnorm **out, const scar_resnorm_config *cfg, void *cuda_stream);
+/* block: HOST, read before the call returns.  DEVICE matrices, rows a pitch of elements apart, at any address their type
+ * allows.  d_f may be NULL (then no post and no gate, and d_y may be NULL), d_n is needed with pre.  y may be x or f
+ * itself (same address and pitch); outputs may overlap nothing in any other way. */
+int scar_resnorm_forward(scar_resnorm *op, const scar_resnorm_block *block, const void *d_x, uint64_t x_pitch, const void *d_f, uint64_t f_pitch,
+                         uint64_t n_rows, void *d_y, uint64_t y_pitch, void *d_n, uint64_t n_pitch);
+/* d_dy may be NULL with pre (y goes nowhere else); d_dn and d_y are needed with pre.  Each gradient may be NULL; one of
+ * something that the block does not have is refused.  dx may be dy or dn itself, df may be f; outputs may overlap nothing
+ * in any other way. */
+int scar_resnorm_backward(scar_resnorm *op, const scar_resnorm_block *block, const void *d_dy, uint64_t dy_pitch, const void *d_dn, uint64_t dn_pitch,
+                          const void *d_y, uint64_t y_pitch, const void *d_f, uint64_t f_pitch, uint64_t n_rows, void *d_dx, uint64_t dx_pitch,
+                          void *d_df, uint64_t df_pitch, void *d_dgate, uint64_t dgate_pitch, void *d_dw_post, void *d_db_post, void *d_dw_pre,
+                          void *d_db_pre);
+uint64_t scar_resnorm_launch_count(const scar_resnorm *op); /* kernels launched so far */
+int scar_resnorm_destroy(scar_resnorm *op);
 
 /* Static description of an error code. */
 const char *scar_strerror(int code);

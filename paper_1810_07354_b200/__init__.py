@@ -11,8 +11,12 @@ from .api import (  # noqa: F401
     SCAR_I32,
     SCAR_BF16,
     SCAR_F16,
+    Dropout,
+    DropoutMask,
     GradientNorm,
     LinearCrossEntropy,
+    LinearLayer,
+    ResidualNorm,
     ScarError,
     ScarCheckpoint,
     lib_path,

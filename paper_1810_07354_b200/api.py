@@ -20,6 +20,8 @@ SCAR_F32, SCAR_I32, SCAR_BF16, SCAR_F16 = 0, 1, 2, 3
 SCAR_NORM_DEFAULT, SCAR_NORM_L1 = 0, 1
 SCAR_MEAN, SCAR_SUM = 0, 1
 SCAR_GNORM_L2, SCAR_GNORM_L1, SCAR_GNORM_MAX = 0, 1, 2
+SCAR_ACT_IDENTITY, SCAR_ACT_RELU, SCAR_ACT_GELU, SCAR_ACT_SILU = 0, 1, 2, 3
+SCAR_RESNORM_RMS, SCAR_RESNORM_LAYER = 0, 1
 SCAR_OK = 0
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -66,6 +68,26 @@ class scar_tensor(C.Structure):
 
 class scar_gnorm_info(C.Structure):
     _fields_ = [("norm", C.c_double), ("coef", C.c_double), ("nonfinite", C.c_uint64)]
+
+
+class scar_dropout(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64), ("d_offset", C.c_void_p)]
+
+
+class scar_linear_config(C.Structure):
+    _fields_ = [("max_rows", C.c_uint64), ("in_features", C.c_uint64), ("out_features", C.c_uint64), ("dtype", C.c_int),
+                ("activation", C.c_int), ("forward_only", C.c_int)]
+
+
+class scar_resnorm_config(C.Structure):
+    _fields_ = [("max_rows", C.c_uint64), ("dim", C.c_uint64), ("eps", C.c_double), ("dtype", C.c_int), ("kind", C.c_int),
+                ("forward_only", C.c_int)]
+
+
+class scar_resnorm_block(C.Structure):
+    _fields_ = [("post", C.c_int), ("pre", C.c_int), ("scale", C.c_float), ("d_gate", C.c_void_p), ("gate_pitch", C.c_uint64),
+                ("rows_per_gate", C.c_uint64), ("d_w_post", C.c_void_p), ("d_b_post", C.c_void_p), ("d_w_pre", C.c_void_p),
+                ("d_b_pre", C.c_void_p)]
 
 
 def lib_path() -> str:
@@ -139,6 +161,22 @@ _SIGS = {
     "scar_gnorm_selftest_arm_timeout": (_int, [_vp]),
     "scar_gnorm_launch_count": (_u64, [_vp]),
     "scar_gnorm_destroy": (_int, [_vp]),
+    "scar_dropout_apply": (_int, [C.POINTER(scar_dropout), _int, _vp, _u64, _vp, _u64, _vp, _u64, _u64, _u64, _vp]),
+    "scar_linear_init": (_int, [C.POINTER(_vp), C.POINTER(scar_linear_config), _vp]),
+    "scar_linear_forward": (_int, [_vp, _vp, _u64, _vp, _u64, _vp, _vp, _u64, C.POINTER(scar_dropout), _u64, _vp, _u64, _vp]),
+    "scar_linear_slope_bytes": (_u64, [_vp, _u64]),
+    "scar_linear_backward": (_int, [_vp, _vp, _u64, _vp, _u64, _vp, _u64, _vp, C.POINTER(scar_dropout), _u64, _vp, _u64, _vp, _u64, _vp]),
+    "scar_linear_status": (_int, [_vp]),
+    "scar_linear_selftest_arm_timeout": (_int, [_vp]),
+    "scar_linear_workspace_bytes": (_u64, [_vp]),
+    "scar_linear_launch_count": (_u64, [_vp]),
+    "scar_linear_destroy": (_int, [_vp]),
+    "scar_resnorm_init": (_int, [C.POINTER(_vp), C.POINTER(scar_resnorm_config), _vp]),
+    "scar_resnorm_forward": (_int, [_vp, C.POINTER(scar_resnorm_block), _vp, _u64, _vp, _u64, _u64, _vp, _u64, _vp, _u64]),
+    "scar_resnorm_backward": (_int, [_vp, C.POINTER(scar_resnorm_block), _vp, _u64, _vp, _u64, _vp, _u64, _vp, _u64, _u64, _vp, _u64, _vp, _u64, _vp,
+                                     _u64, _vp, _vp, _vp, _vp]),
+    "scar_resnorm_launch_count": (_u64, [_vp]),
+    "scar_resnorm_destroy": (_int, [_vp]),
     "scar_ckpt_destroy": (_int, [_vp]),
     "scar_strerror": (C.c_char_p, [_int]),
 }
@@ -541,6 +579,81 @@ def scar_gnorm_destroy(op: int) -> None:
     _check(load_library().scar_gnorm_destroy(op), "scar_gnorm_destroy")
 
 
+def scar_dropout_apply(rule: scar_dropout, dtype: int, d_x, x_pitch: int, d_residual, residual_pitch: int, d_y, y_pitch: int, rows: int, cols: int,
+                       cuda_stream: int = 0) -> None:
+    _check(load_library().scar_dropout_apply(C.byref(rule), dtype, d_x, x_pitch, d_residual, residual_pitch, d_y, y_pitch, rows, cols,
+                                             cuda_stream or None), "scar_dropout_apply")
+
+
+def scar_linear_init(config: scar_linear_config, cuda_stream: int = 0) -> int:
+    op = _vp()
+    _check(load_library().scar_linear_init(C.byref(op), C.byref(config), cuda_stream or None), "scar_linear_init")
+    return op.value
+
+
+def scar_linear_forward(op: int, d_x, x_pitch: int, d_w, w_pitch: int, d_bias, d_residual, residual_pitch: int, dropout: Optional[scar_dropout],
+                        n_rows: int, d_y, y_pitch: int, d_slope=None) -> None:
+    _check(load_library().scar_linear_forward(op, d_x, x_pitch, d_w, w_pitch, d_bias, d_residual, residual_pitch, dropout, n_rows, d_y, y_pitch,
+                                              d_slope), "scar_linear_forward")
+
+
+def scar_linear_slope_bytes(op: int, n_rows: int) -> int:
+    return int(load_library().scar_linear_slope_bytes(op, n_rows))
+
+
+def scar_linear_backward(op: int, d_dy, dy_pitch: int, d_x, x_pitch: int, d_w, w_pitch: int, d_slope, dropout: Optional[scar_dropout], n_rows: int,
+                         d_dx, dx_pitch: int, d_dw, dw_pitch: int, d_dbias) -> None:
+    _check(load_library().scar_linear_backward(op, d_dy, dy_pitch, d_x, x_pitch, d_w, w_pitch, d_slope, dropout, n_rows, d_dx, dx_pitch, d_dw,
+                                               dw_pitch, d_dbias), "scar_linear_backward")
+
+
+def scar_linear_status(op: int) -> None:
+    _check(load_library().scar_linear_status(op), "scar_linear_status")
+
+
+def scar_linear_selftest_arm_timeout(op: int) -> None:
+    _check(load_library().scar_linear_selftest_arm_timeout(op), "scar_linear_selftest_arm_timeout")
+
+
+def scar_linear_workspace_bytes(op: int) -> int:
+    return int(load_library().scar_linear_workspace_bytes(op))
+
+
+def scar_linear_launch_count(op: int) -> int:
+    return int(load_library().scar_linear_launch_count(op))
+
+
+def scar_linear_destroy(op: int) -> None:
+    _check(load_library().scar_linear_destroy(op), "scar_linear_destroy")
+
+
+def scar_resnorm_init(config: scar_resnorm_config, cuda_stream: int = 0) -> int:
+    op = _vp()
+    _check(load_library().scar_resnorm_init(C.byref(op), C.byref(config), cuda_stream or None), "scar_resnorm_init")
+    return op.value
+
+
+def scar_resnorm_forward(op: int, block: scar_resnorm_block, d_x, x_pitch: int, d_f, f_pitch: int, n_rows: int, d_y, y_pitch: int, d_n,
+                         n_pitch: int) -> None:
+    _check(load_library().scar_resnorm_forward(op, C.byref(block), d_x, x_pitch, d_f, f_pitch, n_rows, d_y, y_pitch, d_n, n_pitch),
+           "scar_resnorm_forward")
+
+
+def scar_resnorm_backward(op: int, block: scar_resnorm_block, d_dy, dy_pitch: int, d_dn, dn_pitch: int, d_y, y_pitch: int, d_f, f_pitch: int,
+                          n_rows: int, d_dx, dx_pitch: int, d_df, df_pitch: int, d_dgate, dgate_pitch: int, d_dw_post, d_db_post, d_dw_pre,
+                          d_db_pre) -> None:
+    _check(load_library().scar_resnorm_backward(op, C.byref(block), d_dy, dy_pitch, d_dn, dn_pitch, d_y, y_pitch, d_f, f_pitch, n_rows, d_dx, dx_pitch,
+                                                d_df, df_pitch, d_dgate, dgate_pitch, d_dw_post, d_db_post, d_dw_pre, d_db_pre), "scar_resnorm_backward")
+
+
+def scar_resnorm_launch_count(op: int) -> int:
+    return int(load_library().scar_resnorm_launch_count(op))
+
+
+def scar_resnorm_destroy(op: int) -> None:
+    _check(load_library().scar_resnorm_destroy(op), "scar_resnorm_destroy")
+
+
 # ---------------------------------------------------------------------------------------------
 
 
@@ -856,6 +969,284 @@ class GradientNorm(_OnStream):
     def close(self):
         if getattr(self, "op", None):
             scar_gnorm_destroy(self.op)
+            self.op = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class DropoutMask:
+    """One mask of a :class:`Dropout`: its rule, and the tensor its offset lies in (or None)."""
+
+    def __init__(self, rule: scar_dropout, tensor=None):
+        self.rule, self.tensor = rule, tensor
+
+    def at(self, device):
+        if self.tensor is not None and self.tensor.device != device:
+            raise ValueError(f"offset: a tensor on {device} is wanted")
+        return self.rule
+
+
+class Dropout(_OnStream):
+    """Dropout whose mask is computed from ``(seed, offset)`` and stored nowhere: ``forward`` and ``backward`` with one offset
+    share it, and so does a :class:`LinearLayer` given ``mask(offset)``.  ``p`` is the share that is dropped (taken to the nearest
+    multiple of 2^-16); what is kept is scaled by ``1 / (1 - p)``.  The last dimension of a tensor are its columns, all others its
+    rows.  Offsets that differ give other masks: an int, or a tensor of one int64 on the device that is read when the call runs (a
+    captured graph then takes the mask of its value at each replay)."""
+
+    def __init__(self, p: float, seed: int = 0, stream=None, device="cuda"):
+        if not 0.0 <= p <= 1.0:
+            raise ValueError("p: a share between 0 and 1 is wanted")
+        self.p, self.seed = float(p), seed
+        self._bind_stream(stream, device)
+
+    def mask(self, offset=0) -> DropoutMask:
+        tensor = None
+        if not isinstance(offset, int):
+            if offset.dtype != self._torch.int64 or offset.numel() != 1 or offset.device != self._device:
+                raise TypeError(f"offset: an int or a tensor of one int64 on {self._device} is wanted")
+            tensor, offset = offset, 0
+        return DropoutMask(scar_dropout(p=self.p, seed=self.seed & (2**64 - 1), offset=offset & (2**64 - 1), d_offset=None if tensor is None else tensor.data_ptr()),
+                           tensor)
+
+    def _rows(self, name: str, m, like):
+        if m.device != self._device or m.dtype != like.dtype:
+            raise TypeError(f"{name}: a tensor of {like.dtype} on {self._device} is wanted")
+        if m.shape != like.shape:
+            raise ValueError(f"{name}: shape {tuple(like.shape)} is wanted")
+        if m.numel() == 0:
+            return 0, 0
+        cols = m.shape[-1] if m.dim() else 1
+        if m.dim() > 2 or m.dim() == 0:
+            try:
+                m = m.view(-1, cols)
+            except RuntimeError:
+                raise ValueError(f"{name}: rows the same distance apart are wanted") from None
+        if cols > 1 and m.stride(-1) != 1:
+            raise ValueError(f"{name}: contiguous rows are wanted")
+        return m.data_ptr(), (max(m.stride(0), cols) if m.dim() == 2 and m.shape[0] == 1 else m.stride(0) if m.dim() == 2 else cols)
+
+    def _call(self, x, offset, residual, out):
+        dtype = _operand_type(x.dtype)
+        mask = self.mask(offset)
+        out = self._torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        xp, yp = self._rows("x", x, x), self._rows("out", out, x)
+        rp = (None, 0) if residual is None else self._rows("residual", residual, x)
+        if x.numel() == 0:
+            return out
+        cols = x.shape[-1] if x.dim() else 1
+        here = self._enter(x, residual, out, mask.tensor)
+        with self._torch.cuda.device(self._device):
+            scar_dropout_apply(mask.rule, dtype, *xp, *rp, *yp, x.numel() // cols, cols, self._stream.cuda_stream)
+        self._leave(here)
+        return out
+
+    def forward(self, x, offset=0, residual=None, out=None):
+        """``residual + mask * x``; ``out`` may be ``x`` or the residual."""
+        return self._call(x, offset, residual, out)
+
+    def backward(self, dy, offset=0, out=None):
+        """The gradient of x from that of the output (the residual's is ``dy`` itself)."""
+        return self._call(dy, offset, None, out)
+
+
+class _Rows(_OnStream):
+    """Checks of matrices and vectors of one type on one device."""
+
+    def _matrix(self, name: str, m, rows: int, cols: int):
+        if m.dtype != self.dtype or m.device != self._device:
+            raise TypeError(f"{name}: a tensor of {self.dtype} on {self._device} is wanted")
+        if m.dim() != 2 or tuple(m.shape) != (rows, cols) or (cols > 1 and m.stride(1) != 1):
+            raise ValueError(f"{name}: shape ({rows}, {cols}) with contiguous rows is wanted")
+        if rows > 1 and m.stride(0) < cols:
+            raise ValueError(f"{name}: rows that do not overlap are wanted")
+        return m.data_ptr(), (m.stride(0) if rows > 1 else max(m.stride(0), cols))
+
+    def _vector(self, name: str, v, n: int):
+        if v is None:
+            return None
+        if v.dtype != self.dtype or v.device != self._device:
+            raise TypeError(f"{name}: a tensor of {self.dtype} on {self._device} is wanted")
+        if v.numel() != n or not v.is_contiguous():
+            raise ValueError(f"{name}: {n} contiguous values are wanted")
+        return v.data_ptr()
+
+    def _empty(self, *shape):
+        return self._torch.empty(shape, dtype=self.dtype, device=self._device)
+
+
+_ACTIVATIONS = {"identity": SCAR_ACT_IDENTITY, "relu": SCAR_ACT_RELU, "gelu": SCAR_ACT_GELU, "silu": SCAR_ACT_SILU}
+
+
+class LinearLayer(_Rows):
+    """``residual + mask * act(x @ w.T + bias)`` in one operator, with its gradients.
+
+    ``max_rows`` rows at most per call, ``out_features`` x ``in_features`` weights, all operands of ``dtype`` (float32,
+    bfloat16 or float16).  ``activation``: ``"identity"``, ``"relu"``, ``"gelu"`` (with the Gaussian's distribution function)
+    or ``"silu"``.  ``forward_only`` handles hold no workspace for gradients."""
+
+    def __init__(self, max_rows: int, in_features: int, out_features: int, dtype, activation: str = "gelu", forward_only: bool = False,
+                 stream=None, device="cuda"):
+        import torch
+
+        cfg = scar_linear_config(max_rows=max_rows, in_features=in_features, out_features=out_features, dtype=_operand_type(dtype),
+                                 activation=_ACTIVATIONS[activation], forward_only=int(forward_only))
+        self.max_rows, self.in_features, self.out_features, self.dtype, self.activation = max_rows, in_features, out_features, dtype, activation
+        self._bind_stream(stream, device)
+        with torch.cuda.device(self._device):
+            self.op = scar_linear_init(cfg, self._stream.cuda_stream)
+
+    def _mask(self, dropout):
+        return (None, None) if dropout is None else (dropout.at(self._device), dropout.tensor)
+
+    def _slope_type(self):
+        return self._torch.float32 if self.dtype == self._torch.float32 else self._torch.float16
+
+    def _slope(self, slope, rows: int):
+        if self.activation == "identity":
+            if slope is not None:
+                raise ValueError("slope: the identity has none")
+            return None
+        shape = (rows, -(-self.out_features // 8) * 8)
+        if slope.dtype != self._slope_type() or slope.device != self._device or tuple(slope.shape) != shape or not slope.is_contiguous():
+            raise ValueError(f"slope: a contiguous tensor of {shape} of {self._slope_type()} on {self._device} is wanted")
+        return slope.data_ptr()
+
+    def _forward(self, train, x, w, bias, residual, dropout, out, slope):
+        rows, K, N = x.shape[0] if x.dim() else 0, self.in_features, self.out_features
+        xp, wp, bp = self._matrix("x", x, rows, K), self._matrix("w", w, N, K), self._vector("bias", bias, N)
+        rp = (None, 0) if residual is None else self._matrix("residual", residual, rows, N)
+        out = self._empty(rows, N) if out is None else out
+        yp = self._matrix("out", out, rows, N)
+        if train and slope is None and self.activation != "identity":
+            slope = self._torch.empty((rows, -(-N // 8) * 8), dtype=self._slope_type(), device=self._device)
+        sp = self._slope(slope, rows) if train else None
+        rule, offset = self._mask(dropout)
+        here = self._enter(x, w, bias, residual, out, slope, offset)
+        scar_linear_forward(self.op, *xp, *wp, bp, *rp, rule, rows, *yp, sp)
+        self._leave(here)
+        return (out, slope) if train else out
+
+    def forward(self, x, w, bias=None, residual=None, dropout=None, out=None):
+        """The layer's output.  ``dropout``: a mask of a :class:`Dropout` (``drop.mask(offset)``); ``out`` may be the residual."""
+        return self._forward(False, x, w, bias, residual, dropout, out, None)
+
+    def forward_train(self, x, w, bias=None, residual=None, dropout=None, out=None, slope=None):
+        """``(y, slope)``: the output, and the activation's derivative for :meth:`backward` (None for the identity)."""
+        return self._forward(True, x, w, bias, residual, dropout, out, slope)
+
+    def backward(self, dy, x, w, slope, dropout=None, dx=None, dw=None, dbias=None, need_dx: bool = True, need_dw: bool = True, need_dbias: bool = True):
+        """``(dx, dw, dbias)`` from the gradient of the output, which is the residual's own; None for what is not needed."""
+        rows, K, N = dy.shape[0] if dy.dim() else 0, self.in_features, self.out_features
+        dyp, xp, wp, sp = self._matrix("dy", dy, rows, N), self._matrix("x", x, rows, K), self._matrix("w", w, N, K), self._slope(slope, rows)
+        dx = None if not need_dx else self._empty(rows, K) if dx is None else dx
+        dw = None if not need_dw else self._empty(N, K) if dw is None else dw
+        dbias = None if not need_dbias else self._empty(N) if dbias is None else dbias
+        dxp = (None, 0) if dx is None else self._matrix("dx", dx, rows, K)
+        dwp = (None, 0) if dw is None else self._matrix("dw", dw, N, K)
+        dbp = self._vector("dbias", dbias, N)
+        rule, offset = self._mask(dropout)
+        here = self._enter(dy, x, w, slope, dx, dw, dbias, offset)
+        scar_linear_backward(self.op, *dyp, *xp, *wp, sp, rule, rows, *dxp, *dwp, dbp)
+        self._leave(here)
+        return dx, dw, dbias
+
+    def status(self) -> None:
+        """Waits; raises if a wait inside a kernel of the calls since the last status gave up."""
+        scar_linear_status(self.op)
+
+    def workspace_bytes(self) -> int:
+        return scar_linear_workspace_bytes(self.op)
+
+    def close(self):
+        if getattr(self, "op", None):
+            scar_linear_destroy(self.op)
+            self.op = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class ResidualNorm(_Rows):
+    """The norms around a residual block: ``y = x + scale * gate * N(f; w_post, b_post)`` and ``n = N(y; w_pre, b_pre)`` in one pass
+    over the rows, with the gradients.
+
+    ``max_rows`` rows of ``dim`` values of ``dtype`` (float32, bfloat16 or float16); ``kind``: ``"rms"`` or ``"layer"`` (with means
+    and biases).  ``post`` and ``pre`` say which of the norms a call has; a weight or bias that is None is 1 or 0.  The gate has one
+    row for every ``rows_per_gate`` rows.  Without ``f`` (the first norm of a model) y is x.  ``forward_only`` handles hold no
+    workspace for gradients."""
+
+    def __init__(self, max_rows: int, dim: int, dtype, kind: str = "rms", eps: float = 1e-6, forward_only: bool = False, stream=None, device="cuda"):
+        import torch
+
+        cfg = scar_resnorm_config(max_rows=max_rows, dim=dim, eps=eps, dtype=_operand_type(dtype),
+                                  kind={"rms": SCAR_RESNORM_RMS, "layer": SCAR_RESNORM_LAYER}[kind], forward_only=int(forward_only))
+        self.max_rows, self.dim, self.dtype, self.kind = max_rows, dim, dtype, kind
+        self._bind_stream(stream, device)
+        with torch.cuda.device(self._device):
+            self.op = scar_resnorm_init(cfg, self._stream.cuda_stream)
+
+    def _block(self, rows, post, pre, scale, gate, rows_per_gate, w_post, b_post, w_pre, b_pre):
+        if rows_per_gate < 1:
+            raise ValueError("rows_per_gate: at least 1 is wanted")
+        gp = (None, 0) if gate is None else self._matrix("gate", gate, -(-rows // rows_per_gate), self.dim)
+        return scar_resnorm_block(post=int(post), pre=int(pre), scale=scale, d_gate=gp[0], gate_pitch=gp[1], rows_per_gate=rows_per_gate,
+                                  d_w_post=self._vector("w_post", w_post, self.dim), d_b_post=self._vector("b_post", b_post, self.dim),
+                                  d_w_pre=self._vector("w_pre", w_pre, self.dim), d_b_pre=self._vector("b_pre", b_pre, self.dim))
+
+    def _maybe(self, name, m, rows):
+        return (None, 0) if m is None else self._matrix(name, m, rows, self.dim)
+
+    def forward(self, x, f=None, post: bool = True, pre: bool = True, scale: float = 1.0, gate=None, rows_per_gate: int = 1, w_post=None, b_post=None,
+                w_pre=None, b_pre=None, y=None, n=None):
+        """``(y, n)``; n is None without ``pre``, y is x itself without ``f``.  ``y`` may be given as x or f."""
+        rows = x.shape[0] if x.dim() else 0
+        post = post and f is not None
+        block = self._block(rows, post, pre, scale, gate, rows_per_gate, w_post, b_post, w_pre, b_pre)
+        xp, fp = self._matrix("x", x, rows, self.dim), self._maybe("f", f, rows)
+        if f is None and y is None:
+            yp = (None, 0)
+        else:
+            y = self._empty(rows, self.dim) if y is None else y
+            yp = self._matrix("y", y, rows, self.dim)
+        n = None if not pre else self._empty(rows, self.dim) if n is None else n
+        np_ = self._maybe("n", n, rows)
+        here = self._enter(x, f, gate, w_post, b_post, w_pre, b_pre, y, n)
+        scar_resnorm_forward(self.op, block, *xp, *fp, rows, *yp, *np_)
+        self._leave(here)
+        return (x if y is None else y), n
+
+    def backward(self, dy, dn, y, f=None, post: bool = True, pre: bool = True, scale: float = 1.0, gate=None, rows_per_gate: int = 1, w_post=None,
+                 b_post=None, w_pre=None, b_pre=None, out=None):
+        """The gradients, by name: ``dx``, ``df``, ``dgate``, ``dw_post``, ``db_post``, ``dw_pre``, ``db_pre``, None where the call has no such
+        input.  ``dy`` may be None (with ``pre``) where y goes nowhere else; without ``pre``, ``dn`` is None and ``y`` is not read.
+        ``out``: a dictionary of tensors to write some of them to."""
+        some = dy if dy is not None else dn
+        rows = some.shape[0] if some.dim() else 0
+        post = post and f is not None
+        block = self._block(rows, post, pre, scale, gate, rows_per_gate, w_post, b_post, w_pre, b_pre)
+        dyp, dnp = self._maybe("dy", dy, rows), self._maybe("dn", dn if pre else None, rows)
+        yp, fp = self._maybe("y", y if pre else None, rows), self._maybe("f", f, rows)
+        has = {"dx": some, "df": f, "dgate": gate, "dw_post": w_post if post else None, "db_post": b_post if post else None,
+               "dw_pre": w_pre if pre else None, "db_pre": b_pre if pre else None}
+        out = out or {}
+        got = {k: None if v is None else out[k] if k in out else self._empty(*v.shape) for k, v in has.items()}
+        matrices = [self._maybe(k, got[k], rows if k != "dgate" or gate is None else gate.shape[0]) for k in ("dx", "df", "dgate")]
+        vectors = [self._vector(k, got[k], self.dim) for k in ("dw_post", "db_post", "dw_pre", "db_pre")]
+        here = self._enter(dy, dn, y, f, gate, w_post, b_post, w_pre, b_pre, *got.values())
+        scar_resnorm_backward(self.op, block, *dyp, *dnp, *yp, *fp, rows, *matrices[0], *matrices[1], *matrices[2], *vectors)
+        self._leave(here)
+        return got
+
+    def close(self):
+        if getattr(self, "op", None):
+            scar_resnorm_destroy(self.op)
             self.op = None
 
     def __del__(self):

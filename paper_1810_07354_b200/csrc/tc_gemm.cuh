@@ -21,7 +21,8 @@
 #pragma once
 #include <cuda.h>
 
-#include "train_common.cuh"
+#include "activation.cuh"
+#include "mask.cuh"
 
 namespace scar {
 
@@ -30,7 +31,9 @@ constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = (kEpiWarps + 2) * 32;
 constexpr unsigned long long kWaitNs = 2000000000ull;  // a wait inside the kernel gives up after two seconds
 
-enum class Epi { kPart, kOut, kProb, kStat };
+enum class Epi { kPart, kOut, kProb, kStat, kIdentity, kRelu, kGelu, kSilu };  // the last four: a layer's output, by its activation
+__host__ __device__ constexpr bool is_layer(Epi e) { return e >= Epi::kIdentity; }
+__host__ __device__ constexpr int act_of(Epi e) { return (int)e - (int)Epi::kIdentity; }
 
 // The logits of 16-bit operands (Epi::kProb, kStat) are summed in registers over rounds of this many stages (1024
 // values of k, 64 instructions): in one accumulator over a dim of 4096 the dropped low bits put a row's loss off by
@@ -50,12 +53,22 @@ constexpr int kWarpStage = 32 * 128;  // epilogue: 32 rows of 128 bytes per warp
 constexpr int kTcSmem = 6 * 2 * 128 * kBK * 2 + kEpiWarps * kWarpStage + 1024;
 static_assert(TcShape<1>::kStages * TcShape<1>::kStageBytes == TcShape<3>::kStages * TcShape<3>::kStageBytes, "both fill 192 KiB");
 
+// What a layer's epilogue adds to its product (kIdentity .. kSilu; k_linear_join where the sum was split).
+struct LayerArgs {
+    CUtensorMap slope_map;   // of slope, stored through it
+    void *slope;             // [m][n rounded up to 8] the activation's derivative: float16, float32 beside float32; or nullptr
+    const void *bias, *res;  // each may be nullptr
+    unsigned long long res_pitch;
+    int bias_vec, res_vec;   // on 16-byte boundaries
+    DropRule drop;
+};
+
 struct TcArgs {
     CUtensorMap a, b, c;     // c: the result, where whole boxes of it can be stored (c_map)
     unsigned m, n, k;        // extents; the one `dyn` names is an upper bound
     int dyn;                 // 0: m, 1: k is the number of rows of this piece
     unsigned first, most;    // the piece's rows of the compacted list
-    const unsigned *rows;    // rows that count (device)
+    const unsigned *rows;    // rows that count (device); nullptr: `most` of them
     unsigned a_row0, b_row0; // where the piece starts in the row dimension of the tensor maps
     unsigned splits;         // 1, or more: the product then chooses for the rows it finds (pick_splits) ...
     unsigned *chosen;        // ... and leaves its choice here for the kernel that joins the parts
@@ -85,6 +98,7 @@ struct TcArgs {
     unsigned stat_pitch;
     const int *label;        // of the compacted rows
     float *label_z;
+    LayerArgs layer;
 };
 
 // A probability is held as 2^15 exp(z - maximum of its group) in float16: 11 bits down to 2^-29 of the group's largest.
@@ -264,6 +278,7 @@ __device__ __forceinline__ unsigned pick_splits(const TcArgs &g, unsigned m, uns
     return best;
 }
 __device__ __forceinline__ unsigned rows_of(const TcArgs &g) {
+    if (!g.rows) return g.most;
     const unsigned rows = *g.rows;
     return rows > g.first ? min(g.most, rows - g.first) : 0u;
 }
@@ -598,12 +613,118 @@ template <typename F> __device__ __forceinline__ void store_halves(const CUtenso
     }
 }
 
+// 64 columns of 32 rows of 16-bit values from memory into the stage, a line per eight lanes, and from there this lane's row.
+__device__ __forceinline__ void stage_read16(uint8_t *stage, const unsigned short *base, unsigned long long pitch, bool vec, const EpiRows &rows, unsigned left, unsigned lane, Chunk (&x)[8]) {
+    stage_free();
+    if (vec && left >= 64) {
+        const unsigned c = lane & 7;
+        uint4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned r = i * 4 + (lane >> 3);
+            v[i] = rows.has(r) ? *reinterpret_cast<const uint4 *>(base + (rows.row0 + r) * pitch + c * 8) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *stage_at(stage, i * 4 + (lane >> 3), c) = v[i];
+    } else {
+        unsigned short *st = reinterpret_cast<unsigned short *>(stage);
+#pragma unroll 8
+        for (unsigned r = 0; r < 32; ++r) {
+            const unsigned short *p = base + (rows.row0 + r) * pitch;
+#pragma unroll
+            for (unsigned h = 0; h < 64; h += 32) {
+                const unsigned c = h + lane;
+                st[r * 64 + (((c >> 3) ^ (r & 7)) << 3) + (c & 7)] = rows.has(r) && c < left ? p[c] : (unsigned short)0;
+            }
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[c].u = *stage_at(stage, lane, c);
+}
+
+// Eight values of the bias from column col on, zeros behind the last one.
+template <typename T> __device__ __forceinline__ void bias8(const LayerArgs &l, unsigned col, unsigned n, float (&b)[8]) {
+    const T *p = static_cast<const T *>(l.bias) + col;
+    if (l.bias_vec && col + 8 <= n) {
+        union {
+            uint4 u[sizeof(T) / 2];
+            T v[8];
+        } x;
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(T) / 2; ++i) x.u[i] = reinterpret_cast<const uint4 *>(p)[i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = to_f32(x.v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = col + j < n ? to_f32(p[j]) : 0.f;
+    }
+}
+
+// Eight products of a row become the layer's values (without the residual); slope: their derivatives.
+template <int ACT, typename T> __device__ __forceinline__ void layer8(const LayerArgs &l, unsigned long long offset, unsigned row, unsigned col, unsigned n, float *z, float *slope) {
+    if (l.bias) {
+        float b[8];
+        bias8<T>(l, col, n, b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] += b[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) activate<ACT>(z[j], z[j], slope[j]);
+    if (l.drop.cut) {
+        const uint4 bits = mask_bits(l.drop, offset, row, col >> 3);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = mask_apply(l.drop, bits, j, z[j]);
+    }
+}
+
+// A tile's 128 columns of this thread's row, 64 at a time, from the accumulator to the layer's output and slope (16-bit types).
+template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const TcArgs &g, uint32_t acc, bool any, const EpiRows &rows, unsigned col, uint8_t *stage, unsigned &half, unsigned lane) {
+    const LayerArgs &l = g.layer;
+    const unsigned long long offset = l.drop.cut ? l.drop.at() : 0ull;
+#pragma unroll 1
+    for (unsigned j = 0; j < kCols && col + j < g.n; j += 64) {
+        const unsigned at = col + j, left = g.n - at;
+        Chunk y[8], s[8];  // packed results and slopes
+        if (l.res) stage_read16(stage, static_cast<const unsigned short *>(l.res) + at, l.res_pitch, l.res_vec, rows, left, lane, y);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[32] = {};
+            if (any) {
+                tmem_load32(acc + j + h * 32, v);
+                tmem_loaded(v);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float slope[8];
+                layer8<ACT, T>(l, offset, rows.row0 + lane, at + h * 32 + c * 8, g.n, v + c * 8, slope);
+                Chunk &o = y[h * 4 + c];
+                if (l.res) {
+                    const T *r = reinterpret_cast<const T *>(&o);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[c * 8 + i] += to_f32(r[i]);
+                }
+                o.u = std::is_same<T, __half>::value ? pack_half8(v + c * 8) : pack_bf8(v + c * 8);
+                if (l.slope) s[h * 4 + c].u = pack_half8(slope);
+            }
+        }
+        if (l.slope) store_halves(&l.slope_map, stage, half, lane, rows.has(0), left, (int)at, (int)rows.row0, [&](int c) { return s[c].u; });
+        if (g.c_map) {
+            store_halves(&g.c, stage, half, lane, rows.has(0), left, (int)at, (int)rows.row0, [&](int c) { return y[c].u; });
+        } else {
+            stage_fill(stage, lane, [&](int c) { return y[c].u; });
+            flush16(stage, static_cast<unsigned short *>(g.out) + at, g.out_pitch, g.out_vec, rows, left, lane);
+        }
+    }
+}
+
 // N = 2 runs two products with results of their own (kOut): the first one's A is K-major, the second one's MN-major.
 template <int N> struct TcSet {
     TcArgs p[N];
 };
+// static: every unit that launches it has instances of its own
 template <int PL, bool A_MN, bool B_MN, Epi EPI, int N>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
+static __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 k_tc_gemm(const __grid_constant__ TcSet<N> set) {
     using S = TcShape<PL>;
     __shared__ TileWalk walks[N];
@@ -833,6 +954,23 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
             } else {
                 const EpiRows rows = epi_rows<EPI>(g, walks[t.which].m, t.mi * kBM + rank * 128 + quad * 32, t.s, lane);
                 const unsigned col = t.ni * kBN + half * kCols;
+                if constexpr (is_layer(EPI)) {
+                    if (rounds) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, error));
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    }
+                    if (g.bf16) epi_layer<act_of(EPI), __nv_bfloat16>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, half_next, lane);
+                    else epi_layer<act_of(EPI), __half>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, half_next, lane);
+                    if (rounds) {
+                        acc_release(acc_empty + 8 * ac, lane);
+                        if (++ac == kAccs) {
+                            ac = 0;
+                            aph ^= 1;
+                        }
+                    }
+                    continue;
+                }
                 const F32Out o = f32_out<EPI>(g);
                 const bool to16 = EPI == Epi::kOut && g.out_type != SCAR_F32;
                 const bool last16 = to16 && g.acc && g.acc_last, pack16 = to16 && !g.acc;
