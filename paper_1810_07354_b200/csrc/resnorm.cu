@@ -535,7 +535,7 @@ int check_block(const scar_resnorm *op, const scar_resnorm_block *k, const void 
     for (const void *p : {k->d_w_post, k->d_b_post, k->d_w_pre, k->d_b_pre})
         if ((uintptr_t)p % b) return SCAR_ERR_INVALID_ARG;
     if (op->cfg.kind == SCAR_RESNORM_RMS && (k->d_b_post || k->d_b_pre)) return SCAR_ERR_INVALID_ARG;
-    if (!f && (k->post || k->d_gate)) return SCAR_ERR_INVALID_ARG;
+    if (rows && !f && (k->post || k->d_gate)) return SCAR_ERR_INVALID_ARG;
     if (k->d_gate && !k->rows_per_gate) return SCAR_ERR_INVALID_ARG;
     return check_current_device(op->device);
 }
