@@ -705,6 +705,11 @@ int scar_resnorm_backward(scar_resnorm *op, const scar_resnorm_block *block, con
                           const void *d_y, uint64_t y_pitch, const void *d_f, uint64_t f_pitch, uint64_t n_rows, void *d_dx, uint64_t dx_pitch,
                           void *d_df, uint64_t df_pitch, void *d_dgate, uint64_t dgate_pitch, void *d_dw_post, void *d_db_post, void *d_dw_pre,
                           void *d_db_pre);
+/* Waits for the stream.  SCAR_ERR_TIMEOUT if a wait inside a kernel of the calls since the last status gave up (their
+ * outputs are invalid; the operator stays usable). */
+int scar_resnorm_status(scar_resnorm *op);
+/* Self-test hook: the next call reports a wait that gave up (none does). */
+int scar_resnorm_selftest_arm_timeout(scar_resnorm *op);
 uint64_t scar_resnorm_launch_count(const scar_resnorm *op); /* kernels launched so far */
 int scar_resnorm_destroy(scar_resnorm *op);
 

@@ -175,6 +175,8 @@ _SIGS = {
     "scar_resnorm_forward": (_int, [_vp, C.POINTER(scar_resnorm_block), _vp, _u64, _vp, _u64, _u64, _vp, _u64, _vp, _u64]),
     "scar_resnorm_backward": (_int, [_vp, C.POINTER(scar_resnorm_block), _vp, _u64, _vp, _u64, _vp, _u64, _vp, _u64, _u64, _vp, _u64, _vp, _u64, _vp,
                                      _u64, _vp, _vp, _vp, _vp]),
+    "scar_resnorm_status": (_int, [_vp]),
+    "scar_resnorm_selftest_arm_timeout": (_int, [_vp]),
     "scar_resnorm_launch_count": (_u64, [_vp]),
     "scar_resnorm_destroy": (_int, [_vp]),
     "scar_ckpt_destroy": (_int, [_vp]),
@@ -644,6 +646,14 @@ def scar_resnorm_backward(op: int, block: scar_resnorm_block, d_dy, dy_pitch: in
                           d_db_pre) -> None:
     _check(load_library().scar_resnorm_backward(op, C.byref(block), d_dy, dy_pitch, d_dn, dn_pitch, d_y, y_pitch, d_f, f_pitch, n_rows, d_dx, dx_pitch,
                                                 d_df, df_pitch, d_dgate, dgate_pitch, d_dw_post, d_db_post, d_dw_pre, d_db_pre), "scar_resnorm_backward")
+
+
+def scar_resnorm_status(op: int) -> None:
+    _check(load_library().scar_resnorm_status(op), "scar_resnorm_status")
+
+
+def scar_resnorm_selftest_arm_timeout(op: int) -> None:
+    _check(load_library().scar_resnorm_selftest_arm_timeout(op), "scar_resnorm_selftest_arm_timeout")
 
 
 def scar_resnorm_launch_count(op: int) -> int:
@@ -1243,6 +1253,10 @@ class ResidualNorm(_Rows):
         scar_resnorm_backward(self.op, block, *dyp, *dnp, *yp, *fp, rows, *matrices[0], *matrices[1], *matrices[2], *vectors)
         self._leave(here)
         return got
+
+    def status(self) -> None:
+        """Waits; raises if a wait inside a kernel of the calls since the last status gave up."""
+        scar_resnorm_status(self.op)
 
     def close(self):
         if getattr(self, "op", None):

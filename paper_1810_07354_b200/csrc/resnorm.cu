@@ -10,9 +10,13 @@
 //   dY = dy + r_y (g - mean g - y^ mean(g y^))          dx = dY           dw_pre = sum dn y^    db_pre = sum dn
 //   du = scale gate dY    dgate = scale sum dY u        df = r_f (h - mean h - f^ mean(h f^))   dw_post = sum du f^   db_post = sum du
 //
-// The statistics of a row and the two sums over g come out of one reduction: a thread's count, mean and sum of squared deviations
-// are merged pair by pair (Chan, Golub, LeVeque 1979), and so is its sum of g (y - its own mean).  No sum of squares is taken far
-// from the mean, so rows whose mean is large beside their deviation keep theirs.
+// A row's mean is summed first and its squared deviations from it second: no sum of squares is taken far from the mean, so rows
+// whose mean is large beside their deviation keep theirs.
+//
+// Memory is what bounds it, so the next rows are always on their way: a ring of rows in shared memory, filled by bulk copies
+// (cp.async.bulk) that one warp issues.  A stage is free again at the row's first reduction, when every thread has its values in
+// registers.  Rows longer than 4096 values are cut over the CTAs of a cluster, which exchange their sums through distributed
+// shared memory: a thread has eight values of a row whatever its length, and its columns' sums fit its registers.
 //
 // Sums over rows: a CTA walks a run of rows and keeps its threads' columns in registers; k_resnorm_join adds the CTAs' sums in
 // order.  Gates shared by several rows end inside a CTA's run, or reach over its ends: those leave partial sums too.
@@ -21,432 +25,741 @@
 #include <new>
 #include <type_traits>
 
-#include "train_common.cuh"
+#include "barriers.cuh"
+#include "pairs.cuh"
 
 using namespace scar;
 
 namespace {
 
-constexpr unsigned kMostThreads = 512;
+constexpr unsigned kSpan = 4096;  // columns of a CTA at most
+constexpr unsigned kMostCluster = (SCAR_RESNORM_MAX_DIM + kSpan - 1) / kSpan, kMostStages = 6;
+// Values of a row that a thread has, and rows that it has under way at a time.  Forward: 16, so that what a thread does once per row
+// (waits, sums over the CTA, addresses) is shared by many (16384 x 4096 bfloat16: 110 us, with 8 values 187).  Backward: the sums
+// over rows take two to five registers a value; eight values and two rows share those, and the rows' sums over the CTA are one
+// reduction.  float32 rows leave no room in shared memory for two at a time, and have twice the time.
+constexpr int kForwardValues = 16;
+__host__ __device__ constexpr int back_values(bool layer) { return layer ? 8 : 16; }
+template <typename T> __host__ __device__ constexpr int back_rows(bool layer) { return layer && sizeof(T) == 2 ? 2 : 1; }
+template <typename T> __host__ __device__ constexpr int back_ctas(bool layer) { return layer || sizeof(T) == 4 ? 1 : 2; }
+__host__ __device__ constexpr int threads_of(int values) { return (int)kSpan / values; }
+constexpr unsigned kNoStage = 0xffffffffu;
+
+// Rows that are read: row r of the operator is row r / per of the matrix.
+template <typename T> struct In {
+    const T *p;
+    unsigned long long pitch;
+    unsigned per;
+};
+enum { kX, kF, kGate, kForwardIn };              // forward
+enum { kDy, kDn, kY, kBackF, kBackGate, kBackwardIn };  // backward
 
 template <typename T> struct NormArgs {
     unsigned rows, dim;
     float scale, eps;
-    int post, pre;
-    const T *gate;
-    unsigned long long gate_pitch;
-    unsigned per_gate;
+    int post, pre, has_f, has_gate;
+    In<T> in[kBackwardIn];
     const T *w_post, *b_post, *w_pre, *b_pre;
-    const T *x, *f;  // backward: x is dy (may be nullptr)
-    unsigned long long x_pitch, f_pitch;
-    T *y, *n;        // backward: y is read, n is dx
-    unsigned long long y_pitch, n_pitch;
+    T *y, *n, *df, *dgate;                      // backward: n is dx
+    unsigned long long y_pitch, n_pitch, df_pitch, dgate_pitch;
+    unsigned cluster, span;                     // CTAs of a row, and columns of each but the last
+    unsigned stages, array_bytes, stage_bytes;  // of the ring
+    unsigned slot_off, smem;                    // where sums of rows begin, and bytes in all
+    unsigned *error;
     // backward
-    const T *dn;
-    T *df, *dgate;
-    unsigned long long dn_pitch, df_pitch, dgate_pitch;
-    unsigned per_cta;            // rows
-    float *part;                 // [4][CTAs][dim]: dw_pre, dw_post, db_pre, db_post
-    float *part_gate;            // [CTAs][2][dim]: of a gate that began before the CTA's rows, of one that ends behind them
+    unsigned per_gate, per_run;  // rows
+    float *part;                 // [4][runs][dim]: dw_pre, dw_post, db_pre, db_post
+    float *part_gate;            // [runs][2][dim]: of a gate that began before the run, of one that ends behind it
     T *dw_post, *db_post, *dw_pre, *db_pre;
 };
 
-// A thread's values of one row.  Rows on 16-byte boundaries: groups of eight neighbours, a group per thread and round.  Rows
-// anywhere: single values, neighbouring threads next to one another, so that a warp's access is one run of memory.
-template <typename T, int NC> union Row {
-    uint4 u[NC * sizeof(T) / 2];
-    T v[8 * NC];
+// A thread's N values of one row.  Rows on 16-byte boundaries: 16 bytes of neighbours per thread and round.  Rows anywhere: single
+// values, neighbouring threads next to one another, so that a warp's access is one run of memory.
+template <typename T, int N> union Row {
+    uint4 u[N * sizeof(T) / 16];
+    T v[N];
+    __device__ Row() {}
 };
-template <bool VEC> __device__ __forceinline__ unsigned col_of(int i) {
-    return VEC ? (i / 8 * blockDim.x + threadIdx.x) * 8 + i % 8 : i * blockDim.x + threadIdx.x;
+template <bool VEC, typename T> __device__ __forceinline__ unsigned col_of(int i) {
+    constexpr int kWord = 16 / sizeof(T);
+    return VEC ? (i / kWord * blockDim.x + threadIdx.x) * kWord + i % kWord : i * blockDim.x + threadIdx.x;
 }
-template <bool VEC, typename T, int NC> __device__ __forceinline__ void load_row(Row<T, NC> &r, const T *p, unsigned dim) {
-    if (VEC) {
+template <bool VEC, typename T, int N> __device__ __forceinline__ void load_row(Row<T, N> &r, const T *p, unsigned cols) {
+    if (VEC) {  // rows are whole words
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const unsigned col = col_of<true>(c * 8);
-            if (col + 8 <= dim) {
-#pragma unroll
-                for (unsigned k = 0; k < sizeof(T) / 2; ++k) r.u[c * (sizeof(T) / 2) + k] = reinterpret_cast<const uint4 *>(p + col)[k];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) r.v[c * 8 + j] = col + j < dim ? p[col + j] : from_f32<T>(0.f);
-            }
+        for (unsigned k = 0; k < N * sizeof(T) / 16; ++k) {
+            const unsigned col = col_of<true, T>(k * (16 / sizeof(T)));
+            r.u[k] = col < cols ? *reinterpret_cast<const uint4 *>(p + col) : make_uint4(0, 0, 0, 0);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8 * NC; ++i) {
-            const unsigned col = col_of<false>(i);
-            r.v[i] = col < dim ? p[col] : from_f32<T>(0.f);
+        for (int i = 0; i < N; ++i) {
+            const unsigned col = col_of<false, T>(i);
+            r.v[i] = col < cols ? p[col] : from_f32<T>(0.f);
         }
     }
 }
-template <bool VEC, typename T, int NC> __device__ __forceinline__ void store_row(T *p, const Row<T, NC> &r, unsigned dim) {
+template <bool VEC, typename T, int N> __device__ __forceinline__ void store_row(T *p, const Row<T, N> &r, unsigned cols) {
     if (VEC) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const unsigned col = col_of<true>(c * 8);
-            if (col + 8 <= dim) {
-#pragma unroll
-                for (unsigned k = 0; k < sizeof(T) / 2; ++k) reinterpret_cast<uint4 *>(p + col)[k] = r.u[c * (sizeof(T) / 2) + k];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (col + j < dim) p[col + j] = r.v[c * 8 + j];
-            }
+        for (unsigned k = 0; k < N * sizeof(T) / 16; ++k) {
+            const unsigned col = col_of<true, T>(k * (16 / sizeof(T)));
+            if (col < cols) *reinterpret_cast<uint4 *>(p + col) = r.u[k];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8 * NC; ++i) {
-            const unsigned col = col_of<false>(i);
-            if (col < dim) p[col] = r.v[i];
+        for (int i = 0; i < N; ++i) {
+            const unsigned col = col_of<false, T>(i);
+            if (col < cols) p[col] = r.v[i];
+        }
+    }
+}
+template <bool VEC, typename T, int N> __device__ __forceinline__ void read_row(float2 (&v)[N / 2], const T *p, unsigned cols) {
+    Row<T, N> r;
+    load_row<VEC>(r, p, cols);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[i] = Two<T>::get(r.v + 2 * i);
+}
+// The same from a stage of the ring, where zeros lie behind the row.
+template <bool VEC, typename T, int N> __device__ __forceinline__ void fetch_row(float2 (&v)[N / 2], const T *p) {
+    Row<T, N> r;
+    load_row<VEC>(r, p, ~0u);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[i] = Two<T>::get(r.v + 2 * i);
+}
+template <bool VEC, typename T, int N> __device__ __forceinline__ void write_row(T *p, const float2 (&v)[N / 2], unsigned cols) {
+    Row<T, N> r;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) Two<T>::put(r.v + 2 * i, v[i]);
+    store_row<VEC>(p, r, cols);
+}
+// A thread's own copy of a vector in shared memory, zeros behind its columns.
+template <bool VEC, typename T, int N> __device__ __forceinline__ void put_row(T *p, const Row<T, N> &r) { store_row<VEC>(p, r, ~0u); }
+template <bool VEC, typename T, int N> __device__ __forceinline__ void take_row(Row<T, N> &r, const T *p) { load_row<VEC>(r, p, ~0u); }
+template <bool VEC, typename T, int N> __device__ __forceinline__ void load_vector(Row<T, N> &r, const T *p, unsigned cols, unsigned col0, float otherwise) {
+    if (p) {
+        load_row<VEC>(r, p + col0, cols);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(col_of<VEC, T>(i) < cols ? otherwise : 0.f);
+}
+// v + shift, but zeros stay behind the row.
+template <bool VEC, typename T, int N> __device__ __forceinline__ void shift_row(float2 (&v)[N / 2], float shift, unsigned cols) {
+    constexpr int kWord = VEC ? 16 / sizeof(T) : 1;  // all or none of a word's values lie in the row
+#pragma unroll
+    for (int i = 0; i < N; i += kWord) {
+        const float s = col_of<VEC, T>(i) < cols ? shift : 0.f;
+        if (kWord == 1) {
+            float &x = i & 1 ? v[i / 2].y : v[i / 2].x;
+            x += s;
+        } else {
+#pragma unroll
+            for (int j = i / 2; j < (i + kWord) / 2; ++j) v[j] = add2(v[j], both(s));
+        }
+    }
+}
+template <int M> __device__ __forceinline__ float total(const float2 (&v)[M]) {
+    float2 s = v[0];
+#pragma unroll
+    for (int i = 1; i < M; ++i) s = add2(s, v[i]);
+    return s.x + s.y;
+}
+template <int M> __device__ __forceinline__ float dot(const float2 (&a)[M], const float2 (&b)[M]) {
+    float2 s = mul2(a[0], b[0]);
+#pragma unroll
+    for (int i = 1; i < M; ++i) s = fma2(a[i], b[i], s);
+    return s.x + s.y;
+}
+
+// The CTA's ring of rows.  Its methods that copy are called by all lanes of warp 0 and by no other.
+template <typename T, bool VEC, int IN, int R> struct Ring {
+    const NormArgs<T> &g;
+    uint8_t *smem;
+    uint32_t full;  // barriers, one per stage; rows anywhere: a second arrival reports the values at a row's ends
+    unsigned col0, cols;
+    T edge[R][VEC ? 1 : IN];  // on their way to the stages of the rows that were issued last
+
+    __device__ __forceinline__ const T *source(int a, unsigned row) const {
+        const In<T> &m = g.in[a];
+        return m.p + (unsigned long long)(m.per > 1 ? row / m.per : row) * m.pitch + col0;
+    }
+    // Where a row lies in its stage: as far from a 16-byte boundary as in memory.
+    __device__ __forceinline__ const T *at(int a, unsigned row, unsigned stage) const {
+        const unsigned off = VEC ? 0u : (unsigned)(uintptr_t)source(a, row) & 15u;
+        return reinterpret_cast<const T *>(smem + stage * g.stage_bytes + a * g.array_bytes + off);
+    }
+    // The whole 16-byte words of a row's values.
+    __device__ __forceinline__ void words(const T *p, uintptr_t &from, uintptr_t &to) const {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = a + cols * sizeof(T);
+        from = VEC ? a : (a + 15) & ~uintptr_t(15);
+        to = VEC ? b : b & ~uintptr_t(15);
+        if (to < from) to = from;
+    }
+    // This lane's value at a row's ends: lanes 0 .. 7 those before the first whole word, 8 .. 15 those behind the last.
+    __device__ __forceinline__ unsigned edge_at(const T *p) const {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+        uintptr_t from, to;
+        words(p, from, to);
+        const unsigned lane = threadIdx.x & 31, head = min(cols, (unsigned)((from - a) / sizeof(T))), tail = max(head, (unsigned)((to - a) / sizeof(T)));
+        const unsigned i = lane < 8 ? lane : tail + lane - 8;
+        return (lane < 8 ? i < head : lane < 16 && i < cols) ? i : 0xffffffffu;
+    }
+    __device__ __forceinline__ void put_edges(unsigned row, unsigned stage, int k = 0) {
+        if (VEC) return;
+#pragma unroll
+        for (int a = 0; a < IN; ++a) {
+            if (!g.in[a].p) continue;
+            const unsigned i = edge_at(source(a, row)), lane = threadIdx.x & 31;
+            T *const p = const_cast<T *>(at(a, row, stage));
+            if (i != 0xffffffffu) p[i] = edge[k][VEC ? 0 : a];
+            // a row that began further on may have ended here before
+            const unsigned z = cols + lane - 16;
+            if (lane >= 16 && lane - 16 < 16 / sizeof(T) - 1 && z < (g.array_bytes - 16) / sizeof(T)) p[z] = from_f32<T>(0.f);
+        }
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + 8 * stage) : "memory");
+    }
+    __device__ __forceinline__ void issue(unsigned row, unsigned stage, int k = 0) {
+        if (!VEC) {
+#pragma unroll
+            for (int a = 0; a < IN; ++a) {
+                if (!g.in[a].p) continue;
+                const T *p = source(a, row);
+                const unsigned i = edge_at(p);
+                if (i != 0xffffffffu) edge[k][VEC ? 0 : a] = p[i];
+            }
+        }
+        if ((threadIdx.x & 31) == 0) {
+            const uint32_t bar = full + 8 * stage;
+            unsigned bytes = 0;
+            uintptr_t from, to;
+#pragma unroll
+            for (int a = 0; a < IN; ++a)
+                if (g.in[a].p) {
+                    words(source(a, row), from, to);
+                    bytes += (unsigned)(to - from);
+                }
+            mbar_expect(bar, bytes);
+#pragma unroll
+            for (int a = 0; a < IN; ++a) {
+                if (!g.in[a].p) continue;
+                const T *p = source(a, row);
+                words(p, from, to);
+                if (to == from) continue;
+                const uint32_t dst = smem_addr(at(a, row, stage)) + (uint32_t)(from - reinterpret_cast<uintptr_t>(p));
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from),
+                             "r"((unsigned)(to - from)), "r"(bar)
+                             : "memory");
+            }
+        }
+        __syncwarp();
+    }
+};
+
+__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, unsigned *error) {
+    const unsigned long long until = now_ns() + kWaitNs;
+    for (unsigned i = 1;; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if ((i & 255u) == 0 && now_ns() > until) {
+            atomicExch(error, 1u);
+            return false;
         }
     }
 }
 
-// What is known of some values of a row: how many, their mean, their squared deviations from it (RMS: their squares), and for
-// backward the sums of g and of g times the deviation (RMS: of g times the value).
-struct Stat {
-    float n, mean, m2, g, gv;
+// Sums over a row, K at a time.  Within a warp the lanes halve what they carry at every exchange, until each has one of the K sums
+// of some lanes (three values: 5 exchanges, not 15).  Warps leave theirs in one half of `slot` (of every CTA of the cluster), and every
+// warp adds them up in the same order.  The halves alternate: one is written again only when all warps have arrived at the reduction
+// between, and a warp arrives there after it has read.  A wait that gave up (`ok`) is not repeated: the loops go on without waiting and
+// end.
+struct Shared {
+    unsigned long long full[kMostStages], red[2];
 };
-template <bool LAYER, bool GRAD> __device__ __forceinline__ Stat merge(const Stat &a, const Stat &b) {
-    Stat s;
-    if (!LAYER) {
-        s.n = s.mean = s.g = 0.f;
-        s.m2 = a.m2 + b.m2;
-        s.gv = GRAD ? a.gv + b.gv : 0.f;
-        return s;
+template <int kWarps> struct Sums {  // kWarps: of a CTA at most
+    Shared *sh;
+    float *slot;  // [2][8][warps of the cluster]
+    unsigned half, phase, cluster;
+    unsigned *error;
+    bool ok;
+
+    template <int K> __device__ __forceinline__ void add(float (&v)[K]) {
+        constexpr int P = K == 1 ? 1 : K == 2 ? 2 : K <= 4 ? 4 : 8, kLanes = 32 / P;  // lanes that end up with the same sum
+        const unsigned lane = threadIdx.x & 31, warp = threadIdx.x / 32, warps = blockDim.x / 32;
+        float w[P];
+#pragma unroll
+        for (int k = 0; k < P; ++k) w[k] = k < K ? v[k < K ? k : 0] : 0.f;
+#pragma unroll
+        for (int o = 16, n = P / 2; o >= kLanes; o >>= 1, n >>= 1) {
+#pragma unroll
+            for (int k = 0; k < P / 2; ++k) {
+                if (k >= n) continue;
+                const float keep = lane & o ? w[k + n] : w[k], give = lane & o ? w[k] : w[k + n];
+                w[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+        }
+        float x = w[0];
+#pragma unroll
+        for (int o = kLanes / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        if (blockDim.x * cluster == 32) {
+            __syncwarp();
+        } else {
+            float *at = slot + (half * 8 + lane / kLanes) * (warps * cluster);
+            const unsigned sub = lane % kLanes;
+            if (cluster == 1) {
+                if (sub == 0) at[warp] = x;
+                __syncthreads();
+                x = 0.f;
+                constexpr int kOver = kWarps < kLanes ? kWarps : kLanes;  // lanes that share a sum's warps; the others do the same again
+#pragma unroll
+                for (int e = 0; e < kWarps; e += kOver) {
+                    const unsigned i = e + sub % kOver;
+                    x += i < warps ? at[i] : 0.f;
+                }
+#pragma unroll
+                for (int o = kOver / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+            } else {
+                if (sub == 0) {
+                    const uint32_t here = smem_addr(at + cluster_rank() * warps + warp);
+                    for (unsigned c = 0; c < cluster; ++c)
+                        asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, %1;\n st.shared::cluster.f32 [a], %2;\n}\n" ::"r"(here), "r"(c), "f"(x) : "memory");
+                }
+                __syncwarp();
+                if (lane < cluster)
+                    asm volatile("{\n .reg .b32 b;\n mapa.shared::cluster.u32 b, %0, %1;\n mbarrier.arrive.release.cluster.shared::cluster.b64 _, [b];\n}\n" ::"r"(
+                                     smem_addr(sh->red + half)),
+                                 "r"(lane)
+                                 : "memory");
+                if (ok) ok = wait_cluster(smem_addr(sh->red + half), phase >> half & 1u, error);
+                __syncwarp();
+                phase ^= 1u << half;
+                x = 0.f;
+                for (unsigned i = sub; i < warps * cluster; i += kLanes) x += at[i];
+#pragma unroll
+                for (int o = kLanes / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+            }
+            half ^= 1;
+        }
+        if (K == 1) {
+            v[0] = x;
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] = __shfl_sync(0xffffffffu, x, k * kLanes);
+        }
     }
-    s.n = a.n + b.n;
-    const float inv = s.n > 0.f ? __frcp_rn(s.n) : 0.f, d = a.mean - b.mean;
-    s.mean = (a.n * a.mean + b.n * b.mean) * inv;
-    s.m2 = (a.m2 + b.m2) + d * d * (a.n * b.n * inv);
-    s.g = GRAD ? a.g + b.g : 0.f;
-    // a's deviations are from a's mean: from the common one they are larger by a.mean - s.mean = d b.n / n
-    s.gv = GRAD ? (a.gv + b.gv) + (a.g * (d * (b.n * inv)) - b.g * (d * (a.n * inv))) : 0.f;
-    return s;
+};
+
+// Barriers, and zeros in the ring, before any copy.
+template <bool VEC, typename T> __device__ __forceinline__ void start(const NormArgs<T> &g, Shared &sh, uint8_t *smem) {
+    for (unsigned i = threadIdx.x; i < g.stages * g.stage_bytes / 16; i += blockDim.x) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    if (threadIdx.x == 0) {
+        for (unsigned i = 0; i < g.stages; ++i) mbar_init(smem_addr(sh.full + i), VEC ? 1 : 2);
+        for (int i = 0; i < 2; ++i) mbar_init(smem_addr(sh.red + i), g.cluster * (blockDim.x / 32));
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (g.cluster > 1) cluster_sync_all();
+    else __syncthreads();
 }
-template <bool LAYER, bool GRAD> __device__ __forceinline__ Stat other(const Stat &a, int o) {
-    Stat s{0.f, 0.f, 0.f, 0.f, 0.f};
-    s.m2 = __shfl_xor_sync(0xffffffffu, a.m2, o);
+
+// 1 / sqrt(q / dim + eps)
+__device__ __forceinline__ float deviation(float q, float inv_dim, float eps) { return rsqrtf(fmaf(q, inv_dim, eps)); }
+
+template <typename T, bool LAYER, bool VEC>
+__global__ void __launch_bounds__(threads_of(kForwardValues), 2) k_resnorm_forward(const __grid_constant__ NormArgs<T> g) {
+    constexpr int N = kForwardValues;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(16) Shared sh;
+    const unsigned rank = g.cluster > 1 ? cluster_rank() : 0u, first = blockIdx.x / g.cluster, step = gridDim.x / g.cluster;
+    const unsigned col0 = rank * g.span, cols = min(g.span, g.dim - col0), warp = threadIdx.x / 32;
+    start<VEC>(g, sh, smem);
+    Ring<T, VEC, kForwardIn, 1> ring{g, smem, smem_addr(sh.full), col0, cols};
+    Sums<threads_of(N) / 32> sums{&sh, reinterpret_cast<float *>(smem + g.slot_off), 0u, 0u, g.cluster, g.error, true};
+    if (warp == 0)
+        for (unsigned i = 0; i < g.stages && first + i * step < g.rows; ++i) {
+            ring.issue(first + i * step, i);
+            ring.put_edges(first + i * step, i);
+        }
+    Row<T, N> w_post, b_post, w_pre, b_pre;
+    load_vector<VEC>(w_post, g.w_post, cols, col0, 1.f);
+    load_vector<VEC>(w_pre, g.w_pre, cols, col0, 1.f);
     if (LAYER) {
-        s.n = __shfl_xor_sync(0xffffffffu, a.n, o);
-        s.mean = __shfl_xor_sync(0xffffffffu, a.mean, o);
+        load_vector<VEC>(b_post, g.b_post, cols, col0, 0.f);
+        load_vector<VEC>(b_pre, g.b_pre, cols, col0, 0.f);
     }
-    if (GRAD) s.gv = __shfl_xor_sync(0xffffffffu, a.gv, o);
-    if (GRAD && LAYER) s.g = __shfl_xor_sync(0xffffffffu, a.g, o);
-    return s;
-}
-// Of N sets over the CTA, the same bits in every thread (merging is symmetric).  `sh` holds two halves of 32 * N that alternate
-// from one reduction to the next: a half is written again only behind the barrier of the reduction between.
-template <bool LAYER, bool GRAD, int N> __device__ __forceinline__ void cta_stats(Stat (&s)[N], Stat *sh, unsigned &half) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) s[k] = merge<LAYER, GRAD>(s[k], other<LAYER, GRAD>(s[k], o));
-    }
-    if (blockDim.x == 32) return;
-    Stat *at = sh + half * 32 * N;
-    half ^= 1;
-    const unsigned warps = blockDim.x / 32, lane = threadIdx.x & 31;
-    if (lane == 0) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) at[k * 32 + threadIdx.x / 32] = s[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) s[k] = lane < warps ? at[k * 32 + lane] : Stat{0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {  // of 16 warps at most: the first step adds nothing
-        if (o >= (int)warps) continue;
-#pragma unroll
-        for (int k = 0; k < N; ++k) s[k] = merge<LAYER, GRAD>(s[k], other<LAYER, GRAD>(s[k], o));
-    }
-    // lanes beyond the largest power of two that holds the warps have merged nothing but zeros
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        s[k].n = __shfl_sync(0xffffffffu, s[k].n, 0);
-        s[k].mean = __shfl_sync(0xffffffffu, s[k].mean, 0);
-        s[k].m2 = __shfl_sync(0xffffffffu, s[k].m2, 0);
-        s[k].g = __shfl_sync(0xffffffffu, s[k].g, 0);
-        s[k].gv = __shfl_sync(0xffffffffu, s[k].gv, 0);
-    }
-}
-
-// A thread's own values.
-template <bool LAYER, bool VEC, int N> __device__ __forceinline__ Stat stat_of(const float (&v)[N], unsigned dim) {
-    Stat s{0.f, 0.f, 0.f, 0.f, 0.f};
-    if (!LAYER) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s.m2 = fmaf(v[i], v[i], s.m2);
-        return s;
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {  // what lies behind the row is zero
-        s.n += col_of<VEC>(i) < dim ? 1.f : 0.f;
-        sum += v[i];
-    }
-    s.mean = s.n > 0.f ? sum / s.n : 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float d = col_of<VEC>(i) < dim ? v[i] - s.mean : 0.f;
-        s.m2 = fmaf(d, d, s.m2);
-    }
-    return s;
-}
-__device__ __forceinline__ float deviation_inv(const Stat &s, float dim, float eps) { return rsqrtf(s.m2 / dim + eps); }
-
-template <typename T, bool LAYER, bool VEC, int NC>
-__global__ void __launch_bounds__(kMostThreads) k_resnorm_forward(const __grid_constant__ NormArgs<T> g) {
-    constexpr int N = 8 * NC;
-    __shared__ Stat sh[64];
-    unsigned half = 0;
-    for (unsigned row = blockIdx.x; row < g.rows; row += gridDim.x) {
-        Row<T, NC> rx, rf, rg, out;
-        load_row<VEC>(rx, g.x + row * g.x_pitch, g.dim);
-        float y[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) y[i] = to_f32(rx.v[i]);
-        if (g.f) {
-            load_row<VEC>(rf, g.f + row * g.f_pitch, g.dim);
-            if (g.gate) load_row<VEC>(rg, g.gate + row / g.per_gate * g.gate_pitch, g.dim);
-            float u[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) u[i] = to_f32(rf.v[i]);
+    const float inv_dim = 1.f / (float)g.dim;
+    unsigned stage = 0, parity = 0, edges = kNoStage, edge_row = 0;
+    for (unsigned row = first; row < g.rows; row += step) {
+        if (sums.ok) sums.ok = mbar_wait(smem_addr(sh.full + stage), parity, g.error);
+        __syncwarp();
+        // v becomes its deviation from the mean, the result is 1 / its deviation as a whole
+        const auto normalise = [&](float2 (&v)[N / 2], auto between) {
+            float s[1];
+            if (LAYER) {
+                s[0] = total(v);
+                sums.add(s);
+                between();
+                shift_row<VEC, T, N>(v, -s[0] * inv_dim, cols);
+            }
+            s[0] = dot(v, v);
+            sums.add(s);
+            if (!LAYER) between();
+            return deviation(s[0], inv_dim, g.eps);
+        };
+        float2 y[N / 2];
+        fetch_row<VEC, T, N>(y, ring.at(kX, row, stage));
+        if (g.has_f) {
+            float2 u[N / 2], a[N / 2];
+            fetch_row<VEC, T, N>(u, ring.at(kF, row, stage));
             if (g.post) {
-                Row<T, NC> w, b;
-                if (g.w_post) load_row<VEC>(w, g.w_post, g.dim);
-                if (LAYER && g.b_post) load_row<VEC>(b, g.b_post, g.dim);
-                Stat s[1] = {stat_of<LAYER, VEC>(u, g.dim)};
-                cta_stats<LAYER, false>(s, sh, half);
-                const float r = deviation_inv(s[0], (float)g.dim, g.eps);
+                const float2 r = both(normalise(u, []() {}));
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    u[i] = (u[i] - (LAYER ? s[0].mean : 0.f)) * r;
-                    if (g.w_post) u[i] *= to_f32(w.v[i]);
-                    if (LAYER && g.b_post) u[i] += to_f32(b.v[i]);
+                for (int i = 0; i < N / 2; ++i) {
+                    u[i] = mul2(mul2(u[i], r), Two<T>::get(w_post.v + 2 * i));
+                    if (LAYER) u[i] = add2(u[i], Two<T>::get(b_post.v + 2 * i));
                 }
             }
+            const float2 scale = both(g.scale);
+            if (g.has_gate) {
+                fetch_row<VEC, T, N>(a, ring.at(kGate, row, stage));
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = fmaf(g.gate ? g.scale * to_f32(rg.v[i]) : g.scale, u[i], y[i]);
-        }
+                for (int i = 0; i < N / 2; ++i) y[i] = fma2(mul2(a[i], scale), u[i], y[i]);
+            } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            out.v[i] = from_f32<T>(y[i]);
-            y[i] = to_f32(out.v[i]);  // the norm is that of the values handed on: backward has them and nothing else
+                for (int i = 0; i < N / 2; ++i) y[i] = fma2(scale, u[i], y[i]);
+            }
         }
-        if (g.y) store_row<VEC>(g.y + row * g.y_pitch, out, g.dim);
-        if (!g.pre) continue;
-        Row<T, NC> w, b;
-        if (g.w_pre) load_row<VEC>(w, g.w_pre, g.dim);
-        if (LAYER && g.b_pre) load_row<VEC>(b, g.b_pre, g.dim);
-        if (LAYER) {
+        // Called once the CTA is done with the stage: it takes a row further on.
+        const auto refill = [&]() {
+            if (warp != 0) return;
+            if (!VEC && edges != kNoStage) ring.put_edges(edge_row, edges);
+            edges = kNoStage;
+            const unsigned long long next = row + (unsigned long long)g.stages * step;
+            if (next < g.rows && sums.ok) {
+                ring.issue((unsigned)next, stage);
+                edges = stage;
+                edge_row = (unsigned)next;
+            }
+        };
+        Row<T, N> out;
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = col_of<VEC>(i) < g.dim ? y[i] : 0.f;  // b_post stands nowhere behind the row
+        for (int i = 0; i < N / 2; ++i) {
+            Two<T>::put(out.v + 2 * i, y[i]);
+            y[i] = Two<T>::get(out.v + 2 * i);  // the norm is that of the values handed on: backward has them and nothing else
         }
-        Stat s[1] = {stat_of<LAYER, VEC>(y, g.dim)};
-        cta_stats<LAYER, false>(s, sh, half);
-        const float r = deviation_inv(s[0], (float)g.dim, g.eps);
+        if (g.y) store_row<VEC>(g.y + row * g.y_pitch + col0, out, cols);
+        if (g.pre) {
+            const float2 r = both(normalise(y, refill));  // y is zero behind the row, where x, f and the weights are
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float v = (y[i] - (LAYER ? s[0].mean : 0.f)) * r;
-            if (g.w_pre) v *= to_f32(w.v[i]);
-            if (LAYER && g.b_pre) v += to_f32(b.v[i]);
-            out.v[i] = from_f32<T>(v);
+            for (int i = 0; i < N / 2; ++i) {
+                y[i] = mul2(mul2(y[i], r), Two<T>::get(w_pre.v + 2 * i));
+                if (LAYER) y[i] = add2(y[i], Two<T>::get(b_pre.v + 2 * i));
+            }
+            write_row<VEC, T, N>(g.n + row * g.n_pitch + col0, y, cols);
+        } else {
+            __syncthreads();
+            refill();
         }
-        store_row<VEC>(g.n + row * g.n_pitch, out, g.dim);
+        if (++stage == g.stages) {
+            stage = 0;
+            parity ^= 1;
+        }
     }
+    if (!sums.ok)  // let copies in flight end before their memory is given back
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
-// Two plain sums over the CTA.
-__device__ __forceinline__ float2 cta_sums(float2 v, float2 *sh, unsigned &half) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-    }
-    if (blockDim.x == 32) return v;
-    float2 *at = sh + half * 32;
-    half ^= 1;
-    const unsigned warps = blockDim.x / 32, lane = threadIdx.x & 31;
-    if (lane == 0) at[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = lane < warps ? at[lane] : make_float2(0.f, 0.f);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-    }
-    return v;
-}
-
-template <bool VEC, int N> __device__ __forceinline__ void put_part(float *p, const float (&v)[N], unsigned dim) {
+template <bool VEC, typename T, int N> __device__ __forceinline__ void put_part(float *p, const float2 (&v)[N / 2], unsigned cols) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (col_of<VEC>(i) < dim) p[col_of<VEC>(i)] = v[i];
+        if (col_of<VEC, T>(i) < cols) p[col_of<VEC, T>(i)] = i & 1 ? v[i / 2].y : v[i / 2].x;
 }
 
-template <typename T, bool LAYER, bool VEC, int NC>
-__global__ void __launch_bounds__(kMostThreads, 1) k_resnorm_backward(const __grid_constant__ NormArgs<T> g) {
-    constexpr int N = 8 * NC;
-    __shared__ Stat sh[128];
-    __shared__ float2 sh2[64];
-    unsigned half = 0, half2 = 0;
-    const unsigned r0 = blockIdx.x * g.per_cta, r1 = min(g.rows, r0 + g.per_cta);
-    const float dim = (float)g.dim, inv_dim = 1.f / dim;
-    const bool shared_gate = g.dgate && g.per_gate > 1;
-    float a_wpre[N] = {}, a_wpost[N] = {}, a_bpre[LAYER ? N : 1] = {}, a_bpost[LAYER ? N : 1] = {}, a_gate[N] = {};
-    Row<T, NC> w_pre, w_post, b_post;
-    if (g.pre && g.w_pre) load_row<VEC>(w_pre, g.w_pre, g.dim);
-    if (g.post && g.w_post) load_row<VEC>(w_post, g.w_post, g.dim);
-    if (LAYER && g.post && g.b_post) load_row<VEC>(b_post, g.b_post, g.dim);
-    for (unsigned row = r0; row < r1; ++row) {
-        Row<T, NC> rdy, rdn, ry, rf, rg, out;
-        if (g.x) load_row<VEC>(rdy, g.x + row * g.x_pitch, g.dim);
-        if (g.pre) {
-            load_row<VEC>(rdn, g.dn + row * g.dn_pitch, g.dim);
-            load_row<VEC>(ry, static_cast<const T *>(g.y) + row * g.y_pitch, g.dim);
+template <typename T, bool LAYER, bool VEC, bool SHARED>
+__global__ void __launch_bounds__(threads_of(back_values(LAYER)), back_ctas<T>(LAYER)) k_resnorm_backward(const __grid_constant__ NormArgs<T> g) {
+    constexpr int N = back_values(LAYER), M = N / 2, R = back_rows<T>(LAYER);
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(16) Shared sh;
+    const unsigned rank = g.cluster > 1 ? cluster_rank() : 0u, run = blockIdx.x / g.cluster, runs = gridDim.x / g.cluster;
+    const unsigned col0 = rank * g.span, cols = min(g.span, g.dim - col0), warp = threadIdx.x / 32;
+    const unsigned r0 = run * g.per_run, r1 = min(g.rows, r0 + g.per_run);
+    start<VEC>(g, sh, smem);
+    Ring<T, VEC, kBackwardIn, R> ring{g, smem, smem_addr(sh.full), col0, cols};
+    Sums<threads_of(N) / 32> sums{&sh, reinterpret_cast<float *>(smem + g.slot_off), 0u, 0u, g.cluster, g.error, true};
+    if (warp == 0)
+        for (unsigned i = 0; i < g.stages && r0 + i < r1; ++i) {
+            ring.issue(r0 + i, i);
+            ring.put_edges(r0 + i, i);
         }
-        if (g.f) {
-            load_row<VEC>(rf, g.f + row * g.f_pitch, g.dim);
-            if (g.gate) load_row<VEC>(rg, g.gate + row / g.per_gate * g.gate_pitch, g.dim);
+    const float inv_dim = 1.f / (float)g.dim;
+    const bool norm_f = g.has_f && g.post;
+    const float2 zero = both(0.f);
+    float2 a_wpre[M], a_wpost[M], a_bpre[LAYER ? M : 1], a_bpost[LAYER ? M : 1], a_gate[SHARED ? M : 1];
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        a_wpre[i] = a_wpost[i] = zero;
+        if (SHARED) a_gate[SHARED ? i : 0] = zero;
+        if (LAYER) a_bpre[LAYER ? i : 0] = a_bpost[LAYER ? i : 0] = zero;
+    }
+    // a thread's weights stay in shared memory, where it alone reads them: its registers hold the columns' sums
+    T *const w_pre = reinterpret_cast<T *>(smem + g.stages * g.stage_bytes), *const w_post = w_pre + g.array_bytes / sizeof(T);
+    T *const b_post = w_post + g.array_bytes / sizeof(T);
+    {
+        Row<T, N> w;
+        load_vector<VEC>(w, g.w_pre, cols, col0, 1.f);
+        put_row<VEC>(w_pre, w);
+        load_vector<VEC>(w, g.w_post, cols, col0, 1.f);
+        put_row<VEC>(w_post, w);
+        if (LAYER) {
+            load_vector<VEC>(w, g.b_post, cols, col0, 0.f);
+            put_row<VEC>(b_post, w);
         }
-        Stat s[2] = {{0.f, 0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f, 0.f}};
-        if (g.pre) {
-            float y[N];
+    }
+    T *dx = g.n ? g.n + r0 * g.n_pitch + col0 : nullptr, *df = g.df ? g.df + r0 * g.df_pitch + col0 : nullptr;
+    unsigned stage = 0, parity = 0, edges = 0;  // rows whose edges are on their way
+    // Called behind a barrier that the CTA reaches when it is done with the rows before: their stages take rows further on.
+    const auto refill = [&](unsigned row0) {
+        if (warp != 0 || row0 == r0) return;
+        const unsigned before = (stage ? stage : g.stages) - R;
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = to_f32(ry.v[i]);
-            s[0] = stat_of<LAYER, VEC>(y, g.dim);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float q = to_f32(rdn.v[i]) * (g.w_pre ? to_f32(w_pre.v[i]) : 1.f);
-                if (LAYER) s[0].g += q;
-                s[0].gv = fmaf(q, y[i] - (LAYER ? s[0].mean : 0.f), s[0].gv);
+        for (int k = 0; k < R; ++k)
+            if (row0 - R + k + (unsigned long long)g.stages < r1 && sums.ok) {
+                ring.issue(row0 - R + k + g.stages, before + k, k);
+                edges = k + 1;
             }
-        }
-        if (g.f && g.post) {
-            float f[N];
+    };
+    for (unsigned row0 = r0; row0 < r1; row0 += R) {
+        const unsigned mine = min((unsigned)R, r1 - row0);
+        if (!VEC && warp == 0 && edges) {  // of the rows that the last refill issued
+            const unsigned before = (stage ? stage : g.stages) - R, earlier = (before ? before : g.stages) - R;
 #pragma unroll
-            for (int i = 0; i < N; ++i) f[i] = to_f32(rf.v[i]);
-            s[1] = stat_of<LAYER, VEC>(f, g.dim);
-        }
-        if (g.pre || (g.f && g.post)) cta_stats<LAYER, true>(s, sh, half);
-        float d[N];  // dY
-#pragma unroll
-        for (int i = 0; i < N; ++i) d[i] = g.x ? to_f32(rdy.v[i]) : 0.f;
-        if (g.pre) {
-            const float r = deviation_inv(s[0], dim, g.eps), mg = LAYER ? s[0].g * inv_dim : 0.f, mgy = s[0].gv * r * inv_dim;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float dn = to_f32(rdn.v[i]), hat = (to_f32(ry.v[i]) - (LAYER ? s[0].mean : 0.f)) * r;
-                d[i] += r * (dn * (g.w_pre ? to_f32(w_pre.v[i]) : 1.f) - mg - hat * mgy);
-                if (LAYER && col_of<VEC>(i) >= g.dim) d[i] = 0.f;
-                a_wpre[i] = fmaf(dn, hat, a_wpre[i]);
-                if (LAYER) a_bpre[i] += dn;
-            }
+            for (int k = 0; k < R; ++k)
+                if (k < edges) ring.put_edges(row0 - 2 * R + g.stages + k, earlier + k, k);
+            edges = 0;
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) out.v[i] = from_f32<T>(d[i]);
-        if (g.n) store_row<VEC>(g.n + row * g.n_pitch, out, g.dim);
-        if (!g.f) continue;
-        float hat[N];  // f, normalised where there is a norm
-        const float r = g.post ? deviation_inv(s[1], dim, g.eps) : 1.f, m = g.post && LAYER ? s[1].mean : 0.f;
+        for (int k = 0; k < R; ++k)
+            if (k < mine && sums.ok) sums.ok = mbar_wait(smem_addr(sh.full + stage + k), parity, g.error);
+        __syncwarp();
+        // Minus the means of y and f; then, of their deviations y' and f' and with e = dn w_pre: sums of y'^2, e y', f'^2, e.
+        constexpr int K = LAYER ? 4 : 3;
+        float m[2 * R] = {}, q[K * R] = {};
+        if (LAYER && (g.pre || norm_f)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) hat[i] = (to_f32(rf.v[i]) - m) * r;
-        if (g.dgate) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                float u = hat[i];
-                if (g.post && g.w_post) u *= to_f32(w_post.v[i]);
-                if (LAYER && g.post && g.b_post) u += to_f32(b_post.v[i]);
-                const float e = g.scale * d[i] * u;
-                if (shared_gate) a_gate[i] += e;
-                else out.v[i] = from_f32<T>(e);
-            }
-            const unsigned gate = row / g.per_gate;
-            if (!shared_gate) {
-                store_row<VEC>(g.dgate + row * g.dgate_pitch, out, g.dim);
-            } else if (row + 1 == r1 || row + 1 == (gate + 1) * g.per_gate) {
-                const unsigned first = gate * g.per_gate, end = g.rows - first > g.per_gate ? first + g.per_gate : g.rows;
-                if (first >= r0 && end <= r1) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i) out.v[i] = from_f32<T>(a_gate[i]);
-                    store_row<VEC>(g.dgate + gate * g.dgate_pitch, out, g.dim);
-                } else {
-                    put_part<VEC>(g.part_gate + (blockIdx.x * 2ull + (first < r0 ? 0 : 1)) * g.dim, a_gate, g.dim);
+            for (int k = 0; k < R; ++k) {
+                if (k >= mine) continue;
+                float2 v[M];
+                if (g.pre) {
+                    fetch_row<VEC, T, N>(v, ring.at(kY, row0 + k, stage + k));
+                    m[2 * k] = total(v);
                 }
+                if (norm_f) {
+                    fetch_row<VEC, T, N>(v, ring.at(kBackF, row0 + k, stage + k));
+                    m[2 * k + 1] = total(v);
+                }
+            }
+            sums.add(m);
 #pragma unroll
-                for (int i = 0; i < N; ++i) a_gate[i] = 0.f;
+            for (int k = 0; k < 2 * R; ++k) m[k] *= -inv_dim;
+        }
+        if (g.pre || norm_f) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (k >= mine) continue;
+                if (g.pre) {
+                    float2 y[M], e[M];
+                    Row<T, N> w;
+                    take_row<VEC>(w, w_pre);
+                    fetch_row<VEC, T, N>(y, ring.at(kY, row0 + k, stage + k));
+                    fetch_row<VEC, T, N>(e, ring.at(kDn, row0 + k, stage + k));
+                    if (LAYER) shift_row<VEC, T, N>(y, m[2 * k], cols);
+#pragma unroll
+                    for (int i = 0; i < M; ++i) e[i] = mul2(e[i], Two<T>::get(w.v + 2 * i));
+                    if (LAYER) q[K * k + K - 1] = total(e);
+                    q[K * k] = dot(y, y);
+                    q[K * k + 1] = dot(e, y);
+                }
+                if (norm_f) {
+                    float2 f[M];
+                    fetch_row<VEC, T, N>(f, ring.at(kBackF, row0 + k, stage + k));
+                    if (LAYER) shift_row<VEC, T, N>(f, m[2 * k + 1], cols);
+                    q[K * k + 2] = dot(f, f);
+                }
+            }
+            sums.add(q);
+        } else {
+            __syncthreads();
+        }
+        refill(row0);
+        // With r = 1 / deviation of y, rf of f and t = r dn:  dY = dy + w_pre t - r mean e - y' r^3 mean(e y'),  dw_pre += t y'
+        //   t2 = scale rf dY:  dgate = t2 w_post f' + scale dY b_post,  h = t2 gate (the gradient of f^ times rf, without w_post)
+        //   dw_post += h f',  df = h w - mean(h w) - f' rf^2 mean(h w f')
+        float2 d[R][M];  // dY, then h w
+        float h[(LAYER ? 2 : 1) * R] = {};
+        constexpr int H = LAYER ? 2 : 1;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if (k >= mine) continue;
+            const unsigned row = row0 + k, st = stage + k;
+            if (g.in[kDy].p) {
+                fetch_row<VEC, T, N>(d[k], ring.at(kDy, row, st));
+            } else {
+#pragma unroll
+                for (int i = 0; i < M; ++i) d[k][i] = zero;
+            }
+            if (g.pre) {
+                float2 y[M], e[M];
+                Row<T, N> w;
+                take_row<VEC>(w, w_pre);
+                fetch_row<VEC, T, N>(y, ring.at(kY, row, st));
+                fetch_row<VEC, T, N>(e, ring.at(kDn, row, st));
+                if (LAYER) shift_row<VEC, T, N>(y, m[2 * k], cols);
+                const float r = deviation(q[K * k], inv_dim, g.eps);
+                const float2 rr = both(r), c = both(-(r * r) * (r * q[K * k + 1] * inv_dim));
+                if (LAYER) shift_row<VEC, T, N>(d[k], -r * q[K * k + K - 1] * inv_dim, cols);
+#pragma unroll
+                for (int i = 0; i < M; ++i) {
+                    if (LAYER) a_bpre[LAYER ? i : 0] = add2(a_bpre[LAYER ? i : 0], e[i]);
+                    const float2 t = mul2(e[i], rr);
+                    d[k][i] = fma2(y[i], c, fma2(t, Two<T>::get(w.v + 2 * i), d[k][i]));
+                    a_wpre[i] = fma2(t, y[i], a_wpre[i]);
+                }
+            }
+            if (dx) {
+                write_row<VEC, T, N>(dx, d[k], cols);
+                dx += g.n_pitch;
+            }
+            if (!g.has_f) continue;
+            const float rf = norm_f ? deviation(q[K * k + 2], inv_dim, g.eps) : 1.f;
+            float2 f[M], a[M];
+            Row<T, N> w, out;
+            take_row<VEC>(w, w_post);
+            fetch_row<VEC, T, N>(f, ring.at(kBackF, row, st));
+            if (LAYER) shift_row<VEC, T, N>(f, m[2 * k + 1], cols);
+            if (g.has_gate) {
+                fetch_row<VEC, T, N>(a, ring.at(kBackGate, row, st));
+            } else {
+#pragma unroll
+                for (int i = 0; i < M; ++i) a[i] = both(1.f);
+            }
+            const float2 scale = both(LAYER ? g.scale : g.scale * rf), rr = both(rf);
+            Row<T, N> b;
+            if (LAYER) take_row<VEC>(b, b_post);
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                float2 t = mul2(d[k][i], scale);
+                const float2 ww = Two<T>::get(w.v + 2 * i);
+                float2 e = zero;
+                if (LAYER) {
+                    e = mul2(t, Two<T>::get(b.v + 2 * i));
+                    a_bpost[LAYER ? i : 0] = fma2(t, a[i], a_bpost[LAYER ? i : 0]);
+                    t = mul2(t, rr);
+                }
+                if (SHARED || g.dgate) {
+                    const float2 fw = mul2(f[i], ww);
+                    e = LAYER ? fma2(t, fw, e) : mul2(t, fw);
+                    if (SHARED) a_gate[SHARED ? i : 0] = add2(a_gate[SHARED ? i : 0], e);
+                    else Two<T>::put(out.v + 2 * i, e);
+                }
+                t = mul2(t, a[i]);
+                a_wpost[i] = fma2(t, f[i], a_wpost[i]);
+                d[k][i] = mul2(t, ww);
+            }
+            if constexpr (SHARED) {
+                const unsigned gate = row / g.per_gate, begin = gate * g.per_gate, end = g.rows - begin > g.per_gate ? begin + g.per_gate : g.rows;
+                if (row + 1 == r1 || row + 1 == end) {
+                    if (begin >= r0 && end <= r1) write_row<VEC, T, N>(g.dgate + gate * g.dgate_pitch + col0, a_gate, cols);
+                    else put_part<VEC, T, N>(g.part_gate + (run * 2ull + (begin < r0 ? 0 : 1)) * g.dim + col0, a_gate, cols);
+#pragma unroll
+                    for (int i = 0; i < M; ++i) a_gate[i] = zero;
+                }
+            } else if (g.dgate) {
+                store_row<VEC>(g.dgate + row * g.dgate_pitch + col0, out, cols);
+            }
+            if (norm_f) {
+                h[H * k] = dot(d[k], f);
+                if (LAYER) h[H * k + H - 1] = total(d[k]);
             }
         }
+        if (norm_f) sums.add(h);
+        if (df) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) d[i] *= g.gate ? g.scale * to_f32(rg.v[i]) : g.scale;  // du
-        if (g.post) {
-            float2 sum = make_float2(0.f, 0.f);
+            for (int k = 0; k < R; ++k) {
+                if (k >= mine) continue;
+                if (norm_f) {
+                    float2 f[M];
+                    fetch_row<VEC, T, N>(f, ring.at(kBackF, row0 + k, stage + k));
+                    if (LAYER) {
+                        shift_row<VEC, T, N>(f, m[2 * k + 1], cols);
+                        shift_row<VEC, T, N>(d[k], -h[H * k + H - 1] * inv_dim, cols);
+                    }
+                    const float rf = deviation(q[K * k + 2], inv_dim, g.eps);
+                    const float2 c = both(-(rf * rf) * (h[H * k] * inv_dim));
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                a_wpost[i] = fmaf(d[i], hat[i], a_wpost[i]);
-                if (LAYER) a_bpost[i] += d[i];
-                if (g.w_post) d[i] *= to_f32(w_post.v[i]);
-                // behind the row d is zero, and hat may not be
-                if (LAYER) sum.x += d[i];
-                sum.y = fmaf(d[i], hat[i], sum.y);
+                    for (int i = 0; i < M; ++i) d[k][i] = fma2(f[i], c, d[k][i]);
+                }
+                write_row<VEC, T, N>(df, d[k], cols);
+                df += g.df_pitch;
             }
-            sum = cta_sums(sum, sh2, half2);
-            const float mh = LAYER ? sum.x * inv_dim : 0.f, mhf = sum.y * inv_dim;
-#pragma unroll
-            for (int i = 0; i < N; ++i) d[i] = r * (d[i] - mh - hat[i] * mhf);
         }
-        if (g.df) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) out.v[i] = from_f32<T>(d[i]);
-            store_row<VEC>(g.df + row * g.df_pitch, out, g.dim);
+        stage += R;
+        if (stage == g.stages) {
+            stage = 0;
+            parity ^= 1;
         }
     }
-    const unsigned long long each = (unsigned long long)gridDim.x * g.dim, mine = (unsigned long long)blockIdx.x * g.dim;
-    if (g.dw_pre) put_part<VEC>(g.part + mine, a_wpre, g.dim);
-    if (g.dw_post) put_part<VEC>(g.part + each + mine, a_wpost, g.dim);
+    const unsigned long long each = (unsigned long long)runs * g.dim, mine = (unsigned long long)run * g.dim + col0;
+    if (g.dw_pre) put_part<VEC, T, N>(g.part + mine, a_wpre, cols);
+    if (g.dw_post) put_part<VEC, T, N>(g.part + each + mine, a_wpost, cols);
     if constexpr (LAYER) {
-        if (g.db_pre) put_part<VEC>(g.part + 2 * each + mine, a_bpre, g.dim);
-        if (g.db_post) put_part<VEC>(g.part + 3 * each + mine, a_bpost, g.dim);
+        if (g.db_pre) put_part<VEC, T, N>(g.part + 2 * each + mine, a_bpre, cols);
+        if (g.db_post) put_part<VEC, T, N>(g.part + 3 * each + mine, a_bpost, cols);
     }
+    if (!sums.ok)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
-// Adds the CTAs' sums, 32 columns a CTA, 32 walkers over the rows of the list, in an order that depends on the sizes alone.
-// blockIdx.y 0 .. 3: the vectors; 4 + c: the gate that the last row of CTA c has, where it begins in c and ends behind it.
-template <typename T> __global__ void __launch_bounds__(1024) k_resnorm_join(const __grid_constant__ NormArgs<T> g, unsigned ctas) {
-    __shared__ float sh[32][33];
-    const unsigned col = blockIdx.x * 32 + (threadIdx.x & 31), walker = threadIdx.x >> 5;
-    T *out;
-    const float *from;
-    unsigned long long step = g.dim;
-    unsigned n = ctas;
-    if (blockIdx.y < 4) {
-        T *const to[4] = {g.dw_pre, g.dw_post, g.db_pre, g.db_post};
-        out = to[blockIdx.y];
-        from = g.part + blockIdx.y * (unsigned long long)ctas * g.dim;
-        if (!out) return;
-    } else {
-        const unsigned c = blockIdx.y - 4, r0 = c * g.per_cta, r1 = min(g.rows, r0 + g.per_cta);
-        const unsigned gate = (r1 - 1) / g.per_gate, first = gate * g.per_gate;
-        const unsigned end = g.rows - first > g.per_gate ? first + g.per_gate : g.rows;
-        if (first < r0 || end <= r1) return;
-        out = g.dgate + gate * g.dgate_pitch;
-        n = (end - 1) / g.per_cta - c + 1;
-        from = g.part_gate + c * 2ull * g.dim;  // the first of its parts is the CTA's second, the others' their first
-        step = 2ull * g.dim;
-    }
-    float v = 0.f;
-    if (col < g.dim)
-        for (unsigned k = walker; k < n; k += 32) v += from[k * step + (blockIdx.y >= 4 && k == 0 ? g.dim : 0u) + col];
-    sh[walker][threadIdx.x & 31] = v;
-    __syncthreads();
-    if (walker == 0 && col < g.dim) {
-        v = 0.f;
+// Adds the runs' sums, 32 columns a CTA, eight walkers over the rows of the list, in an order that depends on the sizes alone.
+// blockIdx.y 0 .. 3: the vectors; the others take turns at the runs c: the gate that the last row of c has, where it begins in c and
+// ends behind it.
+constexpr unsigned kJoinGates = 32;
+template <typename T> __global__ void __launch_bounds__(256) k_resnorm_join(const __grid_constant__ NormArgs<T> g, unsigned runs) {
+    __shared__ float sh[8][32];
+    const unsigned lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane, walker = threadIdx.x >> 5;
+    // rows of `from`, `step` apart; the first lies `skip` further on
+    const auto join = [&](const float *from, unsigned long long step, unsigned n, unsigned skip, T *out) {
+        float v = 0.f;
+        if (col < g.dim) {
+#pragma unroll 4
+            for (unsigned k = walker; k < n; k += 8) v += from[k * step + (k == 0 ? skip : 0u) + col];
+        }
+        sh[walker][lane] = v;
+        __syncthreads();
+        if (walker == 0 && col < g.dim) {
+            v = 0.f;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v += sh[k][threadIdx.x];
-        out[col] = from_f32<T>(v);
+            for (int k = 0; k < 8; ++k) v += sh[k][lane];
+            out[col] = from_f32<T>(v);
+        }
+        __syncthreads();
+    };
+    if (blockIdx.y < 4) {
+        T *const out = blockIdx.y == 0 ? g.dw_pre : blockIdx.y == 1 ? g.dw_post : blockIdx.y == 2 ? g.db_pre : g.db_post;
+        if (out) join(g.part + blockIdx.y * (unsigned long long)runs * g.dim, g.dim, runs, 0u, out);
+        return;
+    }
+    for (unsigned c = blockIdx.y - 4; c < runs; c += gridDim.y - 4) {
+        const unsigned r0 = c * g.per_run, r1 = min(g.rows, r0 + g.per_run), gate = (r1 - 1) / g.per_gate, first = gate * g.per_gate;
+        const unsigned end = g.rows - first > g.per_gate ? first + g.per_gate : g.rows;
+        if (first < r0 || end <= r1) continue;
+        // the first of its parts is the run's second, the others' their first
+        join(g.part_gate + c * 2ull * g.dim, 2ull * g.dim, (end - 1) / g.per_run - c + 1, g.dim, g.dgate + gate * g.dgate_pitch);
     }
 }
 
@@ -456,61 +769,117 @@ struct scar_resnorm {
     int device = 0;
     cudaStream_t stream = nullptr;
     scar_resnorm_config cfg{};
-    unsigned sms = 148, threads = 32, rounds = 1;  // threads of a row's CTA, groups of eight values each has
-    unsigned back_ctas = 1;                        // most CTAs of backward
-    float *part = nullptr;
+    unsigned sms = 148, cluster = 1, span = 8, forward_threads = 32, back_threads = 32;
+    unsigned forward_fit = 1, back_fit = 1;  // CTAs of an SM
+    unsigned most_runs = 1;    // of backward
+    float *part = nullptr;     // [6][most_runs][dim]
+    unsigned *error = nullptr; // a wait gave up; cleared when its report has been read
     uint64_t launches = 0;
+    bool arm_error = false;
 };
 
 namespace {
 
-// f(std::integral_constant<int, NC>) for the operator's rounds.
-template <typename F> void with_rounds(unsigned rounds, F &&f) {
-    if (rounds == 1) f(std::integral_constant<int, 1>());
-    else if (rounds == 2) f(std::integral_constant<int, 2>());
-    else f(std::integral_constant<int, 4>());
-}
-
 template <typename T> bool aligned16(const T *p, uint64_t pitch = 0) { return (uintptr_t)p % 16 == 0 && pitch * sizeof(T) % 16 == 0; }
 
-template <typename T> void run_forward(scar_resnorm *op, const NormArgs<T> &g) {
-    const bool vec = aligned16(g.x, g.x_pitch) && aligned16(g.f, g.f_pitch) && aligned16(g.y, g.y_pitch) && aligned16(g.n, g.n_pitch) &&
-                     aligned16(g.gate, g.gate_pitch) && aligned16(g.w_post) && aligned16(g.b_post) && aligned16(g.w_pre) && aligned16(g.b_pre);
-    const bool layer = op->cfg.kind == SCAR_RESNORM_LAYER;
-    const unsigned ctas = std::min(g.rows, op->sms * std::max(1u, 2048 / op->threads));
-    with_rounds(op->rounds, [&](auto nc) {
-        constexpr int NC = decltype(nc)::value;
-        auto kernel = layer ? (vec ? k_resnorm_forward<T, true, true, NC> : k_resnorm_forward<T, true, false, NC>)
-                            : (vec ? k_resnorm_forward<T, false, true, NC> : k_resnorm_forward<T, false, false, NC>);
-        kernel<<<ctas, op->threads, 0, op->stream>>>(g);
-    });
-    op->launches++;
+constexpr unsigned kSmemOfSm = 220 * 1024;  // left to the rings of an SM's CTAs
+
+// The ring of a kernel whose rows consist of `arrays` matrices: as many stages, between two and six, as leave room for
+// `resident` CTAs on an SM, if that is possible.
+template <typename T> void set_ring(const scar_resnorm *op, NormArgs<T> &g, unsigned arrays, unsigned vectors, unsigned at_once, unsigned threads, unsigned values, unsigned resident) {
+    g.array_bytes = (unsigned)(threads * values * sizeof(T) + 16);  // what the threads read, and up to 15 bytes before it
+    g.stage_bytes = arrays * g.array_bytes;
+    const unsigned warps = threads / 32 * g.cluster, slots = warps > 1 ? (unsigned)round_up(2 * 8 * 4 * warps, 16) : 0u;
+    const unsigned other = vectors * g.array_bytes + slots;
+    const unsigned room = kSmemOfSm / resident - (resident > 1 ? (unsigned)sizeof(Shared) + 1024u : 0u);  // 1 KiB a CTA is the system's
+    g.stages = std::max(2 * at_once, std::min(kMostStages, room > other ? (room - other) / g.stage_bytes : 0u) / at_once * at_once);
+    g.slot_off = g.stages * g.stage_bytes + vectors * g.array_bytes;
+    g.smem = g.slot_off + slots;
+    g.error = op->error;
 }
 
-template <typename T> void run_backward(scar_resnorm *op, NormArgs<T> g) {
-    const bool vec = aligned16(g.x, g.x_pitch) && aligned16(g.f, g.f_pitch) && aligned16(g.y, g.y_pitch) && aligned16(g.n, g.n_pitch) &&
-                     aligned16(g.dn, g.dn_pitch) && aligned16(g.df, g.df_pitch) && aligned16(g.dgate, g.dgate_pitch) &&
-                     aligned16(g.gate, g.gate_pitch) && aligned16(g.w_post) && aligned16(g.b_post) && aligned16(g.w_pre);
-    const bool layer = op->cfg.kind == SCAR_RESNORM_LAYER;
-    unsigned ctas = 0;
-    if (g.rows) {
-        ctas = std::min(g.rows, op->back_ctas);
-        g.per_cta = (g.rows + ctas - 1) / ctas;
-        ctas = (g.rows + g.per_cta - 1) / g.per_cta;
-        g.part = op->part;
-        g.part_gate = op->part + 4ull * op->back_ctas * g.dim;
-        with_rounds(op->rounds, [&](auto nc) {
-            constexpr int NC = decltype(nc)::value;
-            auto kernel = layer ? (vec ? k_resnorm_backward<T, true, true, NC> : k_resnorm_backward<T, true, false, NC>)
-                                : (vec ? k_resnorm_backward<T, false, true, NC> : k_resnorm_backward<T, false, false, NC>);
-            kernel<<<ctas, op->threads, 0, op->stream>>>(g);
-        });
-        op->launches++;
-    }
-    const bool gates = g.dgate && g.per_gate > 1 && ctas > 1;
-    if (!g.dw_pre && !g.dw_post && !g.db_pre && !g.db_post && !gates) return;
-    k_resnorm_join<T><<<dim3((g.dim + 31) / 32, 4 + (gates ? ctas : 0)), 1024, 0, op->stream>>>(g, ctas);
+template <typename T> int launch_rows(scar_resnorm *op, void (*kernel)(NormArgs<T>), const NormArgs<T> &g, unsigned groups, unsigned threads) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = groups * g.cluster;
+    cfg.blockDim = threads;
+    cfg.dynamicSmemBytes = g.smem;
+    cfg.stream = op->stream;
+    cudaLaunchAttribute size{};
+    size.id = cudaLaunchAttributeClusterDimension;
+    size.val.clusterDim.x = g.cluster;
+    size.val.clusterDim.y = size.val.clusterDim.z = 1;
+    cfg.attrs = &size;
+    cfg.numAttrs = g.cluster > 1 ? 1 : 0;
+    TRAIN_TRY(cudaLaunchKernelEx(&cfg, kernel, g));
     op->launches++;
+    return SCAR_OK;
+}
+
+template <typename T> auto forward_kernel(bool layer, bool vec) {
+    return layer ? (vec ? k_resnorm_forward<T, true, true> : k_resnorm_forward<T, true, false>)
+                 : (vec ? k_resnorm_forward<T, false, true> : k_resnorm_forward<T, false, false>);
+}
+template <typename T> auto backward_kernel(bool layer, bool vec, bool shared) {
+    if (shared)
+        return layer ? (vec ? k_resnorm_backward<T, true, true, true> : k_resnorm_backward<T, true, false, true>)
+                     : (vec ? k_resnorm_backward<T, false, true, true> : k_resnorm_backward<T, false, false, true>);
+    return layer ? (vec ? k_resnorm_backward<T, true, true, false> : k_resnorm_backward<T, true, false, false>)
+                 : (vec ? k_resnorm_backward<T, false, true, false> : k_resnorm_backward<T, false, false, false>);
+}
+
+template <typename T> int run_forward(scar_resnorm *op, NormArgs<T> g) {
+    bool vec = g.dim * sizeof(T) % 16 == 0 && aligned16(g.y, g.y_pitch) && aligned16(g.n, g.n_pitch) && aligned16(g.w_post) && aligned16(g.b_post) &&
+               aligned16(g.w_pre) && aligned16(g.b_pre);
+    for (const In<T> &m : g.in) vec = vec && aligned16(m.p, m.pitch);
+    const bool layer = op->cfg.kind == SCAR_RESNORM_LAYER;
+    const unsigned fit = op->forward_fit;
+    set_ring(op, g, kForwardIn, 0, 1, op->forward_threads, kForwardValues, fit);
+    const unsigned groups = std::min(g.rows, std::max(1u, op->sms * fit / g.cluster));
+    return launch_rows(op, forward_kernel<T>(layer, vec), g, groups, op->forward_threads);
+}
+
+template <typename T> int run_backward(scar_resnorm *op, NormArgs<T> g) {
+    bool vec = g.dim * sizeof(T) % 16 == 0 && aligned16(g.n, g.n_pitch) && aligned16(g.df, g.df_pitch) && aligned16(g.dgate, g.dgate_pitch) &&
+               aligned16(g.w_post) && aligned16(g.b_post) && aligned16(g.w_pre);
+    for (const In<T> &m : g.in) vec = vec && aligned16(m.p, m.pitch);
+    const bool layer = op->cfg.kind == SCAR_RESNORM_LAYER;
+    unsigned runs = 0;
+    if (g.rows) {
+        runs = std::min(g.rows, op->most_runs);
+        g.per_run = (g.rows + runs - 1) / runs;
+        runs = (g.rows + g.per_run - 1) / g.per_run;
+        g.part = op->part;
+        g.part_gate = op->part + 4ull * op->most_runs * g.dim;
+        set_ring(op, g, kBackwardIn, layer ? 3 : 2, back_rows<T>(layer), op->back_threads, back_values(layer), op->back_fit);
+        const bool shared = g.dgate && g.per_gate > 1;
+        const int rc = launch_rows(op, backward_kernel<T>(layer, vec, shared), g, runs, op->back_threads);
+        if (rc != SCAR_OK) return rc;
+    }
+    const bool gates = g.dgate && g.per_gate > 1 && runs > 1;
+    if (!g.dw_pre && !g.dw_post && !g.db_pre && !g.db_post && !gates) return SCAR_OK;
+    k_resnorm_join<T><<<dim3((g.dim + 31) / 32, 4 + (gates ? std::min(runs, kJoinGates) : 0)), 256, 0, op->stream>>>(g, runs);
+    op->launches++;
+    return SCAR_OK;
+}
+
+// Shared memory for the operator's kernels, and how many of their CTAs an SM's registers hold: the fewest over the ways that rows
+// may lie and gates be shared, so that the order of sums over rows depends on sizes alone.
+template <typename T> int fit_kernels(scar_resnorm *op) {
+    const bool layer = op->cfg.kind == SCAR_RESNORM_LAYER;
+    int rc = SCAR_OK;
+    const auto fit = [&](auto kernel, unsigned threads) {
+        cudaFuncAttributes a{};
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemOfSm) != cudaSuccess || cudaFuncGetAttributes(&a, kernel) != cudaSuccess) {
+            cudaGetLastError();
+            rc = SCAR_ERR_CUDA;
+            return 1u;
+        }
+        return std::max(1u, std::min(32u, 65536u / ((unsigned)round_up(std::max(a.numRegs, 1), 8) * threads)));
+    };
+    op->forward_fit = std::min(fit(forward_kernel<T>(layer, true), op->forward_threads), fit(forward_kernel<T>(layer, false), op->forward_threads));
+    op->back_fit = 32;
+    for (int i = 0; i < 4; ++i) op->back_fit = std::min(op->back_fit, fit(backward_kernel<T>(layer, i & 1, i >> 1), op->back_threads));
+    return rc;
 }
 
 constexpr uint64_t kFar = 1ull << 40;  // elements of a pitch: rows times pitch stays below 2^63 bytes
@@ -547,8 +916,8 @@ template <typename T> NormArgs<T> block_args(const scar_resnorm *op, const scar_
     g.eps = (float)op->cfg.eps;
     g.post = k->post != 0;
     g.pre = k->pre != 0;
-    g.gate = static_cast<const T *>(k->d_gate);
-    g.gate_pitch = k->gate_pitch;
+    g.cluster = op->cluster;
+    g.span = op->span;
     g.per_gate = (unsigned)std::min<uint64_t>(std::max<uint64_t>(k->rows_per_gate, 1), std::max<uint64_t>(rows, 1));
     g.w_post = k->post ? static_cast<const T *>(k->d_w_post) : nullptr;
     g.b_post = k->post ? static_cast<const T *>(k->d_b_post) : nullptr;
@@ -558,8 +927,13 @@ template <typename T> NormArgs<T> block_args(const scar_resnorm *op, const scar_
 }
 uint64_t gates_of(const scar_resnorm_block *k, uint64_t rows) { return k->rows_per_gate ? (rows + k->rows_per_gate - 1) / k->rows_per_gate : 0; }
 
-int done(scar_resnorm *) {
+int done(scar_resnorm *op, int rc) {
+    if (rc != SCAR_OK) return rc;
     TRAIN_TRY(cudaGetLastError());
+    if (op->arm_error) {  // self-test: the report of a wait that gave up
+        op->arm_error = false;
+        TRAIN_TRY(cudaMemsetAsync(op->error, 1, 1, op->stream));
+    }
     return SCAR_OK;
 }
 
@@ -583,17 +957,24 @@ int scar_resnorm_init(scar_resnorm **out, const scar_resnorm_config *cfg, void *
         int sms = 0;
         TRAIN_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, op->device));
         op->sms = std::max(1, sms);
-        const unsigned groups = (unsigned)((cfg->dim + 7) / 8);
-        op->rounds = groups <= kMostThreads ? 1 : groups <= 2 * kMostThreads ? 2 : 4;
-        op->threads = (unsigned)round_up((groups + op->rounds - 1) / op->rounds, 32);
-        // CTAs of backward: as many as run at a time (128 registers a thread), and eight rows each where there are many
-        op->back_ctas = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>((uint64_t)op->sms * std::max(1u, 512 / op->threads), cfg->max_rows));
-        if (!cfg->forward_only) {
-            if (cudaMalloc(&op->part, 6ull * op->back_ctas * cfg->dim * sizeof(float)) != cudaSuccess) {
-                cudaGetLastError();
-                return SCAR_ERR_ALLOC;
-            }
+        op->cluster = (unsigned)((cfg->dim + kSpan - 1) / kSpan);
+        op->span = (unsigned)round_up((cfg->dim + op->cluster - 1) / op->cluster, 8);
+        op->forward_threads = (unsigned)round_up((op->span + kForwardValues - 1) / kForwardValues, 32);
+        const int back = back_values(cfg->kind == SCAR_RESNORM_LAYER);
+        op->back_threads = (unsigned)round_up((op->span + back - 1) / back, 32);
+        int rc = SCAR_OK;
+        dispatch_operand(cfg->dtype, [&](auto e) { rc = fit_kernels<decltype(e)>(op); });
+        if (rc != SCAR_OK) return rc;
+        // runs of backward: as many as are held at a time
+        op->most_runs = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(op->sms * op->back_fit / op->cluster, cfg->max_rows));
+        const uint64_t floats = cfg->forward_only ? 0 : 6ull * op->most_runs * cfg->dim;
+        if (cudaMalloc(&op->part, floats * sizeof(float) + 16) != cudaSuccess) {
+            cudaGetLastError();
+            op->part = nullptr;
+            return SCAR_ERR_ALLOC;
         }
+        op->error = reinterpret_cast<unsigned *>(op->part + floats);
+        TRAIN_TRY(cudaMemsetAsync(op->error, 0, 16, op->stream));
         TRAIN_TRY(cudaStreamSynchronize(op->stream));
         return SCAR_OK;
     };
@@ -618,13 +999,16 @@ int scar_resnorm_forward(scar_resnorm *op, const scar_resnorm_block *block, cons
     dispatch_operand(op->cfg.dtype, [&](auto e) {
         using T = decltype(e);
         NormArgs<T> g = block_args<T>(op, block, n_rows);
-        g.x = static_cast<const T *>(d_x); g.x_pitch = x_pitch;
-        g.f = static_cast<const T *>(d_f); g.f_pitch = f_pitch;
+        g.has_f = d_f != nullptr;
+        g.has_gate = block->d_gate != nullptr;
+        g.in[kX] = {static_cast<const T *>(d_x), x_pitch, 1};
+        g.in[kF] = {static_cast<const T *>(d_f), f_pitch, 1};
+        g.in[kGate] = {static_cast<const T *>(block->d_gate), block->gate_pitch, g.per_gate};
         g.y = static_cast<T *>(d_y); g.y_pitch = y_pitch;
         g.n = block->pre ? static_cast<T *>(d_n) : nullptr; g.n_pitch = n_pitch;
-        run_forward(op, g);
+        rc = run_forward(op, g);
     });
-    return done(op);
+    return done(op, rc);
 }
 
 int scar_resnorm_backward(scar_resnorm *op, const scar_resnorm_block *block, const void *d_dy, uint64_t dy_pitch, const void *d_dn, uint64_t dn_pitch,
@@ -647,10 +1031,15 @@ int scar_resnorm_backward(scar_resnorm *op, const scar_resnorm_block *block, con
     dispatch_operand(op->cfg.dtype, [&](auto e) {
         using T = decltype(e);
         NormArgs<T> g = block_args<T>(op, block, n_rows);
-        g.x = static_cast<const T *>(d_dy); g.x_pitch = dy_pitch;
-        g.dn = static_cast<const T *>(d_dn); g.dn_pitch = dn_pitch;
-        g.y = const_cast<T *>(static_cast<const T *>(d_y)); g.y_pitch = y_pitch;
-        g.f = static_cast<const T *>(d_f); g.f_pitch = f_pitch;
+        g.has_f = d_f != nullptr;
+        g.has_gate = block->d_gate != nullptr;
+        g.in[kDy] = {static_cast<const T *>(d_dy), dy_pitch, 1};
+        if (block->pre) {
+            g.in[kDn] = {static_cast<const T *>(d_dn), dn_pitch, 1};
+            g.in[kY] = {static_cast<const T *>(d_y), y_pitch, 1};
+        }
+        g.in[kBackF] = {static_cast<const T *>(d_f), f_pitch, 1};
+        g.in[kBackGate] = {static_cast<const T *>(block->d_gate), block->gate_pitch, g.per_gate};
         g.n = static_cast<T *>(d_dx); g.n_pitch = dx_pitch;
         g.df = static_cast<T *>(d_df); g.df_pitch = df_pitch;
         g.dgate = static_cast<T *>(d_dgate); g.dgate_pitch = dgate_pitch;
@@ -658,9 +1047,26 @@ int scar_resnorm_backward(scar_resnorm *op, const scar_resnorm_block *block, con
         g.db_post = static_cast<T *>(d_db_post);
         g.dw_pre = static_cast<T *>(d_dw_pre);
         g.db_pre = static_cast<T *>(d_db_pre);
-        run_backward(op, g);
+        rc = run_backward(op, g);
     });
-    return done(op);
+    return done(op, rc);
+}
+
+int scar_resnorm_status(scar_resnorm *op) {
+    if (!op) return SCAR_ERR_INVALID_ARG;
+    const int rc = check_current_device(op->device);
+    if (rc != SCAR_OK) return rc;
+    unsigned error = 0;
+    TRAIN_TRY(cudaMemcpyAsync(&error, op->error, sizeof(error), cudaMemcpyDeviceToHost, op->stream));
+    TRAIN_TRY(cudaMemsetAsync(op->error, 0, sizeof(error), op->stream));
+    TRAIN_TRY(cudaStreamSynchronize(op->stream));
+    return error ? SCAR_ERR_TIMEOUT : SCAR_OK;
+}
+
+int scar_resnorm_selftest_arm_timeout(scar_resnorm *op) {
+    if (!op) return SCAR_ERR_INVALID_ARG;
+    op->arm_error = true;
+    return SCAR_OK;
 }
 
 uint64_t scar_resnorm_launch_count(const scar_resnorm *op) { return op ? op->launches : 0; }

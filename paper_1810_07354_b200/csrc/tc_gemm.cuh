@@ -22,6 +22,7 @@
 #include <cuda.h>
 
 #include "activation.cuh"
+#include "barriers.cuh"
 #include "mask.cuh"
 
 namespace scar {
@@ -29,7 +30,6 @@ namespace scar {
 constexpr int kBM = 256, kBK = 64;  // a pair's rows of A, and k per stage
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = (kEpiWarps + 2) * 32;
-constexpr unsigned long long kWaitNs = 2000000000ull;  // a wait inside the kernel gives up after two seconds
 
 enum class Epi { kPart, kOut, kProb, kStat, kIdentity, kRelu, kGelu, kSilu };  // the last four: a layer's output, by its activation
 __host__ __device__ constexpr bool is_layer(Epi e) { return e >= Epi::kIdentity; }
@@ -106,40 +106,6 @@ constexpr float kProbScale = 32768.f;
 constexpr float kProbLog2 = 15.f;
 constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok;
-}
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-// Bounded wait.  After kWaitNs it records the failure and returns false; the caller leaves its loop.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, unsigned *error) {
-    if (mbar_try(bar, parity)) return true;
-    const unsigned long long until = now_ns() + kWaitNs;
-    for (unsigned i = 1;; ++i) {
-        if (mbar_try(bar, parity)) return true;
-        if ((i & 255u) == 0 && now_ns() > until) {
-            atomicExch(error, 1u);
-            return false;
-        }
-    }
-}
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 // Arrives at the same barrier in the pair's first CTA.  Relaxed: what it reports are reads of tensor memory that are done
 // (tcgen05.wait::ld); releasing would also wait for the warp's stores of the tile before, about 2000 clocks.
 __device__ __forceinline__ void mbar_arrive_leader(uint32_t bar) {
@@ -154,14 +120,6 @@ __device__ __forceinline__ bool elect_one() {
     uint32_t p;
     asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
     return p;
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // A box of the tensor map into this CTA's shared memory; its bytes are counted at the barrier of the pair's first CTA
 // (bit 24 of a shared::cluster address tells the two apart).
