@@ -33,7 +33,7 @@ using namespace scar;
 namespace {
 
 constexpr unsigned kSpan = 4096;  // columns of a CTA at most
-constexpr unsigned kMostCluster = (SCAR_RESNORM_MAX_DIM + kSpan - 1) / kSpan, kMostStages = 6;
+constexpr unsigned kMostStages = 6;
 // Values of a row that a thread has, and rows that it has under way at a time.  Forward: 16, so that what a thread does once per row
 // (waits, sums over the CTA, addresses) is shared by many (16384 x 4096 bfloat16: 110 us, with 8 values 187).  Backward: the sums
 // over rows take two to five registers a value; eight values and two rows share those, and the rows' sums over the CTA are one
@@ -59,6 +59,7 @@ template <typename T> struct NormArgs {
     float scale, eps;
     int post, pre, has_f, has_gate;
     In<T> in[kBackwardIn];
+    unsigned n_in;  // of them there are
     const T *w_post, *b_post, *w_pre, *b_pre;
     T *y, *n, *df, *dgate;                      // backward: n is dx
     unsigned long long y_pitch, n_pitch, df_pitch, dgate_pitch;
@@ -172,13 +173,17 @@ template <int M> __device__ __forceinline__ float dot(const float2 (&a)[M], cons
     return s.x + s.y;
 }
 
-// The CTA's ring of rows.  Its methods that copy are called by all lanes of warp 0 and by no other.
+// The CTA's ring of rows.  Its methods that copy are called by all lanes of one warp and by no other warp: a lane per matrix copies
+// the whole 16-byte words of its row; of rows anywhere, lanes read the values before and behind those words one by one and put them
+// in place a row later.  At the barrier of a stage every matrix arrives once, and the values at the rows' ends together once.
 template <typename T, bool VEC, int IN, int R> struct Ring {
+    static constexpr int kEnd = 16 / sizeof(T) - 1;                         // values at one end of a row, at most
+    static constexpr int kPasses = VEC ? 1 : (2 * kEnd * IN + 31) / 32;     // rounds of a warp over all ends of a row
     const NormArgs<T> &g;
     uint8_t *smem;
-    uint32_t full;  // barriers, one per stage; rows anywhere: a second arrival reports the values at a row's ends
+    uint32_t full;  // barriers, one per stage
     unsigned col0, cols;
-    T edge[R][VEC ? 1 : IN];  // on their way to the stages of the rows that were issued last
+    T edge[R][kPasses];  // on their way to the stages of the rows that were issued last
 
     __device__ __forceinline__ const T *source(int a, unsigned row) const {
         const In<T> &m = g.in[a];
@@ -196,80 +201,76 @@ template <typename T, bool VEC, int IN, int R> struct Ring {
         to = VEC ? b : b & ~uintptr_t(15);
         if (to < from) to = from;
     }
-    // This lane's value at a row's ends: lanes 0 .. 7 those before the first whole word, 8 .. 15 those behind the last.
-    __device__ __forceinline__ unsigned edge_at(const T *p) const {
-        const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-        uintptr_t from, to;
-        words(p, from, to);
-        const unsigned lane = threadIdx.x & 31, head = min(cols, (unsigned)((from - a) / sizeof(T))), tail = max(head, (unsigned)((to - a) / sizeof(T)));
-        const unsigned i = lane < 8 ? lane : tail + lane - 8;
-        return (lane < 8 ? i < head : lane < 16 && i < cols) ? i : 0xffffffffu;
+    // f(matrix, its row, which of the values behind the row's end, which value of the row or none) for each of this lane's ends.
+    template <typename F> __device__ __forceinline__ void ends(unsigned row, F f) const {
+#pragma unroll
+        for (int q = 0; q < kPasses; ++q) {
+            const unsigned id = q * 32 + (threadIdx.x & 31), a = id / (2 * kEnd), j = id % (2 * kEnd);
+            if (a >= IN || !g.in[a].p) continue;
+            const T *p = source(a, row);
+            uintptr_t from, to;
+            words(p, from, to);
+            const unsigned head = min(cols, (unsigned)((from - reinterpret_cast<uintptr_t>(p)) / sizeof(T)));
+            const unsigned tail = max(head, (unsigned)((to - reinterpret_cast<uintptr_t>(p)) / sizeof(T)));
+            const unsigned i = j < kEnd ? j : tail + j - kEnd;
+            f(q, a, p, j, (j < kEnd ? i < head : i < cols) ? i : 0xffffffffu);
+        }
     }
     __device__ __forceinline__ void put_edges(unsigned row, unsigned stage, int k = 0) {
         if (VEC) return;
-#pragma unroll
-        for (int a = 0; a < IN; ++a) {
-            if (!g.in[a].p) continue;
-            const unsigned i = edge_at(source(a, row)), lane = threadIdx.x & 31;
+        ends(row, [&](int q, unsigned a, const T *, unsigned j, unsigned i) {
             T *const p = const_cast<T *>(at(a, row, stage));
-            if (i != 0xffffffffu) p[i] = edge[k][VEC ? 0 : a];
+            if (i != 0xffffffffu) p[i] = edge[k][q];
             // a row that began further on may have ended here before
-            const unsigned z = cols + lane - 16;
-            if (lane >= 16 && lane - 16 < 16 / sizeof(T) - 1 && z < (g.array_bytes - 16) / sizeof(T)) p[z] = from_f32<T>(0.f);
-        }
+            if (j < kEnd && cols + j < (g.array_bytes - 16) / sizeof(T)) p[cols + j] = from_f32<T>(0.f);
+        });
         __syncwarp();
         if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + 8 * stage) : "memory");
     }
     __device__ __forceinline__ void issue(unsigned row, unsigned stage, int k = 0) {
-        if (!VEC) {
-#pragma unroll
-            for (int a = 0; a < IN; ++a) {
-                if (!g.in[a].p) continue;
-                const T *p = source(a, row);
-                const unsigned i = edge_at(p);
-                if (i != 0xffffffffu) edge[k][VEC ? 0 : a] = p[i];
-            }
-        }
-        if ((threadIdx.x & 31) == 0) {
+        if (!VEC)
+            ends(row, [&](int q, unsigned, const T *p, unsigned, unsigned i) {
+                if (i != 0xffffffffu) edge[k][q] = p[i];
+            });
+        const unsigned a = threadIdx.x & 31;
+        if (a < IN && g.in[a].p) {
             const uint32_t bar = full + 8 * stage;
-            unsigned bytes = 0;
+            const T *p = source(a, row);
             uintptr_t from, to;
-#pragma unroll
-            for (int a = 0; a < IN; ++a)
-                if (g.in[a].p) {
-                    words(source(a, row), from, to);
-                    bytes += (unsigned)(to - from);
-                }
-            mbar_expect(bar, bytes);
-#pragma unroll
-            for (int a = 0; a < IN; ++a) {
-                if (!g.in[a].p) continue;
-                const T *p = source(a, row);
-                words(p, from, to);
-                if (to == from) continue;
-                const uint32_t dst = smem_addr(at(a, row, stage)) + (uint32_t)(from - reinterpret_cast<uintptr_t>(p));
-                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from),
-                             "r"((unsigned)(to - from)), "r"(bar)
+            words(p, from, to);
+            mbar_expect(bar, (unsigned)(to - from));
+            if (to != from)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                                 smem_addr(at(a, row, stage)) + (uint32_t)(from - reinterpret_cast<uintptr_t>(p))),
+                             "l"(from), "r"((unsigned)(to - from)), "r"(bar)
                              : "memory");
-            }
         }
         __syncwarp();
     }
 };
 
+// As mbar_wait, for what other CTAs of the cluster have written before they arrived.
+__device__ __forceinline__ bool try_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok;
+}
 __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, unsigned *error) {
-    const unsigned long long until = now_ns() + kWaitNs;
+    if (try_cluster(bar, parity)) return true;
+    unsigned long long until = 0;
     for (unsigned i = 1;; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        if (ok) return true;
-        if ((i & 255u) == 0 && now_ns() > until) {
-            atomicExch(error, 1u);
-            return false;
+        if (try_cluster(bar, parity)) return true;
+        if ((i & 255u) == 0) {
+            const unsigned long long now = now_ns();
+            if (!until) until = now + kWaitNs;
+            if (now > until) {
+                atomicExch(error, 1u);
+                return false;
+            }
         }
     }
 }
@@ -325,17 +326,17 @@ template <int kWarps> struct Sums {  // kWarps: of a CTA at most
 #pragma unroll
                 for (int o = kOver / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
             } else {
+                // Stores that report themselves at the reader's barrier: an arrival that releases would wait for this warp's results
+                // on their way to memory (4096 x 16384 bfloat16, forward: 390 us).
+                const uint32_t mbar = smem_addr(sh->red + half);
+                if (threadIdx.x == 0) mbar_expect(mbar, P * 4 * warps * cluster);
                 if (sub == 0) {
                     const uint32_t here = smem_addr(at + cluster_rank() * warps + warp);
                     for (unsigned c = 0; c < cluster; ++c)
-                        asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, %1;\n st.shared::cluster.f32 [a], %2;\n}\n" ::"r"(here), "r"(c), "f"(x) : "memory");
+                        asm volatile("{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
+                                     " st.async.shared::cluster.mbarrier::complete_tx::bytes.f32 [a], %3, [b];\n}\n" ::"r"(here), "r"(mbar), "r"(c), "f"(x)
+                                     : "memory");
                 }
-                __syncwarp();
-                if (lane < cluster)
-                    asm volatile("{\n .reg .b32 b;\n mapa.shared::cluster.u32 b, %0, %1;\n mbarrier.arrive.release.cluster.shared::cluster.b64 _, [b];\n}\n" ::"r"(
-                                     smem_addr(sh->red + half)),
-                                 "r"(lane)
-                                 : "memory");
                 if (ok) ok = wait_cluster(smem_addr(sh->red + half), phase >> half & 1u, error);
                 __syncwarp();
                 phase ^= 1u << half;
@@ -360,8 +361,8 @@ template <bool VEC, typename T> __device__ __forceinline__ void start(const Norm
     for (unsigned i = threadIdx.x; i < g.stages * g.stage_bytes / 16; i += blockDim.x) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     if (threadIdx.x == 0) {
-        for (unsigned i = 0; i < g.stages; ++i) mbar_init(smem_addr(sh.full + i), VEC ? 1 : 2);
-        for (int i = 0; i < 2; ++i) mbar_init(smem_addr(sh.red + i), g.cluster * (blockDim.x / 32));
+        for (unsigned i = 0; i < g.stages; ++i) mbar_init(smem_addr(sh.full + i), g.n_in + (VEC ? 0 : 1));
+        for (int i = 0; i < 2; ++i) mbar_init(smem_addr(sh.red + i), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (g.cluster > 1) cluster_sync_all();
@@ -786,13 +787,17 @@ constexpr unsigned kSmemOfSm = 220 * 1024;  // left to the rings of an SM's CTAs
 
 // The ring of a kernel whose rows consist of `arrays` matrices: as many stages, between two and six, as leave room for
 // `resident` CTAs on an SM, if that is possible.
+// About 100 KiB of rows on their way to an SM are enough: forward of 16384 x 4096 bfloat16 takes 106 us with that and 124 us with half
+// as much again (reads and writes of more rows take turns at the same memory), without a gate 87 and, with a third less, 91.
 template <typename T> void set_ring(const scar_resnorm *op, NormArgs<T> &g, unsigned arrays, unsigned vectors, unsigned at_once, unsigned threads, unsigned values, unsigned resident) {
     g.array_bytes = (unsigned)(threads * values * sizeof(T) + 16);  // what the threads read, and up to 15 bytes before it
     g.stage_bytes = arrays * g.array_bytes;
     const unsigned warps = threads / 32 * g.cluster, slots = warps > 1 ? (unsigned)round_up(2 * 8 * 4 * warps, 16) : 0u;
     const unsigned other = vectors * g.array_bytes + slots;
     const unsigned room = kSmemOfSm / resident - (resident > 1 ? (unsigned)sizeof(Shared) + 1024u : 0u);  // 1 KiB a CTA is the system's
-    g.stages = std::max(2 * at_once, std::min(kMostStages, room > other ? (room - other) / g.stage_bytes : 0u) / at_once * at_once);
+    for (const In<T> &m : g.in) g.n_in += m.p != nullptr;
+    const unsigned wanted = (100u * 1024u + resident * g.n_in * g.array_bytes / 2) / (resident * g.n_in * g.array_bytes);
+    g.stages = std::max(2 * at_once, std::min(std::min(kMostStages, wanted), room > other ? (room - other) / g.stage_bytes : 0u) / at_once * at_once);
     g.slot_off = g.stages * g.stage_bytes + vectors * g.array_bytes;
     g.smem = g.slot_off + slots;
     g.error = op->error;
