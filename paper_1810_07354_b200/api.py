@@ -825,13 +825,17 @@ class _OnStream:
             here.wait_stream(self._stream)
 
 
-def _operand_type(dtype) -> int:
-    import torch
+_OPERAND_TYPES = {}
 
-    types = {torch.float32: SCAR_F32, torch.bfloat16: SCAR_BF16, torch.float16: SCAR_F16}
-    if dtype not in types:
+
+def _operand_type(dtype) -> int:
+    if not _OPERAND_TYPES:
+        import torch
+
+        _OPERAND_TYPES.update({torch.float32: SCAR_F32, torch.bfloat16: SCAR_BF16, torch.float16: SCAR_F16})
+    if dtype not in _OPERAND_TYPES:
         raise TypeError(f"{dtype}: the training-step operators take float32, bfloat16 and float16")
-    return types[dtype]
+    return _OPERAND_TYPES[dtype]
 
 
 class LinearCrossEntropy(_OnStream):
@@ -1013,44 +1017,56 @@ class Dropout(_OnStream):
         self.p, self.seed = float(p), seed
         self._bind_stream(stream, device)
 
+    def _rule(self, offset):
+        """The rule, and the tensor its offset lies in."""
+        if isinstance(offset, int):
+            return scar_dropout(self.p, self.seed & (2**64 - 1), offset & (2**64 - 1), None), None
+        if offset.dtype != self._torch.int64 or offset.numel() != 1 or offset.device != self._device:
+            raise TypeError(f"offset: an int or a tensor of one int64 on {self._device} is wanted")
+        return scar_dropout(self.p, self.seed & (2**64 - 1), 0, offset.data_ptr()), offset
+
     def mask(self, offset=0) -> DropoutMask:
-        tensor = None
-        if not isinstance(offset, int):
-            if offset.dtype != self._torch.int64 or offset.numel() != 1 or offset.device != self._device:
-                raise TypeError(f"offset: an int or a tensor of one int64 on {self._device} is wanted")
-            tensor, offset = offset, 0
-        return DropoutMask(scar_dropout(p=self.p, seed=self.seed & (2**64 - 1), offset=offset & (2**64 - 1), d_offset=None if tensor is None else tensor.data_ptr()),
-                           tensor)
+        return DropoutMask(*self._rule(offset))
 
     def _rows(self, name: str, m, like):
-        if m.device != self._device or m.dtype != like.dtype:
+        """Address and pitch of m's rows."""
+        if m.dtype != like.dtype or m.device != self._device:
             raise TypeError(f"{name}: a tensor of {like.dtype} on {self._device} is wanted")
-        if m.shape != like.shape:
+        shape = m.shape
+        if shape != like.shape:
             raise ValueError(f"{name}: shape {tuple(like.shape)} is wanted")
-        if m.numel() == 0:
-            return 0, 0
-        cols = m.shape[-1] if m.dim() else 1
-        if m.dim() > 2 or m.dim() == 0:
+        if m.is_contiguous():
+            return m.data_ptr(), (shape[-1] if shape else 1)
+        if len(shape) > 2:
             try:
-                m = m.view(-1, cols)
+                m = m.view(-1, shape[-1])
             except RuntimeError:
                 raise ValueError(f"{name}: rows the same distance apart are wanted") from None
-        if cols > 1 and m.stride(-1) != 1:
+        cols, stride = shape[-1], m.stride()
+        if cols > 1 and stride[-1] != 1:
             raise ValueError(f"{name}: contiguous rows are wanted")
-        return m.data_ptr(), (max(m.stride(0), cols) if m.dim() == 2 and m.shape[0] == 1 else m.stride(0) if m.dim() == 2 else cols)
+        pitch = cols if m.dim() == 1 or m.shape[0] == 1 else stride[0]
+        if pitch < cols:
+            raise ValueError(f"{name}: rows that do not overlap are wanted")
+        return m.data_ptr(), pitch
 
     def _call(self, x, offset, residual, out):
         dtype = _operand_type(x.dtype)
-        mask = self.mask(offset)
-        out = self._torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        rule, tensor = self._rule(offset)
+        if out is None:
+            out = x.new_empty(x.shape)
         xp, yp = self._rows("x", x, x), self._rows("out", out, x)
         rp = (None, 0) if residual is None else self._rows("residual", residual, x)
-        if x.numel() == 0:
+        n = x.numel()
+        if n == 0:
             return out
         cols = x.shape[-1] if x.dim() else 1
-        here = self._enter(x, residual, out, mask.tensor)
-        with self._torch.cuda.device(self._device):
-            scar_dropout_apply(mask.rule, dtype, *xp, *rp, *yp, x.numel() // cols, cols, self._stream.cuda_stream)
+        here = self._enter(x, residual, out, tensor)
+        if self._torch.cuda.current_device() == self._device.index:
+            scar_dropout_apply(rule, dtype, *xp, *rp, *yp, n // cols, cols, self._stream.cuda_stream)
+        else:
+            with self._torch.cuda.device(self._device):
+                scar_dropout_apply(rule, dtype, *xp, *rp, *yp, n // cols, cols, self._stream.cuda_stream)
         self._leave(here)
         return out
 
@@ -1067,13 +1083,19 @@ class _Rows(_OnStream):
     """Checks of matrices and vectors of one type on one device."""
 
     def _matrix(self, name: str, m, rows: int, cols: int):
+        """Address and pitch."""
         if m.dtype != self.dtype or m.device != self._device:
             raise TypeError(f"{name}: a tensor of {self.dtype} on {self._device} is wanted")
-        if m.dim() != 2 or tuple(m.shape) != (rows, cols) or (cols > 1 and m.stride(1) != 1):
-            raise ValueError(f"{name}: shape ({rows}, {cols}) with contiguous rows is wanted")
-        if rows > 1 and m.stride(0) < cols:
+        if m.shape != (rows, cols):
+            raise ValueError(f"{name}: shape ({rows}, {cols}) is wanted")
+        pitch, step = m.stride()
+        if cols > 1 and step != 1:
+            raise ValueError(f"{name}: contiguous rows are wanted")
+        if rows <= 1:
+            return m.data_ptr(), cols
+        if pitch < cols:
             raise ValueError(f"{name}: rows that do not overlap are wanted")
-        return m.data_ptr(), (m.stride(0) if rows > 1 else max(m.stride(0), cols))
+        return m.data_ptr(), pitch
 
     def _vector(self, name: str, v, n: int):
         if v is None:
@@ -1083,9 +1105,6 @@ class _Rows(_OnStream):
         if v.numel() != n or not v.is_contiguous():
             raise ValueError(f"{name}: {n} contiguous values are wanted")
         return v.data_ptr()
-
-    def _empty(self, *shape):
-        return self._torch.empty(shape, dtype=self.dtype, device=self._device)
 
 
 _ACTIVATIONS = {"identity": SCAR_ACT_IDENTITY, "relu": SCAR_ACT_RELU, "gelu": SCAR_ACT_GELU, "silu": SCAR_ACT_SILU}
@@ -1121,18 +1140,18 @@ class LinearLayer(_Rows):
                 raise ValueError("slope: the identity has none")
             return None
         shape = (rows, -(-self.out_features // 8) * 8)
-        if slope.dtype != self._slope_type() or slope.device != self._device or tuple(slope.shape) != shape or not slope.is_contiguous():
+        if slope is None or slope.dtype != self._slope_type() or slope.device != self._device or slope.shape != shape or not slope.is_contiguous():
             raise ValueError(f"slope: a contiguous tensor of {shape} of {self._slope_type()} on {self._device} is wanted")
         return slope.data_ptr()
 
     def _forward(self, train, x, w, bias, residual, dropout, out, slope):
-        rows, K, N = x.shape[0] if x.dim() else 0, self.in_features, self.out_features
+        rows, K, N = len(x) if x.dim() else 0, self.in_features, self.out_features
         xp, wp, bp = self._matrix("x", x, rows, K), self._matrix("w", w, N, K), self._vector("bias", bias, N)
         rp = (None, 0) if residual is None else self._matrix("residual", residual, rows, N)
-        out = self._empty(rows, N) if out is None else out
+        out = x.new_empty((rows, N)) if out is None else out
         yp = self._matrix("out", out, rows, N)
         if train and slope is None and self.activation != "identity":
-            slope = self._torch.empty((rows, -(-N // 8) * 8), dtype=self._slope_type(), device=self._device)
+            slope = x.new_empty((rows, -(-N // 8) * 8), dtype=self._slope_type())
         sp = self._slope(slope, rows) if train else None
         rule, offset = self._mask(dropout)
         here = self._enter(x, w, bias, residual, out, slope, offset)
@@ -1150,11 +1169,11 @@ class LinearLayer(_Rows):
 
     def backward(self, dy, x, w, slope, dropout=None, dx=None, dw=None, dbias=None, need_dx: bool = True, need_dw: bool = True, need_dbias: bool = True):
         """``(dx, dw, dbias)`` from the gradient of the output, which is the residual's own; None for what is not needed."""
-        rows, K, N = dy.shape[0] if dy.dim() else 0, self.in_features, self.out_features
+        rows, K, N = len(dy) if dy.dim() else 0, self.in_features, self.out_features
         dyp, xp, wp, sp = self._matrix("dy", dy, rows, N), self._matrix("x", x, rows, K), self._matrix("w", w, N, K), self._slope(slope, rows)
-        dx = None if not need_dx else self._empty(rows, K) if dx is None else dx
-        dw = None if not need_dw else self._empty(N, K) if dw is None else dw
-        dbias = None if not need_dbias else self._empty(N) if dbias is None else dbias
+        dx = None if not need_dx else dy.new_empty((rows, K)) if dx is None else dx
+        dw = None if not need_dw else dy.new_empty((N, K)) if dw is None else dw
+        dbias = None if not need_dbias else dy.new_empty((N,)) if dbias is None else dbias
         dxp = (None, 0) if dx is None else self._matrix("dx", dx, rows, K)
         dwp = (None, 0) if dw is None else self._matrix("dw", dw, N, K)
         dbp = self._vector("dbias", dbias, N)
@@ -1206,9 +1225,8 @@ class ResidualNorm(_Rows):
         if rows_per_gate < 1:
             raise ValueError("rows_per_gate: at least 1 is wanted")
         gp = (None, 0) if gate is None else self._matrix("gate", gate, -(-rows // rows_per_gate), self.dim)
-        return scar_resnorm_block(post=int(post), pre=int(pre), scale=scale, d_gate=gp[0], gate_pitch=gp[1], rows_per_gate=rows_per_gate,
-                                  d_w_post=self._vector("w_post", w_post, self.dim), d_b_post=self._vector("b_post", b_post, self.dim),
-                                  d_w_pre=self._vector("w_pre", w_pre, self.dim), d_b_pre=self._vector("b_pre", b_pre, self.dim))
+        return scar_resnorm_block(post, pre, scale, *gp, rows_per_gate, self._vector("w_post", w_post, self.dim), self._vector("b_post", b_post, self.dim),
+                                  self._vector("w_pre", w_pre, self.dim), self._vector("b_pre", b_pre, self.dim))
 
     def _maybe(self, name, m, rows):
         return (None, 0) if m is None else self._matrix(name, m, rows, self.dim)
@@ -1216,16 +1234,16 @@ class ResidualNorm(_Rows):
     def forward(self, x, f=None, post: bool = True, pre: bool = True, scale: float = 1.0, gate=None, rows_per_gate: int = 1, w_post=None, b_post=None,
                 w_pre=None, b_pre=None, y=None, n=None):
         """``(y, n)``; n is None without ``pre``, y is x itself without ``f``.  ``y`` may be given as x or f."""
-        rows = x.shape[0] if x.dim() else 0
-        post = post and f is not None
+        rows = len(x) if x.dim() else 0
+        post = bool(post and f is not None)
         block = self._block(rows, post, pre, scale, gate, rows_per_gate, w_post, b_post, w_pre, b_pre)
         xp, fp = self._matrix("x", x, rows, self.dim), self._maybe("f", f, rows)
         if f is None and y is None:
             yp = (None, 0)
         else:
-            y = self._empty(rows, self.dim) if y is None else y
+            y = x.new_empty((rows, self.dim)) if y is None else y
             yp = self._matrix("y", y, rows, self.dim)
-        n = None if not pre else self._empty(rows, self.dim) if n is None else n
+        n = None if not pre else x.new_empty((rows, self.dim)) if n is None else n
         np_ = self._maybe("n", n, rows)
         here = self._enter(x, f, gate, w_post, b_post, w_pre, b_pre, y, n)
         scar_resnorm_forward(self.op, block, *xp, *fp, rows, *yp, *np_)
@@ -1238,15 +1256,15 @@ class ResidualNorm(_Rows):
         input.  ``dy`` may be None (with ``pre``) where y goes nowhere else; without ``pre``, ``dn`` is None and ``y`` is not read.
         ``out``: a dictionary of tensors to write some of them to."""
         some = dy if dy is not None else dn
-        rows = some.shape[0] if some.dim() else 0
-        post = post and f is not None
+        rows = len(some) if some.dim() else 0
+        post = bool(post and f is not None)
         block = self._block(rows, post, pre, scale, gate, rows_per_gate, w_post, b_post, w_pre, b_pre)
         dyp, dnp = self._maybe("dy", dy, rows), self._maybe("dn", dn if pre else None, rows)
         yp, fp = self._maybe("y", y if pre else None, rows), self._maybe("f", f, rows)
         has = {"dx": some, "df": f, "dgate": gate, "dw_post": w_post if post else None, "db_post": b_post if post else None,
                "dw_pre": w_pre if pre else None, "db_pre": b_pre if pre else None}
         out = out or {}
-        got = {k: None if v is None else out[k] if k in out else self._empty(*v.shape) for k, v in has.items()}
+        got = {k: None if v is None else out[k] if k in out else v.new_empty(v.shape) for k, v in has.items()}
         matrices = [self._maybe(k, got[k], rows if k != "dgate" or gate is None else gate.shape[0]) for k in ("dx", "df", "dgate")]
         vectors = [self._vector(k, got[k], self.dim) for k in ("dw_post", "db_post", "dw_pre", "db_pre")]
         here = self._enter(dy, dn, y, f, gate, w_post, b_post, w_pre, b_pre, *got.values())

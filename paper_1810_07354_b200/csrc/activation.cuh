@@ -2,35 +2,50 @@
 #pragma once
 #include <type_traits>
 
-#include "train_common.cuh"
+#include "pairs.cuh"
 
 namespace scar {
 
-// a = act(z), slope = act'(z).  The Gaussian's distribution function comes from Abramowitz and Stegun's formula 7.1.26 for erf
-// (off by 1.5e-7 at most): it needs one reciprocal and the exponential that its derivative needs anyway, and takes the lower
-// tail as a product, so nothing cancels there.
-template <int ACT> __device__ __forceinline__ void activate(float z, float &a, float &slope) {
+__device__ __forceinline__ float2 ex2_pair(float2 x) {
+    float2 y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(x.y));
+    return y;
+}
+__device__ __forceinline__ float2 rcp_pair(float2 x) {
+    float2 y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(x.y));
+    return y;
+}
+
+// a = act(z), slope = act'(z), of two values.  The Gaussian's distribution function comes from Abramowitz and Stegun's formula 7.1.26
+// for erf (off by 1.5e-7 at most): it needs one reciprocal and the exponential that its derivative needs anyway, and takes the
+// lower tail as a product, so nothing cancels there.
+template <int ACT> __device__ __forceinline__ void activate(float2 z, float2 &a, float2 &slope) {
     if (ACT == SCAR_ACT_IDENTITY) {
         a = z;
-        slope = 1.f;
+        slope = both(1.f);
     } else if (ACT == SCAR_ACT_RELU) {
-        slope = z > 0.f ? 1.f : 0.f;
-        a = z < 0.f ? 0.f : z;  // a NaN stays one
+        slope = make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
+        a = make_float2(z.x < 0.f ? 0.f : z.x, z.y < 0.f ? 0.f : z.y);  // a NaN stays one
     } else if (ACT == SCAR_ACT_GELU) {
-        const float e = exp2f(z * z * -0.72134752f);  // exp(-z^2 / 2)
-        const float t = __frcp_rn(fmaf(0.23164189f, fabsf(z), 1.f));  // 1 / (1 + 0.3275911 |z| / sqrt 2)
-        float p = fmaf(t, 1.061405429f, -1.453152027f);
-        p = fmaf(t, p, 1.421413741f);
-        p = fmaf(t, p, -0.284496736f);
-        p = fmaf(t, p, 0.254829592f);
-        const float tail = 0.5f * p * t * e;  // of the distribution beyond |z|
-        const float cdf = z < 0.f ? tail : 1.f - tail;
-        a = z * cdf;
-        slope = fmaf(z * 0.39894228f, e, cdf);
+        const float2 e = ex2_pair(mul2(mul2(z, z), both(-0.72134752f)));  // exp(-z^2 / 2)
+        const float2 t = rcp_pair(fma2(make_float2(fabsf(z.x), fabsf(z.y)), both(0.23164189f), both(1.f)));  // 1 / (1 + 0.3275911 |z| / sqrt 2)
+        // half of the formula's coefficients: the distribution beyond |z|
+        float2 p = fma2(t, both(0.5307027145f), both(-0.7265760135f));
+        p = fma2(t, p, both(0.7107068705f));
+        p = fma2(t, p, both(-0.142248368f));
+        p = fma2(t, p, both(0.127414796f));
+        const float2 tail = mul2(mul2(p, t), e);
+        const float2 body = fma2(tail, both(-1.f), both(1.f));
+        const float2 cdf = make_float2(z.x < 0.f ? tail.x : body.x, z.y < 0.f ? tail.y : body.y);
+        a = mul2(z, cdf);
+        slope = fma2(mul2(z, both(0.39894228f)), e, cdf);
     } else {
-        const float s = __fdividef(1.f, 1.f + __expf(-z));
-        a = z * s;
-        slope = s * fmaf(z, 1.f - s, 1.f);
+        const float2 s = rcp_pair(add2(ex2_pair(mul2(z, both(-1.4426950409f))), both(1.f)));
+        a = mul2(z, s);
+        slope = mul2(s, fma2(z, fma2(s, both(-1.f), both(1.f)), both(1.f)));
     }
 }
 

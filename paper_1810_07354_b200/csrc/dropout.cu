@@ -66,12 +66,12 @@ __global__ void __launch_bounds__(kThreads) k_dropout_words(const __grid_constan
     const unsigned long long offset = g.rule.at();
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        const uint4 bits = mask_bits(g.rule, offset, row[i], block[i]);
+        float2 v[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float v = mask_apply(g.rule, bits, j, to_f32(x[i].v[j]));
-            x[i].v[j] = from_f32<T>(RES ? to_f32(r[i].v[j]) + v : v);
-        }
+        for (int j = 0; j < 4; ++j) v[j] = Two<T>::get(x[i].v + 2 * j);
+        if (g.rule.on) mask_apply(g.rule, mask_bits(g.rule, offset, row[i], block[i]), v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) Two<T>::put(x[i].v + 2 * j, RES ? add2(Two<T>::get(r[i].v + 2 * j), v[j]) : v[j]);
         T *py = g.y + row[i] * g.y_pitch + block[i] * 8ull;
         if (left[i] == 8) {
             store8(py, x[i]);

@@ -76,17 +76,19 @@ __global__ void __launch_bounds__(128) k_linear_join(const __grid_constant__ TcA
     const LayerArgs &l = g.layer;
     const unsigned m = rows_of(g), pitch = (g.n + 7) & ~7u, groups = pitch / 8, splits = parts_of(g);
     const unsigned long long stride = (unsigned long long)g.m * pitch, total = (unsigned long long)m * groups;
-    const unsigned long long offset = l.drop.cut ? l.drop.at() : 0ull;
+    const unsigned long long offset = l.drop.on ? l.drop.at() : 0ull;
     for (unsigned long long i = (unsigned long long)blockIdx.x * 128 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 128) {
         const unsigned row = total >> 32 ? (unsigned)(i / groups) : (unsigned)i / groups;
         const unsigned col = (unsigned)(i - (unsigned long long)row * groups) * 8;
         const float *p = g.part + (unsigned long long)row * pitch + col;
-        float z[8] = {}, slope[8];
+        float2 z[4] = {}, slope[4];
 #pragma unroll 2
         for (unsigned s = 0; s < splits; ++s) {
             const float4 a = *reinterpret_cast<const float4 *>(p + s * stride), b = *reinterpret_cast<const float4 *>(p + s * stride + 4);
-            z[0] += a.x; z[1] += a.y; z[2] += a.z; z[3] += a.w;
-            z[4] += b.x; z[5] += b.y; z[6] += b.z; z[7] += b.w;
+            z[0] = add2(z[0], make_float2(a.x, a.y));
+            z[1] = add2(z[1], make_float2(a.z, a.w));
+            z[2] = add2(z[2], make_float2(b.x, b.y));
+            z[3] = add2(z[3], make_float2(b.z, b.w));
         }
         Pack8<T> r;
         if (l.res) r = row8(static_cast<const T *>(l.res) + row * l.res_pitch, col, g.n, l.res_vec);
@@ -95,15 +97,15 @@ __global__ void __launch_bounds__(128) k_linear_join(const __grid_constant__ TcA
             const unsigned long long at = (unsigned long long)row * pitch + col;
             if constexpr (sizeof(T) == 4) {
                 float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(l.slope) + at);
-                o[0] = make_float4(slope[0], slope[1], slope[2], slope[3]);
-                o[1] = make_float4(slope[4], slope[5], slope[6], slope[7]);
+                o[0] = make_float4(slope[0].x, slope[0].y, slope[1].x, slope[1].y);
+                o[1] = make_float4(slope[2].x, slope[2].y, slope[3].x, slope[3].y);
             } else {
-                *reinterpret_cast<uint4 *>(static_cast<unsigned short *>(l.slope) + at) = pack_half8(slope);
+                *reinterpret_cast<uint4 *>(static_cast<unsigned short *>(l.slope) + at) = pack8<__half>(slope);
             }
         }
         Pack8<T> y;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y.v[j] = from_f32<T>(l.res ? to_f32(r.v[j]) + z[j] : z[j]);
+        for (int j = 0; j < 4; ++j) Two<T>::put(y.v + 2 * j, l.res ? add2(Two<T>::get(r.v + 2 * j), z[j]) : z[j]);
         put8(static_cast<T *>(g.out) + row * g.out_pitch, col, g.n, g.out_vec, y);
     }
 }
@@ -130,45 +132,42 @@ __global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArg
     griddep_start();
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 256 + lane * 8;
     const unsigned r1 = min(g.rows, (blockIdx.y + 1) * g.per_cta);
-    const unsigned long long offset = g.drop.cut ? g.drop.at() : 0ull;
-    float sum[8] = {};
+    const unsigned long long offset = g.drop.on ? g.drop.at() : 0ull;
+    using S = typename std::conditional<sizeof(T) == 4, float, __half>::type;
+    float2 sum[4] = {};
     if (col < g.n) {
         for (unsigned r0 = blockIdx.y * g.per_cta + warp; r0 < r1; r0 += 8 * kDzRows) {
             Pack8<T> d[kDzRows];
-            Pack8<typename std::conditional<sizeof(T) == 4, float, __half>::type> s[kDzRows];
+            Pack8<S> s[kDzRows];
 #pragma unroll
             for (int k = 0; k < kDzRows; ++k) {
                 const unsigned r = r0 + k * 8;
                 if (r >= r1) continue;
                 d[k] = row8(g.dy + r * g.dy_pitch, col, g.n, g.vec);
-                if (g.slope) s[k] = row8(static_cast<const typename std::conditional<sizeof(T) == 4, float, __half>::type *>(g.slope) + r * (unsigned long long)g.np, col, g.np, true);
+                if (g.slope) s[k] = row8(static_cast<const S *>(g.slope) + r * (unsigned long long)g.np, col, g.np, true);
             }
 #pragma unroll
             for (int k = 0; k < kDzRows; ++k) {
                 const unsigned r = r0 + k * 8;
                 if (r >= r1) continue;
-                float z[8];
+                float2 z[4];  // zeros behind the row: row8 fills up with them
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] = col + j < g.n ? to_f32(d[k].v[j]) : 0.f;
-                if (g.drop.cut) {
-                    const uint4 bits = mask_bits(g.drop, offset, r, col >> 3);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) z[j] = mask_apply(g.drop, bits, j, z[j]);
-                }
+                for (int j = 0; j < 4; ++j) z[j] = Two<T>::get(d[k].v + 2 * j);
                 if (g.slope) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) z[j] = col + j < g.n ? z[j] * to_f32(s[k].v[j]) : 0.f;
+                    for (int j = 0; j < 4; ++j) z[j] = mul2(z[j], Two<S>::get(s[k].v + 2 * j));
                 }
+                if (g.drop.on) mask_apply(g.drop, mask_bits(g.drop, offset, r, col >> 3), z);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += z[j];
+                for (int j = 0; j < 4; ++j) sum[j] = add2(sum[j], z[j]);
                 if (!g.dz) continue;
                 unsigned short *o = g.dz + r * (unsigned long long)g.np + col;
                 if constexpr (sizeof(T) == 2) {
-                    *reinterpret_cast<uint4 *>(o) = std::is_same<T, __half>::value ? pack_half8(z) : pack_bf8(z);
+                    *reinterpret_cast<uint4 *>(o) = pack8<T>(z);
                 } else {
                     Eight p[3];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) split3(z[j], p[0].b[j], p[1].b[j], p[2].b[j]);
+                    for (int j = 0; j < 8; ++j) split3(j & 1 ? z[j / 2].y : z[j / 2].x, p[0].b[j], p[1].b[j], p[2].b[j]);
 #pragma unroll
                     for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(o + q * g.plane) = p[q].u;
                 }
@@ -177,7 +176,7 @@ __global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArg
     }
     if (!g.dbias) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[warp][lane * 8 + j] = sum[j];
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<float2 *>(&sums[warp][lane * 8 + 2 * j]) = sum[j];
     __syncthreads();
     const unsigned c = blockIdx.x * 256 + threadIdx.x;
     float v = 0.f;
@@ -349,7 +348,7 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
         return SCAR_OK;
     }
     // dy itself where nothing changes it
-    const bool direct = PL == 1 && !slope && !drop.cut && rows_aligned(dy, dyp, 2);
+    const bool direct = PL == 1 && !slope && !drop.on && rows_aligned(dy, dyp, 2);
     const uint64_t dz_rows = std::max<uint64_t>(op->cfg.max_rows, 1);
     if (!direct && !op->dz && (rc = linear_alloc(op, &op->dz, PL * dz_rows * op->np * 2)) != SCAR_OK) return rc;
     if (!direct || dbias) {

@@ -8,14 +8,15 @@
 #pragma once
 #include <cmath>
 
-#include "train_common.cuh"
+#include "pairs.cuh"
 
 namespace scar {
 
 struct DropRule {
     unsigned key0, key1;
-    unsigned cut;  // a value is kept if its 16 bits are at least this: 0 keeps all, 65536 none
-    float scale;   // of what is kept
+    int on;          // something is dropped
+    unsigned above;  // 65536 cut - 1: a value is kept if its 16 bits, as the upper half of a word, are above this
+    float scale;     // of what is kept
     unsigned long long offset;
     const unsigned long long *d_offset;  // added to it, or nullptr
     __device__ __forceinline__ unsigned long long at() const { return offset + (d_offset ? *d_offset : 0ull); }
@@ -24,13 +25,13 @@ struct DropRule {
 // SCAR_OK, or what is wrong with the caller's rule (nullptr: nothing is dropped).  The probability is taken to the nearest
 // multiple of 2^-16 that is neither 0 nor 1 unless it is 0 or 1 itself; the scale is of the one taken, so means are kept.
 inline int make_rule(const scar_dropout *d, DropRule *out) {
-    *out = DropRule{0, 0, 0, 1.f, 0, nullptr};
+    *out = DropRule{0, 0, 0, 0, 1.f, 0, nullptr};
     if (!d) return SCAR_OK;
     if (!(d->p >= 0. && d->p <= 1.) || (uintptr_t)d->d_offset % 8) return SCAR_ERR_INVALID_ARG;
     unsigned cut = (unsigned)std::floor(d->p * 65536. + 0.5);
     if (d->p > 0. && cut == 0) cut = 1;
     if (d->p < 1. && cut == 65536) cut = 65535;
-    *out = DropRule{(unsigned)d->seed, (unsigned)(d->seed >> 32), cut, cut == 65536 ? 0.f : 65536.f / (float)(65536 - cut), d->offset,
+    *out = DropRule{(unsigned)d->seed, (unsigned)(d->seed >> 32), cut != 0, cut * 65536u - 1u, cut == 65536 ? 0.f : 65536.f / (float)(65536 - cut), d->offset,
                     reinterpret_cast<const unsigned long long *>(d->d_offset)};
     return SCAR_OK;
 }
@@ -50,10 +51,19 @@ __device__ __forceinline__ uint4 mask_bits(const DropRule &r, unsigned long long
 }
 __device__ __forceinline__ bool mask_keeps(const DropRule &r, const uint4 &bits, int j) {
     const unsigned w = j < 2 ? bits.x : j < 4 ? bits.y : j < 6 ? bits.z : bits.w;
-    return (j & 1 ? w >> 16 : w & 0xffffu) >= r.cut;
+    return !r.on || (j & 1 ? w : w << 16) > r.above;
 }
-// x as the mask leaves it: what is dropped is 0 whatever it was.
-__device__ __forceinline__ float mask_apply(const DropRule &r, const uint4 &bits, int j, float x) { return mask_keeps(r, bits, j) ? x * r.scale : 0.f; }
+// Eight neighbours as the mask leaves them: what is dropped is 0 whatever it was.
+__device__ __forceinline__ void mask_apply(const DropRule &r, const uint4 &bits, float2 (&x)[4]) {
+    const unsigned w[4] = {bits.x, bits.y, bits.z, bits.w};
+    const float2 scale = both(r.scale);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 y = mul2(x[j], scale);
+        x[j].x = (w[j] << 16) > r.above ? y.x : 0.f;
+        x[j].y = w[j] > r.above ? y.y : 0.f;
+    }
+}
 // Bit j of the result: column j is kept.
 __device__ __forceinline__ unsigned mask_byte(const DropRule &r, const uint4 &bits) {
     unsigned m = 0;

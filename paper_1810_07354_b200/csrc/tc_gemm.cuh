@@ -28,8 +28,6 @@
 namespace scar {
 
 constexpr int kBM = 256, kBK = 64;  // a pair's rows of A, and k per stage
-constexpr int kEpiWarps = 8;
-constexpr int kGemmThreads = (kEpiWarps + 2) * 32;
 
 enum class Epi { kPart, kOut, kProb, kStat, kIdentity, kRelu, kGelu, kSilu };  // the last four: a layer's output, by its activation
 __host__ __device__ constexpr bool is_layer(Epi e) { return e >= Epi::kIdentity; }
@@ -50,7 +48,15 @@ constexpr int kBN = 256;
 constexpr int kAccs = 512 / kBN;
 constexpr int kCols = kBN / 2;        // columns of one epilogue thread
 constexpr int kWarpStage = 32 * 128;  // epilogue: 32 rows of 128 bytes per warp, on their way to memory
-constexpr int kTcSmem = 6 * 2 * 128 * kBK * 2 + kEpiWarps * kWarpStage + 1024;
+// A layer's epilogue computes more per value than there is time for beside the products of 1024 values of k with eight warps (two per
+// scheduler): 16 of 64 columns each, for one stage of operands less (8192 x 1024 -> 4096 bfloat16, GELU and dropout: 175 us with eight).
+template <Epi EPI> struct EpiShape {
+    static constexpr int kWarps = is_layer(EPI) ? 16 : 8;
+    static constexpr int kThreads = (kWarps + 2) * 32;
+};
+template <int PL, Epi EPI> constexpr int kStagesOf = is_layer(EPI) ? 5 : TcShape<PL>::kStages;
+constexpr int kTcSmem = 6 * 2 * 128 * kBK * 2 + 8 * kWarpStage + 1024;
+static_assert(5 * TcShape<1>::kStageBytes + 16 * kWarpStage + 1024 == kTcSmem, "both shapes fill the same");
 static_assert(TcShape<1>::kStages * TcShape<1>::kStageBytes == TcShape<3>::kStages * TcShape<3>::kStageBytes, "both fill 192 KiB");
 
 // What a layer's epilogue adds to its product (kIdentity .. kSilu; k_linear_join where the sum was split).
@@ -571,108 +577,133 @@ template <typename F> __device__ __forceinline__ void store_halves(const CUtenso
     }
 }
 
-// 64 columns of 32 rows of 16-bit values from memory into the stage, a line per eight lanes, and from there this lane's row.
-__device__ __forceinline__ void stage_read16(uint8_t *stage, const unsigned short *base, unsigned long long pitch, bool vec, const EpiRows &rows, unsigned left, unsigned lane, Chunk (&x)[8]) {
-    stage_free();
-    if (vec && left >= 64) {
-        const unsigned c = lane & 7;
-        uint4 v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const unsigned r = i * 4 + (lane >> 3);
-            v[i] = rows.has(r) ? *reinterpret_cast<const uint4 *>(base + (rows.row0 + r) * pitch + c * 8) : make_uint4(0, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) *stage_at(stage, i * 4 + (lane >> 3), c) = v[i];
-    } else {
-        unsigned short *st = reinterpret_cast<unsigned short *>(stage);
-#pragma unroll 8
-        for (unsigned r = 0; r < 32; ++r) {
-            const unsigned short *p = base + (rows.row0 + r) * pitch;
-#pragma unroll
-            for (unsigned h = 0; h < 64; h += 32) {
-                const unsigned c = h + lane;
-                st[r * 64 + (((c >> 3) ^ (r & 7)) << 3) + (c & 7)] = rows.has(r) && c < left ? p[c] : (unsigned short)0;
-            }
-        }
-    }
-    __syncwarp();
-#pragma unroll
-    for (int c = 0; c < 8; ++c) x[c].u = *stage_at(stage, lane, c);
-}
-
 // Eight values of the bias from column col on, zeros behind the last one.
-template <typename T> __device__ __forceinline__ void bias8(const LayerArgs &l, unsigned col, unsigned n, float (&b)[8]) {
+template <typename T> __device__ __forceinline__ void bias8(const LayerArgs &l, unsigned col, unsigned n, float2 (&b)[4]) {
     const T *p = static_cast<const T *>(l.bias) + col;
+    union {
+        uint4 u[sizeof(T) / 2];
+        T v[8];
+    } x;
     if (l.bias_vec && col + 8 <= n) {
-        union {
-            uint4 u[sizeof(T) / 2];
-            T v[8];
-        } x;
 #pragma unroll
         for (unsigned i = 0; i < sizeof(T) / 2; ++i) x.u[i] = reinterpret_cast<const uint4 *>(p)[i];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = to_f32(x.v[j]);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = col + j < n ? to_f32(p[j]) : 0.f;
+        for (int j = 0; j < 8; ++j) x.v[j] = col + j < n ? p[j] : from_f32<T>(0.f);
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = Two<T>::get(x.v + 2 * j);
 }
 
 // Eight products of a row become the layer's values (without the residual); slope: their derivatives.
-template <int ACT, typename T> __device__ __forceinline__ void layer8(const LayerArgs &l, unsigned long long offset, unsigned row, unsigned col, unsigned n, float *z, float *slope) {
+template <int ACT, typename T> __device__ __forceinline__ void layer8(const LayerArgs &l, unsigned long long offset, unsigned row, unsigned col, unsigned n, float2 (&z)[4], float2 (&slope)[4]) {
     if (l.bias) {
-        float b[8];
+        float2 b[4];
         bias8<T>(l, col, n, b);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] += b[j];
+        for (int j = 0; j < 4; ++j) z[j] = add2(z[j], b[j]);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) activate<ACT>(z[j], z[j], slope[j]);
-    if (l.drop.cut) {
-        const uint4 bits = mask_bits(l.drop, offset, row, col >> 3);
+    for (int j = 0; j < 4; ++j) activate<ACT>(z[j], z[j], slope[j]);
+    if (l.drop.on) mask_apply(l.drop, mask_bits(l.drop, offset, row, col >> 3), z);
+}
+template <typename T> __device__ __forceinline__ uint4 pack8(const float2 (&v)[4]) {
+    union {
+        T v[8];
+        uint4 u;
+    } x;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = mask_apply(l.drop, bits, j, z[j]);
-    }
+    for (int j = 0; j < 4; ++j) Two<T>::put(x.v + 2 * j, v[j]);
+    return x.u;
 }
 
-// A tile's 128 columns of this thread's row, 64 at a time, from the accumulator to the layer's output and slope (16-bit types).
-template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const TcArgs &g, uint32_t acc, bool any, const EpiRows &rows, unsigned col, uint8_t *stage, unsigned &half, unsigned lane) {
+// A warp's stage in a layer's epilogue: two halves of 32 rows of 32 16-bit values, 64 bytes a row; 16-byte chunk c of row r lies at
+// chunk c ^ (r / 2 & 3), the swizzle of the results' maps.
+__device__ __forceinline__ uint4 *half_at(uint8_t *half, unsigned row, unsigned c) { return reinterpret_cast<uint4 *>(half + row * 64 + ((c ^ (row >> 1 & 3)) << 4)); }
+
+// 32 columns of 32 rows from memory into a half, and from there this lane's row.
+__device__ __forceinline__ void half_read(uint8_t *half, const unsigned short *base, unsigned long long pitch, bool vec, const EpiRows &rows, unsigned left, unsigned lane, uint4 (&x)[4]) {
+    if (vec && left >= 32) {
+        uint4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned r = i * 8 + (lane >> 2);
+            v[i] = rows.has(r) ? *reinterpret_cast<const uint4 *>(base + (rows.row0 + r) * pitch + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *half_at(half, i * 8 + (lane >> 2), lane & 3) = v[i];
+    } else {
+#pragma unroll 8
+        for (unsigned r = 0; r < 32; ++r)
+            reinterpret_cast<unsigned short *>(half_at(half, r, lane >> 3))[lane & 7] =
+                rows.has(r) && lane < left ? base[(rows.row0 + r) * pitch + lane] : (unsigned short)0;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 4; ++c) x[c] = *half_at(half, lane, c);
+    __syncwarp();
+}
+// The way back, for results that no map stores: any row may begin between two 4-byte words; of the 16 lanes of a row, lane l then
+// takes columns 2l + 1 and 2l + 2, and the first one column 0.
+__device__ __forceinline__ void half_write(uint8_t *half, unsigned short *base, unsigned long long pitch, bool vec, const EpiRows &rows, unsigned left, unsigned lane) {
+    __syncwarp();
+    if (vec && left >= 32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned r = i * 8 + (lane >> 2);
+            const uint4 x = *half_at(half, r, lane & 3);
+            if (rows.has(r)) *reinterpret_cast<uint4 *>(base + (rows.row0 + r) * pitch + (lane & 3) * 8) = x;
+        }
+    } else {
+        const auto at = [&](unsigned r, unsigned c) { return reinterpret_cast<const unsigned short *>(half_at(half, r, c >> 3))[c & 7]; };
+#pragma unroll 4
+        for (unsigned i = 0; i < 32; i += 2) {
+            const unsigned r = i + (lane >> 4), l = lane & 15;
+            unsigned short *o = base + (rows.row0 + r) * pitch;
+            const unsigned odd = (unsigned)((uintptr_t)o >> 1) & 1u, a = 2 * l + odd, b = a + 1;
+            const unsigned short x = at(r, a), y = b < 32 ? at(r, b) : (unsigned short)0;
+            if (!rows.has(r)) continue;
+            if (b < 32 && b < left) *reinterpret_cast<unsigned *>(o + a) = (unsigned)x | (unsigned)y << 16;
+            else if (a < left) o[a] = x;
+            if (odd && l == 0 && left) o[0] = at(r, 0);
+        }
+    }
+    __syncwarp();
+}
+
+// A tile's 64 columns of this thread's row, 32 at a time, from the accumulator to the layer's output and slope (16-bit types).
+template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const TcArgs &g, uint32_t acc, bool any, const EpiRows &rows, unsigned col, uint8_t *stage, unsigned lane) {
     const LayerArgs &l = g.layer;
-    const unsigned long long offset = l.drop.cut ? l.drop.at() : 0ull;
+    const unsigned long long offset = l.drop.on ? l.drop.at() : 0ull;
+    uint8_t *const out = stage, *const der = stage + 2048;
 #pragma unroll 1
-    for (unsigned j = 0; j < kCols && col + j < g.n; j += 64) {
-        const unsigned at = col + j, left = g.n - at;
-        Chunk y[8], s[8];  // packed results and slopes
-        if (l.res) stage_read16(stage, static_cast<const unsigned short *>(l.res) + at, l.res_pitch, l.res_vec, rows, left, lane, y);
+    for (unsigned j = 0; j < 64; j += 32) {
+        const unsigned at = col + j;
+        if (at >= g.n) break;
+        const unsigned left = g.n - at;
+        float v[32] = {};
+        if (any) tmem_load32(acc + j, v);
+        stage_free();
+        uint4 r[4];
+        if (l.res) half_read(out, static_cast<const unsigned short *>(l.res) + at, l.res_pitch, l.res_vec, rows, left, lane, r);
+        if (any) tmem_loaded(v);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float v[32] = {};
-            if (any) {
-                tmem_load32(acc + j + h * 32, v);
-                tmem_loaded(v);
+        for (int c = 0; c < 4; ++c) {
+            float2 z[4], slope[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = make_float2(v[c * 8 + 2 * i], v[c * 8 + 2 * i + 1]);
+            layer8<ACT, T>(l, offset, rows.row0 + lane, at + c * 8, g.n, z, slope);
+            if (l.res) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = add2(z[i], Two<T>::get(reinterpret_cast<const T *>(r + c) + 2 * i));
             }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                float slope[8];
-                layer8<ACT, T>(l, offset, rows.row0 + lane, at + h * 32 + c * 8, g.n, v + c * 8, slope);
-                Chunk &o = y[h * 4 + c];
-                if (l.res) {
-                    const T *r = reinterpret_cast<const T *>(&o);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[c * 8 + i] += to_f32(r[i]);
-                }
-                o.u = std::is_same<T, __half>::value ? pack_half8(v + c * 8) : pack_bf8(v + c * 8);
-                if (l.slope) s[h * 4 + c].u = pack_half8(slope);
-            }
+            *half_at(out, lane, c) = pack8<T>(z);
+            if (l.slope) *half_at(der, lane, c) = pack8<__half>(slope);
         }
-        if (l.slope) store_halves(&l.slope_map, stage, half, lane, rows.has(0), left, (int)at, (int)rows.row0, [&](int c) { return s[c].u; });
-        if (g.c_map) {
-            store_halves(&g.c, stage, half, lane, rows.has(0), left, (int)at, (int)rows.row0, [&](int c) { return y[c].u; });
-        } else {
-            stage_fill(stage, lane, [&](int c) { return y[c].u; });
-            flush16(stage, static_cast<unsigned short *>(g.out) + at, g.out_pitch, g.out_vec, rows, left, lane);
-        }
+        if (!rows.has(0)) continue;
+        if (l.slope) tma_store(&l.slope_map, smem_addr(der), (int)at, (int)rows.row0, 0);
+        if (g.c_map) tma_store(&g.c, smem_addr(out), (int)at, (int)rows.row0, 0);
+        else half_write(out, static_cast<unsigned short *>(g.out) + at, g.out_pitch, g.out_vec, rows, left, lane);
     }
 }
 
@@ -682,26 +713,27 @@ template <int N> struct TcSet {
 };
 // static: every unit that launches it has instances of its own
 template <int PL, bool A_MN, bool B_MN, Epi EPI, int N>
-static __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
+static __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(EpiShape<EPI>::kThreads, 1)
 k_tc_gemm(const __grid_constant__ TcSet<N> set) {
     using S = TcShape<PL>;
+    constexpr int kStages = kStagesOf<PL, EPI>, kEpiWarps = EpiShape<EPI>::kWarps;
     __shared__ TileWalk walks[N];
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ __align__(8) unsigned long long bars[2 * S::kStages + 2 * kAccs];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 2 * kAccs];
     __shared__ uint32_t tmem_base;
     constexpr bool kLogits = EPI == Epi::kProb || EPI == Epi::kStat;
     constexpr unsigned kPer = PL == 3 ? 1u : kLogits ? kRound : 0xffffffffu;  // stages per accumulator
     const uint32_t stage0 = smem_addr(smem);
-    const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages;
-    const uint32_t acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 8 * kAccs;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages;
+    const uint32_t acc_full = empty + 8 * kStages, acc_empty = acc_full + 8 * kAccs;
     const unsigned warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const unsigned pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
-        for (int i = 0; i < S::kStages; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
         }
@@ -762,7 +794,7 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
                     }
                 }
                 __syncwarp();
-                if (++st == S::kStages) {
+                if (++st == kStages) {
                     st = 0;
                     ph ^= 1;
                 }
@@ -807,7 +839,7 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
                         if (left == 0) mma_commit(acc_full + 8 * ac);
                     }
                     __syncwarp();
-                    if (++st == S::kStages) {
+                    if (++st == kStages) {
                         st = 0;
                         ph ^= 1;
                     }
@@ -820,14 +852,14 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
         }
     } else if (warp < kEpiWarps) {  // epilogue
         const unsigned quad = warp & 3, half = warp >> 2;
-        uint8_t *stage = smem + S::kStages * S::kStageBytes + warp * kWarpStage;
+        uint8_t *stage = smem + kStages * S::kStageBytes + warp * kWarpStage;
         constexpr bool kRegs = PL == 3 || kLogits;  // sums over rounds, or a whole row at a time: all columns in registers
         unsigned ac = 0, aph = 0;
         unsigned half_next = 0;  // of the stage, for store_halves
         for (unsigned i = 0; take_turn<N>(walks, i, pair, pairs, t); ++i) {
             const TcArgs &g = set.p[N == 1 ? 0 : t.which];
             const unsigned rounds = t.k1 > t.k0 ? (kPer == 1 ? t.k1 - t.k0 : (t.k1 - t.k0 - 1) / kPer + 1) : 0u;
-            const uint32_t lanes = tmem + half * kCols + (quad * 32u << 16);
+            const uint32_t lanes = tmem + half * (is_layer(EPI) ? 64 : kCols) + (quad * 32u << 16);
             if constexpr (kRegs) {
                 float v[kCols];
                 if (rounds == 0) {
@@ -911,15 +943,15 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
                 }
             } else {
                 const EpiRows rows = epi_rows<EPI>(g, walks[t.which].m, t.mi * kBM + rank * 128 + quad * 32, t.s, lane);
-                const unsigned col = t.ni * kBN + half * kCols;
+                const unsigned col = t.ni * kBN + half * (is_layer(EPI) ? 64 : kCols);
                 if constexpr (is_layer(EPI)) {
                     if (rounds) {
                         ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, error));
                         if (!ok) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     }
-                    if (g.bf16) epi_layer<act_of(EPI), __nv_bfloat16>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, half_next, lane);
-                    else epi_layer<act_of(EPI), __half>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, half_next, lane);
+                    if (g.bf16) epi_layer<act_of(EPI), __nv_bfloat16>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, lane);
+                    else epi_layer<act_of(EPI), __half>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, lane);
                     if (rounds) {
                         acc_release(acc_empty + 8 * ac, lane);
                         if (++ac == kAccs) {

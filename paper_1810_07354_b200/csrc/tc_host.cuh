@@ -224,7 +224,7 @@ template <int PL, bool A_MN, bool B_MN, Epi EPI> void launch_tc(TcHost *op, TcAr
         if (make_map(op, &g.c, {g.part, pitch, g.m, pitch, g.splits > 1 ? g.most_splits : 1u, g.m * pitch}, 32, 4) != SCAR_OK) op->failed = true;
     }
     const unsigned pairs = (unsigned)std::min<uint64_t>(tiles_of(g), op->pairs);
-    if (pairs) launch(op, k_tc_gemm<PL, A_MN, B_MN, EPI, 1>, 2 * pairs, kGemmThreads, kTcSmem, TcSet<1>{g});
+    if (pairs) launch(op, k_tc_gemm<PL, A_MN, B_MN, EPI, 1>, 2 * pairs, EpiShape<EPI>::kThreads, kTcSmem, TcSet<1>{g});
 }
 
 template <typename K> bool allow_smem(K kernel) {
@@ -260,7 +260,7 @@ template <int PL> void launch_grads(TcHost *op, TcArgs dhg, TcArgs dwg, bool thr
                                           : (float)((tiles0 + pairs - 1) / pairs) * tile0 + (float)((tiles1 + pairs - 1) / pairs) * tile1;
     if (!through_w && together <= apart) {
         dhg.splits = dwg.splits = 1;
-        launch(op, k_tc_gemm<PL, false, true, Epi::kOut, 2>, 2 * (unsigned)std::min<uint64_t>(tiles0 + tiles1, pairs), kGemmThreads, kTcSmem, TcSet<2>{{dhg, dwg}});
+        launch(op, k_tc_gemm<PL, false, true, Epi::kOut, 2>, 2 * (unsigned)std::min<uint64_t>(tiles0 + tiles1, pairs), EpiShape<Epi::kOut>::kThreads, kTcSmem, TcSet<2>{{dhg, dwg}});
         return;
     }
     launch_out<PL, false>(op, dhg);
