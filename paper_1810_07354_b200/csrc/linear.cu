@@ -69,6 +69,29 @@ template <typename T> __device__ __forceinline__ void put8(T *row, unsigned c, u
         if (c + j < n) row[c + j] = x.v[j];
 }
 
+// Eight products of a row to the layer's output and slope.
+template <typename T, int ACT>
+__device__ __forceinline__ void finish8(const LayerArgs &l, T *out, unsigned long long out_pitch, bool out_vec, unsigned n, unsigned row, unsigned col, unsigned long long offset, float2 (&z)[4]) {
+    float2 slope[4];
+    Pack8<T> r;
+    if (l.res) r = row8(static_cast<const T *>(l.res) + row * l.res_pitch, col, n, l.res_vec);
+    layer8<ACT, T>(l, offset, row, col, n, z, slope);
+    if (l.slope) {
+        const unsigned long long at = (unsigned long long)row * ((n + 7) & ~7u) + col;
+        if constexpr (sizeof(T) == 4) {
+            float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(l.slope) + at);
+            o[0] = make_float4(slope[0].x, slope[0].y, slope[1].x, slope[1].y);
+            o[1] = make_float4(slope[2].x, slope[2].y, slope[3].x, slope[3].y);
+        } else {
+            *reinterpret_cast<uint4 *>(static_cast<unsigned short *>(l.slope) + at) = pack8<__half>(slope);
+        }
+    }
+    Pack8<T> y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) Two<T>::put(y.v + 2 * j, l.res ? add2(Two<T>::get(r.v + 2 * j), z[j]) : z[j]);
+    put8(out + row * out_pitch, col, n, out_vec, y);
+}
+
 // The parts of a product whose sum was split (or its float32 result) to the layer's output: what epi_layer does without a split.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(128) k_linear_join(const __grid_constant__ TcArgs g) {
@@ -81,7 +104,7 @@ __global__ void __launch_bounds__(128) k_linear_join(const __grid_constant__ TcA
         const unsigned row = total >> 32 ? (unsigned)(i / groups) : (unsigned)i / groups;
         const unsigned col = (unsigned)(i - (unsigned long long)row * groups) * 8;
         const float *p = g.part + (unsigned long long)row * pitch + col;
-        float2 z[4] = {}, slope[4];
+        float2 z[4] = {};
 #pragma unroll 2
         for (unsigned s = 0; s < splits; ++s) {
             const float4 a = *reinterpret_cast<const float4 *>(p + s * stride), b = *reinterpret_cast<const float4 *>(p + s * stride + 4);
@@ -90,23 +113,222 @@ __global__ void __launch_bounds__(128) k_linear_join(const __grid_constant__ TcA
             z[2] = add2(z[2], make_float2(b.x, b.y));
             z[3] = add2(z[3], make_float2(b.z, b.w));
         }
-        Pack8<T> r;
-        if (l.res) r = row8(static_cast<const T *>(l.res) + row * l.res_pitch, col, g.n, l.res_vec);
-        layer8<ACT, T>(l, offset, row, col, g.n, z, slope);
-        if (l.slope) {
-            const unsigned long long at = (unsigned long long)row * pitch + col;
-            if constexpr (sizeof(T) == 4) {
-                float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(l.slope) + at);
-                o[0] = make_float4(slope[0].x, slope[0].y, slope[1].x, slope[1].y);
-                o[1] = make_float4(slope[2].x, slope[2].y, slope[3].x, slope[3].y);
-            } else {
-                *reinterpret_cast<uint4 *>(static_cast<unsigned short *>(l.slope) + at) = pack8<__half>(slope);
+        finish8<T, ACT>(l, static_cast<T *>(g.out), g.out_pitch, g.out_vec, g.n, row, col, offset, z);
+    }
+}
+
+// ---- Few rows: reading w is everything, so no tile of 256 rows is filled up with zeros.  A CTA has 32 rows of w (eight in
+// float32), its eight warps take turns at the k they read, every load is 16 bytes a lane, and the warps' sums meet in shared
+// memory, where the layer's epilogue takes them.
+template <typename T> struct FewArgs {
+    const T *x, *w;
+    unsigned long long x_pitch, w_pitch;
+    unsigned rows, n, k;
+    unsigned parts;  // CTAs of a cluster that share the sum over k (16-bit types)
+    int act;
+    T *out;
+    unsigned long long out_pitch;
+    int out_vec;
+    LayerArgs layer;
+};
+// The sums `at` of eight columns of a row in every warp's block of `size` floats.
+__device__ __forceinline__ void add_warps(const float *at, unsigned size, float2 (&z)[4]) {
+#pragma unroll
+    for (unsigned w = 0; w < 8; ++w) {
+        const float4 a = *reinterpret_cast<const float4 *>(at + w * size), b = *reinterpret_cast<const float4 *>(at + w * size + 4);
+        z[0] = add2(z[0], make_float2(a.x, a.y));
+        z[1] = add2(z[1], make_float2(a.z, a.w));
+        z[2] = add2(z[2], make_float2(b.x, b.y));
+        z[3] = add2(z[3], make_float2(b.z, b.w));
+    }
+}
+template <typename T> __device__ __forceinline__ void finish_few(const FewArgs<T> &g, unsigned row, unsigned col, float2 (&z)[4]) {
+    const unsigned long long offset = g.layer.drop.on ? g.layer.drop.at() : 0ull;
+    if (g.act == SCAR_ACT_IDENTITY) finish8<T, SCAR_ACT_IDENTITY>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z);
+    else if (g.act == SCAR_ACT_RELU) finish8<T, SCAR_ACT_RELU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z);
+    else if (g.act == SCAR_ACT_GELU) finish8<T, SCAR_ACT_GELU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z);
+    else finish8<T, SCAR_ACT_SILU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z);
+}
+
+template <typename T> __device__ __forceinline__ void mma_16x8x16(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    if constexpr (std::is_same<T, __half>::value)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16-bit types: w's rows are the rows of 16 x 8 x 16 matrix instructions, which tcgen05's 128 would leave empty; 8 * NT rows of x.
+// A lane's 16 bytes of a row, eight values of k, are the operands of two instructions: which k a slot of the instruction stands
+// for does not matter as long as w and x agree.  What a lane reads goes through shared memory, asynchronously and some rounds ahead,
+// and back to the same lane: nothing is exchanged there, it takes the place of registers that the loads would wait in (4096 -> 16384
+// bfloat16: one row 25 us, 16 rows 29; loads straight to registers 24 and 39).
+constexpr int RM = 2;  // 16 rows of w each
+template <int NT> struct Few16 {
+    static constexpr int kLoads = 2 * RM + NT;  // 16 bytes each, of a lane and round
+    static constexpr int kRound = 256 * 16 * kLoads;
+    static constexpr int kAhead = kLoads <= 5 ? 4 : 3;
+    static constexpr int kTokens = 8 * NT, kPad = 16 * RM + 4;
+    static constexpr int kSums = 8 * kTokens * kPad * 4;
+    static constexpr int kSmem = kAhead * kRound > kSums ? kAhead * kRound : kSums;
+};
+__device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+template <typename T, int NT>
+__global__ void __launch_bounds__(256) k_linear_few16(const __grid_constant__ FewArgs<T> g) {
+    using S = Few16<NT>;
+    extern __shared__ __align__(16) uint8_t few_smem[];
+    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x & 31, group = lane >> 2, quad = lane & 3;
+    const unsigned part = g.parts > 1 ? cluster_rank() : 0u, n0 = blockIdx.x / g.parts * (16 * RM), blocks = (g.k + 31) / 32;
+    const T *w[2 * RM], *x[NT];
+    bool has_w[2 * RM], has_x[NT];
+#pragma unroll
+    for (int i = 0; i < 2 * RM; ++i) {
+        const unsigned r = n0 + i * 8 + group;
+        has_w[i] = r < g.n;
+        w[i] = g.w + (has_w[i] ? r : 0u) * g.w_pitch;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const unsigned r = t * 8 + group;
+        has_x[t] = r < g.rows;
+        x[t] = g.x + (has_x[t] ? r : 0u) * g.x_pitch;
+    }
+    griddep_start();
+    uint8_t *const mine = few_smem + threadIdx.x * 16;
+    const uint32_t slot0 = smem_addr(mine);
+    const auto issue = [&](unsigned round, unsigned slot) {
+        const unsigned k = ((round * g.parts + part) * 8 + warp) * 32 + quad * 8;
+        const bool in = k < g.k;  // k is a multiple of 8
+        const unsigned at = in ? k : 0u;
+        const uint32_t to = slot0 + slot * S::kRound;
+#pragma unroll
+        for (int i = 0; i < 2 * RM; ++i) copy16(to + i * 4096, w[i] + at, in && has_w[i]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) copy16(to + (2 * RM + t) * 4096, x[t] + at, in && has_x[t]);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    float acc[RM][NT][4] = {};
+    const unsigned rounds = (blocks + 8 * g.parts - 1) / (8 * g.parts);  // what lies behind the last block is copied as zeros
+#pragma unroll
+    for (int i = 0; i < S::kAhead - 1; ++i) issue(i, i);
+    unsigned slot = 0;
+    for (unsigned r = 0; r < rounds; ++r) {
+        issue(r + S::kAhead - 1, slot ? slot - 1 : S::kAhead - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kAhead - 1) : "memory");
+        const uint8_t *from = mine + slot * S::kRound;
+        uint4 a[2 * RM], v[NT];
+#pragma unroll
+        for (int i = 0; i < 2 * RM; ++i) a[i] = *reinterpret_cast<const uint4 *>(from + i * 4096);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) v[t] = *reinterpret_cast<const uint4 *>(from + (2 * RM + t) * 4096);
+#pragma unroll
+        for (int m = 0; m < RM; ++m)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                mma_16x8x16<T>(acc[m][t], a[2 * m].x, a[2 * m + 1].x, a[2 * m].y, a[2 * m + 1].y, v[t].x, v[t].y);
+                mma_16x8x16<T>(acc[m][t], a[2 * m].z, a[2 * m + 1].z, a[2 * m].w, a[2 * m + 1].w, v[t].z, v[t].w);
+            }
+        if (++slot == S::kAhead) slot = 0;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    float *const sums = reinterpret_cast<float *>(few_smem);  // [8][kTokens][kPad]
+#pragma unroll
+    for (int m = 0; m < RM; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sums[(warp * S::kTokens + t * 8 + quad * 2 + (i & 1)) * S::kPad + m * 16 + (i >> 1) * 8 + group] = acc[m][t][i];
+    __syncthreads();
+    const unsigned row = threadIdx.x / (2 * RM), col = threadIdx.x % (2 * RM) * 8;
+    const bool has = row < g.rows && row < S::kTokens && n0 + col < g.n;
+    float2 z[4] = {};
+    if (has) add_warps(sums + row * S::kPad + col, S::kTokens * S::kPad, z);
+    if (g.parts > 1) {  // the first CTA adds the others' in order
+        float4 *const whole = reinterpret_cast<float4 *>(sums + row * S::kPad + col);  // of the first warp: this thread alone has read it
+        __syncthreads();
+        if (has) {
+            whole[0] = make_float4(z[0].x, z[0].y, z[1].x, z[1].y);
+            whole[1] = make_float4(z[2].x, z[2].y, z[3].x, z[3].y);
+        }
+        cluster_sync_all();
+        if (part == 0 && has) {
+            const uint32_t here = smem_addr(whole);
+            for (unsigned c = 1; c < g.parts; ++c) {
+                float4 v[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n}\n"
+                                 : "=f"(v[i].x), "=f"(v[i].y), "=f"(v[i].z), "=f"(v[i].w)
+                                 : "r"(here + i * 16), "r"(c)
+                                 : "memory");
+                z[0] = add2(z[0], make_float2(v[0].x, v[0].y));
+                z[1] = add2(z[1], make_float2(v[0].z, v[0].w));
+                z[2] = add2(z[2], make_float2(v[1].x, v[1].y));
+                z[3] = add2(z[3], make_float2(v[1].z, v[1].w));
             }
         }
-        Pack8<T> y;
+        cluster_sync_all();  // nobody leaves before it has been read
+    }
+    if (part == 0 && has) finish_few(g, row, n0 + col, z);
+}
+
+// float32: eight rows of w, TT rows of x at a time (blockIdx.y), the products on the ordinary cores, two at an instruction.
+template <int TT>
+__global__ void __launch_bounds__(256) k_linear_few32(const __grid_constant__ FewArgs<float> g) {
+    constexpr int R = 8, V = R * TT;
+    __shared__ __align__(16) float sh[8][TT][R];
+    griddep_start();
+    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x & 31, n0 = blockIdx.x * R, t0 = blockIdx.y * TT;
+    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+    float2 acc[R][TT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) Two<T>::put(y.v + 2 * j, l.res ? add2(Two<T>::get(r.v + 2 * j), z[j]) : z[j]);
-        put8(static_cast<T *>(g.out) + row * g.out_pitch, col, g.n, g.out_vec, y);
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[r][t] = both(0.f);
+    for (unsigned k = (warp * 32 + lane) * 4; k < g.k; k += 1024) {  // k is a multiple of 4
+        float4 w[R], x[TT];
+#pragma unroll
+        for (int r = 0; r < R; ++r) w[r] = n0 + r < g.n ? *reinterpret_cast<const float4 *>(g.w + (n0 + r) * g.w_pitch + k) : none;
+#pragma unroll
+        for (int t = 0; t < TT; ++t) x[t] = t0 + t < g.rows ? *reinterpret_cast<const float4 *>(g.x + (t0 + t) * g.x_pitch + k) : none;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+                acc[r][t] = fma2(make_float2(w[r].z, w[r].w), make_float2(x[t].z, x[t].w), fma2(make_float2(w[r].x, w[r].y), make_float2(x[t].x, x[t].y), acc[r][t]));
+    }
+    // lanes halve what they carry at every exchange, until each has some lanes' sum of one value
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = acc[i % R][i / R].x + acc[i % R][i / R].y;
+#pragma unroll
+    for (int o = 16, n = V / 2; o; o >>= 1, n >>= 1) {
+        if (n == 0) {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            if (i >= n) continue;
+            const float keep = lane & o ? v[i + n] : v[i], give = lane & o ? v[i] : v[i + n];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    constexpr unsigned kLanes = 32 / V;  // with the same value
+    if (lane % kLanes == 0) (&sh[warp][0][0])[lane / kLanes] = v[0];
+    __syncthreads();
+    const unsigned t = threadIdx.x;
+    if (t < TT && t0 + t < g.rows) {
+        float2 z[4] = {};
+        add_warps(&sh[0][t][0], V, z);
+        finish_few(g, t0 + t, n0, z);
     }
 }
 
@@ -294,12 +516,56 @@ int finish(scar_linear *op) {
     return SCAR_OK;
 }
 
-// The join of a layer's parts with its epilogue costs about a launch.
+// Rows up to which w is read this way: 4096 -> 16384 bfloat16 takes 33 us with 32 rows, the product kernel 35 with 64; float32 of 4096 ->
+// 4096 70 and 76.
+constexpr unsigned kFewRows = 32;
+// f(kernel, NT, shared memory) for every instance.
+template <typename T, typename F> void for_few(F &&f) {
+    f(k_linear_few16<T, 1>, 1u, (unsigned)Few16<1>::kSmem);
+    f(k_linear_few16<T, 2>, 2u, (unsigned)Few16<2>::kSmem);
+    f(k_linear_few16<T, 4>, 4u, (unsigned)Few16<4>::kSmem);
+}
+template <typename T> bool allow_few() {
+    bool ok = true;
+    for_few<T>([&](auto kernel, unsigned, unsigned smem) { ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess; });
+    return ok;
+}
+template <typename T> void run_few(scar_linear *op, const FewArgs<T> &f) {
+    if constexpr (sizeof(T) == 4) {
+        const unsigned tt = f.rows == 1 ? 1 : f.rows == 2 ? 2 : 4;
+        auto kernel = tt == 1 ? k_linear_few32<1> : tt == 2 ? k_linear_few32<2> : k_linear_few32<4>;
+        launch(op, kernel, dim3((f.n + 7) / 8, (f.rows + tt - 1) / tt), 256, 0, f);
+    } else {
+        // A CTA for every SM is enough, and with few rows of w the sum over k is shared by the CTAs of a cluster to get there: 16384 ->
+        // 2048, one row 14.0 us, 16 rows 18.5 (half as many CTAs 17.5 and 26.1; CTAs of 16 rows of w, which read x twice as often, 17.3
+        // and 21.1).  Weights from memory, 60 calls.
+        FewArgs<T> g = f;
+        const unsigned nt = f.rows <= 8 ? 1 : f.rows <= 16 ? 2 : 4, tiles = (f.n + 31) / 32, rounds = (f.k + 255) / 256;
+        while (g.parts < 8 && tiles * g.parts < 2 * op->pairs && rounds >= 4 * g.parts) g.parts *= 2;
+        for_few<T>([&](auto kernel, unsigned t, unsigned smem) {
+            if (t == nt) launch_clusters(op, kernel, dim3(tiles * g.parts), 256, smem, g.parts, g);
+        });
+    }
+}
+
 template <typename T>
 int run_forward(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t wp, const T *bias, const T *res, uint64_t rp, const DropRule &drop,
                 unsigned rows, T *y, uint64_t yp, void *slope) {
     constexpr int PL = sizeof(T) == 4 ? 3 : 1;
     const unsigned K = (unsigned)op->cfg.in_features, N = (unsigned)op->cfg.out_features;
+    LayerArgs layer{};
+    layer.slope = slope;
+    layer.bias = bias;
+    layer.bias_vec = (uintptr_t)bias % 16 == 0;
+    layer.res = res;
+    layer.res_pitch = rp;
+    layer.res_vec = rows_aligned(res, rp, sizeof(T));
+    layer.drop = drop;
+    if (rows <= kFewRows && rows_aligned(x, rows > 1 ? xp : 0, sizeof(T)) && rows_aligned(w, N > 1 ? wp : 0, sizeof(T)) && K * sizeof(T) % 16 == 0) {
+        const FewArgs<T> f{x, w, xp, wp, rows, N, K, 1, op->cfg.activation, y, yp, rows_aligned(y, yp, sizeof(T)), layer};
+        run_few(op, f);
+        return SCAR_OK;
+    }
     Operands o;
     int rc = place(op, x, xp, w, wp, rows, true, true, &o);
     if (rc != SCAR_OK) return rc;
@@ -309,13 +575,7 @@ int run_forward(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t w
     g.out_pitch = yp;
     g.out_vec = rows_aligned(y, yp, sizeof(T));
     LayerArgs &l = g.layer;
-    l.slope = slope;
-    l.bias = bias;
-    l.bias_vec = (uintptr_t)bias % 16 == 0;
-    l.res = res;
-    l.res_pitch = rp;
-    l.res_vec = rows_aligned(res, rp, sizeof(T));
-    l.drop = drop;
+    l = layer;
     choose_splits(op, g, PL == 3 ? 0.f : kLaunchS);  // float32 has that launch in any case
     dispatch_activation(op->cfg.activation, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
@@ -435,6 +695,7 @@ int setup(scar_linear *op) {
     if (found != cudaDriverEntryPointSuccess || !fn) return SCAR_ERR_CUDA;
     op->encode = reinterpret_cast<EncodeTiled>(fn);
     const bool f32 = c.dtype == SCAR_F32;
+    if (c.dtype == SCAR_BF16 ? !allow_few<__nv_bfloat16>() : c.dtype == SCAR_F16 && !allow_few<__half>()) return SCAR_ERR_CUDA;
     if (f32 ? !allow_smem_all<3>()
             : !(allow_smem_all<1>() && allow_smem(k_tc_gemm<1, false, false, Epi::kIdentity, 1>) && allow_smem(k_tc_gemm<1, false, false, Epi::kRelu, 1>) &&
                 allow_smem(k_tc_gemm<1, false, false, Epi::kGelu, 1>) && allow_smem(k_tc_gemm<1, false, false, Epi::kSilu, 1>)))

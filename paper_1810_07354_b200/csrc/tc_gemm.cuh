@@ -621,17 +621,20 @@ template <typename T> __device__ __forceinline__ uint4 pack8(const float2 (&v)[4
 // chunk c ^ (r / 2 & 3), the swizzle of the results' maps.
 __device__ __forceinline__ uint4 *half_at(uint8_t *half, unsigned row, unsigned c) { return reinterpret_cast<uint4 *>(half + row * 64 + ((c ^ (row >> 1 & 3)) << 4)); }
 
-// 32 columns of 32 rows from memory into a half, and from there this lane's row.
+// 32 columns of 32 rows: from memory to registers as memory has them, and from there through a half to this lane's row.  The first
+// step may be taken long before the second.
+__device__ __forceinline__ void half_fetch(const unsigned short *base, unsigned long long pitch, bool vec, const EpiRows &rows, unsigned left, unsigned lane, uint4 (&v)[4]) {
+    if (!vec || left < 32) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned r = i * 8 + (lane >> 2);
+        v[i] = rows.has(r) ? *reinterpret_cast<const uint4 *>(base + (rows.row0 + r) * pitch + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
+    }
+}
 __device__ __forceinline__ void half_read(uint8_t *half, const unsigned short *base, unsigned long long pitch, bool vec, const EpiRows &rows, unsigned left, unsigned lane, uint4 (&x)[4]) {
     if (vec && left >= 32) {
-        uint4 v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned r = i * 8 + (lane >> 2);
-            v[i] = rows.has(r) ? *reinterpret_cast<const uint4 *>(base + (rows.row0 + r) * pitch + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) *half_at(half, i * 8 + (lane >> 2), lane & 3) = v[i];
+        for (int i = 0; i < 4; ++i) *half_at(half, i * 8 + (lane >> 2), lane & 3) = x[i];
     } else {
 #pragma unroll 8
         for (unsigned r = 0; r < 32; ++r)
@@ -671,8 +674,9 @@ __device__ __forceinline__ void half_write(uint8_t *half, unsigned short *base, 
     __syncwarp();
 }
 
-// A tile's 64 columns of this thread's row, 32 at a time, from the accumulator to the layer's output and slope (16-bit types).
-template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const TcArgs &g, uint32_t acc, bool any, const EpiRows &rows, unsigned col, uint8_t *stage, unsigned lane) {
+// A tile's 64 columns of this thread's row, 32 at a time, from the accumulator to the layer's output and slope (16-bit types); r: the
+// residual's first 32 columns, fetched.
+template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const TcArgs &g, uint32_t acc, bool any, const EpiRows &rows, unsigned col, uint8_t *stage, unsigned lane, uint4 (&r)[4]) {
     const LayerArgs &l = g.layer;
     const unsigned long long offset = l.drop.on ? l.drop.at() : 0ull;
     uint8_t *const out = stage, *const der = stage + 2048;
@@ -684,7 +688,6 @@ template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const T
         float v[32] = {};
         if (any) tmem_load32(acc + j, v);
         stage_free();
-        uint4 r[4];
         if (l.res) half_read(out, static_cast<const unsigned short *>(l.res) + at, l.res_pitch, l.res_vec, rows, left, lane, r);
         if (any) tmem_loaded(v);
 #pragma unroll
@@ -700,6 +703,7 @@ template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const T
             *half_at(out, lane, c) = pack8<T>(z);
             if (l.slope) *half_at(der, lane, c) = pack8<__half>(slope);
         }
+        if (l.res && j == 0 && left > 32) half_fetch(static_cast<const unsigned short *>(l.res) + at + 32, l.res_pitch, l.res_vec, rows, left - 32, lane, r);
         if (!rows.has(0)) continue;
         if (l.slope) tma_store(&l.slope_map, smem_addr(der), (int)at, (int)rows.row0, 0);
         if (g.c_map) tma_store(&g.c, smem_addr(out), (int)at, (int)rows.row0, 0);
@@ -945,13 +949,15 @@ k_tc_gemm(const __grid_constant__ TcSet<N> set) {
                 const EpiRows rows = epi_rows<EPI>(g, walks[t.which].m, t.mi * kBM + rank * 128 + quad * 32, t.s, lane);
                 const unsigned col = t.ni * kBN + half * (is_layer(EPI) ? 64 : kCols);
                 if constexpr (is_layer(EPI)) {
+                    uint4 res[4];  // the residual's first half, on its way while the products are
+                    if (g.layer.res && col < g.n) half_fetch(static_cast<const unsigned short *>(g.layer.res) + col, g.layer.res_pitch, g.layer.res_vec, rows, g.n - col, lane, res);
                     if (rounds) {
                         ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * ac, aph, error));
                         if (!ok) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     }
-                    if (g.bf16) epi_layer<act_of(EPI), __nv_bfloat16>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, lane);
-                    else epi_layer<act_of(EPI), __half>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, lane);
+                    if (g.bf16) epi_layer<act_of(EPI), __nv_bfloat16>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, lane, res);
+                    else epi_layer<act_of(EPI), __half>(g, lanes + ac * kBN, rounds != 0, rows, col, stage, lane, res);
                     if (rounds) {
                         acc_release(acc_empty + 8 * ac, lane);
                         if (++ac == kAccs) {

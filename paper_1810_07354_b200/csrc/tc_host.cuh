@@ -179,19 +179,25 @@ k_unplace(const T *__restrict__ src, unsigned long long src_pitch, unsigned n, u
 }
 
 // Launches a kernel of the call's chain: it may start while the one before it still runs (griddep_start waits for it).
-template <typename... P, typename... A> void launch(TcHost *op, void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, A... args) {
+template <typename... P, typename... A> void launch_clusters(TcHost *op, void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, unsigned cluster, A... args) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = threads;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = op->stream;
-    cudaLaunchAttribute early{};
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &early;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attrs[2]{};
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = cluster;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess) op->launches++;
     else op->failed = true;
+}
+template <typename... P, typename... A> void launch(TcHost *op, void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, A... args) {
+    launch_clusters(op, kernel, grid, threads, smem, 1, args...);
 }
 
 // Sets the product's `splits`: 1, or more than 1 where cutting the sum over k pays for all the rows the call has.  Returns
