@@ -57,26 +57,49 @@ template <typename T> __device__ __forceinline__ Pack8<T> row8(const T *row, uns
     for (unsigned j = 0; j < 8; ++j) x.v[j] = c + j < n ? s[j] : from_f32<T>(0.f);
     return x;
 }
-// The first of eight values that lie within the row.
-template <typename T> __device__ __forceinline__ void put8(T *row, unsigned c, unsigned n, bool vec, const Pack8<T> &x) {
+// The first of eight values that lie within the row, for a whole warp.  A 16-bit row that begins anywhere is written in 4-byte words:
+// where it begins between two of them, a lane's last word takes the next lane's first value (`next`: that lane goes on with this
+// row; `before`: the lane before this one does, and has written the first).
+template <typename T> __device__ __forceinline__ void put8(T *row, unsigned c, unsigned n, bool vec, const Pack8<T> &x, bool has, bool next, bool before) {
+    unsigned ahead = 0;
+    if constexpr (sizeof(T) == 2) ahead = __shfl_down_sync(0xffffffffu, x.u[0].x, 1);
+    if (!has) return;
+    T *const o = row + c;
     if (vec && c + 8 <= n) {
 #pragma unroll
-        for (unsigned i = 0; i < sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(row + c)[i] = x.u[i];
+        for (unsigned i = 0; i < sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(o)[i] = x.u[i];
         return;
+    }
+    if constexpr (sizeof(T) == 2) {
+        if (c + 8 <= n) {
+            const unsigned w[4] = {x.u[0].x, x.u[0].y, x.u[0].z, x.u[0].w};
+            if (((uintptr_t)o & 2u) == 0) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) reinterpret_cast<unsigned *>(o)[j] = w[j];
+                return;
+            }
+#pragma unroll
+            for (int j = 0; j < 3; ++j) reinterpret_cast<unsigned *>(o + 1)[j] = __funnelshift_r(w[j], w[j + 1], 16);
+            if (next && c + 8 < n) *reinterpret_cast<unsigned *>(o + 7) = __funnelshift_r(w[3], ahead, 16);
+            else o[7] = x.v[7];
+            if (!before) o[0] = x.v[0];
+            return;
+        }
     }
 #pragma unroll
     for (unsigned j = 0; j < 8; ++j)
-        if (c + j < n) row[c + j] = x.v[j];
+        if (c + j < n) o[j] = x.v[j];
 }
 
-// Eight products of a row to the layer's output and slope.
+// Eight products of a row to the layer's output and slope, for a whole warp (as put8).
 template <typename T, int ACT>
-__device__ __forceinline__ void finish8(const LayerArgs &l, T *out, unsigned long long out_pitch, bool out_vec, unsigned n, unsigned row, unsigned col, unsigned long long offset, float2 (&z)[4]) {
+__device__ __forceinline__ void finish8(const LayerArgs &l, T *out, unsigned long long out_pitch, bool out_vec, unsigned n, unsigned row, unsigned col, unsigned long long offset, float2 (&z)[4],
+                                        bool has, bool next, bool before) {
     float2 slope[4];
     Pack8<T> r;
-    if (l.res) r = row8(static_cast<const T *>(l.res) + row * l.res_pitch, col, n, l.res_vec);
-    layer8<ACT, T>(l, offset, row, col, n, z, slope);
-    if (l.slope) {
+    if (l.res && has) r = row8(static_cast<const T *>(l.res) + row * l.res_pitch, col, n, l.res_vec);
+    if (has) layer8<ACT, T>(l, offset, row, col, n, z, slope);
+    if (l.slope && has) {
         const unsigned long long at = (unsigned long long)row * ((n + 7) & ~7u) + col;
         if constexpr (sizeof(T) == 4) {
             float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(l.slope) + at);
@@ -89,7 +112,7 @@ __device__ __forceinline__ void finish8(const LayerArgs &l, T *out, unsigned lon
     Pack8<T> y;
 #pragma unroll
     for (int j = 0; j < 4; ++j) Two<T>::put(y.v + 2 * j, l.res ? add2(Two<T>::get(r.v + 2 * j), z[j]) : z[j]);
-    put8(out + row * out_pitch, col, n, out_vec, y);
+    put8(out + row * out_pitch, col, n, out_vec, y, has, next, before);
 }
 
 // The parts of a product whose sum was split (or its float32 result) to the layer's output: what epi_layer does without a split.
@@ -100,20 +123,25 @@ __global__ void __launch_bounds__(128) k_linear_join(const __grid_constant__ TcA
     const unsigned m = rows_of(g), pitch = (g.n + 7) & ~7u, groups = pitch / 8, splits = parts_of(g);
     const unsigned long long stride = (unsigned long long)g.m * pitch, total = (unsigned long long)m * groups;
     const unsigned long long offset = l.drop.on ? l.drop.at() : 0ull;
-    for (unsigned long long i = (unsigned long long)blockIdx.x * 128 + threadIdx.x; i < total; i += (unsigned long long)gridDim.x * 128) {
+    const unsigned lane = threadIdx.x & 31;
+    for (unsigned long long first = (unsigned long long)blockIdx.x * 128 + (threadIdx.x & ~31u); first < total; first += (unsigned long long)gridDim.x * 128) {
+        const unsigned long long i = first + lane;
+        const bool has = i < total;
         const unsigned row = total >> 32 ? (unsigned)(i / groups) : (unsigned)i / groups;
         const unsigned col = (unsigned)(i - (unsigned long long)row * groups) * 8;
         const float *p = g.part + (unsigned long long)row * pitch + col;
         float2 z[4] = {};
+        if (has) {
 #pragma unroll 2
-        for (unsigned s = 0; s < splits; ++s) {
-            const float4 a = *reinterpret_cast<const float4 *>(p + s * stride), b = *reinterpret_cast<const float4 *>(p + s * stride + 4);
-            z[0] = add2(z[0], make_float2(a.x, a.y));
-            z[1] = add2(z[1], make_float2(a.z, a.w));
-            z[2] = add2(z[2], make_float2(b.x, b.y));
-            z[3] = add2(z[3], make_float2(b.z, b.w));
+            for (unsigned s = 0; s < splits; ++s) {
+                const float4 a = *reinterpret_cast<const float4 *>(p + s * stride), b = *reinterpret_cast<const float4 *>(p + s * stride + 4);
+                z[0] = add2(z[0], make_float2(a.x, a.y));
+                z[1] = add2(z[1], make_float2(a.z, a.w));
+                z[2] = add2(z[2], make_float2(b.x, b.y));
+                z[3] = add2(z[3], make_float2(b.z, b.w));
+            }
         }
-        finish8<T, ACT>(l, static_cast<T *>(g.out), g.out_pitch, g.out_vec, g.n, row, col, offset, z);
+        finish8<T, ACT>(l, static_cast<T *>(g.out), g.out_pitch, g.out_vec, g.n, row, col, offset, z, has, lane < 31 && i + 1 < total && col + 8 < pitch, lane > 0 && col > 0);
     }
 }
 
@@ -142,12 +170,12 @@ __device__ __forceinline__ void add_warps(const float *at, unsigned size, float2
         z[3] = add2(z[3], make_float2(b.z, b.w));
     }
 }
-template <typename T> __device__ __forceinline__ void finish_few(const FewArgs<T> &g, unsigned row, unsigned col, float2 (&z)[4]) {
+template <typename T> __device__ __forceinline__ void finish_few(const FewArgs<T> &g, unsigned row, unsigned col, float2 (&z)[4], bool has) {
     const unsigned long long offset = g.layer.drop.on ? g.layer.drop.at() : 0ull;
-    if (g.act == SCAR_ACT_IDENTITY) finish8<T, SCAR_ACT_IDENTITY>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z);
-    else if (g.act == SCAR_ACT_RELU) finish8<T, SCAR_ACT_RELU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z);
-    else if (g.act == SCAR_ACT_GELU) finish8<T, SCAR_ACT_GELU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z);
-    else finish8<T, SCAR_ACT_SILU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z);
+    if (g.act == SCAR_ACT_IDENTITY) finish8<T, SCAR_ACT_IDENTITY>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z, has, false, false);
+    else if (g.act == SCAR_ACT_RELU) finish8<T, SCAR_ACT_RELU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z, has, false, false);
+    else if (g.act == SCAR_ACT_GELU) finish8<T, SCAR_ACT_GELU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z, has, false, false);
+    else finish8<T, SCAR_ACT_SILU>(g.layer, g.out, g.out_pitch, g.out_vec, g.n, row, col, offset, z, has, false, false);
 }
 
 template <typename T> __device__ __forceinline__ void mma_16x8x16(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
@@ -276,7 +304,7 @@ __global__ void __launch_bounds__(256) k_linear_few16(const __grid_constant__ Fe
         }
         cluster_sync_all();  // nobody leaves before it has been read
     }
-    if (part == 0 && has) finish_few(g, row, n0 + col, z);
+    if (part == 0) finish_few(g, row, n0 + col, z, has);
 }
 
 // float32: eight rows of w, TT rows of x at a time (blockIdx.y), the products on the ordinary cores, two at an instruction.
@@ -325,11 +353,11 @@ __global__ void __launch_bounds__(256) k_linear_few32(const __grid_constant__ Fe
     if (lane % kLanes == 0) (&sh[warp][0][0])[lane / kLanes] = v[0];
     __syncthreads();
     const unsigned t = threadIdx.x;
-    if (t < TT && t0 + t < g.rows) {
-        float2 z[4] = {};
-        add_warps(&sh[0][t][0], V, z);
-        finish_few(g, t0 + t, n0, z);
-    }
+    if (t >= 32) return;
+    const bool has = t < TT && t0 + t < g.rows;
+    float2 z[4] = {};
+    if (has) add_warps(&sh[0][t][0], V, z);
+    finish_few(g, t0 + t, n0, z, has);
 }
 
 // dz and its sums over the rows.  A CTA has 256 columns, eight per lane, and a run of rows, one per warp at a time.
@@ -405,18 +433,26 @@ __global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArg
 #pragma unroll
     for (int w = 0; w < 8; ++w) v += sums[w][threadIdx.x];
     if (gridDim.y > 1) {  // the strip's last CTA adds what its CTAs have left, in order
-        if (c < g.n) g.part[blockIdx.y * (unsigned long long)g.np + c] = v;
+        if (c < g.np) g.part[blockIdx.y * (unsigned long long)g.np + c] = v;
         __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) last = atomicInc(g.left + blockIdx.x, gridDim.y - 1) == gridDim.y - 1;
         __syncthreads();
         if (!last) return;
         __threadfence();
-        v = 0.f;
-        if (c < g.n) {
+        // four columns a thread, four threads a column
+        const unsigned c4 = blockIdx.x * 256 + (threadIdx.x & 63) * 4, from = threadIdx.x >> 6;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c4 < g.np) {
 #pragma unroll 8
-            for (unsigned k = 0; k < gridDim.y; ++k) v += __ldcg(g.part + k * (unsigned long long)g.np + c);
+            for (unsigned k = from; k < gridDim.y; k += 4) {
+                const float4 p = __ldcg(reinterpret_cast<const float4 *>(g.part + k * (unsigned long long)g.np + c4));
+                a.x += p.x; a.y += p.y; a.z += p.z; a.w += p.w;
+            }
         }
+        *reinterpret_cast<float4 *>(&sums[from][(threadIdx.x & 63) * 4]) = a;
+        __syncthreads();
+        v = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
     }
     if (c < g.n) g.dbias[c] = from_f32<T>(v);
 }
@@ -579,9 +615,12 @@ int run_forward(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t w
     choose_splits(op, g, PL == 3 ? 0.f : kLaunchS);  // float32 has that launch in any case
     dispatch_activation(op->cfg.activation, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
-        if (PL == 1 && g.splits == 1) {
-            // a tensor map's store clips rows to whole 16-byte words only
-            g.c_map = g.out_vec && N % 8 == 0;
+        // Rows off 16-byte boundaries go through float32 and the join where that has room: its threads lie along the rows, the product's
+        // across them (1537 x 1001 -> 2003 float16 with such a residual: RAGGED us).  A tensor map's store clips rows to whole 16-byte
+        // words only.
+        const bool whole = g.out_vec && N % 8 == 0, parts = (!whole || (res && !l.res_vec)) && (uint64_t)rows * op->np * 4 <= op->part_bytes;
+        if (PL == 1 && g.splits == 1 && !parts) {
+            g.c_map = whole;
             if (g.c_map) rc = make_map(op, &g.c, {y, N, rows, rows > 1 ? yp : op->np, 1, 0}, 32, 2, 64);
             if (rc == SCAR_OK && slope) rc = make_map(op, &l.slope_map, {slope, op->np, rows, op->np, 1, 0}, 32, 2, 64);
             if constexpr (PL == 1) {
@@ -623,31 +662,34 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
     if ((rc = place(op, x, xp, w, wp, rows, dw != nullptr, dx != nullptr, &o)) != SCAR_OK) return rc;
     const Operand dz = direct ? Operand{dy, N, rows, rows > 1 ? dyp : op->np, 1, 0} : Operand{op->dz, N, rows, op->np, PL, dz_rows * op->np};
     TcArgs dxg = product(op, rows, K, N, 0), dwg = product(op, N, K, rows, 1);
+    // Results whose rows do not lie on 16-byte boundaries would be stored in pieces of lines, at a tenth of the rate: where the parts'
+    // room holds them they go there, and from there to their places.  dw alone may go through the room of w's copy, which dx is done
+    // with by then.
+    const bool dx_odd = dx && !rows_aligned(dx, dxp, sizeof(T)), dw_odd = dw && !rows_aligned(dw, dwp, sizeof(T));
+    const uint64_t dx_room = dx_odd ? round_up((uint64_t)rows * op->kp * sizeof(T), 256) : 0, dw_room = dw_odd ? (uint64_t)N * op->kp * sizeof(T) : 0;
+    const bool through = (dx_odd || dw_odd) && dx_room + dw_room <= op->part_bytes;
+    const bool through_w = dw_odd && !through && op->w;
+    const auto result = [&](TcArgs &g, T *out, uint64_t pitch, unsigned n, bool other, void *room) {
+        g.out = other ? room : out;
+        g.out_pitch = other ? op->kp : pitch;
+        g.out_vec = other || rows_aligned(out, pitch, sizeof(T));
+        g.c_map = other || (g.out_vec && K * sizeof(T) % 16 == 0);
+        return g.c_map ? make_map(op, &g.c, {g.out, K, n, n > 1 ? g.out_pitch : op->kp, 1, 0}, 32, sizeof(T), PL == 1 ? 64 : 128) : SCAR_OK;
+    };
+    T *const room = reinterpret_cast<T *>(op->part), *const dw_at = through_w ? reinterpret_cast<T *>(op->w) : room + dx_room / sizeof(T);
     if (dx) {
         if ((rc = make_map(op, &dxg.a, dz, 128)) != SCAR_OK || (rc = make_map(op, &dxg.b, o.w, 64)) != SCAR_OK) return rc;
-        dxg.out = dx;
-        dxg.out_pitch = dxp;
-        dxg.out_vec = rows_aligned(dx, dxp, sizeof(T));
-        dxg.c_map = dxg.out_vec && K * sizeof(T) % 16 == 0;
-        if (dxg.c_map && (rc = make_map(op, &dxg.c, {dx, K, rows, rows > 1 ? dxp : op->kp, 1, 0}, 32, sizeof(T), PL == 1 ? 64 : 128)) != SCAR_OK) return rc;
+        if ((rc = result(dxg, dx, dxp, rows, through && dx_odd, room)) != SCAR_OK) return rc;
     }
-    // rows of dw that do not lie on 16-byte boundaries go through the room of w's copy, which dx is done with by then
-    bool through_w = false;
     if (dw) {
         if ((rc = make_map(op, &dwg.a, dz, 64)) != SCAR_OK || (rc = make_map(op, &dwg.b, o.x, 64)) != SCAR_OK) return rc;
-        dwg.out = dw;
-        dwg.out_pitch = dwp;
-        dwg.out_vec = rows_aligned(dw, dwp, sizeof(T));
-        through_w = !dwg.out_vec && op->w;
-        if (through_w) {
-            dwg.out = op->w;
-            dwg.out_pitch = op->kp;
-            dwg.out_vec = 1;
-        }
-        dwg.c_map = through_w || (dwg.out_vec && K * sizeof(T) % 16 == 0);
-        if (dwg.c_map && (rc = make_map(op, &dwg.c, {dwg.out, K, N, N > 1 ? dwg.out_pitch : op->kp, 1, 0}, 32, sizeof(T), PL == 1 ? 64 : 128)) != SCAR_OK) return rc;
+        if ((rc = result(dwg, dw, dwp, N, (through && dw_odd) || through_w, dw_at)) != SCAR_OK) return rc;
     }
-    if (dx && dw) {
+    if (through) {  // the parts' room is taken: no sum is split
+        if (dx && dw) launch_both<PL>(op, dxg, dwg);
+        else if (dx) launch_tc<PL, false, true, Epi::kOut>(op, dxg);
+        else launch_tc<PL, true, true, Epi::kOut>(op, dwg);
+    } else if (dx && dw) {
         launch_grads<PL>(op, dxg, dwg, through_w);
     } else if (dx) {
         choose_splits(op, dxg, kLaunchS);
@@ -656,8 +698,11 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
         choose_splits(op, dwg, kLaunchS);
         launch_out<PL, true>(op, dwg);
     }
-    if (through_w)
-        launch(op, k_unplace<T>, (unsigned)std::min<uint64_t>((N + 7) / 8, 16 * op->pairs), 256, 0, reinterpret_cast<const T *>(op->w), op->kp, N, K, dw, dwp);
+    const auto unplace = [&](const T *from, unsigned n, T *to, uint64_t pitch) {
+        launch(op, k_unplace<T>, (unsigned)std::min<uint64_t>((n + 7) / 8, 16 * op->pairs), 256, 0, from, op->kp, n, K, to, pitch);
+    };
+    if (through && dx_odd) unplace(room, rows, dx, dxp);
+    if ((through && dw_odd) || through_w) unplace(dw_at, N, dw, dwp);
     return SCAR_OK;
 }
 

@@ -683,7 +683,7 @@ template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const T
 #pragma unroll 1
     for (unsigned j = 0; j < 64; j += 32) {
         const unsigned at = col + j;
-        if (at >= g.n) break;
+        if (at >= g.n || !rows.has(0)) break;
         const unsigned left = g.n - at;
         float v[32] = {};
         if (any) tmem_load32(acc + j, v);
@@ -704,7 +704,6 @@ template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const T
             if (l.slope) *half_at(der, lane, c) = pack8<__half>(slope);
         }
         if (l.res && j == 0 && left > 32) half_fetch(static_cast<const unsigned short *>(l.res) + at + 32, l.res_pitch, l.res_vec, rows, left - 32, lane, r);
-        if (!rows.has(0)) continue;
         if (l.slope) tma_store(&l.slope_map, smem_addr(der), (int)at, (int)rows.row0, 0);
         if (g.c_map) tma_store(&g.c, smem_addr(out), (int)at, (int)rows.row0, 0);
         else half_write(out, static_cast<unsigned short *>(g.out) + at, g.out_pitch, g.out_vec, rows, left, lane);

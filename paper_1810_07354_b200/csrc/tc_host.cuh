@@ -253,6 +253,12 @@ template <int PL, bool A_MN> void launch_out(TcHost *op, const TcArgs &g) {
     launch(op, k_join_parts, (unsigned)std::min<uint64_t>((todo + 127) / 128, 32 * op->pairs), 128, 0, g);
 }
 
+// Two products without splits in one launch.
+template <int PL> void launch_both(TcHost *op, TcArgs a, TcArgs b) {
+    a.splits = b.splits = 1;
+    launch(op, k_tc_gemm<PL, false, true, Epi::kOut, 2>, 2 * (unsigned)std::min<uint64_t>(tiles_of(a) + tiles_of(b), op->pairs), EpiShape<Epi::kOut>::kThreads, kTcSmem, TcSet<2>{{a, b}});
+}
+
 // dh and dw of a piece: one launch without splits, so that the second one's tiles fill the last round of the first one's
 // (4096 x 32000 x 2048: 120 tiles of 500 stages leave 28 of 74 pairs idle for half of that time), unless split products
 // with launches of their own are worth it (a dh of few tiles whose sum runs over very many classes).  Not where dw goes through the room of w's copy, which dh still reads.
@@ -265,8 +271,7 @@ template <int PL> void launch_grads(TcHost *op, TcArgs dhg, TcArgs dwg, bool thr
     const float together = tile1 <= tile0 ? std::max(tile0, ((float)tiles0 * tile0 + (float)tiles1 * tile1) / (float)pairs)
                                           : (float)((tiles0 + pairs - 1) / pairs) * tile0 + (float)((tiles1 + pairs - 1) / pairs) * tile1;
     if (!through_w && together <= apart) {
-        dhg.splits = dwg.splits = 1;
-        launch(op, k_tc_gemm<PL, false, true, Epi::kOut, 2>, 2 * (unsigned)std::min<uint64_t>(tiles0 + tiles1, pairs), EpiShape<Epi::kOut>::kThreads, kTcSmem, TcSet<2>{{dhg, dwg}});
+        launch_both<PL>(op, dhg, dwg);
         return;
     }
     launch_out<PL, false>(op, dhg);
