@@ -12,6 +12,7 @@
 #include <new>
 #include <vector>
 
+#include "rows.cuh"
 #include "tc_host.cuh"
 
 using namespace scar;
@@ -30,65 +31,6 @@ __global__ void __launch_bounds__(256) k_linear_place(Copy<T> a, Copy<T> b, unsi
         const unsigned r = total >> 32 ? (unsigned)(k / groups) : (unsigned)k / groups;
         copy_eight(second ? b : a, r, r, (unsigned)(k - (unsigned long long)r * groups) * 8, d, dp);
     }
-}
-
-template <typename T> union Pack8 {
-    uint4 u[sizeof(T) / 2];
-    T v[8];
-};
-// Eight values from column c of a row of n that begins anywhere, zeros behind the last one.
-template <typename T> __device__ __forceinline__ Pack8<T> row8(const T *row, unsigned c, unsigned n, bool vec) {
-    Pack8<T> x;
-    const T *s = row + c;
-    if (vec && c + 8 <= n) {
-#pragma unroll
-        for (unsigned i = 0; i < sizeof(T) / 2; ++i) x.u[i] = reinterpret_cast<const uint4 *>(s)[i];
-        return x;
-    }
-    if constexpr (sizeof(T) == 2) {
-        if (!vec && c && c + 16 <= n) {  // the two aligned words that hold it lie within the row
-            const unsigned by = (unsigned)(uintptr_t)s & 15u;
-            const uint4 *a = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(s) - by);
-            x.u[0] = by ? shifted(a[0], a[1], by) : a[0];
-            return x;
-        }
-    }
-#pragma unroll
-    for (unsigned j = 0; j < 8; ++j) x.v[j] = c + j < n ? s[j] : from_f32<T>(0.f);
-    return x;
-}
-// The first of eight values that lie within the row, for a whole warp.  A 16-bit row that begins anywhere is written in 4-byte words:
-// where it begins between two of them, a lane's last word takes the next lane's first value (`next`: that lane goes on with this
-// row; `before`: the lane before this one does, and has written the first).
-template <typename T> __device__ __forceinline__ void put8(T *row, unsigned c, unsigned n, bool vec, const Pack8<T> &x, bool has, bool next, bool before) {
-    unsigned ahead = 0;
-    if constexpr (sizeof(T) == 2) ahead = __shfl_down_sync(0xffffffffu, x.u[0].x, 1);
-    if (!has) return;
-    T *const o = row + c;
-    if (vec && c + 8 <= n) {
-#pragma unroll
-        for (unsigned i = 0; i < sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(o)[i] = x.u[i];
-        return;
-    }
-    if constexpr (sizeof(T) == 2) {
-        if (c + 8 <= n) {
-            const unsigned w[4] = {x.u[0].x, x.u[0].y, x.u[0].z, x.u[0].w};
-            if (((uintptr_t)o & 2u) == 0) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) reinterpret_cast<unsigned *>(o)[j] = w[j];
-                return;
-            }
-#pragma unroll
-            for (int j = 0; j < 3; ++j) reinterpret_cast<unsigned *>(o + 1)[j] = __funnelshift_r(w[j], w[j + 1], 16);
-            if (next && c + 8 < n) *reinterpret_cast<unsigned *>(o + 7) = __funnelshift_r(w[3], ahead, 16);
-            else o[7] = x.v[7];
-            if (!before) o[0] = x.v[0];
-            return;
-        }
-    }
-#pragma unroll
-    for (unsigned j = 0; j < 8; ++j)
-        if (c + j < n) o[j] = x.v[j];
 }
 
 // Eight products of a row to the layer's output and slope, for a whole warp (as put8).
@@ -374,9 +316,11 @@ template <typename T> struct DzArgs {
     T *dbias;            // or nullptr
     unsigned *left;      // per strip: CTAs that are through
 };
-constexpr int kDzRows = 4;  // of a warp, under way together
+// Rows of a warp under way together, and CTAs of an SM that leave the compiler 64 registers: 8192 x 16384 bfloat16 with a mask takes 127 us
+// (6.3 TB/s); four rows and two CTAs 144, two and three 171, one and six 139.
+constexpr int kDzRows = 2, kDzCtas = 4;
 template <typename T>
-__global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArgs<T> g) {
+__global__ void __launch_bounds__(256, kDzCtas) k_linear_dz(const __grid_constant__ DzArgs<T> g) {
     __shared__ float sums[8][256];
     __shared__ bool last;
     griddep_start();
@@ -455,6 +399,17 @@ __global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArg
         v = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
     }
     if (c < g.n) g.dbias[c] = from_f32<T>(v);
+}
+
+// Two matrices of d columns from rows of `src_pitch` on 16-byte boundaries to their places, a warp per row.
+template <typename T>
+__global__ void __launch_bounds__(256) k_linear_unplace(const T *a, T *to_a, unsigned long long pitch_a, unsigned na, const T *b, T *to_b, unsigned long long pitch_b, unsigned nb,
+                                                        unsigned long long src_pitch, unsigned d) {
+    griddep_start();
+    for (unsigned long long r = blockIdx.x * 8ull + (threadIdx.x >> 5); r < (unsigned long long)na + nb; r += gridDim.x * 8ull) {
+        if (r < na) unplace_row(a + r * src_pitch, to_a + r * pitch_a, d);
+        else unplace_row(b + (r - na) * src_pitch, to_b + (r - na) * pitch_b, d);
+    }
 }
 
 struct LinearRecord {
@@ -698,11 +653,9 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
         choose_splits(op, dwg, kLaunchS);
         launch_out<PL, true>(op, dwg);
     }
-    const auto unplace = [&](const T *from, unsigned n, T *to, uint64_t pitch) {
-        launch(op, k_unplace<T>, (unsigned)std::min<uint64_t>((n + 7) / 8, 16 * op->pairs), 256, 0, from, op->kp, n, K, to, pitch);
-    };
-    if (through && dx_odd) unplace(room, rows, dx, dxp);
-    if ((through && dw_odd) || through_w) unplace(dw_at, N, dw, dwp);
+    const unsigned n0 = through && dx_odd ? rows : 0u, n1 = (through && dw_odd) || through_w ? N : 0u;
+    if (n0 + n1)
+        launch(op, k_linear_unplace<T>, (unsigned)std::min<uint64_t>(((uint64_t)n0 + n1 + 7) / 8, 32 * op->pairs), 256, 0, room, dx, dxp, n0, dw_at, dw, dwp, n1, op->kp, K);
     return SCAR_OK;
 }
 

@@ -3,6 +3,7 @@
 #pragma once
 #include <algorithm>
 
+#include "rows.cuh"
 #include "tc_gemm.cuh"
 
 namespace scar {
@@ -35,24 +36,6 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 &p0, __nv_bfloat16
     const float r1 = x - __bfloat162float(p0);
     p1 = __float2bfloat16_rn(r1);
     p2 = __float2bfloat16_rn(r1 - __bfloat162float(p1));
-}
-
-// 16 bytes that begin `by` bytes (even, below 16) into the 32 bytes a, b.
-__device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, unsigned by) {
-    unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    if (by & 8) {
-#pragma unroll
-        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-    }
-    if (by & 4) {
-#pragma unroll
-        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-    }
-    if (by & 2) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Rows and where they are copied to in the layout the products read: rows of dp elements (zeros behind the last),
@@ -157,25 +140,24 @@ inline int make_map(const TcHost *op, CUtensorMap *map, const Operand &x, unsign
     return rc == CUDA_SUCCESS ? SCAR_OK : SCAR_ERR_CUDA;
 }
 
-// A 16-bit or float32 matrix from rows on 16-byte boundaries to rows anywhere, a warp per row: whole 16-byte words of the
-// destination, its ends element by element.
+// A row on a 16-byte boundary to a row anywhere, by a warp: whole 16-byte words of the destination, its ends element by element.
+template <typename T> __device__ __forceinline__ void unplace_row(const T *__restrict__ s, T *__restrict__ o, unsigned d) {
+    constexpr unsigned kVec = 16 / sizeof(T);
+    const unsigned lane = threadIdx.x & 31;
+    const unsigned head = min(d, (unsigned)((0u - (unsigned)(uintptr_t)o) & 15u) / (unsigned)sizeof(T)), words = (d - head) / kVec, tail = head + words * kVec;
+    if (lane < head) o[lane] = s[lane];
+    if (tail + lane < d) o[tail + lane] = s[tail + lane];
+    const uint4 *a = reinterpret_cast<const uint4 *>(s);  // head is shorter than a word: word w lies in a[w] and a[w + 1]
+#pragma unroll 4
+    for (unsigned w = lane; w < words; w += 32)
+        *reinterpret_cast<uint4 *>(o + head + w * kVec) = head ? shifted(a[w], a[w + 1], head * (unsigned)sizeof(T)) : a[w];
+}
+// A matrix from such rows to rows anywhere, a warp per row.
 template <typename T>
 static __global__ void __launch_bounds__(256)
 k_unplace(const T *__restrict__ src, unsigned long long src_pitch, unsigned n, unsigned d, T *__restrict__ dst, unsigned long long pitch) {
     griddep_start();
-    constexpr unsigned kVec = 16 / sizeof(T);
-    const unsigned lane = threadIdx.x & 31;
-    for (unsigned long long r = blockIdx.x * 8ull + (threadIdx.x >> 5); r < n; r += gridDim.x * 8ull) {
-        const T *s = src + r * src_pitch;
-        T *o = dst + r * pitch;
-        const unsigned head = min(d, (unsigned)((0u - (unsigned)(uintptr_t)o) & 15u) / (unsigned)sizeof(T)), words = (d - head) / kVec, tail = head + words * kVec;
-        if (lane < head) o[lane] = s[lane];
-        if (tail + lane < d) o[tail + lane] = s[tail + lane];
-        const uint4 *a = reinterpret_cast<const uint4 *>(s);  // head is shorter than a word: word w lies in a[w] and a[w + 1]
-#pragma unroll 4
-        for (unsigned w = lane; w < words; w += 32)
-            *reinterpret_cast<uint4 *>(o + head + w * kVec) = head ? shifted(a[w], a[w + 1], head * (unsigned)sizeof(T)) : a[w];
-    }
+    for (unsigned long long r = blockIdx.x * 8ull + (threadIdx.x >> 5); r < n; r += gridDim.x * 8ull) unplace_row(src + r * src_pitch, dst + r * pitch, d);
 }
 
 // Launches a kernel of the call's chain: it may start while the one before it still runs (griddep_start waits for it).
