@@ -1054,7 +1054,7 @@ class Dropout(_OnStream):
         dtype = _operand_type(x.dtype)
         rule, tensor = self._rule(offset)
         if out is None:
-            out = x.new_empty(x.shape)
+            out = self._torch.empty_like(x)
         xp, yp = self._rows("x", x, x), self._rows("out", out, x)
         rp = (None, 0) if residual is None else self._rows("residual", residual, x)
         n = x.numel()
@@ -1171,8 +1171,8 @@ class LinearLayer(_Rows):
         """``(dx, dw, dbias)`` from the gradient of the output, which is the residual's own; None for what is not needed."""
         rows, K, N = len(dy) if dy.dim() else 0, self.in_features, self.out_features
         dyp, xp, wp, sp = self._matrix("dy", dy, rows, N), self._matrix("x", x, rows, K), self._matrix("w", w, N, K), self._slope(slope, rows)
-        dx = None if not need_dx else dy.new_empty((rows, K)) if dx is None else dx
-        dw = None if not need_dw else dy.new_empty((N, K)) if dw is None else dw
+        dx = None if not need_dx else self._torch.empty_like(x) if dx is None else dx
+        dw = None if not need_dw else self._torch.empty_like(w) if dw is None else dw
         dbias = None if not need_dbias else dy.new_empty((N,)) if dbias is None else dbias
         dxp = (None, 0) if dx is None else self._matrix("dx", dx, rows, K)
         dwp = (None, 0) if dw is None else self._matrix("dw", dw, N, K)
@@ -1241,9 +1241,9 @@ class ResidualNorm(_Rows):
         if f is None and y is None:
             yp = (None, 0)
         else:
-            y = x.new_empty((rows, self.dim)) if y is None else y
+            y = self._torch.empty_like(x) if y is None else y
             yp = self._matrix("y", y, rows, self.dim)
-        n = None if not pre else x.new_empty((rows, self.dim)) if n is None else n
+        n = None if not pre else self._torch.empty_like(x) if n is None else n
         np_ = self._maybe("n", n, rows)
         here = self._enter(x, f, gate, w_post, b_post, w_pre, b_pre, y, n)
         scar_resnorm_forward(self.op, block, *xp, *fp, rows, *yp, *np_)
@@ -1264,7 +1264,7 @@ class ResidualNorm(_Rows):
         has = {"dx": some, "df": f, "dgate": gate, "dw_post": w_post if post else None, "db_post": b_post if post else None,
                "dw_pre": w_pre if pre else None, "db_pre": b_pre if pre else None}
         out = out or {}
-        got = {k: None if v is None else out[k] if k in out else v.new_empty(v.shape) for k, v in has.items()}
+        got = {k: None if v is None else out[k] if k in out else self._torch.empty_like(v) for k, v in has.items()}
         matrices = [self._maybe(k, got[k], rows if k != "dgate" or gate is None else gate.shape[0]) for k in ("dx", "df", "dgate")]
         vectors = [self._vector(k, got[k], self.dim) for k in ("dw_post", "db_post", "dw_pre", "db_pre")]
         here = self._enter(dy, dn, y, f, gate, w_post, b_post, w_pre, b_pre, *got.values())
