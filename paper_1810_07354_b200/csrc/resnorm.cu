@@ -74,28 +74,31 @@ template <typename T> struct NormArgs {
     T *dw_post, *db_post, *dw_pre, *db_pre;
 };
 
-// A thread's N values of one row.  Rows on 16-byte boundaries: 16 bytes of neighbours per thread and round.  Rows anywhere: single
-// values, neighbouring threads next to one another, so that a warp's access is one run of memory.
+// A thread's N values of one row.  A warp has 32 N neighbouring columns.  Rows on 16-byte boundaries: 16 bytes of neighbours per
+// thread and round.  Rows anywhere: single values, neighbouring threads next to one another, so that a warp's access is one run of
+// memory.  Either way the rounds are a constant distance apart.
 template <typename T, int N> union Row {
     uint4 u[N * sizeof(T) / 16];
     T v[N];
     __device__ Row() {}
 };
-template <bool VEC, typename T> __device__ __forceinline__ unsigned col_of(int i) {
-    constexpr int kWord = 16 / sizeof(T);
-    return VEC ? (i / kWord * blockDim.x + threadIdx.x) * kWord + i % kWord : i * blockDim.x + threadIdx.x;
+template <bool VEC, typename T, int N> __device__ __forceinline__ unsigned col_of(int i) {
+    constexpr int kWord = VEC ? 16 / sizeof(T) : 1;
+    return (threadIdx.x & ~31u) * N + (threadIdx.x & 31) * kWord + i / kWord * (32 * kWord) + i % kWord;
 }
+// All of the warp's columns lie in the row.
+template <int N> __device__ __forceinline__ bool whole_warp(unsigned cols) { return ((threadIdx.x & ~31u) + 32) * N <= cols; }
 template <bool VEC, typename T, int N> __device__ __forceinline__ void load_row(Row<T, N> &r, const T *p, unsigned cols) {
     if (VEC) {  // rows are whole words
 #pragma unroll
         for (unsigned k = 0; k < N * sizeof(T) / 16; ++k) {
-            const unsigned col = col_of<true, T>(k * (16 / sizeof(T)));
+            const unsigned col = col_of<true, T, N>(k * (16 / sizeof(T)));
             r.u[k] = col < cols ? *reinterpret_cast<const uint4 *>(p + col) : make_uint4(0, 0, 0, 0);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const unsigned col = col_of<false, T>(i);
+            const unsigned col = col_of<false, T, N>(i);
             r.v[i] = col < cols ? p[col] : from_f32<T>(0.f);
         }
     }
@@ -104,24 +107,19 @@ template <bool VEC, typename T, int N> __device__ __forceinline__ void store_row
     if (VEC) {
 #pragma unroll
         for (unsigned k = 0; k < N * sizeof(T) / 16; ++k) {
-            const unsigned col = col_of<true, T>(k * (16 / sizeof(T)));
+            const unsigned col = col_of<true, T, N>(k * (16 / sizeof(T)));
             if (col < cols) *reinterpret_cast<uint4 *>(p + col) = r.u[k];
         }
+    } else if (whole_warp<N>(cols)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[col_of<false, T, N>(i)] = r.v[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const unsigned col = col_of<false, T>(i);
-            if (col < cols) p[col] = r.v[i];
-        }
+        for (int i = 0; i < N; ++i)
+            if (col_of<false, T, N>(i) < cols) p[col_of<false, T, N>(i)] = r.v[i];
     }
 }
-template <bool VEC, typename T, int N> __device__ __forceinline__ void read_row(float2 (&v)[N / 2], const T *p, unsigned cols) {
-    Row<T, N> r;
-    load_row<VEC>(r, p, cols);
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) v[i] = Two<T>::get(r.v + 2 * i);
-}
-// The same from a stage of the ring, where zeros lie behind the row.
+// A row from a stage of the ring as float32 pairs; zeros lie behind it there.
 template <bool VEC, typename T, int N> __device__ __forceinline__ void fetch_row(float2 (&v)[N / 2], const T *p) {
     Row<T, N> r;
     load_row<VEC>(r, p, ~0u);
@@ -143,14 +141,14 @@ template <bool VEC, typename T, int N> __device__ __forceinline__ void load_vect
         return;
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(col_of<VEC, T>(i) < cols ? otherwise : 0.f);
+    for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(col_of<VEC, T, N>(i) < cols ? otherwise : 0.f);
 }
 // v + shift, but zeros stay behind the row.
 template <bool VEC, typename T, int N> __device__ __forceinline__ void shift_row(float2 (&v)[N / 2], float shift, unsigned cols) {
     constexpr int kWord = VEC ? 16 / sizeof(T) : 1;  // all or none of a word's values lie in the row
 #pragma unroll
     for (int i = 0; i < N; i += kWord) {
-        const float s = col_of<VEC, T>(i) < cols ? shift : 0.f;
+        const float s = col_of<VEC, T, N>(i) < cols ? shift : 0.f;
         if (kWord == 1) {
             float &x = i & 1 ? v[i / 2].y : v[i / 2].x;
             x += s;
@@ -479,7 +477,7 @@ __global__ void __launch_bounds__(threads_of(kForwardValues), 2) k_resnorm_forwa
 template <bool VEC, typename T, int N> __device__ __forceinline__ void put_part(float *p, const float2 (&v)[N / 2], unsigned cols) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (col_of<VEC, T>(i) < cols) p[col_of<VEC, T>(i)] = i & 1 ? v[i / 2].y : v[i / 2].x;
+        if (col_of<VEC, T, N>(i) < cols) p[col_of<VEC, T, N>(i)] = i & 1 ? v[i / 2].y : v[i / 2].x;
 }
 
 template <typename T, bool LAYER, bool VEC, bool SHARED>
@@ -715,6 +713,7 @@ __global__ void __launch_bounds__(threads_of(back_values(LAYER)), back_ctas<T>(L
             parity ^= 1;
         }
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join: its CTAs get ready while the last sums are written
     const unsigned long long each = (unsigned long long)runs * g.dim, mine = (unsigned long long)run * g.dim + col0;
     if (g.dw_pre) put_part<VEC, T, N>(g.part + mine, a_wpre, cols);
     if (g.dw_post) put_part<VEC, T, N>(g.part + each + mine, a_wpost, cols);
@@ -726,26 +725,27 @@ __global__ void __launch_bounds__(threads_of(back_values(LAYER)), back_ctas<T>(L
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
-// Adds the runs' sums, 32 columns a CTA, eight walkers over the rows of the list, in an order that depends on the sizes alone.
+// Adds the runs' sums, 32 columns a CTA, 16 walkers over the rows of the list, in an order that depends on the sizes alone.
 // blockIdx.y 0 .. 3: the vectors; the others take turns at the runs c: the gate that the last row of c has, where it begins in c and
 // ends behind it.
 constexpr unsigned kJoinGates = 32;
-template <typename T> __global__ void __launch_bounds__(256) k_resnorm_join(const __grid_constant__ NormArgs<T> g, unsigned runs) {
-    __shared__ float sh[8][32];
+template <typename T> __global__ void __launch_bounds__(512) k_resnorm_join(const __grid_constant__ NormArgs<T> g, unsigned runs) {
+    __shared__ float sh[16][32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const unsigned lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane, walker = threadIdx.x >> 5;
     // rows of `from`, `step` apart; the first lies `skip` further on
     const auto join = [&](const float *from, unsigned long long step, unsigned n, unsigned skip, T *out) {
         float v = 0.f;
         if (col < g.dim) {
-#pragma unroll 4
-            for (unsigned k = walker; k < n; k += 8) v += from[k * step + (k == 0 ? skip : 0u) + col];
+#pragma unroll 8
+            for (unsigned k = walker; k < n; k += 16) v += from[k * step + (k == 0 ? skip : 0u) + col];
         }
         sh[walker][lane] = v;
         __syncthreads();
         if (walker == 0 && col < g.dim) {
             v = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v += sh[k][lane];
+            for (int k = 0; k < 16; ++k) v += sh[k][lane];
             out[col] = from_f32<T>(v);
         }
         __syncthreads();
@@ -862,7 +862,16 @@ template <typename T> int run_backward(scar_resnorm *op, NormArgs<T> g) {
     }
     const bool gates = g.dgate && g.per_gate > 1 && runs > 1;
     if (!g.dw_pre && !g.dw_post && !g.db_pre && !g.db_post && !gates) return SCAR_OK;
-    k_resnorm_join<T><<<dim3((g.dim + 31) / 32, 4 + (gates ? std::min(runs, kJoinGates) : 0)), 256, 0, op->stream>>>(g, runs);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((g.dim + 31) / 32, 4 + (gates ? std::min(std::min(runs, (g.rows - 1) / g.per_gate + 1), kJoinGates) : 0));
+    cfg.blockDim = 512;
+    cfg.stream = op->stream;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    TRAIN_TRY(cudaLaunchKernelEx(&cfg, k_resnorm_join<T>, g, runs));
     op->launches++;
     return SCAR_OK;
 }
