@@ -726,8 +726,7 @@ __global__ void __launch_bounds__(threads_of(back_values(LAYER)), back_ctas<T>(L
 }
 
 // Adds the runs' sums, 32 columns a CTA, 16 walkers over the rows of the list, in an order that depends on the sizes alone.
-// blockIdx.y 0 .. 3: the vectors; the others take turns at the runs c: the gate that the last row of c has, where it begins in c and
-// ends behind it.
+// blockIdx.y 0 .. 3: the vectors; the others take turns at the gates whose rows are cut by a run's end.
 constexpr unsigned kJoinGates = 32;
 template <typename T> __global__ void __launch_bounds__(512) k_resnorm_join(const __grid_constant__ NormArgs<T> g, unsigned runs) {
     __shared__ float sh[16][32];
@@ -755,12 +754,15 @@ template <typename T> __global__ void __launch_bounds__(512) k_resnorm_join(cons
         if (out) join(g.part + blockIdx.y * (unsigned long long)runs * g.dim, g.dim, runs, 0u, out);
         return;
     }
-    for (unsigned c = blockIdx.y - 4; c < runs; c += gridDim.y - 4) {
-        const unsigned r0 = c * g.per_run, r1 = min(g.rows, r0 + g.per_run), gate = (r1 - 1) / g.per_gate, first = gate * g.per_gate;
-        const unsigned end = g.rows - first > g.per_gate ? first + g.per_gate : g.rows;
-        if (first < r0 || end <= r1) continue;
+    // gates one by one where they are fewer than runs
+    const unsigned gates = (g.rows - 1) / g.per_gate + 1, turns = min(gates, runs);
+    for (unsigned i = blockIdx.y - 4; i < turns; i += gridDim.y - 4) {
+        const unsigned gate = gates <= runs ? i : (min(g.rows, (i + 1) * g.per_run) - 1) / g.per_gate;
+        const unsigned first = gate * g.per_gate, end = g.rows - first > g.per_gate ? first + g.per_gate : g.rows;
+        const unsigned c = first / g.per_run, last = (end - 1) / g.per_run;
+        if (c == last || (gates > runs && c != i)) continue;
         // the first of its parts is the run's second, the others' their first
-        join(g.part_gate + c * 2ull * g.dim, 2ull * g.dim, (end - 1) / g.per_run - c + 1, g.dim, g.dgate + gate * g.dgate_pitch);
+        join(g.part_gate + c * 2ull * g.dim, 2ull * g.dim, last - c + 1, g.dim, g.dgate + gate * g.dgate_pitch);
     }
 }
 
