@@ -137,10 +137,10 @@ template <typename T> __device__ __forceinline__ void mma_16x8x16(float (&d)[4],
 // and back to the same lane: nothing is exchanged there, it takes the place of registers that the loads would wait in (4096 -> 16384
 // bfloat16: one row 25 us, 16 rows 29; loads straight to registers 24 and 39).
 constexpr int RM = 2;  // 16 rows of w each
-template <int NT> struct Few16 {
+template <int NT, int AHEAD> struct Few16 {
     static constexpr int kLoads = 2 * RM + NT;  // 16 bytes each, of a lane and round
     static constexpr int kRound = 256 * 16 * kLoads;
-    static constexpr int kAhead = kLoads <= 5 ? 4 : 3;
+    static constexpr int kAhead = AHEAD;  // rounds, with the one that is read
     static constexpr int kTokens = 8 * NT, kPad = 16 * RM + 4;
     static constexpr int kSums = 8 * kTokens * kPad * 4;
     static constexpr int kSmem = kAhead * kRound > kSums ? kAhead * kRound : kSums;
@@ -148,9 +148,9 @@ template <int NT> struct Few16 {
 __device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
-template <typename T, int NT>
+template <typename T, int NT, int AHEAD>
 __global__ void __launch_bounds__(256) k_linear_few16(const __grid_constant__ FewArgs<T> g) {
-    using S = Few16<NT>;
+    using S = Few16<NT, AHEAD>;
     extern __shared__ __align__(16) uint8_t few_smem[];
     const unsigned warp = threadIdx.x / 32, lane = threadIdx.x & 31, group = lane >> 2, quad = lane & 3;
     const unsigned part = g.parts > 1 ? cluster_rank() : 0u, n0 = blockIdx.x / g.parts * (16 * RM), blocks = (g.k + 31) / 32;
@@ -510,15 +510,16 @@ int finish(scar_linear *op) {
 // Rows up to which w is read this way: 4096 -> 16384 bfloat16 takes 33 us with 32 rows, the product kernel 35 with 64; float32 of 4096 ->
 // 4096 70 and 76.
 constexpr unsigned kFewRows = 32;
-// f(kernel, NT, shared memory) for every instance.
+// f(kernel, NT, AHEAD, shared memory) for every instance.
 template <typename T, typename F> void for_few(F &&f) {
-    f(k_linear_few16<T, 1>, 1u, (unsigned)Few16<1>::kSmem);
-    f(k_linear_few16<T, 2>, 2u, (unsigned)Few16<2>::kSmem);
-    f(k_linear_few16<T, 4>, 4u, (unsigned)Few16<4>::kSmem);
+    f(k_linear_few16<T, 1, 4>, 1u, 4u, (unsigned)Few16<1, 4>::kSmem);
+    f(k_linear_few16<T, 2, 3>, 2u, 3u, (unsigned)Few16<2, 3>::kSmem);
+    f(k_linear_few16<T, 2, 4>, 2u, 4u, (unsigned)Few16<2, 4>::kSmem);
+    f(k_linear_few16<T, 4, 3>, 4u, 3u, (unsigned)Few16<4, 3>::kSmem);
 }
 template <typename T> bool allow_few() {
     bool ok = true;
-    for_few<T>([&](auto kernel, unsigned, unsigned smem) { ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess; });
+    for_few<T>([&](auto kernel, unsigned, unsigned, unsigned smem) { ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess; });
     return ok;
 }
 template <typename T> void run_few(scar_linear *op, const FewArgs<T> &f) {
@@ -533,8 +534,11 @@ template <typename T> void run_few(scar_linear *op, const FewArgs<T> &f) {
         FewArgs<T> g = f;
         const unsigned nt = f.rows <= 8 ? 1 : f.rows <= 16 ? 2 : 4, tiles = (f.n + 31) / 32, rounds = (f.k + 255) / 256;
         while (g.parts < 8 && tiles * g.parts < 2 * op->pairs && rounds >= 4 * g.parts) g.parts *= 2;
-        for_few<T>([&](auto kernel, unsigned t, unsigned smem) {
-            if (t == nt) launch_clusters(op, kernel, dim3(tiles * g.parts), 256, smem, g.parts, g);
+        // 80 to 96 KiB a CTA, which are two on an SM; up to 16 rows with more CTAs than that, 72 KiB and three (16 rows, 8192 -> 4096: 15.9 us
+        // with the one and 18.7 with the other; 4096 -> 32768 52.5 and 48.3)
+        const unsigned ahead = nt == 4 || (nt == 2 && tiles * g.parts > 4 * op->pairs) ? 3 : 4;
+        for_few<T>([&](auto kernel, unsigned t, unsigned a, unsigned smem) {
+            if (t == nt && a == ahead) launch_clusters(op, kernel, dim3(tiles * g.parts), 256, smem, g.parts, g);
         });
     }
 }
@@ -604,7 +608,6 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
     // dy itself where nothing changes it
     const bool direct = PL == 1 && !slope && !drop.on && rows_aligned(dy, dyp, 2);
     const uint64_t dz_rows = std::max<uint64_t>(op->cfg.max_rows, 1);
-    if (!direct && !op->dz && (rc = linear_alloc(op, &op->dz, PL * dz_rows * op->np * 2)) != SCAR_OK) return rc;
     if (!direct || dbias) {
         const unsigned strips = (N + 255) / 256;
         const unsigned per = (unsigned)round_up((rows + op->dz_ctas - 1) / op->dz_ctas, 8);
@@ -717,7 +720,7 @@ int setup(scar_linear *op) {
         uint64_t bytes;
     } const want[] = {
         {(void **)&op->rec, sizeof(LinearRecord)}, {(void **)&op->part, op->part_bytes}, {(void **)&op->left, 4 * strips},
-        {(void **)&op->sums, c.forward_only ? 0 : 4ull * op->dz_ctas * op->np}, {(void **)&op->dz, c.forward_only || (!f32 && !has_slope(op)) ? 0 : op->planes * T * op->np * 2},
+        {(void **)&op->sums, c.forward_only ? 0 : 4ull * op->dz_ctas * op->np}, {(void **)&op->dz, c.forward_only ? 0 : op->planes * T * op->np * 2},
         {(void **)&op->x, copies ? op->planes * T * op->kp * 2 : 0}, {(void **)&op->w, copies ? op->planes * c.out_features * op->kp * 2 : 0},
     };
     uint64_t total = 0;
