@@ -95,6 +95,7 @@ template <typename T> struct FewArgs {
     unsigned long long x_pitch, w_pitch;
     unsigned rows, n, k;
     unsigned parts;  // CTAs of a cluster that share the sum over k (16-bit types)
+    int x_vec;       // rows of x on 16-byte boundaries
     int act;
     T *out;
     unsigned long long out_pitch;
@@ -267,7 +268,10 @@ __global__ void __launch_bounds__(256) k_linear_few32(const __grid_constant__ Fe
 #pragma unroll
         for (int r = 0; r < R; ++r) w[r] = n0 + r < g.n ? *reinterpret_cast<const float4 *>(g.w + (n0 + r) * g.w_pitch + k) : none;
 #pragma unroll
-        for (int t = 0; t < TT; ++t) x[t] = t0 + t < g.rows ? *reinterpret_cast<const float4 *>(g.x + (t0 + t) * g.x_pitch + k) : none;
+        for (int t = 0; t < TT; ++t) {
+            const float *p = g.x + (t0 + t) * g.x_pitch + k;
+            x[t] = t0 + t >= g.rows ? none : g.x_vec ? *reinterpret_cast<const float4 *>(p) : make_float4(p[0], p[1], p[2], p[3]);
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -507,9 +511,14 @@ int finish(scar_linear *op) {
     return SCAR_OK;
 }
 
-// Rows up to which w is read this way: 4096 -> 16384 bfloat16 takes 33 us with 32 rows, the product kernel 35 with 64; float32 of 4096 ->
-// 4096 70 and 76.
-constexpr unsigned kFewRows = 32;
+// Rows up to which w is read this way: 4096 -> 16384 bfloat16 takes 33 us with 32 rows, the product kernel 35 with 64.  float32 rows
+// go four at a time, the second four with w from L2 where that holds it: 32 rows of 4096 -> 4096 take 70 us (the product kernel 76), 8
+// rows of 4096 -> 8192 81 us and 32 308 (as planes 120).
+constexpr unsigned kFewRows = 32, kFewFar = 8;
+constexpr uint64_t kL2Holds = 64ull << 20;
+template <typename T> bool few_rows(const scar_linear *op, unsigned rows) {
+    return rows <= kFewRows && (sizeof(T) == 2 || rows <= kFewFar || op->cfg.out_features * op->cfg.in_features * 4 <= kL2Holds);
+}
 // f(kernel, NT, AHEAD, shared memory) for every instance.
 template <typename T, typename F> void for_few(F &&f) {
     f(k_linear_few16<T, 1, 4>, 1u, 4u, (unsigned)Few16<1, 4>::kSmem);
@@ -556,10 +565,19 @@ int run_forward(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t w
     layer.res_pitch = rp;
     layer.res_vec = rows_aligned(res, rp, sizeof(T));
     layer.drop = drop;
-    if (rows <= kFewRows && rows_aligned(x, rows > 1 ? xp : 0, sizeof(T)) && rows_aligned(w, N > 1 ? wp : 0, sizeof(T)) && K * sizeof(T) % 16 == 0) {
-        const FewArgs<T> f{x, w, xp, wp, rows, N, K, 1, op->cfg.activation, y, yp, rows_aligned(y, yp, sizeof(T)), layer};
-        run_few(op, f);
-        return SCAR_OK;
+    if (few_rows<T>(op, rows) && rows_aligned(w, N > 1 ? wp : 0, sizeof(T)) && K * sizeof(T) % 16 == 0) {
+        FewArgs<T> f{x, w, xp, wp, rows, N, K, 1, rows_aligned(x, rows > 1 ? xp : 0, sizeof(T)), op->cfg.activation, y, yp, rows_aligned(y, yp, sizeof(T)), layer};
+        const bool copy = PL == 1 && !f.x_vec;  // of x alone, to the parts' room
+        if (!copy || (uint64_t)rows * K * 2 <= op->part_bytes) {
+            if (copy) {
+                const Copy<T> a{x, xp, rows, false, reinterpret_cast<unsigned short *>(op->part), 0}, none{x, xp, 0, false, nullptr, 0};
+                launch(op, k_linear_place<T>, (unsigned)std::min<uint64_t>(((uint64_t)rows * (K / 8) + 255) / 256, 16 * op->pairs), 256, 0, a, none, K, K);
+                f.x = reinterpret_cast<const T *>(op->part);
+                f.x_pitch = K;
+            }
+            run_few(op, f);
+            return SCAR_OK;
+        }
     }
     Operands o;
     int rc = place(op, x, xp, w, wp, rows, true, true, &o);
