@@ -513,7 +513,7 @@ int finish(scar_linear *op) {
 
 // Rows up to which w is read this way: 4096 -> 16384 bfloat16 takes 33 us with 32 rows, the product kernel 35 with 64.  float32 rows
 // go four at a time, the second four with w from L2 where that holds it: 32 rows of 4096 -> 4096 take 70 us (the product kernel 76), 8
-// rows of 4096 -> 8192 81 us and 32 308 (as planes 120).
+// rows of 4096 -> 8192 81 us and 32 308 (as planes 131).
 constexpr unsigned kFewRows = 32, kFewFar = 8;
 constexpr uint64_t kL2Holds = 64ull << 20;
 template <typename T> bool few_rows(const scar_linear *op, unsigned rows) {

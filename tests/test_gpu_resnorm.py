@@ -325,3 +325,19 @@ def test_far_rows():
     op.backward(c.dy, c.dn, y, c.f, out={"dx": wide}, **c.kw)
     assert torch.equal(wide, got["dx"])
     op.close()
+
+
+def test_reports_of_a_wait_that_gave_up():
+    from paper_1810_07354_b200 import api
+
+    op = ResidualNorm(4, 40, torch.float32)
+    x = torch.randn(4, 40, device="cuda")
+    op.forward(x)
+    op.status()
+    api.scar_resnorm_selftest_arm_timeout(op.op)
+    op.forward(x)
+    with pytest.raises(ScarError) as e:
+        op.status()
+    assert e.value.code == -6
+    op.status()
+    op.close()
