@@ -13,7 +13,7 @@
 namespace scar {
 
 struct DropRule {
-    unsigned key0, key1;
+    unsigned key[20];  // of the ten rounds, two each: operands from the kernel's parameters
     int on;          // something is dropped
     unsigned above;  // 65536 cut - 1: a value is kept if its 16 bits, as the upper half of a word, are above this
     float scale;     // of what is kept
@@ -25,27 +25,32 @@ struct DropRule {
 // SCAR_OK, or what is wrong with the caller's rule (nullptr: nothing is dropped).  The probability is taken to the nearest
 // multiple of 2^-16 that is neither 0 nor 1 unless it is 0 or 1 itself; the scale is of the one taken, so means are kept.
 inline int make_rule(const scar_dropout *d, DropRule *out) {
-    *out = DropRule{0, 0, 0, 0, 1.f, 0, nullptr};
+    *out = DropRule{};
+    out->scale = 1.f;
     if (!d) return SCAR_OK;
     if (!(d->p >= 0. && d->p <= 1.) || (uintptr_t)d->d_offset % 8) return SCAR_ERR_INVALID_ARG;
     unsigned cut = (unsigned)std::floor(d->p * 65536. + 0.5);
     if (d->p > 0. && cut == 0) cut = 1;
     if (d->p < 1. && cut == 65536) cut = 65535;
-    *out = DropRule{(unsigned)d->seed, (unsigned)(d->seed >> 32), cut != 0, cut * 65536u - 1u, cut == 65536 ? 0.f : 65536.f / (float)(65536 - cut), d->offset,
-                    reinterpret_cast<const unsigned long long *>(d->d_offset)};
+    for (unsigned i = 0; i < 10; ++i) {
+        out->key[2 * i] = (unsigned)d->seed + i * 0x9E3779B9u;
+        out->key[2 * i + 1] = (unsigned)(d->seed >> 32) + i * 0xBB67AE85u;
+    }
+    out->on = cut != 0;
+    out->above = cut * 65536u - 1u;
+    out->scale = cut == 65536 ? 0.f : 65536.f / (float)(65536 - cut);
+    out->offset = d->offset;
+    out->d_offset = reinterpret_cast<const unsigned long long *>(d->d_offset);
     return SCAR_OK;
 }
 
 // The 16-bit values of columns 8 * block .. 8 * block + 7 of a row, two per word, the lower column in the lower half.
 __device__ __forceinline__ uint4 mask_bits(const DropRule &r, unsigned long long offset, unsigned row, unsigned block) {
     uint4 c = make_uint4(block, row, (unsigned)offset, (unsigned)(offset >> 32));
-    unsigned k0 = r.key0, k1 = r.key1;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
         const unsigned long long a = (unsigned long long)c.x * 0xD2511F53u, b = (unsigned long long)c.z * 0xCD9E8D57u;
-        c = make_uint4((unsigned)(b >> 32) ^ c.y ^ k0, (unsigned)b, (unsigned)(a >> 32) ^ c.w ^ k1, (unsigned)a);
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
+        c = make_uint4((unsigned)(b >> 32) ^ c.y ^ r.key[2 * i], (unsigned)b, (unsigned)(a >> 32) ^ c.w ^ r.key[2 * i + 1], (unsigned)a);
     }
     return c;
 }
