@@ -458,7 +458,6 @@ bool has_slope(const scar_linear *op) { return op->cfg.activation != SCAR_ACT_ID
 // x and w as the products read them: in place, or copied.
 struct Operands {
     Operand x, w;
-    bool w_copied;
 };
 template <typename T>
 int place(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t wp, unsigned rows, bool want_x, bool want_w, Operands *o) {
@@ -470,7 +469,6 @@ int place(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t wp, uns
     if (cw && !op->w && (rc = linear_alloc(op, &op->w, PL * N * op->kp * 2)) != SCAR_OK) return rc;
     o->x = cx ? Operand{op->x, K, rows, op->kp, PL, x_rows * op->kp} : Operand{x, K, rows, rows > 1 ? xp : op->kp, 1, 0};
     o->w = cw ? Operand{op->w, K, N, op->kp, PL, N * op->kp} : Operand{w, K, N, N > 1 ? wp : op->kp, 1, 0};
-    o->w_copied = cw;
     if (!cx && !cw) return SCAR_OK;
     const Copy<T> a{x, xp, cx ? rows : 0u, rows_aligned(x, xp, sizeof(T)), op->x, x_rows * op->kp};
     const Copy<T> b{w, wp, cw ? (unsigned)N : 0u, rows_aligned(w, wp, sizeof(T)), op->w, N * op->kp};
@@ -593,8 +591,8 @@ int run_forward(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t w
     dispatch_activation(op->cfg.activation, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
         // Rows off 16-byte boundaries go through float32 and the join where that has room: its threads lie along the rows, the product's
-        // across them (1537 x 1001 -> 2003 float16 with such a residual: RAGGED us).  A tensor map's store clips rows to whole 16-byte
-        // words only.
+        // across them (1537 x 1001 -> 2003 float16 with such rows, from cold caches: 14 + 11 us against 46).  A tensor map's store clips rows to
+        // whole 16-byte words only.
         const bool whole = g.out_vec && N % 8 == 0, parts = (!whole || (res && !l.res_vec)) && (uint64_t)rows * op->np * 4 <= op->part_bytes;
         if (PL == 1 && g.splits == 1 && !parts) {
             g.c_map = whole;

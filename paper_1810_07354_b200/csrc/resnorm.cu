@@ -3,7 +3,7 @@
 //   u = f or N(f; w_post, b_post)      y = x + scale gate u      n = N(y; w_pre, b_pre)
 //   N(v) = (v - mean) r w + b, r = 1 / sqrt(mean of (v - mean)^2 + eps)      (RMS: without mean and b)
 //
-// and the gradients.  A CTA holds a row in its registers, so x, f and the gate are read once and y and n written once; backward
+// and the gradients.  A CTA has a whole row at hand, so x, f and the gate are read once and y and n written once; backward
 // reads dy, dn, y, f and the gate once and forms the statistics again from them: storing them would save one of two reductions
 // and cost the caller a tensor.  With g = dn w_pre, h = du w_post and hats for normalised rows:
 //
@@ -13,10 +13,11 @@
 // A row's mean is summed first and its squared deviations from it second: no sum of squares is taken far from the mean, so rows
 // whose mean is large beside their deviation keep theirs.
 //
-// Memory is what bounds it, so the next rows are always on their way: a ring of rows in shared memory, filled by bulk copies
-// (cp.async.bulk) that one warp issues.  A stage is free again at the row's first reduction, when every thread has its values in
-// registers.  Rows longer than 4096 values are cut over the CTAs of a cluster, which exchange their sums through distributed
-// shared memory: a thread has eight values of a row whatever its length, and its columns' sums fit its registers.
+// Memory is what bounds it (16384 x 4096 bfloat16, both norms, a gate for each value: 106 us forward, 6.3 TB/s, and 191 backward,
+// 5.6), so the next rows are always on their way: a ring of rows in shared memory, filled by bulk copies (cp.async.bulk) that one warp
+// issues.  A stage is filled again behind the first barrier that every thread reaches when it is done with the row.  Rows longer than
+// 4096 values are cut over the CTAs of a cluster, which exchange their sums through distributed shared memory: a thread has the
+// same number of a row's values whatever its length, and its columns' sums over the rows fit its registers.
 //
 // Sums over rows: a CTA walks a run of rows and keeps its threads' columns in registers; k_resnorm_join adds the CTAs' sums in
 // order.  Gates shared by several rows end inside a CTA's run, or reach over its ends: those leave partial sums too.
@@ -34,10 +35,11 @@ namespace {
 
 constexpr unsigned kSpan = 4096;  // columns of a CTA at most
 constexpr unsigned kMostStages = 6;
-// Values of a row that a thread has, and rows that it has under way at a time.  Forward: 16, so that what a thread does once per row
-// (waits, sums over the CTA, addresses) is shared by many (16384 x 4096 bfloat16: 110 us, with 8 values 187).  Backward: the sums
-// over rows take two to five registers a value; eight values and two rows share those, and the rows' sums over the CTA are one
-// reduction.  float32 rows leave no room in shared memory for two at a time, and have twice the time.
+// Values of a row that a thread has, rows that a CTA takes at a time, CTAs of an SM that the registers are for.  16 values, so that
+// what a thread does once per row (waits, sums over the CTA, addresses) is shared by many: 16384 x 4096 bfloat16 forward 110 us, with
+// eight 187; backward 214 and 317.  Backward with means and biases has four sums over rows for every column, for which 128 registers hold
+// eight columns: there two 16-bit rows at a time share what is done once (282 us; 16 columns and one CTA an SM 317, eight and a single
+// row 324).  Two float32 rows at a time find no room in shared memory.
 constexpr int kForwardValues = 16;
 __host__ __device__ constexpr int back_values(bool layer) { return layer ? 8 : 16; }
 template <typename T> __host__ __device__ constexpr int back_rows(bool layer) { return layer && sizeof(T) == 2 ? 2 : 1; }
