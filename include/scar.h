@@ -609,8 +609,8 @@ int scar_dropout_apply(const scar_dropout *rule, scar_dtype dtype, const void *d
  * and from dy [T, N] (the residual's gradient is dy itself):
  *   dz = mask . dy . act'(z),   dx = dz w,   dw = dz^T x,   dbias = sum_t dz
  * act: z; max(z, 0) (derivative 0 at 0); z Phi(z) with the Gaussian's distribution function Phi; z / (1 + exp(-z)).
- * Forward leaves act'(z) in the caller's d_slope, [T][N rounded up to 8] values of float16 (float32 beside float32
- * operands), for backward; the mask is computed again.  16-bit operands: y is rounded once, dz once for the two
+ * Forward leaves act'(z) in the caller's d_slope, [T][N rounded up to 8] values of float16 beside bfloat16 operands and
+ * of float32 beside the others, for backward; the mask is computed again.  16-bit operands: y is rounded once, dz once for the two
  * products (the matrix instruction takes operands of one type; a float16 dz beyond its range is infinite), dx, dw and
  * dbias once; sums are float32.  In float32 an infinity in x, w or dy acts as a NaN in the products. */
 typedef struct scar_linear scar_linear; /* opaque; created by scar_linear_init, freed by scar_linear_destroy */

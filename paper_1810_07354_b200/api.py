@@ -1132,7 +1132,7 @@ class LinearLayer(_Rows):
         return (None, None) if dropout is None else (dropout.at(self._device), dropout.tensor)
 
     def _slope_type(self):
-        return self._torch.float32 if self.dtype == self._torch.float32 else self._torch.float16
+        return self._torch.float16 if self.dtype == self._torch.bfloat16 else self._torch.float32
 
     def _slope(self, slope, rows: int):
         if self.activation == "identity":

@@ -6,8 +6,8 @@
 //   backward   k_linear_dz: dz = m . dy . slope, rounded to the operands' type (float32: three bfloat16 planes), and its sums
 //              over the rows; dx = dz w and dw = dz^T x in one launch (k_tc_gemm)
 //
-// The derivative and not z is kept: it lies in [-0.13, 1.13], so float16 holds it to 2^-11 of itself whatever the operands'
-// type, and backward needs no activation.  Computing z again instead would be 8 rather than 6 T K N operations.
+// The derivative and not z is kept: it lies in [-0.13, 1.13], so float16 holds it to 2^-11 of itself beside bfloat16 (float32 beside
+// the other types, where that would show), and backward needs no activation.  Computing z again instead would be 8 rather than 6 T K N operations.
 #include <algorithm>
 #include <new>
 #include <vector>
@@ -43,7 +43,7 @@ __device__ __forceinline__ void finish8(const LayerArgs &l, T *out, unsigned lon
     if (has) layer8<ACT, T>(l, offset, row, col, n, z, slope);
     if (l.slope && has) {
         const unsigned long long at = (unsigned long long)row * ((n + 7) & ~7u) + col;
-        if constexpr (sizeof(T) == 4) {
+        if constexpr (!kHalfSlope<T>) {
             float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(l.slope) + at);
             o[0] = make_float4(slope[0].x, slope[0].y, slope[1].x, slope[1].y);
             o[1] = make_float4(slope[2].x, slope[2].y, slope[3].x, slope[3].y);
@@ -95,7 +95,7 @@ template <typename T> struct FewArgs {
     unsigned long long x_pitch, w_pitch;
     unsigned rows, n, k;
     unsigned parts;  // CTAs of a cluster that share the sum over k (16-bit types)
-    int x_vec;       // rows of x on 16-byte boundaries
+    int x_vec, w_vec;  // rows on 16-byte boundaries
     int act;
     T *out;
     unsigned long long out_pitch;
@@ -132,98 +132,27 @@ template <typename T> __device__ __forceinline__ void mma_16x8x16(float (&d)[4],
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 16-bit types: w's rows are the rows of 16 x 8 x 16 matrix instructions, which tcgen05's 128 would leave empty; 8 * NT rows of x.
-// A lane's 16 bytes of a row, eight values of k, are the operands of two instructions: which k a slot of the instruction stands
-// for does not matter as long as w and x agree.  What a lane reads goes through shared memory, asynchronously and some rounds ahead,
-// and back to the same lane: nothing is exchanged there, it takes the place of registers that the loads would wait in (4096 -> 16384
-// bfloat16: one row 25 us, 16 rows 29; loads straight to registers 24 and 39).
+// The accumulators of a CTA's warps (and of its cluster's CTAs) to the layer's columns from n0 on; sums:
+// [8][8 * NT][kFewPad] floats of shared memory.
 constexpr int RM = 2;  // 16 rows of w each
-template <int NT, int AHEAD> struct Few16 {
-    static constexpr int kLoads = 2 * RM + NT;  // 16 bytes each, of a lane and round
-    static constexpr int kRound = 256 * 16 * kLoads;
-    static constexpr int kAhead = AHEAD;  // rounds, with the one that is read
-    static constexpr int kTokens = 8 * NT, kPad = 16 * RM + 4;
-    static constexpr int kSums = 8 * kTokens * kPad * 4;
-    static constexpr int kSmem = kAhead * kRound > kSums ? kAhead * kRound : kSums;
-};
-__device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
-template <typename T, int NT, int AHEAD>
-__global__ void __launch_bounds__(256) k_linear_few16(const __grid_constant__ FewArgs<T> g) {
-    using S = Few16<NT, AHEAD>;
-    extern __shared__ __align__(16) uint8_t few_smem[];
+constexpr int kFewPad = 16 * RM + 4;
+template <typename T, int NT>
+__device__ __forceinline__ void finish_tiles(const FewArgs<T> &g, float *sums, const float (&acc)[RM][NT][4], unsigned part, unsigned n0) {
+    constexpr int kTokens = 8 * NT;
     const unsigned warp = threadIdx.x / 32, lane = threadIdx.x & 31, group = lane >> 2, quad = lane & 3;
-    const unsigned part = g.parts > 1 ? cluster_rank() : 0u, n0 = blockIdx.x / g.parts * (16 * RM), blocks = (g.k + 31) / 32;
-    const T *w[2 * RM], *x[NT];
-    bool has_w[2 * RM], has_x[NT];
-#pragma unroll
-    for (int i = 0; i < 2 * RM; ++i) {
-        const unsigned r = n0 + i * 8 + group;
-        has_w[i] = r < g.n;
-        w[i] = g.w + (has_w[i] ? r : 0u) * g.w_pitch;
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const unsigned r = t * 8 + group;
-        has_x[t] = r < g.rows;
-        x[t] = g.x + (has_x[t] ? r : 0u) * g.x_pitch;
-    }
-    griddep_start();
-    uint8_t *const mine = few_smem + threadIdx.x * 16;
-    const uint32_t slot0 = smem_addr(mine);
-    const auto issue = [&](unsigned round, unsigned slot) {
-        const unsigned k = ((round * g.parts + part) * 8 + warp) * 32 + quad * 8;
-        const bool in = k < g.k;  // k is a multiple of 8
-        const unsigned at = in ? k : 0u;
-        const uint32_t to = slot0 + slot * S::kRound;
-#pragma unroll
-        for (int i = 0; i < 2 * RM; ++i) copy16(to + i * 4096, w[i] + at, in && has_w[i]);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) copy16(to + (2 * RM + t) * 4096, x[t] + at, in && has_x[t]);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    float acc[RM][NT][4] = {};
-    const unsigned rounds = (blocks + 8 * g.parts - 1) / (8 * g.parts);  // what lies behind the last block is copied as zeros
-#pragma unroll
-    for (int i = 0; i < S::kAhead - 1; ++i) issue(i, i);
-    unsigned slot = 0;
-    for (unsigned r = 0; r < rounds; ++r) {
-        issue(r + S::kAhead - 1, slot ? slot - 1 : S::kAhead - 1);
-        asm volatile("cp.async.wait_group %0;" ::"n"(S::kAhead - 1) : "memory");
-        const uint8_t *from = mine + slot * S::kRound;
-        uint4 a[2 * RM], v[NT];
-#pragma unroll
-        for (int i = 0; i < 2 * RM; ++i) a[i] = *reinterpret_cast<const uint4 *>(from + i * 4096);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) v[t] = *reinterpret_cast<const uint4 *>(from + (2 * RM + t) * 4096);
-#pragma unroll
-        for (int m = 0; m < RM; ++m)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                mma_16x8x16<T>(acc[m][t], a[2 * m].x, a[2 * m + 1].x, a[2 * m].y, a[2 * m + 1].y, v[t].x, v[t].y);
-                mma_16x8x16<T>(acc[m][t], a[2 * m].z, a[2 * m + 1].z, a[2 * m].w, a[2 * m + 1].w, v[t].z, v[t].w);
-            }
-        if (++slot == S::kAhead) slot = 0;
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncthreads();
-    float *const sums = reinterpret_cast<float *>(few_smem);  // [8][kTokens][kPad]
 #pragma unroll
     for (int m = 0; m < RM; ++m)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                sums[(warp * S::kTokens + t * 8 + quad * 2 + (i & 1)) * S::kPad + m * 16 + (i >> 1) * 8 + group] = acc[m][t][i];
+            for (int i = 0; i < 4; ++i) sums[(warp * kTokens + t * 8 + quad * 2 + (i & 1)) * kFewPad + m * 16 + (i >> 1) * 8 + group] = acc[m][t][i];
     __syncthreads();
     const unsigned row = threadIdx.x / (2 * RM), col = threadIdx.x % (2 * RM) * 8;
-    const bool has = row < g.rows && row < S::kTokens && n0 + col < g.n;
+    const bool has = row < g.rows && row < kTokens && n0 + col < g.n;
     float2 z[4] = {};
-    if (has) add_warps(sums + row * S::kPad + col, S::kTokens * S::kPad, z);
+    if (has) add_warps(sums + row * kFewPad + col, kTokens * kFewPad, z);
     if (g.parts > 1) {  // the first CTA adds the others' in order
-        float4 *const whole = reinterpret_cast<float4 *>(sums + row * S::kPad + col);  // of the first warp: this thread alone has read it
-        __syncthreads();
+        float4 *const whole = reinterpret_cast<float4 *>(sums + row * kFewPad + col);  // of the first warp: this thread alone has read it
         if (has) {
             whole[0] = make_float4(z[0].x, z[0].y, z[1].x, z[1].y);
             whole[1] = make_float4(z[2].x, z[2].y, z[3].x, z[3].y);
@@ -250,13 +179,174 @@ __global__ void __launch_bounds__(256) k_linear_few16(const __grid_constant__ Fe
     if (part == 0) finish_few(g, row, n0 + col, z, has);
 }
 
-// float32: eight rows of w, TT rows of x at a time (blockIdx.y), the products on the ordinary cores, two at an instruction.
+// w's rows are the rows of 16 x 8 x 16 matrix instructions, which tcgen05's 128 would leave empty; x's rows, 8 * NT of them, the
+// columns.  A lane's eight values of k of a row are the operands of two instructions: which k a slot of the
+// instruction stands for does not matter as long as w and x agree.  float32 values are split into three bfloat16 planes in registers (six
+// products of planes, smallest first).  What a lane reads goes through shared memory, asynchronously and some rounds ahead, and back to
+// the same lane: nothing is exchanged there, it takes the place of registers that the loads would wait in (4096 -> 16384 bfloat16: one
+// row 25 us, 16 rows 29; loads straight to registers 24 and 39).  Rows anywhere (VEC false): a lane copies the aligned 16-byte words
+// that its values begin in, reads the next one from its neighbour's copy, and the last of a row's four lanes has one word more; a word
+// that begins before the matrix is copied value by value, and of one that ends behind it what lies in it.
+template <typename T, int NT, int AHEAD, bool VEC> struct Few {
+    static constexpr int kRows = 2 * RM + NT;           // of a lane
+    static constexpr int kWords = sizeof(T) / 2;        // of 16 bytes, eight values
+    static constexpr int kMore = VEC ? 0 : 1024;        // bytes of the words behind the four lanes', a row
+    static constexpr int kRow = kWords * 4096 + kMore;  // of all threads
+    static constexpr int kRound = kRows * kRow;
+    static constexpr int kAhead = AHEAD;                // rounds, with the one that is read
+    static constexpr int kSums = 8 * 8 * NT * kFewPad * 4;
+    static constexpr int kSmem = kAhead * kRound > kSums ? kAhead * kRound : kSums;
+};
+__device__ __forceinline__ void copy16(uint32_t to, const void *from, unsigned bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+template <typename T, int NT, int AHEAD, bool VEC>
+__global__ void __launch_bounds__(256) k_linear_few(const __grid_constant__ FewArgs<T> g) {
+    using S = Few<T, NT, AHEAD, VEC>;
+    constexpr int PL = sizeof(T) == 4 ? 3 : 1, kPairs = PL == 1 ? 1 : 6;
+    constexpr int pw[6] = {PL == 1 ? 0 : 2, 1, 0, 1, 0, 0}, px[6] = {0, 1, 2, 0, 1, 0};
+    extern __shared__ __align__(16) uint8_t few_smem[];
+    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x & 31, group = lane >> 2, quad = lane & 3;
+    const unsigned part = g.parts > 1 ? cluster_rank() : 0u, n0 = blockIdx.x / g.parts * (16 * RM);
+    const T *row[S::kRows];
+    bool has[S::kRows];
+#pragma unroll
+    for (int i = 0; i < S::kRows; ++i) {
+        const unsigned r = i < 2 * RM ? n0 + i * 8 + group : (i - 2 * RM) * 8 + group;
+        has[i] = r < (i < 2 * RM ? g.n : g.rows);
+        row[i] = i < 2 * RM ? g.w + (has[i] ? r : 0u) * g.w_pitch : g.x + (has[i] ? r : 0u) * g.x_pitch;
+    }
+    griddep_start();
+    uint8_t *const mine = few_smem + threadIdx.x * 16, *const more = few_smem + S::kWords * 4096 + (warp * 8 + group) * 16;
+    const uint32_t slot0 = smem_addr(mine), more0 = smem_addr(more);
+    const auto issue = [&](unsigned round, unsigned slot) {
+        const unsigned k = ((round * g.parts + part) * 8 + warp) * 32 + quad * 8;
+#pragma unroll
+        for (int i = 0; i < S::kRows; ++i) {
+            const uint32_t at = slot * S::kRound + i * S::kRow;
+            if (VEC) {  // k is a multiple of a word's values
+                const bool in = k < g.k && has[i];
+                const T *p = row[i] + (k < g.k ? k : 0u);
+#pragma unroll
+                for (int q = 0; q < S::kWords; ++q) {
+                    const bool there = in && k + q * (16 / sizeof(T)) < g.k;
+                    copy16(slot0 + at + q * 4096, there ? p + q * (16 / sizeof(T)) : p, there ? 16u : 0u);
+                }
+            } else {
+                // this lane's words, and the bytes from there to the end of the row: what lies behind it is not read
+                const unsigned off = (unsigned)(uintptr_t)row[i] & 15u;
+                const char *const word = reinterpret_cast<const char *>(row[i]) - off + (unsigned long long)k * sizeof(T);
+                const long long to_end = has[i] ? (long long)off + ((long long)g.k - (long long)k) * (long long)sizeof(T) : 0ll;
+                const int left = (int)min(max(to_end, 0ll), 64ll);
+                if (word < reinterpret_cast<const char *>(i < 2 * RM ? g.w : g.x)) {
+                    if (has[i])
+#pragma unroll 1
+                        for (unsigned j = 0; j < g.k && off + j * sizeof(T) < 16 * S::kWords; ++j)
+                            *reinterpret_cast<T *>(mine + at + (off + j * sizeof(T)) / 16 * 4096 + (off + j * sizeof(T)) % 16) = row[i][j];
+                } else {
+#pragma unroll
+                    for (int q = 0; q < S::kWords; ++q) {
+                        const int n = min(max(left - q * 16, 0), 16);
+                        copy16(slot0 + at + q * 4096, n ? word + q * 16 : reinterpret_cast<const char *>(row[i]) - off + 16, (unsigned)n);
+                    }
+                }
+                if (quad == 3) {
+                    const int n = min(max(left - 16 * S::kWords, 0), 16);
+                    copy16(more0 + at, n ? word + 16 * S::kWords : reinterpret_cast<const char *>(row[i]) - off + 16, (unsigned)n);
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // The eight values of row i from k on, zeros behind the row's end.
+    const auto fetch = [&](int i, unsigned k, unsigned slot, Pack8<T> &v) {
+        const uint8_t *const from = mine + slot * S::kRound + i * S::kRow;
+        uint4 u[S::kWords + 1];
+#pragma unroll
+        for (int q = 0; q < S::kWords; ++q) u[q] = *reinterpret_cast<const uint4 *>(from + q * 4096);
+        if (VEC) {
+#pragma unroll
+            for (int q = 0; q < S::kWords; ++q) v.u[q] = u[q];
+            return;
+        }
+        u[S::kWords] = *reinterpret_cast<const uint4 *>(quad == 3 ? more + slot * S::kRound + i * S::kRow : from + 16);
+        const unsigned off = (unsigned)(uintptr_t)row[i] & 15u;
+#pragma unroll
+        for (int q = 0; q < S::kWords; ++q) v.u[q] = off ? shifted(u[q], u[q + 1], off) : u[q];
+        if (k + 8 > g.k || !has[i]) {
+#pragma unroll
+            for (unsigned j = 0; j < 8; ++j)
+                if (k + j >= g.k || !has[i]) v.v[j] = from_f32<T>(0.f);
+        }
+    };
+    const auto planes = [&](const Pack8<T> &v, uint4 (&p)[PL]) {
+        if constexpr (PL == 1) {
+            p[0] = v.u[0];
+        } else {
+            // By cutting, not by rounding: 8 + 8 + 8 bits are exact, nothing overflows, and what the six products leave out stays below
+            // 2^-21 of the whole.
+            unsigned *const to[3] = {&p[0].x, &p[1].x, &p[2].x};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 x = make_float2(v.v[2 * j], v.v[2 * j + 1]);
+                const float2 c0 = make_float2(__uint_as_float(__float_as_uint(x.x) & 0xffff0000u), __uint_as_float(__float_as_uint(x.y) & 0xffff0000u));
+                const float2 r1 = add2(x, make_float2(-c0.x, -c0.y));
+                const float2 c1 = make_float2(__uint_as_float(__float_as_uint(r1.x) & 0xffff0000u), __uint_as_float(__float_as_uint(r1.y) & 0xffff0000u));
+                const float2 r2 = add2(r1, make_float2(-c1.x, -c1.y));
+                to[0][j] = __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632);
+                to[1][j] = __byte_perm(__float_as_uint(r1.x), __float_as_uint(r1.y), 0x7632);
+                to[2][j] = __byte_perm(__float_as_uint(r2.x), __float_as_uint(r2.y), 0x7632);
+            }
+        }
+    };
+    using M = typename std::conditional<PL == 3, __nv_bfloat16, T>::type;
+    float acc[RM][NT][4] = {};
+    const unsigned rounds = (g.k + 256 * g.parts - 1) / (256 * g.parts);
+#pragma unroll 1
+    for (int i = 0; i < S::kAhead - 1; ++i) issue(i, i);
+    unsigned slot = 0;
+#pragma unroll 1
+    for (unsigned r = 0; r < rounds; ++r) {
+        if (!VEC) __syncwarp();  // the neighbours have read the slot that is filled now
+        issue(r + S::kAhead - 1, slot ? slot - 1 : S::kAhead - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kAhead - 1) : "memory");
+        if (!VEC) __syncwarp();
+        const unsigned k = ((r * g.parts + part) * 8 + warp) * 32 + quad * 8;
+        uint4 a[2 * RM][PL];
+        Pack8<T> v;
+#pragma unroll
+        for (int i = 0; i < 2 * RM; ++i) {
+            fetch(i, k, slot, v);
+            planes(v, a[i]);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            uint4 b[PL];
+            fetch(2 * RM + t, k, slot, v);
+            planes(v, b);
+#pragma unroll
+            for (int m = 0; m < RM; ++m)
+#pragma unroll
+                for (int q = 0; q < kPairs; ++q) {
+                    const uint4 &p = a[2 * m][pw[q]], &o = a[2 * m + 1][pw[q]], &c = b[px[q]];
+                    mma_16x8x16<M>(acc[m][t], p.x, o.x, p.y, o.y, c.x, c.y);
+                    mma_16x8x16<M>(acc[m][t], p.z, o.z, p.w, o.w, c.z, c.w);
+                }
+        }
+        if (++slot == S::kAhead) slot = 0;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    finish_tiles<T, NT>(g, reinterpret_cast<float *>(few_smem), acc, part, n0);
+}
+
+// float32, up to four rows: eight rows of w, the products on the ordinary cores, two at an instruction (4096 -> 4096 on one row: 11 us).
 template <int TT>
 __global__ void __launch_bounds__(256) k_linear_few32(const __grid_constant__ FewArgs<float> g) {
     constexpr int R = 8, V = R * TT;
     __shared__ __align__(16) float sh[8][TT][R];
     griddep_start();
-    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x & 31, n0 = blockIdx.x * R, t0 = blockIdx.y * TT;
+    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x & 31, n0 = blockIdx.x * R;
     const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
     float2 acc[R][TT];
 #pragma unroll
@@ -269,8 +359,8 @@ __global__ void __launch_bounds__(256) k_linear_few32(const __grid_constant__ Fe
         for (int r = 0; r < R; ++r) w[r] = n0 + r < g.n ? *reinterpret_cast<const float4 *>(g.w + (n0 + r) * g.w_pitch + k) : none;
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            const float *p = g.x + (t0 + t) * g.x_pitch + k;
-            x[t] = t0 + t >= g.rows ? none : g.x_vec ? *reinterpret_cast<const float4 *>(p) : make_float4(p[0], p[1], p[2], p[3]);
+            const float *p = g.x + t * g.x_pitch + k;
+            x[t] = t >= (int)g.rows ? none : g.x_vec ? *reinterpret_cast<const float4 *>(p) : make_float4(p[0], p[1], p[2], p[3]);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -300,10 +390,10 @@ __global__ void __launch_bounds__(256) k_linear_few32(const __grid_constant__ Fe
     __syncthreads();
     const unsigned t = threadIdx.x;
     if (t >= 32) return;
-    const bool has = t < TT && t0 + t < g.rows;
+    const bool has = t < TT && t < g.rows;
     float2 z[4] = {};
     if (has) add_warps(&sh[0][t][0], V, z);
-    finish_few(g, t0 + t, n0, z, has);
+    finish_few(g, t, n0, z, has);
 }
 
 // dz and its sums over the rows.  A CTA has 256 columns, eight per lane, and a run of rows, one per warp at a time.
@@ -331,7 +421,7 @@ __global__ void __launch_bounds__(256, kDzCtas) k_linear_dz(const __grid_constan
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 256 + lane * 8;
     const unsigned r1 = min(g.rows, (blockIdx.y + 1) * g.per_cta);
     const unsigned long long offset = g.drop.on ? g.drop.at() : 0ull;
-    using S = typename std::conditional<sizeof(T) == 4, float, __half>::type;
+    using S = typename std::conditional<kHalfSlope<T>, __half, float>::type;
     float2 sum[4] = {};
     if (col < g.n) {
         for (unsigned r0 = blockIdx.y * g.per_cta + warp; r0 < r1; r0 += 8 * kDzRows) {
@@ -452,7 +542,7 @@ template <typename P> int linear_alloc(scar_linear *op, P **p, uint64_t bytes) {
     return SCAR_OK;
 }
 
-uint64_t slope_size(const scar_linear *op) { return op->cfg.dtype == SCAR_F32 ? 4 : 2; }
+uint64_t slope_size(const scar_linear *op) { return op->cfg.dtype == SCAR_BF16 ? 2 : 4; }
 bool has_slope(const scar_linear *op) { return op->cfg.activation != SCAR_ACT_IDENTITY; }
 
 // x and w as the products read them: in place, or copied.
@@ -509,45 +599,58 @@ int finish(scar_linear *op) {
     return SCAR_OK;
 }
 
-// Rows up to which w is read this way: 4096 -> 16384 bfloat16 takes 33 us with 32 rows, the product kernel 35 with 64.  float32 rows
-// go four at a time, the second four with w from L2 where that holds it: 32 rows of 4096 -> 4096 take 70 us (the product kernel 76), 8
-// rows of 4096 -> 8192 81 us and 32 308 (as planes 131).
-constexpr unsigned kFewRows = 32, kFewFar = 8;
-constexpr uint64_t kL2Holds = 64ull << 20;
-template <typename T> bool few_rows(const scar_linear *op, unsigned rows) {
-    return rows <= kFewRows && (sizeof(T) == 2 || rows <= kFewFar || op->cfg.out_features * op->cfg.in_features * 4 <= kL2Holds);
-}
-// f(kernel, NT, AHEAD, shared memory) for every instance.
+// Rows up to which w is read this way, where it lies on 16-byte boundaries and where it does not.  bfloat16, 4096 -> 16384: 32 rows 33 us,
+// the product kernel 35 with 64.  2395 -> 16196: one row 46 us, 16 rows 55, 32 rows 74, the product kernel with its copies 58.  float32,
+// 4096 -> 8192: 32 rows 107 us, 64 rows 203, the product kernel with its planes 131; 2161 -> 11904, 59 rows: 277 and 120.
+constexpr unsigned kFewRows = 32, kFewOdd = 16;
+// f(kernel, NT, AHEAD, whether rows lie on 16-byte boundaries, shared memory) for every instance: two or three CTAs of an SM where that
+// leaves three rounds or more, else one.
+template <typename T, int NT, int AHEAD, bool VEC, typename F> void one_few(F &&f) { f(k_linear_few<T, NT, AHEAD, VEC>, NT, AHEAD, VEC, (unsigned)Few<T, NT, AHEAD, VEC>::kSmem); }
 template <typename T, typename F> void for_few(F &&f) {
-    f(k_linear_few16<T, 1, 4>, 1u, 4u, (unsigned)Few16<1, 4>::kSmem);
-    f(k_linear_few16<T, 2, 3>, 2u, 3u, (unsigned)Few16<2, 3>::kSmem);
-    f(k_linear_few16<T, 2, 4>, 2u, 4u, (unsigned)Few16<2, 4>::kSmem);
-    f(k_linear_few16<T, 4, 3>, 4u, 3u, (unsigned)Few16<4, 3>::kSmem);
+    if constexpr (sizeof(T) == 2) {
+        one_few<T, 1, 4, true>(f);
+        one_few<T, 2, 3, true>(f);
+        one_few<T, 2, 4, true>(f);
+        one_few<T, 4, 3, true>(f);
+        one_few<T, 1, 4, false>(f);
+        one_few<T, 2, 3, false>(f);
+        one_few<T, 4, 2, false>(f);
+    } else {
+        one_few<T, 1, 2, true>(f);
+        one_few<T, 2, 2, true>(f);
+        one_few<T, 4, 3, true>(f);
+        one_few<T, 1, 2, false>(f);
+        one_few<T, 2, 2, false>(f);
+        one_few<T, 4, 3, false>(f);
+    }
 }
 template <typename T> bool allow_few() {
     bool ok = true;
-    for_few<T>([&](auto kernel, unsigned, unsigned, unsigned smem) { ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess; });
+    for_few<T>([&](auto kernel, int, int, bool, unsigned smem) { ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess; });
     return ok;
 }
-template <typename T> void run_few(scar_linear *op, const FewArgs<T> &f) {
+template <typename T> void run_few(scar_linear *op, FewArgs<T> g) {
+    const unsigned tiles = (g.n + 31) / 32, rounds = (g.k + 255) / 256;
     if constexpr (sizeof(T) == 4) {
-        const unsigned tt = f.rows == 1 ? 1 : f.rows == 2 ? 2 : 4;
-        auto kernel = tt == 1 ? k_linear_few32<1> : tt == 2 ? k_linear_few32<2> : k_linear_few32<4>;
-        launch(op, kernel, dim3((f.n + 7) / 8, (f.rows + tt - 1) / tt), 256, 0, f);
-    } else {
-        // A CTA for every SM is enough, and with few rows of w the sum over k is shared by the CTAs of a cluster to get there: 16384 ->
-        // 2048, one row 14.0 us, 16 rows 18.5 (half as many CTAs 17.5 and 26.1; CTAs of 16 rows of w, which read x twice as often, 17.3
-        // and 21.1).  Weights from memory, 60 calls.
-        FewArgs<T> g = f;
-        const unsigned nt = f.rows <= 8 ? 1 : f.rows <= 16 ? 2 : 4, tiles = (f.n + 31) / 32, rounds = (f.k + 255) / 256;
-        while (g.parts < 8 && tiles * g.parts < 2 * op->pairs && rounds >= 4 * g.parts) g.parts *= 2;
-        // 80 to 96 KiB a CTA, which are two on an SM; up to 16 rows with more CTAs than that, 72 KiB and three (16 rows, 8192 -> 4096: 15.9 us
-        // with the one and 18.7 with the other; 4096 -> 32768 52.5 and 48.3)
-        const unsigned ahead = nt == 4 || (nt == 2 && tiles * g.parts > 4 * op->pairs) ? 3 : 4;
-        for_few<T>([&](auto kernel, unsigned t, unsigned a, unsigned smem) {
-            if (t == nt && a == ahead) launch_clusters(op, kernel, dim3(tiles * g.parts), 256, smem, g.parts, g);
-        });
+        if (g.rows <= 4 && g.w_vec) {
+            const unsigned tt = g.rows == 1 ? 1 : g.rows == 2 ? 2 : 4;
+            auto kernel = tt == 1 ? k_linear_few32<1> : tt == 2 ? k_linear_few32<2> : k_linear_few32<4>;
+            launch(op, kernel, dim3((g.n + 7) / 8), 256, 0, g);
+            return;
+        }
     }
+    // A CTA for every SM is enough, and with few rows of w the sum over k is shared by the CTAs of a cluster to get there: 16384 ->
+    // 2048, one row 14.0 us, 16 rows 18.5 (half as many CTAs 17.5 and 26.1; CTAs of 16 rows of w, which read x twice as often, 17.3
+    // and 21.1).  Weights from memory, 60 calls.
+    while (g.parts < 8 && tiles * g.parts < 2 * op->pairs && rounds >= 4 * g.parts) g.parts *= 2;
+    const int nt = g.rows <= 8 ? 1 : g.rows <= 16 ? 2 : 4;
+    const bool vec = g.w_vec && g.x_vec;
+    // 16 bits, up to 16 rows: 96 KiB a CTA, which are two on an SM, or with more CTAs than that 72 KiB and three (16 rows, 8192 -> 4096: 15.9 us
+    // with the one and 18.7 with the other; 4096 -> 32768 52.5 and 48.3).  Elsewhere there is one.
+    const int ahead = sizeof(T) == 2 && vec && nt == 2 ? (tiles * g.parts > 4 * op->pairs ? 3 : 4) : 0;
+    for_few<T>([&](auto kernel, int t, int a, bool v, unsigned smem) {
+        if (t == nt && v == vec && (!ahead || a == ahead)) launch_clusters(op, kernel, dim3(tiles * g.parts), 256, smem, g.parts, g);
+    });
 }
 
 template <typename T>
@@ -563,16 +666,18 @@ int run_forward(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t w
     layer.res_pitch = rp;
     layer.res_vec = rows_aligned(res, rp, sizeof(T));
     layer.drop = drop;
-    if (few_rows<T>(op, rows) && rows_aligned(w, N > 1 ? wp : 0, sizeof(T)) && K * sizeof(T) % 16 == 0) {
-        FewArgs<T> f{x, w, xp, wp, rows, N, K, 1, rows_aligned(x, rows > 1 ? xp : 0, sizeof(T)), op->cfg.activation, y, yp, rows_aligned(y, yp, sizeof(T)), layer};
-        const bool copy = PL == 1 && !f.x_vec;  // of x alone, to the parts' room
-        if (!copy || (uint64_t)rows * K * 2 <= op->part_bytes) {
-            if (copy) {
-                const Copy<T> a{x, xp, rows, false, reinterpret_cast<unsigned short *>(op->part), 0}, none{x, xp, 0, false, nullptr, 0};
-                launch(op, k_linear_place<T>, (unsigned)std::min<uint64_t>(((uint64_t)rows * (K / 8) + 255) / 256, 16 * op->pairs), 256, 0, a, none, K, K);
-                f.x = reinterpret_cast<const T *>(op->part);
-                f.x_pitch = K;
-            }
+    if (rows <= kFewRows) {
+        const bool words = K * sizeof(T) % 16 == 0;
+        FewArgs<T> f{x, w, xp, wp, rows, N, K, 1, words && rows_aligned(x, rows > 1 ? xp : 0, sizeof(T)), words && rows_aligned(w, N > 1 ? wp : 0, sizeof(T)),
+                     op->cfg.activation, y, yp, rows_aligned(y, yp, sizeof(T)), layer};
+        if (PL == 1 && f.w_vec && !f.x_vec && (uint64_t)rows * K * 2 <= op->part_bytes) {  // with a copy of x alone, in the parts' room
+            const Copy<T> a{x, xp, rows, false, reinterpret_cast<unsigned short *>(op->part), 0}, none{x, xp, 0, false, nullptr, 0};
+            launch(op, k_linear_place<T>, (unsigned)std::min<uint64_t>(((uint64_t)rows * (K / 8) + 255) / 256, 16 * op->pairs), 256, 0, a, none, K, K);
+            f.x = reinterpret_cast<const T *>(op->part);
+            f.x_pitch = K;
+            f.x_vec = 1;
+        }
+        if (rows <= kFewOdd || (f.w_vec && f.x_vec)) {
             run_few(op, f);
             return SCAR_OK;
         }
@@ -597,7 +702,7 @@ int run_forward(scar_linear *op, const T *x, uint64_t xp, const T *w, uint64_t w
         if (PL == 1 && g.splits == 1 && !parts) {
             g.c_map = whole;
             if (g.c_map) rc = make_map(op, &g.c, {y, N, rows, rows > 1 ? yp : op->np, 1, 0}, 32, 2, 64);
-            if (rc == SCAR_OK && slope) rc = make_map(op, &l.slope_map, {slope, op->np, rows, op->np, 1, 0}, 32, 2, 64);
+            if (rc == SCAR_OK && slope) rc = make_map(op, &l.slope_map, {slope, op->np, rows, op->np, 1, 0}, 32, (unsigned)slope_size(op), 64);
             if constexpr (PL == 1) {
                 if (rc == SCAR_OK) launch_tc<1, false, false, (Epi)((int)Epi::kIdentity + ACT)>(op, g);
             }
@@ -712,7 +817,7 @@ int setup(scar_linear *op) {
     if (found != cudaDriverEntryPointSuccess || !fn) return SCAR_ERR_CUDA;
     op->encode = reinterpret_cast<EncodeTiled>(fn);
     const bool f32 = c.dtype == SCAR_F32;
-    if (c.dtype == SCAR_BF16 ? !allow_few<__nv_bfloat16>() : c.dtype == SCAR_F16 && !allow_few<__half>()) return SCAR_ERR_CUDA;
+    if (c.dtype == SCAR_BF16 ? !allow_few<__nv_bfloat16>() : c.dtype == SCAR_F16 ? !allow_few<__half>() : !allow_few<float>()) return SCAR_ERR_CUDA;
     if (f32 ? !allow_smem_all<3>()
             : !(allow_smem_all<1>() && allow_smem(k_tc_gemm<1, false, false, Epi::kIdentity, 1>) && allow_smem(k_tc_gemm<1, false, false, Epi::kRelu, 1>) &&
                 allow_smem(k_tc_gemm<1, false, false, Epi::kGelu, 1>) && allow_smem(k_tc_gemm<1, false, false, Epi::kSilu, 1>)))

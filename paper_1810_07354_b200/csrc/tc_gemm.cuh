@@ -62,7 +62,7 @@ static_assert(TcShape<1>::kStages * TcShape<1>::kStageBytes == TcShape<3>::kStag
 // What a layer's epilogue adds to its product (kIdentity .. kSilu; k_linear_join where the sum was split).
 struct LayerArgs {
     CUtensorMap slope_map;   // of slope, stored through it
-    void *slope;             // [m][n rounded up to 8] the activation's derivative: float16, float32 beside float32; or nullptr
+    void *slope;             // [m][n rounded up to 8] the activation's derivative: float16 beside bfloat16, else float32; or nullptr
     const void *bias, *res;  // each may be nullptr
     unsigned long long res_pitch;
     int bias_vec, res_vec;   // on 16-byte boundaries
@@ -674,6 +674,10 @@ __device__ __forceinline__ void half_write(uint8_t *half, unsigned short *base, 
     __syncwarp();
 }
 
+// The activation's derivative is kept in float16 beside bfloat16: its rounding adds nothing to dz's own there (dx and dw are off by 1.41
+// times what rounding the exact ones costs).  Beside float16 it would (1.73 times), so it is float32 there.
+template <typename T> constexpr bool kHalfSlope = std::is_same<T, __nv_bfloat16>::value;
+
 // A tile's 64 columns of this thread's row, 32 at a time, from the accumulator to the layer's output and slope (16-bit types); r: the
 // residual's first 32 columns, fetched.
 template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const TcArgs &g, uint32_t acc, bool any, const EpiRows &rows, unsigned col, uint8_t *stage, unsigned lane, uint4 (&r)[4]) {
@@ -701,10 +705,19 @@ template <int ACT, typename T> __device__ __forceinline__ void epi_layer(const T
                 for (int i = 0; i < 4; ++i) z[i] = add2(z[i], Two<T>::get(reinterpret_cast<const T *>(r + c) + 2 * i));
             }
             *half_at(out, lane, c) = pack8<T>(z);
-            if (l.slope) *half_at(der, lane, c) = pack8<__half>(slope);
+            if (!l.slope) continue;
+            if constexpr (kHalfSlope<T>) {
+                *half_at(der, lane, c) = pack8<__half>(slope);
+            } else {  // 16 columns of float32 fill the half
+                if (c == 2) stage_free();
+                const float4 s[2] = {make_float4(slope[0].x, slope[0].y, slope[1].x, slope[1].y), make_float4(slope[2].x, slope[2].y, slope[3].x, slope[3].y)};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(half_at(der, lane, (c & 1) * 2 + i)) = s[i];
+                if ((c & 1) && (c == 1 || left > 16)) tma_store(&l.slope_map, smem_addr(der), (int)(at + (c - 1) * 8), (int)rows.row0, 0);
+            }
         }
         if (l.res && j == 0 && left > 32) half_fetch(static_cast<const unsigned short *>(l.res) + at + 32, l.res_pitch, l.res_vec, rows, left - 32, lane, r);
-        if (l.slope) tma_store(&l.slope_map, smem_addr(der), (int)at, (int)rows.row0, 0);
+        if (kHalfSlope<T> && l.slope) tma_store(&l.slope_map, smem_addr(der), (int)at, (int)rows.row0, 0);
         if (g.c_map) tma_store(&g.c, smem_addr(out), (int)at, (int)rows.row0, 0);
         else half_write(out, static_cast<unsigned short *>(g.out) + at, g.out_pitch, g.out_vec, rows, left, lane);
     }

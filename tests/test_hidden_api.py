@@ -109,7 +109,7 @@ class Stand:
 
 def handle(cls, **fields):
     op = object.__new__(cls)
-    fake = types.SimpleNamespace(empty_like=lambda t: Stand(*t.shape, dtype=t.dtype, device=t.device), int64=torch.int64, float32=torch.float32, float16=torch.float16,
+    fake = types.SimpleNamespace(empty_like=lambda t: Stand(*t.shape, dtype=t.dtype, device=t.device), int64=torch.int64, float32=torch.float32, float16=torch.float16, bfloat16=torch.bfloat16,
                                  cuda=types.SimpleNamespace(current_device=lambda: 0))
     op.__dict__.update(_device=HERE, _stream=types.SimpleNamespace(cuda_stream=7), _torch=fake, _here=lambda index: 7, op=0, **fields)
     return op
