@@ -744,7 +744,13 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
     // Results whose rows do not lie on 16-byte boundaries would be stored in pieces of lines, at a tenth of the rate: where the parts'
     // room holds them they go there, and from there to their places.  dw alone may go through the room of w's copy, which dx is done
     // with by then.
-    const bool dx_odd = dx && !rows_aligned(dx, dxp, sizeof(T)), dw_odd = dw && !rows_aligned(dw, dwp, sizeof(T));
+    // A sum that is worth splitting is joined into any place directly.
+    const auto split = [&](TcArgs &g) {
+        choose_splits(op, g, kLaunchS);
+        return g.splits > 1;
+    };
+    const bool dx_split = dx && split(dxg), dw_split = dw && split(dwg);
+    const bool dx_odd = dx && !dx_split && !rows_aligned(dx, dxp, sizeof(T)), dw_odd = dw && !dw_split && !rows_aligned(dw, dwp, sizeof(T));
     const uint64_t dx_room = dx_odd ? round_up((uint64_t)rows * op->kp * sizeof(T), 256) : 0, dw_room = dw_odd ? (uint64_t)N * op->kp * sizeof(T) : 0;
     const bool through = (dx_odd || dw_odd) && dx_room + dw_room <= op->part_bytes;
     const bool through_w = dw_odd && !through && op->w;
@@ -764,17 +770,18 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
         if ((rc = make_map(op, &dwg.a, dz, 64)) != SCAR_OK || (rc = make_map(op, &dwg.b, o.x, 64)) != SCAR_OK) return rc;
         if ((rc = result(dwg, dw, dwp, N, (through && dw_odd) || through_w, dw_at)) != SCAR_OK) return rc;
     }
-    if (through) {  // the parts' room is taken: no sum is split
-        if (dx && dw) launch_both<PL>(op, dxg, dwg);
-        else if (dx) launch_tc<PL, false, true, Epi::kOut>(op, dxg);
-        else launch_tc<PL, true, true, Epi::kOut>(op, dwg);
+    if (through) {  // split ones first: the others then take the parts' room
+        if (dx_split) launch_out<PL, false>(op, dxg);
+        if (dw_split) launch_out<PL, true>(op, dwg);
+        const bool left_dx = dx && !dx_split, left_dw = dw && !dw_split;
+        if (left_dx && left_dw) launch_both<PL>(op, dxg, dwg);
+        else if (left_dx) launch_tc<PL, false, true, Epi::kOut>(op, dxg);
+        else if (left_dw) launch_tc<PL, true, true, Epi::kOut>(op, dwg);
     } else if (dx && dw) {
         launch_grads<PL>(op, dxg, dwg, through_w);
     } else if (dx) {
-        choose_splits(op, dxg, kLaunchS);
         launch_out<PL, false>(op, dxg);
     } else {
-        choose_splits(op, dwg, kLaunchS);
         launch_out<PL, true>(op, dwg);
     }
     const unsigned n0 = through && dx_odd ? rows : 0u, n1 = (through && dw_odd) || through_w ? N : 0u;
