@@ -6,7 +6,7 @@
 //   backward   k_linear_dz: dz = m . dy . slope, rounded to the operands' type (float32: three bfloat16 planes), and its sums
 //              over the rows; dx = dz w and dw = dz^T x in one launch (k_tc_gemm)
 //
-// The derivative and not z is kept: it lies in [-0.13, 1.13], so float16 holds it to 2^-11 of itself beside bfloat16 (float32 beside
+// The derivative and not z is kept: it lies in [-0.13, 1.13], so float16 holds it to 2^-11 of itself or 2^-25 beside bfloat16 (float32 beside
 // the other types, where that would show), and backward needs no activation.  Computing z again instead would be 8 rather than 6 T K N operations.
 #include <algorithm>
 #include <new>

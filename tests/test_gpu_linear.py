@@ -307,3 +307,42 @@ def test_far_rows():
     layer.backward(dy, x, w, slope, dx=out)
     assert torch.equal(out, dx)
     layer.close()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 5, 9, 16, 17, 32])
+@pytest.mark.parametrize("K,N,pad", [(7, 40, 0), (31, 65, 1), (257, 130, 0), (257, 130, 5), (1001, 36, 2), (1002, 300, 0), (1004, 7, 0), (3000, 33, 1)])
+def test_few_rows_anywhere(dt, rows, K, N, pad):
+    layer = LinearLayer(rows, K, N, TYPES[dt], activation="gelu")
+    check(layer, rows, K, N, dt, "gelu", p=0.2, pad=pad)
+    layer.close()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("off,more", [(0, 1), (1, 2), (3, 8), (2, 4), (5, 3)])
+@pytest.mark.parametrize("T,K,N", [(3, 40, 72), (20, 101, 33), (70, 130, 203), (300, 264, 520)])
+def test_results_between_other_values(dt, off, more, T, K, N):
+    """Outputs in the middle of wider rows, wherever these begin: what lies beside them stays, and the results are those of whole tensors."""
+    t = TYPES[dt]
+    layer = LinearLayer(T, K, N, t, activation="silu")
+    x, w, b, res, dy = make(T, K, N, t)
+    y, slope = layer.forward_train(x, w, b, res)
+    dx, dw, _ = layer.backward(dy, x, w, slope)
+    wide = [torch.full((n, off + c + more), 7.0, device="cuda", dtype=t) for n, c in ((T, N), (T, K), (N, K))]
+    part = [v[:, off: off + c] for v, c in zip(wide, (N, K, K))]
+    layer.forward(x, w, b, res, out=part[0])
+    layer.backward(dy, x, w, slope, dx=part[1], dw=part[2])
+    u = 4 * max(unit(t), 2.0 ** -20)  # sums may be split elsewhere: two roundings apart
+    for v, p, whole, c in zip(wide, part, (y, dx, dw), (N, K, K)):
+        assert float((p.double() - whole.double()).norm()) <= u * float(whole.double().norm())
+        assert bool((v[:, :off] == 7).all()) and bool((v[:, off + c:] == 7).all())
+    layer.close()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_many_rows_off_every_boundary(dt):
+    """More than the parts' room holds: results and residual go the product's own way."""
+    T, K, N = 4200, 40, 4101
+    layer = LinearLayer(T, K, N, TYPES[dt], activation="gelu")
+    check(layer, T, K, N, dt, "gelu", p=0.1, pad=1)
+    layer.close()

@@ -341,3 +341,24 @@ def test_reports_of_a_wait_that_gave_up():
     assert e.value.code == -6
     op.status()
     op.close()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("off,more", [(0, 1), (1, 2), (3, 8), (8, 8)])
+@pytest.mark.parametrize("T,D", [(5, 40), (33, 1001), (3, 8200)])
+def test_results_between_other_values(dt, kind, off, more, T, D):
+    """Outputs in the middle of wider rows, wherever these begin: what lies beside them stays, and the results are the same but for the
+    order of a row's sum."""
+    op = ResidualNorm(T, D, TYPES[dt], kind=kind, eps=EPS)
+    c = Case(T, D, dt, kind, group=2)
+    y, n = op.forward(c.x, c.f, **c.kw)
+    got = op.backward(c.dy, c.dn, y, c.f, **c.kw)
+    wide = {k: torch.full((v.shape[0], off + D + more), 7.0, device="cuda", dtype=v.dtype) for k, v in (("y", y), ("n", n), ("dx", y), ("df", y), ("dgate", c.gate))}
+    part = {k: v[:, off: off + D] for k, v in wide.items()}
+    op.forward(c.x, c.f, y=part["y"], n=part["n"], **c.kw)
+    op.backward(c.dy, c.dn, y, c.f, out={k: part[k] for k in ("dx", "df", "dgate")}, **c.kw)
+    for k, whole in (("y", y), ("n", n), *((k, got[k]) for k in ("dx", "df", "dgate"))):
+        assert float((part[k].double() - whole.double()).norm()) <= 2 * max(unit(TYPES[dt]), 2.0 ** -20) * float(whole.double().norm()), k
+        assert bool((wide[k][:, :off] == 7).all()) and bool((wide[k][:, off + D:] == 7).all()), k
+    op.close()
