@@ -1160,7 +1160,8 @@ class LinearLayer(_Rows):
         return (out, slope) if train else out
 
     def forward(self, x, w, bias=None, residual=None, dropout=None, out=None):
-        """The layer's output.  ``dropout``: a mask of a :class:`Dropout` (``drop.mask(offset)``); ``out`` may be the residual."""
+        """The layer's output.  ``dropout``: a mask of a :class:`Dropout` (``drop.mask(offset)``); ``out`` may be the residual and
+        overlaps nothing else."""
         return self._forward(False, x, w, bias, residual, dropout, out, None)
 
     def forward_train(self, x, w, bias=None, residual=None, dropout=None, out=None, slope=None):

@@ -722,7 +722,7 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
     const unsigned K = (unsigned)op->cfg.in_features, N = (unsigned)op->cfg.out_features;
     int rc;
     if (rows == 0) {
-        if (dw) TRAIN_TRY(cudaMemset2DAsync(dw, dwp * sizeof(T), 0, K * sizeof(T), N, op->stream));
+        if (dw) TRAIN_TRY(cudaMemset2DAsync(dw, (N > 1 ? dwp : K) * sizeof(T), 0, K * sizeof(T), N, op->stream));
         if (dbias) TRAIN_TRY(cudaMemsetAsync(dbias, 0, N * sizeof(T), op->stream));
         return SCAR_OK;
     }

@@ -224,6 +224,7 @@ template <typename T, bool VEC, int IN, int R> struct Ring {
             // a row that began further on may have ended here before
             if (j < kEnd && cols + j < (g.array_bytes - 16) / sizeof(T)) p[cols + j] = from_f32<T>(0.f);
         });
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // a later row's copy may write over what was stored here
         __syncwarp();
         if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + 8 * stage) : "memory");
     }

@@ -346,3 +346,15 @@ def test_many_rows_off_every_boundary(dt):
     layer = LinearLayer(T, K, N, TYPES[dt], activation="gelu")
     check(layer, T, K, N, dt, "gelu", p=0.1, pad=1)
     layer.close()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_gradients_of_no_rows_of_a_single_output(dt):
+    """A matrix of one row has no use for its pitch, whatever is given for it."""
+    layer = LinearLayer(8, 37, 1, TYPES[dt], activation="identity")
+    w = torch.ones(1, 37, device="cuda", dtype=TYPES[dt])
+    dw, db = torch.full_like(w, 5), torch.full((1,), 5, device="cuda", dtype=TYPES[dt])
+    api.scar_linear_backward(layer.op, None, 0, None, 0, w.data_ptr(), 0, None, None, 0, None, 0, dw.data_ptr(), 0, db.data_ptr())
+    layer.status()
+    assert bool((dw == 0).all()) and bool((db == 0).all())
+    layer.close()
