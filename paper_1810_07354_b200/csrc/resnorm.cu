@@ -52,6 +52,7 @@ template <typename T> struct In {
     const T *p;
     unsigned long long pitch;
     unsigned per;
+    const T *end;  // of its last row
 };
 enum { kX, kF, kGate, kForwardIn };              // forward
 enum { kDy, kDn, kY, kBackF, kBackGate, kBackwardIn };  // backward
@@ -148,6 +149,11 @@ template <bool VEC, typename T, int N> __device__ __forceinline__ void load_vect
 // v + shift, but zeros stay behind the row.
 template <bool VEC, typename T, int N> __device__ __forceinline__ void shift_row(float2 (&v)[N / 2], float shift, unsigned cols) {
     constexpr int kWord = VEC ? 16 / sizeof(T) : 1;  // all or none of a word's values lie in the row
+    if (!VEC && whole_warp<N>(cols)) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) v[i] = add2(v[i], both(shift));
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < N; i += kWord) {
         const float s = col_of<VEC, T, N>(i) < cols ? shift : 0.f;
@@ -173,9 +179,11 @@ template <int M> __device__ __forceinline__ float dot(const float2 (&a)[M], cons
     return s.x + s.y;
 }
 
-// The CTA's ring of rows.  Its methods that copy are called by all lanes of one warp and by no other warp: a lane per matrix copies
-// the whole 16-byte words of its row; of rows anywhere, lanes read the values before and behind those words one by one and put them
-// in place a row later.  At the barrier of a stage every matrix arrives once, and the values at the rows' ends together once.
+// The CTA's ring of rows.  Its methods that copy are called by all lanes of one warp and by no other warp: a lane per matrix copies the
+// 16-byte words that its row lies in, with what else is in the first and the last one of them.  Where such a word is not the matrix's
+// alone (first and last rows), lanes read the row's values in it one by one and put them in place a row later; done for every row, that
+// takes 192 us forward and 362 backward for 16384 x 4095 bfloat16 instead of 142 and 309.  At the barrier of a stage every matrix arrives
+// once, and the values at the rows' ends together once.
 template <typename T, bool VEC, int IN, int R> struct Ring {
     static constexpr int kEnd = 16 / sizeof(T) - 1;                         // values at one end of a row, at most
     static constexpr int kPasses = VEC ? 1 : (2 * kEnd * IN + 31) / 32;     // rounds of a warp over all ends of a row
@@ -184,6 +192,7 @@ template <typename T, bool VEC, int IN, int R> struct Ring {
     uint32_t full;  // barriers, one per stage
     unsigned col0, cols;
     T edge[R][kPasses];  // on their way to the stages of the rows that were issued last
+    unsigned open[R];    // their matrices, a bit each
 
     __device__ __forceinline__ const T *source(int a, unsigned row) const {
         const In<T> &m = g.in[a];
@@ -194,58 +203,77 @@ template <typename T, bool VEC, int IN, int R> struct Ring {
         const unsigned off = VEC ? 0u : (unsigned)(uintptr_t)source(a, row) & 15u;
         return reinterpret_cast<const T *>(smem + stage * g.stage_bytes + a * g.array_bytes + off);
     }
-    // The whole 16-byte words of a row's values.
-    __device__ __forceinline__ void words(const T *p, uintptr_t &from, uintptr_t &to) const {
+    // The 16-byte words that a row's values are in, or those that hold nothing else.
+    __device__ __forceinline__ bool words(const In<T> &m, const T *p, uintptr_t &from, uintptr_t &to) const {
         const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = a + cols * sizeof(T);
-        from = VEC ? a : (a + 15) & ~uintptr_t(15);
-        to = VEC ? b : b & ~uintptr_t(15);
+        from = a;
+        to = b;
+        if (VEC) return true;
+        from = a & ~uintptr_t(15);
+        to = (b + 15) & ~uintptr_t(15);
+        if (from >= reinterpret_cast<uintptr_t>(m.p) && to <= reinterpret_cast<uintptr_t>(m.end)) return true;
+        from = (a + 15) & ~uintptr_t(15);
+        to = b & ~uintptr_t(15);
         if (to < from) to = from;
+        return false;
     }
     // f(matrix, its row, which of the values behind the row's end, which value of the row or none) for each of this lane's ends.
-    template <typename F> __device__ __forceinline__ void ends(unsigned row, F f) const {
+    template <typename F> __device__ __forceinline__ void ends(unsigned row, unsigned open, F f) const {
 #pragma unroll
         for (int q = 0; q < kPasses; ++q) {
             const unsigned id = q * 32 + (threadIdx.x & 31), a = id / (2 * kEnd), j = id % (2 * kEnd);
-            if (a >= IN || !g.in[a].p) continue;
+            if (a >= IN || !(open >> a & 1u)) continue;
             const T *p = source(a, row);
             uintptr_t from, to;
-            words(p, from, to);
+            words(g.in[a], p, from, to);
             const unsigned head = min(cols, (unsigned)((from - reinterpret_cast<uintptr_t>(p)) / sizeof(T)));
             const unsigned tail = max(head, (unsigned)((to - reinterpret_cast<uintptr_t>(p)) / sizeof(T)));
             const unsigned i = j < kEnd ? j : tail + j - kEnd;
-            f(q, a, p, j, (j < kEnd ? i < head : i < cols) ? i : 0xffffffffu);
+            if (j < kEnd ? i < head : i < cols) f(q, a, p, i);
         }
     }
-    __device__ __forceinline__ void put_edges(unsigned row, unsigned stage, int k = 0) {
-        if (VEC) return;
-        ends(row, [&](int q, unsigned a, const T *, unsigned j, unsigned i) {
-            T *const p = const_cast<T *>(at(a, row, stage));
-            if (i != 0xffffffffu) p[i] = edge[k][q];
-            // a row that began further on may have ended here before
-            if (j < kEnd && cols + j < (g.array_bytes - 16) / sizeof(T)) p[cols + j] = from_f32<T>(0.f);
-        });
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // a later row's copy may write over what was stored here
-        __syncwarp();
+    __device__ __forceinline__ void arrive(unsigned stage) const {
         if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + 8 * stage) : "memory");
     }
+    __device__ __forceinline__ void put_edges(unsigned row, unsigned stage, int k = 0) {
+        if (VEC || !open[k]) return;
+        ends(row, open[k], [&](int q, unsigned a, const T *, unsigned i) { const_cast<T *>(at(a, row, stage))[i] = edge[k][q]; });
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // a later row's copy may write over what was stored here
+        __syncwarp();
+        arrive(stage);
+    }
     __device__ __forceinline__ void issue(unsigned row, unsigned stage, int k = 0) {
-        if (!VEC)
-            ends(row, [&](int q, unsigned, const T *p, unsigned, unsigned i) {
-                if (i != 0xffffffffu) edge[k][q] = p[i];
-            });
         const unsigned a = threadIdx.x & 31;
+        bool all = true;
         if (a < IN && g.in[a].p) {
             const uint32_t bar = full + 8 * stage;
             const T *p = source(a, row);
             uintptr_t from, to;
-            words(p, from, to);
+            all = words(g.in[a], p, from, to);
             mbar_expect(bar, (unsigned)(to - from));
             if (to != from)
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                                 smem_addr(at(a, row, stage)) + (uint32_t)(from - reinterpret_cast<uintptr_t>(p))),
+                                 smem_addr(at(a, row, stage)) + (uint32_t)((intptr_t)from - (intptr_t)p)),
                              "l"(from), "r"((unsigned)(to - from)), "r"(bar)
                              : "memory");
         }
+        if (!VEC) {
+            open[k] = __ballot_sync(0xffffffffu, !all);
+            if (open[k]) ends(row, open[k], [&](int q, unsigned, const T *p, unsigned i) { edge[k][q] = p[i]; });
+            else arrive(stage);
+        }
+        __syncwarp();
+    }
+    // Zeros behind a row of the stage that has arrived, each warp in its own columns: there lie the rest of the row's last word and what a
+    // row that began further on has left.  Before that row there were zeros again.
+    template <int N> __device__ __forceinline__ void close(unsigned row, unsigned stage) const {
+        if (VEC || whole_warp<N>(cols)) return;
+#pragma unroll
+        for (int q = 0; q < (IN * 8 + 31) / 32; ++q) {
+            const unsigned id = q * 32 + (threadIdx.x & 31), a = id / 8, j = id % 8, col = cols + j;
+            if (a < IN && g.in[a].p && j < kEnd && col / (32 * N) == threadIdx.x / 32) const_cast<T *>(at(a, row, stage))[col] = from_f32<T>(0.f);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
     }
 };
@@ -400,6 +428,7 @@ __global__ void __launch_bounds__(threads_of(kForwardValues), 2) k_resnorm_forwa
     for (unsigned row = first; row < g.rows; row += step) {
         if (sums.ok) sums.ok = mbar_wait(smem_addr(sh.full + stage), parity, g.error);
         __syncwarp();
+        ring.template close<N>(row, stage);
         // v becomes its deviation from the mean, the result is 1 / its deviation as a whole
         const auto normalise = [&](float2 (&v)[N / 2], auto between) {
             float s[1];
@@ -549,6 +578,9 @@ __global__ void __launch_bounds__(threads_of(back_values(LAYER)), back_ctas<T>(L
         for (int k = 0; k < R; ++k)
             if (k < mine && sums.ok) sums.ok = mbar_wait(smem_addr(sh.full + stage + k), parity, g.error);
         __syncwarp();
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (k < mine) ring.template close<N>(row0 + k, stage + k);
         // Minus the means of y and f; then, of their deviations y' and f' and with e = dn w_pre: sums of y'^2, e y', f'^2, e.
         constexpr int K = LAYER ? 4 : 3;
         float m[2 * R] = {}, q[K * R] = {};
@@ -837,7 +869,13 @@ template <typename T> auto backward_kernel(bool layer, bool vec, bool shared) {
                  : (vec ? k_resnorm_backward<T, false, true, false> : k_resnorm_backward<T, false, false, false>);
 }
 
+template <typename T> void set_ends(NormArgs<T> &g) {
+    for (In<T> &m : g.in)
+        if (m.p && g.rows) m.end = m.p + (g.rows - 1) / m.per * m.pitch + g.dim;
+}
+
 template <typename T> int run_forward(scar_resnorm *op, NormArgs<T> g) {
+    set_ends(g);
     bool vec = g.dim * sizeof(T) % 16 == 0 && aligned16(g.y, g.y_pitch) && aligned16(g.n, g.n_pitch) && aligned16(g.w_post) && aligned16(g.b_post) &&
                aligned16(g.w_pre) && aligned16(g.b_pre);
     for (const In<T> &m : g.in) vec = vec && aligned16(m.p, m.pitch);
@@ -849,6 +887,7 @@ template <typename T> int run_forward(scar_resnorm *op, NormArgs<T> g) {
 }
 
 template <typename T> int run_backward(scar_resnorm *op, NormArgs<T> g) {
+    set_ends(g);
     bool vec = g.dim * sizeof(T) % 16 == 0 && aligned16(g.n, g.n_pitch) && aligned16(g.df, g.df_pitch) && aligned16(g.dgate, g.dgate_pitch) &&
                aligned16(g.w_post) && aligned16(g.b_post) && aligned16(g.w_pre);
     for (const In<T> &m : g.in) vec = vec && aligned16(m.p, m.pitch);

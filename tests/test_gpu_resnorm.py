@@ -362,3 +362,34 @@ def test_results_between_other_values(dt, kind, off, more, T, D):
         assert float((part[k].double() - whole.double()).norm()) <= 2 * max(unit(TYPES[dt]), 2.0 ** -20) * float(whole.double().norm()), k
         assert bool((wide[k][:, :off] == 7).all()) and bool((wide[k][:, off + D:] == 7).all()), k
     op.close()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("off,more,group", [(0, 1, 0), (1, 0, 1), (1, 2, 2), (3, 9, 7), (5, 3, 500)])
+@pytest.mark.parametrize("T,D", [(1, 9), (2, 1), (40, 3), (37, 70), (700, 513), (350, 1001), (9, 4099), (7, 8195)])
+def test_what_lies_beside_the_rows_is_not_used(dt, kind, off, more, group, T, D):
+    """Matrices in the middle of wider rows of NaN and infinities, each beginning elsewhere: the bits are those of rows that lie alone."""
+    op = ResidualNorm(T, D, TYPES[dt], kind=kind, eps=EPS)
+    c = Case(T, D, dt, kind, group=group)
+
+    def beside(v, at):
+        if v is None:
+            return None
+        w = torch.full((v.shape[0], at + D + more + 1), float("nan"), device="cuda", dtype=v.dtype)
+        w[:, ::2] = float("inf")
+        w[:, at: at + D] = v
+        return w[:, at: at + D]
+
+    def odd(v, at):  # the same distance from words, with ordinary values beside them
+        return None if v is None else torch.ones(v.shape[0], at + D + more + 1, device="cuda", dtype=v.dtype)[:, at: at + D].copy_(v)
+
+    got = []
+    for place in (odd, beside):
+        kw = dict(c.kw, gate=place(c.gate, off + 2))
+        y, n = op.forward(place(c.x, off), place(c.f, off + 1), **kw)
+        g = op.backward(place(c.dy, off), place(c.dn, off + 1), place(y, off), place(c.f, off + 3), **kw)
+        got.append([y, n] + [g[k] for k in sorted(g) if g[k] is not None])
+    for a, b in zip(*got):
+        assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+    op.close()
