@@ -3,8 +3,8 @@
 //   forward    the product's epilogue adds the bias, applies the activation, the mask (computed, mask.cuh) and the residual, and
 //              leaves the activation's derivative for backward; where the product's sum is split, and in float32, k_linear_join
 //              does the same from the float32 sums
-//   backward   k_linear_dz: dz = m . dy . slope, rounded to the operands' type (float32: three bfloat16 planes), and its sums
-//              over the rows; dx = dz w and dw = dz^T x in one launch (k_tc_gemm)
+//   backward   k_linear_dz: dz = m . dy . slope, rounded to the operands' type (few rows: in two values; float32: three bfloat16
+//              planes), and its sums over the rows; dx = dz w and dw = dz^T x in one launch (k_tc_gemm)
 //
 // The derivative and not z is kept: it lies in [-0.13, 1.13], so float16 holds it to 2^-11 of itself or 2^-25 beside bfloat16 (float32 beside
 // the other types, where that would show), and backward needs no activation.  Computing z again instead would be 8 rather than 6 T K N operations.
@@ -405,7 +405,7 @@ template <typename T> struct DzArgs {
     unsigned rows, n, np, per_cta;
     DropRule drop;
     unsigned short *dz;  // [planes][rows][np], or nullptr: dy is dz
-    unsigned long long plane;
+    unsigned long long plane;  // of three in float32, of two in 16 bits, or 0 there: one
     float *part;         // [CTAs of a strip][np]
     T *dbias;            // or nullptr
     unsigned *left;      // per strip: CTAs that are through
@@ -451,7 +451,18 @@ __global__ void __launch_bounds__(256, kDzCtas) k_linear_dz(const __grid_constan
                 if (!g.dz) continue;
                 unsigned short *o = g.dz + r * (unsigned long long)g.np + col;
                 if constexpr (sizeof(T) == 2) {
-                    *reinterpret_cast<uint4 *>(o) = pack8<T>(z);
+                    Pack8<T> hi;
+                    hi.u[0] = pack8<T>(z);
+                    *reinterpret_cast<uint4 *>(o) = hi.u[0];
+                    if (g.plane) {  // what the rounding left
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 h = Two<T>::get(hi.v + 2 * j);
+                            z[j].x = isinf(h.x) ? 0.f : z[j].x - h.x;
+                            z[j].y = isinf(h.y) ? 0.f : z[j].y - h.y;
+                        }
+                        *reinterpret_cast<uint4 *>(o + g.plane) = pack8<T>(z);
+                    }
                 } else {
                     Eight p[3];
 #pragma unroll
@@ -506,6 +517,11 @@ __global__ void __launch_bounds__(256) k_linear_unplace(const T *a, T *to_a, uns
     }
 }
 
+// 16 bits: rows up to which dz goes to the products as two values, the second one what the first one's rounding left.  That rounding comes on
+// top of the results' own: together they are off by 1.41 times the latter alone where dz has many values, by up to 1.95 times where it has
+// few (1 row of 64).  It takes two launches: 16 x 4096 -> 4096 35 us, 17 rows 28.
+constexpr unsigned kFineRows = 16;
+
 struct LinearRecord {
     unsigned error;   // a wait inside a product gave up; cleared when its report has been read
     unsigned splits;  // parts of the split product that ran last
@@ -520,6 +536,7 @@ struct scar_linear : TcHost {
     unsigned short *x = nullptr;   // copies for operands whose rows the products cannot read in place, float32's planes
     unsigned short *w = nullptr;
     unsigned short *dz = nullptr;
+    unsigned short *twice = nullptr;  // [2][kFineRows][kp]: x's few rows, and again
     float *sums = nullptr;         // [dz_ctas][np]
     unsigned *left = nullptr;
     LinearRecord *rec = nullptr;
@@ -728,19 +745,40 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
     }
     // dy itself where nothing changes it
     const bool direct = PL == 1 && !slope && !drop.on && rows_aligned(dy, dyp, 2);
+    const bool fine = PL == 1 && !direct && rows <= kFineRows && 2ull * rows * op->kp * 4 <= op->part_bytes;
     const uint64_t dz_rows = std::max<uint64_t>(op->cfg.max_rows, 1);
     if (!direct || dbias) {
         const unsigned strips = (N + 255) / 256;
         const unsigned per = (unsigned)round_up((rows + op->dz_ctas - 1) / op->dz_ctas, 8);
-        const DzArgs<T> a{dy, dyp, rows_aligned(dy, dyp, sizeof(T)), slope, rows, N, (unsigned)op->np, per, drop, direct ? nullptr : op->dz, dz_rows * op->np,
+        const DzArgs<T> a{dy, dyp, rows_aligned(dy, dyp, sizeof(T)), slope, rows, N, (unsigned)op->np, per, drop, direct ? nullptr : op->dz, PL == 3 ? dz_rows * op->np : fine ? rows * op->np : 0,
                           op->sums, dbias, op->left};
         launch(op, k_linear_dz<T>, dim3(strips, (rows + per - 1) / per), 256, 0, a);
     }
     if (!dx && !dw) return SCAR_OK;
     Operands o;
-    if ((rc = place(op, x, xp, w, wp, rows, dw != nullptr, dx != nullptr, &o)) != SCAR_OK) return rc;
-    const Operand dz = direct ? Operand{dy, N, rows, rows > 1 ? dyp : op->np, 1, 0} : Operand{op->dz, N, rows, op->np, PL, dz_rows * op->np};
-    TcArgs dxg = product(op, rows, K, N, 0), dwg = product(op, N, K, rows, 1);
+    if ((rc = place(op, x, xp, w, wp, rows, dw && !fine, dx != nullptr, &o)) != SCAR_OK) return rc;
+    const unsigned dz_n = fine ? 2 * rows : rows;
+    const Operand dz = direct ? Operand{dy, N, rows, rows > 1 ? dyp : op->np, 1, 0} : Operand{op->dz, N, dz_n, op->np, PL, dz_rows * op->np};
+    if (fine && dw) {
+        const Copy<T> a{x, xp, rows, rows_aligned(x, xp, 2), op->twice, 0}, b{x, xp, rows, a.vec, op->twice + rows * op->kp, 0};
+        o.x = {op->twice, K, dz_n, op->kp, 1, 0};
+        launch(op, k_linear_place<T>, (unsigned)std::min<uint64_t>((2 * rows * (op->kp / 8) + 255) / 256, 16 * op->pairs), 256, 0, a, b, K, (unsigned)op->kp);
+    }
+    if (fine && dx) {  // one product of both values' rows (they fill no tile of 256), joined with its parts
+        TcArgs g = product(op, dz_n, K, N, 0);
+        if ((rc = make_map(op, &g.a, dz, 128)) != SCAR_OK || (rc = make_map(op, &g.b, o.w, 64)) != SCAR_OK) return rc;
+        choose_splits(op, g, 0.f);
+        launch_tc<PL, false, true, Epi::kPart>(op, g);
+        g.out = dx;
+        g.out_pitch = dxp;
+        g.out_vec = rows_aligned(dx, dxp, sizeof(T));
+        g.m = g.most = rows;
+        g.twice = 1;
+        launch(op, k_join_parts, (unsigned)std::min<uint64_t>(((uint64_t)rows * ((K + 3) / 4) + 127) / 128, 32 * op->pairs), 128, 0, g);
+        if (!dw) return SCAR_OK;
+        dx = nullptr;
+    }
+    TcArgs dxg = product(op, rows, K, N, 0), dwg = product(op, N, K, dz_n, 1);
     // Results whose rows do not lie on 16-byte boundaries would be stored in pieces of lines, at a tenth of the rate: where the parts'
     // room holds them they go there, and from there to their places.  dw alone may go through the room of w's copy, which dx is done
     // with by then.
@@ -843,12 +881,13 @@ int setup(scar_linear *op) {
     op->part_bytes = std::min<uint64_t>(64ull << 20, most * 4 * kMostSplits);
     if (f32) op->part_bytes = std::max(op->part_bytes, T * op->np * 4);  // the layer's sums
     const bool copies = f32 || c.in_features % 8;
+    const uint64_t fine = std::min<uint64_t>(T, kFineRows);
     struct {
         void **p;
         uint64_t bytes;
     } const want[] = {
         {(void **)&op->rec, sizeof(LinearRecord)}, {(void **)&op->part, op->part_bytes}, {(void **)&op->left, 4 * strips},
-        {(void **)&op->sums, c.forward_only ? 0 : 4ull * op->dz_ctas * op->np}, {(void **)&op->dz, c.forward_only ? 0 : op->planes * T * op->np * 2},
+        {(void **)&op->sums, c.forward_only ? 0 : 4ull * op->dz_ctas * op->np}, {(void **)&op->dz, c.forward_only ? 0 : std::max(op->planes * T, f32 ? 0 : 2 * fine) * op->np * 2}, {(void **)&op->twice, c.forward_only || f32 ? 0 : 2 * fine * op->kp * 2},
         {(void **)&op->x, copies ? op->planes * T * op->kp * 2 : 0}, {(void **)&op->w, copies ? op->planes * c.out_features * op->kp * 2 : 0},
     };
     uint64_t total = 0;

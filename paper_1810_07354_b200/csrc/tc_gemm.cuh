@@ -78,6 +78,7 @@ struct TcArgs {
     unsigned a_row0, b_row0; // where the piece starts in the row dimension of the tensor maps
     unsigned splits;         // 1, or more: the product then chooses for the rows it finds (pick_splits) ...
     unsigned *chosen;        // ... and leaves its choice here for the kernel that joins the parts
+    unsigned twice;          // for that kernel: 1 where the product had each row twice, all of them and then all again, whose sum is wanted
     unsigned pairs;          // CTA pairs the GPU holds
     unsigned most_splits;    // that fit the buffer of parts
     int planes;
@@ -247,7 +248,7 @@ __device__ __forceinline__ unsigned rows_of(const TcArgs &g) {
     return rows > g.first ? min(g.most, rows - g.first) : 0u;
 }
 
-__device__ __forceinline__ unsigned parts_of(const TcArgs &g) { return g.splits == 1 ? 1u : *g.chosen; }
+__device__ __forceinline__ unsigned parts_of(const TcArgs &g) { return (g.splits == 1 ? 1u : *g.chosen) << g.twice; }
 
 struct TileWalk {
     unsigned m, mt, nt, total, kb, splits;

@@ -358,3 +358,47 @@ def test_gradients_of_no_rows_of_a_single_output(dt):
     layer.status()
     assert bool((dw == 0).all()) and bool((db == 0).all())
     layer.close()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("act,pad", [("gelu", 0), ("silu", 3), ("identity", 8)])
+@pytest.mark.parametrize("K,N", [(40, 17), (129, 64), (1000, 1001), (264, 20000)])
+@pytest.mark.parametrize("T", [1, 2, 7, 16])
+def test_few_rows_have_no_rounding_but_the_results_own(dt, act, pad, K, N, T):
+    """Gradients against the 64-bit ones rounded to the type.  On top of that rounding (a share of up to 1 unit, 0.4 in the mean square at
+    least) there is the derivative's (2^-11 beside bfloat16, 2^-24 beside float16) and dz's second part (2^-16 and 2^-22): below 2^-3 of it,
+    which adds 2^-7 in the mean square; sums of up to 20000 values 2^-13 of a unit of bfloat16, and of float16 2^-12 of their absolute
+    products' sum over 2^-11 of the result: 2^-1.  Together below 1.15 times."""
+    layer = LinearLayer(40, K, N, TYPES[dt], activation=act)
+    x, w, b, res, dy = make(T, K, N, TYPES[dt], pad=pad)
+    drop = Dropout(0.25, 31).mask(T)
+    m = torch.from_numpy(mask(T, N, 0.25, 31, T)).cuda()
+    want = reference(x, w, b, res, dy, act, m)
+    _, slope = layer.forward_train(x, w, bias=b, residual=res, dropout=drop)
+    wide = [torch.zeros(n, K + pad, device="cuda", dtype=TYPES[dt])[:, pad:] for n in (T, N)]
+    dx, dw, db = layer.backward(dy, x, w, slope, dropout=drop, dx=wide[0], dw=wide[1])
+    for k, got in (("dx", dx), ("dw", dw)):
+        v = want[k][0]
+        once = float((v.to(TYPES[dt]).double() - v).norm())
+        assert float((got.double() - v).norm()) <= 1.15 * once + 2 * smallest(TYPES[dt]) * v.numel() ** 0.5, k
+    only = layer.backward(dy, x, w, slope, dropout=drop, need_dw=False)[0], layer.backward(dy, x, w, slope, dropout=drop, need_dx=False)[1]
+    assert torch.equal(only[0], dx) and torch.equal(only[1], dw)
+    layer.close()
+
+
+def test_values_beyond_float16_of_few_rows_are_infinite():
+    layer = LinearLayer(4, 8, 8, torch.float16, activation="identity")
+    x, w = torch.eye(4, 8, device="cuda").half(), torch.eye(8, device="cuda").half()
+    dy = torch.zeros(4, 8, device="cuda").half()
+    dy[1, 2] = 60000.0
+    for seed in range(8):  # where it is kept it is doubled: 120000
+        drop = Dropout(0.5, seed).mask(0)
+        kept = bool(mask(4, 8, 0.5, seed, 0)[1, 2])
+        dx, dw, db = layer.backward(dy, x, w, None, dropout=drop)
+        assert not bool(dx.isnan().any()) or kept
+        assert (float(db[2]) == float("inf")) == kept
+        if not kept:
+            assert bool((dx == 0).all()) and bool((dw == 0).all())
+        else:
+            assert float(dx[1, 2]) == float("inf") and float(dw[2, 1]) == float("inf")
+    layer.close()
