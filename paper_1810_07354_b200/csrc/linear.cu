@@ -340,8 +340,11 @@ __global__ void __launch_bounds__(256) k_linear_few(const __grid_constant__ FewA
     finish_tiles<T, NT>(g, reinterpret_cast<float *>(few_smem), acc, part, n0);
 }
 
-// float32, up to four rows: eight rows of w, the products on the ordinary cores, two at an instruction (4096 -> 4096 on one row: 11 us).
-template <int TT>
+// float32, up to four rows: eight rows of w, the products on the ordinary cores, two at an instruction.  A lane's four values of k of a row
+// are one load (VEC: one or two rows, with w's on 16-byte boundaries; 4000 -> 4096, one row: 7.8 us) or lie 32 apart, so that neighbouring
+// lanes have neighbours wherever rows begin (9.2; four rows of x leave the first form too few registers: 4096 -> 16384 71 us, this one 48;
+// 578 -> 9491 with rows 581 apart 9, in planes 24).
+template <int TT, bool VEC>
 __global__ void __launch_bounds__(256) k_linear_few32(const __grid_constant__ FewArgs<float> g) {
     constexpr int R = 8, V = R * TT;
     __shared__ __align__(16) float sh[8][TT][R];
@@ -353,14 +356,20 @@ __global__ void __launch_bounds__(256) k_linear_few32(const __grid_constant__ Fe
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[r][t] = both(0.f);
-    for (unsigned k = (warp * 32 + lane) * 4; k < g.k; k += 1024) {  // k is a multiple of 4
+    for (unsigned k = warp * 128 + lane * (VEC ? 4 : 1); k < g.k; k += 1024) {  // VEC: a multiple of 4, as g.k
+        const auto apart = [&](const float *p) {
+            return make_float4(p[0], k + 32 < g.k ? p[32] : 0.f, k + 64 < g.k ? p[64] : 0.f, k + 96 < g.k ? p[96] : 0.f);
+        };
         float4 w[R], x[TT];
 #pragma unroll
-        for (int r = 0; r < R; ++r) w[r] = n0 + r < g.n ? *reinterpret_cast<const float4 *>(g.w + (n0 + r) * g.w_pitch + k) : none;
+        for (int r = 0; r < R; ++r) {
+            const float *p = g.w + (n0 + r) * g.w_pitch + k;
+            w[r] = n0 + r >= g.n ? none : VEC ? *reinterpret_cast<const float4 *>(p) : apart(p);
+        }
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             const float *p = g.x + t * g.x_pitch + k;
-            x[t] = t >= (int)g.rows ? none : g.x_vec ? *reinterpret_cast<const float4 *>(p) : make_float4(p[0], p[1], p[2], p[3]);
+            x[t] = t >= (int)g.rows ? none : !VEC ? apart(p) : g.x_vec ? *reinterpret_cast<const float4 *>(p) : make_float4(p[0], p[1], p[2], p[3]);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -649,9 +658,9 @@ template <typename T> bool allow_few() {
 template <typename T> void run_few(scar_linear *op, FewArgs<T> g) {
     const unsigned tiles = (g.n + 31) / 32, rounds = (g.k + 255) / 256;
     if constexpr (sizeof(T) == 4) {
-        if (g.rows <= 4 && g.w_vec) {
-            const unsigned tt = g.rows == 1 ? 1 : g.rows == 2 ? 2 : 4;
-            auto kernel = tt == 1 ? k_linear_few32<1> : tt == 2 ? k_linear_few32<2> : k_linear_few32<4>;
+        if (g.rows <= 4) {
+            auto kernel = g.rows > 2 ? k_linear_few32<4, false> : g.rows == 2 ? (g.w_vec ? k_linear_few32<2, true> : k_linear_few32<2, false>)
+                                                                : (g.w_vec ? k_linear_few32<1, true> : k_linear_few32<1, false>);
             launch(op, kernel, dim3((g.n + 7) / 8), 256, 0, g);
             return;
         }
