@@ -402,3 +402,36 @@ def test_values_beyond_float16_of_few_rows_are_infinite():
         else:
             assert float(dx[1, 2]) == float("inf") and float(dw[2, 1]) == float("inf")
     layer.close()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("T,K,N", [(3, 129, 70), (16, 256, 1000)])
+def test_few_rows_captured(dt, T, K, N):
+    """Forward and backward in one graph, replayed on other inputs: the bits of the same calls made one by one."""
+    stream = torch.cuda.Stream()
+    layer = LinearLayer(16, K, N, TYPES[dt], activation="silu", stream=stream)
+    x, w, b, res, dy = make(T, K, N, TYPES[dt])
+    offset = torch.zeros(1, dtype=torch.int64, device="cuda")
+    drop = Dropout(0.25, 5, stream=stream).mask(offset)
+
+    def step():
+        y, slope = layer.forward_train(x, w, bias=b, residual=res, dropout=drop)
+        return (y, *layer.backward(dy, x, w, slope, dropout=drop))
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got = step()
+        for i in range(3):
+            offset.fill_(i)
+            dy.mul_(-0.5)
+            x.add_(0.25)
+            graph.replay()
+            want = step()
+            stream.synchronize()
+            assert all(torch.equal(a, c) for a, c in zip(got, want))
+    layer.status()
+    layer.close()
