@@ -708,7 +708,8 @@ int scar_resnorm_backward(scar_resnorm *op, const scar_resnorm_block *block, con
 /* Waits for the stream.  SCAR_ERR_TIMEOUT if a wait inside a kernel of the calls since the last status gave up (their
  * outputs are invalid; the operator stays usable). */
 int scar_resnorm_status(scar_resnorm *op);
-/* Self-test hook: the next call reports a wait that gave up (none does). */
+/* Self-test hook: in the next call that has rows, a warp of the first CTA takes its first wait as one that ran out (the one that
+ * copies rows; armed n times, the n-th or the last).  What waits for it runs into the two seconds. */
 int scar_resnorm_selftest_arm_timeout(scar_resnorm *op);
 uint64_t scar_resnorm_launch_count(const scar_resnorm *op); /* kernels launched so far */
 int scar_resnorm_destroy(scar_resnorm *op);

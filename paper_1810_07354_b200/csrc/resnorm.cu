@@ -70,6 +70,7 @@ template <typename T> struct NormArgs {
     unsigned stages, array_bytes, stage_bytes;  // of the ring
     unsigned slot_off, smem;                    // where sums of rows begin, and bytes in all
     unsigned *error;
+    int give_up;                                // self-test: a warp of the first CTA takes its first wait as one that ran out
     // backward
     unsigned per_gate, per_run;  // rows
     float *part;                 // [4][runs][dim]: dw_pre, dw_post, db_pre, db_post
@@ -189,7 +190,8 @@ template <typename T, bool VEC, int IN, int R> struct Ring {
     static constexpr int kPasses = VEC ? 1 : (2 * kEnd * IN + 31) / 32;     // rounds of a warp over all ends of a row
     const NormArgs<T> &g;
     uint8_t *smem;
-    uint32_t full;  // barriers, one per stage
+    uint32_t full;   // barriers, one per stage
+    unsigned *sent;  // where the warp leaves how many rows it had issued when a wait gave up; they take the stages in turn
     unsigned col0, cols;
     T edge[R][kPasses];  // on their way to the stages of the rows that were issued last
     unsigned open[R];    // their matrices, a bit each
@@ -264,6 +266,17 @@ template <typename T, bool VEC, int IN, int R> struct Ring {
         }
         __syncwarp();
     }
+    // After a wait that gave up: no more rows than these n.
+    __device__ __forceinline__ void stop(unsigned n) const {
+        if ((threadIdx.x & 31) == 0 && !*sent) *sent = n;
+    }
+    // And at the end of all `rows`: the copies that may still be under way, with a limit.
+    __device__ __forceinline__ void drain(unsigned rows) const {
+        const unsigned long long until = now_ns() + kWaitNs;
+        const unsigned n = *sent ? *sent : rows;
+        for (unsigned i = n > g.stages ? n - g.stages : 0u; i < n; ++i)
+            while (!mbar_try(full + 8 * (i % g.stages), i / g.stages & 1u) && now_ns() < until) {}
+    }
     // Zeros behind a row of the stage that has arrived, each warp in its own columns: there lie the rest of the row's last word and what a
     // row that began further on has left.  Before that row there were zeros again.
     template <int N> __device__ __forceinline__ void close(unsigned row, unsigned stage) const {
@@ -307,10 +320,12 @@ __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, unsi
 // Sums over a row, K at a time.  Within a warp the lanes halve what they carry at every exchange, until each has one of the K sums
 // of some lanes (three values: 5 exchanges, not 15).  Warps leave theirs in one half of `slot` (of every CTA of the cluster), and every
 // warp adds them up in the same order.  The halves alternate: one is written again only when all warps have arrived at the reduction
-// between, and a warp arrives there after it has read.  A wait that gave up (`ok`) is not repeated: the loops go on without waiting and
-// end.
+// between, and a warp arrives there after it has read.  A wait that gave up (`ok`, a lane's own) is not repeated: the loops go on
+// without waiting and end.  Over a cluster such a lane sends nothing more and announces nothing more at its CTA's barrier: the sum
+// that it leaves out completes nowhere, so all warps of the cluster give up at it, none later, and no barrier sees an arrival too many.
 struct Shared {
     unsigned long long full[kMostStages], red[2];
+    unsigned sent;
 };
 template <int kWarps> struct Sums {  // kWarps: of a CTA at most
     Shared *sh;
@@ -358,15 +373,15 @@ template <int kWarps> struct Sums {  // kWarps: of a CTA at most
                 // Stores that report themselves at the reader's barrier: an arrival that releases would wait for this warp's results
                 // on their way to memory (4096 x 16384 bfloat16, forward: 390 us).
                 const uint32_t mbar = smem_addr(sh->red + half);
-                if (threadIdx.x == 0) mbar_expect(mbar, P * 4 * warps * cluster);
-                if (sub == 0) {
+                if (threadIdx.x == 0 && ok) mbar_expect(mbar, P * 4 * warps * cluster);
+                if (sub == 0 && ok) {
                     const uint32_t here = smem_addr(at + cluster_rank() * warps + warp);
                     for (unsigned c = 0; c < cluster; ++c)
                         asm volatile("{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
                                      " st.async.shared::cluster.mbarrier::complete_tx::bytes.f32 [a], %3, [b];\n}\n" ::"r"(here), "r"(mbar), "r"(c), "f"(x)
                                      : "memory");
                 }
-                if (ok) ok = wait_cluster(smem_addr(sh->red + half), phase >> half & 1u, error);
+                if (ok) ok = wait_cluster(mbar, phase >> half & 1u, error);
                 __syncwarp();
                 phase ^= 1u << half;
                 x = 0.f;
@@ -390,12 +405,32 @@ template <bool VEC, typename T> __device__ __forceinline__ void start(const Norm
     for (unsigned i = threadIdx.x; i < g.stages * g.stage_bytes / 16; i += blockDim.x) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     if (threadIdx.x == 0) {
+        sh.sent = 0;
         for (unsigned i = 0; i < g.stages; ++i) mbar_init(smem_addr(sh.full + i), g.n_in + (VEC ? 0 : 1));
         for (int i = 0; i < 2; ++i) mbar_init(smem_addr(sh.red + i), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (g.cluster > 1) cluster_sync_all();
     else __syncthreads();
+}
+
+// No wait has run out, except for the self-test.
+template <typename T> __device__ __forceinline__ bool begins_well(const NormArgs<T> &g) {
+    const bool ok = !(g.give_up && blockIdx.x == 0 && (int)(threadIdx.x / 32) == g.give_up - 1);
+    if (!ok) atomicExch(g.error, 1u);
+    return ok;
+}
+
+// The end of a CTA.  Where a wait gave up, copies of its own that are under way come first, and the CTAs of a cluster leave together:
+// one whose waits gave up is through long before those that still store into its shared memory.  What these have stored by then
+// is given a millisecond to arrive; elsewhere the last sum has waited for all of it.
+template <typename T, typename R, typename S> __device__ __forceinline__ void leave(const NormArgs<T> &g, const R &ring, const S &sums, unsigned rows) {
+    if (!sums.ok && threadIdx.x < 32) ring.drain(rows);
+    __syncwarp();
+    // relaxed: nothing is handed over, and a release would wait for this warp's results on their way to memory
+    if (g.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
+    if (!sums.ok)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
 // 1 / sqrt(q / dim + eps)
@@ -409,7 +444,7 @@ __global__ void __launch_bounds__(threads_of(kForwardValues), 2) k_resnorm_forwa
     const unsigned rank = g.cluster > 1 ? cluster_rank() : 0u, first = blockIdx.x / g.cluster, step = gridDim.x / g.cluster;
     const unsigned col0 = rank * g.span, cols = min(g.span, g.dim - col0), warp = threadIdx.x / 32;
     start<VEC>(g, sh, smem);
-    Ring<T, VEC, kForwardIn, 1> ring{g, smem, smem_addr(sh.full), col0, cols};
+    Ring<T, VEC, kForwardIn, 1> ring{g, smem, smem_addr(sh.full), &sh.sent, col0, cols};
     Sums<threads_of(N) / 32> sums{&sh, reinterpret_cast<float *>(smem + g.slot_off), 0u, 0u, g.cluster, g.error, true};
     if (warp == 0)
         for (unsigned i = 0; i < g.stages && first + i * step < g.rows; ++i) {
@@ -425,6 +460,7 @@ __global__ void __launch_bounds__(threads_of(kForwardValues), 2) k_resnorm_forwa
     }
     const float inv_dim = 1.f / (float)g.dim;
     unsigned stage = 0, parity = 0, edges = kNoStage, edge_row = 0;
+    sums.ok = begins_well(g);
     for (unsigned row = first; row < g.rows; row += step) {
         if (sums.ok) sums.ok = mbar_wait(smem_addr(sh.full + stage), parity, g.error);
         __syncwarp();
@@ -472,11 +508,14 @@ __global__ void __launch_bounds__(threads_of(kForwardValues), 2) k_resnorm_forwa
             if (!VEC && edges != kNoStage) ring.put_edges(edge_row, edges);
             edges = kNoStage;
             const unsigned long long next = row + (unsigned long long)g.stages * step;
-            if (next < g.rows && sums.ok) {
-                ring.issue((unsigned)next, stage);
-                edges = stage;
-                edge_row = (unsigned)next;
+            if (next >= g.rows) return;
+            if (!__all_sync(0xffffffffu, sums.ok)) {
+                ring.stop((row - first) / step + g.stages);
+                return;
             }
+            ring.issue((unsigned)next, stage);
+            edges = stage;
+            edge_row = (unsigned)next;
         };
         Row<T, N> out;
 #pragma unroll
@@ -502,8 +541,7 @@ __global__ void __launch_bounds__(threads_of(kForwardValues), 2) k_resnorm_forwa
             parity ^= 1;
         }
     }
-    if (!sums.ok)  // let copies in flight end before their memory is given back
-        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    leave(g, ring, sums, first < g.rows ? (g.rows - first - 1) / step + 1 : 0u);
 }
 
 template <bool VEC, typename T, int N> __device__ __forceinline__ void put_part(float *p, const float2 (&v)[N / 2], unsigned cols) {
@@ -521,7 +559,7 @@ __global__ void __launch_bounds__(threads_of(back_values(LAYER)), back_ctas<T>(L
     const unsigned col0 = rank * g.span, cols = min(g.span, g.dim - col0), warp = threadIdx.x / 32;
     const unsigned r0 = run * g.per_run, r1 = min(g.rows, r0 + g.per_run);
     start<VEC>(g, sh, smem);
-    Ring<T, VEC, kBackwardIn, R> ring{g, smem, smem_addr(sh.full), col0, cols};
+    Ring<T, VEC, kBackwardIn, R> ring{g, smem, smem_addr(sh.full), &sh.sent, col0, cols};
     Sums<threads_of(N) / 32> sums{&sh, reinterpret_cast<float *>(smem + g.slot_off), 0u, 0u, g.cluster, g.error, true};
     if (warp == 0)
         for (unsigned i = 0; i < g.stages && r0 + i < r1; ++i) {
@@ -558,13 +596,18 @@ __global__ void __launch_bounds__(threads_of(back_values(LAYER)), back_ctas<T>(L
     const auto refill = [&](unsigned row0) {
         if (warp != 0 || row0 == r0) return;
         const unsigned before = (stage ? stage : g.stages) - R;
+        if (!__all_sync(0xffffffffu, sums.ok)) {
+            ring.stop(min(row0 - R - r0 + g.stages, r1 - r0));
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < R; ++k)
-            if (row0 - R + k + (unsigned long long)g.stages < r1 && sums.ok) {
+            if (row0 - R + k + (unsigned long long)g.stages < r1) {
                 ring.issue(row0 - R + k + g.stages, before + k, k);
                 edges = k + 1;
             }
     };
+    sums.ok = begins_well(g);
     for (unsigned row0 = r0; row0 < r1; row0 += R) {
         const unsigned mine = min((unsigned)R, r1 - row0);
         if (!VEC && warp == 0 && edges) {  // of the rows that the last refill issued
@@ -756,8 +799,7 @@ __global__ void __launch_bounds__(threads_of(back_values(LAYER)), back_ctas<T>(L
         if (g.db_pre) put_part<VEC, T, N>(g.part + 2 * each + mine, a_bpre, cols);
         if (g.db_post) put_part<VEC, T, N>(g.part + 3 * each + mine, a_bpost, cols);
     }
-    if (!sums.ok)
-        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    leave(g, ring, sums, r1 > r0 ? r1 - r0 : 0u);
 }
 
 // Adds the runs' sums, 32 columns a CTA, 16 walkers over the rows of the list, in an order that depends on the sizes alone.
@@ -813,7 +855,7 @@ struct scar_resnorm {
     float *part = nullptr;     // [6][most_runs][dim]
     unsigned *error = nullptr; // a wait gave up; cleared when its report has been read
     uint64_t launches = 0;
-    bool arm_error = false;
+    unsigned armed = 0;        // self-test: which warp of the next call gives up, from 1 on
 };
 
 namespace {
@@ -840,7 +882,9 @@ template <typename T> void set_ring(const scar_resnorm *op, NormArgs<T> &g, unsi
     g.error = op->error;
 }
 
-template <typename T> int launch_rows(scar_resnorm *op, void (*kernel)(NormArgs<T>), const NormArgs<T> &g, unsigned groups, unsigned threads) {
+template <typename T> int launch_rows(scar_resnorm *op, void (*kernel)(NormArgs<T>), NormArgs<T> g, unsigned groups, unsigned threads) {
+    g.give_up = (int)std::min(op->armed, threads / 32);
+    op->armed = 0;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = groups * g.cluster;
     cfg.blockDim = threads;
@@ -985,13 +1029,9 @@ template <typename T> NormArgs<T> block_args(const scar_resnorm *op, const scar_
 }
 uint64_t gates_of(const scar_resnorm_block *k, uint64_t rows) { return k->rows_per_gate ? (rows + k->rows_per_gate - 1) / k->rows_per_gate : 0; }
 
-int done(scar_resnorm *op, int rc) {
+int done(int rc) {
     if (rc != SCAR_OK) return rc;
     TRAIN_TRY(cudaGetLastError());
-    if (op->arm_error) {  // self-test: the report of a wait that gave up
-        op->arm_error = false;
-        TRAIN_TRY(cudaMemsetAsync(op->error, 1, 1, op->stream));
-    }
     return SCAR_OK;
 }
 
@@ -1066,7 +1106,7 @@ int scar_resnorm_forward(scar_resnorm *op, const scar_resnorm_block *block, cons
         g.n = block->pre ? static_cast<T *>(d_n) : nullptr; g.n_pitch = n_pitch;
         rc = run_forward(op, g);
     });
-    return done(op, rc);
+    return done(rc);
 }
 
 int scar_resnorm_backward(scar_resnorm *op, const scar_resnorm_block *block, const void *d_dy, uint64_t dy_pitch, const void *d_dn, uint64_t dn_pitch,
@@ -1107,7 +1147,7 @@ int scar_resnorm_backward(scar_resnorm *op, const scar_resnorm_block *block, con
         g.db_pre = static_cast<T *>(d_db_pre);
         rc = run_backward(op, g);
     });
-    return done(op, rc);
+    return done(rc);
 }
 
 int scar_resnorm_status(scar_resnorm *op) {
@@ -1123,7 +1163,7 @@ int scar_resnorm_status(scar_resnorm *op) {
 
 int scar_resnorm_selftest_arm_timeout(scar_resnorm *op) {
     if (!op) return SCAR_ERR_INVALID_ARG;
-    op->arm_error = true;
+    op->armed++;
     return SCAR_OK;
 }
 
