@@ -182,7 +182,8 @@ __device__ __forceinline__ void finish_tiles(const FewArgs<T> &g, float *sums, c
 // w's rows are the rows of 16 x 8 x 16 matrix instructions, which tcgen05's 128 would leave empty; x's rows, 8 * NT of them, the
 // columns.  A lane's eight values of k of a row are the operands of two instructions: which k a slot of the
 // instruction stands for does not matter as long as w and x agree.  float32 values are split into three bfloat16 planes in registers (six
-// products of planes, smallest first).  What a lane reads goes through shared memory, asynchronously and some rounds ahead, and back to
+// products of planes, smallest first), and every round's products begin with zeros and are added to sums in registers: an instruction drops
+// the low bits of what it adds to (y of 16384 -> 8192 was off by 1.4e-5 of its norm, of positive values by 4.7e-5; 33 rows by 2.2e-7).  What a lane reads goes through shared memory, asynchronously and some rounds ahead, and back to
 // the same lane: nothing is exchanged there, it takes the place of registers that the loads would wait in (4096 -> 16384 bfloat16: one
 // row 25 us, 16 rows 29; loads straight to registers 24 and 39).  Rows anywhere (VEC false): a lane copies the aligned 16-byte words
 // that its values begin in, reads the next one from its neighbour's copy, and the last of a row's four lanes has one word more; a word
@@ -283,18 +284,19 @@ __global__ void __launch_bounds__(256) k_linear_few(const __grid_constant__ FewA
         if constexpr (PL == 1) {
             p[0] = v.u[0];
         } else {
-            // By cutting, not by rounding: 8 + 8 + 8 bits are exact, nothing overflows, and what the six products leave out stays below
-            // 2^-21 of the whole.
+            // 8 + 8 + 8 bits are exact.  The first is cut, so nothing overflows, the second rounded, so the third has either sign: what the
+            // six products leave out stays below 2^-22 of a product and adds up as chance has it.
             unsigned *const to[3] = {&p[0].x, &p[1].x, &p[2].x};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float2 x = make_float2(v.v[2 * j], v.v[2 * j + 1]);
                 const float2 c0 = make_float2(__uint_as_float(__float_as_uint(x.x) & 0xffff0000u), __uint_as_float(__float_as_uint(x.y) & 0xffff0000u));
                 const float2 r1 = add2(x, make_float2(-c0.x, -c0.y));
-                const float2 c1 = make_float2(__uint_as_float(__float_as_uint(r1.x) & 0xffff0000u), __uint_as_float(__float_as_uint(r1.y) & 0xffff0000u));
-                const float2 r2 = add2(r1, make_float2(-c1.x, -c1.y));
+                __nv_bfloat16 b1[2];
+                Two<__nv_bfloat16>::put(b1, r1);
+                const float2 c1 = Two<__nv_bfloat16>::get(b1), r2 = add2(r1, make_float2(-c1.x, -c1.y));
                 to[0][j] = __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632);
-                to[1][j] = __byte_perm(__float_as_uint(r1.x), __float_as_uint(r1.y), 0x7632);
+                to[1][j] = *reinterpret_cast<const unsigned *>(b1);
                 to[2][j] = __byte_perm(__float_as_uint(r2.x), __float_as_uint(r2.y), 0x7632);
             }
         }
@@ -325,13 +327,20 @@ __global__ void __launch_bounds__(256) k_linear_few(const __grid_constant__ FewA
             fetch(2 * RM + t, k, slot, v);
             planes(v, b);
 #pragma unroll
-            for (int m = 0; m < RM; ++m)
+            for (int m = 0; m < RM; ++m) {
+                float fresh[4] = {};
+                float(&d)[4] = PL == 1 ? acc[m][t] : fresh;
 #pragma unroll
                 for (int q = 0; q < kPairs; ++q) {
                     const uint4 &p = a[2 * m][pw[q]], &o = a[2 * m + 1][pw[q]], &c = b[px[q]];
-                    mma_16x8x16<M>(acc[m][t], p.x, o.x, p.y, o.y, c.x, c.y);
-                    mma_16x8x16<M>(acc[m][t], p.z, o.z, p.w, o.w, c.z, c.w);
+                    mma_16x8x16<M>(d, p.x, o.x, p.y, o.y, c.x, c.y);
+                    mma_16x8x16<M>(d, p.z, o.z, p.w, o.w, c.z, c.w);
                 }
+                if (PL == 3) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][t][i] += fresh[i];
+                }
+            }
         }
         if (++slot == S::kAhead) slot = 0;
     }
