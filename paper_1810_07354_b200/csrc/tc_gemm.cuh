@@ -605,7 +605,7 @@ template <int ACT, typename T> __device__ __forceinline__ void layer8(const Laye
         for (int j = 0; j < 4; ++j) z[j] = add2(z[j], b[j]);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) activate<ACT>(z[j], z[j], slope[j]);
+    for (int j = 0; j < 4; ++j) activate<ACT, T>(z[j], z[j], slope[j]);
     if (l.drop.on) mask_apply(l.drop, mask_bits(l.drop, offset, row, col >> 3), z);
 }
 template <typename T> __device__ __forceinline__ uint4 pack8(const float2 (&v)[4]) {

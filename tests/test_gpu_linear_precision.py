@@ -4,6 +4,8 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
+import math  # noqa: E402
+
 from paper_1810_07354_b200 import LinearLayer  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -25,4 +27,32 @@ def test_long_sums_keep_their_precision_whatever_the_rows(rows, positive, pad, K
     layer = LinearLayer(rows, K, N, torch.float32, activation="identity", forward_only=True)
     y, want = layer.forward(x, w), x.double() @ w.double().T
     assert float((y.double() - want).norm()) <= 2.0 ** -20 * float(want.norm())
+    layer.close()
+
+
+@pytest.mark.parametrize("rows", [1, 4, 20, 4096])
+def test_gelu_and_its_derivative_to_a_few_units(rows):
+    """z comes as the bias of a product of zeros, so nothing but the activation is rounded.  The exponential's instruction is off by 2^-22, the
+    reciprocal's by 2^-23, a polynomial's last steps by 2^-22 and three products by 2^-24 each: below 2^-20 of the value, of the
+    derivative 2^-20 of its two terms' sizes.  From -9 on: below -13 results leave float32's ordinary range."""
+    n = 40960 // rows
+    z = torch.linspace(-9.0, 9.0, 40960, device="cuda").view(n, rows).t().contiguous() if rows > 1 else torch.linspace(-9.0, 9.0, n, device="cuda")[None]
+    # one column of x for each output: z = x w^T + bias with x = 1, w = 0 has the bias for z
+    layer = LinearLayer(rows, 1, n, torch.float32, activation="gelu")
+    for r in sorted({0, rows // 2, rows - 1}):
+        bias = z[r].contiguous()
+        y, slope = layer.forward_train(torch.ones(rows, 1, device="cuda"), torch.zeros(n, 1, device="cuda"), bias=bias)
+        b = bias.double()
+        cdf, part = 0.5 * torch.special.erfc(-b / 2 ** 0.5), b * torch.exp(-b * b / 2) / (2 * math.pi) ** 0.5
+        assert float(((y[r].double() - b * cdf).abs() / (b * cdf).abs().clamp(min=1e-300)).max()) <= 2.0 ** -20
+        assert float(((slope[r, :n].double() - cdf - part).abs() / (cdf + part.abs())).max()) <= 2.0 ** -20
+    layer.close()
+
+
+def test_gelu_of_values_at_the_ends_of_the_range():
+    z = torch.tensor([float("nan"), float("inf"), 3e38, 1e20, 40.0, 0.0, -40.0, -1e20, -3e38], device="cuda")
+    layer = LinearLayer(1, 1, 9, torch.float32, activation="gelu")
+    y, slope = layer.forward_train(torch.ones(1, 1, device="cuda"), torch.zeros(9, 1, device="cuda"), bias=z)
+    assert bool(y[0, 0].isnan()) and bool(slope[0, 0].isnan())
+    assert torch.equal(y[0, 1:], z[1:].clamp(min=0)) and torch.equal(slope[0, 2:9], torch.tensor([1, 1, 1, 0.5, 0, 0, 0], device="cuda"))
     layer.close()
