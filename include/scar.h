@@ -611,8 +611,8 @@ int scar_dropout_apply(const scar_dropout *rule, scar_dtype dtype, const void *d
  * act: z; max(z, 0) (derivative 0 at 0); z Phi(z) with the Gaussian's distribution function Phi; z / (1 + exp(-z)).
  * Forward leaves act'(z) in the caller's d_slope, [T][N rounded up to 8] values of float16 beside bfloat16 operands and
  * of float32 beside the others, for backward; the mask is computed again.  16-bit operands: y is rounded once, dz once for the two
- * products (the matrix instruction takes operands of one type; a float16 dz beyond its range is infinite; of up to 16 rows dz
- * goes there as the sum of two values), dx, dw and dbias once; sums are float32.  In float32 an infinity in x, w or dy may act as a NaN in the products. */
+ * products (the matrix instruction takes operands of one type; a float16 dz beyond its range is infinite; of up to 16 rows or
+ * 2048 values dz goes there as the sum of two values), dx, dw and dbias once; sums are float32.  In float32 an infinity in x, w or dy may act as a NaN in the products. */
 typedef struct scar_linear scar_linear; /* opaque; created by scar_linear_init, freed by scar_linear_destroy */
 
 typedef enum { SCAR_ACT_IDENTITY = 0, SCAR_ACT_RELU = 1, SCAR_ACT_GELU = 2, SCAR_ACT_SILU = 3 } scar_activation;

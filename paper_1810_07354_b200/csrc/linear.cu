@@ -3,7 +3,7 @@
 //   forward    the product's epilogue adds the bias, applies the activation, the mask (computed, mask.cuh) and the residual, and
 //              leaves the activation's derivative for backward; where the product's sum is split, and in float32, k_linear_join
 //              does the same from the float32 sums
-//   backward   k_linear_dz: dz = m . dy . slope, rounded to the operands' type (few rows: in two values; float32: three bfloat16
+//   backward   k_linear_dz: dz = m . dy . slope, rounded to the operands' type (few rows or values: in two; float32: three bfloat16
 //              planes), and its sums over the rows; dx = dz w and dw = dz^T x in one launch (k_tc_gemm)
 //
 // The derivative and not z is kept: it lies in [-0.13, 1.13], so float16 holds it to 2^-11 of itself or 2^-25 beside bfloat16 (float32 beside
@@ -535,10 +535,12 @@ __global__ void __launch_bounds__(256) k_linear_unplace(const T *a, T *to_a, uns
     }
 }
 
-// 16 bits: rows up to which dz goes to the products as two values, the second one what the first one's rounding left.  That rounding comes on
-// top of the results' own: together they are off by 1.41 times the latter alone where dz has many values, by up to 1.95 times where it has
-// few (1 row of 64).  It takes two launches: 16 x 4096 -> 4096 35 us, 17 rows 28.
-constexpr unsigned kFineRows = 16;
+// 16 bits: calls whose dz goes to the products as two values, the second one what the first one's rounding left: of few rows, and of few
+// values of dz.  That rounding comes on top of the results' own: together they are off by 1.41 times the latter alone where dz has
+// many values, by up to 1.9 times where it has few (worst of 12 for 17, 128, 512, 1024, 2048 values: 1.9, 1.6, 1.63, 1.53, 1.45).  It takes more
+// launches: 16 x 4096 -> 4096 35 us, 17 rows 28; 32 x 512 -> 32 20 us, rounded once 13.
+constexpr unsigned kFineRows = 16, kFineValues = 2048;
+bool takes_two(uint64_t rows, uint64_t n) { return rows <= kFineRows || rows * n <= kFineValues; }
 
 struct LinearRecord {
     unsigned error;   // a wait inside a product gave up; cleared when its report has been read
@@ -554,7 +556,7 @@ struct scar_linear : TcHost {
     unsigned short *x = nullptr;   // copies for operands whose rows the products cannot read in place, float32's planes
     unsigned short *w = nullptr;
     unsigned short *dz = nullptr;
-    unsigned short *twice = nullptr;  // [2][kFineRows][kp]: x's few rows, and again
+    unsigned short *twice = nullptr;  // [2][such a call's rows][kp]: x's rows, and again
     float *sums = nullptr;         // [dz_ctas][np]
     unsigned *left = nullptr;
     LinearRecord *rec = nullptr;
@@ -763,7 +765,7 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
     }
     // dy itself where nothing changes it
     const bool direct = PL == 1 && !slope && !drop.on && rows_aligned(dy, dyp, 2);
-    const bool fine = PL == 1 && !direct && rows <= kFineRows && 2ull * rows * op->kp * 4 <= op->part_bytes;
+    const bool fine = PL == 1 && !direct && takes_two(rows, N) && 2ull * rows * op->kp * 4 <= op->part_bytes;
     const uint64_t dz_rows = std::max<uint64_t>(op->cfg.max_rows, 1);
     if (!direct || dbias) {
         const unsigned strips = (N + 255) / 256;
@@ -899,7 +901,8 @@ int setup(scar_linear *op) {
     op->part_bytes = std::min<uint64_t>(64ull << 20, most * 4 * kMostSplits);
     if (f32) op->part_bytes = std::max(op->part_bytes, T * op->np * 4);  // the layer's sums
     const bool copies = f32 || c.in_features % 8;
-    const uint64_t fine = std::min<uint64_t>(T, kFineRows);
+    // rows of a call that takes two values of dz
+    const uint64_t fine = std::min<uint64_t>(std::min(T, op->part_bytes / (8 * op->kp)), std::max<uint64_t>(kFineRows, kFineValues / c.out_features));
     struct {
         void **p;
         uint64_t bytes;
