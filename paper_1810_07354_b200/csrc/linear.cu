@@ -799,10 +799,10 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
         dx = nullptr;
     }
     TcArgs dxg = product(op, rows, K, N, 0), dwg = product(op, N, K, dz_n, 1);
-    // Results whose rows do not lie on 16-byte boundaries would be stored in pieces of lines, at a tenth of the rate: where the parts'
-    // room holds them they go there, and from there to their places.  dw alone may go through the room of w's copy, which dx is done
+    // Results of long sums whose rows do not lie on 16-byte boundaries would be stored in pieces of lines: where the parts' room holds
+    // them they go there, and from there to their places.  dw alone may go through the room of w's copy, which dx is done
     // with by then.
-    // A sum that is worth splitting is joined into any place directly.
+    // A sum that is worth splitting on its own is joined into any place directly, or stored there.
     const auto split = [&](TcArgs &g) {
         choose_splits(op, g, kLaunchS);
         return g.splits > 1;
@@ -836,7 +836,11 @@ int run_backward(scar_linear *op, const T *dy, uint64_t dyp, const T *x, uint64_
         else if (left_dx) launch_tc<PL, false, true, Epi::kOut>(op, dxg);
         else if (left_dw) launch_tc<PL, true, true, Epi::kOut>(op, dwg);
     } else if (dx && dw) {
-        launch_grads<PL>(op, dxg, dwg, through_w);
+        // One launch for both leaves sums unsplit that were to be, and rows anywhere to the product.  16 bits are as well off with that (bfloat16,
+        // 3000 x 300 -> 3000 backward 48 us and split 55, 4096 x 100 -> 4096 61 and 61, 8192 x 100 -> 8192 143 and 157), float32 is not (2000 x 301
+        // -> 2000: 92 and 79).
+        const bool split_odd = (dx_split && !dxg.out_vec) || (dw_split && !dwg.out_vec);
+        launch_grads<PL>(op, dxg, dwg, through_w || (PL == 3 && split_odd));
     } else if (dx) {
         launch_out<PL, false>(op, dxg);
     } else {

@@ -243,8 +243,9 @@ template <int PL> void launch_both(TcHost *op, TcArgs a, TcArgs b) {
 
 // dh and dw of a piece: one launch without splits, so that the second one's tiles fill the last round of the first one's
 // (4096 x 32000 x 2048: 120 tiles of 500 stages leave 28 of 74 pairs idle for half of that time), unless split products
-// with launches of their own are worth it (a dh of few tiles whose sum runs over very many classes).  Not where dw goes through the room of w's copy, which dh still reads.
-template <int PL> void launch_grads(TcHost *op, TcArgs dhg, TcArgs dwg, bool through_w) {
+// with launches of their own are worth it (a dh of few tiles whose sum runs over very many classes).  never_one: dw goes
+// through the room of w's copy, which dh still reads, or rows anywhere are better written by the kernel that joins a split sum.
+template <int PL> void launch_grads(TcHost *op, TcArgs dhg, TcArgs dwg, bool never_one) {
     const float apart = choose_splits(op, dhg, kLaunchS) + choose_splits(op, dwg, kLaunchS) + kLaunchS / unit_s(PL);
     const unsigned pairs = op->pairs;
     const float tile0 = (float)((dhg.k + kBK - 1) / kBK + 4), tile1 = (float)((dwg.k + kBK - 1) / kBK + 4);
@@ -252,7 +253,7 @@ template <int PL> void launch_grads(TcHost *op, TcArgs dhg, TcArgs dwg, bool thr
     // the second one's tiles fill gaps where they are the shorter ones, and come on top where they are not
     const float together = tile1 <= tile0 ? std::max(tile0, ((float)tiles0 * tile0 + (float)tiles1 * tile1) / (float)pairs)
                                           : (float)((tiles0 + pairs - 1) / pairs) * tile0 + (float)((tiles1 + pairs - 1) / pairs) * tile1;
-    if (!through_w && together <= apart) {
+    if (!never_one && together <= apart) {
         launch_both<PL>(op, dhg, dwg);
         return;
     }
