@@ -90,11 +90,15 @@ __global__ void __launch_bounds__(128) k_linear_join(const __grid_constant__ TcA
 // ---- Few rows: reading w is everything, so no tile of 256 rows is filled up with zeros.  A CTA has 32 rows of w (eight in
 // float32), its eight warps take turns at the k they read, every load is 16 bytes a lane, and the warps' sums meet in shared
 // memory, where the layer's epilogue takes them.
+// Rows up to which w is read this way, where it lies on 16-byte boundaries and where it does not.  bfloat16, 4096 -> 16384: 32 rows 33 us,
+// the product kernel 35 with 64.  2395 -> 16196: one row 46 us, 16 rows 55, 32 rows 74, the product kernel with its copies 58.  float32,
+// 4096 -> 8192: 32 rows 107 us, 64 rows 203, the product kernel with its planes 131; 2161 -> 11904, 59 rows: 277 and 120.
+constexpr unsigned kFewRows = 32, kFewOdd = 16;
 template <typename T> struct FewArgs {
     const T *x, *w;
     unsigned long long x_pitch, w_pitch;
     unsigned rows, n, k;
-    unsigned parts;  // CTAs of a cluster that share the sum over k (16-bit types)
+    unsigned parts;  // CTAs of a cluster that share the sum over k (k_linear_few)
     int x_vec, w_vec;  // rows on 16-byte boundaries
     int act;
     T *out;
@@ -189,6 +193,7 @@ __device__ __forceinline__ void finish_tiles(const FewArgs<T> &g, float *sums, c
 // that its values begin in, reads the next one from its neighbour's copy, and the last of a row's four lanes has one word more; a word
 // that begins before the matrix is copied value by value, and of one that ends behind it what lies in it.
 template <typename T, int NT, int AHEAD, bool VEC> struct Few {
+    static_assert(VEC || 8 * NT <= (int)kFewOdd, "more rows than that come here on 16-byte boundaries only");
     static constexpr int kRows = 2 * RM + NT;           // of a lane
     static constexpr int kWords = sizeof(T) / 2;        // of 16 bytes, eight values
     static constexpr int kMore = VEC ? 0 : 1024;        // bytes of the words behind the four lanes', a row
@@ -636,10 +641,6 @@ int finish(scar_linear *op) {
     return SCAR_OK;
 }
 
-// Rows up to which w is read this way, where it lies on 16-byte boundaries and where it does not.  bfloat16, 4096 -> 16384: 32 rows 33 us,
-// the product kernel 35 with 64.  2395 -> 16196: one row 46 us, 16 rows 55, 32 rows 74, the product kernel with its copies 58.  float32,
-// 4096 -> 8192: 32 rows 107 us, 64 rows 203, the product kernel with its planes 131; 2161 -> 11904, 59 rows: 277 and 120.
-constexpr unsigned kFewRows = 32, kFewOdd = 16;
 // f(kernel, NT, AHEAD, whether rows lie on 16-byte boundaries, shared memory) for every instance: two or three CTAs of an SM where that
 // leaves three rounds or more, else one.
 template <typename T, int NT, int AHEAD, bool VEC, typename F> void one_few(F &&f) { f(k_linear_few<T, NT, AHEAD, VEC>, NT, AHEAD, VEC, (unsigned)Few<T, NT, AHEAD, VEC>::kSmem); }
@@ -651,14 +652,12 @@ template <typename T, typename F> void for_few(F &&f) {
         one_few<T, 4, 3, true>(f);
         one_few<T, 1, 4, false>(f);
         one_few<T, 2, 3, false>(f);
-        one_few<T, 4, 2, false>(f);
     } else {
         one_few<T, 1, 2, true>(f);
         one_few<T, 2, 2, true>(f);
         one_few<T, 4, 3, true>(f);
         one_few<T, 1, 2, false>(f);
         one_few<T, 2, 2, false>(f);
-        one_few<T, 4, 3, false>(f);
     }
 }
 template <typename T> bool allow_few() {
