@@ -682,7 +682,9 @@ template <typename T> void run_few(scar_linear *op, FewArgs<T> g) {
     const int nt = g.rows <= 8 ? 1 : g.rows <= 16 ? 2 : 4;
     const bool vec = g.w_vec && g.x_vec;
     // 16 bits, up to 16 rows: 96 KiB a CTA, which are two on an SM, or with more CTAs than that 72 KiB and three (16 rows, 8192 -> 4096: 15.9 us
-    // with the one and 18.7 with the other; 4096 -> 32768 52.5 and 48.3).  Elsewhere there is one.
+    // with the one and 18.7 with the other; 4096 -> 32768 52.5 and 48.3).  Elsewhere there is one: up to 8 rows four rounds (8192 -> 4096
+    // 15.0 us, three 17.5, six 18.0; 4096 -> 32768 47.9, 47.7, 53.5), up to 32 rows three (4096 -> 32768 57.5 us, two 61.9, four 66.2;
+    // 16384 -> 2048 20.9, 18.9, 23.2).
     const int ahead = sizeof(T) == 2 && vec && nt == 2 ? (tiles * g.parts > 4 * op->pairs ? 3 : 4) : 0;
     for_few<T>([&](auto kernel, int t, int a, bool v, unsigned smem) {
         if (t == nt && v == vec && (!ahead || a == ahead)) launch_clusters(op, kernel, dim3(tiles * g.parts), 256, smem, g.parts, g);
