@@ -1255,16 +1255,23 @@ class ResidualNorm(_Rows):
                  b_post=None, w_pre=None, b_pre=None, out=None):
         """The gradients, by name: ``dx``, ``df``, ``dgate``, ``dw_post``, ``db_post``, ``dw_pre``, ``db_pre``, None where the call has no such
         input.  ``dy`` may be None (with ``pre``) where y goes nowhere else; without ``pre``, ``dn`` is None and ``y`` is not read.
-        ``out``: a dictionary of tensors to write some of them to."""
+        ``out``: a dictionary of tensors to write some of them to (None: not wanted)."""
+        if dn is not None and not pre:
+            raise ValueError("dn: a call without pre has no such gradient")
         some = dy if dy is not None else dn
+        if some is None:
+            raise ValueError("dy, dn: one of them is wanted")
         rows = len(some) if some.dim() else 0
         post = bool(post and f is not None)
         block = self._block(rows, post, pre, scale, gate, rows_per_gate, w_post, b_post, w_pre, b_pre)
-        dyp, dnp = self._maybe("dy", dy, rows), self._maybe("dn", dn if pre else None, rows)
+        dyp, dnp = self._maybe("dy", dy, rows), self._maybe("dn", dn, rows)
         yp, fp = self._maybe("y", y if pre else None, rows), self._maybe("f", f, rows)
         has = {"dx": some, "df": f, "dgate": gate, "dw_post": w_post if post else None, "db_post": b_post if post else None,
                "dw_pre": w_pre if pre else None, "db_pre": b_pre if pre else None}
         out = out or {}
+        for k in out:
+            if has.get(k) is None:
+                raise ValueError(f"out: {k} is none of this call's gradients")
         got = {k: None if v is None else out[k] if k in out else self._torch.empty_like(v) for k, v in has.items()}
         matrices = [self._maybe(k, got[k], rows if k != "dgate" or gate is None else gate.shape[0]) for k in ("dx", "df", "dgate")]
         vectors = [self._vector(k, got[k], self.dim) for k in ("dw_post", "db_post", "dw_pre", "db_pre")]
