@@ -85,6 +85,12 @@ class HiddenLayers:
         dh = self.norm.backward(dh, dn, h, w_pre=p["pre0"], out={"dw_pre": g["pre0"]})["dx"]
         self.first.backward(dh, x, p["w_in"], slope, dropout=self._mask(step, 0), dw=g["w_in"], dbias=g["b_in"], need_dx=False)
 
+    def status(self) -> None:
+        """Waits; raises if a wait inside a kernel of the calls since the last status gave up: parameters trained on since then are not to
+        be saved."""
+        for op in (self.first, self.up, self.down, self.norm):
+            op.status()
+
     def launches(self) -> int:
         return sum(api.scar_linear_launch_count(op.op) for op in (self.first, self.up, self.down)) + api.scar_resnorm_launch_count(self.norm.op)
 

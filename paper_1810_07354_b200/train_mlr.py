@@ -115,11 +115,13 @@ def _train_hidden(x, y, classes, batch, iterations, lr, max_norm, r, full_period
         params.sub_(grads, alpha=lr)
         losses.append(loss)
         if it % period == 0:
+            net.status()  # nothing is saved that a kernel did not finish
             h.saved_blocks += int(ck.priority_save_k(k).k)
         if it == fail_at:
             info = ck.recover_partial(lost)
             h.perturbation, h.lost_blocks = float(info.l2), int(info.lost_blocks)
             h.perturbation_bound = lr * max_norm * it
+    net.status()
     h.loss, h.grad_norm = [float(v) for v in losses], [float(v) for v in norms]
     h.launches = (net.launches() + api.scar_xent_launch_count(loss_op.op) + api.scar_gnorm_launch_count(norm_op.op) +
                   api.scar_ckpt_launch_count(ck.ctx))
