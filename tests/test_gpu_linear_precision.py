@@ -86,3 +86,32 @@ def test_gradients_of_few_values_have_no_rounding_but_the_results_own(dt, T, K, 
             assert float((got.double() - want).norm()) <= most * once
     layer.close()
     ones.close()
+
+
+@pytest.mark.parametrize("T,N", [(4, 8), (40, 64)])
+def test_a_float16_value_of_dz_beyond_the_range_is_infinite_in_its_row_and_column_alone(T, N):
+    """dy = 60000 where it is kept and doubled; dz in two values and in one.  An infinity times a weight of 0 is a NaN, times others it keeps
+    its sign; everything else is what it is without that value."""
+    K = 8
+    layer = LinearLayer(T, K, N, torch.float16, activation="identity")
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x, w = torch.randn(T, K, generator=g, device="cuda").half(), torch.randn(N, K, generator=g, device="cuda").half()
+    w[2, 5], x[1, 3] = 0, 0
+    dy = torch.randn(T, N, generator=g, device="cuda").half()
+    ones = torch.ones(N, device="cuda").half()
+    for seed in range(6):
+        drop = Dropout(0.5, seed).mask(0)
+        if float(layer.forward(torch.zeros_like(x), w, bias=ones, dropout=drop)[1, 2]) == 0:
+            continue
+        dy[1, 2] = 0.0
+        dx0, dw0, db0 = (v.clone() for v in layer.backward(dy, x, w, None, dropout=drop))
+        dy[1, 2] = 60000.0
+        dx, dw, db = layer.backward(dy, x, w, None, dropout=drop)
+        for got, base, line, other in ((dx, dx0, 1, w[2]), (dw, dw0, 2, x[1])):
+            want = base.clone()
+            want[line] = other.float().sign() * float("inf")  # NaN where the other factor is 0
+            assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(nan=1.0), want.nan_to_num(nan=1.0))
+        want = db0.clone()
+        want[2] = float("inf")
+        assert torch.equal(db, want)
+    layer.close()
