@@ -1269,8 +1269,8 @@ class ResidualNorm(_Rows):
         has = {"dx": some, "df": f, "dgate": gate, "dw_post": w_post if post else None, "db_post": b_post if post else None,
                "dw_pre": w_pre if pre else None, "db_pre": b_pre if pre else None}
         out = out or {}
-        for k in out:
-            if has.get(k) is None:
+        for k, v in out.items():
+            if k not in has or (v is not None and has[k] is None):
                 raise ValueError(f"out: {k} is none of this call's gradients")
         got = {k: None if v is None else out[k] if k in out else self._torch.empty_like(v) for k, v in has.items()}
         matrices = [self._maybe(k, got[k], rows if k != "dgate" or gate is None else gate.shape[0]) for k in ("dx", "df", "dgate")]

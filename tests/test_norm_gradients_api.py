@@ -20,4 +20,7 @@ def test_a_call_without_gradients_or_with_some_it_does_not_have(calls):  # noqa:
     got = norm.backward(x, x, x, f, w_post=w, w_pre=w, gate=gate, rows_per_gate=2, out={"dw_post": w, "dgate": gate, "dx": x, "df": None})
     assert got["dw_post"] is w and got["dgate"] is gate and got["dx"] is x and got["df"] is None and got["dw_pre"] is not None
     assert norm.backward(x, None, None, f, pre=False)["df"] is not None
-    assert calls == ["scar_resnorm_backward"] * 2
+    # one call's gradients are the next one's tensors, None where there was none
+    first = norm.backward(x, x, x, f, w_pre=w)
+    assert first["dgate"] is None and norm.backward(x, x, x, f, w_pre=w, out=first) == first
+    assert calls == ["scar_resnorm_backward"] * 4
