@@ -1,8 +1,9 @@
 // Dropout of a matrix (scar_dropout_apply of scar.h): y = residual + m . x, the mask computed on the way (mask.cuh).  The same
 // call with the same rule is its own gradient.
 //
-// What bounds it: memory (16384 x 8192 bfloat16 with a residual: 115 us, 7.0 TB/s; without 99, where the generator's multiplications
-// show); rows anywhere cost two aligned loads for one (4099 x 5003 float16: 23 us, 3.6 TB/s).
+// What bounds it: memory (16384 x 8192 bfloat16 with a residual: 117 us back to back, 6.9 TB/s, 134 where inputs and outputs change from
+// call to call; without one 99, where the generator's multiplications show); rows anywhere cost two aligned loads for one (4099 x 5003
+// float16: 27 us, 3.1 TB/s; float32 rows 31, 5.3).
 #include <algorithm>
 
 #include "mask.cuh"
@@ -13,8 +14,8 @@ using namespace scar;
 namespace {
 
 constexpr unsigned kThreads = 256;
-// Blocks of a thread: 16384 x 8192 bfloat16 with a residual takes 135 / 115 / 134 us with one, two, four; rows anywhere (4099 x 5003 float16
-// with one) 33 / 36 / 45.
+// Blocks of a thread: 16384 x 8192 bfloat16 with a residual takes 134 / 117 / 132 us with one, two, four; rows anywhere (4099 x 5003 float16
+// with one) 27 / 27 / 30.
 constexpr int kEach = 2;
 
 template <typename T> struct DropArgs {

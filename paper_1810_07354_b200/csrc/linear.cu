@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(128) k_linear_join(const __grid_constant__ TcA
 // memory, where the layer's epilogue takes them.
 // Rows up to which w is read this way, where it lies on 16-byte boundaries and where it does not.  bfloat16, 4096 -> 16384: 32 rows 33 us,
 // the product kernel 35 with 64.  2395 -> 16196: one row 46 us, 16 rows 55, 32 rows 74, the product kernel with its copies 58.  float32,
-// 4096 -> 8192: 32 rows 107 us, 64 rows 203, the product kernel with its planes 131; 2161 -> 11904, 59 rows: 277 and 120.
+// 4096 -> 8192: 32 rows 104 us, 64 rows 203, the product kernel with its planes 131; 2161 -> 11904, 59 rows: 277 and 120.
 constexpr unsigned kFewRows = 32, kFewOdd = 16;
 template <typename T> struct FewArgs {
     const T *x, *w;
