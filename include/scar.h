@@ -627,7 +627,7 @@ typedef struct {
 } scar_linear_config;
 
 /* Creates the operator with its workspaces on the current device.  Waits for the stream.  On error *out is NULL.
- * Calls of one operator share its workspaces: graphs captured from it may not run at the same time. */
+ * Calls of one operator share its workspaces: they may not overlap (other threads, graphs captured from it and run at the same time). */
 int scar_linear_init(scar_linear **out, const scar_linear_config *cfg, void *cuda_stream);
 
 /* d_bias, d_residual, dropout (HOST, read before the call returns) and d_slope may be NULL.  DEVICE matrices, row-major,
@@ -691,7 +691,7 @@ typedef struct {
 } scar_resnorm_block;
 
 /* Creates the operator with its workspace on the current device.  Waits for the stream.  On error *out is NULL.  Calls
- * of one operator share its workspace: graphs captured from it may not run at the same time. */
+ * of one operator share its workspace: they may not overlap (other threads, graphs captured from it and run at the same time). */
 int scar_resnorm_init(scar_resnorm **out, const scar_resnorm_config *cfg, void *cuda_stream);
 /* block: HOST, read before the call returns.  DEVICE matrices, rows a pitch of elements apart, at any address their type
  * allows.  d_f may be NULL (then no post and no gate, and d_y may be NULL), d_n is needed with pre.  y may be x or f

@@ -186,10 +186,11 @@ __device__ __forceinline__ void finish_tiles(const FewArgs<T> &g, float *sums, c
 // w's rows are the rows of 16 x 8 x 16 matrix instructions, which tcgen05's 128 would leave empty; x's rows, 8 * NT of them, the
 // columns.  A lane's eight values of k of a row are the operands of two instructions: which k a slot of the
 // instruction stands for does not matter as long as w and x agree.  float32 values are split into three bfloat16 planes in registers (six
-// products of planes, smallest first), and every round's products begin with zeros and are added to sums in registers: an instruction drops
-// the low bits of what it adds to (y of 16384 -> 8192 was off by 1.4e-5 of its norm, of positive values by 4.7e-5; 33 rows by 2.2e-7).  What a lane reads goes through shared memory, asynchronously and some rounds ahead, and back to
-// the same lane: nothing is exchanged there, it takes the place of registers that the loads would wait in (4096 -> 16384 bfloat16: one
-// row 25 us, 16 rows 29; loads straight to registers 24 and 39).  Rows anywhere (VEC false): a lane copies the aligned 16-byte words
+// products of planes, smallest first), and every round's products begin with zeros and are added to sums in registers: an instruction
+// drops the low bits of what it adds to (y of 16384 -> 8192 was off by 1.4e-5 of its norm, of positive values by 4.7e-5; so 2.2e-7).
+// What a lane reads goes through shared memory, asynchronously and some rounds ahead, and back to the same lane: nothing is
+// exchanged there, it takes the place of registers that the loads would wait in (4096 -> 16384 bfloat16: one row 25 us, 16 rows 29;
+// loads straight to registers 24 and 39).  Rows anywhere (VEC false): a lane copies the aligned 16-byte words
 // that its values begin in, reads the next one from its neighbour's copy, and the last of a row's four lanes has one word more; a word
 // that begins before the matrix is copied value by value, and of one that ends behind it what lies in it.
 template <typename T, int NT, int AHEAD, bool VEC> struct Few {
